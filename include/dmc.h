@@ -58,6 +58,7 @@ typedef enum { DMC_F32 = 0, DMC_BF16 = 1 } dmc_dtype;
 #define DMC_FAULT_NAN_GATE 0x4u         /* k[0] was NaN (treated as append) */
 #define DMC_FAULT_BAD_SEQLENS 0x8u      /* cu_seqlens not monotone / out of range */
 #define DMC_FAULT_WAIT_TIMEOUT 0x10u    /* an in-kernel wait gave up (kernel returned) */
+#define DMC_FAULT_BAD_TARGET 0x20u      /* dmc_retrofit_loss: a target >= vocab (taken as ignored) */
 
 /* Shape of one cache. Storage is paged (the paper stores its variable-length
  * heads with PagedAttention, 32 slots per page, pages allocated on demand per
@@ -242,6 +243,149 @@ dmc_status dmc_cache_export_heads_padded(dmc_cache_t cache, int32_t layer, int32
  * not NULL). Returns DMC_OK, DMC_ERR_PAGES_EXHAUSTED or DMC_ERR_DEVICE_FAULT. */
 dmc_status dmc_cache_status(dmc_cache_t cache, cudaStream_t stream, uint32_t* bits,
                             int64_t* pages_used);
+
+/* ------------------------------------------------------------------------
+ * Retrofitting: the operators of a training step that teaches a model to
+ * compress its cache (Sec. 3.2), each with its gradient.
+ *
+ * While a model is taught, the decision is relaxed to alpha_t in [0, 1] and every
+ * intermediate state of a slot stays visible to the queries of its time:
+ *   alpha_t = sigmoid((k_t[0] - offset + noise_t) / temperature)   (Gumbel-sigmoid:
+ *             logistic noise, offset 5 and temperature 0.1 in the paper)
+ *   omega_t = sigmoid(q_t[0])      (grouped queries: of the group's mean q[0])
+ *   z_t  = alpha_t z_{t-1} + omega_t
+ *   k~_t = (alpha_t z_{t-1} k~_{t-1} + omega_t k_t) / z_t, v~_t alike, k_t[0] = 0
+ * (Eq. partial-accumulation; the first token of a sequence has alpha = 0), and the
+ * queries of token i see the states j <= i with the additive mask
+ * bias_j = log(1 - alpha_{j+1}) for j < i and 0 for j = i (masking appendix).
+ * The calls share a handle that lays their scratch out in a caller's arena, as
+ * a cache does. Tensors of tokens are packed [total_tokens, heads, head_dim]; the
+ * scalars of a token and head (alpha, bias, noise, log-sums) are fp32
+ * [heads, total_tokens]; cu_seqlens, total_tokens and max_seqlen are as in
+ * dmc_prefill_compress. Sequences may be empty. Sums, softmax statistics and
+ * states are held in fp32; every output is rounded once to its type, and no result
+ * depends on the order in which blocks run. All calls on one handle must be ordered
+ * on the GPU: they share its scratch. Calls allocate nothing and can be captured.
+ * ------------------------------------------------------------------------ */
+
+typedef struct {
+  int32_t num_q_heads;   /* states and attention; the first three 0: not used */
+  int32_t num_kv_heads;  /* num_q_heads % num_kv_heads == 0, at most 32 queries per KV head */
+  int32_t head_dim;      /* 64 or 128 */
+  int32_t dtype;         /* dmc_dtype of every tensor of activations, weights and their gradients */
+  int32_t max_tokens;    /* largest total_tokens (num_tokens) of one call */
+  int32_t max_seqs;      /* largest num_seqs of one call */
+  int32_t hidden;        /* loss: row length; rows are multiples of 16 bytes. hidden and vocab 0: not used */
+  int32_t vocab;         /* loss: rows of the vocabulary's matrix */
+} dmc_retrofit_config;
+
+typedef struct dmc_retrofit* dmc_retrofit_t;
+
+/* Bytes of device memory a handle with this config needs (0 if invalid). */
+size_t dmc_retrofit_required_bytes(const dmc_retrofit_config* cfg);
+
+/* Lays the scratch out inside the caller's device arena (256-byte aligned) and
+ * clears the fault bits on `stream`; ownership as in dmc_cache_create. */
+dmc_status dmc_retrofit_create(const dmc_retrofit_config* cfg, void* arena_dev, size_t arena_bytes,
+                               cudaStream_t stream, dmc_retrofit_t* out);
+
+/* Frees the host-side handle (the arena stays the caller's). NULL is a no-op. */
+dmc_status dmc_retrofit_destroy(dmc_retrofit_t h);
+
+/* Bytes of the buffer that dmc_retrofit_states fills for its backward pass
+ * (0 if the arguments are out of the handle's range). */
+size_t dmc_retrofit_saved_bytes(dmc_retrofit_t h, int32_t num_seqs, int32_t total_tokens);
+
+/* The relaxed compression's states of every token.
+ *   q_dev: as in dmc_prefill_compress (only first components are read, strided);
+ *   k_dev, v_dev: [total_tokens, num_kv_heads, head_dim];
+ *   noise_dev: [num_kv_heads, total_tokens] or NULL (none);
+ *   temperature > 0;
+ *   kt_dev, vt_dev (written): k~ (its first components 0) and v~;
+ *   alpha_dev, bias_dev (written): [num_kv_heads, total_tokens]. alpha is 0 at a
+ *          sequence's first token, bias 0 at its last;
+ *   saved_dev (written): dmc_retrofit_saved_bytes, 16-byte aligned: the sums at
+ *          the starts of chunks of tokens. */
+dmc_status dmc_retrofit_states(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev,
+                               int64_t q_token_stride, int64_t q_head_stride, const void* k_dev,
+                               const void* v_dev, const float* noise_dev, float offset,
+                               float temperature, const int32_t* cu_seqlens_dev,
+                               int32_t total_tokens, int32_t max_seqlen, void* kt_dev, void* vt_dev,
+                               float* alpha_dev, float* bias_dev, void* saved_dev,
+                               cudaStream_t stream);
+
+/* Gradients of dmc_retrofit_states. The inputs up to max_seqlen and saved_dev are
+ * those of the forward call.
+ *   dkt_dev, dvt_dev: gradients of k~ (first components are not read into anything)
+ *          and v~; dbias_dev: [num_kv_heads, total_tokens] in the handle's dtype
+ *          (what dmc_retrofit_attention_backward writes); dalpha_dev: fp32, of a
+ *          loss on the decisions themselves, or NULL (none);
+ *   dk_dev, dv_dev (written): gradients of k (its first component: of the
+ *          decision) and v;
+ *   dq_dev (written): element (t, j) at dq_dev[t * dq_token_stride + j *
+ *          dq_head_stride] is the gradient of q's first component; nothing else is
+ *          written, so the full dq of dmc_retrofit_attention_backward, whose first
+ *          components are 0, can be completed in place. */
+dmc_status dmc_retrofit_states_backward(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev,
+                                        int64_t q_token_stride, int64_t q_head_stride,
+                                        const void* k_dev, const void* v_dev, const float* noise_dev,
+                                        float offset, float temperature,
+                                        const int32_t* cu_seqlens_dev, int32_t total_tokens,
+                                        int32_t max_seqlen, const void* saved_dev,
+                                        const void* dkt_dev, const void* dvt_dev,
+                                        const void* dbias_dev, const float* dalpha_dev, void* dq_dev,
+                                        int64_t dq_token_stride, int64_t dq_head_stride,
+                                        void* dk_dev, void* dv_dev, cudaStream_t stream);
+
+/* Attention of whole packed sequences, causal: the score of query i against row
+ * j is q_i k_j / sqrt(head_dim), plus bias_j where j < i (bias_dev NULL: none, plain
+ * causal attention); bias_j = -inf hides row j from all later queries.
+ *   q_dev: [total_tokens, num_q_heads, head_dim]; k_dev, v_dev: [total_tokens,
+ *          num_kv_heads, head_dim]; bias_dev: [num_kv_heads, total_tokens] or NULL;
+ *   out_dev (written): as q_dev; lse_dev (written): [num_q_heads, total_tokens],
+ *          the logarithm of each row's sum of exponentials.
+ * Softmax weights are rounded to bf16 for their product with v in bf16. Sequences
+ * do not affect each other, whatever values they hold. */
+dmc_status dmc_retrofit_attention(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev,
+                                  const void* k_dev, const void* v_dev, const float* bias_dev,
+                                  const int32_t* cu_seqlens_dev, int32_t total_tokens,
+                                  int32_t max_seqlen, void* out_dev, float* lse_dev,
+                                  cudaStream_t stream);
+
+/* Gradients of dmc_retrofit_attention, given its inputs and outputs and dout_dev (as
+ * out_dev). dq_dev, dk_dev, dv_dev (written) are laid out as q, k, v; a KV head's
+ * gradients are summed over its group. dbias_dev (written unless NULL):
+ * [num_kv_heads, total_tokens] in the handle's dtype (it starts from `out`, which
+ * has no more bits). Nothing is accumulated into. */
+dmc_status dmc_retrofit_attention_backward(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev,
+                                           const void* k_dev, const void* v_dev,
+                                           const float* bias_dev, const void* out_dev,
+                                           const float* lse_dev, const void* dout_dev,
+                                           const int32_t* cu_seqlens_dev, int32_t total_tokens,
+                                           int32_t max_seqlen, void* dq_dev, void* dk_dev,
+                                           void* dv_dev, void* dbias_dev, cudaStream_t stream);
+
+/* Softmax cross entropy of num_tokens hidden states against the vocabulary, in
+ * pieces of it; the logits hidden_dev weight_dev^T are never kept.
+ *   hidden_dev: [num_tokens, hidden]; weight_dev: [vocab, hidden];
+ *   targets_dev: int32 [num_tokens]; a target below 0 is an ignored position;
+ *   loss_dev (written): fp32 [num_tokens], the log-sum minus the target's logit, 0
+ *          where ignored; lse_dev (written): fp32 [num_tokens], the log-sum. */
+dmc_status dmc_retrofit_loss(dmc_retrofit_t h, int32_t num_tokens, const void* hidden_dev,
+                             const void* weight_dev, const int32_t* targets_dev, float* loss_dev,
+                             float* lse_dev, cudaStream_t stream);
+
+/* Gradients of dmc_retrofit_loss, given dloss_dev, fp32 [num_tokens] (not read where
+ * the target is ignored): dhidden_dev and dweight_dev (written), laid out as
+ * hidden and weight. */
+dmc_status dmc_retrofit_loss_backward(dmc_retrofit_t h, int32_t num_tokens, const void* hidden_dev,
+                                      const void* weight_dev, const int32_t* targets_dev,
+                                      const float* lse_dev, const float* dloss_dev,
+                                      void* dhidden_dev, void* dweight_dev, cudaStream_t stream);
+
+/* Synchronizes `stream`, then reads the handle's sticky fault bits (into *bits if
+ * not NULL). Returns DMC_OK or DMC_ERR_DEVICE_FAULT. */
+dmc_status dmc_retrofit_status(dmc_retrofit_t h, cudaStream_t stream, uint32_t* bits);
 
 /* Static description of a status code. */
 const char* dmc_status_string(dmc_status status);

@@ -16,6 +16,9 @@ Modules:
                and its own running state); the window-grouping approximation of
                Sec. 3.3 (window = w) in the update, the closed form and the
                masked formulation.
+  retrofit_ref -- torch fp64 definitions of the retrofitting operators (relaxed states,
+               attention under the additive training mask, cross entropy), with
+               bounds on the rounding errors of a correct fp32 or bf16 computation.
   cref      -- ctypes loader for dmc_ref.c, the same Algorithm 1 plus attention in
                plain C (fp64), used for timed CPU baselines and for parity at sizes
                where numpy's per-token loop is too slow.

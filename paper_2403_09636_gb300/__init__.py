@@ -8,7 +8,8 @@ runs in the library's CUDA kernels; there is no fallback of any kind, and a
 missing library raises.
 
 `DmcCache` is a convenience wrapper that owns a torch uint8 arena tensor and
-turns non-OK statuses into exceptions. The synthetic input generator lives in
+turns non-OK statuses into exceptions. `paper_2403_09636_gb300.retrofit` wraps the
+operators of a training step in the same way. The synthetic input generator lives in
 `paper_2403_09636_gb300.synthetic` and is imported separately.
 """
 from __future__ import annotations
@@ -27,12 +28,17 @@ DMC_FAULT_SLOT_CAPACITY = 0x2
 DMC_FAULT_NAN_GATE = 0x4
 DMC_FAULT_BAD_SEQLENS = 0x8
 DMC_FAULT_WAIT_TIMEOUT = 0x10
+DMC_FAULT_BAD_TARGET = 0x20
 PAGE_SIZE = 32
 
 EXPORTED = ("dmc_cache_required_bytes", "dmc_cache_create", "dmc_cache_destroy",
             "dmc_cache_reset", "dmc_prefill_compress", "dmc_prefill_attention", "dmc_decode_step",
             "dmc_decode_step_layers", "dmc_decode_step_static_scratch", "dmc_cache_lengths",
-            "dmc_cache_export_heads", "dmc_cache_export_heads_padded", "dmc_cache_status", "dmc_status_string")
+            "dmc_cache_export_heads", "dmc_cache_export_heads_padded", "dmc_cache_status", "dmc_status_string",
+            "dmc_retrofit_required_bytes", "dmc_retrofit_create", "dmc_retrofit_destroy",
+            "dmc_retrofit_saved_bytes", "dmc_retrofit_states", "dmc_retrofit_states_backward",
+            "dmc_retrofit_attention", "dmc_retrofit_attention_backward", "dmc_retrofit_loss",
+            "dmc_retrofit_loss_backward", "dmc_retrofit_status")
 
 
 class dmc_cache_config(C.Structure):
@@ -41,6 +47,12 @@ class dmc_cache_config(C.Structure):
                 ("page_size", C.c_int32), ("max_slots_per_head", C.c_int32),
                 ("num_pages", C.c_int64), ("max_prefill_tokens", C.c_int32),
                 ("window", C.c_int32)]
+
+
+class dmc_retrofit_config(C.Structure):
+    _fields_ = [("num_q_heads", C.c_int32), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("max_tokens", C.c_int32), ("max_seqs", C.c_int32),
+                ("hidden", C.c_int32), ("vocab", C.c_int32)]
 
 
 class DmcError(RuntimeError):
@@ -61,8 +73,9 @@ def lib():
             raise RuntimeError(f"{LIB_PATH} is missing: build it with "
                                "`python -m paper_2403_09636_gb300.build` (nvcc, sm_103a)")
         l = C.CDLL(LIB_PATH)
-        vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+        vp, i32, i64, sz, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float
         cfgp = C.POINTER(dmc_cache_config)
+        rcfgp = C.POINTER(dmc_retrofit_config)
         sig = {
             "dmc_cache_required_bytes": (sz, [cfgp]),
             "dmc_cache_create": (C.c_int, [cfgp, vp, sz, vp, C.POINTER(vp)]),
@@ -79,6 +92,20 @@ def lib():
             "dmc_cache_export_heads_padded": (C.c_int, [vp, i32, i32, vp, i32, vp, vp, vp, vp, vp]),
             "dmc_cache_status": (C.c_int, [vp, vp, C.POINTER(C.c_uint32), C.POINTER(i64)]),
             "dmc_status_string": (C.c_char_p, [C.c_int]),
+            "dmc_retrofit_required_bytes": (sz, [rcfgp]),
+            "dmc_retrofit_create": (C.c_int, [rcfgp, vp, sz, vp, C.POINTER(vp)]),
+            "dmc_retrofit_destroy": (C.c_int, [vp]),
+            "dmc_retrofit_saved_bytes": (sz, [vp, i32, i32]),
+            "dmc_retrofit_states": (C.c_int, [vp, i32, vp, i64, i64, vp, vp, vp, f32, f32, vp, i32, i32, vp, vp,
+                                              vp, vp, vp, vp]),
+            "dmc_retrofit_states_backward": (C.c_int, [vp, i32, vp, i64, i64, vp, vp, vp, f32, f32, vp, i32, i32,
+                                                       vp, vp, vp, vp, vp, vp, i64, i64, vp, vp, vp]),
+            "dmc_retrofit_attention": (C.c_int, [vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp]),
+            "dmc_retrofit_attention_backward": (C.c_int, [vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp,
+                                                          vp, vp, vp]),
+            "dmc_retrofit_loss": (C.c_int, [vp, i32, vp, vp, vp, vp, vp, vp]),
+            "dmc_retrofit_loss_backward": (C.c_int, [vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]),
+            "dmc_retrofit_status": (C.c_int, [vp, vp, C.POINTER(C.c_uint32)]),
         }
         for name, (res, args) in sig.items():
             f = getattr(l, name)
@@ -164,6 +191,74 @@ def dmc_cache_status(handle, stream):
 
 def dmc_status_string(status: int) -> str:
     return lib().dmc_status_string(int(status)).decode()
+
+
+def dmc_retrofit_required_bytes(cfg: dmc_retrofit_config) -> int:
+    return int(lib().dmc_retrofit_required_bytes(C.byref(cfg)))
+
+
+def dmc_retrofit_create(cfg: dmc_retrofit_config, arena_ptr: int, arena_bytes: int, stream: int):
+    """Returns (status, handle)."""
+    h = C.c_void_p()
+    st = lib().dmc_retrofit_create(C.byref(cfg), arena_ptr, arena_bytes, stream, C.byref(h))
+    return st, h.value
+
+
+def dmc_retrofit_destroy(handle) -> int:
+    return lib().dmc_retrofit_destroy(handle)
+
+
+def dmc_retrofit_saved_bytes(handle, num_seqs, total_tokens) -> int:
+    return int(lib().dmc_retrofit_saved_bytes(handle, num_seqs, total_tokens))
+
+
+def dmc_retrofit_states(handle, num_seqs, q_ptr, q_token_stride, q_head_stride, k_ptr, v_ptr, noise_ptr, offset,
+                        temperature, cu_seqlens_ptr, total_tokens, max_seqlen, kt_ptr, vt_ptr, alpha_ptr, bias_ptr,
+                        saved_ptr, stream) -> int:
+    return lib().dmc_retrofit_states(handle, num_seqs, q_ptr, q_token_stride, q_head_stride, k_ptr, v_ptr, noise_ptr,
+                                     offset, temperature, cu_seqlens_ptr, total_tokens, max_seqlen, kt_ptr, vt_ptr,
+                                     alpha_ptr, bias_ptr, saved_ptr, stream)
+
+
+def dmc_retrofit_states_backward(handle, num_seqs, q_ptr, q_token_stride, q_head_stride, k_ptr, v_ptr, noise_ptr,
+                                 offset, temperature, cu_seqlens_ptr, total_tokens, max_seqlen, saved_ptr, dkt_ptr,
+                                 dvt_ptr, dbias_ptr, dalpha_ptr, dq_ptr, dq_token_stride, dq_head_stride, dk_ptr,
+                                 dv_ptr, stream) -> int:
+    return lib().dmc_retrofit_states_backward(handle, num_seqs, q_ptr, q_token_stride, q_head_stride, k_ptr, v_ptr,
+                                              noise_ptr, offset, temperature, cu_seqlens_ptr, total_tokens,
+                                              max_seqlen, saved_ptr, dkt_ptr, dvt_ptr, dbias_ptr, dalpha_ptr, dq_ptr,
+                                              dq_token_stride, dq_head_stride, dk_ptr, dv_ptr, stream)
+
+
+def dmc_retrofit_attention(handle, num_seqs, q_ptr, k_ptr, v_ptr, bias_ptr, cu_seqlens_ptr, total_tokens, max_seqlen,
+                           out_ptr, lse_ptr, stream) -> int:
+    return lib().dmc_retrofit_attention(handle, num_seqs, q_ptr, k_ptr, v_ptr, bias_ptr, cu_seqlens_ptr,
+                                        total_tokens, max_seqlen, out_ptr, lse_ptr, stream)
+
+
+def dmc_retrofit_attention_backward(handle, num_seqs, q_ptr, k_ptr, v_ptr, bias_ptr, out_ptr, lse_ptr, dout_ptr,
+                                    cu_seqlens_ptr, total_tokens, max_seqlen, dq_ptr, dk_ptr, dv_ptr, dbias_ptr,
+                                    stream) -> int:
+    return lib().dmc_retrofit_attention_backward(handle, num_seqs, q_ptr, k_ptr, v_ptr, bias_ptr, out_ptr, lse_ptr,
+                                                 dout_ptr, cu_seqlens_ptr, total_tokens, max_seqlen, dq_ptr, dk_ptr,
+                                                 dv_ptr, dbias_ptr, stream)
+
+
+def dmc_retrofit_loss(handle, num_tokens, hidden_ptr, weight_ptr, targets_ptr, loss_ptr, lse_ptr, stream) -> int:
+    return lib().dmc_retrofit_loss(handle, num_tokens, hidden_ptr, weight_ptr, targets_ptr, loss_ptr, lse_ptr, stream)
+
+
+def dmc_retrofit_loss_backward(handle, num_tokens, hidden_ptr, weight_ptr, targets_ptr, lse_ptr, dloss_ptr,
+                               dhidden_ptr, dweight_ptr, stream) -> int:
+    return lib().dmc_retrofit_loss_backward(handle, num_tokens, hidden_ptr, weight_ptr, targets_ptr, lse_ptr,
+                                            dloss_ptr, dhidden_ptr, dweight_ptr, stream)
+
+
+def dmc_retrofit_status(handle, stream):
+    """Returns (status, fault_bits). Synchronizes the stream."""
+    bits = C.c_uint32()
+    st = lib().dmc_retrofit_status(handle, stream, C.byref(bits))
+    return st, int(bits.value)
 
 
 def _check(st: int, what: str):

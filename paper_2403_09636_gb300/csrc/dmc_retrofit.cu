@@ -1,0 +1,367 @@
+// Host side of the retrofitting calls of include/dmc.h: checks of arguments, the
+// layout of a handle's scratch in the caller's arena, and the join of the loss's
+// shares of the vocabulary.
+#include <math.h>
+#include <string.h>
+
+#include <new>
+
+#include "dmc_retrofit.cuh"
+
+namespace dmc {
+cudaError_t states_forward(const StatesArgs& a, bool bf16, int D, cudaStream_t stream);
+cudaError_t states_backward(const StatesArgs& a, bool bf16, int D, cudaStream_t stream);
+cudaError_t attn_forward_f32(const AttnArgs& a, bool bf16, int D, cudaStream_t stream);
+cudaError_t attn_backward_f32(const AttnArgs& a, bool bf16, int D, cudaStream_t stream);
+cudaError_t loss_forward_f32(const LossArgs& a, bool bf16, int* shares, cudaStream_t stream);
+cudaError_t loss_backward_f32(const LossArgs& a, bool bf16, cudaStream_t stream);
+
+namespace {
+
+constexpr size_t kAlign = 256;
+size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool given16(const void* p) { return p && aligned16(p); }
+bool given4(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+dmc_status cuda_status(cudaError_t e) { return e == cudaSuccess ? DMC_OK : DMC_ERR_CUDA; }
+
+bool has_heads(const dmc_retrofit_config& c) { return c.num_q_heads > 0; }
+bool has_loss(const dmc_retrofit_config& c) { return c.hidden > 0; }
+
+bool valid(const dmc_retrofit_config* c) {
+  if (!c) return false;
+  if (c->dtype != DMC_F32 && c->dtype != DMC_BF16) return false;
+  if (c->max_tokens < 1 || c->max_seqs < 1) return false;
+  if (c->num_q_heads != 0 || c->num_kv_heads != 0 || c->head_dim != 0) {
+    if (c->num_q_heads < 1 || c->num_kv_heads < 1 || c->num_q_heads % c->num_kv_heads != 0) return false;
+    if (c->num_q_heads / c->num_kv_heads > 32 || c->num_q_heads > 65535) return false;
+    if (c->head_dim != 64 && c->head_dim != 128) return false;
+  }
+  if (c->hidden != 0 || c->vocab != 0) {
+    if (c->hidden < 1 || c->vocab < 1 || c->vocab > (1 << 30)) return false;
+    if ((int64_t)c->hidden * (c->dtype == DMC_F32 ? 4 : 2) % 16 != 0) return false;
+  }
+  return has_heads(*c) || has_loss(*c);
+}
+
+// Words of one piece of the loss's backward pass: the gradient of its logits is
+// kept for all tokens, in at most 512 MB, but no fewer than 1024 words.
+int loss_piece(const dmc_retrofit_config* c) {
+  const int64_t per_word = (int64_t)c->max_tokens * 4;
+  int64_t words = (512ll << 20) / per_word / 256 * 256;
+  const int64_t all = ((int64_t)c->vocab + 255) / 256 * 256;
+  if (words < 1024) words = 1024;
+  return (int)(words < all ? words : all);
+}
+
+struct Offsets {
+  size_t error, sums, delta, part_m, part_l, target_logit, dh, grad, total;
+  int piece;
+};
+
+Offsets offsets(const dmc_retrofit_config* c) {
+  Offsets o = {};
+  size_t at = 0;
+  const size_t tokens = c->max_tokens;
+  o.error = at; at = align_up(at + 4);
+  if (has_heads(*c)) {
+    o.sums = at;
+    at = align_up(at + (size_t)pieces(c->max_tokens, c->max_seqs, kStateChunk) * c->num_kv_heads *
+                           (2 * c->head_dim + 4) * 4);
+    o.delta = at; at = align_up(at + tokens * c->num_q_heads * 4);
+  }
+  if (has_loss(*c)) {
+    o.piece = loss_piece(c);
+    o.part_m = at; at = align_up(at + tokens * kLossSplits * 4);
+    o.part_l = at; at = align_up(at + tokens * kLossSplits * 4);
+    o.target_logit = at; at = align_up(at + tokens * 4);
+    o.dh = at; at = align_up(at + (o.piece < c->vocab ? tokens * c->hidden * 4 : 0));
+    o.grad = at; at = align_up(at + tokens * o.piece * 4);
+  }
+  o.total = at;
+  return o;
+}
+
+// The shares' maxima and sums into each token's log-sum and loss. One warp per token,
+// the shares over its lanes, joined in an order that depends on their number alone.
+__global__ void __launch_bounds__(256) loss_join_kernel(const LossArgs a, int shares) {
+  const int t = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (t >= a.N) return;
+  float m = -INFINITY, l = 0.f;
+  for (int s = lane; s < shares; s += 32) m = fmaxf(m, a.part_m[(long long)s * a.N + t]);
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+  const float ref = m == -INFINITY ? 0.f : m;
+  for (int s = lane; s < shares; s += 32)
+    l = fmaf(a.part_l[(long long)s * a.N + t], expf(a.part_m[(long long)s * a.N + t] - ref), l);
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+  if (lane) return;
+  const float lse = m + logf(l);
+  const int target = a.targets[t];
+  if (target >= a.V) atomicOr(a.error, DMC_FAULT_BAD_TARGET);
+  a.lse[t] = lse;
+  a.loss[t] = target >= 0 && target < a.V ? lse - a.target_logit[t] : 0.f;
+}
+
+}  // namespace
+}  // namespace dmc
+
+struct dmc_retrofit {
+  dmc_retrofit_config cfg;
+  int device;
+  dmc::Offsets at;
+  char* base;
+};
+
+namespace {
+
+// What every call on sequences checks. 1: go on, 0: nothing to do, -1: refused.
+int seqs_arg(dmc_retrofit_t h, int32_t num_seqs, const int32_t* cu, int32_t total, int32_t longest) {
+  if (!h || !dmc::has_heads(h->cfg)) return -1;
+  if (num_seqs < 0 || num_seqs > h->cfg.max_seqs || total < 0 || total > h->cfg.max_tokens) return -1;
+  if (longest < 0 || longest > total) return -1;
+  if (num_seqs == 0 || total == 0) return 0;
+  return dmc::given4(cu) ? 1 : -1;
+}
+
+dmc::StatesArgs states_args(dmc_retrofit_t h, int32_t num_seqs, const void* q, int64_t q_tok, int64_t q_head,
+                            const void* k, const void* v, const float* noise, float offset, float temperature,
+                            const int32_t* cu, int32_t total, int32_t longest, void* saved) {
+  dmc::StatesArgs a = {};
+  a.seqs = {cu, num_seqs, total, longest};
+  a.Hq = h->cfg.num_q_heads;
+  a.Hkv = h->cfg.num_kv_heads;
+  a.G = a.Hq / a.Hkv;
+  a.q = q;
+  a.q_tok = q_tok;
+  a.q_head = q_head;
+  a.k = k;
+  a.v = v;
+  a.noise = noise;
+  a.offset = offset;
+  a.temperature = temperature;
+  a.saved = static_cast<float*>(saved);
+  a.error = reinterpret_cast<unsigned int*>(h->base + h->at.error);
+  a.sums = reinterpret_cast<float*>(h->base + h->at.sums);
+  return a;
+}
+
+dmc::AttnArgs attn_args(dmc_retrofit_t h, int32_t num_seqs, const void* q, const void* k, const void* v,
+                        const float* bias, const int32_t* cu, int32_t total, int32_t longest) {
+  dmc::AttnArgs a = {};
+  a.seqs = {cu, num_seqs, total, longest};
+  a.Hq = h->cfg.num_q_heads;
+  a.Hkv = h->cfg.num_kv_heads;
+  a.G = a.Hq / a.Hkv;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.bias = bias;
+  a.delta = reinterpret_cast<float*>(h->base + h->at.delta);
+  a.error = reinterpret_cast<unsigned int*>(h->base + h->at.error);
+  return a;
+}
+
+dmc::LossArgs loss_args(dmc_retrofit_t h, int32_t n, const void* hidden, const void* weight, const int32_t* targets) {
+  dmc::LossArgs a = {};
+  a.N = n;
+  a.H = h->cfg.hidden;
+  a.V = h->cfg.vocab;
+  a.hidden = hidden;
+  a.weight = weight;
+  a.targets = targets;
+  a.piece = h->at.piece;
+  a.grad = h->base + h->at.grad;
+  a.dh = reinterpret_cast<float*>(h->base + h->at.dh);
+  a.part_m = reinterpret_cast<float*>(h->base + h->at.part_m);
+  a.part_l = reinterpret_cast<float*>(h->base + h->at.part_l);
+  a.target_logit = reinterpret_cast<float*>(h->base + h->at.target_logit);
+  a.error = reinterpret_cast<unsigned int*>(h->base + h->at.error);
+  return a;
+}
+
+bool bf16(dmc_retrofit_t h) { return h->cfg.dtype == DMC_BF16; }
+
+}  // namespace
+
+extern "C" {
+
+size_t dmc_retrofit_required_bytes(const dmc_retrofit_config* cfg) {
+  return dmc::valid(cfg) ? dmc::offsets(cfg).total : 0;
+}
+
+dmc_status dmc_retrofit_create(const dmc_retrofit_config* cfg, void* arena_dev, size_t arena_bytes, cudaStream_t stream,
+                               dmc_retrofit_t* out) {
+  if (!out) return DMC_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (!dmc::valid(cfg) || !arena_dev) return DMC_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(arena_dev) & (dmc::kAlign - 1)) != 0) return DMC_ERR_INVALID_ARG;
+  const dmc::Offsets o = dmc::offsets(cfg);
+  if (arena_bytes < o.total) return DMC_ERR_ARENA_TOO_SMALL;
+  dmc_retrofit* h = new (std::nothrow) dmc_retrofit();
+  if (!h) return DMC_ERR_INVALID_ARG;
+  h->cfg = *cfg;
+  h->at = o;
+  h->base = static_cast<char*>(arena_dev);
+  cudaError_t e = cudaGetDevice(&h->device);
+  if (e == cudaSuccess) e = cudaMemsetAsync(h->base + o.error, 0, 4, stream);
+  if (e != cudaSuccess) {
+    delete h;
+    return DMC_ERR_CUDA;
+  }
+  *out = h;
+  return DMC_OK;
+}
+
+dmc_status dmc_retrofit_destroy(dmc_retrofit_t h) {
+  delete h;
+  return DMC_OK;
+}
+
+size_t dmc_retrofit_saved_bytes(dmc_retrofit_t h, int32_t num_seqs, int32_t total_tokens) {
+  if (!h || !dmc::has_heads(h->cfg) || num_seqs < 0 || num_seqs > h->cfg.max_seqs || total_tokens < 0 ||
+      total_tokens > h->cfg.max_tokens)
+    return 0;
+  return (size_t)dmc::pieces(total_tokens, num_seqs, dmc::kStateChunk) * h->cfg.num_kv_heads *
+         (2 * h->cfg.head_dim + 4) * 4;
+}
+
+dmc_status dmc_retrofit_states(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev, int64_t q_token_stride,
+                               int64_t q_head_stride, const void* k_dev, const void* v_dev, const float* noise_dev,
+                               float offset, float temperature, const int32_t* cu_seqlens_dev, int32_t total_tokens,
+                               int32_t max_seqlen, void* kt_dev, void* vt_dev, float* alpha_dev, float* bias_dev,
+                               void* saved_dev, cudaStream_t stream) {
+  const int go = seqs_arg(h, num_seqs, cu_seqlens_dev, total_tokens, max_seqlen);
+  if (go < 0 || !(temperature > 0.f) || !isfinite(temperature) || !isfinite(offset)) return DMC_ERR_INVALID_ARG;
+  if (go == 0) return DMC_OK;
+  if (!q_dev || q_token_stride < 0 || q_head_stride < 0 || !dmc::given16(k_dev) || !dmc::given16(v_dev) ||
+      !dmc::given16(kt_dev) || !dmc::given16(vt_dev) || !dmc::given4(alpha_dev) || !dmc::given4(bias_dev) ||
+      !dmc::given16(saved_dev) || (noise_dev && !dmc::given4(noise_dev)))
+    return DMC_ERR_INVALID_ARG;
+  dmc::StatesArgs a = states_args(h, num_seqs, q_dev, q_token_stride, q_head_stride, k_dev, v_dev, noise_dev, offset,
+                                  temperature, cu_seqlens_dev, total_tokens, max_seqlen, saved_dev);
+  a.kt = kt_dev;
+  a.vt = vt_dev;
+  a.alpha = alpha_dev;
+  a.bias = bias_dev;
+  return dmc::cuda_status(dmc::states_forward(a, bf16(h), h->cfg.head_dim, stream));
+}
+
+dmc_status dmc_retrofit_states_backward(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev, int64_t q_token_stride,
+                                        int64_t q_head_stride, const void* k_dev, const void* v_dev,
+                                        const float* noise_dev, float offset, float temperature,
+                                        const int32_t* cu_seqlens_dev, int32_t total_tokens, int32_t max_seqlen,
+                                        const void* saved_dev, const void* dkt_dev, const void* dvt_dev,
+                                        const void* dbias_dev, const float* dalpha_dev, void* dq_dev,
+                                        int64_t dq_token_stride, int64_t dq_head_stride, void* dk_dev, void* dv_dev,
+                                        cudaStream_t stream) {
+  const int go = seqs_arg(h, num_seqs, cu_seqlens_dev, total_tokens, max_seqlen);
+  if (go < 0 || !(temperature > 0.f) || !isfinite(temperature) || !isfinite(offset)) return DMC_ERR_INVALID_ARG;
+  if (go == 0) return DMC_OK;
+  if (!q_dev || q_token_stride < 0 || q_head_stride < 0 || !dmc::given16(k_dev) || !dmc::given16(v_dev) ||
+      !dmc::given16(saved_dev) || (noise_dev && !dmc::given4(noise_dev)) || !dmc::given16(dkt_dev) ||
+      !dmc::given16(dvt_dev) || !dbias_dev || (dalpha_dev && !dmc::given4(dalpha_dev)) || !dq_dev ||
+      dq_token_stride < 0 || dq_head_stride < 0 || !dmc::given16(dk_dev) || !dmc::given16(dv_dev))
+    return DMC_ERR_INVALID_ARG;
+  dmc::StatesArgs a = states_args(h, num_seqs, q_dev, q_token_stride, q_head_stride, k_dev, v_dev, noise_dev, offset,
+                                  temperature, cu_seqlens_dev, total_tokens, max_seqlen, const_cast<void*>(saved_dev));
+  a.dkt = dkt_dev;
+  a.dvt = dvt_dev;
+  a.dbias = dbias_dev;
+  a.dalpha = dalpha_dev;
+  a.dq = dq_dev;
+  a.dq_tok = dq_token_stride;
+  a.dq_head = dq_head_stride;
+  a.dk = dk_dev;
+  a.dv = dv_dev;
+  return dmc::cuda_status(dmc::states_backward(a, bf16(h), h->cfg.head_dim, stream));
+}
+
+dmc_status dmc_retrofit_attention(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev, const void* k_dev,
+                                  const void* v_dev, const float* bias_dev, const int32_t* cu_seqlens_dev,
+                                  int32_t total_tokens, int32_t max_seqlen, void* out_dev, float* lse_dev,
+                                  cudaStream_t stream) {
+  const int go = seqs_arg(h, num_seqs, cu_seqlens_dev, total_tokens, max_seqlen);
+  if (go < 0) return DMC_ERR_INVALID_ARG;
+  if (go == 0) return DMC_OK;
+  if (!dmc::given16(q_dev) || !dmc::given16(k_dev) || !dmc::given16(v_dev) || !dmc::given16(out_dev) ||
+      !dmc::given4(lse_dev) || (bias_dev && !dmc::given4(bias_dev)))
+    return DMC_ERR_INVALID_ARG;
+  dmc::AttnArgs a = attn_args(h, num_seqs, q_dev, k_dev, v_dev, bias_dev, cu_seqlens_dev, total_tokens, max_seqlen);
+  a.out = out_dev;
+  a.lse = lse_dev;
+  return dmc::cuda_status(dmc::attn_forward_f32(a, bf16(h), h->cfg.head_dim, stream));
+}
+
+dmc_status dmc_retrofit_attention_backward(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev, const void* k_dev,
+                                           const void* v_dev, const float* bias_dev, const void* out_dev,
+                                           const float* lse_dev, const void* dout_dev, const int32_t* cu_seqlens_dev,
+                                           int32_t total_tokens, int32_t max_seqlen, void* dq_dev, void* dk_dev,
+                                           void* dv_dev, void* dbias_dev, cudaStream_t stream) {
+  const int go = seqs_arg(h, num_seqs, cu_seqlens_dev, total_tokens, max_seqlen);
+  if (go < 0) return DMC_ERR_INVALID_ARG;
+  if (go == 0) return DMC_OK;
+  if (!dmc::given16(q_dev) || !dmc::given16(k_dev) || !dmc::given16(v_dev) || !dmc::given16(out_dev) ||
+      !dmc::given4(lse_dev) || (bias_dev && !dmc::given4(bias_dev)) || !dmc::given16(dout_dev) ||
+      !dmc::given16(dq_dev) || !dmc::given16(dk_dev) || !dmc::given16(dv_dev))
+    return DMC_ERR_INVALID_ARG;
+  dmc::AttnArgs a = attn_args(h, num_seqs, q_dev, k_dev, v_dev, bias_dev, cu_seqlens_dev, total_tokens, max_seqlen);
+  a.out = const_cast<void*>(out_dev);
+  a.lse = const_cast<float*>(lse_dev);
+  a.dout = dout_dev;
+  a.dq = dq_dev;
+  a.dk = dk_dev;
+  a.dv = dv_dev;
+  a.dbias = dbias_dev;
+  return dmc::cuda_status(dmc::attn_backward_f32(a, bf16(h), h->cfg.head_dim, stream));
+}
+
+dmc_status dmc_retrofit_loss(dmc_retrofit_t h, int32_t num_tokens, const void* hidden_dev, const void* weight_dev,
+                             const int32_t* targets_dev, float* loss_dev, float* lse_dev, cudaStream_t stream) {
+  if (!h || !dmc::has_loss(h->cfg) || num_tokens < 0 || num_tokens > h->cfg.max_tokens) return DMC_ERR_INVALID_ARG;
+  if (num_tokens == 0) return DMC_OK;
+  if (!dmc::given16(hidden_dev) || !dmc::given16(weight_dev) || !dmc::given4(targets_dev) || !dmc::given4(loss_dev) ||
+      !dmc::given4(lse_dev))
+    return DMC_ERR_INVALID_ARG;
+  dmc::LossArgs a = loss_args(h, num_tokens, hidden_dev, weight_dev, targets_dev);
+  a.loss = loss_dev;
+  a.lse = lse_dev;
+  int shares = 0;
+  const cudaError_t e = dmc::loss_forward_f32(a, bf16(h), &shares, stream);
+  if (e != cudaSuccess) return DMC_ERR_CUDA;
+  dmc::loss_join_kernel<<<dmc::ceil_div(a.N, 8), 256, 0, stream>>>(a, shares);
+  return dmc::cuda_status(cudaGetLastError());
+}
+
+dmc_status dmc_retrofit_loss_backward(dmc_retrofit_t h, int32_t num_tokens, const void* hidden_dev,
+                                      const void* weight_dev, const int32_t* targets_dev, const float* lse_dev,
+                                      const float* dloss_dev, void* dhidden_dev, void* dweight_dev,
+                                      cudaStream_t stream) {
+  if (!h || !dmc::has_loss(h->cfg) || num_tokens < 0 || num_tokens > h->cfg.max_tokens) return DMC_ERR_INVALID_ARG;
+  if (!dmc::given16(dweight_dev)) return DMC_ERR_INVALID_ARG;
+  if (num_tokens == 0)  // no token: no gradient
+    return dmc::cuda_status(cudaMemsetAsync(
+        dweight_dev, 0, (size_t)h->cfg.vocab * h->cfg.hidden * (bf16(h) ? 2 : 4), stream));
+  if (!dmc::given16(hidden_dev) || !dmc::given16(weight_dev) || !dmc::given4(targets_dev) || !dmc::given4(lse_dev) ||
+      !dmc::given4(dloss_dev) || !dmc::given16(dhidden_dev))
+    return DMC_ERR_INVALID_ARG;
+  dmc::LossArgs a = loss_args(h, num_tokens, hidden_dev, weight_dev, targets_dev);
+  a.lse = const_cast<float*>(lse_dev);
+  a.dloss = dloss_dev;
+  a.dhidden = dhidden_dev;
+  a.dweight = dweight_dev;
+  return dmc::cuda_status(dmc::loss_backward_f32(a, bf16(h), stream));
+}
+
+dmc_status dmc_retrofit_status(dmc_retrofit_t h, cudaStream_t stream, uint32_t* bits) {
+  if (!h) return DMC_ERR_INVALID_ARG;
+  uint32_t b = 0;
+  cudaError_t e = cudaStreamSynchronize(stream);
+  if (e == cudaSuccess) e = cudaMemcpy(&b, h->base + h->at.error, 4, cudaMemcpyDeviceToHost);
+  if (e != cudaSuccess) return DMC_ERR_CUDA;
+  if (bits) *bits = b;
+  return b ? DMC_ERR_DEVICE_FAULT : DMC_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,133 @@
+// What the retrofitting kernels share: the view of a call's packed sequences and
+// of the handle's scratch.
+#pragma once
+
+#include "dmc_internal.cuh"
+
+namespace dmc {
+
+constexpr int kStateChunk = 32;   // tokens per block of the states' kernels: one per lane
+
+// A call's sequences. Work is split into pieces of `piece` tokens of one sequence;
+// sequence s has the piece numbers from cu[s] / piece + s on: as many as it needs
+// fit below the next one's, whatever the lengths, so the number of pieces follows
+// from the call's arguments alone and a piece finds its sequence by a search of cu.
+struct Seqs {
+  const int* cu;
+  int num, total, longest;
+};
+inline long long pieces(int total, int num_seqs, int piece) { return (long long)total / piece + num_seqs; }
+
+struct Piece {
+  int t0, t1;  // the sequence's tokens
+  int at;      // the piece's index in it
+  int seq;
+  bool ok;     // there is such a piece
+};
+
+// Whether a sequence's bounds make sense; nothing outside [0, total) is ever touched.
+__device__ __forceinline__ bool seq_ok(const Seqs& q, int t0, int t1) {
+  return t0 >= 0 && t0 <= t1 && t1 <= q.total && t1 - t0 <= q.longest;
+}
+
+// By a whole warp: 32 sequences are looked at in one step.
+__device__ __forceinline__ Piece find_piece(const Seqs& q, int piece, int index) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = q.num;  // the last sequence whose first piece is not after `index` is in [lo, lo + n)
+  while (n > 1) {
+    const int step = (n + 31) / 32;
+    const int s = lo + lane * step;
+    const bool before = s < lo + n && q.cu[s] / piece + s <= index;
+    const unsigned int b = __ballot_sync(0xffffffffu, before);
+    const int k = b ? 31 - __clz(b) : 0;  // lane 0's sequence is not after it
+    n = min(step, n - k * step);
+    lo += k * step;
+  }
+  Piece p;
+  p.seq = lo;
+  p.t0 = q.cu[lo];
+  p.t1 = q.cu[lo + 1];
+  p.at = index - (p.t0 / piece + lo);
+  p.ok = seq_ok(q, p.t0, p.t1) && p.at >= 0 && p.at < (p.t1 - p.t0 + piece - 1) / piece;
+  return p;
+}
+
+// By one block of a call: faulty cu_seqlens set their bit.
+__device__ __forceinline__ void check_seqs(const Seqs& q, unsigned int* error) {
+  bool bad = false;
+  for (int s = threadIdx.x; s < q.num; s += blockDim.x) bad |= !seq_ok(q, q.cu[s], q.cu[s + 1]);
+  if (threadIdx.x == 0) bad |= q.cu[0] != 0 || q.cu[q.num] != q.total;
+  if (bad) atomicOr(error, DMC_FAULT_BAD_SEQLENS);
+}
+
+// A pair of neighbouring elements in fp32.
+template <typename T> struct Pair;
+template <> struct Pair<float> {
+  using Raw = float2;
+  static __device__ __forceinline__ float2 to_f(Raw r) { return r; }
+  static __device__ __forceinline__ Raw from_f(float2 f) { return f; }
+};
+template <> struct Pair<__nv_bfloat16> {
+  using Raw = uint32_t;
+  static __device__ __forceinline__ float2 to_f(Raw r) {
+    float2 f;
+    Chunk<__nv_bfloat16>::unpack2(r, f.x, f.y);
+    return f;
+  }
+  static __device__ __forceinline__ Raw from_f(float2 f) { return Chunk<__nv_bfloat16>::pack2(f.x, f.y); }
+};
+
+struct StatesArgs {
+  Seqs seqs;
+  int Hq, Hkv, G;
+  const void* q;
+  long long q_tok, q_head;
+  const void *k, *v;
+  const float* noise;
+  float offset, temperature;
+  float* saved;         // [piece][Hkv][2 D + 4]: sums of k, of v, z before the piece's first token
+  unsigned int* error;
+  // forward
+  void *kt, *vt;
+  float *alpha, *bias;
+  // backward
+  const void *dkt, *dvt, *dbias;
+  const float* dalpha;
+  void* dq;
+  long long dq_tok, dq_head;
+  void *dk, *dv;
+  float* sums;          // scratch, [piece][Hkv][2 D + 4]
+};
+
+struct AttnArgs {
+  Seqs seqs;
+  int Hq, Hkv, G;
+  const void *q, *k, *v;
+  const float* bias;
+  void* out;
+  float* lse;           // [Hq][total]
+  const void* dout;
+  void *dq, *dk, *dv, *dbias;
+  float* delta;         // scratch, [Hq][total]
+  unsigned int* error;
+};
+
+struct LossArgs {
+  int N, H, V;
+  const void *hidden, *weight;
+  const int* targets;
+  float *loss, *lse;
+  const float* dloss;
+  void *dhidden, *dweight;
+  int piece;            // words of one piece of the backward pass
+  void* grad;           // scratch, [N][piece]: gradient of a piece's logits
+  float* dh;            // scratch, [N][H]: dhidden of the pieces so far
+  float *part_m, *part_l;  // scratch, [splits][N]: maximum and sum of a share of the vocabulary
+  float* target_logit;  // scratch, [N]
+  unsigned int* error;
+};
+
+// Shares of the vocabulary that the loss kernels keep a maximum and sum for
+constexpr int kLossSplits = 160;
+
+}  // namespace dmc

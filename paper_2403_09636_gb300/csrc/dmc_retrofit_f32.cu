@@ -1,0 +1,521 @@
+// Attention of packed sequences and cross entropy on the CUDA cores, with their
+// gradients: every product and sum in fp32.
+//
+// All products are built from tiles of 64 x 64 in shared memory, a block of 16 x 16
+// threads with 4 rows x 4 (or D / 16) columns each; rows are padded by 16 bytes, so
+// that the 16-byte reads of 8 neighbouring rows fall into different banks.
+#include <math.h>
+
+#include "dmc_retrofit.cuh"
+
+namespace dmc {
+
+namespace {
+
+constexpr int kT = 64;          // rows of a tile
+constexpr int kThreads = 256;
+constexpr int kW = kT + 4;      // row of a tile of weights
+
+// rows [r0, r1) of a matrix of D columns into a tile, zero from r1 on
+template <typename T, int D>
+__device__ __forceinline__ void load_rows(float* tile, const T* src, long long stride, int rows) {
+  for (int i = threadIdx.x; i < kT * (D / 2); i += kThreads) {
+    const int r = i / (D / 2), c = i % (D / 2) * 2;
+    float2 f = make_float2(0.f, 0.f);
+    if (r < rows) f = Pair<T>::to_f(*reinterpret_cast<const typename Pair<T>::Raw*>(src + r * stride + c));
+    *reinterpret_cast<float2*>(tile + r * (D + 4) + c) = f;
+  }
+}
+
+// acc[i][j] += X[ty + 16 i] . Y[tx + 16 j]
+template <int D>
+__device__ __forceinline__ void dot_tile(float (&acc)[4][4], const float* X, const float* Y) {
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll 2
+  for (int c = 0; c < D; c += 4) {
+    float4 x[4], y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4*>(X + (ty + 16 * i) * (D + 4) + c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = *reinterpret_cast<const float4*>(Y + (tx + 16 * i) * (D + 4) + c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        acc[i][j] = fmaf(x[i].x, y[j].x, acc[i][j]);
+        acc[i][j] = fmaf(x[i].y, y[j].y, acc[i][j]);
+        acc[i][j] = fmaf(x[i].z, y[j].z, acc[i][j]);
+        acc[i][j] = fmaf(x[i].w, y[j].w, acc[i][j]);
+      }
+  }
+}
+
+// acc[i][4 c ..] += sum over r < 64 of W[ty + 16 i][r] Y[r][4 tx + 64 c ..]
+template <int D>
+__device__ __forceinline__ void sum_tile(float4 (&acc)[4][D / 64], const float* W, const float* Y) {
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll 2
+  for (int r = 0; r < kT; r += 4) {
+    float4 w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4*>(W + (ty + 16 * i) * kW + r);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
+        const float4 y = *reinterpret_cast<const float4*>(Y + (r + k) * (D + 4) + 4 * tx + 64 * c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = k == 0 ? w[i].x : k == 1 ? w[i].y : k == 2 ? w[i].z : w[i].w;
+          acc[i][c].x = fmaf(x, y.x, acc[i][c].x);
+          acc[i][c].y = fmaf(x, y.y, acc[i][c].y);
+          acc[i][c].z = fmaf(x, y.z, acc[i][c].z);
+          acc[i][c].w = fmaf(x, y.w, acc[i][c].w);
+        }
+      }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T* dst, float4 f) {
+  using P = Pair<T>;
+  *reinterpret_cast<typename P::Raw*>(dst) = P::from_f(make_float2(f.x, f.y));
+  *reinterpret_cast<typename P::Raw*>(dst + 2) = P::from_f(make_float2(f.z, f.w));
+}
+
+__device__ __forceinline__ float4 times(float4 a, float s) { return make_float4(a.x * s, a.y * s, a.z * s, a.w * s); }
+
+// over the 16 threads of a row
+__device__ __forceinline__ float row_max(float x) {
+#pragma unroll
+  for (int off = 8; off >= 1; off >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+  return x;
+}
+__device__ __forceinline__ float row_sum(float x) {
+#pragma unroll
+  for (int off = 8; off >= 1; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+  return x;
+}
+
+// ---------------------------------------------------------------- attention
+
+// Whether query i sees row j
+__device__ __forceinline__ bool sees(int i, int j, float bias) { return j == i || (j < i && bias != -INFINITY); }
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) attn_kernel(const AttnArgs a) {
+  extern __shared__ float smem[];
+  float *Q = smem, *K = Q + kT * (D + 4), *V = K + kT * (D + 4), *W = V + kT * (D + 4);
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, h = blockIdx.y, hk = h / a.G;
+  if (blockIdx.x == 0 && h == 0) check_seqs(a.seqs, a.error);
+  Piece p = find_piece(a.seqs, kT, blockIdx.x);
+  if (!p.ok) return;
+  p.at = (p.t1 - p.t0 + kT - 1) / kT - 1 - p.at;  // the longest rows first
+  const int i0 = p.t0 + p.at * kT, rows = min(kT, p.t1 - i0);
+  const float scale = 1.f / sqrtf((float)D);
+  const long long qs = (long long)a.Hq * D, ks = (long long)a.Hkv * D;
+  load_rows<T, D>(Q, static_cast<const T*>(a.q) + (long long)i0 * qs + (long long)h * D, qs, rows);
+  float4 acc[4][D / 64] = {};
+  float m[4], l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m[i] = -INFINITY, l[i] = 0.f;
+  for (int j0 = p.t0; j0 <= i0; j0 += kT) {
+    const int keys = min(kT, p.t1 - j0);
+    __syncthreads();
+    load_rows<T, D>(K, static_cast<const T*>(a.k) + (long long)j0 * ks + (long long)hk * D, ks, keys);
+    load_rows<T, D>(V, static_cast<const T*>(a.v) + (long long)j0 * ks + (long long)hk * D, ks, keys);
+    __syncthreads();
+    float s[4][4] = {};
+    dot_tile<D>(s, Q, K);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int tok = j0 + tx + 16 * j;
+      const float b = a.bias && tok < p.t1 ? a.bias[(long long)hk * a.seqs.total + tok] : 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int q = i0 + ty + 16 * i;
+        s[i][j] = sees(q, tok, b) ? fmaf(s[i][j], scale, tok < q ? b : 0.f) : -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float mt = row_max(fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3])));
+      const float mn = fmaxf(m[i], mt), ref = mn == -INFINITY ? 0.f : mn;
+      const float corr = expf(m[i] - ref);
+      m[i] = mn;
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float w = expf(s[i][j] - ref);
+        sum += w;
+        W[(ty + 16 * i) * kW + tx + 16 * j] = w;
+      }
+      l[i] = fmaf(l[i], corr, row_sum(sum));
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) acc[i][c] = times(acc[i][c], corr);
+    }
+    __syncthreads();
+    sum_tile<D>(acc, W, V);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = ty + 16 * i;
+    if (r >= rows) continue;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+      store4(static_cast<T*>(a.out) + (long long)(i0 + r) * qs + (long long)h * D + 4 * tx + 64 * c,
+             times(acc[i][c], 1.f / l[i]));
+    if (tx == 0) a.lse[(long long)h * a.seqs.total + i0 + r] = m[i] + logf(l[i]);
+  }
+}
+
+// The rows of Q's gradient: dQ_i = scale sum over j of dS_ij k_j, with
+// dS = P (dO V^T - delta), delta_i = dO_i . out_i
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) attn_dq_kernel(const AttnArgs a) {
+  extern __shared__ float smem[];
+  float *Q = smem, *O = Q + kT * (D + 4), *K = O + kT * (D + 4), *V = K + kT * (D + 4), *W = V + kT * (D + 4);
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, h = blockIdx.y, hk = h / a.G;
+  Piece p = find_piece(a.seqs, kT, blockIdx.x);
+  if (!p.ok) return;
+  p.at = (p.t1 - p.t0 + kT - 1) / kT - 1 - p.at;
+  const int i0 = p.t0 + p.at * kT, rows = min(kT, p.t1 - i0);
+  const float scale = 1.f / sqrtf((float)D);
+  const long long qs = (long long)a.Hq * D, ks = (long long)a.Hkv * D;
+  load_rows<T, D>(Q, static_cast<const T*>(a.q) + (long long)i0 * qs + (long long)h * D, qs, rows);
+  load_rows<T, D>(O, static_cast<const T*>(a.dout) + (long long)i0 * qs + (long long)h * D, qs, rows);
+  float lse[4], delta[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const long long at = (long long)h * a.seqs.total + i0 + ty + 16 * i;
+    const bool in = ty + 16 * i < rows;
+    lse[i] = in ? a.lse[at] : 0.f;
+    delta[i] = in ? a.delta[at] : 0.f;
+  }
+  float4 acc[4][D / 64] = {};
+  for (int j0 = p.t0; j0 <= i0; j0 += kT) {
+    const int keys = min(kT, p.t1 - j0);
+    __syncthreads();
+    load_rows<T, D>(K, static_cast<const T*>(a.k) + (long long)j0 * ks + (long long)hk * D, ks, keys);
+    load_rows<T, D>(V, static_cast<const T*>(a.v) + (long long)j0 * ks + (long long)hk * D, ks, keys);
+    __syncthreads();
+    float s[4][4] = {}, dp[4][4] = {};
+    dot_tile<D>(s, Q, K);
+    dot_tile<D>(dp, O, V);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int tok = j0 + tx + 16 * j;
+      const float b = a.bias && tok < p.t1 ? a.bias[(long long)hk * a.seqs.total + tok] : 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int q = i0 + ty + 16 * i;
+        const float w = expf(fmaf(s[i][j], scale, tok < q ? b : 0.f) - lse[i]);
+        W[(ty + 16 * i) * kW + tx + 16 * j] = sees(q, tok, b) ? w * (dp[i][j] - delta[i]) : 0.f;
+      }
+    }
+    __syncthreads();
+    sum_tile<D>(acc, W, K);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (ty + 16 * i < rows)
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c)
+        store4(static_cast<T*>(a.dq) + (long long)(i0 + ty + 16 * i) * qs + (long long)h * D + 4 * tx + 64 * c,
+               times(acc[i][c], scale));
+}
+
+// The rows of K's and V's gradients and of the bias's, summed over the queries of the
+// group: dV_j = sum of P_ij dO_i, dK_j = scale sum of dS_ij q_i, dbias_j = sum over i > j of dS_ij
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) attn_dkv_kernel(const AttnArgs a) {
+  extern __shared__ float smem[];
+  float *K = smem, *V = K + kT * (D + 4), *Q = V + kT * (D + 4), *O = Q + kT * (D + 4), *W = O + kT * (D + 4);
+  float *S = W + kT * kW, *L = S + kT * kW, *E = L + kT;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, hk = blockIdx.y;
+  const Piece p = find_piece(a.seqs, kT, blockIdx.x);
+  if (!p.ok) return;
+  const int j0 = p.t0 + p.at * kT, keys = min(kT, p.t1 - j0);
+  const float scale = 1.f / sqrtf((float)D);
+  const long long qs = (long long)a.Hq * D, ks = (long long)a.Hkv * D;
+  load_rows<T, D>(K, static_cast<const T*>(a.k) + (long long)j0 * ks + (long long)hk * D, ks, keys);
+  load_rows<T, D>(V, static_cast<const T*>(a.v) + (long long)j0 * ks + (long long)hk * D, ks, keys);
+  float bias[4], db[4] = {};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int r = ty + 16 * j;
+    bias[j] = a.bias && r < keys ? a.bias[(long long)hk * a.seqs.total + j0 + r] : 0.f;
+  }
+  float4 dk[4][D / 64] = {}, dv[4][D / 64] = {};
+  for (int g = 0; g < a.G; ++g) {
+    const int h = hk * a.G + g;
+    for (int i0 = j0; i0 < p.t1; i0 += kT) {
+      const int rows = min(kT, p.t1 - i0);
+      __syncthreads();
+      load_rows<T, D>(Q, static_cast<const T*>(a.q) + (long long)i0 * qs + (long long)h * D, qs, rows);
+      load_rows<T, D>(O, static_cast<const T*>(a.dout) + (long long)i0 * qs + (long long)h * D, qs, rows);
+      if (threadIdx.x < kT) {
+        const long long at = (long long)h * a.seqs.total + i0 + threadIdx.x;
+        const bool in = (int)threadIdx.x < rows;
+        L[threadIdx.x] = in ? a.lse[at] : 0.f;
+        E[threadIdx.x] = in ? a.delta[at] : 0.f;
+      }
+      __syncthreads();
+      float s[4][4] = {}, dp[4][4] = {};
+      dot_tile<D>(s, K, Q);
+      dot_tile<D>(dp, V, O);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int tok = j0 + ty + 16 * j, r = tx + 16 * i, q = i0 + r;
+          const bool seen = r < rows && sees(q, tok, bias[j]);
+          const float w = seen ? expf(fmaf(s[j][i], scale, tok < q ? bias[j] : 0.f) - L[r]) : 0.f;
+          const float ds = seen ? w * (dp[j][i] - E[r]) : 0.f;
+          W[(ty + 16 * j) * kW + r] = w;
+          S[(ty + 16 * j) * kW + r] = ds;
+          if (tok < q) db[j] += ds;
+        }
+      __syncthreads();
+      sum_tile<D>(dv, W, O);
+      sum_tile<D>(dk, S, Q);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int r = ty + 16 * j;
+    const float b = row_sum(db[j]);
+    if (r >= keys) continue;
+    const long long at = (long long)(j0 + r) * ks + (long long)hk * D;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+      store4(static_cast<T*>(a.dk) + at + 4 * tx + 64 * c, times(dk[j][c], scale));
+      store4(static_cast<T*>(a.dv) + at + 4 * tx + 64 * c, dv[j][c]);
+    }
+    if (tx == 0 && a.dbias) static_cast<T*>(a.dbias)[(long long)hk * a.seqs.total + j0 + r] = Elt<T>::from_f(b);
+  }
+}
+
+// delta_i = dO_i . out_i, a warp per (token, head)
+template <typename T, int D>
+__global__ void __launch_bounds__(256) attn_delta_kernel(const AttnArgs a) {
+  const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (blockIdx.x == 0) check_seqs(a.seqs, a.error);
+  if (w >= (long long)a.seqs.total * a.Hq) return;
+  float d = 0.f;
+#pragma unroll
+  for (int c = 2 * lane; c < D; c += 64) {
+    using Raw = typename Pair<T>::Raw;
+    const float2 x = Pair<T>::to_f(*reinterpret_cast<const Raw*>(static_cast<const T*>(a.out) + w * D + c));
+    const float2 y = Pair<T>::to_f(*reinterpret_cast<const Raw*>(static_cast<const T*>(a.dout) + w * D + c));
+    d = fmaf(x.x, y.x, fmaf(x.y, y.y, d));
+  }
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
+  if (lane == 0) a.delta[(w % a.Hq) * a.seqs.total + w / a.Hq] = d;
+}
+
+template <typename K>
+cudaError_t allow(K* kernel, size_t bytes) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+template <typename T, int D>
+cudaError_t attn_f(const AttnArgs& a, cudaStream_t stream) {
+  constexpr size_t bytes = (3 * kT * (D + 4) + kT * kW) * 4;
+  cudaError_t e = allow(attn_kernel<T, D>, bytes);
+  if (e != cudaSuccess) return e;
+  attn_kernel<T, D><<<dim3((unsigned)pieces(a.seqs.total, a.seqs.num, kT), a.Hq), kThreads, bytes, stream>>>(a);
+  return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t attn_b(const AttnArgs& a, cudaStream_t stream) {
+  constexpr size_t dq = (4 * kT * (D + 4) + kT * kW) * 4, dkv = (4 * kT * (D + 4) + 2 * kT * kW + 2 * kT) * 4;
+  cudaError_t e = allow(attn_dq_kernel<T, D>, dq);
+  if (e == cudaSuccess) e = allow(attn_dkv_kernel<T, D>, dkv);
+  if (e != cudaSuccess) return e;
+  const unsigned n = (unsigned)pieces(a.seqs.total, a.seqs.num, kT);
+  attn_delta_kernel<T, D><<<(unsigned)(((long long)a.seqs.total * a.Hq + 7) / 8), 256, 0, stream>>>(a);
+  attn_dkv_kernel<T, D><<<dim3(n, a.Hkv), kThreads, dkv, stream>>>(a);
+  attn_dq_kernel<T, D><<<dim3(n, a.Hq), kThreads, dq, stream>>>(a);
+  return cudaGetLastError();
+}
+
+// ---------------------------------------------------------------- cross entropy
+
+constexpr int kK = 64;  // columns of a K step (a tile of kK + 4 per row)
+
+// acc += A[64 rows from r0] . B[64 rows from c0]^T over all H columns
+template <typename T>
+__device__ __forceinline__ void logits_tile(float (&acc)[4][4], float* X, float* Y, const LossArgs& a, int r0, int c0) {
+  for (int k = 0; k < a.H; k += kK) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * kT * (kK / 2); i += kThreads) {
+      const int side = i / (kT * (kK / 2)), r = i % (kT * (kK / 2)) / (kK / 2), c = i % (kK / 2) * 2;
+      const int row = (side ? c0 : r0) + r;
+      float2 f = make_float2(0.f, 0.f);
+      if (row < (side ? a.V : a.N) && k + c < a.H)
+        f = Pair<T>::to_f(*reinterpret_cast<const typename Pair<T>::Raw*>(
+            static_cast<const T*>(side ? a.weight : a.hidden) + (long long)row * a.H + k + c));
+      *reinterpret_cast<float2*>((side ? Y : X) + r * (kK + 4) + c) = f;
+    }
+    __syncthreads();
+    dot_tile<kK>(acc, X, Y);
+  }
+}
+
+// Maximum and sum of exponentials of a share of the vocabulary for 64 tokens
+template <typename T>
+__global__ void __launch_bounds__(kThreads) loss_kernel(const LossArgs a, int tiles) {
+  __shared__ __align__(16) float X[kT * (kK + 4)], Y[kT * (kK + 4)];
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, r0 = blockIdx.x * kT;
+  float m[4], l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m[i] = -INFINITY, l[i] = 0.f;
+  const int c_end = min((long long)a.V, ((long long)blockIdx.y + 1) * tiles * kT);
+  for (int c0 = blockIdx.y * tiles * kT; c0 < c_end; c0 += kT) {
+    float s[4][4] = {};
+    logits_tile<T>(s, X, Y, a, r0, c0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = r0 + ty + 16 * i;
+      const int target = row < a.N ? a.targets[row] : -1;
+      float mt = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int word = c0 + tx + 16 * j;
+        if (word >= a.V) s[i][j] = -INFINITY;
+        if (word == target) a.target_logit[row] = s[i][j];
+        mt = fmaxf(mt, s[i][j]);
+      }
+      const float mn = fmaxf(m[i], row_max(mt)), ref = mn == -INFINITY ? 0.f : mn;
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum += expf(s[i][j] - ref);
+      l[i] = fmaf(l[i], expf(m[i] - ref), row_sum(sum));
+      m[i] = mn;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = r0 + ty + 16 * i;
+    if (tx == 0 && row < a.N) {
+      a.part_m[(long long)blockIdx.y * a.N + row] = m[i];
+      a.part_l[(long long)blockIdx.y * a.N + row] = l[i];
+    }
+  }
+}
+
+// The gradient of a piece's logits: (softmax - [word = target]) dloss
+template <typename T>
+__global__ void __launch_bounds__(kThreads) loss_grad_kernel(const LossArgs a, int v0) {
+  __shared__ __align__(16) float X[kT * (kK + 4)], Y[kT * (kK + 4)];
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, r0 = blockIdx.x * kT, c0 = v0 + blockIdx.y * kT;
+  float s[4][4] = {};
+  logits_tile<T>(s, X, Y, a, r0, c0);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = r0 + ty + 16 * i;
+    if (row >= a.N) continue;
+    const int target = a.targets[row];
+    const bool counts = target >= 0 && target < a.V;
+    const float lse = a.lse[row], d = counts ? a.dloss[row] : 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int word = c0 + tx + 16 * j;
+      const float p = expf(s[i][j] - lse) - (word == target ? 1.f : 0.f);
+      if (word - v0 < a.piece)
+        static_cast<float*>(a.grad)[(long long)row * a.piece + word - v0] = counts && word < a.V ? p * d : 0.f;
+    }
+  }
+}
+
+// C[64 x 64 tile] = sum over r of A(i, r) B[r][c]: dhidden (A = grad, r over the piece's
+// words, added to what the pieces before gave) and dweight (A = grad^T, r over the tokens)
+template <typename T, bool kWords>
+__global__ void __launch_bounds__(kThreads) loss_product_kernel(const LossArgs a, int v0, bool first, bool last) {
+  __shared__ __align__(16) float W[kT * kW], Y[kT * (64 + 4)];
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, i0 = blockIdx.x * kT, c0 = blockIdx.y * 64;
+  const int words = min(a.piece, a.V - v0);
+  const int rows = kWords ? words : a.N, sum = kWords ? a.N : words;  // rows of C, terms of its sums
+  const T* B = static_cast<const T*>(kWords ? a.hidden : a.weight) + (kWords ? 0 : (long long)v0 * a.H);
+  const float* grad = static_cast<const float*>(a.grad);
+  float4 acc[4][1] = {};
+  for (int r0 = 0; r0 < sum; r0 += kT) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < kT * kT; i += kThreads) {
+      const int hi = i / kT, lo = i % kT;  // lo runs over grad's columns
+      const int tok = kWords ? r0 + hi : i0 + hi, word = kWords ? i0 + lo : r0 + lo;
+      const float g = tok < a.N && word < words ? grad[(long long)tok * a.piece + word] : 0.f;
+      W[kWords ? lo * kW + hi : hi * kW + lo] = g;
+    }
+    for (int i = threadIdx.x; i < kT * 32; i += kThreads) {
+      const int r = i / 32, c = i % 32 * 2;
+      float2 f = make_float2(0.f, 0.f);
+      if (r0 + r < sum && c0 + c < a.H)
+        f = Pair<T>::to_f(*reinterpret_cast<const typename Pair<T>::Raw*>(B + (long long)(r0 + r) * a.H + c0 + c));
+      *reinterpret_cast<float2*>(Y + r * 68 + c) = f;
+    }
+    __syncthreads();
+    sum_tile<64>(acc, W, Y);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = i0 + ty + 16 * i, col = c0 + 4 * tx;
+    if (row >= rows || col >= a.H) continue;
+    const long long at = (long long)(kWords ? v0 + row : row) * a.H + col;
+    float4 f = acc[i][0];
+    if (!kWords && !first) {
+      const float4 o = *reinterpret_cast<const float4*>(a.dh + at);
+      f = make_float4(f.x + o.x, f.y + o.y, f.z + o.z, f.w + o.w);
+    }
+    if (kWords)
+      store4(static_cast<T*>(a.dweight) + at, f);
+    else if (last)
+      store4(static_cast<T*>(a.dhidden) + at, f);
+    else
+      *reinterpret_cast<float4*>(a.dh + at) = f;
+  }
+}
+
+template <typename T>
+cudaError_t loss_f(const LossArgs& a, int* shares, cudaStream_t stream) {
+  const int rows = ceil_div(a.N, kT), cols = ceil_div(a.V, kT);
+  const int tiles = ceil_div(cols, min(cols, min(kLossSplits, max(1, 608 / rows))));
+  *shares = ceil_div(cols, tiles);
+  loss_kernel<T><<<dim3(rows, *shares), kThreads, 0, stream>>>(a, tiles);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t loss_b(const LossArgs& a, cudaStream_t stream) {
+  const int rows = ceil_div(a.N, kT), cols = ceil_div(a.H, 64);
+  for (int v0 = 0; v0 < a.V; v0 += a.piece) {
+    const int words = min(a.piece, a.V - v0);
+    loss_grad_kernel<T><<<dim3(rows, ceil_div(words, kT)), kThreads, 0, stream>>>(a, v0);
+    loss_product_kernel<T, false><<<dim3(rows, cols), kThreads, 0, stream>>>(a, v0, v0 == 0, v0 + a.piece >= a.V);
+    loss_product_kernel<T, true><<<dim3(ceil_div(words, kT), cols), kThreads, 0, stream>>>(a, v0, false, false);
+  }
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t attn_forward_f32(const AttnArgs& a, bool bf16, int D, cudaStream_t stream) {
+  if (bf16) return D == 128 ? attn_f<__nv_bfloat16, 128>(a, stream) : attn_f<__nv_bfloat16, 64>(a, stream);
+  return D == 128 ? attn_f<float, 128>(a, stream) : attn_f<float, 64>(a, stream);
+}
+cudaError_t attn_backward_f32(const AttnArgs& a, bool bf16, int D, cudaStream_t stream) {
+  if (bf16) return D == 128 ? attn_b<__nv_bfloat16, 128>(a, stream) : attn_b<__nv_bfloat16, 64>(a, stream);
+  return D == 128 ? attn_b<float, 128>(a, stream) : attn_b<float, 64>(a, stream);
+}
+cudaError_t loss_forward_f32(const LossArgs& a, bool bf16, int* shares, cudaStream_t stream) {
+  return bf16 ? loss_f<__nv_bfloat16>(a, shares, stream) : loss_f<float>(a, shares, stream);
+}
+cudaError_t loss_backward_f32(const LossArgs& a, bool bf16, cudaStream_t stream) {
+  return bf16 ? loss_b<__nv_bfloat16>(a, stream) : loss_b<float>(a, stream);
+}
+
+}  // namespace dmc
