@@ -49,11 +49,10 @@
 // two halves, so that P V starts before the softmax ends. Slower: 64-slot tiles with
 // two S buffers per query tile (an MMA of N = 64 costs 49 cycles, of N = 128 65);
 // P V of both query tiles before S of both; two MMA warps (they ran in step).
-#include <cuda.h>
 #include <math.h>
 #include <stddef.h>
 
-#include "dmc_internal.cuh"
+#include "dmc_tensor.cuh"
 
 namespace dmc {
 
@@ -134,145 +133,17 @@ __device__ __forceinline__ uint32_t pa_swz(int r, int j) {
   return (uint32_t)((j >> 3) * (kPaRows * 128) + r * 128 + (((j & 7) ^ (r & 7)) << 4));
 }
 
-// tcgen05 shared-memory matrix descriptor: 128B swizzle, start address, leading
-// and stride byte offsets (all in 16-byte units), descriptor version 1
-__device__ __forceinline__ uint64_t pa_desc(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
-  return (uint64_t)((saddr >> 4) & 0x3FFF) | ((uint64_t)((lbo >> 4) & 0x3FFF) << 16) |
-         ((uint64_t)((sbo >> 4) & 0x3FFF) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
-
-// instruction descriptor, kind::f16: bf16 A and B, fp32 D, M = N = 128;
-// b_mn selects an MN-major B operand
-__device__ __forceinline__ uint32_t pa_idesc(bool b_mn) {
-  return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((128u >> 3) << 17) |
-         ((128u >> 4) << 24);
-}
-
-__device__ __forceinline__ void pa_mma(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc,
-                                       bool acc) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "l"(a), "l"(b), "r"(idesc), "r"(acc ? 1 : 0)
-      : "memory");
-}
-
-// the same with A (M x K, bf16 pairs packed in 32-bit columns) read from tensor memory
-__device__ __forceinline__ void pa_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc,
-                                          bool acc) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b), "r"(idesc), "r"(acc ? 1 : 0)
-      : "memory");
-}
-
-// One lane of a full warp, the same one every time. Unlike a comparison of the
-// lane's index it tells the compiler that one lane runs, so that descriptors go
-// to the tensor core from uniform registers (see the tensor-core warp).
-__device__ __forceinline__ bool pa_elect() {
-  uint32_t p;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-  return p != 0;
-}
-
-// A value that all lanes hold, so that the compiler knows they do: control flow
-// and descriptors that depend on it stay on the uniform datapath, which a
-// tcgen05.mma takes its operands from (with the values as read from shared
-// memory an MMA took 65-100 cycles to issue, whatever its shape).
-template <typename T>
-__device__ __forceinline__ T pa_uniform(T x) {
-  return (T)__shfl_sync(0xffffffffu, x, 0);
-}
-
-// 2^x by the SFU (ex2.approx, flushing subnormal results to zero)
-__device__ __forceinline__ float pa_ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-__device__ __forceinline__ void pa_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-                   bar)
-               : "memory");
-}
-
-// requests 32 consecutive fp32 columns of this thread's TMEM lane (pa_wait_ld before use)
-__device__ __forceinline__ void pa_ld32(uint32_t taddr, float* f) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
-      "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-      : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]),
-        "=f"(f[7]), "=f"(f[8]), "=f"(f[9]), "=f"(f[10]), "=f"(f[11]), "=f"(f[12]), "=f"(f[13]),
-        "=f"(f[14]), "=f"(f[15]), "=f"(f[16]), "=f"(f[17]), "=f"(f[18]), "=f"(f[19]), "=f"(f[20]),
-        "=f"(f[21]), "=f"(f[22]), "=f"(f[23]), "=f"(f[24]), "=f"(f[25]), "=f"(f[26]), "=f"(f[27]),
-        "=f"(f[28]), "=f"(f[29]), "=f"(f[30]), "=f"(f[31])
-      : "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void pa_wait_ld() {
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-
-__device__ __forceinline__ void pa_st32(uint32_t taddr, const uint32_t* u) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,"
-      "%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
-      "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]),
-      "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]),
-      "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]),
-      "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]), "r"(u[30]), "r"(u[31])
-      : "memory");
-}
-__device__ __forceinline__ void pa_st16(uint32_t taddr, const uint32_t* u) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
-          taddr),
-      "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]),
-      "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15])
-      : "memory");
-}
-__device__ __forceinline__ void pa_wait_st() {
-  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-}
-
-__device__ __forceinline__ void tc_fence_before() {
-  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-}
-__device__ __forceinline__ void tc_fence_after() {
-  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-}
-__device__ __forceinline__ void fence_async_smem() {
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-}
-
-// TMA load of one box; elements out of the tensor's range are zero
-__device__ __forceinline__ void pa_tma(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
-          dst),
-      "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
-      : "memory");
-}
-
-// asks L2 for a box
-__device__ __forceinline__ void pa_prefetch(const CUtensorMap* map, int x, int y, int z) {
-  asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(x), "r"(y), "r"(z)
-               : "memory");
-}
-
 // multiplies the rows' O (one per lane) by corr
 __device__ __forceinline__ void pa_rescale(uint32_t tO, float corr) {
 #pragma unroll 1
   for (int c0 = 0; c0 < kPaD; c0 += 32) {
     float f[32];
     uint32_t u[32];
-    pa_ld32(tO + c0, f);
-    pa_wait_ld();
+    tc_ld32(tO + c0, f);
+    tc_wait_ld();
 #pragma unroll
     for (int i = 0; i < 32; ++i) u[i] = __float_as_uint(f[i] * corr);
-    pa_st32(tO + c0, u);
+    tc_st32(tO + c0, u);
   }
 }
 
@@ -297,16 +168,16 @@ __device__ __noinline__ void pa_value_clipped(PaShared& sh, uint32_t tmem, int r
   }
   fence_async_smem();
   __syncwarp();
-  if (pa_elect()) {
+  if (tc_elect()) {
     tc_fence_after();
 #pragma unroll 1
     for (int r = 0; r < sees; r += 16)
-      pa_mma_ts(tmem + 256, tmem + r / 2,
-                r + 16 <= sees ? pa_desc(smem_u32(sh.kv[rv]) + r * 128, kPaRows * 128, 1024)
-                               : pa_desc(smem_u32(cut), 16 * 128, 1024),
-                pa_idesc(true), add || r > 0);
-    pa_commit(smem_u32(&sh.o_full[0]));
-    if (last) pa_commit(smem_u32(&sh.kv_empty[rv]));
+      tc_mma_ts(tmem + 256, tmem + r / 2,
+                r + 16 <= sees ? tc_desc(smem_u32(sh.kv[rv]) + r * 128, kPaRows * 128, 1024)
+                               : tc_desc(smem_u32(cut), 16 * 128, 1024),
+                tc_idesc(128, 128, false, true), add || r > 0);
+    tc_commit(smem_u32(&sh.o_full[0]));
+    if (last) tc_commit(smem_u32(&sh.kv_empty[rv]));
   }
   __syncwarp();
 }
@@ -391,7 +262,7 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
   }
   // a programmatic dependent of the scan: what came before reads only cu_seqlens
   griddep_wait();
-  const uint32_t tmem = pa_uniform(sh.tmem);
+  const uint32_t tmem = tc_uniform(sh.tmem);
   const int nitems = sh.pref[a.num_seqs];
   const int parity = *reinterpret_cast<volatile int*>(&L.ctl[a.layer * 4]);
 
@@ -583,12 +454,12 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
       // Q and the raw rows come from HBM: ask L2 for them while the item before
       // still holds the buffers
       if (lane < 4 && im.nvis[lane >> 1] >= 0)
-        pa_prefetch(&maps.q, (lane & 1) * 64, im.h * G, im.tok + (lane >> 1) * TT);
+        tma_prefetch(&maps.q, (lane & 1) * 64, im.h * G, im.tok + (lane >> 1) * TT);
 #pragma unroll 1
       for (int x = lane; x < 4 * nraw * (kPrefillChunk / RAW); x += 32) {
         const int b = x >> 2, t = b / (kPrefillChunk / RAW);
         const int tau = raw_first(im, t) + b % (kPrefillChunk / RAW) * RAW;
-        if (tau < raw_end(im, t)) pa_prefetch(x & 2 ? &maps.v : &maps.k, (x & 1) * 64, im.h, tau);
+        if (tau < raw_end(im, t)) tma_prefetch(x & 2 ? &maps.v : &maps.k, (x & 1) * 64, im.h, tau);
       }
       bool ok = true;
 #pragma unroll 1
@@ -610,14 +481,14 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
           const int p = i * 4 + (lane >> 1);
           const int id = __shfl_sync(0xffffffffu, pid, ((i - pid0) * 4 + (lane >> 1)) & 31);
           if (lane < 8)
-            pa_tma(dst + (lane & 1) * (kPaRows * 128) + (lane >> 1) * (kPage * 128), &maps.pages, bar,
+            tma_load(dst + (lane & 1) * (kPaRows * 128) + (lane >> 1) * (kPage * 128), &maps.pages, bar,
                    (lane & 1) * 64, 0, p < npages ? 2 * id + (x & 1) : oob_page);
         } else {
           // the chunk's rows up to the item's last token, the rest zero
           const int y = x - 2 * nslot, t = y % nraw, which = y / nraw;
           if (lane < 2 * (kPrefillChunk / RAW)) {
             const int b = lane >> 1, tau = raw_first(im, t) + b * RAW;
-            pa_tma(dst + (lane & 1) * (kPaRows * 128) + b * (RAW * 128), which ? &maps.v : &maps.k, bar,
+            tma_load(dst + (lane & 1) * (kPaRows * 128) + b * (RAW * 128), which ? &maps.v : &maps.k, bar,
                    (lane & 1) * 64, im.h, tau < raw_end(im, t) ? tau : a.total_tokens);
           }
         }
@@ -635,7 +506,7 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
             if (lane == 0) mbar_arrive_expect_tx(qb, kPaTileBytes);
             __syncwarp();
             if (lane < 2)
-              pa_tma(smem_u32(sh.q[w]) + lane * (kPaRows * 128), &maps.q, qb, lane * 64, im.h * G, im.tok + w * TT);
+              tma_load(smem_u32(sh.q[w]) + lane * (kPaRows * 128), &maps.q, qb, lane * 64, im.h * G, im.tok + w * TT);
           }
         }
       }
@@ -649,13 +520,13 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
   } else if (warp == 8) {
     // ---------------------------------------------------------------- tensor cores
     uint32_t n = 0;  // ring tiles passed
-    const bool unbounded = pa_uniform(*reinterpret_cast<volatile unsigned int*>(L.unbounded)) != 0;
+    const bool unbounded = tc_uniform(*reinterpret_cast<volatile unsigned int*>(L.unbounded)) != 0;
     // bit w, for query tile w: the parity of the next S / P V / item, and whether
     // there has been one
     uint32_t s_par = 0, v_par = 0, q_par = 0, s_any = 0, v_any = 0;
     bool ok = true;
     // descriptors of K and V tiles but for the address (16-byte units, low bits)
-    const uint64_t k_desc = pa_desc(0, 16, 1024), v_desc = pa_desc(0, kPaRows * 128, 1024);
+    const uint64_t k_desc = tc_desc(0, 16, 1024), v_desc = tc_desc(0, kPaRows * 128, 1024);
     const uint32_t kv0 = smem_u32(sh.kv[0]) >> 4, q0 = smem_u32(sh.q[0]) >> 4;
     // O of query tile w += P V (ring tile rv); `last`: nobody else needs V
     auto value = [&](int w, int rv, bool add, bool last) -> bool {
@@ -664,14 +535,14 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
 #pragma unroll 1
       for (int hf = 0; hf < 2; ++hf) {
         if (!wait(&sh.p_full[w][hf], v_par >> w & 1)) return false;
-        if (pa_elect()) {
+        if (tc_elect()) {
           tc_fence_after();
 #pragma unroll
           for (int kk = 0; kk < kPaSlots / 32; ++kk)
-            pa_mma_ts(tO, tS + (hf * 4 + kk) * 8, vd + (hf * 4 + kk) * (2048 / 16), pa_idesc(true), add || hf || kk > 0);
+            tc_mma_ts(tO, tS + (hf * 4 + kk) * 8, vd + (hf * 4 + kk) * (2048 / 16), tc_idesc(128, 128, false, true), add || hf || kk > 0);
           if (hf) {
-            pa_commit(smem_u32(&sh.o_full[w]));
-            if (last) pa_commit(smem_u32(&sh.kv_empty[rv]));
+            tc_commit(smem_u32(&sh.o_full[w]));
+            if (last) tc_commit(smem_u32(&sh.kv_empty[rv]));
           }
         }
         __syncwarp();
@@ -686,16 +557,16 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
       const uint32_t tS = tmem + w * 128;
       const uint64_t qd = k_desc + (q0 + w * (kPaTileBytes / 16)), kd = k_desc + (kv0 + rk * (kPaTileBytes / 16));
       if ((v_any >> w & 1) && !wait(&sh.o_full[w], ~v_par >> w & 1)) return false;
-      if (pa_elect()) {
+      if (tc_elect()) {
         tc_fence_after();
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
           const uint32_t off = ((kk >> 2) * (kPaRows * 128) + (kk & 3) * 32) / 16;
-          pa_mma(tS, qd + off, kd + off, pa_idesc(false), kk > 0);
+          tc_mma(tS, qd + off, kd + off, tc_idesc(128, 128, false, false), kk > 0);
         }
-        pa_commit(smem_u32(&sh.s_full[w]));
-        if (last) pa_commit(smem_u32(&sh.kv_empty[rk]));
-        if (raw) pa_commit(smem_u32(&sh.q_empty[w]));
+        tc_commit(smem_u32(&sh.s_full[w]));
+        if (last) tc_commit(smem_u32(&sh.kv_empty[rk]));
+        if (raw) tc_commit(smem_u32(&sh.q_empty[w]));
       }
       __syncwarp();
       s_par ^= 1u << w;
@@ -718,11 +589,11 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
       const int sl = it % kPaItems;
       if (!wait(&sh.item_full[sl], (it / kPaItems) & 1)) break;
       PaItem im;
-      im.t0 = pa_uniform(sh.item[sl].t0);
-      im.t1 = pa_uniform(sh.item[sl].t1);
-      im.tok = pa_uniform(sh.item[sl].tok);
-      im.nvis[0] = pa_uniform(sh.item[sl].nvis[0]);
-      im.nvis[1] = pa_uniform(sh.item[sl].nvis[1]);
+      im.t0 = tc_uniform(sh.item[sl].t0);
+      im.t1 = tc_uniform(sh.item[sl].t1);
+      im.tok = tc_uniform(sh.item[sl].tok);
+      im.nvis[0] = tc_uniform(sh.item[sl].nvis[0]);
+      im.nvis[1] = tc_uniform(sh.item[sl].nvis[1]);
       arrive_warp(&sh.item_empty[sl]);
       if (im.t0 > im.t1) break;
       if (max(im.nvis[0], im.nvis[1]) < 0) continue;
@@ -846,7 +717,7 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
       // (rows that saw nothing yet hold zeros).
       auto new_max = [&](float mt) {
         const bool grow = mt > m + 8.f, resc = grow && m != -INFINITY;
-        const float corr = resc ? pa_ex2(m - mt) : 1.f;
+        const float corr = resc ? ex2f(m - mt) : 1.f;
         if (grow) m = mt;
         l *= corr;
         if (__any_sync(0xffffffffu, resc)) pa_rescale(tO, corr);
@@ -859,8 +730,8 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
         // ---- online softmax, in the log2 domain (qscale > 0)
         float s[kPaSlots];
 #pragma unroll
-        for (int c0 = 0; c0 < kPaSlots; c0 += 32) pa_ld32(tS + c0, s + c0);
-        pa_wait_ld();
+        for (int c0 = 0; c0 < kPaSlots; c0 += 32) tc_ld32(tS + c0, s + c0);
+        tc_wait_ld();
         if (!full) {
           // (only the columns that some row of the warp does not see)
           const int seen = __reduce_min_sync(0xffffffffu, vis);
@@ -890,20 +761,20 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             const float2 x = fma2(make_float2(s[c0 + 2 * i], s[c0 + 2 * i + 1]), scale2, shift2);
-            const float2 p = make_float2(pa_ex2(x.x), pa_ex2(x.y));
+            const float2 p = make_float2(ex2f(x.x), ex2f(x.y));
             sum[i & 1] = add2(sum[i & 1], p);
             pk[i] = Chunk<__nv_bfloat16>::pack2(p.x, p.y);
           }
           // P over the row's own S columns: slots c0 + 2 i, + 1 in column c0 / 2 + i
-          pa_st32(tS + c0 / 2, pk);
+          tc_st32(tS + c0 / 2, pk);
           if (c0 == 0) {
-            pa_wait_st();
+            tc_wait_st();
             tc_fence_before();
             arrive_warp(&sh.p_full[w][0]);
           }
         }
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-        pa_wait_st();
+        tc_wait_st();
         tc_fence_before();
         arrive_warp(&sh.p_full[w][1]);
       }
@@ -957,9 +828,9 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
 #pragma unroll 1
       for (int c0 = w_lo & ~31; c0 <= w_hi; c0 += 32) {
         float f[32];
-        pa_ld32(tS + c0, f);
+        tc_ld32(tS + c0, f);
         const uint32_t in = seg_bits(c0);
-        pa_wait_ld();
+        tc_wait_ld();
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
           const float4 om = *reinterpret_cast<const float4*>(M.om + c0 + i);
@@ -971,7 +842,7 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
       }
       const float dsc = wsum * rz * qscale;  // the diagonal score (log2 units)
       new_max(dsc);
-      const float pd = pa_ex2(dsc - m);  // the diagonal's weight, below 2^8
+      const float pd = ex2f(dsc - m);  // the diagonal's weight, below 2^8
       const float pw = pd * rz;
 #pragma unroll 1
       for (int c0 = 0; c0 < kPaSlots; c0 += 32) {
@@ -989,9 +860,9 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
                                                     in & (8u << (2 * i)) ? pw * om.w : 0.f);
           }
         }
-        pa_st16(tS + c0 / 2, pk);
+        tc_st16(tS + c0 / 2, pk);
       }
-      pa_wait_st();
+      tc_wait_st();
       tc_fence_before();
       arrive_warp(&sh.p_full[w][0]);
       arrive_warp(&sh.p_full[w][1]);
@@ -1012,8 +883,8 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
 #pragma unroll 1
       for (int c0 = 0; c0 < D; c0 += 32) {
         float o[32];
-        pa_ld32(tO + c0, o);
-        pa_wait_ld();
+        tc_ld32(tO + c0, o);
+        tc_wait_ld();
         if (carried) {
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
@@ -1066,16 +937,7 @@ dmc_prefill_attn_kernel(const PrefillAttnArgs a, const __grid_constant__ PaMaps 
 // rows of stride `sy` bytes (box by), `nz` planes of stride `sz` bytes (box bz).
 static cudaError_t pa_map(CUtensorMap* map, const void* base, uint64_t ny, uint64_t sy, uint32_t by, uint64_t nz,
                           uint64_t sz, uint32_t bz) {
-  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                              const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                              CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-  static const Encode encode = [] {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    const cudaError_t e =
-        cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
-    return e == cudaSuccess && found == cudaDriverEntryPointSuccess ? reinterpret_cast<Encode>(fn) : nullptr;
-  }();
+  const TensorMapEncode encode = tensor_map_encode();
   if (!encode) return cudaErrorNotSupported;
   const cuuint64_t dims[3] = {(cuuint64_t)kPaD, ny, nz};
   const cuuint64_t strides[2] = {sy, sz};

@@ -13,8 +13,10 @@ cudaError_t states_forward(const StatesArgs& a, bool bf16, int D, cudaStream_t s
 cudaError_t states_backward(const StatesArgs& a, bool bf16, int D, cudaStream_t stream);
 cudaError_t attn_forward_f32(const AttnArgs& a, bool bf16, int D, cudaStream_t stream);
 cudaError_t attn_backward_f32(const AttnArgs& a, bool bf16, int D, cudaStream_t stream);
-cudaError_t loss_forward_f32(const LossArgs& a, bool bf16, int* shares, cudaStream_t stream);
-cudaError_t loss_backward_f32(const LossArgs& a, bool bf16, cudaStream_t stream);
+cudaError_t loss_forward_f32(const LossArgs& a, int* shares, cudaStream_t stream);
+cudaError_t loss_backward_f32(const LossArgs& a, cudaStream_t stream);
+cudaError_t loss_forward_bf16(const LossArgs& a, int* shares, cudaStream_t stream);
+cudaError_t loss_backward_bf16(const LossArgs& a, cudaStream_t stream);
 
 namespace {
 
@@ -47,7 +49,7 @@ bool valid(const dmc_retrofit_config* c) {
 // Words of one piece of the loss's backward pass: the gradient of its logits is
 // kept for all tokens, in at most 512 MB, but no fewer than 1024 words.
 int loss_piece(const dmc_retrofit_config* c) {
-  const int64_t per_word = (int64_t)c->max_tokens * 4;
+  const int64_t per_word = (int64_t)c->max_tokens * (c->dtype == DMC_F32 ? 4 : 2);
   int64_t words = (512ll << 20) / per_word / 256 * 256;
   const int64_t all = ((int64_t)c->vocab + 255) / 256 * 256;
   if (words < 1024) words = 1024;
@@ -72,11 +74,12 @@ Offsets offsets(const dmc_retrofit_config* c) {
   }
   if (has_loss(*c)) {
     o.piece = loss_piece(c);
-    o.part_m = at; at = align_up(at + tokens * kLossSplits * 4);
-    o.part_l = at; at = align_up(at + tokens * kLossSplits * 4);
+    const size_t shares = loss_shares(c->dtype == DMC_BF16, c->vocab);
+    o.part_m = at; at = align_up(at + tokens * shares * 4);
+    o.part_l = at; at = align_up(at + tokens * shares * 4);
     o.target_logit = at; at = align_up(at + tokens * 4);
     o.dh = at; at = align_up(at + (o.piece < c->vocab ? tokens * c->hidden * 4 : 0));
-    o.grad = at; at = align_up(at + tokens * o.piece * 4);
+    o.grad = at; at = align_up(at + tokens * o.piece * (c->dtype == DMC_F32 ? 4 : 2));
   }
   o.total = at;
   return o;
@@ -328,7 +331,7 @@ dmc_status dmc_retrofit_loss(dmc_retrofit_t h, int32_t num_tokens, const void* h
   a.loss = loss_dev;
   a.lse = lse_dev;
   int shares = 0;
-  const cudaError_t e = dmc::loss_forward_f32(a, bf16(h), &shares, stream);
+  const cudaError_t e = (bf16(h) ? dmc::loss_forward_bf16 : dmc::loss_forward_f32)(a, &shares, stream);
   if (e != cudaSuccess) return DMC_ERR_CUDA;
   dmc::loss_join_kernel<<<dmc::ceil_div(a.N, 8), 256, 0, stream>>>(a, shares);
   return dmc::cuda_status(cudaGetLastError());
@@ -351,7 +354,7 @@ dmc_status dmc_retrofit_loss_backward(dmc_retrofit_t h, int32_t num_tokens, cons
   a.dloss = dloss_dev;
   a.dhidden = dhidden_dev;
   a.dweight = dweight_dev;
-  return dmc::cuda_status(dmc::loss_backward_f32(a, bf16(h), stream));
+  return dmc::cuda_status((bf16(h) ? dmc::loss_backward_bf16 : dmc::loss_backward_f32)(a, stream));
 }
 
 dmc_status dmc_retrofit_status(dmc_retrofit_t h, cudaStream_t stream, uint32_t* bits) {

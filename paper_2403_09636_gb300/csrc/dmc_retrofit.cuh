@@ -127,7 +127,9 @@ struct LossArgs {
   unsigned int* error;
 };
 
-// Shares of the vocabulary that the loss kernels keep a maximum and sum for
-constexpr int kLossSplits = 160;
+// Shares of the vocabulary that a token's maximum and sum are kept for: a tile of the
+// tensor-core kernel, at most kLossSplits for the CUDA cores
+constexpr int kLossTile = 256, kLossSplits = 160;
+inline int loss_shares(bool bf16, int vocab) { return bf16 ? ceil_div(vocab, kLossTile) : kLossSplits; }
 
 }  // namespace dmc

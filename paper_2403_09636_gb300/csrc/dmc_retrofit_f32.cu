@@ -348,7 +348,6 @@ cudaError_t attn_b(const AttnArgs& a, cudaStream_t stream) {
 constexpr int kK = 64;  // columns of a K step (a tile of kK + 4 per row)
 
 // acc += A[64 rows from r0] . B[64 rows from c0]^T over all H columns
-template <typename T>
 __device__ __forceinline__ void logits_tile(float (&acc)[4][4], float* X, float* Y, const LossArgs& a, int r0, int c0) {
   for (int k = 0; k < a.H; k += kK) {
     __syncthreads();
@@ -357,8 +356,7 @@ __device__ __forceinline__ void logits_tile(float (&acc)[4][4], float* X, float*
       const int row = (side ? c0 : r0) + r;
       float2 f = make_float2(0.f, 0.f);
       if (row < (side ? a.V : a.N) && k + c < a.H)
-        f = Pair<T>::to_f(*reinterpret_cast<const typename Pair<T>::Raw*>(
-            static_cast<const T*>(side ? a.weight : a.hidden) + (long long)row * a.H + k + c));
+        f = *reinterpret_cast<const float2*>(static_cast<const float*>(side ? a.weight : a.hidden) + (long long)row * a.H + k + c);
       *reinterpret_cast<float2*>((side ? Y : X) + r * (kK + 4) + c) = f;
     }
     __syncthreads();
@@ -367,7 +365,6 @@ __device__ __forceinline__ void logits_tile(float (&acc)[4][4], float* X, float*
 }
 
 // Maximum and sum of exponentials of a share of the vocabulary for 64 tokens
-template <typename T>
 __global__ void __launch_bounds__(kThreads) loss_kernel(const LossArgs a, int tiles) {
   __shared__ __align__(16) float X[kT * (kK + 4)], Y[kT * (kK + 4)];
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, r0 = blockIdx.x * kT;
@@ -377,7 +374,7 @@ __global__ void __launch_bounds__(kThreads) loss_kernel(const LossArgs a, int ti
   const int c_end = min((long long)a.V, ((long long)blockIdx.y + 1) * tiles * kT);
   for (int c0 = blockIdx.y * tiles * kT; c0 < c_end; c0 += kT) {
     float s[4][4] = {};
-    logits_tile<T>(s, X, Y, a, r0, c0);
+    logits_tile(s, X, Y, a, r0, c0);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = r0 + ty + 16 * i;
@@ -409,12 +406,11 @@ __global__ void __launch_bounds__(kThreads) loss_kernel(const LossArgs a, int ti
 }
 
 // The gradient of a piece's logits: (softmax - [word = target]) dloss
-template <typename T>
 __global__ void __launch_bounds__(kThreads) loss_grad_kernel(const LossArgs a, int v0) {
   __shared__ __align__(16) float X[kT * (kK + 4)], Y[kT * (kK + 4)];
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, r0 = blockIdx.x * kT, c0 = v0 + blockIdx.y * kT;
   float s[4][4] = {};
-  logits_tile<T>(s, X, Y, a, r0, c0);
+  logits_tile(s, X, Y, a, r0, c0);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = r0 + ty + 16 * i;
@@ -434,13 +430,13 @@ __global__ void __launch_bounds__(kThreads) loss_grad_kernel(const LossArgs a, i
 
 // C[64 x 64 tile] = sum over r of A(i, r) B[r][c]: dhidden (A = grad, r over the piece's
 // words, added to what the pieces before gave) and dweight (A = grad^T, r over the tokens)
-template <typename T, bool kWords>
+template <bool kWords>
 __global__ void __launch_bounds__(kThreads) loss_product_kernel(const LossArgs a, int v0, bool first, bool last) {
   __shared__ __align__(16) float W[kT * kW], Y[kT * (64 + 4)];
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, i0 = blockIdx.x * kT, c0 = blockIdx.y * 64;
   const int words = min(a.piece, a.V - v0);
   const int rows = kWords ? words : a.N, sum = kWords ? a.N : words;  // rows of C, terms of its sums
-  const T* B = static_cast<const T*>(kWords ? a.hidden : a.weight) + (kWords ? 0 : (long long)v0 * a.H);
+  const float* B = static_cast<const float*>(kWords ? a.hidden : a.weight) + (kWords ? 0 : (long long)v0 * a.H);
   const float* grad = static_cast<const float*>(a.grad);
   float4 acc[4][1] = {};
   for (int r0 = 0; r0 < sum; r0 += kT) {
@@ -455,7 +451,7 @@ __global__ void __launch_bounds__(kThreads) loss_product_kernel(const LossArgs a
       const int r = i / 32, c = i % 32 * 2;
       float2 f = make_float2(0.f, 0.f);
       if (r0 + r < sum && c0 + c < a.H)
-        f = Pair<T>::to_f(*reinterpret_cast<const typename Pair<T>::Raw*>(B + (long long)(r0 + r) * a.H + c0 + c));
+        f = *reinterpret_cast<const float2*>(B + (long long)(r0 + r) * a.H + c0 + c);
       *reinterpret_cast<float2*>(Y + r * 68 + c) = f;
     }
     __syncthreads();
@@ -472,31 +468,29 @@ __global__ void __launch_bounds__(kThreads) loss_product_kernel(const LossArgs a
       f = make_float4(f.x + o.x, f.y + o.y, f.z + o.z, f.w + o.w);
     }
     if (kWords)
-      store4(static_cast<T*>(a.dweight) + at, f);
+      store4(static_cast<float*>(a.dweight) + at, f);
     else if (last)
-      store4(static_cast<T*>(a.dhidden) + at, f);
+      store4(static_cast<float*>(a.dhidden) + at, f);
     else
       *reinterpret_cast<float4*>(a.dh + at) = f;
   }
 }
 
-template <typename T>
 cudaError_t loss_f(const LossArgs& a, int* shares, cudaStream_t stream) {
   const int rows = ceil_div(a.N, kT), cols = ceil_div(a.V, kT);
   const int tiles = ceil_div(cols, min(cols, min(kLossSplits, max(1, 608 / rows))));
   *shares = ceil_div(cols, tiles);
-  loss_kernel<T><<<dim3(rows, *shares), kThreads, 0, stream>>>(a, tiles);
+  loss_kernel<<<dim3(rows, *shares), kThreads, 0, stream>>>(a, tiles);
   return cudaGetLastError();
 }
 
-template <typename T>
 cudaError_t loss_b(const LossArgs& a, cudaStream_t stream) {
   const int rows = ceil_div(a.N, kT), cols = ceil_div(a.H, 64);
   for (int v0 = 0; v0 < a.V; v0 += a.piece) {
     const int words = min(a.piece, a.V - v0);
-    loss_grad_kernel<T><<<dim3(rows, ceil_div(words, kT)), kThreads, 0, stream>>>(a, v0);
-    loss_product_kernel<T, false><<<dim3(rows, cols), kThreads, 0, stream>>>(a, v0, v0 == 0, v0 + a.piece >= a.V);
-    loss_product_kernel<T, true><<<dim3(ceil_div(words, kT), cols), kThreads, 0, stream>>>(a, v0, false, false);
+    loss_grad_kernel<<<dim3(rows, ceil_div(words, kT)), kThreads, 0, stream>>>(a, v0);
+    loss_product_kernel<false><<<dim3(rows, cols), kThreads, 0, stream>>>(a, v0, v0 == 0, v0 + a.piece >= a.V);
+    loss_product_kernel<true><<<dim3(ceil_div(words, kT), cols), kThreads, 0, stream>>>(a, v0, false, false);
   }
   return cudaGetLastError();
 }
@@ -511,11 +505,7 @@ cudaError_t attn_backward_f32(const AttnArgs& a, bool bf16, int D, cudaStream_t 
   if (bf16) return D == 128 ? attn_b<__nv_bfloat16, 128>(a, stream) : attn_b<__nv_bfloat16, 64>(a, stream);
   return D == 128 ? attn_b<float, 128>(a, stream) : attn_b<float, 64>(a, stream);
 }
-cudaError_t loss_forward_f32(const LossArgs& a, bool bf16, int* shares, cudaStream_t stream) {
-  return bf16 ? loss_f<__nv_bfloat16>(a, shares, stream) : loss_f<float>(a, shares, stream);
-}
-cudaError_t loss_backward_f32(const LossArgs& a, bool bf16, cudaStream_t stream) {
-  return bf16 ? loss_b<__nv_bfloat16>(a, stream) : loss_b<float>(a, stream);
-}
+cudaError_t loss_forward_f32(const LossArgs& a, int* shares, cudaStream_t stream) { return loss_f(a, shares, stream); }
+cudaError_t loss_backward_f32(const LossArgs& a, cudaStream_t stream) { return loss_b(a, stream); }
 
 }  // namespace dmc
