@@ -13,6 +13,7 @@ cudaError_t states_forward(const StatesArgs& a, bool bf16, int D, cudaStream_t s
 cudaError_t states_backward(const StatesArgs& a, bool bf16, int D, cudaStream_t stream);
 cudaError_t attn_forward_f32(const AttnArgs& a, bool bf16, int D, cudaStream_t stream);
 cudaError_t attn_backward_f32(const AttnArgs& a, bool bf16, int D, cudaStream_t stream);
+cudaError_t attn_forward_bf16(const AttnArgs& a, int D, cudaStream_t stream);
 cudaError_t loss_forward_f32(const LossArgs& a, int* shares, cudaStream_t stream);
 cudaError_t loss_backward_f32(const LossArgs& a, cudaStream_t stream);
 cudaError_t loss_forward_bf16(const LossArgs& a, int* shares, cudaStream_t stream);
@@ -294,7 +295,8 @@ dmc_status dmc_retrofit_attention(dmc_retrofit_t h, int32_t num_seqs, const void
   dmc::AttnArgs a = attn_args(h, num_seqs, q_dev, k_dev, v_dev, bias_dev, cu_seqlens_dev, total_tokens, max_seqlen);
   a.out = out_dev;
   a.lse = lse_dev;
-  return dmc::cuda_status(dmc::attn_forward_f32(a, bf16(h), h->cfg.head_dim, stream));
+  const int D = h->cfg.head_dim;
+  return dmc::cuda_status(bf16(h) ? dmc::attn_forward_bf16(a, D, stream) : dmc::attn_forward_f32(a, false, D, stream));
 }
 
 dmc_status dmc_retrofit_attention_backward(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev, const void* k_dev,
