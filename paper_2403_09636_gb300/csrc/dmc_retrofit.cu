@@ -11,8 +11,9 @@
 namespace dmc {
 cudaError_t states_forward(const StatesArgs& a, bool bf16, int D, cudaStream_t stream);
 cudaError_t states_backward(const StatesArgs& a, bool bf16, int D, cudaStream_t stream);
-cudaError_t attn_forward_f32(const AttnArgs& a, bool bf16, int D, cudaStream_t stream);
-cudaError_t attn_backward_f32(const AttnArgs& a, bool bf16, int D, cudaStream_t stream);
+cudaError_t attn_forward_f32(const AttnArgs& a, int D, cudaStream_t stream);
+cudaError_t attn_backward_f32(const AttnArgs& a, int D, cudaStream_t stream);
+cudaError_t attn_backward_bf16(const AttnArgs& a, int D, cudaStream_t stream);
 cudaError_t attn_forward_bf16(const AttnArgs& a, int D, cudaStream_t stream);
 cudaError_t loss_forward_f32(const LossArgs& a, int* shares, cudaStream_t stream);
 cudaError_t loss_backward_f32(const LossArgs& a, cudaStream_t stream);
@@ -22,6 +23,7 @@ cudaError_t loss_backward_bf16(const LossArgs& a, cudaStream_t stream);
 namespace {
 
 constexpr size_t kAlign = 256;
+constexpr size_t kControl = 64;  // the fault bits, and from byte 16 the attention kernels' counters, 8 bytes each
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool given16(const void* p) { return p && aligned16(p); }
@@ -58,7 +60,7 @@ int loss_piece(const dmc_retrofit_config* c) {
 }
 
 struct Offsets {
-  size_t error, sums, delta, part_m, part_l, target_logit, dh, grad, total;
+  size_t error, sums, rows, part_m, part_l, target_logit, dh, grad, total;
   int piece;
 };
 
@@ -66,12 +68,15 @@ Offsets offsets(const dmc_retrofit_config* c) {
   Offsets o = {};
   size_t at = 0;
   const size_t tokens = c->max_tokens;
-  o.error = at; at = align_up(at + 4);
+  o.error = at; at = align_up(at + kControl);
   if (has_heads(*c)) {
     o.sums = at;
     at = align_up(at + (size_t)pieces(c->max_tokens, c->max_seqs, kStateChunk) * c->num_kv_heads *
                            (2 * c->head_dim + 4) * 4);
-    o.delta = at; at = align_up(at + tokens * c->num_q_heads * 4);
+    // the backward pass's two numbers per query, padded to tiles of 128 (one in fp32)
+    o.rows = at;
+    at = align_up(at + (c->dtype == DMC_F32 ? tokens * 4 : (size_t)pieces(c->max_tokens, c->max_seqs, 128) * 1024) *
+                           c->num_q_heads);
   }
   if (has_loss(*c)) {
     o.piece = loss_piece(c);
@@ -162,7 +167,8 @@ dmc::AttnArgs attn_args(dmc_retrofit_t h, int32_t num_seqs, const void* q, const
   a.k = k;
   a.v = v;
   a.bias = bias;
-  a.delta = reinterpret_cast<float*>(h->base + h->at.delta);
+  a.rows = reinterpret_cast<float*>(h->base + h->at.rows);
+  a.counter = reinterpret_cast<int*>(h->base + h->at.error + 16);
   a.error = reinterpret_cast<unsigned int*>(h->base + h->at.error);
   return a;
 }
@@ -209,7 +215,7 @@ dmc_status dmc_retrofit_create(const dmc_retrofit_config* cfg, void* arena_dev, 
   h->at = o;
   h->base = static_cast<char*>(arena_dev);
   cudaError_t e = cudaGetDevice(&h->device);
-  if (e == cudaSuccess) e = cudaMemsetAsync(h->base + o.error, 0, 4, stream);
+  if (e == cudaSuccess) e = cudaMemsetAsync(h->base + o.error, 0, dmc::kControl, stream);
   if (e != cudaSuccess) {
     delete h;
     return DMC_ERR_CUDA;
@@ -296,7 +302,7 @@ dmc_status dmc_retrofit_attention(dmc_retrofit_t h, int32_t num_seqs, const void
   a.out = out_dev;
   a.lse = lse_dev;
   const int D = h->cfg.head_dim;
-  return dmc::cuda_status(bf16(h) ? dmc::attn_forward_bf16(a, D, stream) : dmc::attn_forward_f32(a, false, D, stream));
+  return dmc::cuda_status(bf16(h) ? dmc::attn_forward_bf16(a, D, stream) : dmc::attn_forward_f32(a, D, stream));
 }
 
 dmc_status dmc_retrofit_attention_backward(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev, const void* k_dev,
@@ -319,7 +325,8 @@ dmc_status dmc_retrofit_attention_backward(dmc_retrofit_t h, int32_t num_seqs, c
   a.dk = dk_dev;
   a.dv = dv_dev;
   a.dbias = dbias_dev;
-  return dmc::cuda_status(dmc::attn_backward_f32(a, bf16(h), h->cfg.head_dim, stream));
+  const int D = h->cfg.head_dim;
+  return dmc::cuda_status(bf16(h) ? dmc::attn_backward_bf16(a, D, stream) : dmc::attn_backward_f32(a, D, stream));
 }
 
 dmc_status dmc_retrofit_loss(dmc_retrofit_t h, int32_t num_tokens, const void* hidden_dev, const void* weight_dev,

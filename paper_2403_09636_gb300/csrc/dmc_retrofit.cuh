@@ -108,7 +108,8 @@ struct AttnArgs {
   float* lse;           // [Hq][total]
   const void* dout;
   void *dq, *dk, *dv, *dbias;
-  float* delta;         // scratch, [Hq][total]
+  float* rows;          // scratch, per query: see attn_rows_kernel ([Hq][total] deltas for fp32)
+  int* counter;         // work items handed out, CTAs done: zero between launches
   unsigned int* error;
 };
 

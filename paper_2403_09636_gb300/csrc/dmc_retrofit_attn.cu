@@ -14,22 +14,14 @@
 // P is rounded to bf16, the type of the tensor cores' operand; the sum is taken from the
 // unrounded weights. The running maximum moves only when it grows by more than 8 (in log2
 // units): P stays below 2^8, and O is rescaled rarely.
-#include <math.h>
-#include <stddef.h>
-
-#include "dmc_retrofit.cuh"
-#include "dmc_tensor.cuh"
+#include "dmc_retrofit_attn.cuh"
 
 namespace dmc {
 
 namespace {
 
-constexpr int kR = 128;          // rows of a tile
 constexpr int kItem = 2 * kR;    // queries of a work item
-constexpr int kFwdThreads = 384; // warps 10 and 11 only complete the third warpgroup
 constexpr int kRing = 4;
-constexpr int kStageRow = 80;    // bytes of a row of an epilogue stage: 64 and 16 of padding
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 template <int D>
 struct FwdShared {
@@ -40,6 +32,7 @@ struct FwdShared {
   uint64_t kv_full[kRing], kv_empty[kRing];
   uint64_t q_full[2], q_empty[2];
   uint64_t s_full[2], p_full[2][2], o_full[2];  // P in two halves
+  WorkRing work;
   uint32_t tmem;
   int abort;
 };
@@ -70,12 +63,6 @@ __device__ __forceinline__ Item item_of(const AttnArgs& a, int index) {
   return w;
 }
 
-template <int D>
-__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int tok) {
-#pragma unroll
-  for (int c = 0; c < D / 64; ++c) tma_load(dst + c * (kR * 128), map, bar, c * 64, head, tok);
-}
-
 // multiplies the rows' O (one per lane) by corr
 template <int D>
 __device__ __forceinline__ void rescale(uint32_t tO, float corr) {
@@ -91,39 +78,8 @@ __device__ __forceinline__ void rescale(uint32_t tO, float corr) {
   }
 }
 
-// Rows of the epilogue: 32 columns of each lane's row (values f) to global memory through the
-// warp's stage; row r of the warp at dst + r * stride bytes, rows at and after `rows` left out.
-__device__ __forceinline__ void write_rows(unsigned char* stage, const float* f, char* dst, long long stride, int rows) {
-  const int lane = threadIdx.x & 31;
-  __syncwarp();  // the stage has been read
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    *reinterpret_cast<uint4*>(stage + lane * kStageRow + i * 16) = Chunk<__nv_bfloat16>::pack(f + i * 8);
-  __syncwarp();
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int r = k * 8 + (lane >> 2);
-    const uint4 v = *reinterpret_cast<const uint4*>(stage + r * kStageRow + (lane & 3) * 16);
-    if (r < rows) *reinterpret_cast<uint4*>(dst + r * stride + (lane & 3) * 16) = v;
-  }
-}
-
-// Rows [r0, 128) of a tile set to zero, by a warp: weights are zero there, but what lies
-// beyond a sequence's end need not be a number.
-template <int D>
-__device__ __forceinline__ void zero_rows(unsigned char* tile, int r0) {
-  constexpr int kPieces = D / 8;  // of 16 bytes per row
-#pragma unroll 1
-  for (int x = threadIdx.x & 31; x < (kR - r0) * kPieces; x += 32) {
-    const int r = r0 + x / kPieces, j = x % kPieces;
-    *reinterpret_cast<uint4*>(tile + (j >> 3) * (kR * 128) + r * 128 + (j & 7) * 16) = make_uint4(0, 0, 0, 0);
-  }
-  fence_async_smem();
-  __syncwarp();
-}
-
 template <int D, bool kBias>
-__global__ void __launch_bounds__(kFwdThreads, 1)
+__global__ void __launch_bounds__(kAttnThreads, 1)
 attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int items) {
   constexpr int kTile = kR * D * 2;
   extern __shared__ unsigned char smem_raw[];
@@ -145,6 +101,7 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
       for (int hf = 0; hf < 2; ++hf) mbar_init(smem_u32(&sh.p_full[w][hf]), 4);
       mbar_init(smem_u32(&sh.o_full[w]), 1);
     }
+    work_init(sh.work);
     fence_mbar_init();
     sh.abort = 0;
   }
@@ -161,6 +118,13 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(bar));
   };
+  auto next_item = [&](int turn) -> int {  // INT_MAX: a wait gave up
+    const int sl = turn & 1;
+    if (!wait(&sh.work.full[sl], (turn >> 1) & 1)) return INT_MAX;
+    const int index = *reinterpret_cast<volatile int*>(&sh.work.index[sl]);
+    arrive_warp(&sh.work.empty[sl]);
+    return tc_uniform(index);
+  };
 
   if (warp >= 8) {
     // A softmax thread holds a row of scores: 208 registers for those, 88 for the others
@@ -170,7 +134,16 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
       // ---------------------------------------------------------------- loads
       uint32_t n = 0, q_par = 0, q_any = 0;  // bit w: parity of query tile w's next Q, whether there was one
       bool ok = true;
-      for (int index = blockIdx.x; index < items && ok; index += gridDim.x) {
+      int index = blockIdx.x, next = 0;
+      for (int it = 0; ok; ++it, index = __shfl_sync(0xffffffffu, next, 0)) {
+        const int sl = it & 1;
+        if (!wait(&sh.work.empty[sl], ((it >> 1) & 1) ^ 1)) break;
+        if (lane == 0) {
+          sh.work.index[sl] = index;
+          if (index < items) next = (int)gridDim.x + atomicAdd(a.counter, 1);
+        }
+        arrive_warp(&sh.work.full[sl]);
+        if (index >= items) break;
         const Item w = item_of(a, index);
         if (!w.ok) continue;
         const int hk = w.h / a.G, steps = max(w.n[0], w.n[1]);
@@ -265,7 +238,9 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
         s_any |= 1u << t;
         return true;
       };
-      for (int index = blockIdx.x; index < items && ok; index += gridDim.x) {
+      for (int turn = 0; ok; ++turn) {
+        const int index = next_item(turn);
+        if (index >= items) break;
         const Item it = item_of(a, index);
         if (!it.ok) continue;
         const int n0 = tc_uniform(it.n[0]), n1 = tc_uniform(it.n[1]), steps = max(n0, n1);
@@ -312,7 +287,9 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
     const float qscale = kLog2e / sqrtf((float)D);
     uint32_t steps = 0;
     bool ok = true;
-    for (int index = blockIdx.x; index < items && ok; index += gridDim.x) {
+    for (int turn = 0; ok; ++turn) {
+      const int index = next_item(turn);
+      if (index >= items) break;
       const Item it = item_of(a, index);
       const int nt = it.n[t];
       if (!it.ok || nt == 0) continue;
@@ -427,25 +404,7 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
   }
-}
-
-// [token][head][D] in bf16, boxes of 128 tokens x 64 columns of one head; zero beyond the last token
-cudaError_t heads_map(CUtensorMap* map, const void* base, int D, int heads, int tokens) {
-  const TensorMapEncode encode = tensor_map_encode();
-  if (!encode) return cudaErrorNotSupported;
-  const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)tokens};
-  const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)D * 2 * heads};
-  const cuuint32_t box[3] = {64, 1, kR}, unit[3] = {1, 1, 1};
-  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, unit,
-                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
-}
-
-cudaError_t sm_count(int* sms) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  return e == cudaSuccess ? cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) : e;
+  if (tid == 0) work_done(a.counter);
 }
 
 template <int D, bool kBias>
@@ -463,7 +422,7 @@ cudaError_t forward(const AttnArgs& a, cudaStream_t stream) {
   if (e != cudaSuccess) return e;
   const long long items = pieces(a.seqs.total, a.seqs.num, kItem) * a.Hq;
   if (items > INT32_MAX) return cudaErrorInvalidValue;
-  kernel<<<(unsigned)(items < sms ? items : sms), kFwdThreads, bytes, stream>>>(a, maps, (int)items);
+  kernel<<<(unsigned)(items < sms ? items : sms), kAttnThreads, bytes, stream>>>(a, maps, (int)items);
   return cudaGetLastError();
 }
 

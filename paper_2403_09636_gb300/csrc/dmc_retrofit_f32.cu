@@ -17,12 +17,12 @@ constexpr int kThreads = 256;
 constexpr int kW = kT + 4;      // row of a tile of weights
 
 // rows [r0, r1) of a matrix of D columns into a tile, zero from r1 on
-template <typename T, int D>
-__device__ __forceinline__ void load_rows(float* tile, const T* src, long long stride, int rows) {
+template <int D>
+__device__ __forceinline__ void load_rows(float* tile, const float* src, long long stride, int rows) {
   for (int i = threadIdx.x; i < kT * (D / 2); i += kThreads) {
     const int r = i / (D / 2), c = i % (D / 2) * 2;
     float2 f = make_float2(0.f, 0.f);
-    if (r < rows) f = Pair<T>::to_f(*reinterpret_cast<const typename Pair<T>::Raw*>(src + r * stride + c));
+    if (r < rows) f = *reinterpret_cast<const float2*>(src + r * stride + c);
     *reinterpret_cast<float2*>(tile + r * (D + 4) + c) = f;
   }
 }
@@ -76,12 +76,7 @@ __device__ __forceinline__ void sum_tile(float4 (&acc)[4][D / 64], const float* 
   }
 }
 
-template <typename T>
-__device__ __forceinline__ void store4(T* dst, float4 f) {
-  using P = Pair<T>;
-  *reinterpret_cast<typename P::Raw*>(dst) = P::from_f(make_float2(f.x, f.y));
-  *reinterpret_cast<typename P::Raw*>(dst + 2) = P::from_f(make_float2(f.z, f.w));
-}
+__device__ __forceinline__ void store4(float* dst, float4 f) { *reinterpret_cast<float4*>(dst) = f; }
 
 __device__ __forceinline__ float4 times(float4 a, float s) { return make_float4(a.x * s, a.y * s, a.z * s, a.w * s); }
 
@@ -102,7 +97,7 @@ __device__ __forceinline__ float row_sum(float x) {
 // Whether query i sees row j
 __device__ __forceinline__ bool sees(int i, int j, float bias) { return j == i || (j < i && bias != -INFINITY); }
 
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnArgs a) {
   extern __shared__ float smem[];
   float *Q = smem, *K = Q + kT * (D + 4), *V = K + kT * (D + 4), *W = V + kT * (D + 4);
@@ -114,7 +109,7 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnArgs a) {
   const int i0 = p.t0 + p.at * kT, rows = min(kT, p.t1 - i0);
   const float scale = 1.f / sqrtf((float)D);
   const long long qs = (long long)a.Hq * D, ks = (long long)a.Hkv * D;
-  load_rows<T, D>(Q, static_cast<const T*>(a.q) + (long long)i0 * qs + (long long)h * D, qs, rows);
+  load_rows<D>(Q, static_cast<const float*>(a.q) + (long long)i0 * qs + (long long)h * D, qs, rows);
   float4 acc[4][D / 64] = {};
   float m[4], l[4];
 #pragma unroll
@@ -122,8 +117,8 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnArgs a) {
   for (int j0 = p.t0; j0 <= i0; j0 += kT) {
     const int keys = min(kT, p.t1 - j0);
     __syncthreads();
-    load_rows<T, D>(K, static_cast<const T*>(a.k) + (long long)j0 * ks + (long long)hk * D, ks, keys);
-    load_rows<T, D>(V, static_cast<const T*>(a.v) + (long long)j0 * ks + (long long)hk * D, ks, keys);
+    load_rows<D>(K, static_cast<const float*>(a.k) + (long long)j0 * ks + (long long)hk * D, ks, keys);
+    load_rows<D>(V, static_cast<const float*>(a.v) + (long long)j0 * ks + (long long)hk * D, ks, keys);
     __syncthreads();
     float s[4][4] = {};
     dot_tile<D>(s, Q, K);
@@ -163,7 +158,7 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnArgs a) {
     if (r >= rows) continue;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c)
-      store4(static_cast<T*>(a.out) + (long long)(i0 + r) * qs + (long long)h * D + 4 * tx + 64 * c,
+      store4(static_cast<float*>(a.out) + (long long)(i0 + r) * qs + (long long)h * D + 4 * tx + 64 * c,
              times(acc[i][c], 1.f / l[i]));
     if (tx == 0) a.lse[(long long)h * a.seqs.total + i0 + r] = m[i] + logf(l[i]);
   }
@@ -171,7 +166,7 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnArgs a) {
 
 // The rows of Q's gradient: dQ_i = scale sum over j of dS_ij k_j, with
 // dS = P (dO V^T - delta), delta_i = dO_i . out_i
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kThreads) attn_dq_kernel(const AttnArgs a) {
   extern __shared__ float smem[];
   float *Q = smem, *O = Q + kT * (D + 4), *K = O + kT * (D + 4), *V = K + kT * (D + 4), *W = V + kT * (D + 4);
@@ -182,22 +177,22 @@ __global__ void __launch_bounds__(kThreads) attn_dq_kernel(const AttnArgs a) {
   const int i0 = p.t0 + p.at * kT, rows = min(kT, p.t1 - i0);
   const float scale = 1.f / sqrtf((float)D);
   const long long qs = (long long)a.Hq * D, ks = (long long)a.Hkv * D;
-  load_rows<T, D>(Q, static_cast<const T*>(a.q) + (long long)i0 * qs + (long long)h * D, qs, rows);
-  load_rows<T, D>(O, static_cast<const T*>(a.dout) + (long long)i0 * qs + (long long)h * D, qs, rows);
+  load_rows<D>(Q, static_cast<const float*>(a.q) + (long long)i0 * qs + (long long)h * D, qs, rows);
+  load_rows<D>(O, static_cast<const float*>(a.dout) + (long long)i0 * qs + (long long)h * D, qs, rows);
   float lse[4], delta[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const long long at = (long long)h * a.seqs.total + i0 + ty + 16 * i;
     const bool in = ty + 16 * i < rows;
     lse[i] = in ? a.lse[at] : 0.f;
-    delta[i] = in ? a.delta[at] : 0.f;
+    delta[i] = in ? a.rows[at] : 0.f;
   }
   float4 acc[4][D / 64] = {};
   for (int j0 = p.t0; j0 <= i0; j0 += kT) {
     const int keys = min(kT, p.t1 - j0);
     __syncthreads();
-    load_rows<T, D>(K, static_cast<const T*>(a.k) + (long long)j0 * ks + (long long)hk * D, ks, keys);
-    load_rows<T, D>(V, static_cast<const T*>(a.v) + (long long)j0 * ks + (long long)hk * D, ks, keys);
+    load_rows<D>(K, static_cast<const float*>(a.k) + (long long)j0 * ks + (long long)hk * D, ks, keys);
+    load_rows<D>(V, static_cast<const float*>(a.v) + (long long)j0 * ks + (long long)hk * D, ks, keys);
     __syncthreads();
     float s[4][4] = {}, dp[4][4] = {};
     dot_tile<D>(s, Q, K);
@@ -221,13 +216,13 @@ __global__ void __launch_bounds__(kThreads) attn_dq_kernel(const AttnArgs a) {
     if (ty + 16 * i < rows)
 #pragma unroll
       for (int c = 0; c < D / 64; ++c)
-        store4(static_cast<T*>(a.dq) + (long long)(i0 + ty + 16 * i) * qs + (long long)h * D + 4 * tx + 64 * c,
+        store4(static_cast<float*>(a.dq) + (long long)(i0 + ty + 16 * i) * qs + (long long)h * D + 4 * tx + 64 * c,
                times(acc[i][c], scale));
 }
 
 // The rows of K's and V's gradients and of the bias's, summed over the queries of the
 // group: dV_j = sum of P_ij dO_i, dK_j = scale sum of dS_ij q_i, dbias_j = sum over i > j of dS_ij
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kThreads) attn_dkv_kernel(const AttnArgs a) {
   extern __shared__ float smem[];
   float *K = smem, *V = K + kT * (D + 4), *Q = V + kT * (D + 4), *O = Q + kT * (D + 4), *W = O + kT * (D + 4);
@@ -238,8 +233,8 @@ __global__ void __launch_bounds__(kThreads) attn_dkv_kernel(const AttnArgs a) {
   const int j0 = p.t0 + p.at * kT, keys = min(kT, p.t1 - j0);
   const float scale = 1.f / sqrtf((float)D);
   const long long qs = (long long)a.Hq * D, ks = (long long)a.Hkv * D;
-  load_rows<T, D>(K, static_cast<const T*>(a.k) + (long long)j0 * ks + (long long)hk * D, ks, keys);
-  load_rows<T, D>(V, static_cast<const T*>(a.v) + (long long)j0 * ks + (long long)hk * D, ks, keys);
+  load_rows<D>(K, static_cast<const float*>(a.k) + (long long)j0 * ks + (long long)hk * D, ks, keys);
+  load_rows<D>(V, static_cast<const float*>(a.v) + (long long)j0 * ks + (long long)hk * D, ks, keys);
   float bias[4], db[4] = {};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -252,13 +247,13 @@ __global__ void __launch_bounds__(kThreads) attn_dkv_kernel(const AttnArgs a) {
     for (int i0 = j0; i0 < p.t1; i0 += kT) {
       const int rows = min(kT, p.t1 - i0);
       __syncthreads();
-      load_rows<T, D>(Q, static_cast<const T*>(a.q) + (long long)i0 * qs + (long long)h * D, qs, rows);
-      load_rows<T, D>(O, static_cast<const T*>(a.dout) + (long long)i0 * qs + (long long)h * D, qs, rows);
+      load_rows<D>(Q, static_cast<const float*>(a.q) + (long long)i0 * qs + (long long)h * D, qs, rows);
+      load_rows<D>(O, static_cast<const float*>(a.dout) + (long long)i0 * qs + (long long)h * D, qs, rows);
       if (threadIdx.x < kT) {
         const long long at = (long long)h * a.seqs.total + i0 + threadIdx.x;
         const bool in = (int)threadIdx.x < rows;
         L[threadIdx.x] = in ? a.lse[at] : 0.f;
-        E[threadIdx.x] = in ? a.delta[at] : 0.f;
+        E[threadIdx.x] = in ? a.rows[at] : 0.f;
       }
       __syncthreads();
       float s[4][4] = {}, dp[4][4] = {};
@@ -289,15 +284,15 @@ __global__ void __launch_bounds__(kThreads) attn_dkv_kernel(const AttnArgs a) {
     const long long at = (long long)(j0 + r) * ks + (long long)hk * D;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) {
-      store4(static_cast<T*>(a.dk) + at + 4 * tx + 64 * c, times(dk[j][c], scale));
-      store4(static_cast<T*>(a.dv) + at + 4 * tx + 64 * c, dv[j][c]);
+      store4(static_cast<float*>(a.dk) + at + 4 * tx + 64 * c, times(dk[j][c], scale));
+      store4(static_cast<float*>(a.dv) + at + 4 * tx + 64 * c, dv[j][c]);
     }
-    if (tx == 0 && a.dbias) static_cast<T*>(a.dbias)[(long long)hk * a.seqs.total + j0 + r] = Elt<T>::from_f(b);
+    if (tx == 0 && a.dbias) static_cast<float*>(a.dbias)[(long long)hk * a.seqs.total + j0 + r] = b;
   }
 }
 
 // delta_i = dO_i . out_i, a warp per (token, head)
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnArgs a) {
   const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
@@ -306,14 +301,13 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnArgs a) {
   float d = 0.f;
 #pragma unroll
   for (int c = 2 * lane; c < D; c += 64) {
-    using Raw = typename Pair<T>::Raw;
-    const float2 x = Pair<T>::to_f(*reinterpret_cast<const Raw*>(static_cast<const T*>(a.out) + w * D + c));
-    const float2 y = Pair<T>::to_f(*reinterpret_cast<const Raw*>(static_cast<const T*>(a.dout) + w * D + c));
+    const float2 x = *reinterpret_cast<const float2*>(static_cast<const float*>(a.out) + w * D + c);
+    const float2 y = *reinterpret_cast<const float2*>(static_cast<const float*>(a.dout) + w * D + c);
     d = fmaf(x.x, y.x, fmaf(x.y, y.y, d));
   }
 #pragma unroll
   for (int off = 16; off >= 1; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
-  if (lane == 0) a.delta[(w % a.Hq) * a.seqs.total + w / a.Hq] = d;
+  if (lane == 0) a.rows[(w % a.Hq) * a.seqs.total + w / a.Hq] = d;
 }
 
 template <typename K>
@@ -321,25 +315,25 @@ cudaError_t allow(K* kernel, size_t bytes) {
   return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-template <typename T, int D>
+template <int D>
 cudaError_t attn_f(const AttnArgs& a, cudaStream_t stream) {
   constexpr size_t bytes = (3 * kT * (D + 4) + kT * kW) * 4;
-  cudaError_t e = allow(attn_kernel<T, D>, bytes);
+  cudaError_t e = allow(attn_kernel<D>, bytes);
   if (e != cudaSuccess) return e;
-  attn_kernel<T, D><<<dim3((unsigned)pieces(a.seqs.total, a.seqs.num, kT), a.Hq), kThreads, bytes, stream>>>(a);
+  attn_kernel<D><<<dim3((unsigned)pieces(a.seqs.total, a.seqs.num, kT), a.Hq), kThreads, bytes, stream>>>(a);
   return cudaGetLastError();
 }
 
-template <typename T, int D>
+template <int D>
 cudaError_t attn_b(const AttnArgs& a, cudaStream_t stream) {
   constexpr size_t dq = (4 * kT * (D + 4) + kT * kW) * 4, dkv = (4 * kT * (D + 4) + 2 * kT * kW + 2 * kT) * 4;
-  cudaError_t e = allow(attn_dq_kernel<T, D>, dq);
-  if (e == cudaSuccess) e = allow(attn_dkv_kernel<T, D>, dkv);
+  cudaError_t e = allow(attn_dq_kernel<D>, dq);
+  if (e == cudaSuccess) e = allow(attn_dkv_kernel<D>, dkv);
   if (e != cudaSuccess) return e;
   const unsigned n = (unsigned)pieces(a.seqs.total, a.seqs.num, kT);
-  attn_delta_kernel<T, D><<<(unsigned)(((long long)a.seqs.total * a.Hq + 7) / 8), 256, 0, stream>>>(a);
-  attn_dkv_kernel<T, D><<<dim3(n, a.Hkv), kThreads, dkv, stream>>>(a);
-  attn_dq_kernel<T, D><<<dim3(n, a.Hq), kThreads, dq, stream>>>(a);
+  attn_delta_kernel<D><<<(unsigned)(((long long)a.seqs.total * a.Hq + 7) / 8), 256, 0, stream>>>(a);
+  attn_dkv_kernel<D><<<dim3(n, a.Hkv), kThreads, dkv, stream>>>(a);
+  attn_dq_kernel<D><<<dim3(n, a.Hq), kThreads, dq, stream>>>(a);
   return cudaGetLastError();
 }
 
@@ -497,13 +491,11 @@ cudaError_t loss_b(const LossArgs& a, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t attn_forward_f32(const AttnArgs& a, bool bf16, int D, cudaStream_t stream) {
-  if (bf16) return D == 128 ? attn_f<__nv_bfloat16, 128>(a, stream) : attn_f<__nv_bfloat16, 64>(a, stream);
-  return D == 128 ? attn_f<float, 128>(a, stream) : attn_f<float, 64>(a, stream);
+cudaError_t attn_forward_f32(const AttnArgs& a, int D, cudaStream_t stream) {
+  return D == 128 ? attn_f<128>(a, stream) : attn_f<64>(a, stream);
 }
-cudaError_t attn_backward_f32(const AttnArgs& a, bool bf16, int D, cudaStream_t stream) {
-  if (bf16) return D == 128 ? attn_b<__nv_bfloat16, 128>(a, stream) : attn_b<__nv_bfloat16, 64>(a, stream);
-  return D == 128 ? attn_b<float, 128>(a, stream) : attn_b<float, 64>(a, stream);
+cudaError_t attn_backward_f32(const AttnArgs& a, int D, cudaStream_t stream) {
+  return D == 128 ? attn_b<128>(a, stream) : attn_b<64>(a, stream);
 }
 cudaError_t loss_forward_f32(const LossArgs& a, int* shares, cudaStream_t stream) { return loss_f(a, shares, stream); }
 cudaError_t loss_backward_f32(const LossArgs& a, cudaStream_t stream) { return loss_b(a, stream); }
