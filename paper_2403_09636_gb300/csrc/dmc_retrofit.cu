@@ -23,7 +23,8 @@ cudaError_t loss_backward_bf16(const LossArgs& a, cudaStream_t stream);
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr size_t kControl = 64;  // the fault bits, and from byte 16 the attention kernels' counters, 8 bytes each
+// The fault bits, from byte 128 the attention kernels' counter, from byte 256 the states' turns
+constexpr size_t kControl = 768;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool given16(const void* p) { return p && aligned16(p); }
@@ -60,7 +61,7 @@ int loss_piece(const dmc_retrofit_config* c) {
 }
 
 struct Offsets {
-  size_t error, sums, rows, part_m, part_l, target_logit, dh, grad, total;
+  size_t error, flags, cleared, sums, carry, rows, part_m, part_l, target_logit, dh, grad, total;
   int piece;
 };
 
@@ -68,11 +69,14 @@ Offsets offsets(const dmc_retrofit_config* c) {
   Offsets o = {};
   size_t at = 0;
   const size_t tokens = c->max_tokens;
-  o.error = at; at = align_up(at + kControl);
+  const size_t chunks = has_heads(*c) ? (size_t)pieces(c->max_tokens, c->max_seqs, kStateChunk) * c->num_kv_heads : 0;
+  o.error = at; at += kControl;
+  o.flags = at; at = align_up(at + chunks * 4);
+  o.cleared = at;
   if (has_heads(*c)) {
-    o.sums = at;
-    at = align_up(at + (size_t)pieces(c->max_tokens, c->max_seqs, kStateChunk) * c->num_kv_heads *
-                           (2 * c->head_dim + 4) * 4);
+    const size_t sums = chunks * (2 * c->head_dim + 4) * 4;
+    o.sums = at; at = align_up(at + sums);
+    o.carry = at; at = align_up(at + sums);
     // the backward pass's two numbers per query, padded to tiles of 128 (one in fp32)
     o.rows = at;
     at = align_up(at + (c->dtype == DMC_F32 ? tokens * 4 : (size_t)pieces(c->max_tokens, c->max_seqs, 128) * 1024) *
@@ -153,6 +157,9 @@ dmc::StatesArgs states_args(dmc_retrofit_t h, int32_t num_seqs, const void* q, i
   a.saved = static_cast<float*>(saved);
   a.error = reinterpret_cast<unsigned int*>(h->base + h->at.error);
   a.sums = reinterpret_cast<float*>(h->base + h->at.sums);
+  a.carry = reinterpret_cast<float*>(h->base + h->at.carry);
+  a.flags = reinterpret_cast<unsigned int*>(h->base + h->at.flags);
+  a.turns = reinterpret_cast<unsigned int*>(h->base + h->at.error + 256);
   return a;
 }
 
@@ -168,7 +175,7 @@ dmc::AttnArgs attn_args(dmc_retrofit_t h, int32_t num_seqs, const void* q, const
   a.v = v;
   a.bias = bias;
   a.rows = reinterpret_cast<float*>(h->base + h->at.rows);
-  a.counter = reinterpret_cast<int*>(h->base + h->at.error + 16);
+  a.counter = reinterpret_cast<int*>(h->base + h->at.error + 128);
   a.error = reinterpret_cast<unsigned int*>(h->base + h->at.error);
   return a;
 }
@@ -215,7 +222,7 @@ dmc_status dmc_retrofit_create(const dmc_retrofit_config* cfg, void* arena_dev, 
   h->at = o;
   h->base = static_cast<char*>(arena_dev);
   cudaError_t e = cudaGetDevice(&h->device);
-  if (e == cudaSuccess) e = cudaMemsetAsync(h->base + o.error, 0, dmc::kControl, stream);
+  if (e == cudaSuccess) e = cudaMemsetAsync(h->base + o.error, 0, o.cleared - o.error, stream);
   if (e != cudaSuccess) {
     delete h;
     return DMC_ERR_CUDA;

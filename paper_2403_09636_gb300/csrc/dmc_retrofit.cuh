@@ -96,7 +96,10 @@ struct StatesArgs {
   void* dq;
   long long dq_tok, dq_head;
   void *dk, *dv;
-  float* sums;          // scratch, [piece][Hkv][2 D + 4]
+  // scratch
+  float *sums, *carry;  // [piece][Hkv][2 D + 4]: a piece's own sums; what comes into it (backward)
+  unsigned int* flags;  // [piece][Hkv]: what of these is there, and in which launch
+  unsigned int* turns;  // blocks come, blocks gone, number of the launch
 };
 
 struct AttnArgs {
