@@ -61,7 +61,7 @@ int loss_piece(const dmc_retrofit_config* c) {
 }
 
 struct Offsets {
-  size_t error, flags, cleared, sums, carry, rows, part_m, part_l, target_logit, dh, grad, total;
+  size_t error, sums, carry, cleared, rows, part_m, part_l, target_logit, dh, grad, total;
   int piece;
 };
 
@@ -70,13 +70,14 @@ Offsets offsets(const dmc_retrofit_config* c) {
   size_t at = 0;
   const size_t tokens = c->max_tokens;
   const size_t chunks = has_heads(*c) ? (size_t)pieces(c->max_tokens, c->max_seqs, kStateChunk) * c->num_kv_heads : 0;
-  o.error = at; at += kControl;
-  o.flags = at; at = align_up(at + chunks * 4);
-  o.cleared = at;
+  o.error = at; at = align_up(at + kControl);
   if (has_heads(*c)) {
-    const size_t sums = chunks * (2 * c->head_dim + 4) * 4;
+    const size_t sums = (size_t)pieces(c->max_tokens, c->max_seqs, kStateChunk) * c->num_kv_heads * 2 * (c->head_dim + 2) * 8;
     o.sums = at; at = align_up(at + sums);
     o.carry = at; at = align_up(at + sums);
+  }
+  o.cleared = at;
+  if (has_heads(*c)) {
     // the backward pass's two numbers per query, padded to tiles of 128 (one in fp32)
     o.rows = at;
     at = align_up(at + (c->dtype == DMC_F32 ? tokens * 4 : (size_t)pieces(c->max_tokens, c->max_seqs, 128) * 1024) *
@@ -156,9 +157,8 @@ dmc::StatesArgs states_args(dmc_retrofit_t h, int32_t num_seqs, const void* q, i
   a.temperature = temperature;
   a.saved = static_cast<float*>(saved);
   a.error = reinterpret_cast<unsigned int*>(h->base + h->at.error);
-  a.sums = reinterpret_cast<float*>(h->base + h->at.sums);
-  a.carry = reinterpret_cast<float*>(h->base + h->at.carry);
-  a.flags = reinterpret_cast<unsigned int*>(h->base + h->at.flags);
+  a.sums = reinterpret_cast<uint64_t*>(h->base + h->at.sums);
+  a.carry = reinterpret_cast<uint64_t*>(h->base + h->at.carry);
   a.turns = reinterpret_cast<unsigned int*>(h->base + h->at.error + 256);
   return a;
 }

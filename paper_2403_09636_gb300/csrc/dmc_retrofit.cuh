@@ -97,9 +97,8 @@ struct StatesArgs {
   long long dq_tok, dq_head;
   void *dk, *dv;
   // scratch
-  float *sums, *carry;  // [piece][Hkv][2 D + 4]: a piece's own sums; what comes into it (backward)
-  unsigned int* flags;  // [piece][Hkv]: what of these is there, and in which launch
-  unsigned int* turns;  // blocks come, blocks gone, number of the launch
+  uint64_t *sums, *carry;  // [piece][Hkv][2][D + 2]: a piece's own sums; what comes into it (with their launch)
+  unsigned int* turns;     // come, gone, number of the launch
 };
 
 struct AttnArgs {

@@ -12,17 +12,22 @@
 // chunk's start, which the forward pass saves in fp32: from the rounded states the
 // difference that dalpha stands for would be lost where z is much larger than omega.
 //
-// A sequence is cut into chunks of 32 tokens, a block per chunk and head with two
-// neighbouring elements of k or v per thread, which reads its tokens once: it publishes the
-// chunk's own sums and the product of its alphas, takes what comes in from the chunks before
-// (after) it, and writes. What comes in follows the chain
+// A sequence is cut into chunks of 32 tokens, a warp per chunk, head and tensor (k or v): a token
+// per lane for the gates, D / 32 neighbouring elements per lane for the rows, which each lane
+// copies for itself to shared memory, once. A warp publishes the chunk's own sums and the
+// product of its alphas, takes what comes in from the chunks before (after) it, and writes. What
+// comes in follows the chain
 //   in_{c+1} = own_c + prod_c in_c
 // from the nearest chunk whose own `in` is known or whose product is 0: decisions that are
 // nearly binary make the product of 32 alphas underflow, so that mostly one chunk is looked
 // at. The chain is always evaluated in this order, so results do not depend on how far others
-// have come. Blocks take their chunks from a counter, so that those a block waits for
-// have started; they publish before they wait. Flags carry the launch's number, kept in
-// device memory, so that nothing has to be cleared between launches (or replays of a graph).
+// have come. Chunks are taken from a counter, so that those a warp waits for have
+// started; they publish before they wait. Every published number carries the number of the launch
+// in the same 8 bytes: no fence or flag stands between it and its reader (a fence waited for
+// the warp's loads and stores, 4 us of the 18 that a chunk took), and nothing has to be cleared
+// between launches or replays of a graph.
+#include <type_traits>
+
 #include "dmc_retrofit.cuh"
 
 namespace dmc {
@@ -93,439 +98,500 @@ __device__ __forceinline__ float scan_z(float alpha, float omega, float before) 
   return fmaf(a, before, z);
 }
 
-// Of 32 values per lane: lane t gets the sum of all lanes' v[t].
-__device__ __forceinline__ float transposed_sum(float* v) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int off = 16; off >= 1; off >>= 1) {
-    const bool up = lane & off;
-#pragma unroll
-    for (int i = 0; i < off; ++i) {
-      const float send = up ? v[i] : v[i + off], keep = up ? v[i + off] : v[i];
-      v[i] = keep + __shfl_xor_sync(0xffffffffu, send, off);
+// ---- a lane's elements of a row
+
+template <typename T, int D>
+struct Row {
+  static constexpr int kE = D / 32, kP = kE / 2;  // elements and pairs per lane
+  static constexpr int kBytes = kE * (int)sizeof(T);
+  using Word = typename std::conditional<kBytes == 4, uint32_t, typename std::conditional<kBytes == 8, uint2, uint4>::type>::type;
+
+  // asynchronously, n rows `stride` elements apart
+  static __device__ __forceinline__ void copy(T* to, const T* from, long long stride, int n) {
+#pragma unroll 4
+    for (int t = 0; t < n; ++t) {
+      const uint32_t dst = smem_u32(to + t * D);
+      const T* src = from + t * stride;
+      if (kBytes == 16)
+        cp_async16(dst, src);
+      else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(kBytes) : "memory");
     }
   }
-  return v[0];
-}
-
-template <int D>
-struct StatesShared {
-  float alpha[kC], omega[kC], rz[kC];
-  float prod[kC];       // product of the alphas up to the token
-  float dot[3][D / 32][kC];
-  float e1[kC];         // second element of dk
-  float zin;            // z (Z) that comes in
-  int index, far;
-  bool known;
-  unsigned int launch;
+  static __device__ __forceinline__ void zero(T* at) { *reinterpret_cast<Word*>(at) = Word{}; }
+  static __device__ __forceinline__ void read(const T* at, float2 (&f)[kP]) {
+    const Word u = *reinterpret_cast<const Word*>(at);
+    const typename Pair<T>::Raw* r = reinterpret_cast<const typename Pair<T>::Raw*>(&u);
+#pragma unroll
+    for (int i = 0; i < kP; ++i) f[i] = Pair<T>::to_f(r[i]);
+  }
+  static __device__ __forceinline__ void write(T* at, const float2 (&f)[kP]) {
+    Word u;
+    typename Pair<T>::Raw* r = reinterpret_cast<typename Pair<T>::Raw*>(&u);
+#pragma unroll
+    for (int i = 0; i < kP; ++i) r[i] = Pair<T>::from_f(f[i]);
+    *reinterpret_cast<Word*>(at) = u;
+  }
 };
 
-// A chunk's rows of two tensors in shared memory: [tensor][token][D]
-template <typename T, int D>
-__device__ __forceinline__ void load_chunk(char* to, const void* k, const void* v, long long row, long long stride, int n) {
-  constexpr int kRow = D * sizeof(T), kPieces = kRow / 16;
-  for (int i = threadIdx.x; i < 2 * n * kPieces; i += D) {
-    const int c = i % kPieces, t = i / kPieces % n, w = i / (kPieces * n);
-    cp_async16(smem_u32(to) + (w * kC + t) * kRow + c * 16,
-               static_cast<const char*>(w ? v : k) + (row + t * stride) * sizeof(T) + c * 16);
-  }
-}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
-// ---- the order of blocks
+// ---- the order of warps
 
-// words of StatesArgs::turns, each in a line of its own (all blocks add to the first two)
+// words of StatesArgs::turns, each in a line of its own (everybody adds to the first two)
 constexpr int kCome = 0, kGone = 32, kLaunch = 64;
 
-// The block's chunk and head, in the order in which blocks come.
-template <int D>
-__device__ __forceinline__ int take_turn(const StatesArgs& a, StatesShared<D>& sh) {
-  if (threadIdx.x == 0) {
-    sh.index = (int)atomicAdd(&a.turns[kCome], 1u);
-    sh.launch = *reinterpret_cast<volatile unsigned int*>(&a.turns[kLaunch]);
-  }
-  __syncthreads();
-  return sh.index;
+struct Turn {
+  int index;         // in the order in which they come
+  unsigned int tag;  // the launch
+};
+// one thread
+__device__ __forceinline__ Turn take_turn(const StatesArgs& a) {
+  Turn t;
+  t.index = (int)atomicAdd(&a.turns[kCome], 1u);
+  t.tag = *reinterpret_cast<volatile unsigned int*>(&a.turns[kLaunch]) + 1;
+  return t;
 }
-// Thread 0, when the block needs no other any more: how many have come so far before it.
-__device__ __forceinline__ unsigned int gone(const StatesArgs& a) { return atomicAdd(&a.turns[kGone], 1u); }
-// The last block prepares the next launch.
-__device__ __forceinline__ void leave(const StatesArgs& a, unsigned int before, unsigned int launch) {
-  if (before != gridDim.x - 1) return;
+// One thread, when its block has read all it needs from others; the last one prepares the next launch.
+__device__ __forceinline__ void leave(const StatesArgs& a, const Turn& t) {
+  if (atomicAdd(&a.turns[kGone], 1u) != gridDim.x - 1) return;
   a.turns[kCome] = a.turns[kGone] = 0;
-  a.turns[kLaunch] = launch + 1;
+  a.turns[kLaunch] = t.tag;
 }
 
-constexpr unsigned int kOwn = 1, kIn = 2;  // published: the chunk's own sums; what comes into it, too
+// ---- published numbers: {value, launch}
 
-// By the whole block, after its values have been written.
-__device__ __forceinline__ void publish(unsigned int* flag, unsigned int launch, unsigned int what) {
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    __threadfence();
-    asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(flag), "r"(launch << 2 | what) : "memory");
-  }
+__device__ __forceinline__ uint64_t tagged(float x, unsigned int tag) { return (uint64_t)tag << 32 | __float_as_uint(x); }
+
+template <int kE>
+__device__ __forceinline__ void publish(uint64_t* row, const float2* f, unsigned int tag) {
+  uint64_t* at = row + (threadIdx.x & 31) * kE;
+#pragma unroll
+  for (int i = 0; i < kE / 2; ++i)
+    asm volatile("st.relaxed.gpu.global.v2.b64 [%0], {%1, %2};" ::"l"(at + 2 * i), "l"(tagged(f[i].x, tag)),
+                 "l"(tagged(f[i].y, tag))
+                 : "memory");
 }
-// What a chunk has published, once there is something. 0: waited too long, or a fault has been
-// found (a wait that gave up, or cu_seqlens that do not fit, where a chunk may have no neighbour).
-__device__ __forceinline__ unsigned int published(const unsigned int* flag, unsigned int launch, unsigned int* error) {
+// z and the product of the chunk's alphas, by one lane
+template <int D>
+__device__ __forceinline__ void publish_zp(uint64_t* row, float z, float prod, unsigned int tag) {
+  asm volatile("st.relaxed.gpu.global.v2.b64 [%0], {%1, %2};" ::"l"(row + D), "l"(tagged(z, tag)), "l"(tagged(prod, tag))
+               : "memory");
+}
+// The lane's elements of a row, its z and product; whether all of the warp's were there.
+template <int D>
+__device__ __forceinline__ bool look(const uint64_t* row, float2 (&f)[D / 64], float2& zp, unsigned int tag) {
+  constexpr int kE = D / 32;
+  bool there = true;
+  auto two = [&](const uint64_t* at) {
+    uint64_t u, v;
+    asm volatile("ld.relaxed.gpu.global.v2.b64 {%0, %1}, [%2];" : "=l"(u), "=l"(v) : "l"(at) : "memory");
+    there &= (unsigned int)(u >> 32) == tag && (unsigned int)(v >> 32) == tag;
+    return make_float2(__uint_as_float((unsigned int)u), __uint_as_float((unsigned int)v));
+  };
+#pragma unroll
+  for (int i = 0; i < kE / 2; ++i) f[i] = two(row + (threadIdx.x & 31) * kE + 2 * i);
+  zp = two(row + D);
+  return __all_sync(0xffffffffu, there);
+}
+// The same, once they are there. False: waited too long, or a fault has been found (a wait that
+// gave up, or cu_seqlens that do not fit, where a chunk may have no neighbour).
+template <int D>
+__device__ __forceinline__ bool await(const uint64_t* row, float2 (&f)[D / 64], float2& zp, unsigned int tag,
+                                      unsigned int* error) {
   uint64_t since = 0;
   for (int tries = 0;; ++tries) {
-    unsigned int f;
-    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(f) : "l"(flag) : "memory");
-    if (f >> 2 == (launch & 0x3fffffffu) && (f & 3)) return f & 3;
+    if (look<D>(row, f, zp, tag)) return true;
     if (tries < 64) continue;
     __nanosleep(500);
-    if (*reinterpret_cast<volatile unsigned int*>(error)) return 0;
+    bool give_up = *reinterpret_cast<volatile unsigned int*>(error) != 0;
     const uint64_t t = globaltimer_ns();
     if (since == 0) since = t;
     if (t - since > kWaitLimitNs) {
       atomicOr(error, DMC_FAULT_WAIT_TIMEOUT);
-      return 0;
+      give_up = true;
     }
+    if (__any_sync(0xffffffffu, give_up)) return false;
   }
 }
 
-// What comes into a chunk from its neighbours `dir` (-1: before it, 1: after it), of which
-// there are `n`: the thread's pair of sums, and z (Z) in `zin`. own, in: the neighbours' rows.
+// What comes into a chunk from its n neighbours on one side, `step` apart: the lane's sums x,
+// and z (Z). own, in: this chunk's rows.
 template <int D>
-__device__ __forceinline__ float2 come_in(const StatesArgs& a, StatesShared<D>& sh, const float* own, const float* in,
-                                          int chunk, int h, int n, int dir, unsigned int launch, float& zin) {
-  const int tid = threadIdx.x;
-  const long long stride = (long long)a.Hkv * sums_row(D);
-  own += ((long long)chunk * a.Hkv + h) * sums_row(D);
-  in += ((long long)chunk * a.Hkv + h) * sums_row(D);
-  if (tid == 0) {  // how many chunks to look at, and whether what came into the last is known
-    int far = 0;
-    unsigned int f = kOwn;
-    while (far < n && f == kOwn) {
-      ++far;
-      f = published(a.flags + (long long)(chunk + dir * far) * a.Hkv + h, launch, a.error);
-      if (__ldcg(own + dir * far * stride + 2 * D + 1) == 0.f) f = 0;
+__device__ __forceinline__ float come_in(const uint64_t* own, const uint64_t* in, int n, long long step, unsigned int tag,
+                                         unsigned int* error, float2 (&x)[D / 64]) {
+  constexpr int kP = D / 64;
+  float2 o[kP], zp;
+  float z;
+  int far = 1;  // chunks to look at
+  for (;; ++far) {
+    if (!await<D>(own + far * step, x, zp, tag, error)) break;
+    z = zp.x;
+    if (zp.y == 0.f || far == n) break;
+    float2 zi;
+    if (look<D>(in + far * step, o, zi, tag)) {
+#pragma unroll
+      for (int i = 0; i < kP; ++i) x[i] = fma2(both(zp.y), o[i], x[i]);
+      z = fmaf(zp.y, zi.x, z);
+      break;
     }
-    sh.far = far;
-    sh.known = f == kIn;
   }
-  __syncthreads();
-  int far = sh.far;
-  const bool known = sh.known;
-  const float* row = own + dir * far * stride;
-  float2 x = make_float2(0.f, 0.f), o = __ldcg(reinterpret_cast<const float2*>(row) + tid);
-  float2 zp = __ldcg(reinterpret_cast<const float2*>(row + 2 * D));  // z, product
-  zin = 0.f;
-  if (known) {
-    x = __ldcg(reinterpret_cast<const float2*>(in + dir * far * stride) + tid);
-    zin = __ldcg(in + dir * far * stride + 2 * D);
+#pragma unroll 1
+  for (--far; far > 0; --far) {
+    look<D>(own + far * step, o, zp, tag);
+#pragma unroll
+    for (int i = 0; i < kP; ++i) x[i] = fma2(both(zp.y), x[i], o[i]);
+    z = fmaf(zp.y, z, zp.x);
   }
-  while (true) {
-    x.x = fmaf(zp.y, x.x, o.x);
-    x.y = fmaf(zp.y, x.y, o.y);
-    zin = fmaf(zp.y, zin, zp.x);
-    if (--far == 0) return x;
-    row = own + dir * far * stride;
-    o = __ldcg(reinterpret_cast<const float2*>(row) + tid);
-    zp = __ldcg(reinterpret_cast<const float2*>(row + 2 * D));
-  }
+  return z;
+}
+
+template <int D>
+__device__ __forceinline__ long long row_of(const StatesArgs& a, int chunk, int h, int which) {
+  return (((long long)chunk * a.Hkv + h) * 2 + which) * (D + 2);
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(D) states_kernel(const StatesArgs a) {
-  using P = Pair<T>;
-  using Raw = typename P::Raw;
-  __shared__ StatesShared<D> sh;
-  __shared__ __align__(16) T rows[2 * kC * D];
-  const int tid = threadIdx.x, lane = tid & 31;
-  const int index = take_turn(a, sh), h = index % a.Hkv, chunk = index / a.Hkv;
-  const unsigned int launch = sh.launch;
-  if (index == 0) check_seqs(a.seqs, a.error);
+__global__ void __launch_bounds__(32) states_kernel(const StatesArgs a) {
+  using R = Row<T, D>;
+  __shared__ __align__(16) T rows[kC * D];
+  __shared__ float4 coef[kC];  // alpha, omega, 1 / z
+  __shared__ float weight[kC]; // omega times the product of the alphas after it
+  const int lane = threadIdx.x;
+  Turn turn;
+  if (lane == 0) turn = take_turn(a);
+  turn.index = __shfl_sync(0xffffffffu, turn.index, 0);
+  turn.tag = __shfl_sync(0xffffffffu, turn.tag, 0);
+  const int which = turn.index & 1, h = (turn.index >> 1) % a.Hkv, chunk = (turn.index >> 1) / a.Hkv;  // which: 0 k, 1 v
+  if (turn.index == 0) check_seqs(a.seqs, a.error);
   const Piece p = find_piece(a.seqs, kC, chunk);
   if (!p.ok) {
-    if (tid == 0) leave(a, gone(a), launch);
+    if (lane == 0) leave(a, turn);
     return;
   }
-  const int tok0 = p.t0 + p.at * kC, n = min(kC, p.t1 - tok0);
-  const bool in = lane < n, goes_on = tok0 + kC < p.t1;
-  GateIn gi;
-  if (tid < 32) gi = gate_in<T, D>(a, h, tok0 + lane, in);
-  const long long row0 = ((long long)tok0 * a.Hkv + h) * D, step = (long long)a.Hkv * D;
-  load_chunk<T, D>(reinterpret_cast<char*>(rows), a.k, a.v, row0, step, n);
+  const int tok0 = p.t0 + p.at * kC, n = min(kC, p.t1 - tok0), tok = tok0 + lane;
+  const bool in_chunk = lane < n, goes_on = tok0 + kC < p.t1;
+  const GateIn gi = gate_in<T, D>(a, h, tok, in_chunk);
+  const long long step = (long long)a.Hkv * D, at = ((long long)tok0 * a.Hkv + h) * D + lane * R::kE;
+  T* mine = rows + lane * R::kE;
+  R::copy(mine, static_cast<const T*>(which ? a.v : a.k) + at, step, n);
   cp_async_commit();
-  float* own = a.sums + ((long long)chunk * a.Hkv + h) * sums_row(D);
-  Gate g;
-  float prod = 1.f;
-  if (tid < 32) {
-    g = gate_of(a, gi, in, tok0 + lane == p.t0);
-    sh.alpha[lane] = g.alpha;
-    sh.omega[lane] = g.omega;
-    const float z = scan_z(g.alpha, g.omega, 0.f);
-    prod = g.alpha;
+  const Gate g = gate_of(a, gi, in_chunk, tok == p.t0);
+  const long long row = row_of<D>(a, chunk, h, which), row_step = row_of<D>(a, 1, 0, 0);
+  float after = g.alpha;  // product of the alphas from the token on
 #pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) prod *= __shfl_xor_sync(0xffffffffu, prod, off);
-    if (lane == 31) *reinterpret_cast<float2*>(own + 2 * D) = make_float2(z, prod);
-    if (lane == 0) sh.prod[0] = prod;
+  for (int off = 1; off < 32; off <<= 1) {
+    const float o = __shfl_down_sync(0xffffffffu, after, off);
+    if (lane + off < 32) after *= o;
+  }
+  const float prod = __shfl_sync(0xffffffffu, after, 0);
+  const bool gate_lane = which == 0 && lane == 0;
+  auto value = [&](int t, float2 (&x)[R::kP]) {
+    R::read(mine + t * D, x);
+    if (gate_lane) x[0].x = 0.f;  // k's first component
+  };
+  if (goes_on) {
+    const float rest = __shfl_down_sync(0xffffffffu, after, 1);
+    const float w = g.omega * (lane == 31 ? 1.f : rest);
+    weight[lane] = w;
+    float z = w;
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) z += __shfl_xor_sync(0xffffffffu, z, off);
+    if (lane == 0) publish_zp<D>(a.sums + row, z, prod, turn.tag);
+    __syncwarp();
   }
   cp_async_wait<0>();
-  __syncthreads();
-  const int which = tid / (D / 2), e = tid % (D / 2) * 2;
-  const bool gate_pair = which == 0 && e == 0;
-  auto value = [&](int t) {
-    float2 x = P::to_f(*reinterpret_cast<const Raw*>(rows + (which * kC + t) * D + e));
-    if (gate_pair) x.x = 0.f;
-    return x;
-  };
-  unsigned int* flag = a.flags + (long long)chunk * a.Hkv + h;
+  float2 sum[R::kP];
+#pragma unroll
+  for (int i = 0; i < R::kP; ++i) sum[i] = both(0.f);
   if (goes_on) {
-    float2 sum = make_float2(0.f, 0.f);
 #pragma unroll 8
     for (int t = 0; t < kC; ++t) {
-      const float2 x = value(t);
-      const float al = sh.alpha[t], om = sh.omega[t];
-      sum.x = fmaf(al, sum.x, om * x.x);
-      sum.y = fmaf(al, sum.y, om * x.y);
+      float2 x[R::kP];
+      value(t, x);
+      const float2 w = both(weight[t]);
+#pragma unroll
+      for (int i = 0; i < R::kP; ++i) sum[i] = fma2(w, x[i], sum[i]);
     }
-    reinterpret_cast<float2*>(own)[tid] = sum;
-    publish(flag, launch, kOwn);
+    publish<R::kE>(a.sums + row, sum, turn.tag);
   }
-  float2 sum = make_float2(0.f, 0.f);
+  float zin = 0.f;
+#pragma unroll
+  for (int i = 0; i < R::kP; ++i) sum[i] = both(0.f);
   if (p.at > 0) {
-    float zin;
-    sum = come_in<D>(a, sh, a.sums, a.saved, chunk, h, p.at, -1, launch, zin);
-    float* saved = a.saved + ((long long)chunk * a.Hkv + h) * sums_row(D);
-    reinterpret_cast<float2*>(saved)[tid] = sum;
-    if (tid == 0) {
-      saved[2 * D] = zin;
-      sh.zin = zin;
+    zin = come_in<D>(a.sums + row, a.carry + row, p.at, -row_step, turn.tag, a.error, sum);
+    if (goes_on && prod != 0.f) {  // (with a product of 0 nobody asks for it)
+      publish<R::kE>(a.carry + row, sum, turn.tag);
+      if (lane == 0) publish_zp<D>(a.carry + row, zin, 0.f, turn.tag);
     }
-    // (with a product of 0 nobody asks for what came in)
-    if (goes_on && sh.prod[0] != 0.f)
-      publish(flag, launch, kIn);
-    else
-      __syncthreads();
+    float* saved = a.saved + ((long long)chunk * a.Hkv + h) * sums_row(D);
+#pragma unroll
+    for (int i = 0; i < R::kP; ++i) *reinterpret_cast<float2*>(saved + which * D + lane * R::kE + 2 * i) = sum[i];
+    if (gate_lane) saved[2 * D] = zin;
   }
-  if (tid < 32) sh.rz[lane] = 1.f / scan_z(g.alpha, g.omega, p.at > 0 ? sh.zin : 0.f);
-  __syncthreads();
-  unsigned int before = 0;
-  if (tid == 0) before = gone(a);
-  T* dst = static_cast<T*>(which ? a.vt : a.kt) + row0 + e;
+  if (lane == 0) leave(a, turn);
+  coef[lane] = make_float4(g.alpha, g.omega, 1.f / scan_z(g.alpha, g.omega, zin), 0.f);
+  __syncwarp();
+  T* dst = static_cast<T*>(which ? a.vt : a.kt) + at;
 #pragma unroll 8
   for (int t = 0; t < n; ++t) {
-    const float2 x = value(t);
-    const float al = sh.alpha[t], om = sh.omega[t], rz = sh.rz[t];
-    sum.x = fmaf(al, sum.x, om * x.x);
-    sum.y = fmaf(al, sum.y, om * x.y);
-    *reinterpret_cast<Raw*>(dst + t * step) = P::from_f(make_float2(sum.x * rz, sum.y * rz));
+    float2 x[R::kP], y[R::kP];
+    value(t, x);
+    const float4 c = coef[t];
+#pragma unroll
+    for (int i = 0; i < R::kP; ++i) {
+      sum[i] = fma2(both(c.x), sum[i], mul2(both(c.y), x[i]));
+      y[i] = mul2(both(c.z), sum[i]);
+    }
+    R::write(dst + t * step, y);
   }
-  if (tid < 32 && in) {
-    const int tok = tok0 + lane;
+  if (in_chunk && which == 0) {
     const long long i = (long long)h * a.seqs.total + tok;
     a.alpha[i] = g.alpha;
     if (tok > p.t0) a.bias[i - 1] = g.log_rest;
     if (tok == p.t1 - 1) a.bias[i] = 0.f;
   }
-  if (tid == 0) leave(a, before, launch);
 }
 
-// Chunks from the last to the first. A chunk passes on the sum over t of (its alphas up
-// to t) u_t, and w_t alike.
+// Chunks from the last to the first, a block of a warp for k and a warp for v per chunk and
+// head. A chunk passes on the sum over t of (its alphas up to t) u_t, and w_t alike. Dots over all
+// elements go through shared memory: 16 partial sums per token, then a token per lane.
 template <typename T, int D>
-__global__ void __launch_bounds__(D) states_backward_kernel(const StatesArgs a) {
-  using P = Pair<T>;
-  using Raw = typename P::Raw;
+struct BackShared {
+  T rows[2][kC * D], grads[2][kC * D];
+  float4 coef[2][kC];         // alpha, omega, 1 / z, product of the alphas up to it over z
+  float dots[2][kC][17];
+  float other[2][kC];         // v's share of a dot
+  float first[kC];            // second element of dk
+  Turn turn;
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a) {
+  using R = Row<T, D>;
   constexpr int kH = kC / 2;  // tokens whose sums are held at a time
-  __shared__ StatesShared<D> sh;
-  extern __shared__ __align__(16) char chunk_rows[];  // k, v, then dk~, dv~
-  T* rows = reinterpret_cast<T*>(chunk_rows);
-  T* grads = rows + 2 * kC * D;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int index = take_turn(a, sh), chunks = gridDim.x / a.Hkv;
-  const int h = index % a.Hkv, chunk = chunks - 1 - index / a.Hkv;
-  const unsigned int launch = sh.launch;
-  if (index == 0) check_seqs(a.seqs, a.error);
+  extern __shared__ __align__(16) char raw[];
+  BackShared<T, D>& sh = *reinterpret_cast<BackShared<T, D>*>(raw);
+  const int lane = threadIdx.x & 31, which = threadIdx.x >> 5;
+  if (threadIdx.x == 0) sh.turn = take_turn(a);
+  __syncthreads();
+  const Turn turn = sh.turn;
+  const int chunks = gridDim.x / a.Hkv, h = turn.index % a.Hkv, chunk = chunks - 1 - turn.index / a.Hkv;
+  if (turn.index == 0) check_seqs(a.seqs, a.error);
   const Piece p = find_piece(a.seqs, kC, chunk);
   if (!p.ok) {
-    if (tid == 0) leave(a, gone(a), launch);
+    if (threadIdx.x == 0) leave(a, turn);
     return;
   }
   const int tok0 = p.t0 + p.at * kC, n = min(kC, p.t1 - tok0), tok = tok0 + lane;
   const int after = (p.t1 - p.t0 + kC - 1) / kC - 1 - p.at;  // chunks after this one
   const bool in_chunk = lane < n;
-  GateIn gi;
-  if (tid < 32) gi = gate_in<T, D>(a, h, tok, in_chunk);
-  const long long row0 = ((long long)tok0 * a.Hkv + h) * D, step = (long long)a.Hkv * D;
-  load_chunk<T, D>(reinterpret_cast<char*>(rows), a.k, a.v, row0, step, n);
-  load_chunk<T, D>(reinterpret_cast<char*>(grads), a.dkt, a.dvt, row0, step, n);
+  const GateIn gi = gate_in<T, D>(a, h, tok, in_chunk);
+  const long long step = (long long)a.Hkv * D, at = ((long long)tok0 * a.Hkv + h) * D + lane * R::kE;
+  T *mine = sh.rows[which] + lane * R::kE, *grads = sh.grads[which] + lane * R::kE;
+  R::copy(mine, static_cast<const T*>(which ? a.v : a.k) + at, step, n);
+  R::copy(grads, static_cast<const T*>(which ? a.dvt : a.dkt) + at, step, n);
   cp_async_commit();
-  const float* saved = a.saved + ((long long)chunk * a.Hkv + h) * sums_row(D);
-  float* own = a.sums + ((long long)chunk * a.Hkv + h) * sums_row(D);
-  float2 sum0 = make_float2(0.f, 0.f);
-  if (p.at > 0) sum0 = reinterpret_cast<const float2*>(saved)[tid];
-  const float zbefore0 = p.at > 0 ? saved[2 * D] : 0.f;
-  Gate g;
-  float z = 0.f, prod = 0.f, dbias = 0.f, dalpha_out = 0.f;
-  if (tid < 32) {
-    if (in_chunk && tok > p.t0) {
-      const long long i = (long long)h * a.seqs.total + tok;
-      dbias = element<T>(a.dbias, i - 1);
-      if (a.dalpha) dalpha_out = a.dalpha[i];
-    }
-    g = gate_of(a, gi, in_chunk, tok == p.t0);
-    z = scan_z(g.alpha, g.omega, zbefore0);
-    prod = g.alpha;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const float o = __shfl_up_sync(0xffffffffu, prod, off);
-      if (lane >= off) prod *= o;
-    }
-    sh.alpha[lane] = g.alpha;
-    sh.omega[lane] = g.omega;
-    sh.rz[lane] = 1.f / z;
-    sh.prod[lane] = prod;
-  }
   // tokens from n on: zeros, and alpha 1, so that they change nothing
-  for (int i = tid; i < 4 * (kC - n) * (D / 2); i += D) {
-    const int w = i / ((kC - n) * (D / 2)), x = i % ((kC - n) * (D / 2));
-    reinterpret_cast<Raw*>(rows + (w * kC + n) * D)[x] = P::from_f(make_float2(0.f, 0.f));
+  for (int t = n; t < kC; ++t) {
+    R::zero(mine + t * D);
+    R::zero(grads + t * D);
   }
-  cp_async_wait<0>();
-  __syncthreads();
-  const int which = tid / (D / 2), e = tid % (D / 2) * 2;
-  const bool gate_pair = which == 0 && e == 0;
-  auto pair = [&](const T* of, int t) {
-    float2 x = P::to_f(*reinterpret_cast<const Raw*>(of + (which * kC + t) * D + e));
-    if (gate_pair) x.x = 0.f;
+  const float* saved = a.saved + ((long long)chunk * a.Hkv + h) * sums_row(D);
+  float2 sum0[R::kP], middle[R::kP];  // the sums before the chunk, before its second half
+#pragma unroll
+  for (int i = 0; i < R::kP; ++i) sum0[i] = both(0.f);
+  float zbefore0 = 0.f, dbias = 0.f, dalpha = 0.f;
+  if (p.at > 0) {
+#pragma unroll
+    for (int i = 0; i < R::kP; ++i) sum0[i] = *reinterpret_cast<const float2*>(saved + which * D + lane * R::kE + 2 * i);
+    zbefore0 = saved[2 * D];
+  }
+  if (which == 0 && in_chunk && tok > p.t0) {
+    const long long i = (long long)h * a.seqs.total + tok;
+    dbias = element<T>(a.dbias, i - 1);
+    if (a.dalpha) dalpha = a.dalpha[i];
+  }
+  const Gate g = gate_of(a, gi, in_chunk, tok == p.t0);
+  const float z = scan_z(g.alpha, g.omega, zbefore0), rz = 1.f / z;
+  float prod = g.alpha;  // of the alphas up to the token
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const float o = __shfl_up_sync(0xffffffffu, prod, off);
+    if (lane >= off) prod *= o;
+  }
+  const float prod_all = __shfl_sync(0xffffffffu, prod, 31);
+  const float4* coef = sh.coef[which];
+  sh.coef[which][lane] = make_float4(g.alpha, g.omega, rz, prod * rz);
+  const bool gate_lane = threadIdx.x == 0;
+  auto value = [&](const T* of, int t, float2 (&x)[R::kP]) {
+    R::read(of + t * D, x);
+    if (gate_lane) x[0].x = 0.f;  // k's first component
+  };
+  // a token's dot: 16 partial sums
+  auto put = [&](int t, float2 d) {
+    float x = d.x + d.y;
+    x += __shfl_xor_sync(0xffffffffu, x, 16);
+    if (lane < 16) sh.dots[which][t][lane] = x;
+  };
+  auto take = [&]() {  // the lane's token's, over the warp's elements
+    __syncwarp();
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x += sh.dots[which][lane][i];
+    __syncwarp();
     return x;
   };
+  cp_async_wait<0>();
+  __syncwarp();
+  const long long row = row_of<D>(a, chunk, h, which), row_step = row_of<D>(a, 1, 0, 0);
   // forward over the chunk: the sums, g . A, and what the chunk passes on
-  float2 middle = sum0;  // the sums before the second half
   {
-    float2 pass = make_float2(0.f, 0.f), sum = sum0;
-    float dot[kC];
+    float2 sum[R::kP], pass[R::kP];
 #pragma unroll
-    for (int t = 0; t < kC; ++t) {
-      const float2 x = pair(rows, t), gr = pair(grads, t);
-      const float al = sh.alpha[t], om = sh.omega[t], w = sh.prod[t] * sh.rz[t];
-      if (t == kH) middle = sum;
-      sum.x = fmaf(al, sum.x, om * x.x);
-      sum.y = fmaf(al, sum.y, om * x.y);
-      dot[t] = fmaf(gr.x, sum.x, gr.y * sum.y);
-      pass.x = fmaf(w, gr.x, pass.x);
-      pass.y = fmaf(w, gr.y, pass.y);
+    for (int i = 0; i < R::kP; ++i) {
+      sum[i] = sum0[i];
+      pass[i] = both(0.f);
     }
-    if (p.at > 0) reinterpret_cast<float2*>(own)[tid] = pass;
-    sh.dot[0][warp][lane] = transposed_sum(dot);
-  }
-  __syncthreads();
-  float zeta = 0.f;
-  if (tid < 32) {
-    float d = 0.f;
+#pragma unroll 8
+    for (int t = 0; t < kC; ++t) {
+      float2 x[R::kP], gr[R::kP], d = both(0.f);
+      value(mine, t, x);
+      value(grads, t, gr);
+      const float4 c = coef[t];
+      if (t == kH)
 #pragma unroll
-    for (int w = 0; w < D / 32; ++w) d += sh.dot[0][w][lane];
-    const float rz = sh.rz[lane];
-    zeta = in_chunk ? -d * rz * rz : 0.f;
+        for (int i = 0; i < R::kP; ++i) middle[i] = sum[i];
+#pragma unroll
+      for (int i = 0; i < R::kP; ++i) {
+        sum[i] = fma2(both(c.x), sum[i], mul2(both(c.y), x[i]));
+        d = fma2(gr[i], sum[i], d);
+        pass[i] = fma2(both(c.w), gr[i], pass[i]);
+      }
+      put(t, d);
+    }
+    if (p.at > 0) publish<R::kE>(a.sums + row, pass, turn.tag);
+  }
+  float zeta = take();
+  if (which) sh.other[0][lane] = zeta;
+  __syncthreads();
+  zeta = in_chunk ? -(zeta + sh.other[0][lane]) * rz * rz : 0.f;  // (of use to the first warp)
+  if (p.at > 0) {
     float s = zeta * prod;
 #pragma unroll
     for (int off = 16; off >= 1; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-    if (lane == 31) *reinterpret_cast<float2*>(own + 2 * D) = make_float2(s, prod);
+    if (lane == 0) publish_zp<D>(a.sums + row, which ? 0.f : s, prod_all, turn.tag);
   }
-  unsigned int* flag = a.flags + (long long)chunk * a.Hkv + h;
-  if (p.at > 0) publish(flag, launch, kOwn);
-  float2 in = make_float2(0.f, 0.f);  // alpha L of the next token
+  float2 in[R::kP];  // alpha L of the next token
   float zin = 0.f;
+#pragma unroll
+  for (int i = 0; i < R::kP; ++i) in[i] = both(0.f);
   if (after > 0) {
-    in = come_in<D>(a, sh, a.sums, a.carry, chunk, h, after, 1, launch, zin);
-    if (p.at > 0 && sh.prod[kC - 1] != 0.f) {  // (with a product of 0 nobody asks for what came in)
-      float* carry = a.carry + ((long long)chunk * a.Hkv + h) * sums_row(D);
-      reinterpret_cast<float2*>(carry)[tid] = in;
-      if (tid == 0) carry[2 * D] = zin;
-      publish(flag, launch, kIn);
+    zin = come_in<D>(a.sums + row, a.carry + row, after, row_step, turn.tag, a.error, in);
+    if (p.at > 0 && prod_all != 0.f) {  // (with a product of 0 nobody asks for what came in)
+      publish<R::kE>(a.carry + row, in, turn.tag);
+      if (lane == 0) publish_zp<D>(a.carry + row, zin, 0.f, turn.tag);
     }
   }
   // from the last token to the first, half a chunk at a time: L, and its dots with the
   // values and with the sums before
-  T* dst = static_cast<T*>(which ? a.dv : a.dk) + row0 + e;
+  T* dst = static_cast<T*>(which ? a.dv : a.dk) + at;
+  float domega = 0.f, dsum = 0.f;
 #pragma unroll 1
   for (int half = 1; half >= 0; --half) {
     const int t0 = half * kH;
-    float2 A[kH];  // the sums before token t0 + i
-    float2 sum = half ? middle : sum0;
+    float2 A[kH][R::kP], sum[R::kP];  // the sums before token t0 + j
 #pragma unroll
-    for (int i = 0; i < kH; ++i) {
-      const float2 x = pair(rows, t0 + i);
-      const float al = sh.alpha[t0 + i], om = sh.omega[t0 + i];
-      A[i] = sum;
-      sum.x = fmaf(al, sum.x, om * x.x);
-      sum.y = fmaf(al, sum.y, om * x.y);
-    }
-    float dots[kC];  // with the values, with the sums
+    for (int i = 0; i < R::kP; ++i) sum[i] = half ? middle[i] : sum0[i];
 #pragma unroll
-    for (int i = kH - 1; i >= 0; --i) {
-      const int t = t0 + i;
-      const float2 x = pair(rows, t), gr = pair(grads, t);
-      const float rz = sh.rz[t], om = sh.omega[t], al = sh.alpha[t];
-      const float2 l = make_float2(fmaf(gr.x, rz, in.x), fmaf(gr.y, rz, in.y));
-      dots[i] = fmaf(l.x, x.x, l.y * x.y);
-      dots[kH + i] = fmaf(l.x, A[i].x, l.y * A[i].y);
-      const float2 out = make_float2(om * l.x, om * l.y);
-      if (gate_pair)
-        sh.e1[t] = out.y;
-      else if (t < n)
-        *reinterpret_cast<Raw*>(dst + t * step) = P::from_f(out);
-      in = make_float2(al * l.x, al * l.y);
+    for (int j = 0; j < kH; ++j) {
+      float2 x[R::kP];
+      value(mine, t0 + j, x);
+      const float4 c = coef[t0 + j];
+#pragma unroll
+      for (int i = 0; i < R::kP; ++i) {
+        A[j][i] = sum[i];
+        sum[i] = fma2(both(c.x), sum[i], mul2(both(c.y), x[i]));
+      }
     }
-    sh.dot[1 + half][warp][lane] = transposed_sum(dots);
+#pragma unroll
+    for (int j = kH - 1; j >= 0; --j) {
+      const int t = t0 + j;
+      float2 x[R::kP], gr[R::kP], dx = both(0.f), da = both(0.f), out[R::kP];
+      value(mine, t, x);
+      value(grads, t, gr);
+      const float4 c = coef[t];
+#pragma unroll
+      for (int i = 0; i < R::kP; ++i) {
+        const float2 l = fma2(gr[i], both(c.z), in[i]);
+        dx = fma2(l, x[i], dx);
+        da = fma2(l, A[j][i], da);
+        out[i] = mul2(both(c.y), l);
+        in[i] = mul2(both(c.x), l);
+      }
+      put(j, dx);
+      put(kH + j, da);
+      if (gate_lane) sh.first[t] = out[0].y;
+      if (t < n) R::write(dst + t * step, out);  // (the first component of dk comes below)
+    }
+    // lanes 0-15: with the values, 16-31: with the sums; to the lanes of their tokens
+    const float d = take();
+    const float lo = __shfl_sync(0xffffffffu, d, lane & 15), hi = __shfl_sync(0xffffffffu, d, 16 + (lane & 15));
+    if (lane >> 4 == half) {
+      domega = lo;
+      dsum = hi;
+    }
+  }
+  if (which) {
+    sh.other[0][lane] = domega;
+    sh.other[1][lane] = dsum;
   }
   __syncthreads();
-  unsigned int before = 0;
-  if (tid == 0) before = gone(a);
-  if (tid < 32) {
-    // Z_t = w_t + alpha_{t+1} Z_{t+1}; what comes in has its alpha already, and lanes from n on
-    // are the identity (alpha 1, w 0)
-    float next = __shfl_down_sync(0xffffffffu, g.alpha, 1);
-    if (lane == 31) {
-      next = 0.f;
-      zeta += zin;
-    }
+  if (which) return;
+  if (lane == 0) leave(a, turn);
+  // Z_t = w_t + alpha_{t+1} Z_{t+1}; what comes in has its alpha already, and lanes from n on
+  // are the identity (alpha 1, w 0)
+  float next = __shfl_down_sync(0xffffffffu, g.alpha, 1);
+  if (lane == 31) {
+    next = 0.f;
+    zeta += zin;
+  }
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const float on = __shfl_down_sync(0xffffffffu, next, off), oz = __shfl_down_sync(0xffffffffu, zeta, off);
-      if (lane + off < 32) {
-        zeta = fmaf(next, oz, zeta);
-        next *= on;
-      }
-    }
-    float zbefore = __shfl_up_sync(0xffffffffu, z, 1);
-    if (lane == 0) zbefore = zbefore0;
-    if (in_chunk) {
-      float domega = zeta, dalpha = fmaf(zeta, zbefore, dalpha_out);
-#pragma unroll
-      for (int w = 0; w < D / 32; ++w) {
-        domega += sh.dot[1 + lane / kH][w][lane % kH];
-        dalpha += sh.dot[1 + lane / kH][w][kH + lane % kH];
-      }
-      float dx = 0.f;
-      if (tok > p.t0) dx = (dalpha * g.alpha * g.rest - dbias * g.alpha) / a.temperature;
-      *reinterpret_cast<Raw*>(static_cast<T*>(a.dk) + ((long long)tok * a.Hkv + h) * D) =
-          P::from_f(make_float2(dx, sh.e1[lane]));
-      const T dq = Elt<T>::from_f(domega * g.omega * (1.f - g.omega) / (float)a.G);
-      for (int j = 0; j < a.G; ++j)
-        static_cast<T*>(a.dq)[(long long)tok * a.dq_tok + (long long)(h * a.G + j) * a.dq_head] = dq;
+  for (int off = 1; off < 32; off <<= 1) {
+    const float on = __shfl_down_sync(0xffffffffu, next, off), oz = __shfl_down_sync(0xffffffffu, zeta, off);
+    if (lane + off < 32) {
+      zeta = fmaf(next, oz, zeta);
+      next *= on;
     }
   }
-  if (tid == 0) leave(a, before, launch);
+  float zbefore = __shfl_up_sync(0xffffffffu, z, 1);
+  if (lane == 0) zbefore = zbefore0;
+  if (in_chunk) {
+    domega += sh.other[0][lane] + zeta;
+    dalpha += dsum + sh.other[1][lane] + zeta * zbefore;
+    float dx = 0.f;
+    if (tok > p.t0) dx = (dalpha * g.alpha * g.rest - dbias * g.alpha) / a.temperature;
+    *reinterpret_cast<typename Pair<T>::Raw*>(static_cast<T*>(a.dk) + ((long long)tok * a.Hkv + h) * D) =
+        Pair<T>::from_f(make_float2(dx, sh.first[lane]));
+    const T dq = Elt<T>::from_f(domega * g.omega * (1.f - g.omega) / (float)a.G);
+    for (int j = 0; j < a.G; ++j)
+      static_cast<T*>(a.dq)[(long long)tok * a.dq_tok + (long long)(h * a.G + j) * a.dq_head] = dq;
+  }
 }
 
 template <typename T, int D>
 cudaError_t forward(const StatesArgs& a, cudaStream_t stream) {
-  states_kernel<T, D><<<(unsigned)(pieces(a.seqs.total, a.seqs.num, kC) * a.Hkv), D, 0, stream>>>(a);
+  states_kernel<T, D><<<(unsigned)(pieces(a.seqs.total, a.seqs.num, kC) * a.Hkv * 2), 32, 0, stream>>>(a);
   return cudaGetLastError();
 }
 
 template <typename T, int D>
 cudaError_t backward(const StatesArgs& a, cudaStream_t stream) {
-  constexpr int bytes = 4 * kC * D * sizeof(T);
+  constexpr int bytes = sizeof(BackShared<T, D>);
   const cudaError_t e =
       cudaFuncSetAttribute(states_backward_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e != cudaSuccess) return e;
-  states_backward_kernel<T, D><<<(unsigned)(pieces(a.seqs.total, a.seqs.num, kC) * a.Hkv), D, bytes, stream>>>(a);
+  states_backward_kernel<T, D><<<(unsigned)(pieces(a.seqs.total, a.seqs.num, kC) * a.Hkv), 64, bytes, stream>>>(a);
   return cudaGetLastError();
 }
 
