@@ -8,8 +8,8 @@
 //   warp 9          TMA loads: the Q tiles, and a ring of K and V tiles
 // and per query tile and 128 rows of K
 //   S = Q K^T          into tensor memory
-//   softmax            x = S log2(e) / sqrt(d) + bias log2(e), the running maximum and sum,
-//                      P = 2^(x - max) in bf16 over the row's S columns
+//   softmax            S / sqrt(d) + bias, the running maximum and sum, P = e^(score - max)
+//                      in bf16 over the row's S columns
 //   O += P V           P read from tensor memory
 // P is rounded to bf16, the type of the tensor cores' operand; the sum is taken from the
 // unrounded weights. The running maximum moves only when it grows by more than 8 (in log2
@@ -41,26 +41,33 @@ struct AttnMaps {
   CUtensorMap q, k, v;  // [token][head][D], box: 128 tokens x 64 columns
 };
 
-// A work item's share of its sequence
+// A work item: queries [q0, q0 + 256) as the query tiles 0 and 1, or, where they all lie in one
+// tile, the two tiles' places in turn, so that one such item's softmax runs beside the
+// epilogue of the one before.
 struct Item {
-  bool ok;
-  int t0, t1;  // the sequence's tokens
-  int q0;      // first query
-  int n[2];    // K tiles that each query tile sees (0: it has no rows)
+  int t0, t1;     // the sequence's tokens
+  int q[2];       // first query of each tile
+  int n[2];       // K tiles that it sees (0: it has no rows)
   int h;
 };
-__device__ __forceinline__ Item item_of(const AttnArgs& a, int index) {
-  const Piece p = find_piece(a.seqs, kItem, index / a.Hq);
-  Item w;
-  w.ok = p.ok;
-  w.t0 = p.t0;
-  w.t1 = p.t1;
-  w.h = index % a.Hq;
-  const int at = (p.t1 - p.t0 + kItem - 1) / kItem - 1 - p.at;  // the longest first
-  w.q0 = p.t0 + at * kItem;
-  w.n[0] = 2 * at + 1;
-  w.n[1] = w.q0 + kR < p.t1 ? 2 * at + 2 : 0;
-  return w;
+__device__ __forceinline__ Item item_of(const Work& w, int& single) {
+  Item it;
+  it.t0 = w.t0;
+  it.t1 = w.t1;
+  it.h = w.head;
+  it.q[0] = w.t0 + w.at * kItem;
+  it.q[1] = it.q[0] + kR;
+  it.n[0] = 2 * w.at + 1;
+  it.n[1] = it.q[1] < w.t1 ? 2 * w.at + 2 : 0;
+  if (it.n[1] == 0) {
+    if (single & 1) {
+      it.q[1] = it.q[0];
+      it.n[1] = it.n[0];
+      it.n[0] = 0;
+    }
+    ++single;
+  }
+  return it;
 }
 
 // multiplies the rows' O (one per lane) by corr
@@ -118,34 +125,20 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(bar));
   };
-  auto next_item = [&](int turn) -> int {  // INT_MAX: a wait gave up
-    const int sl = turn & 1;
-    if (!wait(&sh.work.full[sl], (turn >> 1) & 1)) return INT_MAX;
-    const int index = *reinterpret_cast<volatile int*>(&sh.work.index[sl]);
-    arrive_warp(&sh.work.empty[sl]);
-    return tc_uniform(index);
-  };
-
   if (warp >= 8) {
     // A softmax thread holds a row of scores: 208 registers for those, 88 for the others
     // (256 x 208 + 128 x 88 of the 384 x 168 launched).
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 9) {
       // ---------------------------------------------------------------- loads
-      uint32_t n = 0, q_par = 0, q_any = 0;  // bit w: parity of query tile w's next Q, whether there was one
+      uint32_t n = 0, q_par = 0, q_any = 0;  // bit t: parity of query tile t's next Q, whether there was one
       bool ok = true;
-      int index = blockIdx.x, next = 0;
-      for (int it = 0; ok; ++it, index = __shfl_sync(0xffffffffu, next, 0)) {
-        const int sl = it & 1;
-        if (!wait(&sh.work.empty[sl], ((it >> 1) & 1) ^ 1)) break;
-        if (lane == 0) {
-          sh.work.index[sl] = index;
-          if (index < items) next = (int)gridDim.x + atomicAdd(a.counter, 1);
-        }
-        arrive_warp(&sh.work.full[sl]);
-        if (index >= items) break;
-        const Item w = item_of(a, index);
-        if (!w.ok) continue;
+      WorkSource src = work_source();
+      int single = 0;
+      while (ok) {
+        const Work work = take_work(sh.work, src, a.seqs, kItem, false, a.Hq, items, a.counter, wait);
+        if (work.head < 0) break;
+        const Item w = item_of(work, single);
         const int hk = w.h / a.G, steps = max(w.n[0], w.n[1]);
 #pragma unroll 1
         for (int x = 0; x < 2 * steps; ++x, ++n) {
@@ -169,7 +162,7 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
               if (tc_elect()) {
                 const uint32_t bar = smem_u32(&sh.q_full[t]);
                 mbar_arrive_expect_tx(bar, kTile);
-                load_tile<D>(smem_u32(sh.q[t]), &maps.q, bar, w.h, w.q0 + t * kR);
+                load_tile<D>(smem_u32(sh.q[t]), &maps.q, bar, w.h, w.q[t]);
               }
               __syncwarp();
             }
@@ -238,13 +231,13 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
         s_any |= 1u << t;
         return true;
       };
-      for (int turn = 0; ok; ++turn) {
-        const int index = next_item(turn);
-        if (index >= items) break;
-        const Item it = item_of(a, index);
-        if (!it.ok) continue;
-        const int n0 = tc_uniform(it.n[0]), n1 = tc_uniform(it.n[1]), steps = max(n0, n1);
-        const int keys = tc_uniform(it.t1 - it.t0 - (steps - 1) * kR);  // of the last K tile
+      int turn = 0, single = 0;
+      while (ok) {
+        const Work work = next_work(sh.work, turn, wait);
+        if (work.head < 0) break;
+        const Item it = item_of(work, single);
+        const int n0 = it.n[0], n1 = it.n[1], steps = max(n0, n1);
+        const int keys = it.t1 - it.t0 - (steps - 1) * kR;  // of the last K tile
         // step j: P V of K tile j - 1, then S of tile j, query tile by query tile
 #pragma unroll 1
         for (int j = 0; j <= steps && ok; ++j) {
@@ -284,36 +277,58 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
     const int t = warp >> 2, r = tid & (kR - 1), wq = warp & 3;
     const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
     const uint32_t tS = tmem + t * 128 + lane_base, tO = tmem + 256 + t * D + lane_base;
-    const float qscale = kLog2e / sqrtf((float)D);
+    const float scale = 1.f / sqrtf((float)D);
+    const float log2_unit = kBias ? kLog2e : kLog2e * scale;  // of a score as it is kept, in log2 units
     uint32_t steps = 0;
     bool ok = true;
-    for (int turn = 0; ok; ++turn) {
-      const int index = next_item(turn);
-      if (index >= items) break;
-      const Item it = item_of(a, index);
-      const int nt = it.n[t];
-      if (!it.ok || nt == 0) continue;
-      const int row0 = it.q0 + t * kR + wq * 32;  // the warp's first query
-      const float* bias = kBias ? a.bias + (long long)(it.h / a.G) * a.seqs.total : nullptr;
-      float nb[4];  // the next step's biases, four per lane
-      auto fetch = [&](int j) {
-        if (kBias)
+    int turn = 0, single = 0;
+    struct Mine {  // an item, for this query tile
+      int t1, h, n, row0;  // the sequence's end, head (below 0: no more items), K tiles, the warp's first query
+      const float* bias;   // of the first row of K
+      int key;             // that row
+    };
+    // the biases of step j, to this warp's copy
+    auto fetch = [&](const Mine& it, int j) {
+      if (kBias) {
+        const uint32_t dst = smem_u32(sh.bias[warp][j & 1]) + lane * 4;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int tok = it.t0 + j * kR + 32 * i + lane;
-            nb[i] = tok < it.t1 ? bias[tok] * kLog2e : 0.f;
-          }
-      };
-      fetch(0);
+        for (int i = 0; i < 4; ++i) {
+          const int row = j * kR + 32 * i + lane;
+          const bool in = it.key + row < it.t1;
+          cp_async4_zfill(dst + 128 * i, it.bias + (in ? row : 0), in);
+        }
+        cp_async_commit();
+      }
+    };
+    // the next item that this query tile has rows of, its first biases on their way
+    auto next = [&]() {
+      Mine it;
+      do {
+        const Work work = next_work(sh.work, turn, wait);
+        it.h = -1;
+        if (work.head < 0) return it;
+        const Item x = item_of(work, single);
+        it.t1 = x.t1;
+        it.h = x.h;
+        it.n = t ? x.n[1] : x.n[0];
+        it.row0 = (t ? x.q[1] : x.q[0]) + wq * 32;
+        it.key = x.t0;
+        if (kBias) it.bias = a.bias + (long long)(x.h / a.G) * a.seqs.total + it.key;
+      } while (it.n == 0);
+      fetch(it, 0);
+      return it;
+    };
+    Mine it = next();
+    while (it.h >= 0) {
+      const int nt = it.n, row0 = it.row0;
       float m = -INFINITY, l = 0.f;
 #pragma unroll 1
       for (int j = 0; j < nt; ++j, ++steps) {
-        float* b = sh.bias[warp][j & 1];
+        const float* b = sh.bias[warp][j & 1];
         if (kBias) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) b[32 * i + lane] = nb[i];
+          cp_async_wait<0>();
           __syncwarp();
-          if (j + 1 < nt) fetch(j + 1);
+          if (j + 1 < nt) fetch(it, j + 1);
         }
         if (!(ok = wait(&sh.s_full[t], steps & 1))) break;
         tc_fence_after();
@@ -321,27 +336,28 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
 #pragma unroll
         for (int c0 = 0; c0 < kR; c0 += 32) tc_ld32(tS + c0, s + c0);
         tc_wait_ld();
-        const float2 scale2 = make_float2(qscale, qscale);
-        if (j < nt - 1) {
+        if (kBias && j < nt - 1) {
+          // scores in natural units
 #pragma unroll
           for (int i = 0; i < kR; i += 4) {
-            float4 c = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (kBias) c = *reinterpret_cast<const float4*>(b + i);
-            const float2 x = fma2(make_float2(s[i], s[i + 1]), scale2, make_float2(c.x, c.y));
-            const float2 y = fma2(make_float2(s[i + 2], s[i + 3]), scale2, make_float2(c.z, c.w));
+            const float4 c = *reinterpret_cast<const float4*>(b + i);
+            const float2 x = fma2(make_float2(s[i], s[i + 1]), make_float2(scale, scale), make_float2(c.x, c.y));
+            const float2 y = fma2(make_float2(s[i + 2], s[i + 3]), make_float2(scale, scale), make_float2(c.z, c.w));
             s[i] = x.x; s[i + 1] = x.y; s[i + 2] = y.x; s[i + 3] = y.y;
           }
-        } else {
+        } else if (kBias) {
           // the diagonal tile: rows up to the query's own, which has no bias
 #pragma unroll
           for (int i = 0; i < kR; i += 4) {
-            float4 c = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (kBias) c = *reinterpret_cast<const float4*>(b + i);
+            const float4 c = *reinterpret_cast<const float4*>(b + i);
             const float e[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              s[i + k] = i + k > r ? -INFINITY : fmaf(s[i + k], qscale, i + k == r ? 0.f : e[k]);
+              s[i + k] = i + k > r ? -INFINITY : fmaf(s[i + k], scale, i + k == r ? 0.f : e[k]);
           }
+        } else if (j == nt - 1) {
+#pragma unroll
+          for (int i = 0; i < kR; ++i) s[i] = i > r ? -INFINITY : s[i];
         }
         float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
@@ -352,34 +368,37 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
         }
         const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         {
-          const bool grow = mt > m + 8.f, resc = grow && m != -INFINITY;
-          const float corr = resc ? ex2f(m - mt) : 1.f;
+          const bool grow = (mt - m) * log2_unit > 8.f || m == -INFINITY, resc = grow && m != -INFINITY;
+          const float corr = resc ? ex2f((m - mt) * log2_unit) : 1.f;
           if (grow) m = mt;
           l *= corr;
           if (__any_sync(0xffffffffu, resc)) rescale<D>(tO, corr);
         }
-        const float nm = m == -INFINITY ? 0.f : -m;  // nothing seen yet: every x is -inf
-        const float2 shift2 = make_float2(nm, nm);
+        const float nm = m == -INFINITY ? 0.f : -m * log2_unit;  // nothing seen yet: every score is -inf
+        const float2 shift2 = make_float2(nm, nm), unit2 = make_float2(log2_unit, log2_unit);
         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-        for (int c0 = 0; c0 < kR; c0 += 64) {
-          uint32_t pk[32];
+        for (int c0 = 0; c0 < kR; c0 += 32) {
+          uint32_t pk[16];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const float2 x = add2(make_float2(s[c0 + 2 * i], s[c0 + 2 * i + 1]), shift2);
+          for (int i = 0; i < 16; ++i) {
+            const float2 x = fma2(make_float2(s[c0 + 2 * i], s[c0 + 2 * i + 1]), unit2, shift2);
             const float2 p = make_float2(ex2f(x.x), ex2f(x.y));
             sum[i & 1] = add2(sum[i & 1], p);
             pk[i] = Chunk<__nv_bfloat16>::pack2(p.x, p.y);
           }
-          tc_st32(tS + c0 / 2, pk);
-          tc_wait_st();
-          tc_fence_before();
-          arrive_warp(&sh.p_full[t][c0 / 64]);
+          tc_st16(tS + c0 / 2, pk);
+          if (c0 & 32) {
+            tc_wait_st();
+            tc_fence_before();
+            arrive_warp(&sh.p_full[t][c0 / 64]);
+          }
         }
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       }
       if (!ok) break;
       // ---- the row of O over the row's sum
+      const Mine after = next();
       const float inv = 1.f / l;
       if (!(ok = wait(&sh.o_full[t], (steps - 1) & 1))) break;
       tc_fence_after();
@@ -394,8 +413,9 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
         for (int i = 0; i < 32; ++i) o[i] *= inv;
         write_rows(sh.stage[warp], o, out + c0 * 2, (long long)a.Hq * D * 2, rows);
       }
-      if (lane < rows) a.lse[(long long)it.h * a.seqs.total + row0 + lane] = (m + log2f(l)) * kLn2;
+      if (lane < rows) a.lse[(long long)it.h * a.seqs.total + row0 + lane] = fmaf(m, log2_unit, log2f(l)) * kLn2;
       tc_fence_before();  // the loads of O are done before the next item's P is announced
+      it = after;
     }
   }
   tc_fence_before();

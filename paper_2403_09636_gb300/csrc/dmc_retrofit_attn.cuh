@@ -15,11 +15,102 @@ constexpr int kAttnThreads = 384; // 12 warps: 0-7 rows, 8 products, 9 loads; th
 constexpr int kStageRow = 80;     // bytes of a row of an epilogue stage: 64 and 16 of padding
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// Work items are taken from a counter: index 0 .. gridDim - 1 without one, then in the
-// order in which CTAs come for more. Warp 9 takes an item ahead of the others and hands
-// it to them. The last CTA resets the counter for the next launch.
+// A piece of a sequence's tokens and a head.
+struct Work {
+  int t0, t1;  // the sequence's tokens
+  int seq, at; // the sequence, the piece's index in it
+  int head;    // below 0: no more work
+};
+
+// Pieces by cost: the k-th of all, when those of the highest index (kFromEnd: of the most
+// pieces from it on) come first, whatever sequence they belong to, so that the last ones
+// to be handed out are the cheapest. With f(L) = sum over sequences of max(0, pieces - L), the
+// number of pieces with L others before (after) them, L is the largest with f(L) > k. For
+// up to 128 sequences, by a whole warp (four sequences per lane). More are taken in their
+// order (ordered_work), where one sequence matters less and the search over L would take longer
+// than a short item. False: there are no more.
+constexpr int kRankedSeqs = 128;
+__device__ __forceinline__ bool ranked_work(const Seqs& q, int piece, bool from_end, int k, Work& w) {
+  const int lane = threadIdx.x & 31;
+  int n[kRankedSeqs / 32], most = 0;
+#pragma unroll
+  for (int i = 0; i < kRankedSeqs / 32; ++i) {
+    const int s = i * 32 + lane;
+    n[i] = 0;
+    if (s < q.num) {
+      const int t0 = q.cu[s], t1 = q.cu[s + 1];
+      if (seq_ok(q, t0, t1)) n[i] = (t1 - t0 + piece - 1) / piece;
+    }
+    most = max(most, n[i]);
+  }
+  auto f = [&](int L) {
+    int x = 0;
+#pragma unroll
+    for (int i = 0; i < kRankedSeqs / 32; ++i) x += max(0, n[i] - L);
+    return __reduce_add_sync(0xffffffffu, x);
+  };
+  if (k >= f(0)) return false;
+  int lo = 0, hi = __reduce_max_sync(0xffffffffu, most);  // f(lo) > k >= f(hi)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (f(mid) > k) lo = mid; else hi = mid;
+  }
+  int left = k - f(lo + 1), seq = 0;  // the left-th sequence of more than lo pieces
+#pragma unroll
+  for (int i = 0; i < kRankedSeqs / 32; ++i) {
+    const unsigned int b = __ballot_sync(0xffffffffu, n[i] > lo);
+    const int c = __popc(b);
+    if (left >= 0 && left < c) {
+      unsigned int m = b;
+      for (int j = 0; j < left; ++j) m &= m - 1;
+      seq = i * 32 + __ffs(m) - 1;
+    }
+    left -= c;
+  }
+  w.seq = seq;
+  w.t0 = q.cu[seq];
+  w.t1 = q.cu[seq + 1];
+  w.at = from_end ? (w.t1 - w.t0 + piece - 1) / piece - 1 - lo : lo;
+  return true;
+}
+
+__device__ __forceinline__ bool ordered_work(const Seqs& q, int piece, bool from_end, int k, Work& w) {
+  const int lane = threadIdx.x & 31;
+  for (int base = 0; base < q.num; base += 32) {
+    const int s = base + lane;
+    int n = 0, t0 = 0, t1 = 0;
+    if (s < q.num) {
+      t0 = q.cu[s];
+      t1 = q.cu[s + 1];
+      if (seq_ok(q, t0, t1)) n = (t1 - t0 + piece - 1) / piece;
+    }
+    const int all = __reduce_add_sync(0xffffffffu, n);
+    if (k >= all) {
+      k -= all;
+      continue;
+    }
+    int upto = n;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, upto, off);
+      if (lane >= off) upto += o;
+    }
+    const int hit = __ffs(__ballot_sync(0xffffffffu, k < upto)) - 1;
+    const int i = k - __shfl_sync(0xffffffffu, upto - n, hit);
+    w.seq = base + hit;
+    w.t0 = __shfl_sync(0xffffffffu, t0, hit);
+    w.t1 = __shfl_sync(0xffffffffu, t1, hit);
+    w.at = from_end ? i : __shfl_sync(0xffffffffu, n, hit) - 1 - i;  // the most expensive first
+    return true;
+  }
+  return false;
+}
+
+// Work is numbered by piece, heads fastest. The numbers 0 .. gridDim - 1 go to the CTAs, then
+// each takes the next from a counter. Warp 9 does so, one piece of work ahead of the other
+// warps, and hands it to them. The last CTA resets the counter for the next launch.
 struct WorkRing {
-  int index[2];
+  Work work[2];
   uint64_t full[2], empty[2];
 };
 __device__ __forceinline__ void work_init(WorkRing& w) {
@@ -35,6 +126,62 @@ __device__ __forceinline__ void work_done(int* counter) {
     counter[1] = 0;
     __threadfence();
   }
+}
+
+// Warp 9's side.
+struct WorkSource {
+  int number, turn;  // the next work's, the next place in the ring
+};
+__device__ __forceinline__ WorkSource work_source() { return {(int)blockIdx.x, 0}; }
+// The next work, handed to the other warps too (head < 0: there is none, or a wait gave up).
+template <typename Wait>
+__device__ __forceinline__ Work take_work(WorkRing& ring, WorkSource& src, const Seqs& q, int piece, bool from_end, int heads,
+                                          int most, int* counter, const Wait& wait) {
+  Work w;
+  w.t0 = w.t1 = w.seq = w.at = 0;
+  w.head = -1;
+  if (src.number < most) {
+    int next = 0;
+    if ((threadIdx.x & 31) == 0) next = (int)gridDim.x + atomicAdd(counter, 1);
+    const int k = src.number / heads;
+    const bool there = q.num <= kRankedSeqs ? ranked_work(q, piece, from_end, k, w) : ordered_work(q, piece, from_end, k, w);
+    if (there) w.head = src.number % heads;
+    src.number = __shfl_sync(0xffffffffu, next, 0);
+  }
+  const int sl = src.turn & 1;
+  if (!wait(&ring.empty[sl], ((src.turn >> 1) & 1) ^ 1)) {
+    w.head = -1;
+    return w;
+  }
+  if ((threadIdx.x & 31) == 0) ring.work[sl] = w;
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&ring.full[sl]));
+  ++src.turn;
+  return w;
+}
+// The other warps' side (head < 0: no more work, or a wait gave up).
+template <typename Wait>
+__device__ __forceinline__ Work next_work(WorkRing& ring, int& turn, const Wait& wait) {
+  const int sl = turn & 1;
+  Work w;
+  w.t0 = w.t1 = w.seq = w.at = 0;
+  w.head = -1;
+  if (!wait(&ring.full[sl], (turn >> 1) & 1)) return w;
+  w.t0 = tc_uniform(ring.work[sl].t0);
+  w.t1 = tc_uniform(ring.work[sl].t1);
+  w.seq = tc_uniform(ring.work[sl].seq);
+  w.at = tc_uniform(ring.work[sl].at);
+  w.head = tc_uniform(ring.work[sl].head);
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&ring.empty[sl]));
+  ++turn;
+  return w;
+}
+
+// Four bytes to shared memory, asynchronously; zero unless `valid` (src is a valid address anyway).
+__device__ __forceinline__ void cp_async4_zfill(uint32_t dst, const void* src, bool valid) {
+  const uint32_t n = valid ? 4u : 0u;
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
 
 template <int D>

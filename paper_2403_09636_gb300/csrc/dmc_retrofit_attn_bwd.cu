@@ -93,23 +93,18 @@ struct DkvShared {
 };
 
 struct DkvItem {
-  bool ok;
-  int t0, t1, j0;  // the sequence's tokens, the first row of K
+  int t1, j0;      // the sequence's end, the first row of K
   int hk, tile0;   // KV head, the row tile (attn_rows_kernel) of the query tile at j0
   int tiles;       // query tiles that see the rows
 };
-__device__ __forceinline__ DkvItem dkv_item(const AttnArgs& a, int index) {
-  const int piece = index / a.Hkv;
-  const Piece p = find_piece(a.seqs, kR, piece);
-  DkvItem w;
-  w.ok = p.ok;
-  w.t0 = p.t0;
-  w.t1 = p.t1;
-  w.j0 = p.t0 + p.at * kR;
-  w.hk = index % a.Hkv;
-  w.tile0 = piece;
-  w.tiles = (p.t1 - w.j0 + kR - 1) / kR;
-  return w;
+__device__ __forceinline__ DkvItem dkv_item(const Work& w) {
+  DkvItem it;
+  it.t1 = w.t1;
+  it.j0 = w.t0 + w.at * kR;
+  it.hk = w.head;
+  it.tile0 = w.t0 / kR + w.seq + w.at;
+  it.tiles = (w.t1 - it.j0 + kR - 1) / kR;
+  return it;
 }
 
 template <int D, bool kBias>
@@ -150,32 +145,17 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(bar));
   };
-  auto next_item = [&](int turn) -> int {  // INT_MAX: a wait gave up
-    const int sl = turn & 1;
-    if (!wait(&sh.work.full[sl], (turn >> 1) & 1)) return INT_MAX;
-    const int index = *reinterpret_cast<volatile int*>(&sh.work.index[sl]);
-    arrive_warp(&sh.work.empty[sl]);
-    return tc_uniform(index);
-  };
-
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 9) {
       // ---------------------------------------------------------------- loads
       uint32_t n = 0, ni = 0;  // query tiles, items
       bool ok = true;
-      int index = blockIdx.x, next = 0;
-      for (int it = 0; ok; ++it, index = __shfl_sync(0xffffffffu, next, 0)) {
-        const int sl = it & 1;
-        if (!wait(&sh.work.empty[sl], ((it >> 1) & 1) ^ 1)) break;
-        if (lane == 0) {
-          sh.work.index[sl] = index;
-          if (index < items) next = (int)gridDim.x + atomicAdd(a.counter, 1);
-        }
-        arrive_warp(&sh.work.full[sl]);
-        if (index >= items) break;
-        const DkvItem w = dkv_item(a, index);
-        if (!w.ok) continue;
+      WorkSource src = work_source();
+      while (ok) {
+        const Work work = take_work(sh.work, src, a.seqs, kR, true, a.Hkv, items, a.counter, wait);
+        if (work.head < 0) break;
+        const DkvItem w = dkv_item(work);
         ok = wait(&sh.k_empty, (ni & 1) ^ 1) && wait(&sh.v_empty, (ni & 1) ^ 1);
         if (!ok) break;
         if (tc_elect()) {
@@ -253,13 +233,13 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
           tc_mma_ts(tC, tX + (kk >> 2) * 64 + (kk & 3) * 8, md + (y + kk * (2048 / 16)), tc_idesc(kR, D, false, true),
                     add || kk > 0);
       };
-      for (int turn = 0; ok; ++turn) {
-        const int index = next_item(turn);
-        if (index >= items) break;
-        const DkvItem w = dkv_item(a, index);
-        if (!w.ok) continue;
-        const int tiles = tc_uniform(w.tiles), steps = a.G * tiles;
-        const int last_rows = tc_uniform(w.t1 - w.j0 - (tiles - 1) * kR);  // queries of the last tile
+      int turn = 0;
+      while (ok) {
+        const Work work = next_work(sh.work, turn, wait);
+        if (work.head < 0) break;
+        const DkvItem w = dkv_item(work);
+        const int tiles = w.tiles, steps = a.G * tiles;
+        const int last_rows = w.t1 - w.j0 - (tiles - 1) * kR;  // queries of the last tile
         ok = wait(&sh.k_full, ni & 1) && wait(&sh.v_full, ni & 1);
         int i = 0;  // query tile of step x
 #pragma unroll 1
@@ -328,14 +308,19 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
     const float2 scale2 = make_float2(qscale, qscale);
     uint32_t n = 0, ni = 0;
     bool ok = true;
-    for (int turn = 0; ok; ++turn) {
-      const int index = next_item(turn);
-      if (index >= items) break;
-      const DkvItem w = dkv_item(a, index);
-      if (!w.ok) continue;
+    int turn = 0;
+    float nb = 0.f;  // the next item's bias
+    auto next = [&]() {
+      const Work work = next_work(sh.work, turn, wait);
+      const DkvItem w = dkv_item(work);
+      nb = 0.f;
+      if (kBias && work.head >= 0 && w.j0 + r < w.t1) nb = a.bias[(long long)w.hk * a.seqs.total + w.j0 + r] * kLog2e;
+      return w;
+    };
+    DkvItem w = next();
+    while (w.hk >= 0) {
       const int row = w.j0 + r;
-      float b = 0.f;
-      if (kBias && row < w.t1) b = a.bias[(long long)w.hk * a.seqs.total + row] * kLog2e;
+      const float b = nb;
       const float2 b2 = make_float2(b, b);
       const int steps = a.G * w.tiles;
       float2 db = make_float2(0.f, 0.f);
@@ -419,6 +404,7 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
       }
       if (!ok) break;
       // ---- the rows of dV (the first four warps) and dK
+      const DkvItem after = next();
       if (!(ok = wait(half ? &sh.dk_done : &sh.dv_done, (n - 1) & 1))) break;
       tc_fence_after();
       const int row0 = w.j0 + wq * 32, rows = w.t1 - row0;
@@ -448,6 +434,7 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
       }
       ++ni;
       tc_fence_before();  // the loads of dV and dK are done before the next item's P is announced
+      w = after;
     }
   }
   tc_fence_before();
@@ -476,24 +463,19 @@ struct DqShared {
 };
 
 struct DqItem {
-  bool ok;
   int t0, t1, q0;  // the sequence's tokens, the first query
   int h, tile;     // head, row tile (attn_rows_kernel)
   int steps;       // K tiles
 };
-__device__ __forceinline__ DqItem dq_item(const AttnArgs& a, int index) {
-  const int piece = index / a.Hq;
-  const Piece p = find_piece(a.seqs, kR, piece);
-  DqItem w;
-  w.ok = p.ok;
-  w.t0 = p.t0;
-  w.t1 = p.t1;
-  w.h = index % a.Hq;
-  const int at = (p.t1 - p.t0 + kR - 1) / kR - 1 - p.at;  // the longest first
-  w.q0 = p.t0 + at * kR;
-  w.tile = piece - p.at + at;
-  w.steps = at + 1;
-  return w;
+__device__ __forceinline__ DqItem dq_item(const Work& w) {
+  DqItem it;
+  it.t0 = w.t0;
+  it.t1 = w.t1;
+  it.q0 = w.t0 + w.at * kR;
+  it.h = w.head;
+  it.tile = w.t0 / kR + w.seq + w.at;
+  it.steps = w.at + 1;
+  return it;
 }
 
 template <int D, bool kBias>
@@ -537,32 +519,17 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(bar));
   };
-  auto next_item = [&](int turn) -> int {  // INT_MAX: a wait gave up
-    const int sl = turn & 1;
-    if (!wait(&sh.work.full[sl], (turn >> 1) & 1)) return INT_MAX;
-    const int index = *reinterpret_cast<volatile int*>(&sh.work.index[sl]);
-    arrive_warp(&sh.work.empty[sl]);
-    return tc_uniform(index);
-  };
-
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 9) {
       // ---------------------------------------------------------------- loads
       uint32_t nk = 0, nv = 0, nq = 0, ni = 0;  // K tiles, V halves, Q tiles and dO tiles requested
       bool ok = true;
-      int index = blockIdx.x, next = 0;
-      for (int it = 0; ok; ++it, index = __shfl_sync(0xffffffffu, next, 0)) {
-        const int sl = it & 1;
-        if (!wait(&sh.work.empty[sl], ((it >> 1) & 1) ^ 1)) break;
-        if (lane == 0) {
-          sh.work.index[sl] = index;
-          if (index < items) next = (int)gridDim.x + atomicAdd(a.counter, 1);
-        }
-        arrive_warp(&sh.work.full[sl]);
-        if (index >= items) break;
-        const DqItem w = dq_item(a, index);
-        if (!w.ok) continue;
+      WorkSource src = work_source();
+      while (ok) {
+        const Work work = take_work(sh.work, src, a.seqs, kR, false, a.Hq, items, a.counter, wait);
+        if (work.head < 0) break;
+        const DqItem w = dq_item(work);
         const int hk = w.h / a.G;
 #pragma unroll 1
         for (int j = 0; j < w.steps && ok; ++j) {
@@ -617,13 +584,13 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
                      vs = smem_u32(sh.v[0]) >> 4;
       uint32_t n = 0, ni = 0;  // steps, items
       bool ok = true;
-      for (int turn = 0; ok; ++turn) {
-        const int index = next_item(turn);
-        if (index >= items) break;
-        const DqItem w = dq_item(a, index);
-        if (!w.ok) continue;
-        const int steps = tc_uniform(w.steps);
-        const int keys = tc_uniform(w.t1 - w.q0);  // rows of the last K tile, the queries' own
+      int turn = 0;
+      while (ok) {
+        const Work work = next_work(sh.work, turn, wait);
+        if (work.head < 0) break;
+        const DqItem w = dq_item(work);
+        const int steps = w.steps;
+        const int keys = w.t1 - w.q0;  // rows of the last K tile, the queries' own
         ok = wait(&sh.q_full, ni & 1);
 #pragma unroll 1
         for (int x = 0; x <= steps && ok; ++x, ++n) {
@@ -701,33 +668,45 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
     const float2 scale2 = make_float2(qscale, qscale);
     uint32_t n = 0;
     bool ok = true;
-    for (int turn = 0; ok; ++turn) {
-      const int index = next_item(turn);
-      if (index >= items) break;
-      const DqItem w = dq_item(a, index);
-      if (!w.ok) continue;
-      const float* bias = kBias ? a.bias + (long long)(w.h / a.G) * a.seqs.total : nullptr;
-      const float* rows = row_tile(a, row_tiles, w.h, w.tile);
-      const float nl = rows[r], delta = rows[kR + r];
-      const float2 nl2 = make_float2(nl, nl), nd2 = make_float2(-delta, -delta);
-      float nb[2];
-      auto fetch = [&](int j) {
-        if (kBias)
+    int turn = 0;
+    float nrow[2] = {0.f, 0.f};   // the next item's row
+    const float* bias = nullptr;  // of the item's first row of K
+    // the biases of step j, to this warp's copy
+    auto fetch = [&](const DqItem& w, int j) {
+      if (kBias) {
+        const uint32_t dst = smem_u32(sh.bias[warp][j & 1]) + lane * 4;
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int tok = w.t0 + j * kR + half * 64 + 32 * i + lane;
-            nb[i] = tok < w.t1 ? bias[tok] * kLog2e : 0.f;
-          }
-      };
-      fetch(0);
+        for (int i = 0; i < 2; ++i) {
+          const int row = j * kR + half * 64 + 32 * i + lane;
+          const bool in = w.t0 + row < w.t1;
+          cp_async4_zfill(dst + 128 * i, bias + (in ? row : 0), in);
+        }
+        cp_async_commit();
+      }
+    };
+    auto next = [&]() {  // its numbers on their way
+      const Work work = next_work(sh.work, turn, wait);
+      const DqItem w = dq_item(work);
+      if (work.head >= 0) {
+        if (kBias) bias = a.bias + (long long)(w.h / a.G) * a.seqs.total + w.t0;
+        fetch(w, 0);
+        const float* rows = row_tile(a, row_tiles, w.h, w.tile);
+        nrow[0] = rows[r];
+        nrow[1] = rows[kR + r];
+      }
+      return w;
+    };
+    DqItem w = next();
+    while (w.h >= 0) {
+      const float nl = nrow[0], delta = nrow[1];
+      const float2 nl2 = make_float2(nl, nl), nd2 = make_float2(-delta, -delta);
 #pragma unroll 1
       for (int j = 0; j < w.steps; ++j, ++n) {
-        float* b = sh.bias[warp][j & 1];
+        const float* b = sh.bias[warp][j & 1];
         if (kBias) {
-          b[lane] = nb[0];
-          b[32 + lane] = nb[1];
+          cp_async_wait<0>();
           __syncwarp();
-          if (j + 1 < w.steps) fetch(j + 1);
+          if (j + 1 < w.steps) fetch(w, j + 1);
         }
         if (!(ok = wait(&sh.s_full, n & 1))) break;
         tc_fence_after();
@@ -741,11 +720,14 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
         if (!diag) {
 #pragma unroll
           for (int c = 0; c < 64; c += 4) {
-            float2 u = fma2(make_float2(p[c], p[c + 1]), scale2, nl2), v = fma2(make_float2(p[c + 2], p[c + 3]), scale2, nl2);
+            float2 u = make_float2(p[c], p[c + 1]), v = make_float2(p[c + 2], p[c + 3]);
             if (kBias) {
               const float4 e = *reinterpret_cast<const float4*>(b + c);
-              u = add2(u, make_float2(e.x, e.y));
-              v = add2(v, make_float2(e.z, e.w));
+              u = fma2(fma2(u, make_float2(scale, scale), make_float2(e.x, e.y)), make_float2(kLog2e, kLog2e), nl2);
+              v = fma2(fma2(v, make_float2(scale, scale), make_float2(e.z, e.w)), make_float2(kLog2e, kLog2e), nl2);
+            } else {
+              u = fma2(u, scale2, nl2);
+              v = fma2(v, scale2, nl2);
             }
             p[c] = ex2f(u.x); p[c + 1] = ex2f(u.y); p[c + 2] = ex2f(v.x); p[c + 3] = ex2f(v.y);
           }
@@ -753,7 +735,7 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
           const int own = r - half * 64;
 #pragma unroll
           for (int c = 0; c < 64; ++c) {
-            const float e = fmaf(p[c], qscale, nl) + (kBias && c < own ? b[c] : 0.f);
+            const float e = fmaf(fmaf(p[c], scale, kBias && c < own ? b[c] : 0.f), kLog2e, nl);
             p[c] = c > own ? 0.f : ex2f(e);
           }
         }
@@ -781,6 +763,7 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
       }
       if (!ok) break;
       // ---- this thread's half of its row of dQ
+      const DqItem after = next();
       if (!(ok = wait(&sh.dq_done[(n - 1) & 1], ((n - 1) >> 1) & 1))) break;
       tc_fence_after();
       constexpr int kCols = D / 2;
@@ -798,6 +781,7 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
           for (int c = 0; c < 4; ++c) dst[c0 / 8 + c] = Chunk<__nv_bfloat16>::pack(f + 8 * c);
       }
       tc_fence_before();  // the loads of dQ are done before the next item's dS is announced
+      w = after;
     }
   }
   tc_fence_before();

@@ -78,6 +78,16 @@ def test_attention_sequences_are_apart(cuda_dev, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [128, 129, 300])
+def test_attention_many_sequences(cuda_dev, n, dtype):
+    """Short and empty sequences in great number, a long one among them."""
+    lens = [(7 * i) % 41 for i in range(n)]
+    lens[n // 2] = 270
+    x = attention_inputs(lens, 2, 1, 64, dtype)
+    check_attention(x, lens, dtype, run_attention(cuda_dev, x, lens, (2, 1, 64), dtype))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_attention_twice_the_same(cuda_dev, dtype):
     lens, heads = [513, 260], (8, 2, 128)
     x = attention_inputs(lens, *heads, dtype)
