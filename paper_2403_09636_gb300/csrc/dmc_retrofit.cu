@@ -15,10 +15,8 @@ cudaError_t attn_forward_f32(const AttnArgs& a, int D, cudaStream_t stream);
 cudaError_t attn_backward_f32(const AttnArgs& a, int D, cudaStream_t stream);
 cudaError_t attn_backward_bf16(const AttnArgs& a, int D, cudaStream_t stream);
 cudaError_t attn_forward_bf16(const AttnArgs& a, int D, cudaStream_t stream);
-cudaError_t loss_forward_f32(const LossArgs& a, int* shares, cudaStream_t stream);
-cudaError_t loss_backward_f32(const LossArgs& a, cudaStream_t stream);
-cudaError_t loss_forward_bf16(const LossArgs& a, int* shares, cudaStream_t stream);
-cudaError_t loss_backward_bf16(const LossArgs& a, cudaStream_t stream);
+cudaError_t loss_forward(const LossArgs& a, bool bf16, cudaStream_t stream);
+cudaError_t loss_backward(const LossArgs& a, bool bf16, cudaStream_t stream);
 
 namespace {
 
@@ -50,18 +48,18 @@ bool valid(const dmc_retrofit_config* c) {
   return has_heads(*c) || has_loss(*c);
 }
 
-// Words of one piece of the loss's backward pass: the gradient of its logits is
-// kept for all tokens, in at most 512 MB, but no fewer than 1024 words.
+// Words of one piece of the vocabulary: the gradient of its logits is kept for all tokens
+// (in fp32 the parts of its weights, too), in about 512 MB, but no fewer than 1024 words.
 int loss_piece(const dmc_retrofit_config* c) {
-  const int64_t per_word = (int64_t)c->max_tokens * (c->dtype == DMC_F32 ? 4 : 2);
-  int64_t words = (512ll << 20) / per_word / 256 * 256;
-  const int64_t all = ((int64_t)c->vocab + 255) / 256 * 256;
+  const int64_t per_word = c->dtype == DMC_F32 ? 6 * ((int64_t)c->max_tokens + loss_stride(c->hidden)) : 2ll * c->max_tokens;
+  int64_t words = (512ll << 20) / per_word / kLossTile * kLossTile;
+  const int64_t all = ((int64_t)c->vocab + kLossTile - 1) / kLossTile * kLossTile;
   if (words < 1024) words = 1024;
   return (int)(words < all ? words : all);
 }
 
 struct Offsets {
-  size_t error, sums, carry, cleared, rows, part_m, part_l, target_logit, dh, grad, total;
+  size_t error, sums, carry, cleared, rows, part_m, part_l, target_logit, dh, grad, hidden_parts, weight_parts, total;
   int piece;
 };
 
@@ -85,12 +83,15 @@ Offsets offsets(const dmc_retrofit_config* c) {
   }
   if (has_loss(*c)) {
     o.piece = loss_piece(c);
-    const size_t shares = loss_shares(c->dtype == DMC_BF16, c->vocab);
+    const size_t shares = ceil_div(c->vocab, kLossShare), parts = c->dtype == DMC_F32 ? 3 : 0;
+    const size_t row = (size_t)loss_stride(c->hidden) * 2;
     o.part_m = at; at = align_up(at + tokens * shares * 4);
     o.part_l = at; at = align_up(at + tokens * shares * 4);
     o.target_logit = at; at = align_up(at + tokens * 4);
-    o.dh = at; at = align_up(at + (o.piece < c->vocab ? tokens * c->hidden * 4 : 0));
-    o.grad = at; at = align_up(at + tokens * o.piece * (c->dtype == DMC_F32 ? 4 : 2));
+    o.dh = at; at = align_up(at + (!parts && o.piece < c->vocab ? tokens * c->hidden * 4 : 0));
+    o.grad = at; at = align_up(at + tokens * o.piece * 2 * (parts ? parts : 1));
+    o.hidden_parts = at; at = align_up(at + parts * tokens * row);
+    o.weight_parts = at; at = align_up(at + parts * o.piece * row);
   }
   o.total = at;
   return o;
@@ -190,6 +191,8 @@ dmc::LossArgs loss_args(dmc_retrofit_t h, int32_t n, const void* hidden, const v
   a.targets = targets;
   a.piece = h->at.piece;
   a.grad = h->base + h->at.grad;
+  a.hidden_parts = h->base + h->at.hidden_parts;
+  a.weight_parts = h->base + h->at.weight_parts;
   a.dh = reinterpret_cast<float*>(h->base + h->at.dh);
   a.part_m = reinterpret_cast<float*>(h->base + h->at.part_m);
   a.part_l = reinterpret_cast<float*>(h->base + h->at.part_l);
@@ -346,10 +349,8 @@ dmc_status dmc_retrofit_loss(dmc_retrofit_t h, int32_t num_tokens, const void* h
   dmc::LossArgs a = loss_args(h, num_tokens, hidden_dev, weight_dev, targets_dev);
   a.loss = loss_dev;
   a.lse = lse_dev;
-  int shares = 0;
-  const cudaError_t e = (bf16(h) ? dmc::loss_forward_bf16 : dmc::loss_forward_f32)(a, &shares, stream);
-  if (e != cudaSuccess) return DMC_ERR_CUDA;
-  dmc::loss_join_kernel<<<dmc::ceil_div(a.N, 8), 256, 0, stream>>>(a, shares);
+  if (dmc::loss_forward(a, bf16(h), stream) != cudaSuccess) return DMC_ERR_CUDA;
+  dmc::loss_join_kernel<<<dmc::ceil_div(a.N, 8), 256, 0, stream>>>(a, dmc::ceil_div(a.V, dmc::kLossShare));
   return dmc::cuda_status(cudaGetLastError());
 }
 
@@ -370,7 +371,7 @@ dmc_status dmc_retrofit_loss_backward(dmc_retrofit_t h, int32_t num_tokens, cons
   a.dloss = dloss_dev;
   a.dhidden = dhidden_dev;
   a.dweight = dweight_dev;
-  return dmc::cuda_status((bf16(h) ? dmc::loss_backward_bf16 : dmc::loss_backward_f32)(a, stream));
+  return dmc::cuda_status(dmc::loss_backward(a, bf16(h), stream));
 }
 
 dmc_status dmc_retrofit_status(dmc_retrofit_t h, cudaStream_t stream, uint32_t* bits) {

@@ -122,17 +122,19 @@ struct LossArgs {
   float *loss, *lse;
   const float* dloss;
   void *dhidden, *dweight;
-  int piece;            // words of one piece of the backward pass
-  void* grad;           // scratch, [N][piece]: gradient of a piece's logits
-  float* dh;            // scratch, [N][H]: dhidden of the pieces so far
-  float *part_m, *part_l;  // scratch, [splits][N]: maximum and sum of a share of the vocabulary
-  float* target_logit;  // scratch, [N]
+  int piece;            // words of one piece of the backward pass (fp32: of both)
+  // scratch
+  void* grad;           // [N][piece] in bf16 (fp32: three parts): gradient of a piece's logits
+  void *hidden_parts, *weight_parts;  // fp32: [3][N][stride], [3][piece][stride]
+  float* dh;            // bf16: [N][H]: dhidden of the pieces so far
+  float *part_m, *part_l;  // [shares][N]: maximum and sum of half a tile of the vocabulary
+  float* target_logit;  // [N]
   unsigned int* error;
 };
 
-// Shares of the vocabulary that a token's maximum and sum are kept for: a tile of the
-// tensor-core kernel, at most kLossSplits for the CUDA cores
-constexpr int kLossTile = 256, kLossSplits = 160;
-inline int loss_shares(bool bf16, int vocab) { return bf16 ? ceil_div(vocab, kLossTile) : kLossSplits; }
+// Words of a tile of the vocabulary; a token's maximum and sum are kept for each half of one
+constexpr int kLossTile = 256, kLossShare = kLossTile / 2;
+// Row length of an fp32 matrix's bf16 parts: rows of multiples of 16 bytes
+inline int loss_stride(int H) { return (H + 7) / 8 * 8; }
 
 }  // namespace dmc

@@ -1,5 +1,5 @@
-// Attention of packed sequences and cross entropy on the CUDA cores, with their
-// gradients: every product and sum in fp32.
+// Attention of packed sequences in fp32 on the CUDA cores, with its gradients: every product
+// and sum in fp32.
 //
 // All products are built from tiles of 64 x 64 in shared memory, a block of 16 x 16
 // threads with 4 rows x 4 (or D / 16) columns each; rows are padded by 16 bytes, so
@@ -337,158 +337,6 @@ cudaError_t attn_b(const AttnArgs& a, cudaStream_t stream) {
   return cudaGetLastError();
 }
 
-// ---------------------------------------------------------------- cross entropy
-
-constexpr int kK = 64;  // columns of a K step (a tile of kK + 4 per row)
-
-// acc += A[64 rows from r0] . B[64 rows from c0]^T over all H columns
-__device__ __forceinline__ void logits_tile(float (&acc)[4][4], float* X, float* Y, const LossArgs& a, int r0, int c0) {
-  for (int k = 0; k < a.H; k += kK) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * kT * (kK / 2); i += kThreads) {
-      const int side = i / (kT * (kK / 2)), r = i % (kT * (kK / 2)) / (kK / 2), c = i % (kK / 2) * 2;
-      const int row = (side ? c0 : r0) + r;
-      float2 f = make_float2(0.f, 0.f);
-      if (row < (side ? a.V : a.N) && k + c < a.H)
-        f = *reinterpret_cast<const float2*>(static_cast<const float*>(side ? a.weight : a.hidden) + (long long)row * a.H + k + c);
-      *reinterpret_cast<float2*>((side ? Y : X) + r * (kK + 4) + c) = f;
-    }
-    __syncthreads();
-    dot_tile<kK>(acc, X, Y);
-  }
-}
-
-// Maximum and sum of exponentials of a share of the vocabulary for 64 tokens
-__global__ void __launch_bounds__(kThreads) loss_kernel(const LossArgs a, int tiles) {
-  __shared__ __align__(16) float X[kT * (kK + 4)], Y[kT * (kK + 4)];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, r0 = blockIdx.x * kT;
-  float m[4], l[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) m[i] = -INFINITY, l[i] = 0.f;
-  const int c_end = min((long long)a.V, ((long long)blockIdx.y + 1) * tiles * kT);
-  for (int c0 = blockIdx.y * tiles * kT; c0 < c_end; c0 += kT) {
-    float s[4][4] = {};
-    logits_tile(s, X, Y, a, r0, c0);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = r0 + ty + 16 * i;
-      const int target = row < a.N ? a.targets[row] : -1;
-      float mt = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int word = c0 + tx + 16 * j;
-        if (word >= a.V) s[i][j] = -INFINITY;
-        if (word == target) a.target_logit[row] = s[i][j];
-        mt = fmaxf(mt, s[i][j]);
-      }
-      const float mn = fmaxf(m[i], row_max(mt)), ref = mn == -INFINITY ? 0.f : mn;
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum += expf(s[i][j] - ref);
-      l[i] = fmaf(l[i], expf(m[i] - ref), row_sum(sum));
-      m[i] = mn;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = r0 + ty + 16 * i;
-    if (tx == 0 && row < a.N) {
-      a.part_m[(long long)blockIdx.y * a.N + row] = m[i];
-      a.part_l[(long long)blockIdx.y * a.N + row] = l[i];
-    }
-  }
-}
-
-// The gradient of a piece's logits: (softmax - [word = target]) dloss
-__global__ void __launch_bounds__(kThreads) loss_grad_kernel(const LossArgs a, int v0) {
-  __shared__ __align__(16) float X[kT * (kK + 4)], Y[kT * (kK + 4)];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, r0 = blockIdx.x * kT, c0 = v0 + blockIdx.y * kT;
-  float s[4][4] = {};
-  logits_tile(s, X, Y, a, r0, c0);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = r0 + ty + 16 * i;
-    if (row >= a.N) continue;
-    const int target = a.targets[row];
-    const bool counts = target >= 0 && target < a.V;
-    const float lse = a.lse[row], d = counts ? a.dloss[row] : 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int word = c0 + tx + 16 * j;
-      const float p = expf(s[i][j] - lse) - (word == target ? 1.f : 0.f);
-      if (word - v0 < a.piece)
-        static_cast<float*>(a.grad)[(long long)row * a.piece + word - v0] = counts && word < a.V ? p * d : 0.f;
-    }
-  }
-}
-
-// C[64 x 64 tile] = sum over r of A(i, r) B[r][c]: dhidden (A = grad, r over the piece's
-// words, added to what the pieces before gave) and dweight (A = grad^T, r over the tokens)
-template <bool kWords>
-__global__ void __launch_bounds__(kThreads) loss_product_kernel(const LossArgs a, int v0, bool first, bool last) {
-  __shared__ __align__(16) float W[kT * kW], Y[kT * (64 + 4)];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, i0 = blockIdx.x * kT, c0 = blockIdx.y * 64;
-  const int words = min(a.piece, a.V - v0);
-  const int rows = kWords ? words : a.N, sum = kWords ? a.N : words;  // rows of C, terms of its sums
-  const float* B = static_cast<const float*>(kWords ? a.hidden : a.weight) + (kWords ? 0 : (long long)v0 * a.H);
-  const float* grad = static_cast<const float*>(a.grad);
-  float4 acc[4][1] = {};
-  for (int r0 = 0; r0 < sum; r0 += kT) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < kT * kT; i += kThreads) {
-      const int hi = i / kT, lo = i % kT;  // lo runs over grad's columns
-      const int tok = kWords ? r0 + hi : i0 + hi, word = kWords ? i0 + lo : r0 + lo;
-      const float g = tok < a.N && word < words ? grad[(long long)tok * a.piece + word] : 0.f;
-      W[kWords ? lo * kW + hi : hi * kW + lo] = g;
-    }
-    for (int i = threadIdx.x; i < kT * 32; i += kThreads) {
-      const int r = i / 32, c = i % 32 * 2;
-      float2 f = make_float2(0.f, 0.f);
-      if (r0 + r < sum && c0 + c < a.H)
-        f = *reinterpret_cast<const float2*>(B + (long long)(r0 + r) * a.H + c0 + c);
-      *reinterpret_cast<float2*>(Y + r * 68 + c) = f;
-    }
-    __syncthreads();
-    sum_tile<64>(acc, W, Y);
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = i0 + ty + 16 * i, col = c0 + 4 * tx;
-    if (row >= rows || col >= a.H) continue;
-    const long long at = (long long)(kWords ? v0 + row : row) * a.H + col;
-    float4 f = acc[i][0];
-    if (!kWords && !first) {
-      const float4 o = *reinterpret_cast<const float4*>(a.dh + at);
-      f = make_float4(f.x + o.x, f.y + o.y, f.z + o.z, f.w + o.w);
-    }
-    if (kWords)
-      store4(static_cast<float*>(a.dweight) + at, f);
-    else if (last)
-      store4(static_cast<float*>(a.dhidden) + at, f);
-    else
-      *reinterpret_cast<float4*>(a.dh + at) = f;
-  }
-}
-
-cudaError_t loss_f(const LossArgs& a, int* shares, cudaStream_t stream) {
-  const int rows = ceil_div(a.N, kT), cols = ceil_div(a.V, kT);
-  const int tiles = ceil_div(cols, min(cols, min(kLossSplits, max(1, 608 / rows))));
-  *shares = ceil_div(cols, tiles);
-  loss_kernel<<<dim3(rows, *shares), kThreads, 0, stream>>>(a, tiles);
-  return cudaGetLastError();
-}
-
-cudaError_t loss_b(const LossArgs& a, cudaStream_t stream) {
-  const int rows = ceil_div(a.N, kT), cols = ceil_div(a.H, 64);
-  for (int v0 = 0; v0 < a.V; v0 += a.piece) {
-    const int words = min(a.piece, a.V - v0);
-    loss_grad_kernel<<<dim3(rows, ceil_div(words, kT)), kThreads, 0, stream>>>(a, v0);
-    loss_product_kernel<false><<<dim3(rows, cols), kThreads, 0, stream>>>(a, v0, v0 == 0, v0 + a.piece >= a.V);
-    loss_product_kernel<true><<<dim3(ceil_div(words, kT), cols), kThreads, 0, stream>>>(a, v0, false, false);
-  }
-  return cudaGetLastError();
-}
-
 }  // namespace
 
 cudaError_t attn_forward_f32(const AttnArgs& a, int D, cudaStream_t stream) {
@@ -497,7 +345,5 @@ cudaError_t attn_forward_f32(const AttnArgs& a, int D, cudaStream_t stream) {
 cudaError_t attn_backward_f32(const AttnArgs& a, int D, cudaStream_t stream) {
   return D == 128 ? attn_b<128>(a, stream) : attn_b<64>(a, stream);
 }
-cudaError_t loss_forward_f32(const LossArgs& a, int* shares, cudaStream_t stream) { return loss_f(a, shares, stream); }
-cudaError_t loss_backward_f32(const LossArgs& a, cudaStream_t stream) { return loss_b(a, stream); }
 
 }  // namespace dmc

@@ -1,4 +1,4 @@
-// Cross entropy against a vocabulary and its gradient in bf16, on the tensor cores.
+// Cross entropy against a vocabulary and its gradient on the tensor cores, in bf16 and in fp32.
 //
 // One matrix product with four operand layouts and ends (C is never the logits):
 //   statistics   hidden W^T, per token and tile of 256 words the maximum and the sum of
@@ -7,6 +7,11 @@
 //                rounded to bf16 for the products that follow, for one piece of the words
 //   dhidden      g W, added up over the pieces in fp32
 //   dweight      g^T hidden
+// In fp32 every operand x is the sum of three bf16 numbers, x0 = bf16(x), x1 = bf16(x - x0), x2 =
+// bf16(x - x0 - x1), which hold its 24 bits; a product is the sum of the six products of parts
+// whose indices add up to at most 2 (what is left out is below 2^-24 of the whole), the smallest
+// first, in the same fp32 accumulator. Six passes over K at the tensor cores' rate are about four
+// times as fast as fp32 multiply-adds.
 // 8 N H V operations for a forward and a backward pass, of which 6 are the least
 // possible: the logits of N tokens and V words in fp32 would be kept otherwise.
 //
@@ -14,11 +19,17 @@
 // tcgen05.mma with cta_group::2, M = N = 256, K = 16, issued by the even CTA, both
 // operands split between the two CTAs' shared memory, so that an SM loads 32 KB per 64
 // columns of K where one CTA alone would load 48 KB for its 128 x 256 (the SMs' share of
-// L2 bandwidth is about what the former needs). Warps are specialised: warp 4 loads
-// tiles by TMA into a ring of six, warp 5 issues the products, warps 0-3 (a row of C
+// L2 bandwidth is about what the former needs). Warps are specialised: warp 8 loads
+// tiles by TMA into a ring of six, warp 9 issues the products, warps 0-7 (half a row of C
 // per thread) work on the result of one tile while the next is computed: two
 // accumulators of 256 columns fill the tensor memory. Clusters walk over the tiles with a
 // fixed stride, down groups of rows, so that both operands of the tiles in flight are in L2.
+//
+// The tensor cores' accumulator drops the bits below its last one at every step of 16 terms, which
+// shrinks a sum by about 2^-25 per step: over 4096 terms log-sums came out 1.3e-6 too small, where
+// rounded fp32 sums are 4e-8 off. Where the result is fp32 the row warps therefore take the
+// sums out of tensor memory every 1024 terms (256 in fp32 products) and add them up rounded;
+// what is rounded to bf16 afterwards is left in one accumulator.
 #include <math.h>
 
 #include "dmc_retrofit.cuh"
@@ -33,7 +44,8 @@ constexpr int kN = kLossTile;  // columns of C
 constexpr int kK = 64;         // columns of a step
 constexpr int kStages = 6;
 constexpr int kHalf = 128 * kK * 2;  // bytes of a CTA's half of an operand's tile
-constexpr int kProductThreads = 192;
+constexpr int kProductThreads = 320;
+constexpr int kHalfN = kN / 2;   // columns of a row thread
 
 struct ProductShared {
   unsigned char a[kStages][kHalf], b[kStages][kHalf];
@@ -50,6 +62,7 @@ enum class End { kStats, kGrad, kHidden, kWeight };
 struct ProductArgs {
   LossArgs a;
   int rows, cols, depth;  // C is rows x cols, depth its sums' terms
+  int passes;             // over depth: products of the operands' parts
   int group;              // row tiles of a group
   int v0;                 // first word of the piece
   bool first, last;       // of the pieces
@@ -76,13 +89,16 @@ __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // TMA load into this CTA's shared memory that completes on a barrier of the cluster
-__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int part) {
   asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], "
-      "[%2];" ::"r"(dst),
-      "l"(map), "r"(bar), "r"(x), "r"(y)
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, "
+      "%5}], [%2];" ::"r"(dst),
+      "l"(map), "r"(bar), "r"(x), "r"(y), "r"(part)
       : "memory");
 }
+// the operands' parts in pass i of six (of one: parts 0): (2, 0), (0, 2), (1, 1), (1, 0), (0, 1), (0, 0)
+__device__ __forceinline__ int part_a(int passes, int i) { return passes == 1 ? 0 : (0x201100 >> (4 * (5 - i))) & 15; }
+__device__ __forceinline__ int part_b(int passes, int i) { return passes == 1 ? 0 : (0x021010 >> (4 * (5 - i))) & 15; }
 __device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -113,10 +129,12 @@ __device__ __forceinline__ Tile tile_of(const ProductArgs& p, int u) {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-template <End kEnd>
+template <End kEnd, bool kF32>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
 loss_product_kernel(const __grid_constant__ ProductArgs p) {
   // operands whose rows run along the sums' terms are MN-major
+  // sums leave tensor memory every few steps, see above
+  constexpr bool kOften = kF32 || kEnd == End::kStats;
   constexpr bool kAmn = kEnd == End::kWeight, kBmn = kEnd == End::kHidden || kEnd == End::kWeight;
   extern __shared__ unsigned char smem_raw[];
   ProductShared& sh = *reinterpret_cast<ProductShared*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
@@ -127,6 +145,8 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
   const int clusters = gridDim.x / 2, cluster = blockIdx.x / 2;
   const int tiles = ((p.rows + kM - 1) / kM) * ((p.cols + kN - 1) / kN);
   const int steps = (p.depth + kK - 1) / kK;
+  const int all = steps * p.passes;  // steps of a tile
+  const int chunk = kF32 ? 4 : kOften ? 16 : all;  // of them in one accumulator
   volatile int* s_abort = &sh.abort;
   auto wait = [&](uint64_t* bar, uint32_t ph) -> bool { return warp_wait(smem_u32(bar), ph, s_abort, a.error); };
 
@@ -137,12 +157,12 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&sh.done[i]), 1);
-      mbar_init(smem_u32(&sh.taken[i]), 8);  // the four row warps of both CTAs
+      mbar_init(smem_u32(&sh.taken[i]), 16);  // the eight row warps of both CTAs
     }
     fence_mbar_init();
     sh.abort = 0;
   }
-  if (warp == 5) {
+  if (warp == 9) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(512));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
   }
@@ -152,15 +172,16 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
   tc_fence_after();
   const uint32_t tmem = tc_uniform(sh.tmem);
 
-  if (warp == 4) {
+  if (warp == 8) {
     // ---------------------------------------------------------------- loads
     uint32_t n = 0;
     bool ok = true;
     for (int u = cluster; u < tiles && ok; u += clusters) {
       const Tile t = tile_of(p, u);
       const int m = t.m + (int)rank * 128, c = t.n + (int)rank * 128;  // this CTA's half
+      int k = 0, pass = 0, pa = part_a(p.passes, 0), pb = part_b(p.passes, 0);
 #pragma unroll 1
-      for (int k = 0; k < steps; ++k, ++n) {
+      for (int x = 0; x < steps * p.passes; ++x, ++n) {
         const int s = n % kStages;
         ok = wait(&sh.empty[s], ((n / kStages) & 1) ^ 1);
         if (!ok) break;
@@ -169,25 +190,31 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
           const uint32_t bar = in_leader(smem_u32(&sh.full[s]));
           const uint32_t da = smem_u32(sh.a[s]), db = smem_u32(sh.b[s]);
           if (kAmn) {
-            tma_load_pair(da, &p.ma, bar, m, k * kK);
-            tma_load_pair(da + kHalf / 2, &p.ma, bar, m + 64, k * kK);
+            tma_load_pair(da, &p.ma, bar, m, k * kK, pa);
+            tma_load_pair(da + kHalf / 2, &p.ma, bar, m + 64, k * kK, pa);
           } else {
-            tma_load_pair(da, &p.ma, bar, k * kK, m);
+            tma_load_pair(da, &p.ma, bar, k * kK, m, pa);
           }
           if (kBmn) {
-            tma_load_pair(db, &p.mb, bar, c, k * kK);
-            tma_load_pair(db + kHalf / 2, &p.mb, bar, c + 64, k * kK);
+            tma_load_pair(db, &p.mb, bar, c, k * kK, pb);
+            tma_load_pair(db + kHalf / 2, &p.mb, bar, c + 64, k * kK, pb);
           } else {
-            tma_load_pair(db, &p.mb, bar, k * kK, c);
+            tma_load_pair(db, &p.mb, bar, k * kK, c, pb);
           }
         }
         __syncwarp();
+        if (++k == steps) {
+          k = 0;
+          ++pass;
+          pa = part_a(p.passes, pass);
+          pb = part_b(p.passes, pass);
+        }
       }
     }
     // the last tiles have been read (so every copy has landed, and every signal has come)
     for (uint32_t i = n > kStages ? n - kStages : 0; i < n; ++i)
       mbar_wait(smem_u32(&sh.empty[i % kStages]), (i / kStages) & 1, a.error);
-  } else if (warp == 5) {
+  } else if (warp == 9) {
     // ---------------------------------------------------------------- products
     if (rank == 0) {
       constexpr uint32_t idesc = tc_idesc(kM, kN, kAmn, kBmn);
@@ -195,42 +222,47 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
       // row per 128 bytes, the next 64 half a tile on
       const uint64_t da = tc_desc(smem_u32(sh.a[0]), kAmn ? kHalf / 2 : 16, 1024);
       const uint64_t db = tc_desc(smem_u32(sh.b[0]), kBmn ? kHalf / 2 : 16, 1024);
-      uint32_t n = 0, tile = 0;
+      uint32_t n = 0, sums = 0;  // steps, accumulators begun
       bool ok = true;
-      for (int u = cluster; u < tiles && ok; u += clusters, ++tile) {
-        const uint32_t acc = tile & 1;
-        ok = wait(&sh.taken[acc], ((tile >> 1) & 1) ^ 1);
-        if (!ok) break;
-        tc_fence_after();
+      for (int u = cluster; u < tiles && ok; u += clusters) {
 #pragma unroll 1
-        for (int k = 0; k < steps; ++k, ++n) {
-          const int s = n % kStages;
-          ok = wait(&sh.full[s], (n / kStages) & 1);
+        for (int k0 = 0; k0 < all && ok; k0 += chunk, ++sums) {
+          const uint32_t acc = sums & 1;
+          const int end = min(all, k0 + chunk);
+          ok = wait(&sh.taken[acc], ((sums >> 1) & 1) ^ 1);
           if (!ok) break;
-          if (tc_elect()) {
-            tc_fence_after();
+          tc_fence_after();
+#pragma unroll 1
+          for (int k = k0; k < end; ++k, ++n) {
+            const int s = n % kStages;
+            ok = wait(&sh.full[s], (n / kStages) & 1);
+            if (!ok) break;
+            if (tc_elect()) {
+              tc_fence_after();
 #pragma unroll
-            for (int kk = 0; kk < kK / 16; ++kk)
-              mma_pair(tmem + acc * kN, da + (s * kHalf + kk * (kAmn ? 2048 : 32)) / 16,
-                       db + (s * kHalf + kk * (kBmn ? 2048 : 32)) / 16, idesc, k > 0 || kk > 0);
-            commit_pair(smem_u32(&sh.empty[s]));
-            if (k == steps - 1) commit_pair(smem_u32(&sh.done[acc]));
+              for (int kk = 0; kk < kK / 16; ++kk)
+                mma_pair(tmem + acc * kN, da + (s * kHalf + kk * (kAmn ? 2048 : 32)) / 16,
+                         db + (s * kHalf + kk * (kBmn ? 2048 : 32)) / 16, idesc, k > k0 || kk > 0);
+              commit_pair(smem_u32(&sh.empty[s]));
+              if (k == end - 1) commit_pair(smem_u32(&sh.done[acc]));
+            }
+            __syncwarp();
           }
-          __syncwarp();
         }
       }
       // the other CTA's signals have come
-      for (uint32_t i = tile > 2 ? tile - 2 : 0; i < tile; ++i)
+      for (uint32_t i = sums > 2 ? sums - 2 : 0; i < sums; ++i)
         mbar_wait(smem_u32(&sh.taken[i & 1]), (i >> 1) & 1, a.error);
     }
   } else {
     // ---------------------------------------------------------------- rows
-    const uint32_t t_row = tmem + ((uint32_t)(warp * 32) << 16);
-    uint32_t tile = 0;
-    for (int u = cluster; u < tiles; u += clusters, ++tile) {
+    const int half = warp >> 2;  // of the tile's columns
+    const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * kHalfN;
+    uint32_t sums = 0;
+    bool ok = true;
+    for (int u = cluster; u < tiles && ok; u += clusters) {
       const Tile t = tile_of(p, u);
-      const uint32_t acc = tile & 1;
-      const int row = t.m + (int)rank * 128 + tid;
+      const int row = t.m + (int)rank * 128 + (warp & 3) * 32 + lane, col = t.n + half * kHalfN;
       const bool in = row < p.rows;
       // what the row needs beside C is on its way while the product runs
       int target = -1;
@@ -243,117 +275,195 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
         lse = a.lse[row] * kLog2e;
         d = target >= 0 ? a.dloss[row] : 0.f;
       }
-      if (!wait(&sh.done[acc], (tile >> 1) & 1)) break;
-      tc_fence_after();
-      float mx = -INFINITY, sum = 0.f, hit = 0.f;
-      const int word0 = (kEnd == End::kGrad ? p.v0 : 0) + t.n;
-      const bool mine = target >= word0 && target < word0 + kN;
-      const bool any = (kEnd == End::kStats || kEnd == End::kGrad) && __any_sync(0xffffffffu, mine);
-#pragma unroll 1
-      for (int c = 0; c < kN; c += 32) {
-        if (t.n + c >= p.cols) break;
-        float f[32];
-        tc_ld32(t_row + acc * kN + c, f);
-        tc_wait_ld();
-        const int left = p.cols - (t.n + c);  // columns that count
-        if (kEnd == End::kStats) {
-          if (any)
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (target == word0 + c + i) hit = f[i];
-          if (left < 32)
-#pragma unroll
-            for (int i = 0; i < 32; ++i) f[i] = i < left ? f[i] : -INFINITY;
-          float m4[4] = {f[0], f[1], f[2], f[3]};
-#pragma unroll
-          for (int i = 4; i < 32; ++i) m4[i & 3] = fmaxf(m4[i & 3], f[i]);
-          const float m = fmaxf(mx, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])));
-          const float ref = m == -INFINITY ? 0.f : m * kLog2e;
-          sum *= ex2f(mx * kLog2e - ref);
-          mx = m;
-          float s4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int i = 0; i < 32; ++i) s4[i & 3] += ex2f(fmaf(f[i], kLog2e, -ref));
-          sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-        }
+      const int left = p.cols - col;  // columns that count (may be over 128 or below 1)
+      const int word0 = p.v0 + col;
+      // the end of the columns c .. c + 15
+      auto finish = [&](int c, float* f) {
+        if (!in || c >= left) return;
         if (kEnd == End::kGrad) {
+          char* g = static_cast<char*>(a.grad) + ((long long)row * a.piece + col + c) * 2;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
+          for (int i = 0; i < 16; ++i) {
             const float pr = ex2f(fmaf(f[i], kLog2e, -lse));
             // an ignored position's gradient is zero whatever its logits are
-            f[i] = target >= 0 ? ((any && target == word0 + c + i) ? pr - 1.f : pr) * d : 0.f;
+            f[i] = target >= 0 ? (target == word0 + c + i ? pr - 1.f : pr) * d : 0.f;
           }
-          if (in) {
-            char* g = static_cast<char*>(a.grad) + ((long long)row * a.piece + t.n + c) * 2;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (8 * i < left)  // (the piece's rows are multiples of 16 bytes)
-                reinterpret_cast<uint4*>(g)[i] = Chunk<__nv_bfloat16>::pack(f + 8 * i);
+          for (int part = 0; part < (kF32 ? 3 : 1); ++part) {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              w[i] = Chunk<__nv_bfloat16>::pack2(f[2 * i], f[2 * i + 1]);
+              if (kF32) {  // what is left for the next part
+                float lo, hi;
+                Chunk<__nv_bfloat16>::unpack2(w[i], lo, hi);
+                f[2 * i] -= lo;
+                f[2 * i + 1] -= hi;
+              }
+            }
+            uint4* dst = reinterpret_cast<uint4*>(g + (long long)part * a.N * a.piece * 2);
+            dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            if (c + 8 < left) dst[1] = make_uint4(w[4], w[5], w[6], w[7]);  // (the piece's rows are multiples of 16 bytes)
           }
         }
         if (kEnd == End::kHidden || kEnd == End::kWeight) {
-          const long long at = (long long)(kEnd == End::kWeight ? p.v0 + row : row) * a.H + t.n + c;
-          if (in) {
-            if (kEnd == End::kHidden && !p.first) {
+          const long long at = (long long)(kEnd == End::kWeight ? p.v0 + row : row) * a.H + col + c;
+          // in fp32 the pieces are added up where the result goes
+          float* sum = kF32 ? static_cast<float*>(kEnd == End::kWeight ? a.dweight : a.dhidden) : a.dh;
+          if (kEnd == End::kHidden && !p.first) {
 #pragma unroll
-              for (int i = 0; i < 8; ++i)
-                if (4 * i < left) {
-                  const float4 o = *reinterpret_cast<const float4*>(a.dh + at + 4 * i);
-                  f[4 * i] += o.x;
-                  f[4 * i + 1] += o.y;
-                  f[4 * i + 2] += o.z;
-                  f[4 * i + 3] += o.w;
-                }
-            }
-            if (kEnd == End::kWeight || p.last) {
-              uint4* out = reinterpret_cast<uint4*>(static_cast<char*>(kEnd == End::kWeight ? a.dweight : a.dhidden) + at * 2);
+            for (int i = 0; i < 16; i += 4)
+              if (c + i < left) {
+                const float4 o = *reinterpret_cast<const float4*>(sum + at + i);
+                f[i] += o.x;
+                f[i + 1] += o.y;
+                f[i + 2] += o.z;
+                f[i + 3] += o.w;
+              }
+          }
+          if (!kF32 && (kEnd == End::kWeight || p.last)) {
+            uint4* out = reinterpret_cast<uint4*>(static_cast<char*>(kEnd == End::kWeight ? a.dweight : a.dhidden) + at * 2);
+            out[0] = Chunk<__nv_bfloat16>::pack(f);
+            if (c + 8 < left) out[1] = Chunk<__nv_bfloat16>::pack(f + 8);
+          } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (8 * i < left) out[i] = Chunk<__nv_bfloat16>::pack(f + 8 * i);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                if (4 * i < left)
-                  *reinterpret_cast<float4*>(a.dh + at + 4 * i) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
-            }
+            for (int i = 0; i < 16; i += 4)
+              if (c + i < left) *reinterpret_cast<float4*>(sum + at + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
           }
         }
+      };
+      auto release = [&](uint32_t acc) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_cluster(in_leader(smem_u32(&sh.taken[acc])));
+      };
+      if (!kOften) {
+        const uint32_t acc = sums & 1;
+        if (!(ok = wait(&sh.done[acc], (sums >> 1) & 1))) break;
+        tc_fence_after();
+#pragma unroll 1
+        for (int c = 0; c < kHalfN; c += 32) {
+          float f[32];
+          tc_ld32(t_row + acc * kN + c, f);
+          tc_wait_ld();
+          finish(c, f);
+          finish(c + 16, f + 16);
+        }
+        release(acc);
+        ++sums;
+        continue;
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) arrive_cluster(in_leader(smem_u32(&sh.taken[acc])));
-      if (kEnd == End::kStats && in) {
-        a.part_m[(long long)(t.n / kN) * a.N + row] = mx;
-        a.part_l[(long long)(t.n / kN) * a.N + row] = sum;
-        if (mine) a.target_logit[row] = hit;
+      float f[kHalfN];
+#pragma unroll 1
+      for (int k0 = 0; k0 < all; k0 += chunk, ++sums) {
+        const uint32_t acc = sums & 1;
+        if (!(ok = wait(&sh.done[acc], (sums >> 1) & 1))) break;
+        tc_fence_after();
+        if (k0 == 0) {
+#pragma unroll
+          for (int c = 0; c < kHalfN; c += 32) tc_ld32(t_row + acc * kN + c, f + c);
+          tc_wait_ld();
+        } else {
+#pragma unroll
+          for (int c = 0; c < kHalfN; c += 16) {
+            float g[16];
+            tc_ld16(t_row + acc * kN + c, g);
+            tc_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) f[c + i] += g[i];
+          }
+        }
+        release(acc);
+      }
+      if (!ok) break;
+      if (kEnd == End::kStats) {
+        const bool mine = target >= word0 && target < word0 + kHalfN;
+        float hit = 0.f;
+        if (__any_sync(0xffffffffu, mine)) {
+#pragma unroll
+          for (int i = 0; i < kHalfN; ++i)
+            if (target == word0 + i) hit = f[i];
+        }
+        if (left < kHalfN) {
+#pragma unroll
+          for (int i = 0; i < kHalfN; ++i) f[i] = i < left ? f[i] : -INFINITY;
+        }
+        float m4[4] = {f[0], f[1], f[2], f[3]};
+#pragma unroll
+        for (int i = 4; i < kHalfN; ++i) m4[i & 3] = fmaxf(m4[i & 3], f[i]);
+        const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+        const float ref = m == -INFINITY ? 0.f : m;
+        float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kHalfN; ++i) s4[i & 3] += ex2f((f[i] - ref) * kLog2e);
+        if (in && left > 0) {
+          a.part_m[(long long)(word0 / kHalfN) * a.N + row] = m;
+          a.part_l[(long long)(word0 / kHalfN) * a.N + row] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+          if (mine && target < p.v0 + p.cols) a.target_logit[row] = hit;
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < kHalfN; c += 16) finish(c, f + c);
       }
     }
   }
   tc_fence_before();
   __syncthreads();
   cluster_sync();  // neither CTA's shared or tensor memory is in use by the other
-  if (warp == 5) {
+  if (warp == 9) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
   }
 }
 
-// A matrix of `rows` x `cols` in bf16, rows `stride` bytes apart, in boxes of `box` rows x
-// 64 columns; what lies outside reads as zero.
-cudaError_t matrix_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t stride, uint32_t box) {
+// x in fp32, rows of H, as three bf16 numbers that add up to it: parts[3][rows][stride], four
+// elements per thread. Bound by HBM.
+__global__ void __launch_bounds__(256) loss_parts_kernel(const float* x, long long rows, int H, int stride, char* parts) {
+  const int per = H / 4;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * per) return;
+  const long long r = i / per;
+  const int c = (int)(i % per) * 4;
+  const float4 v = *reinterpret_cast<const float4*>(x + r * H + c);
+  float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int part = 0; part < 3; ++part) {
+    uint32_t u[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      u[k] = Chunk<__nv_bfloat16>::pack2(f[2 * k], f[2 * k + 1]);
+      float lo, hi;
+      Chunk<__nv_bfloat16>::unpack2(u[k], lo, hi);
+      f[2 * k] -= lo;
+      f[2 * k + 1] -= hi;
+    }
+    *reinterpret_cast<uint2*>(parts + ((part * rows + r) * stride + c) * 2) = make_uint2(u[0], u[1]);
+  }
+}
+cudaError_t to_parts(const void* x, long long rows, int H, void* parts, cudaStream_t stream) {
+  const long long n = rows * (H / 4);
+  loss_parts_kernel<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(static_cast<const float*>(x), rows, H, loss_stride(H),
+                                                                     static_cast<char*>(parts));
+  return cudaGetLastError();
+}
+
+// An operand: a matrix of `rows` x `cols` in bf16, or its three parts, rows `stride` elements
+// apart, in boxes of `box` rows x 64 columns; what lies outside reads as zero.
+cudaError_t matrix_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t stride, uint32_t box,
+                       int parts) {
   const TensorMapEncode encode = tensor_map_encode();
   if (!encode) return cudaErrorNotSupported;
-  const cuuint64_t dims[2] = {cols, rows}, strides[1] = {stride};
-  const cuuint32_t boxes[2] = {64, box}, unit[2] = {1, 1};
-  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, boxes, unit,
+  const cuuint64_t dims[3] = {cols, rows, (cuuint64_t)parts}, strides[2] = {stride * 2, stride * 2 * rows};
+  const cuuint32_t boxes[3] = {64, box, 1}, unit[3] = {1, 1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, boxes, unit,
                             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <End kEnd>
+template <End kEnd, bool kF32>
 cudaError_t launch_product(ProductArgs& p, cudaStream_t stream) {
-  auto* kernel = loss_product_kernel<kEnd>;
+  auto* kernel = loss_product_kernel<kEnd, kF32>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
   if (e != cudaSuccess) return e;
   int dev = 0, sms = 0;
@@ -361,8 +471,9 @@ cudaError_t launch_product(ProductArgs& p, cudaStream_t stream) {
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
   const long long tm = (p.rows + kM - 1) / kM, tn = (p.cols + kN - 1) / kN;
+  p.passes = kF32 ? 6 : 1;
   // row tiles whose operand takes about a third of L2
-  const long long group = (40ll << 20) / ((long long)kM * p.depth * 2);
+  const long long group = (40ll << 20) / ((long long)kM * p.depth * (kF32 ? 6 : 2));
   p.group = (int)(group < 1 ? 1 : group > tm ? tm : group);
   const long long tiles = tm * tn;
   const int pairs = sms / 2;
@@ -370,49 +481,73 @@ cudaError_t launch_product(ProductArgs& p, cudaStream_t stream) {
   return cudaGetLastError();
 }
 
-}  // namespace
-
-cudaError_t loss_forward_bf16(const LossArgs& a, int* shares, cudaStream_t stream) {
-  ProductArgs p = {};
-  p.a = a;
-  p.rows = a.N;
-  p.cols = a.V;
-  p.depth = a.H;
-  *shares = ceil_div(a.V, kN);
-  cudaError_t e = matrix_map(&p.ma, a.hidden, a.N, a.H, (uint64_t)a.H * 2, 128);
-  if (e == cudaSuccess) e = matrix_map(&p.mb, a.weight, a.V, a.H, (uint64_t)a.H * 2, 128);
-  return e == cudaSuccess ? launch_product<End::kStats>(p, stream) : e;
+template <bool kF32>
+cudaError_t forward(const LossArgs& a, cudaStream_t stream) {
+  const int parts = kF32 ? 3 : 1, stride = kF32 ? loss_stride(a.H) : a.H;
+  cudaError_t e = kF32 ? to_parts(a.hidden, a.N, a.H, a.hidden_parts, stream) : cudaSuccess;
+  // fp32: by pieces, as the weights' parts are made; bf16: all words at once
+  const int piece = kF32 ? a.piece : a.V;
+  for (int v0 = 0; v0 < a.V && e == cudaSuccess; v0 += piece) {
+    const int words = min(piece, a.V - v0);
+    const char* w = static_cast<const char*>(a.weight) + (long long)v0 * a.H * (kF32 ? 4 : 2);
+    if (kF32) e = to_parts(w, words, a.H, a.weight_parts, stream);
+    ProductArgs p = {};
+    p.a = a;
+    p.v0 = v0;
+    p.rows = a.N;
+    p.cols = words;
+    p.depth = a.H;
+    if (e == cudaSuccess) e = matrix_map(&p.ma, kF32 ? a.hidden_parts : a.hidden, a.N, a.H, stride, 128, parts);
+    if (e == cudaSuccess) e = matrix_map(&p.mb, kF32 ? a.weight_parts : w, words, a.H, stride, 128, parts);
+    if (e == cudaSuccess) e = launch_product<End::kStats, kF32>(p, stream);
+  }
+  return e;
 }
 
-cudaError_t loss_backward_bf16(const LossArgs& a, cudaStream_t stream) {
-  const uint64_t row = (uint64_t)a.H * 2, grow = (uint64_t)a.piece * 2;
-  for (int v0 = 0; v0 < a.V; v0 += a.piece) {
+template <bool kF32>
+cudaError_t backward(const LossArgs& a, cudaStream_t stream) {
+  const int parts = kF32 ? 3 : 1, stride = kF32 ? loss_stride(a.H) : a.H;
+  cudaError_t e = kF32 ? to_parts(a.hidden, a.N, a.H, a.hidden_parts, stream) : cudaSuccess;
+  const void* hidden = kF32 ? a.hidden_parts : a.hidden;
+  for (int v0 = 0; v0 < a.V && e == cudaSuccess; v0 += a.piece) {
     ProductArgs p = {};
     p.a = a;
     p.v0 = v0;
     p.first = v0 == 0;
     p.last = a.V - v0 <= a.piece;
     const int words = p.last ? a.V - v0 : a.piece;
-    const char* w = static_cast<const char*>(a.weight) + v0 * row;
+    const char* w = static_cast<const char*>(a.weight) + (long long)v0 * a.H * (kF32 ? 4 : 2);
+    if (kF32) {
+      e = to_parts(w, words, a.H, a.weight_parts, stream);
+      w = static_cast<const char*>(a.weight_parts);
+    }
     p.rows = a.N;
     p.cols = words;
     p.depth = a.H;
-    cudaError_t e = matrix_map(&p.ma, a.hidden, a.N, a.H, row, 128);
-    if (e == cudaSuccess) e = matrix_map(&p.mb, w, words, a.H, row, 128);
-    if (e == cudaSuccess) e = launch_product<End::kGrad>(p, stream);
+    if (e == cudaSuccess) e = matrix_map(&p.ma, hidden, a.N, a.H, stride, 128, parts);
+    if (e == cudaSuccess) e = matrix_map(&p.mb, w, words, a.H, stride, 128, parts);
+    if (e == cudaSuccess) e = launch_product<End::kGrad, kF32>(p, stream);
     p.cols = a.H;
     p.depth = words;
-    if (e == cudaSuccess) e = matrix_map(&p.ma, a.grad, a.N, words, grow, 128);
-    if (e == cudaSuccess) e = matrix_map(&p.mb, w, words, a.H, row, 64);
-    if (e == cudaSuccess) e = launch_product<End::kHidden>(p, stream);
+    if (e == cudaSuccess) e = matrix_map(&p.ma, a.grad, a.N, words, a.piece, 128, parts);
+    if (e == cudaSuccess) e = matrix_map(&p.mb, w, words, a.H, stride, 64, parts);
+    if (e == cudaSuccess) e = launch_product<End::kHidden, kF32>(p, stream);
     p.rows = words;
     p.depth = a.N;
-    if (e == cudaSuccess) e = matrix_map(&p.ma, a.grad, a.N, words, grow, 64);
-    if (e == cudaSuccess) e = matrix_map(&p.mb, a.hidden, a.N, a.H, row, 64);
-    if (e == cudaSuccess) e = launch_product<End::kWeight>(p, stream);
-    if (e != cudaSuccess) return e;
+    if (e == cudaSuccess) e = matrix_map(&p.ma, a.grad, a.N, words, a.piece, 64, parts);
+    if (e == cudaSuccess) e = matrix_map(&p.mb, hidden, a.N, a.H, stride, 64, parts);
+    if (e == cudaSuccess) e = launch_product<End::kWeight, kF32>(p, stream);
   }
-  return cudaSuccess;
+  return e;
+}
+
+}  // namespace
+
+cudaError_t loss_forward(const LossArgs& a, bool bf16, cudaStream_t stream) {
+  return bf16 ? forward<false>(a, stream) : forward<true>(a, stream);
+}
+cudaError_t loss_backward(const LossArgs& a, bool bf16, cudaStream_t stream) {
+  return bf16 ? backward<false>(a, stream) : backward<true>(a, stream);
 }
 
 }  // namespace dmc
