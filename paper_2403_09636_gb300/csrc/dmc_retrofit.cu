@@ -15,7 +15,7 @@ cudaError_t attn_forward_f32(const AttnArgs& a, int D, cudaStream_t stream);
 cudaError_t attn_backward_f32(const AttnArgs& a, int D, cudaStream_t stream);
 cudaError_t attn_backward_bf16(const AttnArgs& a, int D, cudaStream_t stream);
 cudaError_t attn_forward_bf16(const AttnArgs& a, int D, cudaStream_t stream);
-cudaError_t loss_forward(const LossArgs& a, bool bf16, cudaStream_t stream);
+cudaError_t loss_forward(const LossArgs& a, bool bf16, int* share, cudaStream_t stream);
 cudaError_t loss_backward(const LossArgs& a, bool bf16, cudaStream_t stream);
 
 namespace {
@@ -83,8 +83,8 @@ Offsets offsets(const dmc_retrofit_config* c) {
   }
   if (has_loss(*c)) {
     o.piece = loss_piece(c);
-    const size_t shares = ceil_div(c->vocab, kLossShare), parts = c->dtype == DMC_F32 ? 3 : 0;
-    const size_t row = (size_t)loss_stride(c->hidden) * 2;
+    const size_t parts = c->dtype == DMC_F32 ? 3 : 0, row = (size_t)loss_stride(c->hidden) * 2;
+    const size_t shares = ceil_div(c->vocab, kLossTile / 4);  // of half a tile of half the columns at least
     o.part_m = at; at = align_up(at + tokens * shares * 4);
     o.part_l = at; at = align_up(at + tokens * shares * 4);
     o.target_logit = at; at = align_up(at + tokens * 4);
@@ -349,8 +349,9 @@ dmc_status dmc_retrofit_loss(dmc_retrofit_t h, int32_t num_tokens, const void* h
   dmc::LossArgs a = loss_args(h, num_tokens, hidden_dev, weight_dev, targets_dev);
   a.loss = loss_dev;
   a.lse = lse_dev;
-  if (dmc::loss_forward(a, bf16(h), stream) != cudaSuccess) return DMC_ERR_CUDA;
-  dmc::loss_join_kernel<<<dmc::ceil_div(a.N, 8), 256, 0, stream>>>(a, dmc::ceil_div(a.V, dmc::kLossShare));
+  int share = 1;
+  if (dmc::loss_forward(a, bf16(h), &share, stream) != cudaSuccess) return DMC_ERR_CUDA;
+  dmc::loss_join_kernel<<<dmc::ceil_div(a.N, 8), 256, 0, stream>>>(a, dmc::ceil_div(a.V, share));
   return dmc::cuda_status(cudaGetLastError());
 }
 

@@ -132,8 +132,8 @@ struct LossArgs {
   unsigned int* error;
 };
 
-// Words of a tile of the vocabulary; a token's maximum and sum are kept for each half of one
-constexpr int kLossTile = 256, kLossShare = kLossTile / 2;
+// Words of the largest tile of the vocabulary; a token's maximum and sum are kept for each half of one
+constexpr int kLossTile = 256;
 // Row length of an fp32 matrix's bf16 parts: rows of multiples of 16 bytes
 inline int loss_stride(int H) { return (H + 7) / 8 * 8; }
 

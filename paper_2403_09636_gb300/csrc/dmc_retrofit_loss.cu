@@ -40,12 +40,10 @@ namespace dmc {
 namespace {
 
 constexpr int kM = 256;        // rows of C per cluster
-constexpr int kN = kLossTile;  // columns of C
 constexpr int kK = 64;         // columns of a step
 constexpr int kStages = 6;
-constexpr int kHalf = 128 * kK * 2;  // bytes of a CTA's half of an operand's tile
+constexpr int kHalf = 128 * kK * 2;  // bytes of a CTA's half of an operand's tile (of B at most)
 constexpr int kProductThreads = 320;
-constexpr int kHalfN = kN / 2;   // columns of a row thread
 
 struct ProductShared {
   unsigned char a[kStages][kHalf], b[kStages][kHalf];
@@ -117,6 +115,7 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
 struct Tile {
   int m, n;  // first row and column of C
 };
+template <int kN>
 __device__ __forceinline__ Tile tile_of(const ProductArgs& p, int u) {
   const int tm = (p.rows + kM - 1) / kM, tn = (p.cols + kN - 1) / kN;
   const int per = p.group * tn, g = u / per, r = u % per;
@@ -129,9 +128,11 @@ __device__ __forceinline__ Tile tile_of(const ProductArgs& p, int u) {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-template <End kEnd, bool kF32>
+template <End kEnd, bool kF32, int kN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
 loss_product_kernel(const __grid_constant__ ProductArgs p) {
+  constexpr int kHalfN = kN / 2;          // columns of a row thread
+  constexpr int kHalfB = kHalf * kN / 256;  // bytes of a CTA's half of B's tile
   // operands whose rows run along the sums' terms are MN-major
   // sums leave tensor memory every few steps, see above
   constexpr bool kOften = kF32 || kEnd == End::kStats;
@@ -146,7 +147,12 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
   const int tiles = ((p.rows + kM - 1) / kM) * ((p.cols + kN - 1) / kN);
   const int steps = (p.depth + kK - 1) / kK;
   const int all = steps * p.passes;  // steps of a tile
-  const int chunk = kF32 ? 4 : kOften ? 16 : all;  // of them in one accumulator
+  // one past the last step that goes into the accumulator begun at step k (of fp32's passes the
+  // last one alone has large terms)
+  auto chunk_end = [&](int k) -> int {
+    if (kF32) return k < 5 * steps ? 5 * steps : min(all, k + 4);
+    return kOften ? min(all, k + 16) : all;
+  };
   volatile int* s_abort = &sh.abort;
   auto wait = [&](uint64_t* bar, uint32_t ph) -> bool { return warp_wait(smem_u32(bar), ph, s_abort, a.error); };
 
@@ -177,8 +183,8 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
     uint32_t n = 0;
     bool ok = true;
     for (int u = cluster; u < tiles && ok; u += clusters) {
-      const Tile t = tile_of(p, u);
-      const int m = t.m + (int)rank * 128, c = t.n + (int)rank * 128;  // this CTA's half
+      const Tile t = tile_of<kN>(p, u);
+      const int m = t.m + (int)rank * 128, c = t.n + (int)rank * kHalfN;  // this CTA's half
       int k = 0, pass = 0, pa = part_a(p.passes, 0), pb = part_b(p.passes, 0);
 #pragma unroll 1
       for (int x = 0; x < steps * p.passes; ++x, ++n) {
@@ -186,7 +192,7 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
         ok = wait(&sh.empty[s], ((n / kStages) & 1) ^ 1);
         if (!ok) break;
         if (tc_elect()) {
-          if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sh.full[s]), 4 * kHalf);
+          if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sh.full[s]), 2 * (kHalf + kHalfB));
           const uint32_t bar = in_leader(smem_u32(&sh.full[s]));
           const uint32_t da = smem_u32(sh.a[s]), db = smem_u32(sh.b[s]);
           if (kAmn) {
@@ -197,7 +203,7 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
           }
           if (kBmn) {
             tma_load_pair(db, &p.mb, bar, c, k * kK, pb);
-            tma_load_pair(db + kHalf / 2, &p.mb, bar, c + 64, k * kK, pb);
+            if (kN == 256) tma_load_pair(db + kHalfB / 2, &p.mb, bar, c + 64, k * kK, pb);
           } else {
             tma_load_pair(db, &p.mb, bar, k * kK, c, pb);
           }
@@ -221,14 +227,14 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
       // K-major: rows of 128 bytes, eight of them every 1024; MN-major: 64 elements of a
       // row per 128 bytes, the next 64 half a tile on
       const uint64_t da = tc_desc(smem_u32(sh.a[0]), kAmn ? kHalf / 2 : 16, 1024);
-      const uint64_t db = tc_desc(smem_u32(sh.b[0]), kBmn ? kHalf / 2 : 16, 1024);
+      const uint64_t db = tc_desc(smem_u32(sh.b[0]), kBmn ? kHalfB / 2 : 16, 1024);
       uint32_t n = 0, sums = 0;  // steps, accumulators begun
       bool ok = true;
       for (int u = cluster; u < tiles && ok; u += clusters) {
 #pragma unroll 1
-        for (int k0 = 0; k0 < all && ok; k0 += chunk, ++sums) {
+        for (int k0 = 0, end; k0 < all && ok; k0 = end, ++sums) {
           const uint32_t acc = sums & 1;
-          const int end = min(all, k0 + chunk);
+          end = chunk_end(k0);
           ok = wait(&sh.taken[acc], ((sums >> 1) & 1) ^ 1);
           if (!ok) break;
           tc_fence_after();
@@ -261,7 +267,7 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
     uint32_t sums = 0;
     bool ok = true;
     for (int u = cluster; u < tiles && ok; u += clusters) {
-      const Tile t = tile_of(p, u);
+      const Tile t = tile_of<kN>(p, u);
       const int row = t.m + (int)rank * 128 + (warp & 3) * 32 + lane, col = t.n + half * kHalfN;
       const bool in = row < p.rows;
       // what the row needs beside C is on its way while the product runs
@@ -337,7 +343,7 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
         __syncwarp();
         if (lane == 0) arrive_cluster(in_leader(smem_u32(&sh.taken[acc])));
       };
-      if (!kOften) {
+      if constexpr (!kOften) {
         const uint32_t acc = sums & 1;
         if (!(ok = wait(&sh.done[acc], (sums >> 1) & 1))) break;
         tc_fence_after();
@@ -351,11 +357,10 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
         }
         release(acc);
         ++sums;
-        continue;
-      }
+      } else {
       float f[kHalfN];
 #pragma unroll 1
-      for (int k0 = 0; k0 < all; k0 += chunk, ++sums) {
+      for (int k0 = 0; k0 < all; k0 = chunk_end(k0), ++sums) {
         const uint32_t acc = sums & 1;
         if (!(ok = wait(&sh.done[acc], (sums >> 1) & 1))) break;
         tc_fence_after();
@@ -404,6 +409,7 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
       } else {
 #pragma unroll
         for (int c = 0; c < kHalfN; c += 16) finish(c, f + c);
+      }
       }
     }
   }
@@ -461,16 +467,19 @@ cudaError_t matrix_map(CUtensorMap* map, const void* base, uint64_t rows, uint64
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <End kEnd, bool kF32>
-cudaError_t launch_product(ProductArgs& p, cudaStream_t stream) {
-  auto* kernel = loss_product_kernel<kEnd, kF32>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
+// Columns of a tile: 256, or 128 where tiles of 256 would be too few for half of the pairs of
+// SMs: twice as many clusters, each with half the work per step.
+inline int tile_columns(int rows, int cols, int sms) {
+  const long long tiles = (long long)ceil_div(rows, kM) * ceil_div(cols, 256);
+  return tiles * 4 <= sms ? 128 : 256;
+}
+
+template <End kEnd, bool kF32, int kN>
+cudaError_t launch_product(ProductArgs& p, int sms, cudaStream_t stream) {
+  auto* kernel = loss_product_kernel<kEnd, kF32, kN>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
   if (e != cudaSuccess) return e;
-  int dev = 0, sms = 0;
-  e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e != cudaSuccess) return e;
-  const long long tm = (p.rows + kM - 1) / kM, tn = (p.cols + kN - 1) / kN;
+  const long long tm = ceil_div(p.rows, kM), tn = ceil_div(p.cols, kN);
   p.passes = kF32 ? 6 : 1;
   // row tiles whose operand takes about a third of L2
   const long long group = (40ll << 20) / ((long long)kM * p.depth * (kF32 ? 6 : 2));
@@ -481,10 +490,32 @@ cudaError_t launch_product(ProductArgs& p, cudaStream_t stream) {
   return cudaGetLastError();
 }
 
+// C = A B, with the boxes of rows of B's map for its layout
+template <End kEnd, bool kF32>
+cudaError_t product(ProductArgs& p, const void* a, uint64_t a_rows, uint64_t a_cols, uint64_t a_stride, const void* b,
+                    uint64_t b_rows, uint64_t b_cols, uint64_t b_stride, int columns, int sms, cudaStream_t stream) {
+  constexpr bool kAmn = kEnd == End::kWeight, kBmn = kEnd == End::kHidden || kEnd == End::kWeight;
+  const int parts = kF32 ? 3 : 1;
+  cudaError_t e = matrix_map(&p.ma, a, a_rows, a_cols, a_stride, kAmn ? 64 : 128, parts);
+  if (e == cudaSuccess) e = matrix_map(&p.mb, b, b_rows, b_cols, b_stride, kBmn ? 64 : columns / 2, parts);
+  if (e != cudaSuccess) return e;
+  return columns == 128 ? launch_product<kEnd, kF32, 128>(p, sms, stream) : launch_product<kEnd, kF32, 256>(p, sms, stream);
+}
+
+cudaError_t sm_count(int* sms) {
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  return e == cudaSuccess ? cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) : e;
+}
+
 template <bool kF32>
-cudaError_t forward(const LossArgs& a, cudaStream_t stream) {
-  const int parts = kF32 ? 3 : 1, stride = kF32 ? loss_stride(a.H) : a.H;
-  cudaError_t e = kF32 ? to_parts(a.hidden, a.N, a.H, a.hidden_parts, stream) : cudaSuccess;
+cudaError_t forward(const LossArgs& a, int* share, cudaStream_t stream) {
+  const int stride = kF32 ? loss_stride(a.H) : a.H;
+  int sms = 0;
+  cudaError_t e = sm_count(&sms);
+  const int columns = tile_columns(a.N, a.V, sms);
+  *share = columns / 2;
+  if (kF32 && e == cudaSuccess) e = to_parts(a.hidden, a.N, a.H, a.hidden_parts, stream);
   // fp32: by pieces, as the weights' parts are made; bf16: all words at once
   const int piece = kF32 ? a.piece : a.V;
   for (int v0 = 0; v0 < a.V && e == cudaSuccess; v0 += piece) {
@@ -497,17 +528,19 @@ cudaError_t forward(const LossArgs& a, cudaStream_t stream) {
     p.rows = a.N;
     p.cols = words;
     p.depth = a.H;
-    if (e == cudaSuccess) e = matrix_map(&p.ma, kF32 ? a.hidden_parts : a.hidden, a.N, a.H, stride, 128, parts);
-    if (e == cudaSuccess) e = matrix_map(&p.mb, kF32 ? a.weight_parts : w, words, a.H, stride, 128, parts);
-    if (e == cudaSuccess) e = launch_product<End::kStats, kF32>(p, stream);
+    if (e == cudaSuccess)
+      e = product<End::kStats, kF32>(p, kF32 ? a.hidden_parts : a.hidden, a.N, a.H, stride, kF32 ? a.weight_parts : w, words,
+                                     a.H, stride, columns, sms, stream);
   }
   return e;
 }
 
 template <bool kF32>
 cudaError_t backward(const LossArgs& a, cudaStream_t stream) {
-  const int parts = kF32 ? 3 : 1, stride = kF32 ? loss_stride(a.H) : a.H;
-  cudaError_t e = kF32 ? to_parts(a.hidden, a.N, a.H, a.hidden_parts, stream) : cudaSuccess;
+  const int stride = kF32 ? loss_stride(a.H) : a.H;
+  int sms = 0;
+  cudaError_t e = sm_count(&sms);
+  if (kF32 && e == cudaSuccess) e = to_parts(a.hidden, a.N, a.H, a.hidden_parts, stream);
   const void* hidden = kF32 ? a.hidden_parts : a.hidden;
   for (int v0 = 0; v0 < a.V && e == cudaSuccess; v0 += a.piece) {
     ProductArgs p = {};
@@ -524,27 +557,28 @@ cudaError_t backward(const LossArgs& a, cudaStream_t stream) {
     p.rows = a.N;
     p.cols = words;
     p.depth = a.H;
-    if (e == cudaSuccess) e = matrix_map(&p.ma, hidden, a.N, a.H, stride, 128, parts);
-    if (e == cudaSuccess) e = matrix_map(&p.mb, w, words, a.H, stride, 128, parts);
-    if (e == cudaSuccess) e = launch_product<End::kGrad, kF32>(p, stream);
+    if (e == cudaSuccess)
+      e = product<End::kGrad, kF32>(p, hidden, a.N, a.H, stride, w, words, a.H, stride, tile_columns(a.N, words, sms), sms,
+                                    stream);
     p.cols = a.H;
     p.depth = words;
-    if (e == cudaSuccess) e = matrix_map(&p.ma, a.grad, a.N, words, a.piece, 128, parts);
-    if (e == cudaSuccess) e = matrix_map(&p.mb, w, words, a.H, stride, 64, parts);
-    if (e == cudaSuccess) e = launch_product<End::kHidden, kF32>(p, stream);
+    if (e == cudaSuccess)
+      e = product<End::kHidden, kF32>(p, a.grad, a.N, words, a.piece, w, words, a.H, stride, tile_columns(a.N, a.H, sms), sms,
+                                      stream);
     p.rows = words;
     p.depth = a.N;
-    if (e == cudaSuccess) e = matrix_map(&p.ma, a.grad, a.N, words, a.piece, 64, parts);
-    if (e == cudaSuccess) e = matrix_map(&p.mb, hidden, a.N, a.H, stride, 64, parts);
-    if (e == cudaSuccess) e = launch_product<End::kWeight, kF32>(p, stream);
+    if (e == cudaSuccess)
+      e = product<End::kWeight, kF32>(p, a.grad, a.N, words, a.piece, hidden, a.N, a.H, stride, tile_columns(words, a.H, sms),
+                                      sms, stream);
   }
   return e;
 }
 
 }  // namespace
 
-cudaError_t loss_forward(const LossArgs& a, bool bf16, cudaStream_t stream) {
-  return bf16 ? forward<false>(a, stream) : forward<true>(a, stream);
+// share: words of each of the shares whose maxima and sums are left in part_m, part_l
+cudaError_t loss_forward(const LossArgs& a, bool bf16, int* share, cudaStream_t stream) {
+  return bf16 ? forward<false>(a, share, stream) : forward<true>(a, share, stream);
 }
 cudaError_t loss_backward(const LossArgs& a, bool bf16, cudaStream_t stream) {
   return bf16 ? backward<false>(a, stream) : backward<true>(a, stream);
