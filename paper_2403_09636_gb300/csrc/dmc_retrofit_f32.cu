@@ -1,9 +1,13 @@
 // Attention of packed sequences in fp32 on the CUDA cores, with its gradients: every product
 // and sum in fp32.
 //
-// All products are built from tiles of 64 x 64 in shared memory, a block of 16 x 16
-// threads with 4 rows x 4 (or D / 16) columns each; rows are padded by 16 bytes, so
-// that the 16-byte reads of 8 neighbouring rows fall into different banks.
+// All products are built from tiles of kT rows in shared memory, by a block of 16 columns of
+// threads; a thread takes every 16th (kT / 16 of them) and every (threads / 16)-th row. Rows are
+// padded by 16 bytes, so that the 16-byte reads of 8 neighbouring rows fall into different banks.
+// Multiply-adds come in pairs (fma.rn.f32x2), two neighbouring terms of a sum or two
+// neighbouring columns, which leaves issue slots for the reads: 12 reads of 16 bytes per 32 pairs.
+// Tiles of 64 rows, 256 threads; 32 rows and 128 threads where tiles of 64 would leave SMs without
+// a block: twice as many blocks, whose steps take less than half as long.
 #include <math.h>
 
 #include "dmc_retrofit.cuh"
@@ -12,73 +16,89 @@ namespace dmc {
 
 namespace {
 
-constexpr int kT = 64;          // rows of a tile
-constexpr int kThreads = 256;
-constexpr int kW = kT + 4;      // row of a tile of weights
+template <int kRows>
+struct Shape {
+  static constexpr int kT = kRows;                     // rows of a tile
+  static constexpr int kThreads = kRows == 64 ? 256 : 128;
+  static constexpr int kI = kT * 16 / kThreads;        // rows of a thread
+  static constexpr int kJ = kT / 16;                   // columns of a thread
+  static constexpr int kTy = kThreads / 16;
+  static constexpr int kW = kT + 4;                    // row of a tile of weights
+};
 
-// rows [r0, r1) of a matrix of D columns into a tile, zero from r1 on
-template <int D>
+// `rows` rows of D columns, asynchronously, into a tile; zero from there on
+template <int D, class S>
 __device__ __forceinline__ void load_rows(float* tile, const float* src, long long stride, int rows) {
-  for (int i = threadIdx.x; i < kT * (D / 2); i += kThreads) {
-    const int r = i / (D / 2), c = i % (D / 2) * 2;
-    float2 f = make_float2(0.f, 0.f);
-    if (r < rows) f = *reinterpret_cast<const float2*>(src + r * stride + c);
-    *reinterpret_cast<float2*>(tile + r * (D + 4) + c) = f;
+#pragma unroll
+  for (int i = threadIdx.x; i < S::kT * (D / 4); i += S::kThreads) {
+    const int r = i / (D / 4), c = i % (D / 4) * 4;
+    cp_async16_zfill(smem_u32(tile + r * (D + 4) + c), src + (r < rows ? r * stride : 0) + c, r < rows);
   }
 }
 
-// acc[i][j] += X[ty + 16 i] . Y[tx + 16 j]
-template <int D>
-__device__ __forceinline__ void dot_tile(float (&acc)[4][4], const float* X, const float* Y) {
+// acc[i][j] += X[ty + kTy i] . Y[tx + 16 j], even and odd terms apart
+template <int D, class S>
+__device__ __forceinline__ void dot_tile(float2 (&acc)[S::kI][S::kJ], const float* X, const float* Y) {
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-#pragma unroll 2
+#pragma unroll 4
   for (int c = 0; c < D; c += 4) {
-    float4 x[4], y[4];
+    float4 x[S::kI], y[S::kJ];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4*>(X + (ty + 16 * i) * (D + 4) + c);
+    for (int i = 0; i < S::kI; ++i) x[i] = *reinterpret_cast<const float4*>(X + (ty + S::kTy * i) * (D + 4) + c);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = *reinterpret_cast<const float4*>(Y + (tx + 16 * i) * (D + 4) + c);
+    for (int j = 0; j < S::kJ; ++j) y[j] = *reinterpret_cast<const float4*>(Y + (tx + 16 * j) * (D + 4) + c);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < S::kI; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        acc[i][j] = fmaf(x[i].x, y[j].x, acc[i][j]);
-        acc[i][j] = fmaf(x[i].y, y[j].y, acc[i][j]);
-        acc[i][j] = fmaf(x[i].z, y[j].z, acc[i][j]);
-        acc[i][j] = fmaf(x[i].w, y[j].w, acc[i][j]);
+      for (int j = 0; j < S::kJ; ++j) {
+        acc[i][j] = fma2(make_float2(x[i].x, x[i].y), make_float2(y[j].x, y[j].y), acc[i][j]);
+        acc[i][j] = fma2(make_float2(x[i].z, x[i].w), make_float2(y[j].z, y[j].w), acc[i][j]);
       }
   }
 }
 
-// acc[i][4 c ..] += sum over r < 64 of W[ty + 16 i][r] Y[r][4 tx + 64 c ..]
-template <int D>
-__device__ __forceinline__ void sum_tile(float4 (&acc)[4][D / 64], const float* W, const float* Y) {
+// acc[i][2 c], acc[i][2 c + 1] (columns 4 tx + 64 c ..) += sum over r < kT of W[ty + kTy i][r] Y[r][.]
+template <int D, class S>
+__device__ __forceinline__ void sum_tile(float2 (&acc)[S::kI][D / 32], const float* W, const float* Y) {
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll 2
-  for (int r = 0; r < kT; r += 4) {
-    float4 w[4];
+  for (int r = 0; r < S::kT; r += 4) {
+    float4 w[S::kI];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4*>(W + (ty + 16 * i) * kW + r);
+    for (int i = 0; i < S::kI; ++i) w[i] = *reinterpret_cast<const float4*>(W + (ty + S::kTy * i) * S::kW + r);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) {
         const float4 y = *reinterpret_cast<const float4*>(Y + (r + k) * (D + 4) + 4 * tx + 64 * c);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < S::kI; ++i) {
           const float x = k == 0 ? w[i].x : k == 1 ? w[i].y : k == 2 ? w[i].z : w[i].w;
-          acc[i][c].x = fmaf(x, y.x, acc[i][c].x);
-          acc[i][c].y = fmaf(x, y.y, acc[i][c].y);
-          acc[i][c].z = fmaf(x, y.z, acc[i][c].z);
-          acc[i][c].w = fmaf(x, y.w, acc[i][c].w);
+          acc[i][2 * c] = fma2(make_float2(x, x), make_float2(y.x, y.y), acc[i][2 * c]);
+          acc[i][2 * c + 1] = fma2(make_float2(x, x), make_float2(y.z, y.w), acc[i][2 * c + 1]);
         }
       }
   }
 }
 
-__device__ __forceinline__ void store4(float* dst, float4 f) { *reinterpret_cast<float4*>(dst) = f; }
+template <int D>
+__device__ __forceinline__ void store_row(float* dst, const float2 (&f)[D / 32], float scale) {
+  const int tx = threadIdx.x & 15;
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c)
+    *reinterpret_cast<float4*>(dst + 4 * tx + 64 * c) =
+        make_float4(f[2 * c].x * scale, f[2 * c].y * scale, f[2 * c + 1].x * scale, f[2 * c + 1].y * scale);
+}
 
-__device__ __forceinline__ float4 times(float4 a, float s) { return make_float4(a.x * s, a.y * s, a.z * s, a.w * s); }
+template <int I, int J>
+__device__ __forceinline__ void clear(float2 (&x)[I][J]) {
+#pragma unroll
+  for (int i = 0; i < I; ++i)
+#pragma unroll
+    for (int j = 0; j < J; ++j) x[i][j] = make_float2(0.f, 0.f);
+}
+
+__device__ __forceinline__ float sum2(float2 x) { return x.x + x.y; }
 
 // over the 16 threads of a row
 __device__ __forceinline__ float row_max(float x) {
@@ -92,201 +112,225 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// ---------------------------------------------------------------- attention
+__device__ __forceinline__ void loaded() {
+  cp_async_commit();
+  cp_async_wait<0>();
+  __syncthreads();
+}
 
 // Whether query i sees row j
 __device__ __forceinline__ bool sees(int i, int j, float bias) { return j == i || (j < i && bias != -INFINITY); }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads) attn_kernel(const AttnArgs a) {
+template <int D, int kRows>
+constexpr size_t tiles_bytes(int tiles, int weights) {
+  return ((size_t)tiles * kRows * (D + 4) + (size_t)weights * kRows * (kRows + 4) + 2 * kRows) * 4;
+}
+
+// Weights take K's place once the scores are there.
+template <int D, int kRows>
+__global__ void __launch_bounds__(Shape<kRows>::kThreads, 2) attn_kernel(const AttnArgs a) {
+  using S = Shape<kRows>;
   extern __shared__ float smem[];
-  float *Q = smem, *K = Q + kT * (D + 4), *V = K + kT * (D + 4), *W = V + kT * (D + 4);
+  float *Q = smem, *K = Q + S::kT * (D + 4), *V = K + S::kT * (D + 4), *W = K;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, h = blockIdx.y, hk = h / a.G;
   if (blockIdx.x == 0 && h == 0) check_seqs(a.seqs, a.error);
-  Piece p = find_piece(a.seqs, kT, blockIdx.x);
+  Piece p = find_piece(a.seqs, S::kT, blockIdx.x);
   if (!p.ok) return;
-  p.at = (p.t1 - p.t0 + kT - 1) / kT - 1 - p.at;  // the longest rows first
-  const int i0 = p.t0 + p.at * kT, rows = min(kT, p.t1 - i0);
+  p.at = (p.t1 - p.t0 + S::kT - 1) / S::kT - 1 - p.at;  // the longest rows first
+  const int i0 = p.t0 + p.at * S::kT, rows = min(S::kT, p.t1 - i0);
   const float scale = 1.f / sqrtf((float)D);
   const long long qs = (long long)a.Hq * D, ks = (long long)a.Hkv * D;
-  load_rows<D>(Q, static_cast<const float*>(a.q) + (long long)i0 * qs + (long long)h * D, qs, rows);
-  float4 acc[4][D / 64] = {};
-  float m[4], l[4];
+  const float *k = static_cast<const float*>(a.k) + (long long)hk * D, *v = static_cast<const float*>(a.v) + (long long)hk * D;
+  load_rows<D, S>(Q, static_cast<const float*>(a.q) + (long long)i0 * qs + (long long)h * D, qs, rows);
+  float2 acc[S::kI][D / 32];
+  clear(acc);
+  float m[S::kI], l[S::kI];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) m[i] = -INFINITY, l[i] = 0.f;
-  for (int j0 = p.t0; j0 <= i0; j0 += kT) {
-    const int keys = min(kT, p.t1 - j0);
+  for (int i = 0; i < S::kI; ++i) m[i] = -INFINITY, l[i] = 0.f;
+  for (int j0 = p.t0; j0 <= i0; j0 += S::kT) {
+    const int keys = min(S::kT, p.t1 - j0);
     __syncthreads();
-    load_rows<D>(K, static_cast<const float*>(a.k) + (long long)j0 * ks + (long long)hk * D, ks, keys);
-    load_rows<D>(V, static_cast<const float*>(a.v) + (long long)j0 * ks + (long long)hk * D, ks, keys);
-    __syncthreads();
-    float s[4][4] = {};
-    dot_tile<D>(s, Q, K);
+    load_rows<D, S>(K, k + j0 * ks, ks, keys);
+    load_rows<D, S>(V, v + j0 * ks, ks, keys);
+    float b[S::kJ];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < S::kJ; ++j) {
       const int tok = j0 + tx + 16 * j;
-      const float b = a.bias && tok < p.t1 ? a.bias[(long long)hk * a.seqs.total + tok] : 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int q = i0 + ty + 16 * i;
-        s[i][j] = sees(q, tok, b) ? fmaf(s[i][j], scale, tok < q ? b : 0.f) : -INFINITY;
-      }
+      b[j] = a.bias && tok < p.t1 ? a.bias[(long long)hk * a.seqs.total + tok] : 0.f;
     }
+    loaded();
+    float2 s2[S::kI][S::kJ];
+    clear(s2);
+    dot_tile<D, S>(s2, Q, K);
+    __syncthreads();  // K has been read
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float mt = row_max(fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3])));
-      const float mn = fmaxf(m[i], mt), ref = mn == -INFINITY ? 0.f : mn;
+    for (int i = 0; i < S::kI; ++i) {
+      const int q = i0 + ty + S::kTy * i;
+      float s[S::kJ], mt = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < S::kJ; ++j) {
+        const int tok = j0 + tx + 16 * j;
+        s[j] = sees(q, tok, b[j]) ? fmaf(sum2(s2[i][j]), scale, tok < q ? b[j] : 0.f) : -INFINITY;
+        mt = fmaxf(mt, s[j]);
+      }
+      const float mn = fmaxf(m[i], row_max(mt)), ref = mn == -INFINITY ? 0.f : mn;
       const float corr = expf(m[i] - ref);
       m[i] = mn;
       float sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float w = expf(s[i][j] - ref);
+      for (int j = 0; j < S::kJ; ++j) {
+        const float w = expf(s[j] - ref);
         sum += w;
-        W[(ty + 16 * i) * kW + tx + 16 * j] = w;
+        W[(ty + S::kTy * i) * S::kW + tx + 16 * j] = w;
       }
       l[i] = fmaf(l[i], corr, row_sum(sum));
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c) acc[i][c] = times(acc[i][c], corr);
+      for (int c = 0; c < D / 32; ++c) acc[i][c] = mul2(acc[i][c], make_float2(corr, corr));
     }
     __syncthreads();
-    sum_tile<D>(acc, W, V);
+    sum_tile<D, S>(acc, W, V);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = ty + 16 * i;
+  for (int i = 0; i < S::kI; ++i) {
+    const int r = ty + S::kTy * i;
     if (r >= rows) continue;
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c)
-      store4(static_cast<float*>(a.out) + (long long)(i0 + r) * qs + (long long)h * D + 4 * tx + 64 * c,
-             times(acc[i][c], 1.f / l[i]));
+    store_row<D>(static_cast<float*>(a.out) + (long long)(i0 + r) * qs + (long long)h * D, acc[i], 1.f / l[i]);
     if (tx == 0) a.lse[(long long)h * a.seqs.total + i0 + r] = m[i] + logf(l[i]);
   }
 }
 
 // The rows of Q's gradient: dQ_i = scale sum over j of dS_ij k_j, with
-// dS = P (dO V^T - delta), delta_i = dO_i . out_i
-template <int D>
-__global__ void __launch_bounds__(kThreads) attn_dq_kernel(const AttnArgs a) {
+// dS = P (dO V^T - delta), delta_i = dO_i . out_i. Weights take V's place.
+template <int D, int kRows>
+__global__ void __launch_bounds__(Shape<kRows>::kThreads) attn_dq_kernel(const AttnArgs a) {
+  using S = Shape<kRows>;
   extern __shared__ float smem[];
-  float *Q = smem, *O = Q + kT * (D + 4), *K = O + kT * (D + 4), *V = K + kT * (D + 4), *W = V + kT * (D + 4);
+  float *Q = smem, *O = Q + S::kT * (D + 4), *K = O + S::kT * (D + 4), *V = K + S::kT * (D + 4), *W = V;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, h = blockIdx.y, hk = h / a.G;
-  Piece p = find_piece(a.seqs, kT, blockIdx.x);
+  Piece p = find_piece(a.seqs, S::kT, blockIdx.x);
   if (!p.ok) return;
-  p.at = (p.t1 - p.t0 + kT - 1) / kT - 1 - p.at;
-  const int i0 = p.t0 + p.at * kT, rows = min(kT, p.t1 - i0);
+  p.at = (p.t1 - p.t0 + S::kT - 1) / S::kT - 1 - p.at;
+  const int i0 = p.t0 + p.at * S::kT, rows = min(S::kT, p.t1 - i0);
   const float scale = 1.f / sqrtf((float)D);
-  const long long qs = (long long)a.Hq * D, ks = (long long)a.Hkv * D;
-  load_rows<D>(Q, static_cast<const float*>(a.q) + (long long)i0 * qs + (long long)h * D, qs, rows);
-  load_rows<D>(O, static_cast<const float*>(a.dout) + (long long)i0 * qs + (long long)h * D, qs, rows);
-  float lse[4], delta[4];
+  const long long qs = (long long)a.Hq * D, ks = (long long)a.Hkv * D, at = (long long)i0 * qs + (long long)h * D;
+  const float *k = static_cast<const float*>(a.k) + (long long)hk * D, *v = static_cast<const float*>(a.v) + (long long)hk * D;
+  load_rows<D, S>(Q, static_cast<const float*>(a.q) + at, qs, rows);
+  load_rows<D, S>(O, static_cast<const float*>(a.dout) + at, qs, rows);
+  float lse[S::kI], delta[S::kI];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const long long at = (long long)h * a.seqs.total + i0 + ty + 16 * i;
-    const bool in = ty + 16 * i < rows;
-    lse[i] = in ? a.lse[at] : 0.f;
-    delta[i] = in ? a.rows[at] : 0.f;
+  for (int i = 0; i < S::kI; ++i) {
+    const long long n = (long long)h * a.seqs.total + i0 + ty + S::kTy * i;
+    const bool in = ty + S::kTy * i < rows;
+    lse[i] = in ? a.lse[n] : 0.f;
+    delta[i] = in ? a.rows[n] : 0.f;
   }
-  float4 acc[4][D / 64] = {};
-  for (int j0 = p.t0; j0 <= i0; j0 += kT) {
-    const int keys = min(kT, p.t1 - j0);
+  float2 acc[S::kI][D / 32];
+  clear(acc);
+  for (int j0 = p.t0; j0 <= i0; j0 += S::kT) {
+    const int keys = min(S::kT, p.t1 - j0);
     __syncthreads();
-    load_rows<D>(K, static_cast<const float*>(a.k) + (long long)j0 * ks + (long long)hk * D, ks, keys);
-    load_rows<D>(V, static_cast<const float*>(a.v) + (long long)j0 * ks + (long long)hk * D, ks, keys);
-    __syncthreads();
-    float s[4][4] = {}, dp[4][4] = {};
-    dot_tile<D>(s, Q, K);
-    dot_tile<D>(dp, O, V);
+    load_rows<D, S>(K, k + j0 * ks, ks, keys);
+    load_rows<D, S>(V, v + j0 * ks, ks, keys);
+    float b[S::kJ];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < S::kJ; ++j) {
       const int tok = j0 + tx + 16 * j;
-      const float b = a.bias && tok < p.t1 ? a.bias[(long long)hk * a.seqs.total + tok] : 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int q = i0 + ty + 16 * i;
-        const float w = expf(fmaf(s[i][j], scale, tok < q ? b : 0.f) - lse[i]);
-        W[(ty + 16 * i) * kW + tx + 16 * j] = sees(q, tok, b) ? w * (dp[i][j] - delta[i]) : 0.f;
-      }
+      b[j] = a.bias && tok < p.t1 ? a.bias[(long long)hk * a.seqs.total + tok] : 0.f;
     }
+    loaded();
+    float2 s[S::kI][S::kJ], dp[S::kI][S::kJ];
+    clear(s);
+    clear(dp);
+    dot_tile<D, S>(s, Q, K);
+    dot_tile<D, S>(dp, O, V);
+    __syncthreads();  // V has been read
+#pragma unroll
+    for (int i = 0; i < S::kI; ++i)
+#pragma unroll
+      for (int j = 0; j < S::kJ; ++j) {
+        const int q = i0 + ty + S::kTy * i, tok = j0 + tx + 16 * j;
+        const float w = expf(fmaf(sum2(s[i][j]), scale, tok < q ? b[j] : 0.f) - lse[i]);
+        W[(ty + S::kTy * i) * S::kW + tx + 16 * j] = sees(q, tok, b[j]) ? w * (sum2(dp[i][j]) - delta[i]) : 0.f;
+      }
     __syncthreads();
-    sum_tile<D>(acc, W, K);
+    sum_tile<D, S>(acc, W, K);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (ty + 16 * i < rows)
-#pragma unroll
-      for (int c = 0; c < D / 64; ++c)
-        store4(static_cast<float*>(a.dq) + (long long)(i0 + ty + 16 * i) * qs + (long long)h * D + 4 * tx + 64 * c,
-               times(acc[i][c], scale));
+  for (int i = 0; i < S::kI; ++i)
+    if (ty + S::kTy * i < rows)
+      store_row<D>(static_cast<float*>(a.dq) + at + (long long)(ty + S::kTy * i) * qs, acc[i], scale);
 }
 
 // The rows of K's and V's gradients and of the bias's, summed over the queries of the
 // group: dV_j = sum of P_ij dO_i, dK_j = scale sum of dS_ij q_i, dbias_j = sum over i > j of dS_ij
-template <int D>
-__global__ void __launch_bounds__(kThreads) attn_dkv_kernel(const AttnArgs a) {
+template <int D, int kRows>
+__global__ void __launch_bounds__(Shape<kRows>::kThreads) attn_dkv_kernel(const AttnArgs a) {
+  using S = Shape<kRows>;
   extern __shared__ float smem[];
-  float *K = smem, *V = K + kT * (D + 4), *Q = V + kT * (D + 4), *O = Q + kT * (D + 4), *W = O + kT * (D + 4);
-  float *S = W + kT * kW, *L = S + kT * kW, *E = L + kT;
+  float *K = smem, *V = K + S::kT * (D + 4), *Q = V + S::kT * (D + 4), *O = Q + S::kT * (D + 4), *W = O + S::kT * (D + 4);
+  float *X = W + S::kT * S::kW, *L = X + S::kT * S::kW, *E = L + S::kT;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, hk = blockIdx.y;
-  const Piece p = find_piece(a.seqs, kT, blockIdx.x);
+  const Piece p = find_piece(a.seqs, S::kT, blockIdx.x);
   if (!p.ok) return;
-  const int j0 = p.t0 + p.at * kT, keys = min(kT, p.t1 - j0);
+  const int j0 = p.t0 + p.at * S::kT, keys = min(S::kT, p.t1 - j0);
   const float scale = 1.f / sqrtf((float)D);
-  const long long qs = (long long)a.Hq * D, ks = (long long)a.Hkv * D;
-  load_rows<D>(K, static_cast<const float*>(a.k) + (long long)j0 * ks + (long long)hk * D, ks, keys);
-  load_rows<D>(V, static_cast<const float*>(a.v) + (long long)j0 * ks + (long long)hk * D, ks, keys);
-  float bias[4], db[4] = {};
+  const long long qs = (long long)a.Hq * D, ks = (long long)a.Hkv * D, at = (long long)j0 * ks + (long long)hk * D;
+  load_rows<D, S>(K, static_cast<const float*>(a.k) + at, ks, keys);
+  load_rows<D, S>(V, static_cast<const float*>(a.v) + at, ks, keys);
+  float bias[S::kI], db[S::kI];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int r = ty + 16 * j;
+  for (int j = 0; j < S::kI; ++j) {
+    const int r = ty + S::kTy * j;
     bias[j] = a.bias && r < keys ? a.bias[(long long)hk * a.seqs.total + j0 + r] : 0.f;
+    db[j] = 0.f;
   }
-  float4 dk[4][D / 64] = {}, dv[4][D / 64] = {};
+  float2 dk[S::kI][D / 32], dv[S::kI][D / 32];
+  clear(dk);
+  clear(dv);
   for (int g = 0; g < a.G; ++g) {
     const int h = hk * a.G + g;
-    for (int i0 = j0; i0 < p.t1; i0 += kT) {
-      const int rows = min(kT, p.t1 - i0);
+    for (int i0 = j0; i0 < p.t1; i0 += S::kT) {
+      const int rows = min(S::kT, p.t1 - i0);
       __syncthreads();
-      load_rows<D>(Q, static_cast<const float*>(a.q) + (long long)i0 * qs + (long long)h * D, qs, rows);
-      load_rows<D>(O, static_cast<const float*>(a.dout) + (long long)i0 * qs + (long long)h * D, qs, rows);
-      if (threadIdx.x < kT) {
-        const long long at = (long long)h * a.seqs.total + i0 + threadIdx.x;
+      const long long q0 = (long long)i0 * qs + (long long)h * D;
+      load_rows<D, S>(Q, static_cast<const float*>(a.q) + q0, qs, rows);
+      load_rows<D, S>(O, static_cast<const float*>(a.dout) + q0, qs, rows);
+      if (threadIdx.x < S::kT) {
+        const long long n = (long long)h * a.seqs.total + i0 + threadIdx.x;
         const bool in = (int)threadIdx.x < rows;
-        L[threadIdx.x] = in ? a.lse[at] : 0.f;
-        E[threadIdx.x] = in ? a.rows[at] : 0.f;
+        L[threadIdx.x] = in ? a.lse[n] : 0.f;
+        E[threadIdx.x] = in ? a.rows[n] : 0.f;
       }
-      __syncthreads();
-      float s[4][4] = {}, dp[4][4] = {};
-      dot_tile<D>(s, K, Q);
-      dot_tile<D>(dp, V, O);
+      loaded();
+      float2 s[S::kI][S::kJ], dp[S::kI][S::kJ];
+      clear(s);
+      clear(dp);
+      dot_tile<D, S>(s, K, Q);
+      dot_tile<D, S>(dp, V, O);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < S::kI; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int tok = j0 + ty + 16 * j, r = tx + 16 * i, q = i0 + r;
+        for (int i = 0; i < S::kJ; ++i) {
+          const int tok = j0 + ty + S::kTy * j, r = tx + 16 * i, q = i0 + r;
           const bool seen = r < rows && sees(q, tok, bias[j]);
-          const float w = seen ? expf(fmaf(s[j][i], scale, tok < q ? bias[j] : 0.f) - L[r]) : 0.f;
-          const float ds = seen ? w * (dp[j][i] - E[r]) : 0.f;
-          W[(ty + 16 * j) * kW + r] = w;
-          S[(ty + 16 * j) * kW + r] = ds;
+          const float w = seen ? expf(fmaf(sum2(s[j][i]), scale, tok < q ? bias[j] : 0.f) - L[r]) : 0.f;
+          const float ds = seen ? w * (sum2(dp[j][i]) - E[r]) : 0.f;
+          W[(ty + S::kTy * j) * S::kW + r] = w;
+          X[(ty + S::kTy * j) * S::kW + r] = ds;
           if (tok < q) db[j] += ds;
         }
       __syncthreads();
-      sum_tile<D>(dv, W, O);
-      sum_tile<D>(dk, S, Q);
+      sum_tile<D, S>(dv, W, O);
+      sum_tile<D, S>(dk, X, Q);
     }
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int r = ty + 16 * j;
+  for (int j = 0; j < S::kI; ++j) {
+    const int r = ty + S::kTy * j;
     const float b = row_sum(db[j]);
     if (r >= keys) continue;
-    const long long at = (long long)(j0 + r) * ks + (long long)hk * D;
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-      store4(static_cast<float*>(a.dk) + at + 4 * tx + 64 * c, times(dk[j][c], scale));
-      store4(static_cast<float*>(a.dv) + at + 4 * tx + 64 * c, dv[j][c]);
-    }
+    store_row<D>(static_cast<float*>(a.dk) + at + r * ks, dk[j], scale);
+    store_row<D>(static_cast<float*>(a.dv) + at + r * ks, dv[j], 1.f);
     if (tx == 0 && a.dbias) static_cast<float*>(a.dbias)[(long long)hk * a.seqs.total + j0 + r] = b;
   }
 }
@@ -311,39 +355,45 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnArgs a) {
 }
 
 template <typename K>
-cudaError_t allow(K* kernel, size_t bytes) {
-  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-}
-
-template <int D>
-cudaError_t attn_f(const AttnArgs& a, cudaStream_t stream) {
-  constexpr size_t bytes = (3 * kT * (D + 4) + kT * kW) * 4;
-  cudaError_t e = allow(attn_kernel<D>, bytes);
+cudaError_t launch(K* kernel, const AttnArgs& a, int heads, int rows, int threads, size_t bytes, cudaStream_t stream) {
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   if (e != cudaSuccess) return e;
-  attn_kernel<D><<<dim3((unsigned)pieces(a.seqs.total, a.seqs.num, kT), a.Hq), kThreads, bytes, stream>>>(a);
+  kernel<<<dim3((unsigned)pieces(a.seqs.total, a.seqs.num, rows), heads), threads, bytes, stream>>>(a);
   return cudaGetLastError();
 }
 
-template <int D>
-cudaError_t attn_b(const AttnArgs& a, cudaStream_t stream) {
-  constexpr size_t dq = (4 * kT * (D + 4) + kT * kW) * 4, dkv = (4 * kT * (D + 4) + 2 * kT * kW + 2 * kT) * 4;
-  cudaError_t e = allow(attn_dq_kernel<D>, dq);
-  if (e == cudaSuccess) e = allow(attn_dkv_kernel<D>, dkv);
-  if (e != cudaSuccess) return e;
-  const unsigned n = (unsigned)pieces(a.seqs.total, a.seqs.num, kT);
+template <int D, int kRows>
+cudaError_t forward(const AttnArgs& a, cudaStream_t stream) {
+  return launch(attn_kernel<D, kRows>, a, a.Hq, kRows, Shape<kRows>::kThreads, tiles_bytes<D, kRows>(3, 0), stream);
+}
+
+template <int D, int kRows>
+cudaError_t backward(const AttnArgs& a, cudaStream_t stream) {
+  constexpr int threads = Shape<kRows>::kThreads;
   attn_delta_kernel<D><<<(unsigned)(((long long)a.seqs.total * a.Hq + 7) / 8), 256, 0, stream>>>(a);
-  attn_dkv_kernel<D><<<dim3(n, a.Hkv), kThreads, dkv, stream>>>(a);
-  attn_dq_kernel<D><<<dim3(n, a.Hq), kThreads, dq, stream>>>(a);
-  return cudaGetLastError();
+  cudaError_t e = cudaGetLastError();
+  if (e == cudaSuccess) e = launch(attn_dkv_kernel<D, kRows>, a, a.Hkv, kRows, threads, tiles_bytes<D, kRows>(4, 2), stream);
+  if (e == cudaSuccess) e = launch(attn_dq_kernel<D, kRows>, a, a.Hq, kRows, threads, tiles_bytes<D, kRows>(4, 0), stream);
+  return e;
+}
+
+// Whether tiles of 64 rows would be fewer than two blocks per SM, for the heads of `a` that share them
+bool small(const AttnArgs& a, int heads) {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return false;
+  return pieces(a.seqs.total, a.seqs.num, 64) * heads < 2 * sms;
 }
 
 }  // namespace
 
 cudaError_t attn_forward_f32(const AttnArgs& a, int D, cudaStream_t stream) {
-  return D == 128 ? attn_f<128>(a, stream) : attn_f<64>(a, stream);
+  if (small(a, a.Hq)) return D == 128 ? forward<128, 32>(a, stream) : forward<64, 32>(a, stream);
+  return D == 128 ? forward<128, 64>(a, stream) : forward<64, 64>(a, stream);
 }
 cudaError_t attn_backward_f32(const AttnArgs& a, int D, cudaStream_t stream) {
-  return D == 128 ? attn_b<128>(a, stream) : attn_b<64>(a, stream);
+  if (small(a, a.Hkv)) return D == 128 ? backward<128, 32>(a, stream) : backward<64, 32>(a, stream);
+  return D == 128 ? backward<128, 64>(a, stream) : backward<64, 64>(a, stream);
 }
 
 }  // namespace dmc
