@@ -2,9 +2,40 @@
 // of the handle's scratch.
 #pragma once
 
+#include <atomic>
+
 #include "dmc_internal.cuh"
 
 namespace dmc {
+
+// What a launch asks of the runtime once per device and process: the number of SMs, and leave
+// for a kernel to use so much shared memory.
+constexpr int kMostDevices = 64;
+inline cudaError_t this_device(int* dev) {
+  const cudaError_t e = cudaGetDevice(dev);
+  return e == cudaSuccess && *dev >= kMostDevices ? cudaErrorInvalidDevice : e;
+}
+inline cudaError_t sm_count(int* sms) {
+  static std::atomic<int> known[kMostDevices];
+  int dev = 0;
+  cudaError_t e = this_device(&dev);
+  if (e != cudaSuccess) return e;
+  *sms = known[dev].load(std::memory_order_relaxed);
+  if (*sms > 0) return cudaSuccess;
+  e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess) known[dev].store(*sms, std::memory_order_relaxed);
+  return e;
+}
+template <auto* kernel>
+cudaError_t allow_shared(int bytes) {
+  static std::atomic<bool> allowed[kMostDevices];
+  int dev = 0;
+  cudaError_t e = this_device(&dev);
+  if (e != cudaSuccess || allowed[dev].load(std::memory_order_relaxed)) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) allowed[dev].store(true, std::memory_order_relaxed);
+  return e;
+}
 
 constexpr int kStateChunk = 32;   // tokens per block of the states' kernels: one per lane
 

@@ -431,10 +431,9 @@ template <int D, bool kBias>
 cudaError_t forward(const AttnArgs& a, cudaStream_t stream) {
   constexpr int bytes = sizeof(FwdShared<D>) + 1024;
   static_assert(bytes <= 227 * 1024, "one CTA's shared memory");
-  auto* kernel = attn_forward_kernel<D, kBias>;
   AttnMaps maps;
   int sms = 0;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  cudaError_t e = allow_shared<attn_forward_kernel<D, kBias>>(bytes);
   if (e == cudaSuccess) e = sm_count(&sms);
   if (e == cudaSuccess) e = heads_map(&maps.q, a.q, D, a.Hq, a.seqs.total);
   if (e == cudaSuccess) e = heads_map(&maps.k, a.k, D, a.Hkv, a.seqs.total);
@@ -442,7 +441,7 @@ cudaError_t forward(const AttnArgs& a, cudaStream_t stream) {
   if (e != cudaSuccess) return e;
   const long long items = pieces(a.seqs.total, a.seqs.num, kItem) * a.Hq;
   if (items > INT32_MAX) return cudaErrorInvalidValue;
-  kernel<<<(unsigned)(items < sms ? items : sms), kAttnThreads, bytes, stream>>>(a, maps, (int)items);
+  attn_forward_kernel<D, kBias><<<(unsigned)(items < sms ? items : sms), kAttnThreads, bytes, stream>>>(a, maps, (int)items);
   return cudaGetLastError();
 }
 

@@ -801,8 +801,8 @@ cudaError_t backward(const AttnArgs& a, cudaStream_t stream) {
   auto* dq = attn_dq_kernel<D, kBias>;
   BwdMaps maps;
   int sms = 0;
-  cudaError_t e = cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, dkv_bytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(dq, cudaFuncAttributeMaxDynamicSharedMemorySize, dq_bytes);
+  cudaError_t e = allow_shared<attn_dkv_kernel<D, kBias>>(dkv_bytes);
+  if (e == cudaSuccess) e = allow_shared<attn_dq_kernel<D, kBias>>(dq_bytes);
   if (e == cudaSuccess) e = sm_count(&sms);
   if (e == cudaSuccess) e = heads_map(&maps.q, a.q, D, a.Hq, a.seqs.total);
   if (e == cudaSuccess) e = heads_map(&maps.k, a.k, D, a.Hkv, a.seqs.total);

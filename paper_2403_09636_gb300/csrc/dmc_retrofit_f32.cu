@@ -354,9 +354,9 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnArgs a) {
   if (lane == 0) a.rows[(w % a.Hq) * a.seqs.total + w / a.Hq] = d;
 }
 
-template <typename K>
-cudaError_t launch(K* kernel, const AttnArgs& a, int heads, int rows, int threads, size_t bytes, cudaStream_t stream) {
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+template <auto* kernel>
+cudaError_t launch(const AttnArgs& a, int heads, int rows, int threads, size_t bytes, cudaStream_t stream) {
+  const cudaError_t e = allow_shared<kernel>((int)bytes);
   if (e != cudaSuccess) return e;
   kernel<<<dim3((unsigned)pieces(a.seqs.total, a.seqs.num, rows), heads), threads, bytes, stream>>>(a);
   return cudaGetLastError();
@@ -364,7 +364,7 @@ cudaError_t launch(K* kernel, const AttnArgs& a, int heads, int rows, int thread
 
 template <int D, int kRows>
 cudaError_t forward(const AttnArgs& a, cudaStream_t stream) {
-  return launch(attn_kernel<D, kRows>, a, a.Hq, kRows, Shape<kRows>::kThreads, tiles_bytes<D, kRows>(3, 0), stream);
+  return launch<attn_kernel<D, kRows>>(a, a.Hq, kRows, Shape<kRows>::kThreads, tiles_bytes<D, kRows>(3, 0), stream);
 }
 
 template <int D, int kRows>
@@ -372,17 +372,15 @@ cudaError_t backward(const AttnArgs& a, cudaStream_t stream) {
   constexpr int threads = Shape<kRows>::kThreads;
   attn_delta_kernel<D><<<(unsigned)(((long long)a.seqs.total * a.Hq + 7) / 8), 256, 0, stream>>>(a);
   cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess) e = launch(attn_dkv_kernel<D, kRows>, a, a.Hkv, kRows, threads, tiles_bytes<D, kRows>(4, 2), stream);
-  if (e == cudaSuccess) e = launch(attn_dq_kernel<D, kRows>, a, a.Hq, kRows, threads, tiles_bytes<D, kRows>(4, 0), stream);
+  if (e == cudaSuccess) e = launch<attn_dkv_kernel<D, kRows>>(a, a.Hkv, kRows, threads, tiles_bytes<D, kRows>(4, 2), stream);
+  if (e == cudaSuccess) e = launch<attn_dq_kernel<D, kRows>>(a, a.Hq, kRows, threads, tiles_bytes<D, kRows>(4, 0), stream);
   return e;
 }
 
-// Whether tiles of 64 rows would be fewer than two blocks per SM, for the heads of `a` that share them
+// Whether tiles of 64 rows would be fewer than two blocks per SM
 bool small(const AttnArgs& a, int heads) {
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return false;
-  return pieces(a.seqs.total, a.seqs.num, 64) * heads < 2 * sms;
+  int sms = 0;
+  return sm_count(&sms) == cudaSuccess && pieces(a.seqs.total, a.seqs.num, 64) * heads < 2 * sms;
 }
 
 }  // namespace

@@ -476,8 +476,7 @@ inline int tile_columns(int rows, int cols, int sms) {
 
 template <End kEnd, bool kF32, int kN>
 cudaError_t launch_product(ProductArgs& p, int sms, cudaStream_t stream) {
-  auto* kernel = loss_product_kernel<kEnd, kF32, kN>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
+  const cudaError_t e = allow_shared<loss_product_kernel<kEnd, kF32, kN>>(kProductSmem);
   if (e != cudaSuccess) return e;
   const long long tm = ceil_div(p.rows, kM), tn = ceil_div(p.cols, kN);
   p.passes = kF32 ? 6 : 1;
@@ -486,7 +485,7 @@ cudaError_t launch_product(ProductArgs& p, int sms, cudaStream_t stream) {
   p.group = (int)(group < 1 ? 1 : group > tm ? tm : group);
   const long long tiles = tm * tn;
   const int pairs = sms / 2;
-  kernel<<<2 * (unsigned)(tiles < pairs ? tiles : pairs), kProductThreads, kProductSmem, stream>>>(p);
+  loss_product_kernel<kEnd, kF32, kN><<<2 * (unsigned)(tiles < pairs ? tiles : pairs), kProductThreads, kProductSmem, stream>>>(p);
   return cudaGetLastError();
 }
 
@@ -500,12 +499,6 @@ cudaError_t product(ProductArgs& p, const void* a, uint64_t a_rows, uint64_t a_c
   if (e == cudaSuccess) e = matrix_map(&p.mb, b, b_rows, b_cols, b_stride, kBmn ? 64 : columns / 2, parts);
   if (e != cudaSuccess) return e;
   return columns == 128 ? launch_product<kEnd, kF32, 128>(p, sms, stream) : launch_product<kEnd, kF32, 256>(p, sms, stream);
-}
-
-cudaError_t sm_count(int* sms) {
-  int dev = 0;
-  const cudaError_t e = cudaGetDevice(&dev);
-  return e == cudaSuccess ? cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) : e;
 }
 
 template <bool kF32>

@@ -588,8 +588,7 @@ cudaError_t forward(const StatesArgs& a, cudaStream_t stream) {
 template <typename T, int D>
 cudaError_t backward(const StatesArgs& a, cudaStream_t stream) {
   constexpr int bytes = sizeof(BackShared<T, D>);
-  const cudaError_t e =
-      cudaFuncSetAttribute(states_backward_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  const cudaError_t e = allow_shared<states_backward_kernel<T, D>>(bytes);
   if (e != cudaSuccess) return e;
   states_backward_kernel<T, D><<<(unsigned)(pieces(a.seqs.total, a.seqs.num, kC) * a.Hkv), 64, bytes, stream>>>(a);
   return cudaGetLastError();

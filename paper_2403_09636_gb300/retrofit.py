@@ -18,10 +18,8 @@ from __future__ import annotations
 
 import torch
 
-from . import (DMC_BF16, DMC_ERR_INVALID_ARG, DMC_F32, DmcError, _check, dmc_retrofit_attention,
-               dmc_retrofit_attention_backward, dmc_retrofit_config, dmc_retrofit_create, dmc_retrofit_destroy,
-               dmc_retrofit_loss, dmc_retrofit_loss_backward, dmc_retrofit_required_bytes, dmc_retrofit_saved_bytes,
-               dmc_retrofit_states, dmc_retrofit_states_backward, dmc_retrofit_status)
+from . import (DMC_BF16, DMC_ERR_INVALID_ARG, DMC_F32, DmcError, _check, dmc_retrofit_config, dmc_retrofit_create,
+               dmc_retrofit_destroy, dmc_retrofit_required_bytes, dmc_retrofit_saved_bytes, dmc_retrofit_status, lib)
 
 _F32, _I32 = torch.float32, torch.int32
 
@@ -42,7 +40,7 @@ class DmcRetrofit:
         dev = torch.device(device if device is not None else "cuda")
         if dev.type == "cuda" and dev.index is None and torch.cuda.is_available():
             dev = torch.device("cuda", torch.cuda.current_device())
-        self.dtype, self.device = dtype, dev
+        self.dtype, self.device, self.index = dtype, dev, dev.index if dev.type == "cuda" else -1
         self.cfg = dmc_retrofit_config(int(num_q_heads), int(num_kv_heads), int(head_dim), codes[dtype],
                                        int(max_tokens), int(max_seqs), int(hidden), int(vocab))
         self.nbytes = dmc_retrofit_required_bytes(self.cfg)
@@ -51,10 +49,12 @@ class DmcRetrofit:
         self.arena = torch.empty(self.nbytes, dtype=torch.uint8, device=self.device)
         st, self.handle = dmc_retrofit_create(self.cfg, self.arena.data_ptr(), self.nbytes, self._s(stream))
         _check(st, "dmc_retrofit_create")
+        self.lib = lib()
+        self._saved = {}  # floats of `saved` by (sequences, tokens)
 
     def _s(self, stream):
         if stream is None:
-            return torch._C._cuda_getCurrentRawStream(self.device.index)
+            return torch._C._cuda_getCurrentRawStream(self.index)
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
     def close(self):
@@ -68,45 +68,47 @@ class DmcRetrofit:
         except Exception:
             pass
 
-    # ---- checks
+    # ---- checks (of a call's 13 us on the host, with outputs given, they were 6; they are 3)
 
     def _is(self, name, t, shape, dtype):
-        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != self.device or tuple(t.shape) != shape:
-            what = f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
-            raise ValueError(f"{name} must be {dtype} {shape} on {self.device}, got {what}")
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-        return t.data_ptr()
+        if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == self.index
+                and t.is_contiguous()):
+            return t.data_ptr()
+        what = f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
+        raise ValueError(f"{name} must be contiguous {dtype} {shape} on {self.device}, got {what}")
 
-    def _may(self, name, t, shape, dtype):
-        return None if t is None else self._is(name, t, shape, dtype)
-
-    def _out(self, out, *specs):
-        """The call's outputs: new ones of the (name, shape, dtype) given, or the caller's."""
-        if out is None:
-            return tuple(torch.empty(shape, dtype=dtype, device=self.device) for _, shape, dtype in specs)
-        if len(out) != len(specs):
-            raise ValueError(f"out must hold {len(specs)} tensors: {', '.join(s[0] for s in specs)}")
-        for t, (name, shape, dtype) in zip(out, specs):
-            self._is(name, t, shape, dtype)
-        return tuple(out)
+    def _new(self, shape, dtype):
+        return torch.empty(shape, dtype=dtype, device=self.device)
 
     def _seqs(self, k, cu_seqlens):
+        """Tokens, sequences and the pointer of cu_seqlens."""
         if not self.cfg.num_q_heads:
             raise ValueError("this handle was made without heads")
         if not isinstance(k, torch.Tensor) or k.dim() != 3:
             raise ValueError("k must be [tokens, KV heads, head_dim]")
         if not isinstance(cu_seqlens, torch.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1:
             raise ValueError("cu_seqlens must be int32 [sequences + 1]")
-        n = cu_seqlens.numel() - 1
-        return k.shape[0], n, self._is("cu_seqlens", cu_seqlens, (n + 1,), _I32)
+        n = cu_seqlens.numel()
+        return k.shape[0], n - 1, self._is("cu_seqlens", cu_seqlens, (n,), _I32)
 
     def _first(self, name, q0, T):
-        """q's first components: [T, Hq] of any strides."""
-        if (not isinstance(q0, torch.Tensor) or q0.dtype != self.dtype or q0.device != self.device
-                or tuple(q0.shape) != (T, self.cfg.num_q_heads)):
+        """q's first components, [T, Hq] of any strides: pointer and strides."""
+        if (not isinstance(q0, torch.Tensor) or q0.dtype is not self.dtype or q0.get_device() != self.index
+                or q0.shape != (T, self.cfg.num_q_heads)):
             raise ValueError(f"{name} must be {self.dtype} {(T, self.cfg.num_q_heads)} on {self.device}")
-        return q0.data_ptr(), q0.stride(0), q0.stride(1)
+        return q0.data_ptr(), *q0.stride()
+
+    def _saved_floats(self, n, T):
+        floats = self._saved.get((n, T))
+        if floats is None:
+            floats = self._saved[(n, T)] = dmc_retrofit_saved_bytes(self.handle, n, T) // 4
+        return floats
+
+    @staticmethod
+    def _given(out, names):
+        if len(out) != len(names):
+            raise ValueError(f"out must hold {len(names)} tensors: {', '.join(names)}")
+        return out
 
     # ---- states
 
@@ -115,16 +117,22 @@ class DmcRetrofit:
         [T, Hkv, D], noise [Hkv, T] or None; alpha and bias are fp32 [Hkv, T], saved is for the
         backward pass."""
         T, n, cu = self._seqs(k, cu_seqlens)
-        H, D = self.cfg.num_kv_heads, self.cfg.head_dim
+        H, D, dt, check, new = self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is, self._new
+        rows, scalars, saved = (T, H, D), (H, T), self._saved_floats(n, T)
         q = self._first("q0", q0, T)
-        ptrs = [self._is(i, t, (T, H, D), self.dtype) for i, t in (("k", k), ("v", v))]
-        ptrs.append(self._may("noise", noise, (H, T), _F32))
-        saved = dmc_retrofit_saved_bytes(self.handle, n, T) // 4
-        out = self._out(out, ("kt", (T, H, D), self.dtype), ("vt", (T, H, D), self.dtype), ("alpha", (H, T), _F32),
-                        ("bias", (H, T), _F32), ("saved", (saved,), _F32))
-        _check(dmc_retrofit_states(self.handle, n, *q, *ptrs, float(offset), float(temperature), cu, T,
-                                   int(max_seqlen), *(t.data_ptr() for t in out), self._s(stream)),
-               "dmc_retrofit_states")
+        kp, vp = check("k", k, rows, dt), check("v", v, rows, dt)
+        np_ = None if noise is None else check("noise", noise, scalars, _F32)
+        if out is None:
+            out = (new(rows, dt), new(rows, dt), new(scalars, _F32), new(scalars, _F32), new((saved,), _F32))
+            ptrs = [t.data_ptr() for t in out]
+        else:
+            kt, vt, alpha, bias, keep = out = self._given(out, ("kt", "vt", "alpha", "bias", "saved"))
+            ptrs = (check("kt", kt, rows, dt), check("vt", vt, rows, dt), check("alpha", alpha, scalars, _F32),
+                    check("bias", bias, scalars, _F32), check("saved", keep, (saved,), _F32))
+        st = self.lib.dmc_retrofit_states(self.handle, n, *q, kp, vp, np_, offset, temperature, cu, T, max_seqlen, *ptrs,
+                                          self._s(stream))
+        if st:
+            _check(st, "dmc_retrofit_states")
         return out
 
     def states_backward(self, q0, k, v, cu_seqlens, max_seqlen, saved, dkt, dvt, dbias, dalpha=None, noise=None,
@@ -132,26 +140,23 @@ class DmcRetrofit:
         """(dq0, dk, dv) from the states' gradients: dbias [Hkv, T] in the handle's dtype, dalpha fp32
         [Hkv, T] or None. out's dq0 may be strided (dq[..., 0] of the attention's dq)."""
         T, n, cu = self._seqs(k, cu_seqlens)
-        H, D, dt = self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype
+        H, D, dt, check, new = self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is, self._new
+        rows, scalars = (T, H, D), (H, T)
         q = self._first("q0", q0, T)
-        ptrs = [self._is(i, t, (T, H, D), dt) for i, t in (("k", k), ("v", v))]
-        ptrs.append(self._may("noise", noise, (H, T), _F32))
-        grads = [self._is("saved", saved, (dmc_retrofit_saved_bytes(self.handle, n, T) // 4,), _F32)]
-        grads += [self._is(i, t, (T, H, D), dt) for i, t in (("dkt", dkt), ("dvt", dvt))]
-        grads += [self._is("dbias", dbias, (H, T), dt), self._may("dalpha", dalpha, (H, T), _F32)]
+        ptrs = (check("k", k, rows, dt), check("v", v, rows, dt),
+                None if noise is None else check("noise", noise, scalars, _F32))
+        grads = (check("saved", saved, (self._saved_floats(n, T),), _F32), check("dkt", dkt, rows, dt),
+                 check("dvt", dvt, rows, dt), check("dbias", dbias, scalars, dt),
+                 None if dalpha is None else check("dalpha", dalpha, scalars, _F32))
         if out is None:
-            dq0 = torch.empty((T, self.cfg.num_q_heads), dtype=dt, device=self.device)
-            rest = None
-        elif len(out) == 3:
-            dq0, rest = out[0], out[1:]
-        else:
-            raise ValueError("out must hold 3 tensors: dq0, dk, dv")
-        rest = self._out(rest, ("dk", (T, H, D), dt), ("dv", (T, H, D), dt))
-        _check(dmc_retrofit_states_backward(self.handle, n, *q, *ptrs, float(offset), float(temperature), cu, T,
-                                            int(max_seqlen), *grads, *self._first("dq0", dq0, T),
-                                            *(t.data_ptr() for t in rest), self._s(stream)),
-               "dmc_retrofit_states_backward")
-        return (dq0, *rest)
+            out = (new((T, self.cfg.num_q_heads), dt), new(rows, dt), new(rows, dt))
+        dq0, dk, dv = out = self._given(out, ("dq0", "dk", "dv"))
+        st = self.lib.dmc_retrofit_states_backward(
+            self.handle, n, *q, *ptrs, offset, temperature, cu, T, max_seqlen, *grads, *self._first("dq0", dq0, T),
+            check("dk", dk, rows, dt), check("dv", dv, rows, dt), self._s(stream))
+        if st:
+            _check(st, "dmc_retrofit_states_backward")
+        return out
 
     # ---- attention
 
@@ -159,31 +164,36 @@ class DmcRetrofit:
         """(out, lse): causal attention of packed sequences, q [T, Hq, D], k and v [T, Hkv, D], bias
         [Hkv, T] added to the scores of earlier rows (None: none); lse fp32 [Hq, T]."""
         T, n, cu = self._seqs(k, cu_seqlens)
-        Hq, H, D = self.cfg.num_q_heads, self.cfg.num_kv_heads, self.cfg.head_dim
-        ptrs = [self._is("q", q, (T, Hq, D), self.dtype)]
-        ptrs += [self._is(i, t, (T, H, D), self.dtype) for i, t in (("k", k), ("v", v))]
-        ptrs.append(self._may("bias", bias, (H, T), _F32))
-        out = self._out(out, ("out", (T, Hq, D), self.dtype), ("lse", (Hq, T), _F32))
-        _check(dmc_retrofit_attention(self.handle, n, *ptrs, cu, T, int(max_seqlen), *(t.data_ptr() for t in out),
-                                      self._s(stream)), "dmc_retrofit_attention")
+        Hq, H, D, dt, check = self.cfg.num_q_heads, self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is
+        queries, rows = (T, Hq, D), (T, H, D)
+        ptrs = (check("q", q, queries, dt), check("k", k, rows, dt), check("v", v, rows, dt),
+                None if bias is None else check("bias", bias, (H, T), _F32))
+        if out is None:
+            out = (self._new(queries, dt), self._new((Hq, T), _F32))
+        o, lse = out = self._given(out, ("out", "lse"))
+        st = self.lib.dmc_retrofit_attention(self.handle, n, *ptrs, cu, T, max_seqlen, check("out", o, queries, dt),
+                                             check("lse", lse, (Hq, T), _F32), self._s(stream))
+        if st:
+            _check(st, "dmc_retrofit_attention")
         return out
 
     def attention_backward(self, dout, q, k, v, o, lse, cu_seqlens, max_seqlen, bias=None, out=None, stream=None):
         """(dq, dk, dv, dbias) of `attention`, given its outputs o and lse; dbias [Hkv, T] in the
         handle's dtype, None without a bias."""
         T, n, cu = self._seqs(k, cu_seqlens)
-        Hq, H, D, dt = self.cfg.num_q_heads, self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype
-        ptrs = [self._is("q", q, (T, Hq, D), dt)]
-        ptrs += [self._is(i, t, (T, H, D), dt) for i, t in (("k", k), ("v", v))]
-        ptrs += [self._may("bias", bias, (H, T), _F32), self._is("o", o, (T, Hq, D), dt),
-                 self._is("lse", lse, (Hq, T), _F32), self._is("dout", dout, (T, Hq, D), dt)]
-        specs = [("dq", (T, Hq, D), dt), ("dk", (T, H, D), dt), ("dv", (T, H, D), dt)]
-        if bias is not None:
-            specs.append(("dbias", (H, T), dt))
-        out = self._out(out, *specs)
-        given = [t.data_ptr() for t in out] + [None] * (4 - len(out))
-        _check(dmc_retrofit_attention_backward(self.handle, n, *ptrs, cu, T, int(max_seqlen), *given,
-                                               self._s(stream)), "dmc_retrofit_attention_backward")
+        Hq, H, D, dt, check = self.cfg.num_q_heads, self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is
+        queries, rows, scalars, new = (T, Hq, D), (T, H, D), (H, T), self._new
+        ptrs = (check("q", q, queries, dt), check("k", k, rows, dt), check("v", v, rows, dt),
+                None if bias is None else check("bias", bias, scalars, _F32), check("o", o, queries, dt),
+                check("lse", lse, (Hq, T), _F32), check("dout", dout, queries, dt))
+        if out is None:
+            out = (new(queries, dt), new(rows, dt), new(rows, dt)) + (() if bias is None else (new(scalars, dt),))
+        self._given(out, ("dq", "dk", "dv") if bias is None else ("dq", "dk", "dv", "dbias"))
+        grads = (check("dq", out[0], queries, dt), check("dk", out[1], rows, dt), check("dv", out[2], rows, dt),
+                 None if bias is None else check("dbias", out[3], scalars, dt))
+        st = self.lib.dmc_retrofit_attention_backward(self.handle, n, *ptrs, cu, T, max_seqlen, *grads, self._s(stream))
+        if st:
+            _check(st, "dmc_retrofit_attention_backward")
         return out if bias is not None else (*out, None)
 
     # ---- loss
@@ -193,28 +203,35 @@ class DmcRetrofit:
             raise ValueError("this handle was made without a vocabulary")
         if not isinstance(hidden, torch.Tensor) or hidden.dim() != 2:
             raise ValueError("hidden must be [tokens, hidden]")
-        N = hidden.shape[0]
-        return N, [self._is("hidden", hidden, (N, self.cfg.hidden), self.dtype),
-                   self._is("weight", weight, (self.cfg.vocab, self.cfg.hidden), self.dtype),
-                   self._is("targets", targets, (N,), _I32)]
+        N, H, dt = hidden.shape[0], self.cfg.hidden, self.dtype
+        return N, (self._is("hidden", hidden, (N, H), dt), self._is("weight", weight, (self.cfg.vocab, H), dt),
+                   self._is("targets", targets, (N,), _I32))
 
     def loss(self, hidden, weight, targets, out=None, stream=None):
         """(loss, lse), fp32 [N]: cross entropy of hidden [N, hidden] against weight [vocab, hidden] at
         int32 targets [N]; below 0 a position is ignored."""
         N, ptrs = self._words(hidden, weight, targets)
-        out = self._out(out, ("loss", (N,), _F32), ("lse", (N,), _F32))
-        _check(dmc_retrofit_loss(self.handle, N, *ptrs, *(t.data_ptr() for t in out), self._s(stream)),
-               "dmc_retrofit_loss")
+        if out is None:
+            out = (self._new((N,), _F32), self._new((N,), _F32))
+        loss, lse = out = self._given(out, ("loss", "lse"))
+        st = self.lib.dmc_retrofit_loss(self.handle, N, *ptrs, self._is("loss", loss, (N,), _F32),
+                                        self._is("lse", lse, (N,), _F32), self._s(stream))
+        if st:
+            _check(st, "dmc_retrofit_loss")
         return out
 
     def loss_backward(self, dloss, hidden, weight, targets, lse, out=None, stream=None):
         """(dhidden, dweight) of `loss` from dloss, fp32 [N], and its lse."""
         N, ptrs = self._words(hidden, weight, targets)
-        ptrs += [self._is("lse", lse, (N,), _F32), self._is("dloss", dloss, (N,), _F32)]
-        out = self._out(out, ("dhidden", (N, self.cfg.hidden), self.dtype),
-                        ("dweight", (self.cfg.vocab, self.cfg.hidden), self.dtype))
-        _check(dmc_retrofit_loss_backward(self.handle, N, *ptrs, *(t.data_ptr() for t in out), self._s(stream)),
-               "dmc_retrofit_loss_backward")
+        given = (self._is("lse", lse, (N,), _F32), self._is("dloss", dloss, (N,), _F32))
+        shapes = (N, self.cfg.hidden), (self.cfg.vocab, self.cfg.hidden)
+        if out is None:
+            out = (self._new(shapes[0], self.dtype), self._new(shapes[1], self.dtype))
+        dh, dw = out = self._given(out, ("dhidden", "dweight"))
+        st = self.lib.dmc_retrofit_loss_backward(self.handle, N, *ptrs, *given, self._is("dhidden", dh, shapes[0], self.dtype),
+                                                 self._is("dweight", dw, shapes[1], self.dtype), self._s(stream))
+        if st:
+            _check(st, "dmc_retrofit_loss_backward")
         return out
 
     def status(self, stream=None):
