@@ -106,18 +106,6 @@ struct Row {
   static constexpr int kBytes = kE * (int)sizeof(T);
   using Word = typename std::conditional<kBytes == 4, uint32_t, typename std::conditional<kBytes == 8, uint2, uint4>::type>::type;
 
-  // asynchronously, n rows `stride` elements apart
-  static __device__ __forceinline__ void copy(T* to, const T* from, long long stride, int n) {
-#pragma unroll 4
-    for (int t = 0; t < n; ++t) {
-      const uint32_t dst = smem_u32(to + t * D);
-      const T* src = from + t * stride;
-      if (kBytes == 16)
-        cp_async16(dst, src);
-      else
-        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(kBytes) : "memory");
-    }
-  }
   static __device__ __forceinline__ void zero(T* at) { *reinterpret_cast<Word*>(at) = Word{}; }
   static __device__ __forceinline__ void read(const T* at, float2 (&f)[kP]) {
     const Word u = *reinterpret_cast<const Word*>(at);
@@ -135,6 +123,26 @@ struct Row {
 };
 
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// n rows of D elements, `stride` elements apart, by a warp: a row per lane, completing on `bar`
+template <typename T, int D>
+__device__ __forceinline__ void load_chunk(T* to, const T* from, long long stride, int n, uint32_t bar) {
+  const int lane = threadIdx.x & 31;
+  if (lane < n)
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                     smem_u32(to + lane * D)),
+                 "l"(from + lane * stride), "n"(D * (int)sizeof(T)), "r"(bar)
+                 : "memory");
+}
+
+// A token's numbers for the passes over its elements, each twice: the two halves of a paired
+// operation
+struct Coef {
+  float4 alpha_omega;  // alpha, alpha, omega, omega
+  float4 rz_other;     // 1 / z, 1 / z; backward: the product of the alphas up to the token over z, twice
+};
+__device__ __forceinline__ float2 lo2(float4 f) { return make_float2(f.x, f.y); }
+__device__ __forceinline__ float2 hi2(float4 f) { return make_float2(f.z, f.w); }
 
 // ---- the order of warps
 
@@ -254,12 +262,17 @@ __device__ __forceinline__ long long row_of(const StatesArgs& a, int chunk, int 
 template <typename T, int D>
 __global__ void __launch_bounds__(32) states_kernel(const StatesArgs a) {
   using R = Row<T, D>;
-  __shared__ __align__(16) T rows[kC * D];
-  __shared__ float4 coef[kC];  // alpha, omega, 1 / z
-  __shared__ float weight[kC]; // omega times the product of the alphas after it
+  __shared__ __align__(128) T rows[kC * D];
+  __shared__ Coef coef[kC];
+  __shared__ float2 weight[kC];  // omega times the product of the alphas after it, twice
+  __shared__ uint64_t loaded;
   const int lane = threadIdx.x;
   Turn turn;
-  if (lane == 0) turn = take_turn(a);
+  if (lane == 0) {
+    mbar_init(smem_u32(&loaded), 1);
+    fence_mbar_init();
+    turn = take_turn(a);
+  }
   turn.index = __shfl_sync(0xffffffffu, turn.index, 0);
   turn.tag = __shfl_sync(0xffffffffu, turn.tag, 0);
   const int which = turn.index & 1, h = (turn.index >> 1) % a.Hkv, chunk = (turn.index >> 1) / a.Hkv;  // which: 0 k, 1 v
@@ -272,10 +285,11 @@ __global__ void __launch_bounds__(32) states_kernel(const StatesArgs a) {
   const int tok0 = p.t0 + p.at * kC, n = min(kC, p.t1 - tok0), tok = tok0 + lane;
   const bool in_chunk = lane < n, goes_on = tok0 + kC < p.t1;
   const GateIn gi = gate_in<T, D>(a, h, tok, in_chunk);
-  const long long step = (long long)a.Hkv * D, at = ((long long)tok0 * a.Hkv + h) * D + lane * R::kE;
+  const long long step = (long long)a.Hkv * D, at = ((long long)tok0 * a.Hkv + h) * D;
   T* mine = rows + lane * R::kE;
-  R::copy(mine, static_cast<const T*>(which ? a.v : a.k) + at, step, n);
-  cp_async_commit();
+  if (lane == 0) mbar_arrive_expect_tx(smem_u32(&loaded), n * D * sizeof(T));
+  __syncwarp();
+  load_chunk<T, D>(rows, static_cast<const T*>(which ? a.v : a.k) + at, step, n, smem_u32(&loaded));
   const Gate g = gate_of(a, gi, in_chunk, tok == p.t0);
   const long long row = row_of<D>(a, chunk, h, which), row_step = row_of<D>(a, 1, 0, 0);
   float after = g.alpha;  // product of the alphas from the token on
@@ -285,22 +299,18 @@ __global__ void __launch_bounds__(32) states_kernel(const StatesArgs a) {
     if (lane + off < 32) after *= o;
   }
   const float prod = __shfl_sync(0xffffffffu, after, 0);
-  const bool gate_lane = which == 0 && lane == 0;
-  auto value = [&](int t, float2 (&x)[R::kP]) {
-    R::read(mine + t * D, x);
-    if (gate_lane) x[0].x = 0.f;  // k's first component
-  };
   if (goes_on) {
     const float rest = __shfl_down_sync(0xffffffffu, after, 1);
     const float w = g.omega * (lane == 31 ? 1.f : rest);
-    weight[lane] = w;
+    weight[lane] = both(w);
     float z = w;
 #pragma unroll
     for (int off = 16; off >= 1; off >>= 1) z += __shfl_xor_sync(0xffffffffu, z, off);
     if (lane == 0) publish_zp<D>(a.sums + row, z, prod, turn.tag);
-    __syncwarp();
   }
-  cp_async_wait<0>();
+  mbar_wait(smem_u32(&loaded), 0, a.error);  // (if it gives up, the fault bit is set and the results mean nothing)
+  if (which == 0 && in_chunk) rows[lane * D] = Elt<T>::from_f(0.f);  // k's first component is the gate
+  __syncwarp();
   float2 sum[R::kP];
 #pragma unroll
   for (int i = 0; i < R::kP; ++i) sum[i] = both(0.f);
@@ -308,8 +318,8 @@ __global__ void __launch_bounds__(32) states_kernel(const StatesArgs a) {
 #pragma unroll 8
     for (int t = 0; t < kC; ++t) {
       float2 x[R::kP];
-      value(t, x);
-      const float2 w = both(weight[t]);
+      R::read(mine + t * D, x);
+      const float2 w = weight[t];
 #pragma unroll
       for (int i = 0; i < R::kP; ++i) sum[i] = fma2(w, x[i], sum[i]);
     }
@@ -327,21 +337,24 @@ __global__ void __launch_bounds__(32) states_kernel(const StatesArgs a) {
     float* saved = a.saved + ((long long)chunk * a.Hkv + h) * sums_row(D);
 #pragma unroll
     for (int i = 0; i < R::kP; ++i) *reinterpret_cast<float2*>(saved + which * D + lane * R::kE + 2 * i) = sum[i];
-    if (gate_lane) saved[2 * D] = zin;
+    if (which == 0 && lane == 0) saved[2 * D] = zin;
   }
   if (lane == 0) leave(a, turn);
-  coef[lane] = make_float4(g.alpha, g.omega, 1.f / scan_z(g.alpha, g.omega, zin), 0.f);
+  const float rz = 1.f / scan_z(g.alpha, g.omega, zin);
+  coef[lane].alpha_omega = make_float4(g.alpha, g.alpha, g.omega, g.omega);
+  coef[lane].rz_other = make_float4(rz, rz, 0.f, 0.f);
   __syncwarp();
-  T* dst = static_cast<T*>(which ? a.vt : a.kt) + at;
+  T* dst = static_cast<T*>(which ? a.vt : a.kt) + at + lane * R::kE;
 #pragma unroll 8
   for (int t = 0; t < n; ++t) {
     float2 x[R::kP], y[R::kP];
-    value(t, x);
-    const float4 c = coef[t];
+    R::read(mine + t * D, x);
+    const float4 ao = coef[t].alpha_omega;
+    const float2 z = *reinterpret_cast<const float2*>(&coef[t].rz_other);
 #pragma unroll
     for (int i = 0; i < R::kP; ++i) {
-      sum[i] = fma2(both(c.x), sum[i], mul2(both(c.y), x[i]));
-      y[i] = mul2(both(c.z), sum[i]);
+      sum[i] = fma2(lo2(ao), sum[i], mul2(hi2(ao), x[i]));
+      y[i] = mul2(z, sum[i]);
     }
     R::write(dst + t * step, y);
   }
@@ -359,10 +372,10 @@ __global__ void __launch_bounds__(32) states_kernel(const StatesArgs a) {
 template <typename T, int D>
 struct BackShared {
   T rows[2][kC * D], grads[2][kC * D];
-  float4 coef[2][kC];         // alpha, omega, 1 / z, product of the alphas up to it over z
+  Coef coef[2][kC];
   float dots[2][kC][17];
   float other[2][kC];         // v's share of a dot
-  float first[kC];            // second element of dk
+  uint64_t loaded[2];
   Turn turn;
 };
 
@@ -373,7 +386,11 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
   extern __shared__ __align__(16) char raw[];
   BackShared<T, D>& sh = *reinterpret_cast<BackShared<T, D>*>(raw);
   const int lane = threadIdx.x & 31, which = threadIdx.x >> 5;
-  if (threadIdx.x == 0) sh.turn = take_turn(a);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sh.loaded[i]), 1);
+    fence_mbar_init();
+    sh.turn = take_turn(a);
+  }
   __syncthreads();
   const Turn turn = sh.turn;
   const int chunks = gridDim.x / a.Hkv, h = turn.index % a.Hkv, chunk = chunks - 1 - turn.index / a.Hkv;
@@ -387,11 +404,13 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
   const int after = (p.t1 - p.t0 + kC - 1) / kC - 1 - p.at;  // chunks after this one
   const bool in_chunk = lane < n;
   const GateIn gi = gate_in<T, D>(a, h, tok, in_chunk);
-  const long long step = (long long)a.Hkv * D, at = ((long long)tok0 * a.Hkv + h) * D + lane * R::kE;
+  const long long step = (long long)a.Hkv * D, at = ((long long)tok0 * a.Hkv + h) * D;
   T *mine = sh.rows[which] + lane * R::kE, *grads = sh.grads[which] + lane * R::kE;
-  R::copy(mine, static_cast<const T*>(which ? a.v : a.k) + at, step, n);
-  R::copy(grads, static_cast<const T*>(which ? a.dvt : a.dkt) + at, step, n);
-  cp_async_commit();
+  const uint32_t bar = smem_u32(&sh.loaded[which]);
+  if (lane == 0) mbar_arrive_expect_tx(bar, 2 * n * D * sizeof(T));
+  __syncwarp();
+  load_chunk<T, D>(sh.rows[which], static_cast<const T*>(which ? a.v : a.k) + at, step, n, bar);
+  load_chunk<T, D>(sh.grads[which], static_cast<const T*>(which ? a.dvt : a.dkt) + at, step, n, bar);
   // tokens from n on: zeros, and alpha 1, so that they change nothing
   for (int t = n; t < kC; ++t) {
     R::zero(mine + t * D);
@@ -421,20 +440,17 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
     if (lane >= off) prod *= o;
   }
   const float prod_all = __shfl_sync(0xffffffffu, prod, 31);
-  const float4* coef = sh.coef[which];
-  sh.coef[which][lane] = make_float4(g.alpha, g.omega, rz, prod * rz);
-  const bool gate_lane = threadIdx.x == 0;
-  auto value = [&](const T* of, int t, float2 (&x)[R::kP]) {
-    R::read(of + t * D, x);
-    if (gate_lane) x[0].x = 0.f;  // k's first component
+  const Coef* coef = sh.coef[which];
+  sh.coef[which][lane].alpha_omega = make_float4(g.alpha, g.alpha, g.omega, g.omega);
+  sh.coef[which][lane].rz_other = make_float4(rz, rz, prod * rz, prod * rz);
+  // two dots, the 16 partial sums of one in row t, those of the other in row t + 16
+  auto put = [&](int t, float2 c, float2 d) {
+    const float x = c.x + c.y, y = d.x + d.y;
+    const bool up = lane & 16;
+    const float sum = (up ? y : x) + __shfl_xor_sync(0xffffffffu, up ? x : y, 16);
+    sh.dots[which][t + (lane & 16)][lane & 15] = sum;
   };
-  // a token's dot: 16 partial sums
-  auto put = [&](int t, float2 d) {
-    float x = d.x + d.y;
-    x += __shfl_xor_sync(0xffffffffu, x, 16);
-    if (lane < 16) sh.dots[which][t][lane] = x;
-  };
-  auto take = [&]() {  // the lane's token's, over the warp's elements
+  auto take = [&]() {  // the dot of the lane's row
     __syncwarp();
     float x = 0.f;
 #pragma unroll
@@ -442,7 +458,11 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
     __syncwarp();
     return x;
   };
-  cp_async_wait<0>();
+  mbar_wait(bar, 0, a.error);  // (if it gives up, the fault bit is set and the results mean nothing)
+  if (which == 0) {  // k's first component is the gate
+    sh.rows[0][lane * D] = Elt<T>::from_f(0.f);
+    sh.grads[0][lane * D] = Elt<T>::from_f(0.f);
+  }
   __syncwarp();
   const long long row = row_of<D>(a, chunk, h, which), row_step = row_of<D>(a, 1, 0, 0);
   // forward over the chunk: the sums, g . A, and what the chunk passes on
@@ -456,19 +476,21 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
 #pragma unroll 8
     for (int t = 0; t < kC; ++t) {
       float2 x[R::kP], gr[R::kP], d = both(0.f);
-      value(mine, t, x);
-      value(grads, t, gr);
-      const float4 c = coef[t];
+      R::read(mine + t * D, x);
+      R::read(grads + t * D, gr);
+      const float4 ao = coef[t].alpha_omega;
+      const float2 w = hi2(coef[t].rz_other);
       if (t == kH)
 #pragma unroll
         for (int i = 0; i < R::kP; ++i) middle[i] = sum[i];
 #pragma unroll
       for (int i = 0; i < R::kP; ++i) {
-        sum[i] = fma2(both(c.x), sum[i], mul2(both(c.y), x[i]));
+        sum[i] = fma2(lo2(ao), sum[i], mul2(hi2(ao), x[i]));
         d = fma2(gr[i], sum[i], d);
-        pass[i] = fma2(both(c.w), gr[i], pass[i]);
+        pass[i] = fma2(w, gr[i], pass[i]);
       }
-      put(t, d);
+      const float one = d.x + d.y;  // 16 partial sums, written by both halves of the warp
+      sh.dots[which][t][lane & 15] = one + __shfl_xor_sync(0xffffffffu, one, 16);
     }
     if (p.at > 0) publish<R::kE>(a.sums + row, pass, turn.tag);
   }
@@ -495,7 +517,7 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
   }
   // from the last token to the first, half a chunk at a time: L, and its dots with the
   // values and with the sums before
-  T* dst = static_cast<T*>(which ? a.dv : a.dk) + at;
+  T* dst = static_cast<T*>(which ? a.dv : a.dk) + at + lane * R::kE;
   float domega = 0.f, dsum = 0.f;
 #pragma unroll 1
   for (int half = 1; half >= 0; --half) {
@@ -506,32 +528,31 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
 #pragma unroll
     for (int j = 0; j < kH; ++j) {
       float2 x[R::kP];
-      value(mine, t0 + j, x);
-      const float4 c = coef[t0 + j];
+      R::read(mine + (t0 + j) * D, x);
+      const float4 ao = coef[t0 + j].alpha_omega;
 #pragma unroll
       for (int i = 0; i < R::kP; ++i) {
         A[j][i] = sum[i];
-        sum[i] = fma2(both(c.x), sum[i], mul2(both(c.y), x[i]));
+        sum[i] = fma2(lo2(ao), sum[i], mul2(hi2(ao), x[i]));
       }
     }
 #pragma unroll
     for (int j = kH - 1; j >= 0; --j) {
       const int t = t0 + j;
       float2 x[R::kP], gr[R::kP], dx = both(0.f), da = both(0.f), out[R::kP];
-      value(mine, t, x);
-      value(grads, t, gr);
-      const float4 c = coef[t];
+      R::read(mine + t * D, x);
+      R::read(grads + t * D, gr);
+      const float4 ao = coef[t].alpha_omega;
+      const float2 z2 = lo2(coef[t].rz_other);
 #pragma unroll
       for (int i = 0; i < R::kP; ++i) {
-        const float2 l = fma2(gr[i], both(c.z), in[i]);
+        const float2 l = fma2(gr[i], z2, in[i]);
         dx = fma2(l, x[i], dx);
         da = fma2(l, A[j][i], da);
-        out[i] = mul2(both(c.y), l);
-        in[i] = mul2(both(c.x), l);
+        out[i] = mul2(hi2(ao), l);
+        in[i] = mul2(lo2(ao), l);
       }
-      put(j, dx);
-      put(kH + j, da);
-      if (gate_lane) sh.first[t] = out[0].y;
+      put(j, dx, da);
       if (t < n) R::write(dst + t * step, out);  // (the first component of dk comes below)
     }
     // lanes 0-15: with the values, 16-31: with the sums; to the lanes of their tokens
@@ -571,8 +592,8 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
     dalpha += dsum + sh.other[1][lane] + zeta * zbefore;
     float dx = 0.f;
     if (tok > p.t0) dx = (dalpha * g.alpha * g.rest - dbias * g.alpha) / a.temperature;
-    *reinterpret_cast<typename Pair<T>::Raw*>(static_cast<T*>(a.dk) + ((long long)tok * a.Hkv + h) * D) =
-        Pair<T>::from_f(make_float2(dx, sh.first[lane]));
+    // over what lane 0 has written there
+    static_cast<T*>(a.dk)[((long long)tok * a.Hkv + h) * D] = Elt<T>::from_f(dx);
     const T dq = Elt<T>::from_f(domega * g.omega * (1.f - g.omega) / (float)a.G);
     for (int j = 0; j < a.G; ++j)
       static_cast<T*>(a.dq)[(long long)tok * a.dq_tok + (long long)(h * a.G + j) * a.dq_head] = dq;
