@@ -18,9 +18,10 @@
 // product of its alphas, takes what comes in from the chunks before (after) it, and writes. What
 // comes in follows the chain
 //   in_{c+1} = own_c + prod_c in_c
-// from the nearest chunk whose own `in` is known or whose product is 0: decisions that are
-// nearly binary make the product of 32 alphas underflow, so that mostly one chunk is looked
-// at. The chain is always evaluated in this order, so results do not depend on how far others
+// over its neighbours back to where the product of the alphas between falls below 2^-126 (nearly
+// binary decisions: two or three chunks) or to the nearest of every 16th chunk, whose own `in`
+// is waited for. Where the chain begins follows from the data alone, so results do not depend on
+// how far others
 // have come. Chunks are taken from a counter, so that those a warp waits for have
 // started; they publish before they wait. Every published number carries the number of the launch
 // in the same 8 bytes: no fence or flag stands between it and its reader (a fence waited for
@@ -186,70 +187,100 @@ __device__ __forceinline__ void publish_zp(uint64_t* row, float z, float prod, u
   asm volatile("st.relaxed.gpu.global.v2.b64 [%0], {%1, %2};" ::"l"(row + D), "l"(tagged(z, tag)), "l"(tagged(prod, tag))
                : "memory");
 }
-// The lane's elements of a row, its z and product; whether all of the warp's were there.
-template <int D>
-__device__ __forceinline__ bool look(const uint64_t* row, float2 (&f)[D / 64], float2& zp, unsigned int tag) {
-  constexpr int kE = D / 32;
-  bool there = true;
-  auto two = [&](const uint64_t* at) {
-    uint64_t u, v;
-    asm volatile("ld.relaxed.gpu.global.v2.b64 {%0, %1}, [%2];" : "=l"(u), "=l"(v) : "l"(at) : "memory");
-    there &= (unsigned int)(u >> 32) == tag && (unsigned int)(v >> 32) == tag;
-    return make_float2(__uint_as_float((unsigned int)u), __uint_as_float((unsigned int)v));
-  };
-#pragma unroll
-  for (int i = 0; i < kE / 2; ++i) f[i] = two(row + (threadIdx.x & 31) * kE + 2 * i);
-  zp = two(row + D);
-  return __all_sync(0xffffffffu, there);
+__device__ __forceinline__ bool look_two(const uint64_t* at, float2& f, unsigned int tag) {
+  uint64_t u, v;
+  asm volatile("ld.relaxed.gpu.global.v2.b64 {%0, %1}, [%2];" : "=l"(u), "=l"(v) : "l"(at) : "memory");
+  f = make_float2(__uint_as_float((unsigned int)u), __uint_as_float((unsigned int)v));
+  return (unsigned int)(u >> 32) == tag && (unsigned int)(v >> 32) == tag;
 }
-// The same, once they are there. False: waited too long, or a fault has been found (a wait that
-// gave up, or cu_seqlens that do not fit, where a chunk may have no neighbour).
+// A row's z and product; the lane's elements of a row; whether they were there.
 template <int D>
-__device__ __forceinline__ bool await(const uint64_t* row, float2 (&f)[D / 64], float2& zp, unsigned int tag,
-                                      unsigned int* error) {
-  uint64_t since = 0;
-  for (int tries = 0;; ++tries) {
-    if (look<D>(row, f, zp, tag)) return true;
-    if (tries < 64) continue;
-    __nanosleep(500);
-    bool give_up = *reinterpret_cast<volatile unsigned int*>(error) != 0;
-    const uint64_t t = globaltimer_ns();
-    if (since == 0) since = t;
-    if (t - since > kWaitLimitNs) {
-      atomicOr(error, DMC_FAULT_WAIT_TIMEOUT);
-      give_up = true;
-    }
-    if (__any_sync(0xffffffffu, give_up)) return false;
+__device__ __forceinline__ bool look_zp(const uint64_t* row, float2& zp, unsigned int tag) {
+  return look_two(row + D, zp, tag);
+}
+template <int D>
+__device__ __forceinline__ bool look(const uint64_t* row, float2 (&f)[D / 64], unsigned int tag) {
+  bool there = true;
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) there &= look_two(row + (threadIdx.x & 31) * (D / 32) + 2 * i, f[i], tag);
+  return there;
+}
+// After tries that found nothing, by a whole warp: whether to give up, since this has taken too long or
+// a fault has been found (a wait that gave up, or cu_seqlens that do not fit, where a chunk may have no
+// neighbour).
+__device__ __forceinline__ bool give_up(uint64_t& since, unsigned int* error) {
+  __nanosleep(500);
+  bool over = *reinterpret_cast<volatile unsigned int*>(error) != 0;
+  const uint64_t t = globaltimer_ns();
+  if (since == 0) since = t;
+  if (t - since > kWaitLimitNs) {
+    atomicOr(error, DMC_FAULT_WAIT_TIMEOUT);
+    over = true;
   }
+  return __any_sync(0xffffffffu, over);
+}
+template <int D>
+__device__ __forceinline__ void await(const uint64_t* row, float2 (&f)[D / 64], unsigned int tag, unsigned int* error) {
+  uint64_t since = 0;
+  for (int tries = 0; !__all_sync(0xffffffffu, look<D>(row, f, tag)); ++tries)
+    if (tries >= 64 && give_up(since, error)) return;
 }
 
-// What comes into a chunk from its n neighbours on one side, `step` apart: the lane's sums x,
+// Chunks between two whose `in` others may wait for; products of alphas below kTiny carry nothing.
+constexpr int kAnchor = 16;
+constexpr float kTiny = 1.17549435e-38f;  // 2^-126
+
+// Whether others may ask for what comes into the chunk that has n neighbours on the side it comes from.
+__device__ __forceinline__ bool asked_for(int n, float prod) { return n > 0 && n % kAnchor == 0 && !(prod < kTiny); }
+
+// What comes into a chunk from its n > 0 neighbours on one side, `step` apart: the lane's sums x,
 // and z (Z). own, in: this chunk's rows.
 template <int D>
 __device__ __forceinline__ float come_in(const uint64_t* own, const uint64_t* in, int n, long long step, unsigned int tag,
                                          unsigned int* error, float2 (&x)[D / 64]) {
   constexpr int kP = D / 64;
-  float2 o[kP], zp;
-  float z;
-  int far = 1;  // chunks to look at
-  for (;; ++far) {
-    if (!await<D>(own + far * step, x, zp, tag, error)) break;
-    z = zp.x;
-    if (zp.y == 0.f || far == n) break;
-    float2 zi;
-    if (look<D>(in + far * step, o, zi, tag)) {
-#pragma unroll
-      for (int i = 0; i < kP; ++i) x[i] = fma2(both(zp.y), o[i], x[i]);
-      z = fmaf(zp.y, zi.x, z);
-      break;
-    }
+  const int lane = threadIdx.x & 31, d = (n - 1) % kAnchor + 1;  // the d-th neighbour is an anchor or the last
+  // a neighbour per lane: its z and the product of its alphas
+  float2 zp = make_float2(0.f, 1.f);
+  uint64_t since = 0;
+  for (int tries = 0;; ++tries) {
+    const bool there = lane >= d || look_zp<D>(own + (lane + 1) * step, zp, tag);
+    if (__all_sync(0xffffffffu, there)) break;
+    if (tries >= 64 && give_up(since, error)) break;
   }
-#pragma unroll 1
-  for (--far; far > 0; --far) {
-    look<D>(own + far * step, o, zp, tag);
+  float upto = zp.y;  // the product of the nearest lane + 1
 #pragma unroll
-    for (int i = 0; i < kP; ++i) x[i] = fma2(both(zp.y), x[i], o[i]);
-    z = fmaf(zp.y, z, zp.x);
+  for (int off = 1; off < kAnchor; off <<= 1) {
+    const float o = __shfl_up_sync(0xffffffffu, upto, off);
+    if (lane >= off) upto *= o;
+  }
+  const unsigned int end = __ballot_sync(0xffffffffu, lane < d && upto < kTiny);
+  const int far = end ? __ffs(end) : d;
+  float z = 0.f;
+#pragma unroll
+  for (int i = 0; i < kP; ++i) x[i] = both(0.f);
+  if (!end && d < n) {
+    float2 zi;
+    await<D>(in + d * step, x, tag, error);
+    for (int tries = 0; !look_zp<D>(in + d * step, zi, tag); ++tries)
+      if (tries >= 64 && give_up(since, error)) break;
+    z = zi.x;
+  }
+  float2 o[kP], next[kP];
+  bool there = look<D>(own + far * step, o, tag);
+#pragma unroll 1
+  for (int i = far; i > 0; --i) {
+    bool soon = true;
+    if (i > 1) soon = look<D>(own + (i - 1) * step, next, tag);
+    if (!__all_sync(0xffffffffu, there)) await<D>(own + i * step, o, tag, error);
+    const float zo = __shfl_sync(0xffffffffu, zp.x, i - 1), prod = __shfl_sync(0xffffffffu, zp.y, i - 1);
+#pragma unroll
+    for (int k = 0; k < kP; ++k) {
+      x[k] = fma2(both(prod), x[k], o[k]);
+      o[k] = next[k];
+    }
+    z = fmaf(prod, z, zo);
+    there = soon;
   }
   return z;
 }
@@ -330,7 +361,7 @@ __global__ void __launch_bounds__(32) states_kernel(const StatesArgs a) {
   for (int i = 0; i < R::kP; ++i) sum[i] = both(0.f);
   if (p.at > 0) {
     zin = come_in<D>(a.sums + row, a.carry + row, p.at, -row_step, turn.tag, a.error, sum);
-    if (goes_on && prod != 0.f) {  // (with a product of 0 nobody asks for it)
+    if (goes_on && asked_for(p.at, prod)) {
       publish<R::kE>(a.carry + row, sum, turn.tag);
       if (lane == 0) publish_zp<D>(a.carry + row, zin, 0.f, turn.tag);
     }
@@ -510,7 +541,7 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
   for (int i = 0; i < R::kP; ++i) in[i] = both(0.f);
   if (after > 0) {
     zin = come_in<D>(a.sums + row, a.carry + row, after, row_step, turn.tag, a.error, in);
-    if (p.at > 0 && prod_all != 0.f) {  // (with a product of 0 nobody asks for what came in)
+    if (p.at > 0 && asked_for(after, prod_all)) {
       publish<R::kE>(a.carry + row, in, turn.tag);
       if (lane == 0) publish_zp<D>(a.carry + row, zin, 0.f, turn.tag);
     }
