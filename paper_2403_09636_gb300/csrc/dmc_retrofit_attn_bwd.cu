@@ -17,6 +17,11 @@
 // dQ: a work item is 128 queries of one head; it walks over the K and V tiles they see.
 //   S (j + 1), dP (j + 1), dQ += dS K (j)
 // with two dP buffers, so that a step's row work runs beside three products.
+// delta from the rounded `out` is off by up to 2^-8 |dO| |out|, which in short sequences is the
+// largest error of all. But the weights of a row add up to 1, so that the sum of its dS with
+// an approximate delta is what delta lacks: dQ's kernel, which runs first, adds it up unrounded, puts
+// delta right for dK, dV and dbias, and for its own dS in items of a single tile, whose rows
+// see few others (in longer ones the sum over the row of P k, by which it enters, is small).
 // In both, warps 0-7 do the row work, four warps for each half of the 128 columns.
 #include "dmc_retrofit_attn.cuh"
 
@@ -456,7 +461,8 @@ struct DqShared {
   float bias[8][2][64];          // each row warp's copy, this step's and the next's
   uint64_t q_full, q_empty, o_full, o_empty;
   uint64_t k_full[3], k_empty[3], v_full[3], v_empty[3];
-  uint64_t s_full, s_free, dp_full[2], ds_ready[2], dq_done[2];
+  uint64_t s_full, s_free, dp_full[2], ds_ready[2], dq_done[2], lack_full;
+  float lack[2][2][kR];  // what delta lacks, by the two halves of the columns, of every other item
   WorkRing work;
   uint32_t tmem;
   int abort;
@@ -502,6 +508,7 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
       mbar_init(smem_u32(&sh.dq_done[i]), 1);
     }
     mbar_init(smem_u32(&sh.s_free), 8);
+    mbar_init(smem_u32(&sh.lack_full), 8);
     work_init(sh.work);
     fence_mbar_init();
     sh.abort = 0;
@@ -666,7 +673,7 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
     const uint32_t tS = tmem + lane_base + half * 64;
     const float scale = 1.f / sqrtf((float)D), qscale = kLog2e * scale;
     const float2 scale2 = make_float2(qscale, qscale);
-    uint32_t n = 0;
+    uint32_t n = 0, ni = 0;
     bool ok = true;
     int turn = 0;
     float nrow[2] = {0.f, 0.f};   // the next item's row
@@ -700,6 +707,17 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
     while (w.h >= 0) {
       const float nl = nrow[0], delta = nrow[1];
       const float2 nl2 = make_float2(nl, nl), nd2 = make_float2(-delta, -delta);
+      float2 lack = make_float2(0.f, 0.f);
+      // the row's, from both halves of its columns; by all row warps, once per item
+      auto whole = [&](float& sum) {
+        float(&l)[2][kR] = sh.lack[ni & 1];
+        l[half][r] = lack.x + lack.y;
+        arrive_warp(&sh.lack_full);
+        if (!wait(&sh.lack_full, ni & 1)) return false;
+        sum = l[0][r] + l[1][r];
+        return true;
+      };
+      float sum = 0.f;
 #pragma unroll 1
       for (int j = 0; j < w.steps; ++j, ++n) {
         const float* b = sh.bias[warp][j & 1];
@@ -746,7 +764,6 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
         tc_ld32(tP, d);
         tc_ld32(tP + 32, d + 32);
         tc_wait_ld();
-        uint32_t pk[32];
 #pragma unroll
         for (int c = 0; c < 32; ++c) {
           float2 u = mul2(make_float2(p[2 * c], p[2 * c + 1]), add2(make_float2(d[2 * c], d[2 * c + 1]), nd2));
@@ -754,15 +771,32 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
             if (2 * c > r - half * 64) u.x = 0.f;
             if (2 * c + 1 > r - half * 64) u.y = 0.f;
           }
-          pk[c] = Chunk<__nv_bfloat16>::pack2(u.x, u.y);
+          lack = add2(lack, u);
+          d[2 * c] = u.x;
+          d[2 * c + 1] = u.y;
         }
+        if (w.steps == 1) {
+          if (!(ok = whole(sum))) break;
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            const float2 u = fma2(make_float2(p[2 * c], p[2 * c + 1]), make_float2(-sum, -sum), make_float2(d[2 * c], d[2 * c + 1]));
+            d[2 * c] = u.x;
+            d[2 * c + 1] = u.y;
+          }
+        }
+        uint32_t pk[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) pk[c] = Chunk<__nv_bfloat16>::pack2(d[2 * c], d[2 * c + 1]);
         tc_st32(tP, pk);
         tc_wait_st();
         tc_fence_before();
         arrive_warp(&sh.ds_ready[n & 1]);
       }
       if (!ok) break;
-      // ---- this thread's half of its row of dQ
+      // ---- delta as it should be, and this thread's half of its row of dQ
+      if (w.steps > 1 && !(ok = whole(sum))) break;
+      ++ni;
+      if (half == 0 && w.q0 + r < w.t1) row_tile(a, row_tiles, w.h, w.tile)[kR + r] = delta + sum;
       const DqItem after = next();
       if (!(ok = wait(&sh.dq_done[(n - 1) & 1], ((n - 1) >> 1) & 1))) break;
       tc_fence_after();
@@ -813,8 +847,8 @@ cudaError_t backward(const AttnArgs& a, cudaStream_t stream) {
   const long long dkv_items = (long long)tiles * a.Hkv, dq_items = (long long)tiles * a.Hq;
   if (dq_items > INT_MAX / 2) return cudaErrorInvalidValue;
   attn_rows_kernel<D><<<dim3(tiles, a.Hq), 256, 0, stream>>>(a, tiles);
-  dkv<<<(unsigned)(dkv_items < sms ? dkv_items : sms), kAttnThreads, dkv_bytes, stream>>>(a, maps, (int)dkv_items, tiles);
   dq<<<(unsigned)(dq_items < sms ? dq_items : sms), kAttnThreads, dq_bytes, stream>>>(a, maps, (int)dq_items, tiles);
+  dkv<<<(unsigned)(dkv_items < sms ? dkv_items : sms), kAttnThreads, dkv_bytes, stream>>>(a, maps, (int)dkv_items, tiles);
   return cudaGetLastError();
 }
 
