@@ -59,7 +59,7 @@ int loss_piece(const dmc_retrofit_config* c) {
 }
 
 struct Offsets {
-  size_t error, sums, carry, cleared, rows, part_m, part_l, target_logit, dh, grad, hidden_parts, weight_parts, total;
+  size_t error, sums, carry, cleared, rows, shares, part_m, part_l, target_logit, dh, grad, hidden_parts, weight_parts, total;
   int piece;
 };
 
@@ -80,6 +80,9 @@ Offsets offsets(const dmc_retrofit_config* c) {
     o.rows = at;
     at = align_up(at + (c->dtype == DMC_F32 ? tokens * 4 : (size_t)pieces(c->max_tokens, c->max_seqs, 128) * 1024) *
                            c->num_q_heads);
+    o.shares = at;
+    if (c->dtype == DMC_BF16)
+      at = align_up(at + attn_sums(c->max_tokens, c->num_kv_heads, c->num_q_heads / c->num_kv_heads, c->head_dim) * 4);
   }
   if (has_loss(*c)) {
     o.piece = loss_piece(c);
@@ -176,6 +179,7 @@ dmc::AttnArgs attn_args(dmc_retrofit_t h, int32_t num_seqs, const void* q, const
   a.v = v;
   a.bias = bias;
   a.rows = reinterpret_cast<float*>(h->base + h->at.rows);
+  a.sums = reinterpret_cast<float*>(h->base + h->at.shares);
   a.counter = reinterpret_cast<int*>(h->base + h->at.error + 128);
   a.error = reinterpret_cast<unsigned int*>(h->base + h->at.error);
   return a;

@@ -142,9 +142,26 @@ struct AttnArgs {
   const void* dout;
   void *dq, *dk, *dv, *dbias;
   float* rows;          // scratch, per query: see attn_rows_kernel ([Hq][total] deltas for fp32)
+  float* sums;          // scratch: sums of shares of a group's queries, see attn_shares
+  int shares;
   int* counter;         // work items handed out, CTAs done: zero between launches
   unsigned int* error;
 };
+
+// Shares into which the bf16 kernel of dK and dV splits each group's queries: one, unless
+// the tiles of its KV heads (`items`) are fewer than two per SM of this GPU, when shares of whole heads make
+// up for it. So there are never 4 * 152 items of more than one share, and their sums' scratch is bounded.
+constexpr int kSplitItems = 2 * 152;
+inline int attn_shares(long long items, int G) {
+  if (items >= kSplitItems) return 1;
+  const int n = (int)((kSplitItems + items - 1) / items), heads = (G + n - 1) / n;
+  return (G + heads - 1) / heads;  // no more than the longest share asks for
+}
+// Numbers of the shares' sums: 2 D + 1 per row of 128 of each of their items
+inline size_t attn_sums(int max_tokens, int Hkv, int G, int D) {
+  const size_t all = (size_t)max_tokens * Hkv * G, most = 2 * kSplitItems * 128;
+  return G == 1 ? 0 : (all < most ? all : most) * (2 * D + 1);
+}
 
 struct LossArgs {
   int N, H, V;

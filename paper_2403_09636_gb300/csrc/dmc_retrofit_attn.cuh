@@ -190,14 +190,13 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, 
   for (int c = 0; c < D / 64; ++c) tma_load(dst + c * (kR * 128), map, bar, c * 64, head, tok);
 }
 
-// Rows of the epilogue: 32 columns of each lane's row (values f) to global memory through the
-// warp's stage; row r of the warp at dst + r * stride bytes, rows at and after `rows` left out.
-__device__ __forceinline__ void write_rows(unsigned char* stage, const float* f, char* dst, long long stride, int rows) {
+// Rows of the epilogue: 64 bytes of each lane's row to global memory through the warp's
+// stage; row r of the warp at dst + r * stride bytes, rows at and after `rows` left out.
+__device__ __forceinline__ void write_rows(unsigned char* stage, const uint4 (&x)[4], char* dst, long long stride, int rows) {
   const int lane = threadIdx.x & 31;
   __syncwarp();  // the stage has been read
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    *reinterpret_cast<uint4*>(stage + lane * kStageRow + i * 16) = Chunk<__nv_bfloat16>::pack(f + i * 8);
+  for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(stage + lane * kStageRow + i * 16) = x[i];
   __syncwarp();
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -205,6 +204,13 @@ __device__ __forceinline__ void write_rows(unsigned char* stage, const float* f,
     const uint4 v = *reinterpret_cast<const uint4*>(stage + r * kStageRow + (lane & 3) * 16);
     if (r < rows) *reinterpret_cast<uint4*>(dst + r * stride + (lane & 3) * 16) = v;
   }
+}
+// 32 values of each row, as bf16
+__device__ __forceinline__ void write_rows(unsigned char* stage, const float* f, char* dst, long long stride, int rows) {
+  uint4 x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = Chunk<__nv_bfloat16>::pack(f + i * 8);
+  write_rows(stage, x, dst, stride, rows);
 }
 
 // Rows [r0, 128) of a tile set to zero, by a warp: weights are zero there, but what lies

@@ -101,15 +101,32 @@ struct DkvItem {
   int t1, j0;      // the sequence's end, the first row of K
   int hk, tile0;   // KV head, the row tile (attn_rows_kernel) of the query tile at j0
   int tiles;       // query tiles that see the rows
+  int share, h0;   // share of the group's queries, its first head
+  int heads;       // its heads
 };
-__device__ __forceinline__ DkvItem dkv_item(const Work& w) {
+// The group's queries are split over `a.shares` items when there are few (see backward): whole heads,
+// the same number in each but for one. KV heads fastest, so that neighbours in the order share tiles of Q and dO.
+__device__ __forceinline__ DkvItem dkv_item(const AttnArgs& a, const Work& w) {
   DkvItem it;
   it.t1 = w.t1;
   it.j0 = w.t0 + w.at * kR;
-  it.hk = w.head;
+  it.hk = w.head < 0 ? -1 : w.head % a.Hkv;
+  it.share = w.head < 0 ? 0 : w.head / a.Hkv;
+  const int g0 = it.share * a.G / a.shares;
+  it.h0 = it.hk * a.G + g0;
+  it.heads = (it.share + 1) * a.G / a.shares - g0;
   it.tile0 = w.t0 / kR + w.seq + w.at;
   it.tiles = (w.t1 - it.j0 + kR - 1) / kR;
   return it;
+}
+
+// The shares' sums, to be added up by attn_join_kernel: [share][KV head][token][D] of dV, then of
+// dK, then [share][KV head][token] of dbias.
+__device__ __forceinline__ float* share_rows(const AttnArgs& a, int D, bool dk, int share, int hk, int token) {
+  return a.sums + ((((long long)(dk ? a.shares : 0) + share) * a.Hkv + hk) * a.seqs.total + token) * D;
+}
+__device__ __forceinline__ float* share_dbias(const AttnArgs& a, int D, int share, int hk) {
+  return a.sums + (2ll * a.shares * D * a.Hkv + (long long)share * a.Hkv + hk) * a.seqs.total;
 }
 
 template <int D, bool kBias>
@@ -158,9 +175,9 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
       bool ok = true;
       WorkSource src = work_source();
       while (ok) {
-        const Work work = take_work(sh.work, src, a.seqs, kR, true, a.Hkv, items, a.counter, wait);
+        const Work work = take_work(sh.work, src, a.seqs, kR, true, a.Hkv * a.shares, items, a.counter, wait);
         if (work.head < 0) break;
-        const DkvItem w = dkv_item(work);
+        const DkvItem w = dkv_item(a, work);
         ok = wait(&sh.k_empty, (ni & 1) ^ 1) && wait(&sh.v_empty, (ni & 1) ^ 1);
         if (!ok) break;
         if (tc_elect()) {
@@ -171,11 +188,11 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
         }
         __syncwarp();
         ++ni;
-        const int steps = a.G * w.tiles;
-        int g = 0, i = 0;
+        const int steps = w.heads * w.tiles;
+        int h = w.h0, i = 0;
 #pragma unroll 1
         for (int x = 0; x < steps; ++x, ++n) {
-          const int s = n & 1, h = w.hk * a.G + g;
+          const int s = n & 1;
           ok = wait(&sh.q_empty[s], ((n >> 1) & 1) ^ 1);
           if (!ok) break;
           if (tc_elect()) {
@@ -198,7 +215,7 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
           __syncwarp();
           if (++i == w.tiles) {
             i = 0;
-            ++g;
+            ++h;
           }
           if (!ok) {
             ++n;
@@ -242,8 +259,8 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
       while (ok) {
         const Work work = next_work(sh.work, turn, wait);
         if (work.head < 0) break;
-        const DkvItem w = dkv_item(work);
-        const int tiles = w.tiles, steps = a.G * tiles;
+        const DkvItem w = dkv_item(a, work);
+        const int tiles = w.tiles, steps = w.heads * tiles;
         const int last_rows = w.t1 - w.j0 - (tiles - 1) * kR;  // queries of the last tile
         ok = wait(&sh.k_full, ni & 1) && wait(&sh.v_full, ni & 1);
         int i = 0;  // query tile of step x
@@ -317,7 +334,7 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
     float nb = 0.f;  // the next item's bias
     auto next = [&]() {
       const Work work = next_work(sh.work, turn, wait);
-      const DkvItem w = dkv_item(work);
+      const DkvItem w = dkv_item(a, work);
       nb = 0.f;
       if (kBias && work.head >= 0 && w.j0 + r < w.t1) nb = a.bias[(long long)w.hk * a.seqs.total + w.j0 + r] * kLog2e;
       return w;
@@ -327,7 +344,7 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
       const int row = w.j0 + r;
       const float b = nb;
       const float2 b2 = make_float2(b, b);
-      const int steps = a.G * w.tiles;
+      const int steps = w.heads * w.tiles;
       float2 db = make_float2(0.f, 0.f);
       int i = 0;
 #pragma unroll 1
@@ -422,7 +439,20 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
         if (half)
 #pragma unroll
           for (int c = 0; c < 32; ++c) f[c] *= scale;
-        write_rows(sh.stage[warp], f, dst + c0 * 2, (long long)a.Hkv * D * 2, rows);
+        if (a.shares == 1) {
+          write_rows(sh.stage[warp], f, dst + c0 * 2, (long long)a.Hkv * D * 2, rows);
+        } else {
+          char* sums = reinterpret_cast<char*>(share_rows(a, D, half, w.share, w.hk, row0) + c0);
+#pragma unroll
+          for (int c = 0; c < 32; c += 16) {
+            uint4 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              x[i] = make_uint4(__float_as_uint(f[c + 4 * i]), __float_as_uint(f[c + 4 * i + 1]),
+                                __float_as_uint(f[c + 4 * i + 2]), __float_as_uint(f[c + 4 * i + 3]));
+            write_rows(sh.stage[warp], x, sums + c * 4, D * 4, rows);
+          }
+        }
       }
       if (kBias && a.dbias) {
         // the sum of the two halves of the columns (the second half's next value is written
@@ -433,8 +463,13 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
           arrive_warp(&sh.db_full);
         } else {
           if (!(ok = wait(&sh.db_full, ni & 1))) break;
-          if (row < w.t1)
-            static_cast<__nv_bfloat16*>(a.dbias)[(long long)w.hk * a.seqs.total + row] = __float2bfloat16_rn(own + sh.db[r]);
+          const float all = own + sh.db[r];
+          if (row < w.t1) {
+            if (a.shares == 1)
+              static_cast<__nv_bfloat16*>(a.dbias)[(long long)w.hk * a.seqs.total + row] = __float2bfloat16_rn(all);
+            else
+              share_dbias(a, D, w.share, w.hk)[row] = all;
+          }
         }
       }
       ++ni;
@@ -449,6 +484,46 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
   }
   if (tid == 0) work_done(a.counter);
+}
+
+// The shares' sums of 128 rows of a KV head, in the shares' order: blockIdx.z / 2 is a quarter of
+// the rows, its lowest bit dV or dK. Bound by the L2 cache, where the sums still are.
+template <int D>
+__global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
+  constexpr int kLanes = D / 4, kPer = 256 / kLanes, kRows = kR / 4;
+  const int hk = blockIdx.y;
+  const bool dk = blockIdx.z & 1;
+  const Piece p = find_piece(a.seqs, kR, blockIdx.x);
+  if (!p.ok) return;
+  const int tok0 = p.t0 + p.at * kR + (blockIdx.z >> 1) * kRows, rows = min(kRows, p.t1 - tok0);
+  const int c = threadIdx.x % kLanes * 4;
+  float4 x[kRows / kPer];
+#pragma unroll
+  for (int i = 0; i < kRows / kPer; ++i) x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = 0; s < a.shares; ++s) {
+#pragma unroll
+    for (int i = 0; i < kRows / kPer; ++i) {
+      const int r = threadIdx.x / kLanes + i * kPer;
+      if (r >= rows) continue;
+      const float4 y = *reinterpret_cast<const float4*>(share_rows(a, D, dk, s, hk, tok0 + r) + c);
+      x[i].x += y.x;
+      x[i].y += y.y;
+      x[i].z += y.z;
+      x[i].w += y.w;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kRows / kPer; ++i) {
+    const int r = threadIdx.x / kLanes + i * kPer;
+    if (r >= rows) continue;
+    const uint2 y = make_uint2(Chunk<__nv_bfloat16>::pack2(x[i].x, x[i].y), Chunk<__nv_bfloat16>::pack2(x[i].z, x[i].w));
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(dk ? a.dk : a.dv) + ((long long)(tok0 + r) * a.Hkv + hk) * D + c) = y;
+  }
+  if (!dk && a.bias && a.dbias && (int)threadIdx.x < rows) {
+    float b = 0.f;
+    for (int s = 0; s < a.shares; ++s) b += share_dbias(a, D, s, hk)[tok0 + threadIdx.x];
+    static_cast<__nv_bfloat16*>(a.dbias)[(long long)hk * a.seqs.total + tok0 + threadIdx.x] = __float2bfloat16_rn(b);
+  }
 }
 
 // ---------------------------------------------------------------- dQ
@@ -828,7 +903,7 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
 }
 
 template <int D, bool kBias>
-cudaError_t backward(const AttnArgs& a, cudaStream_t stream) {
+cudaError_t backward(AttnArgs a, cudaStream_t stream) {
   constexpr int dkv_bytes = sizeof(DkvShared<D>) + 1024, dq_bytes = sizeof(DqShared<D>) + 1024;
   static_assert(dkv_bytes <= 227 * 1024 && dq_bytes <= 227 * 1024, "one CTA's shared memory");
   auto* dkv = attn_dkv_kernel<D, kBias>;
@@ -844,11 +919,14 @@ cudaError_t backward(const AttnArgs& a, cudaStream_t stream) {
   if (e == cudaSuccess) e = heads_map(&maps.o, a.dout, D, a.Hq, a.seqs.total);
   if (e != cudaSuccess) return e;
   const int tiles = row_tiles(a);
-  const long long dkv_items = (long long)tiles * a.Hkv, dq_items = (long long)tiles * a.Hq;
+  long long dkv_items = (long long)tiles * a.Hkv, dq_items = (long long)tiles * a.Hq;
   if (dq_items > INT_MAX / 2) return cudaErrorInvalidValue;
+  a.shares = attn_shares(dkv_items, a.G);
+  dkv_items *= a.shares;
   attn_rows_kernel<D><<<dim3(tiles, a.Hq), 256, 0, stream>>>(a, tiles);
   dq<<<(unsigned)(dq_items < sms ? dq_items : sms), kAttnThreads, dq_bytes, stream>>>(a, maps, (int)dq_items, tiles);
   dkv<<<(unsigned)(dkv_items < sms ? dkv_items : sms), kAttnThreads, dkv_bytes, stream>>>(a, maps, (int)dkv_items, tiles);
+  if (a.shares > 1) attn_join_kernel<D><<<dim3(tiles, a.Hkv, 8), 256, 0, stream>>>(a);
   return cudaGetLastError();
 }
 
