@@ -133,7 +133,7 @@ attn_forward_kernel(const AttnArgs a, const __grid_constant__ AttnMaps maps, int
       // ---------------------------------------------------------------- loads
       uint32_t n = 0, q_par = 0, q_any = 0;  // bit t: parity of query tile t's next Q, whether there was one
       bool ok = true;
-      WorkSource src = work_source();
+      WorkSource src = work_source(a.seqs);
       int single = 0;
       while (ok) {
         const Work work = take_work(sh.work, src, a.seqs, kItem, false, a.Hq, items, a.counter, wait);

@@ -30,17 +30,26 @@ struct Work {
 // order (ordered_work), where one sequence matters less and the search over L would take longer
 // than a short item. False: there are no more.
 constexpr int kRankedSeqs = 128;
-__device__ __forceinline__ bool ranked_work(const Seqs& q, int piece, bool from_end, int k, Work& w) {
+struct RankedSeqs {
+  int t0[kRankedSeqs / 32], t1[kRankedSeqs / 32];  // the lane's sequences, empty where there is none
+};
+__device__ __forceinline__ void ranked_seqs(const Seqs& q, RankedSeqs& r) {
+#pragma unroll
+  for (int i = 0; i < kRankedSeqs / 32; ++i) {
+    const int s = i * 32 + (threadIdx.x & 31);
+    r.t0[i] = r.t1[i] = 0;
+    if (q.num > kRankedSeqs || s >= q.num) continue;
+    r.t0[i] = q.cu[s];
+    r.t1[i] = q.cu[s + 1];
+    if (!seq_ok(q, r.t0[i], r.t1[i])) r.t1[i] = r.t0[i];
+  }
+}
+__device__ __forceinline__ bool ranked_work(const RankedSeqs& q, int piece, bool from_end, int k, Work& w) {
   const int lane = threadIdx.x & 31;
   int n[kRankedSeqs / 32], most = 0;
 #pragma unroll
   for (int i = 0; i < kRankedSeqs / 32; ++i) {
-    const int s = i * 32 + lane;
-    n[i] = 0;
-    if (s < q.num) {
-      const int t0 = q.cu[s], t1 = q.cu[s + 1];
-      if (seq_ok(q, t0, t1)) n[i] = (t1 - t0 + piece - 1) / piece;
-    }
+    n[i] = (q.t1[i] - q.t0[i] + piece - 1) / piece;
     most = max(most, n[i]);
   }
   auto f = [&](int L) {
@@ -55,21 +64,19 @@ __device__ __forceinline__ bool ranked_work(const Seqs& q, int piece, bool from_
     const int mid = (lo + hi) >> 1;
     if (f(mid) > k) lo = mid; else hi = mid;
   }
-  int left = k - f(lo + 1), seq = 0;  // the left-th sequence of more than lo pieces
+  int left = k - f(lo + 1);  // the left-th sequence of more than lo pieces
 #pragma unroll
   for (int i = 0; i < kRankedSeqs / 32; ++i) {
     const unsigned int b = __ballot_sync(0xffffffffu, n[i] > lo);
-    const int c = __popc(b);
-    if (left >= 0 && left < c) {
-      unsigned int m = b;
-      for (int j = 0; j < left; ++j) m &= m - 1;
-      seq = i * 32 + __ffs(m) - 1;
+    const unsigned int hit = __ballot_sync(0xffffffffu, n[i] > lo && __popc(b & ((1u << lane) - 1)) == left);
+    if (hit) {
+      const int from = __ffs(hit) - 1;
+      w.seq = i * 32 + from;
+      w.t0 = __shfl_sync(0xffffffffu, q.t0[i], from);
+      w.t1 = __shfl_sync(0xffffffffu, q.t1[i], from);
     }
-    left -= c;
+    left -= __popc(b);
   }
-  w.seq = seq;
-  w.t0 = q.cu[seq];
-  w.t1 = q.cu[seq + 1];
   w.at = from_end ? (w.t1 - w.t0 + piece - 1) / piece - 1 - lo : lo;
   return true;
 }
@@ -130,9 +137,17 @@ __device__ __forceinline__ void work_done(int* counter) {
 
 // Warp 9's side.
 struct WorkSource {
-  int number, turn;  // the next work's, the next place in the ring
+  int number;  // the next work's, in the first lane (elsewhere it would be waited for)
+  int turn;    // the next place in the ring
+  RankedSeqs seqs;
 };
-__device__ __forceinline__ WorkSource work_source() { return {(int)blockIdx.x, 0}; }
+__device__ __forceinline__ WorkSource work_source(const Seqs& q) {
+  WorkSource src;
+  src.number = blockIdx.x;
+  src.turn = 0;
+  ranked_seqs(q, src.seqs);
+  return src;
+}
 // The next work, handed to the other warps too (head < 0: there is none, or a wait gave up).
 template <typename Wait>
 __device__ __forceinline__ Work take_work(WorkRing& ring, WorkSource& src, const Seqs& q, int piece, bool from_end, int heads,
@@ -140,13 +155,12 @@ __device__ __forceinline__ Work take_work(WorkRing& ring, WorkSource& src, const
   Work w;
   w.t0 = w.t1 = w.seq = w.at = 0;
   w.head = -1;
-  if (src.number < most) {
-    int next = 0;
-    if ((threadIdx.x & 31) == 0) next = (int)gridDim.x + atomicAdd(counter, 1);
-    const int k = src.number / heads;
-    const bool there = q.num <= kRankedSeqs ? ranked_work(q, piece, from_end, k, w) : ordered_work(q, piece, from_end, k, w);
-    if (there) w.head = src.number % heads;
-    src.number = __shfl_sync(0xffffffffu, next, 0);
+  const int number = __shfl_sync(0xffffffffu, src.number, 0);
+  if (number < most) {
+    if ((threadIdx.x & 31) == 0) src.number = (int)gridDim.x + atomicAdd(counter, 1);
+    const int k = number / heads;
+    const bool there = q.num <= kRankedSeqs ? ranked_work(src.seqs, piece, from_end, k, w) : ordered_work(q, piece, from_end, k, w);
+    if (there) w.head = number % heads;
   }
   const int sl = src.turn & 1;
   if (!wait(&ring.empty[sl], ((src.turn >> 1) & 1) ^ 1)) {
@@ -217,12 +231,12 @@ __device__ __forceinline__ void write_rows(unsigned char* stage, const float* f,
 // beyond a sequence's end need not be a number.
 template <int D>
 __device__ __forceinline__ void zero_rows(unsigned char* tile, int r0) {
-  constexpr int kPieces = D / 8;  // of 16 bytes per row
-#pragma unroll 1
-  for (int x = threadIdx.x & 31; x < (kR - r0) * kPieces; x += 32) {
-    const int r = r0 + x / kPieces, j = x % kPieces;
-    *reinterpret_cast<uint4*>(tile + (j >> 3) * (kR * 128) + r * 128 + (j & 7) * 16) = make_uint4(0, 0, 0, 0);
-  }
+  constexpr int kPieces = D / 8, kRows = 32 / kPieces;  // 16-byte pieces of a row, rows at a time
+  const int j = threadIdx.x % kPieces;
+  unsigned char* at = tile + (j >> 3) * (kR * 128) + (j & 7) * 16;
+#pragma unroll 4
+  for (int r = r0 + (threadIdx.x & 31) / kPieces; r < kR; r += kRows)
+    *reinterpret_cast<uint4*>(at + r * 128) = make_uint4(0, 0, 0, 0);
   fence_async_smem();
   __syncwarp();
 }

@@ -173,7 +173,7 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
       // ---------------------------------------------------------------- loads
       uint32_t n = 0, ni = 0;  // query tiles, items
       bool ok = true;
-      WorkSource src = work_source();
+      WorkSource src = work_source(a.seqs);
       while (ok) {
         const Work work = take_work(sh.work, src, a.seqs, kR, true, a.Hkv * a.shares, items, a.counter, wait);
         if (work.head < 0) break;
@@ -607,7 +607,7 @@ attn_dq_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int items
       // ---------------------------------------------------------------- loads
       uint32_t nk = 0, nv = 0, nq = 0, ni = 0;  // K tiles, V halves, Q tiles and dO tiles requested
       bool ok = true;
-      WorkSource src = work_source();
+      WorkSource src = work_source(a.seqs);
       while (ok) {
         const Work work = take_work(sh.work, src, a.seqs, kR, false, a.Hq, items, a.counter, wait);
         if (work.head < 0) break;
