@@ -81,8 +81,7 @@ Offsets offsets(const dmc_retrofit_config* c) {
     at = align_up(at + (c->dtype == DMC_F32 ? tokens * 4 : (size_t)pieces(c->max_tokens, c->max_seqs, 128) * 1024) *
                            c->num_q_heads);
     o.shares = at;
-    if (c->dtype == DMC_BF16)
-      at = align_up(at + attn_sums(c->max_tokens, c->num_kv_heads, c->num_q_heads / c->num_kv_heads, c->head_dim) * 4);
+    at = align_up(at + attn_sums(c->max_tokens, c->num_kv_heads, c->num_q_heads / c->num_kv_heads, c->head_dim) * 4);
   }
   if (has_loss(*c)) {
     o.piece = loss_piece(c);
@@ -122,7 +121,63 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const LossArgs a, int sh
   a.loss[t] = target >= 0 && target < a.V ? lse - a.target_logit[t] : 0.f;
 }
 
+// The shares' sums of 128 rows of a KV head, in the shares' order: blockIdx.z / 2 is a quarter of
+// the rows, its lowest bit dV or dK. Bound by the L2 cache, where the sums still are.
+template <int D, typename T>
+__global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
+  constexpr int kLanes = D / 4, kPer = 256 / kLanes, kRows = 128 / 4;
+  const int hk = blockIdx.y;
+  const bool dk = blockIdx.z & 1;
+  const Piece p = find_piece(a.seqs, 128, blockIdx.x);
+  if (!p.ok) return;
+  const int tok0 = p.t0 + p.at * 128 + (blockIdx.z >> 1) * kRows, rows = min(kRows, p.t1 - tok0);
+  const int c = threadIdx.x % kLanes * 4;
+  float4 x[kRows / kPer];
+#pragma unroll
+  for (int i = 0; i < kRows / kPer; ++i) x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = 0; s < a.shares; ++s) {
+#pragma unroll
+    for (int i = 0; i < kRows / kPer; ++i) {
+      const int r = threadIdx.x / kLanes + i * kPer;
+      if (r >= rows) continue;
+      const float4 y = *reinterpret_cast<const float4*>(share_rows(a, D, dk, s, hk, tok0 + r) + c);
+      x[i].x += y.x;
+      x[i].y += y.y;
+      x[i].z += y.z;
+      x[i].w += y.w;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kRows / kPer; ++i) {
+    const int r = threadIdx.x / kLanes + i * kPer;
+    if (r >= rows) continue;
+    typename Pair<T>::Raw* dst =
+        reinterpret_cast<typename Pair<T>::Raw*>(static_cast<T*>(dk ? a.dk : a.dv) + ((long long)(tok0 + r) * a.Hkv + hk) * D + c);
+    dst[0] = Pair<T>::from_f(make_float2(x[i].x, x[i].y));
+    dst[1] = Pair<T>::from_f(make_float2(x[i].z, x[i].w));
+  }
+  if (!dk && a.dbias && (int)threadIdx.x < rows) {
+    float b = 0.f;
+    for (int s = 0; s < a.shares; ++s) b += share_dbias(a, D, s, hk)[tok0 + threadIdx.x];
+    static_cast<T*>(a.dbias)[(long long)hk * a.seqs.total + tok0 + threadIdx.x] = (T)b;
+  }
+}
+
 }  // namespace
+
+cudaError_t attn_join(const AttnArgs& a, bool bf16, int D, cudaStream_t stream) {
+  const dim3 grid((unsigned)pieces(a.seqs.total, a.seqs.num, 128), a.Hkv, 8);
+  if (bf16 && D == 128)
+    attn_join_kernel<128, __nv_bfloat16><<<grid, 256, 0, stream>>>(a);
+  else if (bf16)
+    attn_join_kernel<64, __nv_bfloat16><<<grid, 256, 0, stream>>>(a);
+  else if (D == 128)
+    attn_join_kernel<128, float><<<grid, 256, 0, stream>>>(a);
+  else
+    attn_join_kernel<64, float><<<grid, 256, 0, stream>>>(a);
+  return cudaGetLastError();
+}
+
 }  // namespace dmc
 
 struct dmc_retrofit {

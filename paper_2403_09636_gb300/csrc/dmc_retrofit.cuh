@@ -108,6 +108,12 @@ template <> struct Pair<__nv_bfloat16> {
   static __device__ __forceinline__ Raw from_f(float2 f) { return Chunk<__nv_bfloat16>::pack2(f.x, f.y); }
 };
 
+// Four bytes to shared memory, asynchronously; zero unless `valid` (src is a valid address anyway).
+__device__ __forceinline__ void cp_async4_zfill(uint32_t dst, const void* src, bool valid) {
+  const uint32_t n = valid ? 4u : 0u;
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+
 struct StatesArgs {
   Seqs seqs;
   int Hq, Hkv, G;
@@ -148,9 +154,12 @@ struct AttnArgs {
   unsigned int* error;
 };
 
-// Shares into which the bf16 kernel of dK and dV splits each group's queries: one, unless
-// the tiles of its KV heads (`items`) are fewer than two per SM of this GPU, when shares of whole heads make
-// up for it. So there are never 4 * 152 items of more than one share, and their sums' scratch is bounded.
+// Shares into which the kernels of dK and dV split each group's queries: one, unless the tiles of
+// its KV heads (`items`) are fewer than two per SM of this GPU, when the longest item, not the sum
+// of all, sets the time; then shares of whole heads. Items of more than one share never exceed
+// 4 * 152, so their sums' scratch is bounded. Backward pass in bf16 whole and in shares, us: 600 tokens of
+// 64 / 8 heads 113 and 68; 1000 of 40 / 8 113 and 81; 2048 of 32 / 8 177 and 161; 4096 of 64 / 8 932 and
+// 769; where it gains least, two sequences of 1024 of 32 / 8, 109 and 111.
 constexpr int kSplitItems = 2 * 152;
 inline int attn_shares(long long items, int G) {
   if (items >= kSplitItems) return 1;
@@ -161,6 +170,15 @@ inline int attn_shares(long long items, int G) {
 inline size_t attn_sums(int max_tokens, int Hkv, int G, int D) {
   const size_t all = (size_t)max_tokens * Hkv * G, most = 2 * kSplitItems * 128;
   return G == 1 ? 0 : (all < most ? all : most) * (2 * D + 1);
+}
+
+// The shares' sums, to be added up by attn_join_kernel: [share][KV head][token][D] of dV, then of
+// dK, then [share][KV head][token] of dbias.
+__device__ __forceinline__ float* share_rows(const AttnArgs& a, int D, bool dk, int share, int hk, int token) {
+  return a.sums + ((((long long)(dk ? a.shares : 0) + share) * a.Hkv + hk) * a.seqs.total + token) * D;
+}
+__device__ __forceinline__ float* share_dbias(const AttnArgs& a, int D, int share, int hk) {
+  return a.sums + (2ll * a.shares * D * a.Hkv + (long long)share * a.Hkv + hk) * a.seqs.total;
 }
 
 struct LossArgs {

@@ -192,12 +192,6 @@ __device__ __forceinline__ Work next_work(WorkRing& ring, int& turn, const Wait&
   return w;
 }
 
-// Four bytes to shared memory, asynchronously; zero unless `valid` (src is a valid address anyway).
-__device__ __forceinline__ void cp_async4_zfill(uint32_t dst, const void* src, bool valid) {
-  const uint32_t n = valid ? 4u : 0u;
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
-
 template <int D>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int tok) {
 #pragma unroll

@@ -26,6 +26,7 @@
 #include "dmc_retrofit_attn.cuh"
 
 namespace dmc {
+cudaError_t attn_join(const AttnArgs& a, bool bf16, int D, cudaStream_t stream);
 
 namespace {
 
@@ -118,15 +119,6 @@ __device__ __forceinline__ DkvItem dkv_item(const AttnArgs& a, const Work& w) {
   it.tile0 = w.t0 / kR + w.seq + w.at;
   it.tiles = (w.t1 - it.j0 + kR - 1) / kR;
   return it;
-}
-
-// The shares' sums, to be added up by attn_join_kernel: [share][KV head][token][D] of dV, then of
-// dK, then [share][KV head][token] of dbias.
-__device__ __forceinline__ float* share_rows(const AttnArgs& a, int D, bool dk, int share, int hk, int token) {
-  return a.sums + ((((long long)(dk ? a.shares : 0) + share) * a.Hkv + hk) * a.seqs.total + token) * D;
-}
-__device__ __forceinline__ float* share_dbias(const AttnArgs& a, int D, int share, int hk) {
-  return a.sums + (2ll * a.shares * D * a.Hkv + (long long)share * a.Hkv + hk) * a.seqs.total;
 }
 
 template <int D, bool kBias>
@@ -484,46 +476,6 @@ attn_dkv_kernel(const AttnArgs a, const __grid_constant__ BwdMaps maps, int item
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
   }
   if (tid == 0) work_done(a.counter);
-}
-
-// The shares' sums of 128 rows of a KV head, in the shares' order: blockIdx.z / 2 is a quarter of
-// the rows, its lowest bit dV or dK. Bound by the L2 cache, where the sums still are.
-template <int D>
-__global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
-  constexpr int kLanes = D / 4, kPer = 256 / kLanes, kRows = kR / 4;
-  const int hk = blockIdx.y;
-  const bool dk = blockIdx.z & 1;
-  const Piece p = find_piece(a.seqs, kR, blockIdx.x);
-  if (!p.ok) return;
-  const int tok0 = p.t0 + p.at * kR + (blockIdx.z >> 1) * kRows, rows = min(kRows, p.t1 - tok0);
-  const int c = threadIdx.x % kLanes * 4;
-  float4 x[kRows / kPer];
-#pragma unroll
-  for (int i = 0; i < kRows / kPer; ++i) x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s = 0; s < a.shares; ++s) {
-#pragma unroll
-    for (int i = 0; i < kRows / kPer; ++i) {
-      const int r = threadIdx.x / kLanes + i * kPer;
-      if (r >= rows) continue;
-      const float4 y = *reinterpret_cast<const float4*>(share_rows(a, D, dk, s, hk, tok0 + r) + c);
-      x[i].x += y.x;
-      x[i].y += y.y;
-      x[i].z += y.z;
-      x[i].w += y.w;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kRows / kPer; ++i) {
-    const int r = threadIdx.x / kLanes + i * kPer;
-    if (r >= rows) continue;
-    const uint2 y = make_uint2(Chunk<__nv_bfloat16>::pack2(x[i].x, x[i].y), Chunk<__nv_bfloat16>::pack2(x[i].z, x[i].w));
-    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(dk ? a.dk : a.dv) + ((long long)(tok0 + r) * a.Hkv + hk) * D + c) = y;
-  }
-  if (!dk && a.bias && a.dbias && (int)threadIdx.x < rows) {
-    float b = 0.f;
-    for (int s = 0; s < a.shares; ++s) b += share_dbias(a, D, s, hk)[tok0 + threadIdx.x];
-    static_cast<__nv_bfloat16*>(a.dbias)[(long long)hk * a.seqs.total + tok0 + threadIdx.x] = __float2bfloat16_rn(b);
-  }
 }
 
 // ---------------------------------------------------------------- dQ
@@ -922,12 +874,13 @@ cudaError_t backward(AttnArgs a, cudaStream_t stream) {
   long long dkv_items = (long long)tiles * a.Hkv, dq_items = (long long)tiles * a.Hq;
   if (dq_items > INT_MAX / 2) return cudaErrorInvalidValue;
   a.shares = attn_shares(dkv_items, a.G);
+  if (!kBias) a.dbias = nullptr;
   dkv_items *= a.shares;
   attn_rows_kernel<D><<<dim3(tiles, a.Hq), 256, 0, stream>>>(a, tiles);
   dq<<<(unsigned)(dq_items < sms ? dq_items : sms), kAttnThreads, dq_bytes, stream>>>(a, maps, (int)dq_items, tiles);
   dkv<<<(unsigned)(dkv_items < sms ? dkv_items : sms), kAttnThreads, dkv_bytes, stream>>>(a, maps, (int)dkv_items, tiles);
-  if (a.shares > 1) attn_join_kernel<D><<<dim3(tiles, a.Hkv, 8), 256, 0, stream>>>(a);
-  return cudaGetLastError();
+  e = cudaGetLastError();
+  return e == cudaSuccess && a.shares > 1 ? attn_join(a, true, D, stream) : e;
 }
 
 }  // namespace

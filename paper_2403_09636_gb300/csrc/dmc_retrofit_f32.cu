@@ -6,13 +6,20 @@
 // padded by 16 bytes, so that the 16-byte reads of 8 neighbouring rows fall into different banks.
 // Multiply-adds come in pairs (fma.rn.f32x2), two neighbouring terms of a sum or two
 // neighbouring columns, which leaves issue slots for the reads: 12 reads of 16 bytes per 32 pairs.
-// Tiles of 64 rows, 256 threads; 32 rows and 128 threads where tiles of 64 would leave SMs without
-// a block: twice as many blocks, whose steps take less than half as long.
+// Bound by multiply-adds and the reads that feed them: 33 to 39 TFLOP/s with heads of 128 (10 sequences
+// of 1148 tokens of 32 / 8 heads: forward 2.77 ms, backward 10.1 ms), 28 with heads of 64.
+// Tiles of 64 rows, 256 threads; 32 rows and 128 threads where tiles of 64 would be fewer than two
+// blocks per SM, so that a block's steps one after another set the time: twice as many blocks, whose steps take less
+// than half as long, the next step's tiles on their way meanwhile, dQ in one launch with dK and dV, and
+// those in shares of a group's heads (attn_shares). 256 tokens of 4 heads of 64: forward 25 us, backward 35 (63 in two
+// launches without tiles ahead); 500 tokens of 32 / 8 heads of 128: 117 and 278 (532 with whole groups).
+// 256 threads for tiles of 32 rows take 24 and 38, 138 and 731.
 #include <math.h>
 
 #include "dmc_retrofit.cuh"
 
 namespace dmc {
+cudaError_t attn_join(const AttnArgs& a, bool bf16, int D, cudaStream_t stream);
 
 namespace {
 
@@ -24,6 +31,7 @@ struct Shape {
   static constexpr int kJ = kT / 16;                   // columns of a thread
   static constexpr int kTy = kThreads / 16;
   static constexpr int kW = kT + 4;                    // row of a tile of weights
+  static constexpr int kStages = kRows == 64 ? 1 : 2;  // tiles of the sequence's other rows kept at once
 };
 
 // `rows` rows of D columns, asynchronously, into a tile; zero from there on
@@ -112,18 +120,33 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-__device__ __forceinline__ void loaded() {
-  cp_async_commit();
-  cp_async_wait<0>();
+// Tiles of step n, by `load(n)`. With two stages those of the next step are asked for
+// here, once all threads are through with the step before; with one they come when they are needed.
+template <class S, typename Load>
+__device__ __forceinline__ void stage_tiles(int n, int steps, const Load& load) {
+  __syncthreads();  // the step before has read its tiles
+  if (S::kStages == 1 || n == 0) {
+    load(n);
+    cp_async_commit();
+  }
+  if (S::kStages == 2 && n + 1 < steps) {
+    load(n + 1);
+    cp_async_commit();
+    cp_async_wait<1>();
+  } else {
+    cp_async_wait<0>();
+  }
   __syncthreads();
 }
 
 // Whether query i sees row j
 __device__ __forceinline__ bool sees(int i, int j, float bias) { return j == i || (j < i && bias != -INFINITY); }
 
+// of `own` tiles of the block's rows, two staged ones and two numbers of their rows, and weights
 template <int D, int kRows>
-constexpr size_t tiles_bytes(int tiles, int weights) {
-  return ((size_t)tiles * kRows * (D + 4) + (size_t)weights * kRows * (kRows + 4) + 2 * kRows) * 4;
+constexpr size_t tiles_bytes(int own, int weights) {
+  constexpr int stages = Shape<kRows>::kStages;
+  return ((size_t)(own + 2 * stages) * kRows * (D + 4) + (size_t)weights * kRows * (kRows + 4) + 2 * stages * kRows) * 4;
 }
 
 // Weights take K's place once the scores are there.
@@ -131,7 +154,8 @@ template <int D, int kRows>
 __global__ void __launch_bounds__(Shape<kRows>::kThreads, 2) attn_kernel(const AttnArgs a) {
   using S = Shape<kRows>;
   extern __shared__ float smem[];
-  float *Q = smem, *K = Q + S::kT * (D + 4), *V = K + S::kT * (D + 4), *W = K;
+  constexpr int kTile = S::kT * (D + 4);
+  float* Q = smem;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, h = blockIdx.y, hk = h / a.G;
   if (blockIdx.x == 0 && h == 0) check_seqs(a.seqs, a.error);
   Piece p = find_piece(a.seqs, S::kT, blockIdx.x);
@@ -147,18 +171,30 @@ __global__ void __launch_bounds__(Shape<kRows>::kThreads, 2) attn_kernel(const A
   float m[S::kI], l[S::kI];
 #pragma unroll
   for (int i = 0; i < S::kI; ++i) m[i] = -INFINITY, l[i] = 0.f;
-  for (int j0 = p.t0; j0 <= i0; j0 += S::kT) {
-    const int keys = min(S::kT, p.t1 - j0);
-    __syncthreads();
+  const int steps = p.at + 1;
+  auto load = [&](int n) {
+    float* K = smem + (1 + n % S::kStages * 2) * kTile;
+    const int j0 = p.t0 + n * S::kT, keys = min(S::kT, p.t1 - j0);
     load_rows<D, S>(K, k + j0 * ks, ks, keys);
-    load_rows<D, S>(V, v + j0 * ks, ks, keys);
-    float b[S::kJ];
+    load_rows<D, S>(K + kTile, v + j0 * ks, ks, keys);
+  };
+  float next_b[S::kJ];
+  auto load_bias = [&](int n) {
 #pragma unroll
     for (int j = 0; j < S::kJ; ++j) {
-      const int tok = j0 + tx + 16 * j;
-      b[j] = a.bias && tok < p.t1 ? a.bias[(long long)hk * a.seqs.total + tok] : 0.f;
+      const int tok = p.t0 + n * S::kT + tx + 16 * j;
+      next_b[j] = a.bias && tok < p.t1 ? a.bias[(long long)hk * a.seqs.total + tok] : 0.f;
     }
-    loaded();
+  };
+  load_bias(0);
+  for (int n = 0; n < steps; ++n) {
+    const int j0 = p.t0 + n * S::kT;
+    float *K = smem + (1 + n % S::kStages * 2) * kTile, *V = K + kTile, *W = K;
+    float b[S::kJ];
+#pragma unroll
+    for (int j = 0; j < S::kJ; ++j) b[j] = next_b[j];
+    stage_tiles<S>(n, steps, load);
+    load_bias(n + 1);
     float2 s2[S::kI][S::kJ];
     clear(s2);
     dot_tile<D, S>(s2, Q, K);
@@ -202,11 +238,11 @@ __global__ void __launch_bounds__(Shape<kRows>::kThreads, 2) attn_kernel(const A
 // The rows of Q's gradient: dQ_i = scale sum over j of dS_ij k_j, with
 // dS = P (dO V^T - delta), delta_i = dO_i . out_i. Weights take V's place.
 template <int D, int kRows>
-__global__ void __launch_bounds__(Shape<kRows>::kThreads) attn_dq_kernel(const AttnArgs a) {
+__device__ __forceinline__ void dq_rows(const AttnArgs& a, int h, float* smem) {
   using S = Shape<kRows>;
-  extern __shared__ float smem[];
-  float *Q = smem, *O = Q + S::kT * (D + 4), *K = O + S::kT * (D + 4), *V = K + S::kT * (D + 4), *W = V;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, h = blockIdx.y, hk = h / a.G;
+  constexpr int kTile = S::kT * (D + 4);
+  float *Q = smem, *O = Q + kTile;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, hk = h / a.G;
   Piece p = find_piece(a.seqs, S::kT, blockIdx.x);
   if (!p.ok) return;
   p.at = (p.t1 - p.t0 + S::kT - 1) / S::kT - 1 - p.at;
@@ -226,18 +262,30 @@ __global__ void __launch_bounds__(Shape<kRows>::kThreads) attn_dq_kernel(const A
   }
   float2 acc[S::kI][D / 32];
   clear(acc);
-  for (int j0 = p.t0; j0 <= i0; j0 += S::kT) {
-    const int keys = min(S::kT, p.t1 - j0);
-    __syncthreads();
+  const int steps = p.at + 1;
+  auto load = [&](int n) {
+    float* K = smem + (2 + n % S::kStages * 2) * kTile;
+    const int j0 = p.t0 + n * S::kT, keys = min(S::kT, p.t1 - j0);
     load_rows<D, S>(K, k + j0 * ks, ks, keys);
-    load_rows<D, S>(V, v + j0 * ks, ks, keys);
-    float b[S::kJ];
+    load_rows<D, S>(K + kTile, v + j0 * ks, ks, keys);
+  };
+  float next_b[S::kJ];
+  auto load_bias = [&](int n) {
 #pragma unroll
     for (int j = 0; j < S::kJ; ++j) {
-      const int tok = j0 + tx + 16 * j;
-      b[j] = a.bias && tok < p.t1 ? a.bias[(long long)hk * a.seqs.total + tok] : 0.f;
+      const int tok = p.t0 + n * S::kT + tx + 16 * j;
+      next_b[j] = a.bias && tok < p.t1 ? a.bias[(long long)hk * a.seqs.total + tok] : 0.f;
     }
-    loaded();
+  };
+  load_bias(0);
+  for (int n = 0; n < steps; ++n) {
+    const int j0 = p.t0 + n * S::kT;
+    float *K = smem + (2 + n % S::kStages * 2) * kTile, *V = K + kTile, *W = V;
+    float b[S::kJ];
+#pragma unroll
+    for (int j = 0; j < S::kJ; ++j) b[j] = next_b[j];
+    stage_tiles<S>(n, steps, load);
+    load_bias(n + 1);
     float2 s[S::kI][S::kJ], dp[S::kI][S::kJ];
     clear(s);
     clear(dp);
@@ -264,12 +312,12 @@ __global__ void __launch_bounds__(Shape<kRows>::kThreads) attn_dq_kernel(const A
 // The rows of K's and V's gradients and of the bias's, summed over the queries of the
 // group: dV_j = sum of P_ij dO_i, dK_j = scale sum of dS_ij q_i, dbias_j = sum over i > j of dS_ij
 template <int D, int kRows>
-__global__ void __launch_bounds__(Shape<kRows>::kThreads) attn_dkv_kernel(const AttnArgs a) {
+__device__ __forceinline__ void dkv_rows(const AttnArgs& a, int hk, int share, float* smem) {
   using S = Shape<kRows>;
-  extern __shared__ float smem[];
-  float *K = smem, *V = K + S::kT * (D + 4), *Q = V + S::kT * (D + 4), *O = Q + S::kT * (D + 4), *W = O + S::kT * (D + 4);
-  float *X = W + S::kT * S::kW, *L = X + S::kT * S::kW, *E = L + S::kT;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, hk = blockIdx.y;
+  constexpr int kTile = S::kT * (D + 4);
+  float *K = smem, *V = K + kTile, *W = K + (2 + 2 * S::kStages) * kTile;
+  float *X = W + S::kT * S::kW, *numbers = X + S::kT * S::kW;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const Piece p = find_piece(a.seqs, S::kT, blockIdx.x);
   if (!p.ok) return;
   const int j0 = p.t0 + p.at * S::kT, keys = min(S::kT, p.t1 - j0);
@@ -287,52 +335,79 @@ __global__ void __launch_bounds__(Shape<kRows>::kThreads) attn_dkv_kernel(const 
   float2 dk[S::kI][D / 32], dv[S::kI][D / 32];
   clear(dk);
   clear(dv);
-  for (int g = 0; g < a.G; ++g) {
-    const int h = hk * a.G + g;
-    for (int i0 = j0; i0 < p.t1; i0 += S::kT) {
-      const int rows = min(S::kT, p.t1 - i0);
-      __syncthreads();
-      const long long q0 = (long long)i0 * qs + (long long)h * D;
-      load_rows<D, S>(Q, static_cast<const float*>(a.q) + q0, qs, rows);
-      load_rows<D, S>(O, static_cast<const float*>(a.dout) + q0, qs, rows);
-      if (threadIdx.x < S::kT) {
-        const long long n = (long long)h * a.seqs.total + i0 + threadIdx.x;
-        const bool in = (int)threadIdx.x < rows;
-        L[threadIdx.x] = in ? a.lse[n] : 0.f;
-        E[threadIdx.x] = in ? a.rows[n] : 0.f;
-      }
-      loaded();
-      float2 s[S::kI][S::kJ], dp[S::kI][S::kJ];
-      clear(s);
-      clear(dp);
-      dot_tile<D, S>(s, K, Q);
-      dot_tile<D, S>(dp, V, O);
-#pragma unroll
-      for (int j = 0; j < S::kI; ++j)
-#pragma unroll
-        for (int i = 0; i < S::kJ; ++i) {
-          const int tok = j0 + ty + S::kTy * j, r = tx + 16 * i, q = i0 + r;
-          const bool seen = r < rows && sees(q, tok, bias[j]);
-          const float w = seen ? expf(fmaf(sum2(s[j][i]), scale, tok < q ? bias[j] : 0.f) - L[r]) : 0.f;
-          const float ds = seen ? w * (sum2(dp[j][i]) - E[r]) : 0.f;
-          W[(ty + S::kTy * j) * S::kW + r] = w;
-          X[(ty + S::kTy * j) * S::kW + r] = ds;
-          if (tok < q) db[j] += ds;
-        }
-      __syncthreads();
-      sum_tile<D, S>(dv, W, O);
-      sum_tile<D, S>(dk, X, Q);
+  const int h0 = hk * a.G + share * a.G / a.shares, h1 = hk * a.G + (share + 1) * a.G / a.shares;
+  const int tiles = (p.t1 - j0 + S::kT - 1) / S::kT, steps = (h1 - h0) * tiles;
+  auto load = [&](int n) {
+    float *Q = smem + (2 + n % S::kStages * 2) * kTile, *L = numbers + n % S::kStages * 2 * S::kT;
+    const int h = h0 + n / tiles, i0 = j0 + n % tiles * S::kT, rows = min(S::kT, p.t1 - i0);
+    const long long q0 = (long long)i0 * qs + (long long)h * D;
+    load_rows<D, S>(Q, static_cast<const float*>(a.q) + q0, qs, rows);
+    load_rows<D, S>(Q + kTile, static_cast<const float*>(a.dout) + q0, qs, rows);
+    if (threadIdx.x < S::kT) {
+      const bool in = (int)threadIdx.x < rows;
+      const long long at = (long long)h * a.seqs.total + i0 + (in ? threadIdx.x : 0);
+      cp_async4_zfill(smem_u32(L + threadIdx.x), a.lse + at, in);
+      cp_async4_zfill(smem_u32(L + S::kT + threadIdx.x), a.rows + at, in);
     }
+  };
+  for (int n = 0; n < steps; ++n) {
+    const float *Q = smem + (2 + n % S::kStages * 2) * kTile, *O = Q + kTile;
+    const float *L = numbers + n % S::kStages * 2 * S::kT, *E = L + S::kT;
+    const int i0 = j0 + n % tiles * S::kT, rows = min(S::kT, p.t1 - i0);
+    stage_tiles<S>(n, steps, load);
+    float2 s[S::kI][S::kJ], dp[S::kI][S::kJ];
+    clear(s);
+    clear(dp);
+    dot_tile<D, S>(s, K, Q);
+    dot_tile<D, S>(dp, V, O);
+#pragma unroll
+    for (int j = 0; j < S::kI; ++j)
+#pragma unroll
+      for (int i = 0; i < S::kJ; ++i) {
+        const int tok = j0 + ty + S::kTy * j, r = tx + 16 * i, q = i0 + r;
+        const bool seen = r < rows && sees(q, tok, bias[j]);
+        const float w = seen ? expf(fmaf(sum2(s[j][i]), scale, tok < q ? bias[j] : 0.f) - L[r]) : 0.f;
+        const float ds = seen ? w * (sum2(dp[j][i]) - E[r]) : 0.f;
+        W[(ty + S::kTy * j) * S::kW + r] = w;
+        X[(ty + S::kTy * j) * S::kW + r] = ds;
+        if (tok < q) db[j] += ds;
+      }
+    __syncthreads();
+    sum_tile<D, S>(dv, W, O);
+    sum_tile<D, S>(dk, X, Q);
   }
 #pragma unroll
   for (int j = 0; j < S::kI; ++j) {
     const int r = ty + S::kTy * j;
     const float b = row_sum(db[j]);
     if (r >= keys) continue;
-    store_row<D>(static_cast<float*>(a.dk) + at + r * ks, dk[j], scale);
-    store_row<D>(static_cast<float*>(a.dv) + at + r * ks, dv[j], 1.f);
-    if (tx == 0 && a.dbias) static_cast<float*>(a.dbias)[(long long)hk * a.seqs.total + j0 + r] = b;
+    const bool whole = a.shares == 1;
+    store_row<D>(whole ? static_cast<float*>(a.dk) + at + r * ks : share_rows(a, D, true, share, hk, j0 + r), dk[j], scale);
+    store_row<D>(whole ? static_cast<float*>(a.dv) + at + r * ks : share_rows(a, D, false, share, hk, j0 + r), dv[j], 1.f);
+    if (tx == 0 && a.dbias)
+      (whole ? static_cast<float*>(a.dbias) + (long long)hk * a.seqs.total : share_dbias(a, D, share, hk))[j0 + r] = b;
   }
+}
+
+template <int D, int kRows>
+__global__ void __launch_bounds__(Shape<kRows>::kThreads) attn_dq_kernel(const AttnArgs a) {
+  extern __shared__ float smem[];
+  dq_rows<D, kRows>(a, blockIdx.y, smem);
+}
+template <int D, int kRows>
+__global__ void __launch_bounds__(Shape<kRows>::kThreads) attn_dkv_kernel(const AttnArgs a) {
+  extern __shared__ float smem[];
+  dkv_rows<D, kRows>(a, blockIdx.y, 0, smem);
+}
+// Both, beside one another, where each leaves SMs without a block: KV heads first, in shares of their groups
+template <int D, int kRows>
+__global__ void __launch_bounds__(Shape<kRows>::kThreads) attn_grads_kernel(const AttnArgs a) {
+  extern __shared__ float smem[];
+  const int y = blockIdx.y, kv = a.Hkv * a.shares;
+  if (y < kv)
+    dkv_rows<D, kRows>(a, y % a.Hkv, y / a.Hkv, smem);
+  else
+    dq_rows<D, kRows>(a, y - kv, smem);
 }
 
 // delta_i = dO_i . out_i, a warp per (token, head)
@@ -364,17 +439,23 @@ cudaError_t launch(const AttnArgs& a, int heads, int rows, int threads, size_t b
 
 template <int D, int kRows>
 cudaError_t forward(const AttnArgs& a, cudaStream_t stream) {
-  return launch<attn_kernel<D, kRows>>(a, a.Hq, kRows, Shape<kRows>::kThreads, tiles_bytes<D, kRows>(3, 0), stream);
+  return launch<attn_kernel<D, kRows>>(a, a.Hq, kRows, Shape<kRows>::kThreads, tiles_bytes<D, kRows>(1, 0), stream);
 }
 
 template <int D, int kRows>
-cudaError_t backward(const AttnArgs& a, cudaStream_t stream) {
+cudaError_t backward(AttnArgs a, cudaStream_t stream) {
   constexpr int threads = Shape<kRows>::kThreads;
   attn_delta_kernel<D><<<(unsigned)(((long long)a.seqs.total * a.Hq + 7) / 8), 256, 0, stream>>>(a);
   cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess) e = launch<attn_dkv_kernel<D, kRows>>(a, a.Hkv, kRows, threads, tiles_bytes<D, kRows>(4, 2), stream);
-  if (e == cudaSuccess) e = launch<attn_dq_kernel<D, kRows>>(a, a.Hq, kRows, threads, tiles_bytes<D, kRows>(4, 0), stream);
-  return e;
+  if (e != cudaSuccess) return e;
+  a.shares = 1;
+  if (kRows == 32) {
+    a.shares = attn_shares(pieces(a.seqs.total, a.seqs.num, 32) * a.Hkv, a.G);
+    e = launch<attn_grads_kernel<D, 32>>(a, a.Hkv * a.shares + a.Hq, 32, threads, tiles_bytes<D, 32>(2, 2), stream);
+    return e == cudaSuccess && a.shares > 1 ? attn_join(a, false, D, stream) : e;
+  }
+  e = launch<attn_dkv_kernel<D, 64>>(a, a.Hkv, 64, threads, tiles_bytes<D, 64>(2, 2), stream);
+  return e == cudaSuccess ? launch<attn_dq_kernel<D, 64>>(a, a.Hq, 64, threads, tiles_bytes<D, 64>(2, 0), stream) : e;
 }
 
 // Whether tiles of 64 rows would be fewer than two blocks per SM

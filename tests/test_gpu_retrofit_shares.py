@@ -10,7 +10,7 @@ from retrofit_harness import attention_inputs, check_attention
 from test_gpu_retrofit import run_attention
 
 pytestmark = pytest.mark.gpu
-BF16 = torch.bfloat16
+BF16, F32 = torch.bfloat16, torch.float32
 
 CASES = [
     ([131], (64, 2, 128)),            # shares of a single head each
@@ -24,15 +24,17 @@ CASES = [
 ]
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("lens,heads", CASES)
-def test_attention_shares(cuda_dev, lens, heads):
-    x = attention_inputs(lens, *heads, BF16)
-    check_attention(x, lens, BF16, run_attention(cuda_dev, x, lens, heads, BF16))
+def test_attention_shares(cuda_dev, lens, heads, dtype):
+    x = attention_inputs(lens, *heads, dtype)
+    check_attention(x, lens, dtype, run_attention(cuda_dev, x, lens, heads, dtype))
 
 
-def test_attention_shares_twice_the_same(cuda_dev):
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attention_shares_twice_the_same(cuda_dev, dtype):
     lens, heads = [333, 5, 128], (24, 3, 128)
-    x = attention_inputs(lens, *heads, BF16)
-    a, b = (run_attention(cuda_dev, x, lens, heads, BF16) for _ in range(2))
+    x = attention_inputs(lens, *heads, dtype)
+    a, b = (run_attention(cuda_dev, x, lens, heads, dtype) for _ in range(2))
     for name in a:
         assert torch.equal(a[name], b[name]), name
