@@ -59,7 +59,7 @@ int loss_piece(const dmc_retrofit_config* c) {
 }
 
 struct Offsets {
-  size_t error, sums, carry, cleared, rows, shares, part_m, part_l, target_logit, dh, grad, hidden_parts, weight_parts, total;
+  size_t error, sums, carry, cleared, rows, shares, loss_sums, part_m, part_l, target_logit, dh, grad, hidden_parts, weight_parts, total;
   int piece;
 };
 
@@ -91,6 +91,7 @@ Offsets offsets(const dmc_retrofit_config* c) {
     o.part_l = at; at = align_up(at + tokens * shares * 4);
     o.target_logit = at; at = align_up(at + tokens * 4);
     o.dh = at; at = align_up(at + (!parts && o.piece < c->vocab ? tokens * c->hidden * 4 : 0));
+    o.loss_sums = at; at = align_up(at + kSumTiles * kLossTile * kLossTile * 4);
     o.grad = at; at = align_up(at + tokens * o.piece * 2 * (parts ? parts : 1));
     o.hidden_parts = at; at = align_up(at + parts * tokens * row);
     o.weight_parts = at; at = align_up(at + parts * o.piece * row);
@@ -253,6 +254,7 @@ dmc::LossArgs loss_args(dmc_retrofit_t h, int32_t n, const void* hidden, const v
   a.hidden_parts = h->base + h->at.hidden_parts;
   a.weight_parts = h->base + h->at.weight_parts;
   a.dh = reinterpret_cast<float*>(h->base + h->at.dh);
+  a.sums = reinterpret_cast<float*>(h->base + h->at.loss_sums);
   a.part_m = reinterpret_cast<float*>(h->base + h->at.part_m);
   a.part_l = reinterpret_cast<float*>(h->base + h->at.part_l);
   a.target_logit = reinterpret_cast<float*>(h->base + h->at.target_logit);

@@ -193,6 +193,7 @@ struct LossArgs {
   void* grad;           // [N][piece] in bf16 (fp32: three parts): gradient of a piece's logits
   void *hidden_parts, *weight_parts;  // fp32: [3][N][stride], [3][piece][stride]
   float* dh;            // bf16: [N][H]: dhidden of the pieces so far
+  float* sums;          // shares of a gradient's sums: [share][rows][H]
   float *part_m, *part_l;  // [shares][N]: maximum and sum of half a tile of the vocabulary
   float* target_logit;  // [N]
   unsigned int* error;
@@ -200,6 +201,8 @@ struct LossArgs {
 
 // Words of the largest tile of the vocabulary; a token's maximum and sum are kept for each half of one
 constexpr int kLossTile = 256;
+// Tiles of 256 x 256 of shares of a gradient's sums: one per pair of SMs of this GPU
+constexpr long long kSumTiles = 152 / 2;
 // Row length of an fp32 matrix's bf16 parts: rows of multiples of 16 bytes
 inline int loss_stride(int H) { return (H + 7) / 8 * 8; }
 

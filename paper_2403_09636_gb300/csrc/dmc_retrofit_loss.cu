@@ -64,6 +64,7 @@ struct ProductArgs {
   int group;              // row tiles of a group
   int v0;                 // first word of the piece
   bool first, last;       // of the pieces
+  int shares;             // of a gradient's sums, see sum_shares
   CUtensorMap ma, mb;
 };
 
@@ -133,9 +134,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
 loss_product_kernel(const __grid_constant__ ProductArgs p) {
   constexpr int kHalfN = kN / 2;          // columns of a row thread
   constexpr int kHalfB = kHalf * kN / 256;  // bytes of a CTA's half of B's tile
+  constexpr bool kOften = kF32 || kEnd == End::kStats;  // sums leave tensor memory every few steps, see above
   // operands whose rows run along the sums' terms are MN-major
-  // sums leave tensor memory every few steps, see above
-  constexpr bool kOften = kF32 || kEnd == End::kStats;
   constexpr bool kAmn = kEnd == End::kWeight, kBmn = kEnd == End::kHidden || kEnd == End::kWeight;
   extern __shared__ unsigned char smem_raw[];
   ProductShared& sh = *reinterpret_cast<ProductShared*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
@@ -145,11 +145,16 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
   const uint32_t rank = cluster_rank();
   const int clusters = gridDim.x / 2, cluster = blockIdx.x / 2;
   const int tiles = ((p.rows + kM - 1) / kM) * ((p.cols + kN - 1) / kN);
-  const int steps = (p.depth + kK - 1) / kK;
-  const int all = steps * p.passes;  // steps of a tile
-  // one past the last step that goes into the accumulator begun at step k (of fp32's passes the
-  // last one alone has large terms)
-  auto chunk_end = [&](int k) -> int {
+  constexpr bool kShares = kEnd == End::kHidden || kEnd == End::kWeight;
+  const int shares = kShares ? p.shares : 1, units = tiles * shares;  // work: a share of a tile's sums
+  const int depth = (p.depth + kK - 1) / kK;                          // steps of a pass
+  // the steps of a pass that are unit u's
+  auto first_step = [&](int u) -> int { return kShares ? (int)((long long)depth * (u / tiles) / shares) : 0; };
+  auto last_step = [&](int u) -> int { return kShares ? (int)((long long)depth * (u / tiles + 1) / shares) : depth; };
+  // one past the last step that goes into the accumulator begun at step k of a unit's steps (of fp32's
+  // passes the last one alone has large terms)
+  auto chunk_end = [&](int steps, int k) -> int {
+    const int all = steps * p.passes;
     if (kF32) return k < 5 * steps ? 5 * steps : min(all, k + 4);
     return kOften ? min(all, k + 16) : all;
   };
@@ -182,12 +187,13 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
     // ---------------------------------------------------------------- loads
     uint32_t n = 0;
     bool ok = true;
-    for (int u = cluster; u < tiles && ok; u += clusters) {
-      const Tile t = tile_of<kN>(p, u);
+    for (int u = cluster; u < units && ok; u += clusters) {
+      const Tile t = tile_of<kN>(p, kShares ? u % tiles : u);
       const int m = t.m + (int)rank * 128, c = t.n + (int)rank * kHalfN;  // this CTA's half
-      int k = 0, pass = 0, pa = part_a(p.passes, 0), pb = part_b(p.passes, 0);
+      const int begin = first_step(u), end = last_step(u);
+      int k = begin, pass = 0, pa = part_a(p.passes, 0), pb = part_b(p.passes, 0);
 #pragma unroll 1
-      for (int x = 0; x < steps * p.passes; ++x, ++n) {
+      for (int x = 0; x < (end - begin) * p.passes; ++x, ++n) {
         const int s = n % kStages;
         ok = wait(&sh.empty[s], ((n / kStages) & 1) ^ 1);
         if (!ok) break;
@@ -209,8 +215,8 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
           }
         }
         __syncwarp();
-        if (++k == steps) {
-          k = 0;
+        if (++k == end) {
+          k = begin;
           ++pass;
           pa = part_a(p.passes, pass);
           pb = part_b(p.passes, pass);
@@ -230,11 +236,12 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
       const uint64_t db = tc_desc(smem_u32(sh.b[0]), kBmn ? kHalfB / 2 : 16, 1024);
       uint32_t n = 0, sums = 0;  // steps, accumulators begun
       bool ok = true;
-      for (int u = cluster; u < tiles && ok; u += clusters) {
+      for (int u = cluster; u < units && ok; u += clusters) {
+        const int steps = last_step(u) - first_step(u);
 #pragma unroll 1
-        for (int k0 = 0, end; k0 < all && ok; k0 = end, ++sums) {
+        for (int k0 = 0, end; k0 < steps * p.passes && ok; k0 = end, ++sums) {
           const uint32_t acc = sums & 1;
-          end = chunk_end(k0);
+          end = chunk_end(steps, k0);
           ok = wait(&sh.taken[acc], ((sums >> 1) & 1) ^ 1);
           if (!ok) break;
           tc_fence_after();
@@ -266,8 +273,8 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
     const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * kHalfN;
     uint32_t sums = 0;
     bool ok = true;
-    for (int u = cluster; u < tiles && ok; u += clusters) {
-      const Tile t = tile_of<kN>(p, u);
+    for (int u = cluster; u < units && ok; u += clusters) {
+      const Tile t = tile_of<kN>(p, kShares ? u % tiles : u);
       const int row = t.m + (int)rank * 128 + (warp & 3) * 32 + lane, col = t.n + half * kHalfN;
       const bool in = row < p.rows;
       // what the row needs beside C is on its way while the product runs
@@ -313,6 +320,13 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
           }
         }
         if (kEnd == End::kHidden || kEnd == End::kWeight) {
+          if (shares > 1) {
+            float* sum = a.sums + ((long long)(u / tiles) * p.rows + row) * a.H + col + c;
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+              if (c + i < left) *reinterpret_cast<float4*>(sum + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+            return;
+          }
           const long long at = (long long)(kEnd == End::kWeight ? p.v0 + row : row) * a.H + col + c;
           // in fp32 the pieces are added up where the result goes
           float* sum = kF32 ? static_cast<float*>(kEnd == End::kWeight ? a.dweight : a.dhidden) : a.dh;
@@ -358,58 +372,59 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
         release(acc);
         ++sums;
       } else {
-      float f[kHalfN];
+        const int steps = last_step(u) - first_step(u);
+        float f[kHalfN];
 #pragma unroll 1
-      for (int k0 = 0; k0 < all; k0 = chunk_end(k0), ++sums) {
-        const uint32_t acc = sums & 1;
-        if (!(ok = wait(&sh.done[acc], (sums >> 1) & 1))) break;
-        tc_fence_after();
-        if (k0 == 0) {
+        for (int k0 = 0; k0 < steps * p.passes; k0 = chunk_end(steps, k0), ++sums) {
+          const uint32_t acc = sums & 1;
+          if (!(ok = wait(&sh.done[acc], (sums >> 1) & 1))) break;
+          tc_fence_after();
+          if (k0 == 0) {
 #pragma unroll
-          for (int c = 0; c < kHalfN; c += 32) tc_ld32(t_row + acc * kN + c, f + c);
-          tc_wait_ld();
+            for (int c = 0; c < kHalfN; c += 32) tc_ld32(t_row + acc * kN + c, f + c);
+            tc_wait_ld();
+          } else {
+#pragma unroll
+            for (int c = 0; c < kHalfN; c += 16) {
+              float g[16];
+              tc_ld16(t_row + acc * kN + c, g);
+              tc_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) f[c + i] += g[i];
+            }
+          }
+          release(acc);
+        }
+        if (!ok) break;
+        if (kEnd == End::kStats) {
+          const bool mine = target >= word0 && target < word0 + kHalfN;
+          float hit = 0.f;
+          if (__any_sync(0xffffffffu, mine)) {
+#pragma unroll
+            for (int i = 0; i < kHalfN; ++i)
+              if (target == word0 + i) hit = f[i];
+          }
+          if (left < kHalfN) {
+#pragma unroll
+            for (int i = 0; i < kHalfN; ++i) f[i] = i < left ? f[i] : -INFINITY;
+          }
+          float m4[4] = {f[0], f[1], f[2], f[3]};
+#pragma unroll
+          for (int i = 4; i < kHalfN; ++i) m4[i & 3] = fmaxf(m4[i & 3], f[i]);
+          const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+          const float ref = m == -INFINITY ? 0.f : m;
+          float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < kHalfN; ++i) s4[i & 3] += ex2f((f[i] - ref) * kLog2e);
+          if (in && left > 0) {
+            a.part_m[(long long)(word0 / kHalfN) * a.N + row] = m;
+            a.part_l[(long long)(word0 / kHalfN) * a.N + row] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+            if (mine && target < p.v0 + p.cols) a.target_logit[row] = hit;
+          }
         } else {
 #pragma unroll
-          for (int c = 0; c < kHalfN; c += 16) {
-            float g[16];
-            tc_ld16(t_row + acc * kN + c, g);
-            tc_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) f[c + i] += g[i];
-          }
+          for (int c = 0; c < kHalfN; c += 16) finish(c, f + c);
         }
-        release(acc);
-      }
-      if (!ok) break;
-      if (kEnd == End::kStats) {
-        const bool mine = target >= word0 && target < word0 + kHalfN;
-        float hit = 0.f;
-        if (__any_sync(0xffffffffu, mine)) {
-#pragma unroll
-          for (int i = 0; i < kHalfN; ++i)
-            if (target == word0 + i) hit = f[i];
-        }
-        if (left < kHalfN) {
-#pragma unroll
-          for (int i = 0; i < kHalfN; ++i) f[i] = i < left ? f[i] : -INFINITY;
-        }
-        float m4[4] = {f[0], f[1], f[2], f[3]};
-#pragma unroll
-        for (int i = 4; i < kHalfN; ++i) m4[i & 3] = fmaxf(m4[i & 3], f[i]);
-        const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-        const float ref = m == -INFINITY ? 0.f : m;
-        float s4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < kHalfN; ++i) s4[i & 3] += ex2f((f[i] - ref) * kLog2e);
-        if (in && left > 0) {
-          a.part_m[(long long)(word0 / kHalfN) * a.N + row] = m;
-          a.part_l[(long long)(word0 / kHalfN) * a.N + row] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
-          if (mine && target < p.v0 + p.cols) a.target_logit[row] = hit;
-        }
-      } else {
-#pragma unroll
-        for (int c = 0; c < kHalfN; c += 16) finish(c, f + c);
-      }
       }
     }
   }
@@ -423,14 +438,22 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
 }
 
 // x in fp32, rows of H, as three bf16 numbers that add up to it: parts[3][rows][stride], four
-// elements per thread. Bound by HBM.
-__global__ void __launch_bounds__(256) loss_parts_kernel(const float* x, long long rows, int H, int stride, char* parts) {
+// elements per thread, of one matrix or of two. Bound by HBM.
+struct ToParts {
+  const float* x;
+  long long rows;
+  char* parts;
+};
+__global__ void __launch_bounds__(256) loss_parts_kernel(const ToParts first, const ToParts second, int H, int stride) {
   const int per = H / 4;
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= rows * per) return;
+  long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  const bool one = i < first.rows * per;
+  if (!one) i -= first.rows * per;
+  const ToParts& m = one ? first : second;
+  if (i >= m.rows * per) return;
   const long long r = i / per;
   const int c = (int)(i % per) * 4;
-  const float4 v = *reinterpret_cast<const float4*>(x + r * H + c);
+  const float4 v = *reinterpret_cast<const float4*>(m.x + r * H + c);
   float f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
   for (int part = 0; part < 3; ++part) {
@@ -443,14 +466,38 @@ __global__ void __launch_bounds__(256) loss_parts_kernel(const float* x, long lo
       f[2 * k] -= lo;
       f[2 * k + 1] -= hi;
     }
-    *reinterpret_cast<uint2*>(parts + ((part * rows + r) * stride + c) * 2) = make_uint2(u[0], u[1]);
+    *reinterpret_cast<uint2*>(m.parts + ((part * m.rows + r) * stride + c) * 2) = make_uint2(u[0], u[1]);
   }
 }
-cudaError_t to_parts(const void* x, long long rows, int H, void* parts, cudaStream_t stream) {
-  const long long n = rows * (H / 4);
-  loss_parts_kernel<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(static_cast<const float*>(x), rows, H, loss_stride(H),
-                                                                     static_cast<char*>(parts));
+// the parts of `words` rows of the weights, and with the first of them those of the hidden states
+cudaError_t to_parts(const LossArgs& a, int v0, int words, cudaStream_t stream) {
+  const ToParts weight = {static_cast<const float*>(a.weight) + (long long)v0 * a.H, words, static_cast<char*>(a.weight_parts)};
+  const ToParts hidden = {static_cast<const float*>(a.hidden), v0 == 0 ? a.N : 0, static_cast<char*>(a.hidden_parts)};
+  const long long n = (weight.rows + hidden.rows) * (a.H / 4);
+  loss_parts_kernel<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(weight, hidden, a.H, loss_stride(a.H));
   return cudaGetLastError();
+}
+
+// The shares' sums of a gradient, in their order, and dhidden of the pieces before: to `sum` in
+// fp32 or to `out` in bf16. Bound by the L2 cache, where the sums still are.
+__global__ void __launch_bounds__(256) loss_sums_kernel(const float* sums, int shares, long long n, float* sum, bool add,
+                                                        __nv_bfloat16* out) {
+  const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  float4 x = add ? *reinterpret_cast<const float4*>(sum + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int s = 0; s < shares; ++s) {
+    const float4 y = *reinterpret_cast<const float4*>(sums + s * n + i);
+    x.x += y.x;
+    x.y += y.y;
+    x.z += y.z;
+    x.w += y.w;
+  }
+  if (out)
+    *reinterpret_cast<uint2*>(out + i) =
+        make_uint2(Chunk<__nv_bfloat16>::pack2(x.x, x.y), Chunk<__nv_bfloat16>::pack2(x.z, x.w));
+  else
+    *reinterpret_cast<float4*>(sum + i) = x;
 }
 
 // An operand: a matrix of `rows` x `cols` in bf16, or its three parts, rows `stride` elements
@@ -474,18 +521,36 @@ inline int tile_columns(int rows, int cols, int sms) {
   return tiles * 4 <= sms ? 128 : 256;
 }
 
+// Shares of a gradient's sums: as many as there are pairs of SMs for each tile, if their steps
+// are eight at least.
+inline int sum_shares(long long tiles, int steps, int passes, int pairs) {
+  const long long most = min(steps, steps * passes / 8), n = min((long long)pairs, kSumTiles) / tiles;
+  return (int)(n < 2 || most < 2 ? 1 : n < most ? n : most);
+}
+
 template <End kEnd, bool kF32, int kN>
 cudaError_t launch_product(ProductArgs& p, int sms, cudaStream_t stream) {
-  const cudaError_t e = allow_shared<loss_product_kernel<kEnd, kF32, kN>>(kProductSmem);
+  constexpr bool kShares = kEnd == End::kHidden || kEnd == End::kWeight;
+  cudaError_t e = allow_shared<loss_product_kernel<kEnd, kF32, kN>>(kProductSmem);
   if (e != cudaSuccess) return e;
   const long long tm = ceil_div(p.rows, kM), tn = ceil_div(p.cols, kN);
   p.passes = kF32 ? 6 : 1;
   // row tiles whose operand takes about a third of L2
   const long long group = (40ll << 20) / ((long long)kM * p.depth * (kF32 ? 6 : 2));
   p.group = (int)(group < 1 ? 1 : group > tm ? tm : group);
-  const long long tiles = tm * tn;
   const int pairs = sms / 2;
-  loss_product_kernel<kEnd, kF32, kN><<<2 * (unsigned)(tiles < pairs ? tiles : pairs), kProductThreads, kProductSmem, stream>>>(p);
+  p.shares = kShares ? sum_shares(tm * tn, ceil_div(p.depth, kK), p.passes, pairs) : 1;
+  const long long units = tm * tn * p.shares;
+  loss_product_kernel<kEnd, kF32, kN><<<2 * (unsigned)(units < pairs ? units : pairs), kProductThreads, kProductSmem, stream>>>(p);
+  e = cudaGetLastError();
+  if (e != cudaSuccess || p.shares == 1) return e;
+  const LossArgs& a = p.a;
+  const long long n = (long long)p.rows * a.H, at = kEnd == End::kWeight ? (long long)p.v0 * a.H : 0;
+  void* result = kEnd == End::kWeight ? a.dweight : a.dhidden;
+  float* sum = kF32 ? static_cast<float*>(result) + at : a.dh;
+  __nv_bfloat16* out = !kF32 && (kEnd == End::kWeight || p.last) ? static_cast<__nv_bfloat16*>(result) + at : nullptr;
+  loss_sums_kernel<<<(unsigned)((n / 4 + 255) / 256), 256, 0, stream>>>(a.sums, p.shares, n, sum, kEnd == End::kHidden && !p.first,
+                                                                        out);
   return cudaGetLastError();
 }
 
@@ -508,13 +573,12 @@ cudaError_t forward(const LossArgs& a, int* share, cudaStream_t stream) {
   cudaError_t e = sm_count(&sms);
   const int columns = tile_columns(a.N, a.V, sms);
   *share = columns / 2;
-  if (kF32 && e == cudaSuccess) e = to_parts(a.hidden, a.N, a.H, a.hidden_parts, stream);
   // fp32: by pieces, as the weights' parts are made; bf16: all words at once
   const int piece = kF32 ? a.piece : a.V;
   for (int v0 = 0; v0 < a.V && e == cudaSuccess; v0 += piece) {
     const int words = min(piece, a.V - v0);
     const char* w = static_cast<const char*>(a.weight) + (long long)v0 * a.H * (kF32 ? 4 : 2);
-    if (kF32) e = to_parts(w, words, a.H, a.weight_parts, stream);
+    if (kF32) e = to_parts(a, v0, words, stream);
     ProductArgs p = {};
     p.a = a;
     p.v0 = v0;
@@ -533,7 +597,6 @@ cudaError_t backward(const LossArgs& a, cudaStream_t stream) {
   const int stride = kF32 ? loss_stride(a.H) : a.H;
   int sms = 0;
   cudaError_t e = sm_count(&sms);
-  if (kF32 && e == cudaSuccess) e = to_parts(a.hidden, a.N, a.H, a.hidden_parts, stream);
   const void* hidden = kF32 ? a.hidden_parts : a.hidden;
   for (int v0 = 0; v0 < a.V && e == cudaSuccess; v0 += a.piece) {
     ProductArgs p = {};
@@ -544,7 +607,7 @@ cudaError_t backward(const LossArgs& a, cudaStream_t stream) {
     const int words = p.last ? a.V - v0 : a.piece;
     const char* w = static_cast<const char*>(a.weight) + (long long)v0 * a.H * (kF32 ? 4 : 2);
     if (kF32) {
-      e = to_parts(w, words, a.H, a.weight_parts, stream);
+      e = to_parts(a, v0, words, stream);
       w = static_cast<const char*>(a.weight_parts);
     }
     p.rows = a.N;
