@@ -105,13 +105,18 @@ Offsets offsets(const dmc_retrofit_config* c) {
 __global__ void __launch_bounds__(256) loss_join_kernel(const LossArgs a, int shares) {
   const int t = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (t >= a.N) return;
-  float m = -INFINITY, l = 0.f;
-  for (int s = lane; s < shares; s += 32) m = fmaxf(m, a.part_m[(long long)s * a.N + t]);
+  float m = -INFINITY, l = 0.f;  // of this lane's shares, the sum relative to the maximum
+#pragma unroll 4
+  for (int s = lane; s < shares; s += 32) {
+    const float pm = a.part_m[(long long)s * a.N + t], pl = a.part_l[(long long)s * a.N + t];
+    const float to = fmaxf(m, pm), ref = to == -INFINITY ? 0.f : to;
+    l = fmaf(l, expf(m - ref), pl * expf(pm - ref));
+    m = to;
+  }
+  const float own = m;
 #pragma unroll
   for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-  const float ref = m == -INFINITY ? 0.f : m;
-  for (int s = lane; s < shares; s += 32)
-    l = fmaf(a.part_l[(long long)s * a.N + t], expf(a.part_m[(long long)s * a.N + t] - ref), l);
+  l *= expf(own - (m == -INFINITY ? 0.f : m));
 #pragma unroll
   for (int off = 16; off >= 1; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
   if (lane) return;

@@ -44,9 +44,11 @@ constexpr int kK = 64;         // columns of a step
 constexpr int kStages = 6;
 constexpr int kHalf = 128 * kK * 2;  // bytes of a CTA's half of an operand's tile (of B at most)
 constexpr int kProductThreads = 320;
+constexpr int kStageRow = 80;  // bytes of a row of a result's stage: 64 and 16 of padding
 
 struct ProductShared {
   unsigned char a[kStages][kHalf], b[kStages][kHalf];
+  unsigned char stage[8][32 * kStageRow];
   uint64_t full[kStages], empty[kStages];
   uint64_t done[2], taken[2];  // an accumulator is complete; its rows have been read (both CTAs)
   uint32_t tmem;
@@ -134,6 +136,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
 loss_product_kernel(const __grid_constant__ ProductArgs p) {
   constexpr int kHalfN = kN / 2;          // columns of a row thread
   constexpr int kHalfB = kHalf * kN / 256;  // bytes of a CTA's half of B's tile
+  constexpr int kFinish = kF32 ? 16 : 32;   // columns that go to memory at a time
   constexpr bool kOften = kF32 || kEnd == End::kStats;  // sums leave tensor memory every few steps, see above
   // operands whose rows run along the sums' terms are MN-major
   constexpr bool kAmn = kEnd == End::kWeight, kBmn = kEnd == End::kHidden || kEnd == End::kWeight;
@@ -276,6 +279,7 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
     for (int u = cluster; u < units && ok; u += clusters) {
       const Tile t = tile_of<kN>(p, kShares ? u % tiles : u);
       const int row = t.m + (int)rank * 128 + (warp & 3) * 32 + lane, col = t.n + half * kHalfN;
+      const int row0 = row - lane;  // of the warp
       const bool in = row < p.rows;
       // what the row needs beside C is on its way while the product runs
       int target = -1;
@@ -290,66 +294,97 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
       }
       const int left = p.cols - col;  // columns that count (may be over 128 or below 1)
       const int word0 = p.v0 + col;
-      // the end of the columns c .. c + 15
-      auto finish = [&](int c, float* f) {
-        if (!in || c >= left) return;
-        if (kEnd == End::kGrad) {
-          char* g = static_cast<char*>(a.grad) + ((long long)row * a.piece + col + c) * 2;
+      // 64 bytes of each of the warp's rows, the first row's at `dst`, through the warp's stage, so that
+      // a store has four neighbouring lanes per row; `bytes` of them (may be over 64) count
+      auto put = [&](const uint4 (&x)[4], char* dst, long long stride, long long bytes) {
+        unsigned char* stage = sh.stage[warp];
+        __syncwarp();  // the stage has been read
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(stage + lane * kStageRow + i * 16) = x[i];
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = k * 8 + (lane >> 2), at = (lane & 3) * 16;
+          const uint4 v = *reinterpret_cast<const uint4*>(stage + r * kStageRow + at);
+          if (row0 + r < p.rows && at < bytes) *reinterpret_cast<uint4*>(dst + r * stride + at) = v;
+        }
+      };
+      auto put_f32 = [&](const float* f, float* dst, long long stride, int columns) {
+#pragma unroll
+        for (int c = 0; c < kFinish; c += 16) {
+          uint4 x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            x[i] = make_uint4(__float_as_uint(f[c + 4 * i]), __float_as_uint(f[c + 4 * i + 1]),
+                              __float_as_uint(f[c + 4 * i + 2]), __float_as_uint(f[c + 4 * i + 3]));
+          put(x, reinterpret_cast<char*>(dst + c), stride * 4, (columns - c) * 4ll);
+        }
+      };
+      auto put_bf16 = [&](const float* f, void* dst, long long stride, int columns) {
+        uint4 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = Chunk<__nv_bfloat16>::pack(f + 8 * i);
+        put(x, static_cast<char*>(dst), stride * 2, columns * 2ll);
+      };
+      // the end of the columns c .. c + kFinish - 1, by the whole warp
+      auto finish = [&](int c, float* f) {
+        if (c >= left) return;
+        if (kEnd == End::kGrad) {
+#pragma unroll
+          for (int i = 0; i < kFinish; ++i) {
             const float pr = ex2f(fmaf(f[i], kLog2e, -lse));
             // an ignored position's gradient is zero whatever its logits are
             f[i] = target >= 0 ? (target == word0 + c + i ? pr - 1.f : pr) * d : 0.f;
           }
+          // (the piece's rows are multiples of 16 bytes)
+          if constexpr (!kF32) {
+            put_bf16(f, static_cast<__nv_bfloat16*>(a.grad) + (long long)row0 * a.piece + col + c, a.piece, left - c);
+          } else {
+            char* g = static_cast<char*>(a.grad) + ((long long)row * a.piece + col + c) * 2;
 #pragma unroll
-          for (int part = 0; part < (kF32 ? 3 : 1); ++part) {
-            uint32_t w[8];
+            for (int part = 0; part < 3; ++part) {
+              uint32_t w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              w[i] = Chunk<__nv_bfloat16>::pack2(f[2 * i], f[2 * i + 1]);
-              if (kF32) {  // what is left for the next part
-                float lo, hi;
+              for (int i = 0; i < 8; ++i) {
+                w[i] = Chunk<__nv_bfloat16>::pack2(f[2 * i], f[2 * i + 1]);
+                float lo, hi;  // what is left for the next part
                 Chunk<__nv_bfloat16>::unpack2(w[i], lo, hi);
                 f[2 * i] -= lo;
                 f[2 * i + 1] -= hi;
               }
+              uint4* dst = reinterpret_cast<uint4*>(g + (long long)part * a.N * a.piece * 2);
+              if (in) dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+              if (in && c + 8 < left) dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
             }
-            uint4* dst = reinterpret_cast<uint4*>(g + (long long)part * a.N * a.piece * 2);
-            dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
-            if (c + 8 < left) dst[1] = make_uint4(w[4], w[5], w[6], w[7]);  // (the piece's rows are multiples of 16 bytes)
           }
         }
         if (kEnd == End::kHidden || kEnd == End::kWeight) {
           if (shares > 1) {
-            float* sum = a.sums + ((long long)(u / tiles) * p.rows + row) * a.H + col + c;
-#pragma unroll
-            for (int i = 0; i < 16; i += 4)
-              if (c + i < left) *reinterpret_cast<float4*>(sum + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+            put_f32(f, a.sums + ((long long)(u / tiles) * p.rows + row0) * a.H + col + c, a.H, left - c);
             return;
           }
-          const long long at = (long long)(kEnd == End::kWeight ? p.v0 + row : row) * a.H + col + c;
+          const long long at = (long long)(kEnd == End::kWeight ? p.v0 + row0 : row0) * a.H + col + c;
           // in fp32 the pieces are added up where the result goes
           float* sum = kF32 ? static_cast<float*>(kEnd == End::kWeight ? a.dweight : a.dhidden) : a.dh;
-          if (kEnd == End::kHidden && !p.first) {
+          if (kEnd == End::kHidden && !p.first && in) {
+            const float* before = sum + at + (long long)lane * a.H;
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)
+            for (int i = 0; i < kFinish; i += 4)
               if (c + i < left) {
-                const float4 o = *reinterpret_cast<const float4*>(sum + at + i);
+                const float4 o = *reinterpret_cast<const float4*>(before + i);
                 f[i] += o.x;
                 f[i + 1] += o.y;
                 f[i + 2] += o.z;
                 f[i + 3] += o.w;
               }
           }
-          if (!kF32 && (kEnd == End::kWeight || p.last)) {
-            uint4* out = reinterpret_cast<uint4*>(static_cast<char*>(kEnd == End::kWeight ? a.dweight : a.dhidden) + at * 2);
-            out[0] = Chunk<__nv_bfloat16>::pack(f);
-            if (c + 8 < left) out[1] = Chunk<__nv_bfloat16>::pack(f + 8);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 16; i += 4)
-              if (c + i < left) *reinterpret_cast<float4*>(sum + at + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+          if constexpr (!kF32) {
+            if (kEnd == End::kWeight || p.last) {
+              put_bf16(f, static_cast<__nv_bfloat16*>(kEnd == End::kWeight ? a.dweight : a.dhidden) + at, a.H, left - c);
+              return;
+            }
           }
+          put_f32(f, sum + at, a.H, left - c);
         }
       };
       auto release = [&](uint32_t acc) {
@@ -367,7 +402,6 @@ loss_product_kernel(const __grid_constant__ ProductArgs p) {
           tc_ld32(t_row + acc * kN + c, f);
           tc_wait_ld();
           finish(c, f);
-          finish(c + 16, f + 16);
         }
         release(acc);
         ++sums;
