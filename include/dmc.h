@@ -345,7 +345,8 @@ dmc_status dmc_retrofit_states_backward(dmc_retrofit_t h, int32_t num_seqs, cons
  *   out_dev (written): as q_dev; lse_dev (written): [num_q_heads, total_tokens],
  *          the logarithm of each row's sum of exponentials.
  * Softmax weights are rounded to bf16 for their product with v in bf16. Sequences
- * do not affect each other, whatever values they hold. */
+ * do not affect each other, whatever values they hold; within one, a value of v
+ * that is not finite may reach every output (a weight of zero times NaN is NaN). */
 dmc_status dmc_retrofit_attention(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev,
                                   const void* k_dev, const void* v_dev, const float* bias_dev,
                                   const int32_t* cu_seqlens_dev, int32_t total_tokens,
@@ -354,9 +355,10 @@ dmc_status dmc_retrofit_attention(dmc_retrofit_t h, int32_t num_seqs, const void
 
 /* Gradients of dmc_retrofit_attention, given its inputs and outputs and dout_dev (as
  * out_dev). dq_dev, dk_dev, dv_dev (written) are laid out as q, k, v; a KV head's
- * gradients are summed over its group. dbias_dev (written unless NULL):
- * [num_kv_heads, total_tokens] in the handle's dtype (it starts from `out`, which
- * has no more bits). Nothing is accumulated into. */
+ * gradients are summed over its group. dbias_dev (written unless it or bias_dev is
+ * NULL): [num_kv_heads, total_tokens] in the handle's dtype, as the other gradients.
+ * In bf16, weights and the scores' gradients are rounded to bf16 for their products;
+ * dbias is summed from the unrounded ones. Nothing is accumulated into. */
 dmc_status dmc_retrofit_attention_backward(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev,
                                            const void* k_dev, const void* v_dev,
                                            const float* bias_dev, const void* out_dev,

@@ -445,6 +445,7 @@ cudaError_t forward(const AttnArgs& a, cudaStream_t stream) {
 template <int D, int kRows>
 cudaError_t backward(AttnArgs a, cudaStream_t stream) {
   constexpr int threads = Shape<kRows>::kThreads;
+  if (!a.bias) a.dbias = nullptr;
   attn_delta_kernel<D><<<(unsigned)(((long long)a.seqs.total * a.Hq + 7) / 8), 256, 0, stream>>>(a);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;

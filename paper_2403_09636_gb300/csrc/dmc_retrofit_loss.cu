@@ -30,6 +30,13 @@
 // rounded fp32 sums are 4e-8 off. Where the result is fp32 the row warps therefore take the
 // sums out of tensor memory every 1024 terms (256 in fp32 products) and add them up rounded;
 // what is rounded to bf16 afterwards is left in one accumulator.
+//
+// Bound by the tensor cores where tokens are many: 8192 x 4096 x 32000 forward 1.02 ms, 2.1 PFLOP/s, backward
+// 3.32 ms, 1.94 PFLOP/s of its three products; 6001 x 8192 x 32003 1.75 and 5.35 ms. By the weights'
+// bytes where they are few: 256 x 4096 x 32000 59 us for the statistics (262 MB, 4.5 TB/s), 51, 62 and 89
+// for gradient, dhidden and dweight. fp32: 137 TFLOP/s of the product it stands for, 25 with fp32 multiply-adds.
+// Results leave through a stage in shared memory: with a row per lane, 16 bytes each, dweight took 139 us
+// of the latter and 8192 tokens 4.46 ms instead of 4.34.
 #include <math.h>
 
 #include "dmc_retrofit.cuh"
@@ -549,14 +556,16 @@ cudaError_t matrix_map(CUtensorMap* map, const void* base, uint64_t rows, uint64
 }
 
 // Columns of a tile: 256, or 128 where tiles of 256 would be too few for half of the pairs of
-// SMs: twice as many clusters, each with half the work per step.
+// SMs: twice as many clusters, each with half the work per step (257 x 256 x 1009 in fp32, forward and
+// backward, 135 us with 256, 80 with 128).
 inline int tile_columns(int rows, int cols, int sms) {
   const long long tiles = (long long)ceil_div(rows, kM) * ceil_div(cols, 256);
   return tiles * 4 <= sms ? 128 : 256;
 }
 
 // Shares of a gradient's sums: as many as there are pairs of SMs for each tile, if their steps
-// are eight at least.
+// are eight at least. 8 x 1024 x 100000 forward and backward 512 us whole, 257 in shares; 100 x 2048 x 32000
+// in fp32 1289 and 862; 257 x 256 x 1009 in fp32 62 and 49; 8192 x 256 x 1000 74 and 54.
 inline int sum_shares(long long tiles, int steps, int passes, int pairs) {
   const long long most = min(steps, steps * passes / 8), n = min((long long)pairs, kSumTiles) / tiles;
   return (int)(n < 2 || most < 2 ? 1 : n < most ? n : most);

@@ -21,12 +21,17 @@
 // over its neighbours back to where the product of the alphas between falls below 2^-126 (nearly
 // binary decisions: two or three chunks) or to the nearest of every 16th chunk, whose own `in`
 // is waited for. Where the chain begins follows from the data alone, so results do not depend on
-// how far others
-// have come. Chunks are taken from a counter, so that those a warp waits for have
+// how far others have come. Chunks are taken from a counter, so that those a warp waits for have
 // started; they publish before they wait. Every published number carries the number of the launch
 // in the same 8 bytes: no fence or flag stands between it and its reader (a fence waited for
 // the warp's loads and stores, 4 us of the 18 that a chunk took), and nothing has to be cleared
 // between launches or replays of a graph.
+//
+// Bound by the instructions of a chunk's two passes, at half of the copy bandwidth or less. Four sequences
+// of 2048 tokens, 32 heads of 128, bf16: forward 70 us (272 MB, 3.9 TB/s), backward 158 us (407 MB,
+// 2.6 TB/s: both dots of every token on top). Slower: warps that stay and take one chunk after another
+// (backward 164; with chunks taken ahead, whose neighbours wait for one that has not begun, 217),
+// rows read a second time from L2 instead of kept in shared memory (168 to 188).
 #include <type_traits>
 
 #include "dmc_retrofit.cuh"

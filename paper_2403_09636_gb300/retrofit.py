@@ -68,7 +68,7 @@ class DmcRetrofit:
         except Exception:
             pass
 
-    # ---- checks (of a call's 13 us on the host, with outputs given, they were 6; they are 3)
+    # ---- checks, of one expression each: 3 of the 10 us that a call with its outputs given takes on the host
 
     def _is(self, name, t, shape, dtype):
         if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == self.index
