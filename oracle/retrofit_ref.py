@@ -79,7 +79,8 @@ def attention_all(q, k, v, bias, dout, dtype):
         qh, doh = q.permute(1, 0, 2), dout.double().permute(1, 0, 2)
         terms = qh.abs() @ kx.abs().transpose(1, 2) * c
         seen = p > 0
-        e = 2.0 ** -22 * (8 + (terms * seen).amax() + (0 if b is None else b[b > -math.inf].abs().max().clamp(max=200.0)))
+        shift = torch.zeros(()) if b is None or not bool((b > -math.inf).any()) else b[b > -math.inf].abs().max()
+        e = 2.0 ** -22 * (8 + (terms * seen).amax() + shift.clamp(max=200.0))
         rp = e if dtype == torch.float32 else e + u       # relative, of a weight in a product
         o_sum = p @ vx.abs()
         o_bound = (u * out.permute(1, 0, 2).abs() + (rp + e) * o_sum)

@@ -1,7 +1,7 @@
 """Attention's backward pass where its work on K and V is split over a group's queries, and where it is not.
 
 Tiles of 128 tokens times KV heads decide: few of them are split into shares of whole
-heads, added up afterwards; from 304 on they are not.
+heads, added up afterwards; from 304 on they are not, nor, in bf16, are sequences of up to 384 tokens.
 """
 import pytest
 import torch
@@ -21,6 +21,10 @@ CASES = [
     ([40] * 18, (32, 16, 64)),        # just below the limit
     ([100, 33] * 20, (24, 8, 64)),    # above it: whole groups
     ([64] * 150, (10, 5, 128)),
+    ([431], (64, 2, 128)),               # longer than three tiles: shares in bf16 too
+    ([1, 390, 127], (30, 6, 64)),
+    ([410, 129, 129, 1], (36, 12, 64)),
+    ([385, 384], (7, 1, 128)),
 ]
 
 
