@@ -455,7 +455,7 @@ cudaError_t attn_forward_f32(const AttnArgs& a, int D, cudaStream_t stream) {
   return D == 128 ? forward<128>(a, stream) : forward<64>(a, stream);
 }
 // From five tiles of KV heads per four SMs on: 160 tiles (300 tokens, 32 heads of 128) 131 and 143, 192 (1500
-// tokens, 40 / 8 heads of 64) 1285 and 1124, 272 (two sequences of 1024, 8 heads of 128) 523 and 491.
+// tokens, 40 / 8 heads of 64) 1285 and 1067, 272 (two sequences of 1024, 8 heads of 128) 523 and 451.
 cudaError_t attn_backward_f32(const AttnArgs& args, int D, cudaStream_t stream) {
   AttnArgs a = args;
   if (!a.bias) a.dbias = nullptr;

@@ -14,8 +14,8 @@
 // eight rows of a matrix read fall into different banks. 8 warps, one block per SM (209 KB).
 // Bound by the tensor cores' rate for these instructions (597 TFLOP/s, a sixth of which is 99 of fp32 products; busy
 // for half of the time) and, between barriers that all warps pass, by the exponentials and the splitting:
-// 10 sequences of 1148 tokens, 32 / 8 heads of 128, forward 2.03 ms (53 TFLOP/s), backward 7.62 ms (50); fp32
-// multiply-adds in tiles of 64 took 2.77 and 10.1 (39, 37). 8 of 700 tokens, 16 / 8 heads of 64, 216 and 707
+// 10 sequences of 1148 tokens, 32 / 8 heads of 128, forward 2.03 ms (53 TFLOP/s), backward 7.09 ms (53); fp32
+// multiply-adds in tiles of 64 took 2.77 and 10.1 (39, 37). 8 of 700 tokens, 16 / 8 heads of 64, 217 and 681
 // us; 291 and 1069 so. The tests of a pair's mask only where queries and rows meet: 2.38 ms forward without.
 #include <math.h>
 
@@ -36,12 +36,12 @@ struct Tile {
   static constexpr int kPer = kT * (D / 4) / kThreads;  // 16-byte pieces of a thread
 };
 
-// a tile's rows, the thread's share of them; zero from `rows` on
-template <int D>
-__device__ __forceinline__ void fetch(float4 (&x)[Tile<D>::kPer], const float* src, long long stride, int rows) {
+// Rows of a tile, thread t's share of them when kN threads load 64 kN / 256 rows; zero from `rows` on
+template <int D, int kN>
+__device__ __forceinline__ void fetch(float4 (&x)[Tile<D>::kPer], int t, const float* src, long long stride, int rows) {
 #pragma unroll
   for (int i = 0; i < Tile<D>::kPer; ++i) {
-    const int at = threadIdx.x + i * kThreads, r = at / (D / 4), c = at % (D / 4) * 4;
+    const int at = t + i * kN, r = at / (D / 4), c = at % (D / 4) * 4;
     x[i] = r < rows ? *reinterpret_cast<const float4*>(src + r * stride + c) : make_float4(0.f, 0.f, 0.f, 0.f);
   }
 }
@@ -56,11 +56,11 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t (&w)[3]) {
     y -= b;
   }
 }
-template <int D>
-__device__ __forceinline__ void keep(unsigned char* tile, const float4 (&x)[Tile<D>::kPer]) {
+template <int D, int kN>
+__device__ __forceinline__ void keep(unsigned char* tile, int t, const float4 (&x)[Tile<D>::kPer]) {
 #pragma unroll
   for (int i = 0; i < Tile<D>::kPer; ++i) {
-    const int at = threadIdx.x + i * kThreads, r = at / (D / 4), c = at % (D / 4) * 4;
+    const int at = t + i * kN, r = at / (D / 4), c = at % (D / 4) * 4;
     uint32_t u[3], v[3];
     split2(x[i].x, x[i].y, u);
     split2(x[i].z, x[i].w, v);
@@ -69,12 +69,15 @@ __device__ __forceinline__ void keep(unsigned char* tile, const float4 (&x)[Tile
       *reinterpret_cast<uint2*>(tile + p * Tile<D>::kPart + r * Tile<D>::kRow + c * 2) = make_uint2(u[p], v[p]);
   }
 }
-template <int D>
-__device__ __forceinline__ void load(unsigned char* tile, const float* src, long long stride, int rows) {
+template <int D, int kN>
+__device__ __forceinline__ void load(unsigned char* tile, int t, const float* src, long long stride, int rows) {
   float4 x[Tile<D>::kPer];
-  fetch<D>(x, src, stride, rows);
-  keep<D>(tile, x);
+  fetch<D, kN>(x, t, src, stride, rows);
+  keep<D, kN>(tile, t, x);
 }
+
+// A barrier of one half of the block's warps
+__device__ __forceinline__ void half_sync(int half) { asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory"); }
 
 __device__ __forceinline__ void matrices(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -236,7 +239,8 @@ __device__ __forceinline__ void gather(const float* at, float (&x)[D / 8][4]) {
 }
 
 // A block: 128 queries of a head, 16 per warp. K's next tile is fetched while S is computed and V's while
-// O is, into registers, and kept when all warps are through with the present one.
+// O is, into registers, and kept when all warps are through with the present one. (Half of the warps half a
+// step behind the others, so that exponentials run beside products, was 4 % slower: two more barriers.)
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) parts_forward_kernel(const AttnArgs a) {
   extern __shared__ unsigned char smem[];
@@ -254,10 +258,10 @@ __global__ void __launch_bounds__(kThreads, 1) parts_forward_kernel(const AttnAr
   const float *q = static_cast<const float*>(a.q) + (long long)i0 * qs + (long long)h * D;
   const float *k = static_cast<const float*>(a.k) + (long long)hk * D, *v = static_cast<const float*>(a.v) + (long long)hk * D;
   const float* bias = a.bias ? a.bias + (long long)hk * a.seqs.total : nullptr;
-  load<D>(Q, q, qs, p.t1 - i0);
-  if (p.t1 - i0 > kT) load<D>(Q + Tile<D>::kBytes, q + kT * qs, qs, p.t1 - i0 - kT);
-  load<D>(K, k + p.t0 * ks, ks, p.t1 - p.t0);
-  load<D>(V, v + p.t0 * ks, ks, p.t1 - p.t0);
+  load<D, kThreads>(Q, tid, q, qs, p.t1 - i0);
+  if (p.t1 - i0 > kT) load<D, kThreads>(Q + Tile<D>::kBytes, tid, q + kT * qs, qs, p.t1 - i0 - kT);
+  load<D, kThreads>(K, tid, k + p.t0 * ks, ks, p.t1 - p.t0);
+  load<D, kThreads>(V, tid, v + p.t0 * ks, ks, p.t1 - p.t0);
   if (tid < kT) biases[tid] = bias && p.t0 + tid < p.t1 ? bias[p.t0 + tid] : 0.f;
   __syncthreads();
   const uint32_t sq = smem_u32(Q) + (warp >> 2) * Tile<D>::kBytes + (warp & 3) * 16 * Tile<D>::kRow;
@@ -273,16 +277,16 @@ __global__ void __launch_bounds__(kThreads, 1) parts_forward_kernel(const AttnAr
     float4 next[Tile<D>::kPer];
     float next_b = 0.f;
     if (more) {
-      fetch<D>(next, k + (long long)(j0 + kT) * ks, ks, p.t1 - j0 - kT);
+      fetch<D, kThreads>(next, tid, k + (long long)(j0 + kT) * ks, ks, p.t1 - j0 - kT);
       if (bias && tid < kT && j0 + kT + tid < p.t1) next_b = bias[j0 + kT + tid];
     }
     float s[8][4];
     if (use) scores<D, 8>(s, sq, sk);
     __syncthreads();  // K has been read
     if (more) {
-      keep<D>(K, next);
+      keep<D, kThreads>(K, tid, next);
       if (tid < kT) biases[((n + 1) & 1) * kT + tid] = next_b;
-      fetch<D>(next, v + (long long)(j0 + kT) * ks, ks, p.t1 - j0 - kT);
+      fetch<D, kThreads>(next, tid, v + (long long)(j0 + kT) * ks, ks, p.t1 - j0 - kT);
     }
     if (use) {
       if (j0 + kT <= row0) {  // rows before all of the warp's queries
@@ -333,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1) parts_forward_kernel(const AttnAr
     }
     __syncthreads();  // V has been read
     if (more) {
-      keep<D>(V, next);
+      keep<D, kThreads>(V, tid, next);
       __syncthreads();
     }
   }
@@ -346,7 +350,9 @@ __global__ void __launch_bounds__(kThreads, 1) parts_forward_kernel(const AttnAr
 }
 
 // dQ of 64 queries of a head (see dmc_retrofit_f32.cu for the formulas): a warp has 16 of them and half of
-// the rows of a tile of K and V.
+// the rows of a tile of K and V. The halves load their own rows and go their own ways, the second
+// from where the first has its first products, so that one's exponentials run beside the other's products
+// (10 x 1148 tokens, backward 7.62 ms with barriers of the whole block, 7.09 so).
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) parts_dq_kernel(const AttnArgs a) {
   extern __shared__ unsigned char smem[];
@@ -361,10 +367,10 @@ __global__ void __launch_bounds__(kThreads, 1) parts_dq_kernel(const AttnArgs a)
   const long long qs = (long long)a.Hq * D, ks = (long long)a.Hkv * D, at = (long long)i0 * qs + (long long)h * D;
   const float *k = static_cast<const float*>(a.k) + (long long)hk * D, *v = static_cast<const float*>(a.v) + (long long)hk * D;
   const float* bias = a.bias ? a.bias + (long long)hk * a.seqs.total : nullptr;
-  load<D>(Q, static_cast<const float*>(a.q) + at, qs, p.t1 - i0);
-  load<D>(O, static_cast<const float*>(a.dout) + at, qs, p.t1 - i0);
-  load<D>(K, k + p.t0 * ks, ks, p.t1 - p.t0);
-  load<D>(V, v + p.t0 * ks, ks, p.t1 - p.t0);
+  load<D, kThreads>(Q, tid, static_cast<const float*>(a.q) + at, qs, p.t1 - i0);
+  load<D, kThreads>(O, tid, static_cast<const float*>(a.dout) + at, qs, p.t1 - i0);
+  load<D, kThreads>(K, tid, k + p.t0 * ks, ks, p.t1 - p.t0);
+  load<D, kThreads>(V, tid, v + p.t0 * ks, ks, p.t1 - p.t0);
   if (tid < kT) biases[tid] = bias && p.t0 + tid < p.t1 ? bias[p.t0 + tid] : 0.f;
   const int group = warp & 3, half = warp >> 2;
   const int row0 = i0 + group * 16, mine = row0 + (lane >> 2), c0 = half * 32 + (lane & 3) * 2;
@@ -381,26 +387,29 @@ __global__ void __launch_bounds__(kThreads, 1) parts_dq_kernel(const AttnArgs a)
   const uint32_t sq = smem_u32(Q) + own, so = smem_u32(O) + own, sk = smem_u32(K) + other, sv = smem_u32(V) + other;
   float dq[D / 8][4];
   clear(dq);
+  const int t = tid & 127;  // of the half
+  if (half) asm volatile("bar.sync 3, 256;" ::: "memory");
 #pragma unroll 1
   for (int n = 0; n < steps; ++n) {
-    const int j0 = p.t0 + n * kT;
+    const int j0 = p.t0 + n * kT, j1 = j0 + kT + half * 32;  // the next tile's first row of this half
     const bool more = n + 1 < steps;
     const float* b = biases + (n & 1) * kT;
     float4 next[Tile<D>::kPer];
     float next_b = 0.f;
     if (more) {
-      fetch<D>(next, v + (long long)(j0 + kT) * ks, ks, p.t1 - j0 - kT);
-      if (bias && tid < kT && j0 + kT + tid < p.t1) next_b = bias[j0 + kT + tid];
+      fetch<D, 128>(next, t, v + (long long)j1 * ks, ks, p.t1 - j1);
+      if (bias && t < 32 && j1 + t < p.t1) next_b = bias[j1 + t];
     }
     float dp[4][4], s[4][4];
     scores<D, 4>(dp, so, sv);
-    __syncthreads();  // V has been read
+    half_sync(half);  // V has been read
     if (more) {
-      keep<D>(V, next);
-      if (tid < kT) biases[((n + 1) & 1) * kT + tid] = next_b;
-      fetch<D>(next, k + (long long)(j0 + kT) * ks, ks, p.t1 - j0 - kT);
+      keep<D, 128>(V + half * 32 * Tile<D>::kRow, t, next);
+      if (t < 32) biases[((n + 1) & 1) * kT + half * 32 + t] = next_b;
+      fetch<D, 128>(next, t, k + (long long)j1 * ks, ks, p.t1 - j1);
     }
     scores<D, 4>(s, sq, sk);
+    if (n == 0 && !half) asm volatile("bar.arrive 3, 256;" ::: "memory");
     if (j0 + kT <= i0) {  // rows before all of the queries
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
@@ -426,12 +435,13 @@ __global__ void __launch_bounds__(kThreads, 1) parts_dq_kernel(const AttnArgs a)
 #pragma unroll
     for (int x = 0; x < 2; ++x) operand(w[x], s[2 * x], s[2 * x + 1]);
     sums<D, 2, 4>(dq, w, sk);
-    __syncthreads();  // K has been read
+    half_sync(half);  // K has been read
     if (more) {
-      keep<D>(K, next);
-      __syncthreads();
+      keep<D, 128>(K + half * 32 * Tile<D>::kRow, t, next);
+      half_sync(half);
     }
   }
+  __syncthreads();
   float* through = reinterpret_cast<float*>(K) + group * 16 * (D + 4);
   if (half) leave<D>(through, dq);
   __syncthreads();
@@ -441,7 +451,7 @@ __global__ void __launch_bounds__(kThreads, 1) parts_dq_kernel(const AttnArgs a)
 }
 
 // dK, dV and dbias of 64 rows of a KV head: a warp has 16 of them and half of the queries of a tile, everything
-// transposed, so that the weights' rows are rows of K.
+// transposed, so that the weights' rows are rows of K. The halves are apart as in dQ's kernel.
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) parts_dkv_kernel(const AttnArgs a) {
   extern __shared__ unsigned char smem[];
@@ -453,8 +463,8 @@ __global__ void __launch_bounds__(kThreads, 1) parts_dkv_kernel(const AttnArgs a
   const int j0 = p.t0 + p.at * kT;
   const float scale = 1.f / sqrtf((float)D);
   const long long qs = (long long)a.Hq * D, ks = (long long)a.Hkv * D, at = (long long)j0 * ks + (long long)hk * D;
-  load<D>(K, static_cast<const float*>(a.k) + at, ks, p.t1 - j0);
-  load<D>(V, static_cast<const float*>(a.v) + at, ks, p.t1 - j0);
+  load<D, kThreads>(K, tid, static_cast<const float*>(a.k) + at, ks, p.t1 - j0);
+  load<D, kThreads>(V, tid, static_cast<const float*>(a.v) + at, ks, p.t1 - j0);
   const int group = warp & 3, half = warp >> 2;
   const int row0 = j0 + group * 16, mine = row0 + (lane >> 2), c0 = half * 32 + (lane & 3) * 2;
   float b[2], db[2] = {0.f, 0.f};
@@ -466,23 +476,27 @@ __global__ void __launch_bounds__(kThreads, 1) parts_dkv_kernel(const AttnArgs a
   float dk[D / 8][4], dv[D / 8][4];
   clear(dk);
   clear(dv);
-  const int tiles = (p.t1 - j0 + kT - 1) / kT;
+  const int tiles = (p.t1 - j0 + kT - 1) / kT, t = tid & 127;  // t: of the half
+  __syncthreads();
+  if (half) asm volatile("bar.sync 3, 256;" ::: "memory");
 #pragma unroll 1
   for (int n = 0; n < a.G * tiles; ++n) {
     const int h = hk * a.G + n / tiles, i0 = j0 + n % tiles * kT, rows = min(kT, p.t1 - i0);
-    const long long q0 = (long long)i0 * qs + (long long)h * D;
-    __syncthreads();  // the tiles before have been read
-    load<D>(Q, static_cast<const float*>(a.q) + q0, qs, rows);
-    load<D>(O, static_cast<const float*>(a.dout) + q0, qs, rows);
-    if (tid < kT) {
-      const long long x = (long long)h * a.seqs.total + i0 + tid;
-      L[tid] = tid < rows ? a.lse[x] : 0.f;
-      E[tid] = tid < rows ? a.rows[x] : 0.f;
+    const int r0 = half * 32;  // this half's first query of the tile
+    const long long q0 = (long long)(i0 + r0) * qs + (long long)h * D;
+    half_sync(half);  // the tiles before have been read
+    load<D, 128>(Q + r0 * Tile<D>::kRow, t, static_cast<const float*>(a.q) + q0, qs, rows - r0);
+    load<D, 128>(O + r0 * Tile<D>::kRow, t, static_cast<const float*>(a.dout) + q0, qs, rows - r0);
+    if (t < 32) {
+      const long long x = (long long)h * a.seqs.total + i0 + r0 + t;
+      L[r0 + t] = r0 + t < rows ? a.lse[x] : 0.f;
+      E[r0 + t] = r0 + t < rows ? a.rows[x] : 0.f;
     }
-    __syncthreads();
+    half_sync(half);
     float s[4][4], dp[4][4];
     scores<D, 4>(s, sk, sq);
     scores<D, 4>(dp, sv, so);
+    if (n == 0 && !half) asm volatile("bar.arrive 3, 256;" ::: "memory");
     if (i0 >= j0 + kT && rows == kT) {  // queries after all of the rows
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
