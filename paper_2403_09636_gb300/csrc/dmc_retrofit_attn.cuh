@@ -113,7 +113,9 @@ __device__ __forceinline__ bool ordered_work(const Seqs& q, int piece, bool from
   return false;
 }
 
-// Work is numbered by piece, heads fastest. The numbers 0 .. gridDim - 1 go to the CTAs, then
+// Work is numbered by piece, heads fastest: items of one length run side by side. (Groups of heads whose
+// K and V fit in L2, one group after another, are slower: four sequences of 2048 tokens, 32 heads, forward
+// 134 -> 151 us; 8192 tokens of 64 / 8 heads, backward 2.74 -> 3.34 ms.) The numbers 0 .. gridDim - 1 go to the CTAs, then
 // each takes the next from a counter. Warp 9 does so, one piece of work ahead of the other
 // warps, and hands it to them. The last CTA resets the counter for the next launch.
 struct WorkRing {
