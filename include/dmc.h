@@ -264,8 +264,10 @@ dmc_status dmc_cache_status(dmc_cache_t cache, cudaStream_t stream, uint32_t* bi
  * [heads, total_tokens]; cu_seqlens, total_tokens and max_seqlen are as in
  * dmc_prefill_compress. Sequences may be empty. Sums, softmax statistics and
  * states are held in fp32; every output is rounded once to its type, and no result
- * depends on the order in which blocks run. All calls on one handle must be ordered
- * on the GPU: they share its scratch. Calls allocate nothing and can be captured.
+ * depends on the order in which blocks run. fp32 products on the tensor cores (the
+ * loss, and attention of calls that fill the GPU) take an operand's 24 bits as three
+ * bf16 numbers: an infinite one gives NaN, one below 2^-110 loses its last bits.
+ * All calls on one handle must be ordered on the GPU: they share its scratch. Calls allocate nothing and can be captured.
  * ------------------------------------------------------------------------ */
 
 typedef struct {
