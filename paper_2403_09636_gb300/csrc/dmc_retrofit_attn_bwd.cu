@@ -9,9 +9,10 @@
 //
 // dK, dV: a work item is 128 rows of K and V of one KV head; it walks over the query
 // tiles that see them, for all queries of the group, so that a shared head's gradients are
-// sums in tensor memory. Everything is transposed, S^T = K Q^T, so that a thread's
-// row is a row of K: P^T and dS^T are written over S^T and dP^T and multiply dO and Q from
-// tensor memory, and dbias is a sum within a thread. The order of products,
+// sums in tensor memory (where such items are few, for a share of the group's heads: attn_shares).
+// Everything is transposed, S^T = K Q^T, so that a thread's row is a row of K: P^T and dS^T are
+// written over S^T and dP^T and multiply dO and Q from tensor memory, and dbias is a sum within a
+// thread. The order of products,
 //   dV += P^T dO (step i), dK += dS^T Q (i), S^T (i + 1), dP^T (i + 1),
 // leaves one between any two of which the second overwrites what the first reads.
 // dQ: a work item is 128 queries of one head; it walks over the K and V tiles they see.
