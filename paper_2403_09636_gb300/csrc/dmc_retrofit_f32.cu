@@ -9,9 +9,10 @@
 // neighbouring columns, which leaves issue slots for the reads.
 // Where SMs are left without a block, a block's steps one after another set the time: so small
 // tiles, the next step's on their way meanwhile, dQ in one launch with dK and dV, and
-// those in shares of a group's heads (attn_shares). 256 tokens of 4 heads of 64: forward 25 us, backward 35 (63 in two
-// launches without tiles ahead); 500 tokens of 32 / 8 heads of 128: backward 278 (532 with whole groups).
-// 256 threads per block take 24 and 38, 731.
+// those in shares of a group's heads (attn_shares); products unrolled as a whole, whose reads then run
+// ahead. 256 tokens of 4 heads of 64: forward 21 us, backward 31 (25 and 35 unrolled by 4 and 2; 26 and 63 in
+// two launches without tiles ahead); 500 tokens of 32 / 8 heads of 128: backward 290 (280 by 4 and 2, 532 with
+// whole groups). 256 threads per block were no faster (24 and 38, 731).
 #include <math.h>
 
 #include "dmc_retrofit.cuh"
@@ -44,7 +45,7 @@ __device__ __forceinline__ void load_rows(float* tile, const float* src, long lo
 template <int D>
 __device__ __forceinline__ void dot_tile(float2 (&acc)[kI][kJ], const float* X, const float* Y) {
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-#pragma unroll 4
+#pragma unroll
   for (int c = 0; c < D; c += 4) {
     float4 x[kI], y[kJ];
 #pragma unroll
@@ -65,7 +66,7 @@ __device__ __forceinline__ void dot_tile(float2 (&acc)[kI][kJ], const float* X, 
 template <int D>
 __device__ __forceinline__ void sum_tile(float2 (&acc)[kI][D / 32], const float* W, const float* Y) {
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-#pragma unroll 2
+#pragma unroll
   for (int r = 0; r < kT; r += 4) {
     float4 w[kI];
 #pragma unroll
