@@ -405,12 +405,13 @@ __global__ void __launch_bounds__(32) states_kernel(const StatesArgs a) {
 // Chunks from the last to the first, a block of a warp for k and a warp for v per chunk and
 // head. A chunk passes on the sum over t of (its alphas up to t) u_t, and w_t alike. Dots over all
 // elements go through shared memory: 16 partial sums per token, then a token per lane.
+constexpr int kOfZeta = 0, kOfOmega = 1, kOfSum = 2;  // rows of `other`
 template <typename T, int D>
 struct BackShared {
   T rows[2][kC * D], grads[2][kC * D];
   Coef coef[2][kC];
   float dots[2][kC][17];
-  float other[2][kC];         // v's share of a dot
+  float other[3][kC];         // v's shares of the dots, a row each: what one warp reads the other does not write again
   uint64_t loaded[2];
   Turn turn;
 };
@@ -531,9 +532,9 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
     if (p.at > 0) publish<R::kE>(a.sums + row, pass, turn.tag);
   }
   float zeta = take();
-  if (which) sh.other[0][lane] = zeta;
+  if (which) sh.other[kOfZeta][lane] = zeta;
   __syncthreads();
-  zeta = in_chunk ? -(zeta + sh.other[0][lane]) * rz * rz : 0.f;  // (of use to the first warp)
+  zeta = in_chunk ? -(zeta + sh.other[kOfZeta][lane]) * rz * rz : 0.f;  // (of use to the first warp)
   if (p.at > 0) {
     float s = zeta * prod;
 #pragma unroll
@@ -600,8 +601,8 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
     }
   }
   if (which) {
-    sh.other[0][lane] = domega;
-    sh.other[1][lane] = dsum;
+    sh.other[kOfOmega][lane] = domega;
+    sh.other[kOfSum][lane] = dsum;
   }
   __syncthreads();
   if (which) return;
@@ -624,8 +625,8 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
   float zbefore = __shfl_up_sync(0xffffffffu, z, 1);
   if (lane == 0) zbefore = zbefore0;
   if (in_chunk) {
-    domega += sh.other[0][lane] + zeta;
-    dalpha += dsum + sh.other[1][lane] + zeta * zbefore;
+    domega += sh.other[kOfOmega][lane] + zeta;
+    dalpha += dsum + sh.other[kOfSum][lane] + zeta * zbefore;
     float dx = 0.f;
     if (tok > p.t0) dx = (dalpha * g.alpha * g.rest - dbias * g.alpha) / a.temperature;
     // over what lane 0 has written there
