@@ -267,7 +267,7 @@ __device__ __forceinline__ float come_in(const uint64_t* own, const uint64_t* in
   if (!end && d < n) {
     float2 zi;
     await<D>(in + d * step, x, tag, error);
-    for (int tries = 0; !look_zp<D>(in + d * step, zi, tag); ++tries)
+    for (int tries = 0; !__all_sync(0xffffffffu, look_zp<D>(in + d * step, zi, tag)); ++tries)
       if (tries >= 64 && give_up(since, error)) break;
     z = zi.x;
   }
