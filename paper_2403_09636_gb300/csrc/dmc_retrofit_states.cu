@@ -20,7 +20,7 @@
 //   in_{c+1} = own_c + prod_c in_c
 // over its neighbours back to where the product of the alphas between falls below 2^-126 (nearly
 // binary decisions: two or three chunks) or to the nearest of every 16th chunk, whose own `in`
-// is waited for. Where the chain begins follows from the data alone, so results do not depend on
+// is waited for (dmc_chain.h). Where the chain begins follows from the data alone, so results do not depend on
 // how far others have come. Chunks are taken from a counter, so that those a warp waits for have
 // started; they publish before they wait. Every published number carries the number of the launch
 // in the same 8 bytes: no fence or flag stands between it and its reader (a fence waited for
@@ -34,6 +34,7 @@
 // rows read a second time from L2 instead of kept in shared memory (168 to 188).
 #include <type_traits>
 
+#include "dmc_chain.h"
 #include "dmc_retrofit.cuh"
 
 namespace dmc {
@@ -231,20 +232,13 @@ __device__ __forceinline__ void await(const uint64_t* row, float2 (&f)[D / 64], 
     if (tries >= 64 && give_up(since, error)) return;
 }
 
-// Chunks between two whose `in` others may wait for; products of alphas below kTiny carry nothing.
-constexpr int kAnchor = 16;
-constexpr float kTiny = 1.17549435e-38f;  // 2^-126
-
-// Whether others may ask for what comes into the chunk that has n neighbours on the side it comes from.
-__device__ __forceinline__ bool asked_for(int n, float prod) { return n > 0 && n % kAnchor == 0 && !(prod < kTiny); }
-
 // What comes into a chunk from its n > 0 neighbours on one side, `step` apart: the lane's sums x,
 // and z (Z). own, in: this chunk's rows.
 template <int D>
 __device__ __forceinline__ float come_in(const uint64_t* own, const uint64_t* in, int n, long long step, unsigned int tag,
                                          unsigned int* error, float2 (&x)[D / 64]) {
   constexpr int kP = D / 64;
-  const int lane = threadIdx.x & 31, d = (n - 1) % kAnchor + 1;  // the d-th neighbour is an anchor or the last
+  const int lane = threadIdx.x & 31, d = chain_reach(n);
   // a neighbour per lane: its z and the product of its alphas
   float2 zp = make_float2(0.f, 1.f);
   uint64_t since = 0;
@@ -259,7 +253,7 @@ __device__ __forceinline__ float come_in(const uint64_t* own, const uint64_t* in
     const float o = __shfl_up_sync(0xffffffffu, upto, off);
     if (lane >= off) upto *= o;
   }
-  const unsigned int end = __ballot_sync(0xffffffffu, lane < d && upto < kTiny);
+  const unsigned int end = __ballot_sync(0xffffffffu, lane < d && chain_ends(zp.y, upto));
   const int far = end ? __ffs(end) : d;
   float z = 0.f;
 #pragma unroll
