@@ -83,12 +83,13 @@ __device__ __forceinline__ Piece find_piece(const Seqs& q, int piece, int index)
   return p;
 }
 
-// By one block of a call: faulty cu_seqlens set their bit.
-__device__ __forceinline__ void check_seqs(const Seqs& q, unsigned int* error) {
+// By one block of a call: faulty cu_seqlens set their bit. Whether this thread has found any.
+__device__ __forceinline__ bool check_seqs(const Seqs& q, unsigned int* error) {
   bool bad = false;
   for (int s = threadIdx.x; s < q.num; s += blockDim.x) bad |= !seq_ok(q, q.cu[s], q.cu[s + 1]);
   if (threadIdx.x == 0) bad |= q.cu[0] != 0 || q.cu[q.num] != q.total;
   if (bad) atomicOr(error, DMC_FAULT_BAD_SEQLENS);
+  return bad;
 }
 
 // A pair of neighbouring elements in fp32.
@@ -135,7 +136,7 @@ struct StatesArgs {
   void *dk, *dv;
   // scratch
   uint64_t *sums, *carry;  // [piece][Hkv][2][D + 2]: a piece's own sums; what comes into it (with their launch)
-  unsigned int* turns;     // come, gone, number of the launch
+  unsigned int* turns;     // come, gone, number of the launch, of the launch that has to stop
 };
 
 struct AttnArgs {

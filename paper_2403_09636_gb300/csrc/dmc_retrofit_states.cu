@@ -154,7 +154,7 @@ __device__ __forceinline__ float2 hi2(float4 f) { return make_float2(f.z, f.w); 
 // ---- the order of warps
 
 // words of StatesArgs::turns, each in a line of its own (everybody adds to the first two)
-constexpr int kCome = 0, kGone = 32, kLaunch = 64;
+constexpr int kCome = 0, kGone = 32, kLaunch = 64, kStop = 96;  // kStop: the launch whose waits have to end
 
 struct Turn {
   int index;         // in the order in which they come
@@ -172,6 +172,12 @@ __device__ __forceinline__ void leave(const StatesArgs& a, const Turn& t) {
   if (atomicAdd(&a.turns[kGone], 1u) != gridDim.x - 1) return;
   a.turns[kCome] = a.turns[kGone] = 0;
   a.turns[kLaunch] = t.tag;
+}
+
+// Faulty cu_seqlens, where a chunk may have no neighbour, end this launch's waits (the fault bits stay from call
+// to call and say nothing about it). One block.
+__device__ __forceinline__ void check_seqs(const StatesArgs& a, unsigned int tag) {
+  if (check_seqs(a.seqs, a.error)) *reinterpret_cast<volatile unsigned int*>(&a.turns[kStop]) = tag;
 }
 
 // ---- published numbers: {value, launch}
@@ -212,31 +218,32 @@ __device__ __forceinline__ bool look(const uint64_t* row, float2 (&f)[D / 64], u
   return there;
 }
 // After tries that found nothing, by a whole warp: whether to give up, since this has taken too long or
-// a fault has been found (a wait that gave up, or cu_seqlens that do not fit, where a chunk may have no
-// neighbour).
-__device__ __forceinline__ bool give_up(uint64_t& since, unsigned int* error) {
+// another wait of the launch has (or its cu_seqlens do not fit).
+__device__ __forceinline__ bool give_up(uint64_t& since, const StatesArgs& a, unsigned int tag) {
   __nanosleep(500);
-  bool over = *reinterpret_cast<volatile unsigned int*>(error) != 0;
+  volatile unsigned int* stop = &a.turns[kStop];
+  bool over = *stop == tag;
   const uint64_t t = globaltimer_ns();
   if (since == 0) since = t;
   if (t - since > kWaitLimitNs) {
-    atomicOr(error, DMC_FAULT_WAIT_TIMEOUT);
+    atomicOr(a.error, DMC_FAULT_WAIT_TIMEOUT);
+    *stop = tag;
     over = true;
   }
   return __any_sync(0xffffffffu, over);
 }
 template <int D>
-__device__ __forceinline__ void await(const uint64_t* row, float2 (&f)[D / 64], unsigned int tag, unsigned int* error) {
+__device__ __forceinline__ void await(const StatesArgs& a, const uint64_t* row, float2 (&f)[D / 64], unsigned int tag) {
   uint64_t since = 0;
   for (int tries = 0; !__all_sync(0xffffffffu, look<D>(row, f, tag)); ++tries)
-    if (tries >= 64 && give_up(since, error)) return;
+    if (tries >= 64 && give_up(since, a, tag)) return;
 }
 
 // What comes into a chunk from its n > 0 neighbours on one side, `step` apart: the lane's sums x,
 // and z (Z). own, in: this chunk's rows.
 template <int D>
-__device__ __forceinline__ float come_in(const uint64_t* own, const uint64_t* in, int n, long long step, unsigned int tag,
-                                         unsigned int* error, float2 (&x)[D / 64]) {
+__device__ __forceinline__ float come_in(const StatesArgs& a, const uint64_t* own, const uint64_t* in, int n, long long step,
+                                         unsigned int tag, float2 (&x)[D / 64]) {
   constexpr int kP = D / 64;
   const int lane = threadIdx.x & 31, d = chain_reach(n);
   // a neighbour per lane: its z and the product of its alphas
@@ -245,7 +252,7 @@ __device__ __forceinline__ float come_in(const uint64_t* own, const uint64_t* in
   for (int tries = 0;; ++tries) {
     const bool there = lane >= d || look_zp<D>(own + (lane + 1) * step, zp, tag);
     if (__all_sync(0xffffffffu, there)) break;
-    if (tries >= 64 && give_up(since, error)) break;
+    if (tries >= 64 && give_up(since, a, tag)) break;
   }
   float upto = zp.y;  // the product of the nearest lane + 1
 #pragma unroll
@@ -260,9 +267,9 @@ __device__ __forceinline__ float come_in(const uint64_t* own, const uint64_t* in
   for (int i = 0; i < kP; ++i) x[i] = both(0.f);
   if (!end && d < n) {
     float2 zi;
-    await<D>(in + d * step, x, tag, error);
+    await<D>(a, in + d * step, x, tag);
     for (int tries = 0; !__all_sync(0xffffffffu, look_zp<D>(in + d * step, zi, tag)); ++tries)
-      if (tries >= 64 && give_up(since, error)) break;
+      if (tries >= 64 && give_up(since, a, tag)) break;
     z = zi.x;
   }
   float2 o[kP], next[kP];
@@ -271,7 +278,7 @@ __device__ __forceinline__ float come_in(const uint64_t* own, const uint64_t* in
   for (int i = far; i > 0; --i) {
     bool soon = true;
     if (i > 1) soon = look<D>(own + (i - 1) * step, next, tag);
-    if (!__all_sync(0xffffffffu, there)) await<D>(own + i * step, o, tag, error);
+    if (!__all_sync(0xffffffffu, there)) await<D>(a, own + i * step, o, tag);
     const float zo = __shfl_sync(0xffffffffu, zp.x, i - 1), prod = __shfl_sync(0xffffffffu, zp.y, i - 1);
 #pragma unroll
     for (int k = 0; k < kP; ++k) {
@@ -306,7 +313,7 @@ __global__ void __launch_bounds__(32) states_kernel(const StatesArgs a) {
   turn.index = __shfl_sync(0xffffffffu, turn.index, 0);
   turn.tag = __shfl_sync(0xffffffffu, turn.tag, 0);
   const int which = turn.index & 1, h = (turn.index >> 1) % a.Hkv, chunk = (turn.index >> 1) / a.Hkv;  // which: 0 k, 1 v
-  if (turn.index == 0) check_seqs(a.seqs, a.error);
+  if (turn.index == 0) check_seqs(a, turn.tag);
   const Piece p = find_piece(a.seqs, kC, chunk);
   if (!p.ok) {
     if (lane == 0) leave(a, turn);
@@ -359,7 +366,7 @@ __global__ void __launch_bounds__(32) states_kernel(const StatesArgs a) {
 #pragma unroll
   for (int i = 0; i < R::kP; ++i) sum[i] = both(0.f);
   if (p.at > 0) {
-    zin = come_in<D>(a.sums + row, a.carry + row, p.at, -row_step, turn.tag, a.error, sum);
+    zin = come_in<D>(a, a.sums + row, a.carry + row, p.at, -row_step, turn.tag, sum);
     if (goes_on && asked_for(p.at, prod)) {
       publish<R::kE>(a.carry + row, sum, turn.tag);
       if (lane == 0) publish_zp<D>(a.carry + row, zin, 0.f, turn.tag);
@@ -425,7 +432,7 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
   __syncthreads();
   const Turn turn = sh.turn;
   const int chunks = gridDim.x / a.Hkv, h = turn.index % a.Hkv, chunk = chunks - 1 - turn.index / a.Hkv;
-  if (turn.index == 0) check_seqs(a.seqs, a.error);
+  if (turn.index == 0) check_seqs(a, turn.tag);
   const Piece p = find_piece(a.seqs, kC, chunk);
   if (!p.ok) {
     if (threadIdx.x == 0) leave(a, turn);
@@ -540,7 +547,7 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
 #pragma unroll
   for (int i = 0; i < R::kP; ++i) in[i] = both(0.f);
   if (after > 0) {
-    zin = come_in<D>(a.sums + row, a.carry + row, after, row_step, turn.tag, a.error, in);
+    zin = come_in<D>(a, a.sums + row, a.carry + row, after, row_step, turn.tag, in);
     if (p.at > 0 && asked_for(after, prod_all)) {
       publish<R::kE>(a.carry + row, in, turn.tag);
       if (lane == 0) publish_zp<D>(a.carry + row, zin, 0.f, turn.tag);

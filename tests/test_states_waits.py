@@ -12,7 +12,9 @@ import pytest
 import torch
 
 from retrofit_harness import OFFSET, TEMPERATURE, cu_of, handle, on, states_inputs
+from paper_2403_09636_gb300 import DMC_FAULT_BAD_SEQLENS, DMC_FAULT_BAD_TARGET
 from paper_2403_09636_gb300 import build as B
+from paper_2403_09636_gb300.retrofit import DmcRetrofit
 
 
 def source():
@@ -121,3 +123,34 @@ def test_a_gate_that_is_not_a_number(cuda_dev, dtype, where, merge):
         for t in (a, b):
             t[700:2200, head] = 0.0
         assert torch.equal(a, b), name
+
+
+# ---------------------------------------------------------------- faults of earlier calls
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fault", ["target", "seqlens"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_fault_of_an_earlier_call_changes_nothing(cuda_dev, dtype, fault):
+    """A sticky bit (a target beyond the vocabulary, faulty cu_seqlens) says what happened; later calls give what a fresh
+    handle's give, long waits along the chain among them."""
+    lens, heads = [16384], (2, 2, 64)
+    d = on(long_inputs(lens, heads, dtype, True), cuda_dev)
+    cu = cu_of(lens, cuda_dev)
+
+    def both():
+        return DmcRetrofit(*heads, dtype=dtype, max_tokens=sum(lens), max_seqs=2, hidden=64, vocab=50, device=cuda_dev)
+
+    want = run_states(both(), d, cu, max(lens))
+    h = both()
+    if fault == "target":
+        h.loss(torch.zeros(3, 64, dtype=dtype, device=cuda_dev), torch.zeros(50, 64, dtype=dtype, device=cuda_dev),
+               torch.tensor([1, 50, 2], dtype=torch.int32, device=cuda_dev))
+    else:
+        run_states(h, d, torch.tensor([0, 9000, 8000], dtype=torch.int32, device=cuda_dev), max(lens))
+    bits = h.status()[1]
+    assert bits == (DMC_FAULT_BAD_TARGET if fault == "target" else DMC_FAULT_BAD_SEQLENS)
+    for _ in range(5):
+        got = run_states(h, d, cu, max(lens))
+        for name in got:
+            assert torch.equal(got[name], want[name]), name
+    assert h.status()[1] == bits
