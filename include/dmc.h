@@ -252,8 +252,10 @@ dmc_status dmc_cache_status(dmc_cache_t cache, cudaStream_t stream, uint32_t* bi
  * intermediate state of a slot stays visible to the queries of its time:
  *   alpha_t = sigmoid((k_t[0] - offset + noise_t) / temperature)   (Gumbel-sigmoid:
  *             logistic noise, offset 5 and temperature 0.1 in the paper)
- *   omega_t = sigmoid(q_t[0])      (grouped queries: of the group's mean q[0])
- *   z_t  = alpha_t z_{t-1} + omega_t
+ *   omega_t = sigmoid(q_t[0])      (grouped queries: of the group's mean q[0]; one below
+ *             -110.9 counts as that, without a gradient)
+ *   z_t  = alpha_t z_{t-1} + omega_t   (across chunks of 32 tokens, products of alphas
+ *             below 2^-126 count as zero)
  *   k~_t = (alpha_t z_{t-1} k~_{t-1} + omega_t k_t) / z_t, v~_t alike, k_t[0] = 0
  * (Eq. partial-accumulation; the first token of a sequence has alpha = 0), and the
  * queries of token i see the states j <= i with the additive mask

@@ -48,9 +48,15 @@ __host__ __device__ constexpr int sums_row(int D) { return 2 * D + kPad; }
 
 // A token's gates, one token per lane; beyond the chunk's end the identity of the recurrence.
 struct Gate {
-  float alpha, rest, omega;  // rest: 1 - alpha
-  float log_rest;
+  float alpha, rest, omega;  // rest: 1 - alpha; omega in units of 1 / kUnit
+  float log_rest, slope;     // slope: of log(omega)
 };
+
+// Only ratios of the weights omega count, so they are kept larger by a power of two: sums of sigmoids
+// far below the smallest fp32 number keep their bits, and those of others have the bits they have without. A
+// mean of q[0] below kLeast counts as that, with 2^28 between the largest 1 / z and fp32's range.
+constexpr float kUnit = 1152921504606846976.f;  // 2^60
+constexpr float kLeast = -110.9f;               // omega kUnit = 2^-100
 
 template <typename T>
 __device__ __forceinline__ float element(const void* p, long long i) {
@@ -70,13 +76,38 @@ __device__ __forceinline__ GateIn gate_in(const StatesArgs& a, int h, int tok, b
   for (int j = 0; j < a.G; ++j) g.q += element<T>(a.q, (long long)tok * a.q_tok + (long long)(h * a.G + j) * a.q_head);
   return g;
 }
-__device__ __forceinline__ Gate gate_of(const StatesArgs& a, GateIn v, bool in, bool first) {
+// kUnit e^m for a mean m of the group's q[0] far below zero, as a product of numbers in range. The mean is taken again
+// with what its sum and quotient round off: half a unit in the last place of -100 is 4e-6 of the weight.
+template <typename T>
+__device__ __noinline__ float small_omega(const StatesArgs& a, int h, int tok) {
+  float sum = 0.f, rest = 0.f;
+  for (int j = 0; j < a.G; ++j) {
+    const float x = element<T>(a.q, (long long)tok * a.q_tok + (long long)(h * a.G + j) * a.q_head);
+    const float to = sum + x, of_x = to - sum;
+    rest += (sum - (to - of_x)) + (x - of_x);
+    sum = to;
+  }
+  const float m = sum / (float)a.G;
+  if (m < kLeast) return 7.88860905e-31f;  // 2^-100
+  rest = (fmaf(-m, (float)a.G, sum) + rest) / (float)a.G;
+  const float root = expf(0.5f * m);
+  return root * kUnit * root * (1.f + rest);
+}
+template <typename T>
+__device__ __forceinline__ Gate gate_of(const StatesArgs& a, GateIn v, int h, int tok, bool in, bool first) {
   Gate g;
   g.alpha = 1.f;
-  g.rest = g.omega = g.log_rest = 0.f;
+  g.rest = g.omega = g.log_rest = g.slope = 0.f;
   if (!in) return g;
   const float x = (v.k - a.offset + v.noise) / a.temperature;
-  g.omega = 1.f / (1.f + expf(-v.q / (float)a.G));
+  const float m = v.q / (float)a.G;
+  if (m < -80.f) {
+    g.omega = small_omega<T>(a, h, tok);
+    g.slope = m < kLeast ? 0.f : 1.f;
+  } else {
+    g.omega = kUnit / (1.f + expf(-m));
+    g.slope = 1.f - g.omega * (1.f / kUnit);
+  }
   // both sides from the exponential that does not overflow
   const float e = expf(-fabsf(x)), big = 1.f / (1.f + e), small = e / (1.f + e);
   g.alpha = x >= 0.f ? big : small;
@@ -327,7 +358,7 @@ __global__ void __launch_bounds__(32) states_kernel(const StatesArgs a) {
   if (lane == 0) mbar_arrive_expect_tx(smem_u32(&loaded), n * D * sizeof(T));
   __syncwarp();
   load_chunk<T, D>(rows, static_cast<const T*>(which ? a.v : a.k) + at, step, n, smem_u32(&loaded));
-  const Gate g = gate_of(a, gi, in_chunk, tok == p.t0);
+  const Gate g = gate_of<T>(a, gi, h, tok, in_chunk, tok == p.t0);
   const long long row = row_of<D>(a, chunk, h, which), row_step = row_of<D>(a, 1, 0, 0);
   float after = g.alpha;  // product of the alphas from the token on
 #pragma unroll
@@ -469,7 +500,7 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
     dbias = element<T>(a.dbias, i - 1);
     if (a.dalpha) dalpha = a.dalpha[i];
   }
-  const Gate g = gate_of(a, gi, in_chunk, tok == p.t0);
+  const Gate g = gate_of<T>(a, gi, h, tok, in_chunk, tok == p.t0);
   const float z = scan_z(g.alpha, g.omega, zbefore0), rz = 1.f / z;
   float prod = g.alpha;  // of the alphas up to the token
 #pragma unroll
@@ -632,7 +663,7 @@ __global__ void __launch_bounds__(64) states_backward_kernel(const StatesArgs a)
     if (tok > p.t0) dx = (dalpha * g.alpha * g.rest - dbias * g.alpha) / a.temperature;
     // over what lane 0 has written there
     static_cast<T*>(a.dk)[((long long)tok * a.Hkv + h) * D] = Elt<T>::from_f(dx);
-    const T dq = Elt<T>::from_f(domega * g.omega * (1.f - g.omega) / (float)a.G);
+    const T dq = Elt<T>::from_f(domega * g.omega * g.slope / (float)a.G);
     for (int j = 0; j < a.G; ++j)
       static_cast<T*>(a.dq)[(long long)tok * a.dq_tok + (long long)(h * a.G + j) * a.dq_head] = dq;
   }
