@@ -362,7 +362,9 @@ dmc_status dmc_retrofit_attention(dmc_retrofit_t h, int32_t num_seqs, const void
  * gradients are summed over its group. dbias_dev (written unless it or bias_dev is
  * NULL): [num_kv_heads, total_tokens] in the handle's dtype, as the other gradients.
  * In bf16, weights and the scores' gradients are rounded to bf16 for their products;
- * dbias is summed from the unrounded ones. Nothing is accumulated into. */
+ * dbias is summed from the unrounded ones. Nothing is accumulated into. In bf16 calls with
+ * max_seqlen up to 384 a sequence's gradients do not depend on the others to the bit; in
+ * longer ones, and in fp32, dk, dv and dbias may be added up in another order in another call. */
 dmc_status dmc_retrofit_attention_backward(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev,
                                            const void* k_dev, const void* v_dev,
                                            const float* bias_dev, const void* out_dev,

@@ -901,8 +901,10 @@ cudaError_t backward(AttnArgs a, cudaStream_t stream) {
   const int tiles = row_tiles(a);
   long long dkv_items = (long long)tiles * a.Hkv, dq_items = (long long)tiles * a.Hq;
   if (dq_items > INT_MAX / 2) return cudaErrorInvalidValue;
-  // Sequences of up to three tiles have the same gradients to the bit whatever company they are in: no
-  // shares for them, which would save up to a quarter (two of 300 tokens, 64 / 8 heads, 82 us, 60 in shares).
+  // Calls of sequences of up to three tiles (by their max_seqlen) are not split: there a sequence has the same
+  // gradients to the bit alone and in any company, a long pack among them. Shares would save up to a quarter (two of
+  // 300 tokens, 64 / 8 heads, 82 us, 59 in shares). Whole groups for the short sequences of any other call would hold
+  // for those, too, but set its time (300 and 700 tokens, 64 / 8 heads: 96 us, 121 so; 385 and 384, 7 / 1: 45, 74).
   a.shares = a.seqs.longest > 3 * kR ? attn_shares(dkv_items, a.G) : 1;
   if (!kBias) a.dbias = nullptr;
   dkv_items *= a.shares;
