@@ -269,7 +269,9 @@ dmc_status dmc_cache_status(dmc_cache_t cache, cudaStream_t stream, uint32_t* bi
  * depends on the order in which blocks run. fp32 products on the tensor cores (the
  * loss, and attention of calls that fill the GPU) take an operand's 24 bits as three
  * bf16 numbers: an infinite one gives NaN, one below 2^-110 loses its last bits.
- * All calls on one handle must be ordered on the GPU: they share its scratch. Calls allocate nothing and can be captured.
+ * All calls on one handle must be ordered on the GPU: they share its scratch. Calls allocate nothing and can be
+ * captured. A handle belongs to the device that was current when it was created: with another current one its calls
+ * return DMC_ERR_INVALID_ARG.
  * ------------------------------------------------------------------------ */
 
 typedef struct {

@@ -195,9 +195,15 @@ struct dmc_retrofit {
 
 namespace {
 
+// A handle whose device is the current one: kernels go there, whatever the stream's number means elsewhere.
+bool usable(dmc_retrofit_t h) {
+  int dev = 0;
+  return h && cudaGetDevice(&dev) == cudaSuccess && dev == h->device;
+}
+
 // What every call on sequences checks. 1: go on, 0: nothing to do, -1: refused.
 int seqs_arg(dmc_retrofit_t h, int32_t num_seqs, const int32_t* cu, int32_t total, int32_t longest) {
-  if (!h || !dmc::has_heads(h->cfg)) return -1;
+  if (!usable(h) || !dmc::has_heads(h->cfg)) return -1;
   if (num_seqs < 0 || num_seqs > h->cfg.max_seqs || total < 0 || total > h->cfg.max_tokens) return -1;
   if (longest < 0 || longest > total) return -1;
   if (num_seqs == 0 || total == 0) return 0;
@@ -290,7 +296,13 @@ dmc_status dmc_retrofit_create(const dmc_retrofit_config* cfg, void* arena_dev, 
   h->cfg = *cfg;
   h->at = o;
   h->base = static_cast<char*>(arena_dev);
+  cudaPointerAttributes where;
   cudaError_t e = cudaGetDevice(&h->device);
+  if (e == cudaSuccess) e = cudaPointerGetAttributes(&where, arena_dev);
+  if (e == cudaSuccess && where.type == cudaMemoryTypeDevice && where.device != h->device) {
+    delete h;
+    return DMC_ERR_INVALID_ARG;  // another device's memory
+  }
   if (e == cudaSuccess) e = cudaMemsetAsync(h->base + o.error, 0, o.cleared - o.error, stream);
   if (e != cudaSuccess) {
     delete h;
@@ -407,7 +419,7 @@ dmc_status dmc_retrofit_attention_backward(dmc_retrofit_t h, int32_t num_seqs, c
 
 dmc_status dmc_retrofit_loss(dmc_retrofit_t h, int32_t num_tokens, const void* hidden_dev, const void* weight_dev,
                              const int32_t* targets_dev, float* loss_dev, float* lse_dev, cudaStream_t stream) {
-  if (!h || !dmc::has_loss(h->cfg) || num_tokens < 0 || num_tokens > h->cfg.max_tokens) return DMC_ERR_INVALID_ARG;
+  if (!usable(h) || !dmc::has_loss(h->cfg) || num_tokens < 0 || num_tokens > h->cfg.max_tokens) return DMC_ERR_INVALID_ARG;
   if (num_tokens == 0) return DMC_OK;
   if (!dmc::given16(hidden_dev) || !dmc::given16(weight_dev) || !dmc::given4(targets_dev) || !dmc::given4(loss_dev) ||
       !dmc::given4(lse_dev))
@@ -425,7 +437,7 @@ dmc_status dmc_retrofit_loss_backward(dmc_retrofit_t h, int32_t num_tokens, cons
                                       const void* weight_dev, const int32_t* targets_dev, const float* lse_dev,
                                       const float* dloss_dev, void* dhidden_dev, void* dweight_dev,
                                       cudaStream_t stream) {
-  if (!h || !dmc::has_loss(h->cfg) || num_tokens < 0 || num_tokens > h->cfg.max_tokens) return DMC_ERR_INVALID_ARG;
+  if (!usable(h) || !dmc::has_loss(h->cfg) || num_tokens < 0 || num_tokens > h->cfg.max_tokens) return DMC_ERR_INVALID_ARG;
   if (!dmc::given16(dweight_dev)) return DMC_ERR_INVALID_ARG;
   if (num_tokens == 0)  // no token: no gradient
     return dmc::cuda_status(cudaMemsetAsync(
@@ -442,7 +454,7 @@ dmc_status dmc_retrofit_loss_backward(dmc_retrofit_t h, int32_t num_tokens, cons
 }
 
 dmc_status dmc_retrofit_status(dmc_retrofit_t h, cudaStream_t stream, uint32_t* bits) {
-  if (!h) return DMC_ERR_INVALID_ARG;
+  if (!usable(h)) return DMC_ERR_INVALID_ARG;
   uint32_t b = 0;
   cudaError_t e = cudaStreamSynchronize(stream);
   if (e == cudaSuccess) e = cudaMemcpy(&b, h->base + h->at.error, 4, cudaMemcpyDeviceToHost);

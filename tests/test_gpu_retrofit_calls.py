@@ -1,0 +1,56 @@
+"""What the retrofitting calls refuse beside shapes and types: another device than the handle's."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2403_09636_gb300 as P
+from paper_2403_09636_gb300.retrofit import DmcRetrofit
+from retrofit_harness import attention_inputs, cu_of, handle, on, states_inputs
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+LENS, HEADS = [40, 24], (4, 2, 64)
+
+
+@pytest.fixture(scope="module")
+def ready():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    dev = torch.device("cuda:0")
+    x, s = on(attention_inputs(LENS, *HEADS, BF16), dev), on(states_inputs(LENS, *HEADS, BF16), dev)
+    return x, s, cu_of(LENS, dev), dev
+
+
+def both(dev):
+    return DmcRetrofit(*HEADS, dtype=BF16, max_tokens=sum(LENS), max_seqs=2, hidden=64, vocab=50, device=dev)
+
+
+def test_another_device_than_the_handles(ready):
+    """A handle that says it belongs to another device than the current one (the number behind its config is
+    changed for that): every call refuses before it launches anything."""
+    x, s, cu, dev = ready
+    h = both(dev)
+    saved = h.states(s["q0"], s["k"], s["v"], cu, 40)[-1]
+    o, lse = h.attention(x["q"], x["k"], x["v"], cu, 40)
+    hid, w = torch.zeros(8, 64, dtype=BF16, device=dev), torch.zeros(50, 64, dtype=BF16, device=dev)
+    t, f = torch.zeros(8, dtype=torch.int32, device=dev), torch.zeros(8, device=dev)
+    device = C.c_int.from_address(h.handle + C.sizeof(P.dmc_retrofit_config))
+    assert device.value == torch.cuda.current_device()
+    calls = [lambda: h.states(s["q0"], s["k"], s["v"], cu, 40),
+             lambda: h.states_backward(s["q0"], s["k"], s["v"], cu, 40, saved, s["dkt"], s["dvt"], s["dbias"]),
+             lambda: h.attention(x["q"], x["k"], x["v"], cu, 40),
+             lambda: h.attention_backward(x["dout"], x["q"], x["k"], x["v"], o, lse, cu, 40),
+             lambda: h.loss(hid, w, t), lambda: h.loss_backward(f, hid, w, t, f)]
+    for call in calls:
+        call()
+    device.value += 1
+    try:
+        for i, call in enumerate(calls):
+            with pytest.raises(P.DmcError) as e:
+                call()
+            assert e.value.status == P.DMC_ERR_INVALID_ARG, i
+        assert h.status()[0] == P.DMC_ERR_INVALID_ARG
+    finally:
+        device.value -= 1
+    assert h.status() == (0, 0)
