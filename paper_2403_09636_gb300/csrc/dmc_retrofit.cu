@@ -274,6 +274,8 @@ dmc::LossArgs loss_args(dmc_retrofit_t h, int32_t n, const void* hidden, const v
 }
 
 bool bf16(dmc_retrofit_t h) { return h->cfg.dtype == DMC_BF16; }
+// an address of elements of the handle's type
+bool given(dmc_retrofit_t h, const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & (bf16(h) ? 1u : 3u)) == 0; }
 
 }  // namespace
 
@@ -333,7 +335,7 @@ dmc_status dmc_retrofit_states(dmc_retrofit_t h, int32_t num_seqs, const void* q
   const int go = seqs_arg(h, num_seqs, cu_seqlens_dev, total_tokens, max_seqlen);
   if (go < 0 || !(temperature > 0.f) || !isfinite(temperature) || !isfinite(offset)) return DMC_ERR_INVALID_ARG;
   if (go == 0) return DMC_OK;
-  if (!q_dev || q_token_stride < 0 || q_head_stride < 0 || !dmc::given16(k_dev) || !dmc::given16(v_dev) ||
+  if (!given(h, q_dev) || q_token_stride < 0 || q_head_stride < 0 || !dmc::given16(k_dev) || !dmc::given16(v_dev) ||
       !dmc::given16(kt_dev) || !dmc::given16(vt_dev) || !dmc::given4(alpha_dev) || !dmc::given4(bias_dev) ||
       !dmc::given16(saved_dev) || (noise_dev && !dmc::given4(noise_dev)))
     return DMC_ERR_INVALID_ARG;
@@ -357,11 +359,13 @@ dmc_status dmc_retrofit_states_backward(dmc_retrofit_t h, int32_t num_seqs, cons
   const int go = seqs_arg(h, num_seqs, cu_seqlens_dev, total_tokens, max_seqlen);
   if (go < 0 || !(temperature > 0.f) || !isfinite(temperature) || !isfinite(offset)) return DMC_ERR_INVALID_ARG;
   if (go == 0) return DMC_OK;
-  if (!q_dev || q_token_stride < 0 || q_head_stride < 0 || !dmc::given16(k_dev) || !dmc::given16(v_dev) ||
+  if (!given(h, q_dev) || q_token_stride < 0 || q_head_stride < 0 || !dmc::given16(k_dev) || !dmc::given16(v_dev) ||
       !dmc::given16(saved_dev) || (noise_dev && !dmc::given4(noise_dev)) || !dmc::given16(dkt_dev) ||
-      !dmc::given16(dvt_dev) || !dbias_dev || (dalpha_dev && !dmc::given4(dalpha_dev)) || !dq_dev ||
+      !dmc::given16(dvt_dev) || !given(h, dbias_dev) || (dalpha_dev && !dmc::given4(dalpha_dev)) || !given(h, dq_dev) ||
       dq_token_stride < 0 || dq_head_stride < 0 || !dmc::given16(dk_dev) || !dmc::given16(dv_dev))
     return DMC_ERR_INVALID_ARG;
+  // what is written may not lie in one place
+  if ((dq_token_stride == 0 && total_tokens > 1) || (dq_head_stride == 0 && h->cfg.num_q_heads > 1)) return DMC_ERR_INVALID_ARG;
   dmc::StatesArgs a = states_args(h, num_seqs, q_dev, q_token_stride, q_head_stride, k_dev, v_dev, noise_dev, offset,
                                   temperature, cu_seqlens_dev, total_tokens, max_seqlen, const_cast<void*>(saved_dev));
   a.dkt = dkt_dev;
@@ -403,7 +407,7 @@ dmc_status dmc_retrofit_attention_backward(dmc_retrofit_t h, int32_t num_seqs, c
   if (go == 0) return DMC_OK;
   if (!dmc::given16(q_dev) || !dmc::given16(k_dev) || !dmc::given16(v_dev) || !dmc::given16(out_dev) ||
       !dmc::given4(lse_dev) || (bias_dev && !dmc::given4(bias_dev)) || !dmc::given16(dout_dev) ||
-      !dmc::given16(dq_dev) || !dmc::given16(dk_dev) || !dmc::given16(dv_dev))
+      !dmc::given16(dq_dev) || !dmc::given16(dk_dev) || !dmc::given16(dv_dev) || (dbias_dev && !given(h, dbias_dev)))
     return DMC_ERR_INVALID_ARG;
   dmc::AttnArgs a = attn_args(h, num_seqs, q_dev, k_dev, v_dev, bias_dev, cu_seqlens_dev, total_tokens, max_seqlen);
   a.out = const_cast<void*>(out_dev);

@@ -1,4 +1,5 @@
-"""What the retrofitting calls refuse beside shapes and types: another device than the handle's."""
+"""What the retrofitting calls refuse beside shapes and types: another device than the handle's, addresses that are
+not aligned to their elements, outputs that lie in one place."""
 import ctypes as C
 
 import pytest
@@ -54,3 +55,28 @@ def test_another_device_than_the_handles(ready):
     finally:
         device.value -= 1
     assert h.status() == (0, 0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+def test_addresses_that_are_not_their_elements(ready, dtype):
+    """q's and dq's first components may lie anywhere, but on whole elements; dbias too."""
+    _, _, cu, dev = ready
+    size = 4 if dtype == torch.float32 else 2
+    h = handle(dev, *HEADS, dtype, LENS)
+    buf = torch.zeros(1 << 20, dtype=torch.uint8, device=dev)
+    p, T = buf.data_ptr(), 64
+
+    def states(q=p):
+        return P.dmc_retrofit_states(h.handle, 2, q, 4, 1, p, p, None, 5.0, 0.1, cu.data_ptr(), T, 40, p, p, p, p, p, 0)
+
+    def states_backward(q=p, dq=p, db=p, st=4, sh=1):
+        return P.dmc_retrofit_states_backward(h.handle, 2, q, 4, 1, p, p, None, 5.0, 0.1, cu.data_ptr(), T, 40, p, p, p, db,
+                                              None, dq, st, sh, p, p, 0)
+
+    def attention_backward(db):
+        return P.dmc_retrofit_attention_backward(h.handle, 2, p, p, p, p, p, p, p, cu.data_ptr(), T, 40, p, p, p, db, 0)
+
+    bad = p + size // 2
+    assert states(q=bad) == states_backward(q=bad) == states_backward(dq=bad) == P.DMC_ERR_INVALID_ARG
+    assert states_backward(db=bad) == attention_backward(bad) == P.DMC_ERR_INVALID_ARG
+    assert states_backward(st=0) == states_backward(sh=0) == P.DMC_ERR_INVALID_ARG  # tokens, heads in one place
