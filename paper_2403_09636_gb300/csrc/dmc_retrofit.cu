@@ -32,6 +32,10 @@ dmc_status cuda_status(cudaError_t e) { return e == cudaSuccess ? DMC_OK : DMC_E
 bool has_heads(const dmc_retrofit_config& c) { return c.num_q_heads > 0; }
 bool has_loss(const dmc_retrofit_config& c) { return c.hidden > 0; }
 
+// Elements of the largest tensor of a call that a handle may be made for, beyond any memory: so sizes of scratch
+// stay far below 64 bits.
+constexpr int64_t kMostElements = 1ll << 48;
+
 bool valid(const dmc_retrofit_config* c) {
   if (!c) return false;
   if (c->dtype != DMC_F32 && c->dtype != DMC_BF16) return false;
@@ -40,10 +44,12 @@ bool valid(const dmc_retrofit_config* c) {
     if (c->num_q_heads < 1 || c->num_kv_heads < 1 || c->num_q_heads % c->num_kv_heads != 0) return false;
     if (c->num_q_heads / c->num_kv_heads > 32 || c->num_q_heads > 65535) return false;
     if (c->head_dim != 64 && c->head_dim != 128) return false;
+    if (((int64_t)c->max_tokens + c->max_seqs) * c->num_q_heads * c->head_dim > kMostElements) return false;
   }
   if (c->hidden != 0 || c->vocab != 0) {
     if (c->hidden < 1 || c->vocab < 1 || c->vocab > (1 << 30)) return false;
     if ((int64_t)c->hidden * (c->dtype == DMC_F32 ? 4 : 2) % 16 != 0) return false;
+    if ((int64_t)c->hidden * c->max_tokens > kMostElements || (int64_t)c->hidden * c->vocab > kMostElements) return false;
   }
   return has_heads(*c) || has_loss(*c);
 }
@@ -67,7 +73,6 @@ Offsets offsets(const dmc_retrofit_config* c) {
   Offsets o = {};
   size_t at = 0;
   const size_t tokens = c->max_tokens;
-  const size_t chunks = has_heads(*c) ? (size_t)pieces(c->max_tokens, c->max_seqs, kStateChunk) * c->num_kv_heads : 0;
   o.error = at; at = align_up(at + kControl);
   if (has_heads(*c)) {
     const size_t sums = (size_t)pieces(c->max_tokens, c->max_seqs, kStateChunk) * c->num_kv_heads * 2 * (c->head_dim + 2) * 8;
