@@ -7,7 +7,7 @@ entropy against a vocabulary whose logits are never kept, each with its gradient
 Arguments are checked (type, shape, device, contiguity) and refused with ValueError;
 statuses of the library become DmcError.
 
-`attention` and `cross_entropy` are the same as autograd functions:
+`attention` and `cross_entropy` are the same as autograd functions (second derivatives are refused):
 
     dmc = DmcRetrofit(32, 32, 128, torch.bfloat16, max_tokens=8192, max_seqs=4, hidden=4096, vocab=32000)
     out, alpha = attention(dmc, q, k, v, cu_seqlens, max_seqlen, noise=noise)
@@ -17,6 +17,7 @@ statuses of the library become DmcError.
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import (DMC_BF16, DMC_ERR_INVALID_ARG, DMC_F32, DmcError, _check, dmc_retrofit_config, dmc_retrofit_create,
                dmc_retrofit_destroy, dmc_retrofit_required_bytes, dmc_retrofit_saved_bytes, dmc_retrofit_status, lib)
@@ -245,27 +246,30 @@ class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, dmc, q, k, v, cu_seqlens, max_seqlen, noise, offset, temperature):
         q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
-        gates = {"noise": noise, "offset": offset, "temperature": temperature}
-        kt, vt, alpha, bias, saved = dmc.states(q[..., 0], k, v, cu_seqlens, max_seqlen, **gates)
+        gates = {"offset": offset, "temperature": temperature}
+        kt, vt, alpha, bias, saved = dmc.states(q[..., 0], k, v, cu_seqlens, max_seqlen, noise, **gates)
         o, lse = dmc.attention(q, kt, vt, cu_seqlens, max_seqlen, bias)
-        ctx.save_for_backward(q, k, v, kt, vt, bias, saved, o, lse, cu_seqlens)
+        ctx.save_for_backward(q, k, v, kt, vt, bias, saved, o, lse, cu_seqlens, noise)
         ctx.dmc, ctx.max_seqlen, ctx.gates = dmc, max_seqlen, gates
         return o, alpha
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do, dalpha):
-        q, k, v, kt, vt, bias, saved, o, lse, cu = ctx.saved_tensors
+        q, k, v, kt, vt, bias, saved, o, lse, cu, noise = ctx.saved_tensors
         dmc, longest = ctx.dmc, ctx.max_seqlen
         dq, dkt, dvt, dbias = dmc.attention_backward(do.contiguous(), q, kt, vt, o, lse, cu, longest, bias)
         dk, dv = torch.empty_like(k), torch.empty_like(v)
-        dmc.states_backward(q[..., 0], k, v, cu, longest, saved, dkt, dvt, dbias, dalpha.contiguous(), **ctx.gates,
+        dmc.states_backward(q[..., 0], k, v, cu, longest, saved, dkt, dvt, dbias, dalpha.contiguous(), noise, **ctx.gates,
                             out=(dq[..., 0], dk, dv))
-        return None, dq, dk, dv, None, None, None, None, None
+        # the noise is added to k's first component
+        dnoise = dk[..., 0].t().float() if ctx.needs_input_grad[6] else None
+        return None, dq, dk, dv, None, None, dnoise, None, None
 
 
 def attention(dmc, q, k, v, cu_seqlens, max_seqlen, noise=None, offset=5.0, temperature=0.1):
-    """DMC's training attention of packed sequences, differentiable in q, k and v: (out [T, Hq, D],
-    alpha [Hkv, T]). The first components of q and k are the gates, as at inference."""
+    """DMC's training attention of packed sequences, differentiable (once) in q, k, v and noise: (out
+    [T, Hq, D], alpha [Hkv, T]). The first components of q and k are the gates, as at inference."""
     return _Attention.apply(dmc, q, k, v, cu_seqlens, int(max_seqlen), noise, float(offset), float(temperature))
 
 
@@ -279,12 +283,13 @@ class _CrossEntropy(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dloss):
         hidden, weight, targets, lse = ctx.saved_tensors
         return None, *ctx.dmc.loss_backward(dloss.float().contiguous(), hidden, weight, targets, lse), None
 
 
 def cross_entropy(dmc, hidden, weight, targets):
-    """Each position's cross entropy (fp32 [N], 0 where the target is below 0), differentiable in
+    """Each position's cross entropy (fp32 [N], 0 where the target is below 0), differentiable (once) in
     hidden and weight."""
     return _CrossEntropy.apply(dmc, hidden, weight, targets)
