@@ -29,8 +29,9 @@ class DmcRetrofit:
     """Scratch and entry points of the retrofitting operators for one shape of heads and
     (or) one vocabulary. Calls on one handle must be ordered on the GPU.
 
-    Outputs are new tensors, or those given as `out` (a tuple in the order of the
-    results). Tensors must be contiguous and on the handle's device; q0 may be strided."""
+    Outputs are new tensors of the call's stream, the current one unless `stream` names another, or those
+    given as `out` (a tuple in the order of the results). Tensors must be contiguous and on the handle's device; q0
+    may be strided."""
 
     def __init__(self, num_q_heads=0, num_kv_heads=0, head_dim=0, dtype=torch.bfloat16, max_tokens=0, max_seqs=1,
                  hidden=0, vocab=0, device=None, stream=None):
@@ -47,16 +48,25 @@ class DmcRetrofit:
         self.nbytes = dmc_retrofit_required_bytes(self.cfg)
         if self.nbytes == 0:
             raise DmcError(DMC_ERR_INVALID_ARG, "dmc_retrofit_required_bytes")
-        self.arena = torch.empty(self.nbytes, dtype=torch.uint8, device=self.device)
+        self.arena = self._maker(stream)((self.nbytes,), torch.uint8)
+        self._streams = {self._raw(stream)}  # that the arena's memory waits for when it is given up
         st, self.handle = dmc_retrofit_create(self.cfg, self.arena.data_ptr(), self.nbytes, self._s(stream))
         _check(st, "dmc_retrofit_create")
         self.lib = lib()
         self._saved = {}  # floats of `saved` by (sequences, tokens)
 
-    def _s(self, stream):
+    def _raw(self, stream):
         if stream is None:
             return torch._C._cuda_getCurrentRawStream(self.index)
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+    def _s(self, stream):
+        """The number of the stream of a call."""
+        raw = self._raw(stream)
+        if raw not in self._streams:
+            self.arena.record_stream(torch.cuda.ExternalStream(raw, device=self.device))
+            self._streams.add(raw)
+        return raw
 
     def close(self):
         if getattr(self, "handle", None):
@@ -80,6 +90,19 @@ class DmcRetrofit:
 
     def _new(self, shape, dtype):
         return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _maker(self, stream):
+        """`_new`, of memory that belongs to the stream of a call: work of the current one that still uses what was
+        freed there does not run beside the call."""
+        if stream is None or self._raw(stream) == self._raw(None):
+            return self._new
+        other = torch.cuda.ExternalStream(self._raw(stream), device=self.device)
+
+        def new(shape, dtype):
+            with torch.cuda.stream(other):
+                return self._new(shape, dtype)
+
+        return new
 
     def _seqs(self, k, cu_seqlens):
         """Tokens, sequences and the pointer of cu_seqlens."""
@@ -118,7 +141,7 @@ class DmcRetrofit:
         [T, Hkv, D], noise [Hkv, T] or None; alpha and bias are fp32 [Hkv, T], saved is for the
         backward pass."""
         T, n, cu = self._seqs(k, cu_seqlens)
-        H, D, dt, check, new = self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is, self._new
+        H, D, dt, check, new = self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is, self._maker(stream)
         rows, scalars, saved = (T, H, D), (H, T), self._saved_floats(n, T)
         q = self._first("q0", q0, T)
         kp, vp = check("k", k, rows, dt), check("v", v, rows, dt)
@@ -141,7 +164,7 @@ class DmcRetrofit:
         """(dq0, dk, dv) from the states' gradients: dbias [Hkv, T] in the handle's dtype, dalpha fp32
         [Hkv, T] or None. out's dq0 may be strided (dq[..., 0] of the attention's dq)."""
         T, n, cu = self._seqs(k, cu_seqlens)
-        H, D, dt, check, new = self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is, self._new
+        H, D, dt, check, new = self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is, self._maker(stream)
         rows, scalars = (T, H, D), (H, T)
         q = self._first("q0", q0, T)
         ptrs = (check("k", k, rows, dt), check("v", v, rows, dt),
@@ -170,7 +193,8 @@ class DmcRetrofit:
         ptrs = (check("q", q, queries, dt), check("k", k, rows, dt), check("v", v, rows, dt),
                 None if bias is None else check("bias", bias, (H, T), _F32))
         if out is None:
-            out = (self._new(queries, dt), self._new((Hq, T), _F32))
+            new = self._maker(stream)
+            out = (new(queries, dt), new((Hq, T), _F32))
         o, lse = out = self._given(out, ("out", "lse"))
         st = self.lib.dmc_retrofit_attention(self.handle, n, *ptrs, cu, T, max_seqlen, check("out", o, queries, dt),
                                              check("lse", lse, (Hq, T), _F32), self._s(stream))
@@ -183,7 +207,7 @@ class DmcRetrofit:
         handle's dtype, None without a bias."""
         T, n, cu = self._seqs(k, cu_seqlens)
         Hq, H, D, dt, check = self.cfg.num_q_heads, self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is
-        queries, rows, scalars, new = (T, Hq, D), (T, H, D), (H, T), self._new
+        queries, rows, scalars, new = (T, Hq, D), (T, H, D), (H, T), self._maker(stream)
         ptrs = (check("q", q, queries, dt), check("k", k, rows, dt), check("v", v, rows, dt),
                 None if bias is None else check("bias", bias, scalars, _F32), check("o", o, queries, dt),
                 check("lse", lse, (Hq, T), _F32), check("dout", dout, queries, dt))
@@ -213,7 +237,8 @@ class DmcRetrofit:
         int32 targets [N]; below 0 a position is ignored."""
         N, ptrs = self._words(hidden, weight, targets)
         if out is None:
-            out = (self._new((N,), _F32), self._new((N,), _F32))
+            new = self._maker(stream)
+            out = (new((N,), _F32), new((N,), _F32))
         loss, lse = out = self._given(out, ("loss", "lse"))
         st = self.lib.dmc_retrofit_loss(self.handle, N, *ptrs, self._is("loss", loss, (N,), _F32),
                                         self._is("lse", lse, (N,), _F32), self._s(stream))
@@ -227,7 +252,8 @@ class DmcRetrofit:
         given = (self._is("lse", lse, (N,), _F32), self._is("dloss", dloss, (N,), _F32))
         shapes = (N, self.cfg.hidden), (self.cfg.vocab, self.cfg.hidden)
         if out is None:
-            out = (self._new(shapes[0], self.dtype), self._new(shapes[1], self.dtype))
+            new = self._maker(stream)
+            out = (new(shapes[0], self.dtype), new(shapes[1], self.dtype))
         dh, dw = out = self._given(out, ("dhidden", "dweight"))
         st = self.lib.dmc_retrofit_loss_backward(self.handle, N, *ptrs, *given, self._is("dhidden", dh, shapes[0], self.dtype),
                                                  self._is("dweight", dw, shapes[1], self.dtype), self._s(stream))

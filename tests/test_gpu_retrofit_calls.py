@@ -1,5 +1,5 @@
 """What the retrofitting calls refuse beside shapes and types: another device than the handle's, addresses that are
-not aligned to their elements, outputs that lie in one place."""
+not aligned to their elements, outputs that lie in one place; and whose memory a call on another stream uses."""
 import ctypes as C
 
 import pytest
@@ -80,3 +80,50 @@ def test_addresses_that_are_not_their_elements(ready, dtype):
     assert states(q=bad) == states_backward(q=bad) == states_backward(dq=bad) == P.DMC_ERR_INVALID_ARG
     assert states_backward(db=bad) == attention_backward(bad) == P.DMC_ERR_INVALID_ARG
     assert states_backward(st=0) == states_backward(sh=0) == P.DMC_ERR_INVALID_ARG  # tokens, heads in one place
+
+
+def test_outputs_of_another_stream(ready):
+    """They are that stream's: memory that work of the current stream may still use is not handed to a call that
+    runs beside it."""
+    x, s, cu, dev = ready
+    h = both(dev)
+    side = torch.cuda.Stream()
+    hid, w = torch.zeros(64, 64, dtype=BF16, device=dev), torch.zeros(50, 64, dtype=BF16, device=dev)
+    t, f = torch.zeros(64, dtype=torch.int32, device=dev), torch.zeros(64, device=dev)
+    calls = [lambda **k: h.attention(x["q"], x["k"], x["v"], cu, 40, x["bias"], **k),
+             lambda **k: h.states(s["q0"], s["k"], s["v"], cu, 40, s["noise"], **k),
+             lambda **k: h.loss(hid, w, t, **k), lambda **k: h.loss_backward(f, hid, w, t, f, **k)]
+    saved, (o, lse) = calls[1]()[-1], calls[0]()
+    calls += [lambda **k: h.states_backward(s["q0"], s["k"], s["v"], cu, 40, saved, s["dkt"], s["dvt"], s["dbias"], **k),
+              lambda **k: h.attention_backward(x["dout"], x["q"], x["k"], x["v"], o, lse, cu, 40, x["bias"], **k)]
+    torch.cuda.synchronize()
+    for call in calls:
+        for stream in (side, side.cuda_stream):
+            want = [t.clone() for t in call()]
+            torch.cuda.synchronize()
+            shapes = [(t.shape, t.dtype) for t in want]
+            freed = [torch.empty(a, dtype=b, device=dev) for _ in range(4) for a, b in shapes]
+            places = {t.data_ptr() for t in freed}
+            del freed  # their places are the current stream's to use again
+            got = call(stream=stream)
+            side.synchronize()
+            assert not places & {t.data_ptr() for t in got}
+            for a, b in zip(got[:4], want):  # (states' fifth has rows that nobody writes or reads)
+                assert torch.equal(a, b)
+    assert h.status() == (0, 0)
+
+
+def test_a_handle_dropped_while_another_stream_works(ready):
+    """Its arena is not handed out again before that stream is done."""
+    x, _, cu, dev = ready
+    h = both(dev)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+        h.attention(x["q"], x["k"], x["v"], cu, 40, x["bias"])
+    place, size = h.arena.data_ptr(), h.nbytes
+    del h
+    again = torch.empty(size, dtype=torch.uint8, device=dev)
+    assert again.data_ptr() != place
+    side.synchronize()
