@@ -113,6 +113,8 @@ class DmcRetrofit:
         if not isinstance(cu_seqlens, torch.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1:
             raise ValueError("cu_seqlens must be int32 [sequences + 1]")
         n = cu_seqlens.numel()
+        if n == 1 and k.shape[0]:
+            raise ValueError(f"cu_seqlens has no sequence for {k.shape[0]} tokens")
         return k.shape[0], n - 1, self._is("cu_seqlens", cu_seqlens, (n,), _I32)
 
     def _first(self, name, q0, T):

@@ -1,5 +1,6 @@
 """What the retrofitting calls refuse beside shapes and types: another device than the handle's, addresses that are
-not aligned to their elements, outputs that lie in one place; and whose memory a call on another stream uses."""
+not aligned to their elements, outputs that lie in one place, tokens of no sequence; and whose memory a call on
+another stream uses."""
 import ctypes as C
 
 import pytest
@@ -80,6 +81,18 @@ def test_addresses_that_are_not_their_elements(ready, dtype):
     assert states(q=bad) == states_backward(q=bad) == states_backward(dq=bad) == P.DMC_ERR_INVALID_ARG
     assert states_backward(db=bad) == attention_backward(bad) == P.DMC_ERR_INVALID_ARG
     assert states_backward(st=0) == states_backward(sh=0) == P.DMC_ERR_INVALID_ARG  # tokens, heads in one place
+
+
+def test_tokens_without_sequences(ready):
+    x, s, _, dev = ready
+    h = handle(dev, *HEADS, BF16, LENS)
+    none = torch.zeros(1, dtype=torch.int32, device=dev)
+    with pytest.raises(ValueError):
+        h.attention(x["q"], x["k"], x["v"], none, 40)
+    with pytest.raises(ValueError):
+        h.states(s["q0"], s["k"], s["v"], none, 40)
+    empty = h.attention(x["q"][:0], x["k"][:0], x["v"][:0], none, 0)
+    assert empty[0].shape == (0, 4, 64)
 
 
 def test_outputs_of_another_stream(ready):
