@@ -60,11 +60,15 @@ class DmcRetrofit:
             return torch._C._cuda_getCurrentRawStream(self.index)
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
+    def _stream(self, raw):
+        # (an ExternalStream of the number 0 would be another one)
+        return torch.cuda.ExternalStream(raw, device=self.device) if raw else torch.cuda.default_stream(self.device)
+
     def _s(self, stream):
         """The number of the stream of a call."""
         raw = self._raw(stream)
         if raw not in self._streams:
-            self.arena.record_stream(torch.cuda.ExternalStream(raw, device=self.device))
+            self.arena.record_stream(self._stream(raw))
             self._streams.add(raw)
         return raw
 
@@ -96,7 +100,7 @@ class DmcRetrofit:
         freed there does not run beside the call."""
         if stream is None or self._raw(stream) == self._raw(None):
             return self._new
-        other = torch.cuda.ExternalStream(self._raw(stream), device=self.device)
+        other = self._stream(self._raw(stream))
 
         def new(shape, dtype):
             with torch.cuda.stream(other):

@@ -140,3 +140,26 @@ def test_a_handle_dropped_while_another_stream_works(ready):
     again = torch.empty(size, dtype=torch.uint8, device=dev)
     assert again.data_ptr() != place
     side.synchronize()
+
+
+def test_the_default_stream_named_from_another(ready):
+    """Its number is 0: outputs and arena come from its memory, too."""
+    x, _, cu, dev = ready
+
+    def stream_of(t):
+        at = t.data_ptr()
+        return [s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"]]
+
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        h = DmcRetrofit(*HEADS, dtype=BF16, max_tokens=sum(LENS), max_seqs=2, device=dev, stream=0)
+        outs = h.attention(x["q"], x["k"], x["v"], cu, 40, x["bias"], stream=0)
+        outs += h.attention(x["q"], x["k"], x["v"], cu, 40, x["bias"], stream=torch.cuda.default_stream())
+        there = h.attention(x["q"], x["k"], x["v"], cu, 40, x["bias"])
+    torch.cuda.synchronize()
+    for t in (*outs, h.arena):
+        assert stream_of(t) == [0]
+    for t in there:
+        assert stream_of(t) == [side.cuda_stream]
+    assert h.status() == (0, 0)
