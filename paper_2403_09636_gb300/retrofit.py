@@ -66,7 +66,7 @@ class DmcRetrofit:
 
     def _s(self, stream):
         """The number of the stream of a call."""
-        raw = self._raw(stream)
+        raw = torch._C._cuda_getCurrentRawStream(self.index) if stream is None else self._raw(stream)
         if raw not in self._streams:
             self.arena.record_stream(self._stream(raw))
             self._streams.add(raw)
@@ -98,7 +98,7 @@ class DmcRetrofit:
     def _maker(self, stream):
         """`_new`, of memory that belongs to the stream of a call: work of the current one that still uses what was
         freed there does not run beside the call."""
-        if stream is None or self._raw(stream) == self._raw(None):
+        if self._raw(stream) == self._raw(None):
             return self._new
         other = self._stream(self._raw(stream))
 
@@ -147,12 +147,13 @@ class DmcRetrofit:
         [T, Hkv, D], noise [Hkv, T] or None; alpha and bias are fp32 [Hkv, T], saved is for the
         backward pass."""
         T, n, cu = self._seqs(k, cu_seqlens)
-        H, D, dt, check, new = self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is, self._maker(stream)
+        H, D, dt, check = self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is
         rows, scalars, saved = (T, H, D), (H, T), self._saved_floats(n, T)
         q = self._first("q0", q0, T)
         kp, vp = check("k", k, rows, dt), check("v", v, rows, dt)
         np_ = None if noise is None else check("noise", noise, scalars, _F32)
         if out is None:
+            new = self._new if stream is None else self._maker(stream)
             out = (new(rows, dt), new(rows, dt), new(scalars, _F32), new(scalars, _F32), new((saved,), _F32))
             ptrs = [t.data_ptr() for t in out]
         else:
@@ -170,7 +171,7 @@ class DmcRetrofit:
         """(dq0, dk, dv) from the states' gradients: dbias [Hkv, T] in the handle's dtype, dalpha fp32
         [Hkv, T] or None. out's dq0 may be strided (dq[..., 0] of the attention's dq)."""
         T, n, cu = self._seqs(k, cu_seqlens)
-        H, D, dt, check, new = self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is, self._maker(stream)
+        H, D, dt, check = self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is
         rows, scalars = (T, H, D), (H, T)
         q = self._first("q0", q0, T)
         ptrs = (check("k", k, rows, dt), check("v", v, rows, dt),
@@ -179,6 +180,7 @@ class DmcRetrofit:
                  check("dvt", dvt, rows, dt), check("dbias", dbias, scalars, dt),
                  None if dalpha is None else check("dalpha", dalpha, scalars, _F32))
         if out is None:
+            new = self._new if stream is None else self._maker(stream)
             out = (new((T, self.cfg.num_q_heads), dt), new(rows, dt), new(rows, dt))
         dq0, dk, dv = out = self._given(out, ("dq0", "dk", "dv"))
         st = self.lib.dmc_retrofit_states_backward(
@@ -199,7 +201,7 @@ class DmcRetrofit:
         ptrs = (check("q", q, queries, dt), check("k", k, rows, dt), check("v", v, rows, dt),
                 None if bias is None else check("bias", bias, (H, T), _F32))
         if out is None:
-            new = self._maker(stream)
+            new = self._new if stream is None else self._maker(stream)
             out = (new(queries, dt), new((Hq, T), _F32))
         o, lse = out = self._given(out, ("out", "lse"))
         st = self.lib.dmc_retrofit_attention(self.handle, n, *ptrs, cu, T, max_seqlen, check("out", o, queries, dt),
@@ -213,11 +215,12 @@ class DmcRetrofit:
         handle's dtype, None without a bias."""
         T, n, cu = self._seqs(k, cu_seqlens)
         Hq, H, D, dt, check = self.cfg.num_q_heads, self.cfg.num_kv_heads, self.cfg.head_dim, self.dtype, self._is
-        queries, rows, scalars, new = (T, Hq, D), (T, H, D), (H, T), self._maker(stream)
+        queries, rows, scalars = (T, Hq, D), (T, H, D), (H, T)
         ptrs = (check("q", q, queries, dt), check("k", k, rows, dt), check("v", v, rows, dt),
                 None if bias is None else check("bias", bias, scalars, _F32), check("o", o, queries, dt),
                 check("lse", lse, (Hq, T), _F32), check("dout", dout, queries, dt))
         if out is None:
+            new = self._new if stream is None else self._maker(stream)
             out = (new(queries, dt), new(rows, dt), new(rows, dt)) + (() if bias is None else (new(scalars, dt),))
         self._given(out, ("dq", "dk", "dv") if bias is None else ("dq", "dk", "dv", "dbias"))
         grads = (check("dq", out[0], queries, dt), check("dk", out[1], rows, dt), check("dv", out[2], rows, dt),
@@ -243,7 +246,7 @@ class DmcRetrofit:
         int32 targets [N]; below 0 a position is ignored."""
         N, ptrs = self._words(hidden, weight, targets)
         if out is None:
-            new = self._maker(stream)
+            new = self._new if stream is None else self._maker(stream)
             out = (new((N,), _F32), new((N,), _F32))
         loss, lse = out = self._given(out, ("loss", "lse"))
         st = self.lib.dmc_retrofit_loss(self.handle, N, *ptrs, self._is("loss", loss, (N,), _F32),
@@ -258,7 +261,7 @@ class DmcRetrofit:
         given = (self._is("lse", lse, (N,), _F32), self._is("dloss", dloss, (N,), _F32))
         shapes = (N, self.cfg.hidden), (self.cfg.vocab, self.cfg.hidden)
         if out is None:
-            new = self._maker(stream)
+            new = self._new if stream is None else self._maker(stream)
             out = (new(shapes[0], self.dtype), new(shapes[1], self.dtype))
         dh, dw = out = self._given(out, ("dhidden", "dweight"))
         st = self.lib.dmc_retrofit_loss_backward(self.handle, N, *ptrs, *given, self._is("dhidden", dh, shapes[0], self.dtype),
