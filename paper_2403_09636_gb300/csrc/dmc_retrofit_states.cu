@@ -105,8 +105,10 @@ __device__ __forceinline__ Gate gate_of(const StatesArgs& a, GateIn v, int h, in
     g.omega = small_omega<T>(a, h, tok);
     g.slope = m < kLeast ? 0.f : 1.f;
   } else {
-    g.omega = kUnit / (1.f + expf(-m));
-    g.slope = 1.f - g.omega * (1.f / kUnit);
+    const float e = expf(-m);
+    g.omega = kUnit / (1.f + e);
+    // 1 - omega, from the exponential where the difference would have lost its bits
+    g.slope = m > 0.f ? e * (g.omega * (1.f / kUnit)) : 1.f - g.omega * (1.f / kUnit);
   }
   // both sides from the exponential that does not overflow
   const float e = expf(-fabsf(x)), big = 1.f / (1.f + e), small = e / (1.f + e);

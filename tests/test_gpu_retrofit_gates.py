@@ -42,3 +42,15 @@ def test_no_importance_at_all(cuda_dev, dtype):
         assert bool(torch.isfinite(t).all()), name
     assert torch.equal(got["kt"][0, :, 1:].cpu(), x["k"][0, :, 1:]) and torch.equal(got["vt"][0].cpu(), x["v"][0])
     assert not bool(got["dq0"].any())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("heads", [(4, 4, 64), (8, 2, 128)])
+def test_importance_near_one(cuda_dev, heads, dtype):
+    """1 - omega is far smaller than what rounding leaves of a difference: q[0]'s gradient keeps its precision."""
+    lens = [1, 2, 70, 200]
+    x = states_inputs(lens, *heads, dtype)
+    g = torch.Generator().manual_seed(8)
+    # exact sums of a group; up to 17, where the 64-bit reference still has 1 - omega to 3e-9
+    x["q0"] = (5.0 + 12.0 * torch.rand(x["q0"].shape, generator=g)).mul(8).round().div(8).to(dtype)
+    check_states(x, lens, dtype, run_states(cuda_dev, x, lens, heads, dtype))
