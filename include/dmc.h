@@ -366,7 +366,8 @@ dmc_status dmc_retrofit_attention(dmc_retrofit_t h, int32_t num_seqs, const void
  * In bf16, weights and the scores' gradients are rounded to bf16 for their products;
  * dbias is summed from the unrounded ones. Nothing is accumulated into. In bf16 calls with
  * max_seqlen up to 384 a sequence's gradients do not depend on the others to the bit; in
- * longer ones, and in fp32, dk, dv and dbias may be added up in another order in another call. */
+ * longer ones, and in fp32, dk, dv and dbias may be added up in another order in another call.
+ * A value that is not finite may reach every gradient of its own sequence. */
 dmc_status dmc_retrofit_attention_backward(dmc_retrofit_t h, int32_t num_seqs, const void* q_dev,
                                            const void* k_dev, const void* v_dev,
                                            const float* bias_dev, const void* out_dev,
@@ -376,7 +377,10 @@ dmc_status dmc_retrofit_attention_backward(dmc_retrofit_t h, int32_t num_seqs, c
                                            void* dv_dev, void* dbias_dev, cudaStream_t stream);
 
 /* Softmax cross entropy of num_tokens hidden states against the vocabulary, in
- * pieces of it; the logits hidden_dev weight_dev^T are never kept.
+ * pieces of it. The logits hidden_dev weight_dev^T are not written to memory; the backward
+ * pass computes them again and keeps the gradient of those of one piece at a time in the
+ * handle's arena: bf16 [max_tokens, words of a piece] (three times that in fp32), about 512 MB
+ * or the whole vocabulary, whichever is less, but 1024 words at least.
  *   hidden_dev: [num_tokens, hidden]; weight_dev: [vocab, hidden];
  *   targets_dev: int32 [num_tokens]; a target below 0 is an ignored position;
  *   loss_dev (written): fp32 [num_tokens], the log-sum minus the target's logit, 0
@@ -387,7 +391,8 @@ dmc_status dmc_retrofit_loss(dmc_retrofit_t h, int32_t num_tokens, const void* h
 
 /* Gradients of dmc_retrofit_loss, given dloss_dev, fp32 [num_tokens] (not read where
  * the target is ignored): dhidden_dev and dweight_dev (written), laid out as
- * hidden and weight. */
+ * hidden and weight. An ignored position's hidden state enters the sums of dweight with
+ * a gradient of zero, so it has to be finite. */
 dmc_status dmc_retrofit_loss_backward(dmc_retrofit_t h, int32_t num_tokens, const void* hidden_dev,
                                       const void* weight_dev, const int32_t* targets_dev,
                                       const float* lse_dev, const float* dloss_dev,

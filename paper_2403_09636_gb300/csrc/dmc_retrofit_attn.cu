@@ -17,8 +17,9 @@
 //
 // Bound by the softmax warps' instructions beside the tensor cores, which are busy for about 70 % of a long
 // sequence: 8192 tokens of 64 / 8 heads of 128 800 us, 1.37 PFLOP/s (767 us without biases, 1.43); four
-// sequences of 2048, 32 heads, 133 us, 1.03; heads of 64 do half the products per exponential, seven ragged
-// sequences of 40 / 8 heads 188 us, 0.58. Short sequences are chains of S, softmax, P V and epilogue, two
+// sequences of 2048, 32 heads, 133 us, 1.03. Heads of 64 do half the products per exponential and are bound by the
+// chain of a query tile, S, softmax, P V and the next S over P's columns: tensor pipe 29 %, issue slots 43 %; seven ragged
+// sequences of 40 / 8 heads 186 us, 0.58. Short sequences are chains of S, softmax, P V and epilogue, two
 // at a time: 24 of 1 to 211 tokens, 32 / 8 heads, 32 us. Slower: the next item's first S before an item's last
 // P V (133 -> 138, 800 -> 819; short ones 35 -> 33), the diagonal tile's biases by selects in one loop for
 // all tiles (800 -> 915).

@@ -8,6 +8,8 @@
 // step of 16 terms, so that few steps may go into the large one, D / 16 for a score and 4 or less for a sum over
 // rows, which is added to the row's sum in fp32 afterwards.
 //
+// (tcgen05 would multiply faster. The forward pass, and heads of 64, would fit its tiles; the gradients of heads of
+// 128 would not, three parts of K, V, Q and dO of 128 rows being 384 KB. It has not been written.)
 // Tiles of 64 rows lie in shared memory as their three parts, split once when they are loaded;
 // warps multiply 16 rows with mma.sync.m16n8k16, whose operands' layout lets a tile of weights become the
 // left operand of the next product without leaving the registers. Rows are padded by 16 bytes: the

@@ -27,9 +27,10 @@
 // the warp's loads and stores, 4 us of the 18 that a chunk took), and nothing has to be cleared
 // between launches or replays of a graph.
 //
-// Bound by the instructions of a chunk's two passes, at half of the copy bandwidth or less. Four sequences
-// of 2048 tokens, 32 heads of 128, bf16: forward 70 us (272 MB, 3.9 TB/s), backward 158 us (407 MB,
-// 2.6 TB/s: both dots of every token on top). Slower: warps that stay and take one chunk after another
+// Bound by latency: a chunk is one chain of passes, scans and the wait for what comes in, and shared memory (9.5 KB
+// per warp, 38.7 KB per two in the backward pass) leaves few warps per SM (30 and 15 % of the most) to fill the gaps: issue
+// slots are 39 and 36 % busy, DRAM 48 and 33 %. Four sequences of 2048 tokens, 32 heads of 128, bf16: forward 70 us (272 MB,
+// 3.9 TB/s), backward 156 us (407 MB, 2.6 TB/s: both dots of every token on top). Slower: warps that stay and take one chunk after another
 // (backward 164; with chunks taken ahead, whose neighbours wait for one that has not begun, 217),
 // rows read a second time from L2 instead of kept in shared memory (168 to 188).
 #include <type_traits>

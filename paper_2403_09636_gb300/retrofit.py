@@ -3,7 +3,7 @@
 `DmcRetrofit` owns a torch uint8 arena and forwards to the dmc_retrofit_* functions
 of the C ABI (include/dmc.h has the mathematics): the relaxed compression's states,
 attention over packed sequences with the bias that hides merged states, and cross
-entropy against a vocabulary whose logits are never kept, each with its gradient.
+entropy against a vocabulary whose logits are not kept for the backward pass, each with its gradient.
 Arguments are checked (type, shape, device, contiguity) and refused with ValueError;
 statuses of the library become DmcError.
 
