@@ -83,6 +83,31 @@ def test_addresses_that_are_not_their_elements(ready, dtype):
     assert states_backward(st=0) == states_backward(sh=0) == P.DMC_ERR_INVALID_ARG  # tokens, heads in one place
 
 
+def test_statuses_of_the_loss(ready):
+    dev = ready[-1]
+    h = both(dev)
+    hid, w = torch.zeros(64, 64, dtype=BF16, device=dev), torch.zeros(50, 64, dtype=BF16, device=dev)
+    f, t = torch.zeros(64, device=dev), torch.zeros(64, dtype=torch.int32, device=dev)
+    dh, dw = torch.ones_like(hid), torch.ones_like(w)
+    inv = P.DMC_ERR_INVALID_ARG
+
+    def loss(n=64, hidden=hid.data_ptr(), weight=w.data_ptr(), targets=t.data_ptr(), out=f.data_ptr()):
+        return P.dmc_retrofit_loss(h.handle, n, hidden, weight, targets, out, f.data_ptr(), 0)
+
+    def backward(n=64, hidden=hid.data_ptr(), dloss=f.data_ptr(), dhidden=dh.data_ptr(), dweight=dw.data_ptr()):
+        return P.dmc_retrofit_loss_backward(h.handle, n, hidden, w.data_ptr(), t.data_ptr(), f.data_ptr(), dloss, dhidden,
+                                            dweight, 0)
+
+    assert loss(n=-1) == loss(n=65) == loss(hidden=0) == loss(hidden=hid.data_ptr() + 8) == loss(weight=0) == inv
+    assert loss(targets=0) == loss(targets=t.data_ptr() + 2) == loss(out=f.data_ptr() + 2) == inv
+    assert backward(n=-1) == backward(n=65) == backward(hidden=0) == backward(dloss=0) == backward(dhidden=0) == inv
+    assert backward(dweight=0) == backward(dweight=dw.data_ptr() + 4) == inv
+    assert loss(n=0) == backward(n=0) == P.DMC_OK
+    torch.cuda.synchronize()
+    assert not bool(dw.any()) and bool(dh.all())  # no token: a gradient of zero
+    assert h.status() == (0, 0)
+
+
 def test_tokens_without_sequences(ready):
     x, s, _, dev = ready
     h = handle(dev, *HEADS, BF16, LENS)
