@@ -59,6 +59,7 @@ typedef enum { DMC_F32 = 0, DMC_BF16 = 1 } dmc_dtype;
 #define DMC_FAULT_BAD_SEQLENS 0x8u      /* cu_seqlens not monotone / out of range */
 #define DMC_FAULT_WAIT_TIMEOUT 0x10u    /* an in-kernel wait gave up (kernel returned) */
 #define DMC_FAULT_BAD_TARGET 0x20u      /* dmc_retrofit_loss: a target >= vocab (taken as ignored) */
+#define DMC_FAULT_BAD_PARENT 0x40u      /* dmc_cache_reorder: a parent outside the call's sequences (taken as unmoved) */
 
 /* Shape of one cache. Storage is paged (the paper stores its variable-length
  * heads with PagedAttention, 32 slots per page, pages allocated on demand per
@@ -214,6 +215,71 @@ dmc_status dmc_decode_step_layers(dmc_cache_t cache, int32_t first_layer, int32_
 dmc_status dmc_decode_step_static_scratch(dmc_cache_t cache, int32_t layer, const void* q_dev,
                                           const void* k_dev, const void* v_dev, void* out_dev,
                                           cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Position rotation. Rotary models turn pair i of a head's dimensions (i and
+ * i + head_dim / 2, or 2 i and 2 i + 1 where `interleaved`) by position *
+ * frequency_i:  x' = x cos - y sin,  y' = y cos + x sin.  The method takes
+ * dimension 0 of q and k out of the attention and uses it as a gate, so the pair
+ * that holds it is not rotated: both of its dimensions stay as they are.
+ * Frequencies are given in turns per token, times 2^64: turns_dev[i] =
+ * round(frequency_i / (2 pi) * 2^64), head_dim / 2 of them ([0] is not read). The
+ * phase of any position, negative ones too, is then exact modulo a turn; cos and sin
+ * are those of fp32. Each result is rounded once.
+ * ------------------------------------------------------------------------ */
+
+/* Rotates queries and keys of num_tokens tokens, in one launch.
+ *   dtype: DMC_F32 or DMC_BF16; head_dim: 64 or 128;
+ *   positions_dev: int32 [num_tokens];
+ *   inverse: rotates back (the rotation's gradient);
+ *   q_dev, k_dev: token t's heads, contiguous, at t * stride elements; strides are
+ *          multiples of 16 bytes. num_k_heads (or num_q_heads) 0: none;
+ *   q_out_dev, k_out_dev (written): the same with strides of their own. An output
+ *          may be its input (with the same stride). */
+dmc_status dmc_rotate(int32_t dtype, int32_t head_dim, int32_t num_tokens, const int32_t* positions_dev,
+                      const uint64_t* turns_dev, int32_t interleaved, int32_t inverse, int32_t num_q_heads,
+                      const void* q_dev, int64_t q_token_stride, void* q_out_dev, int64_t q_out_token_stride,
+                      int32_t num_k_heads, const void* k_dev, int64_t k_token_stride, void* k_out_dev,
+                      int64_t k_out_token_stride, cudaStream_t stream);
+
+/* Appends new tokens to the caches of the sequences [first_seq, first_seq + num_seqs)
+ * of one layer, as dmc_decode_step and dmc_prefill_compress do (Algorithm 1), without
+ * attention and with the rotation on the way: keys join the cache rotated to their
+ * positions, the rotated queries come back for the attention that follows. The gates
+ * are the unrotated first components, which the rotation leaves alone. Any cache.
+ *   q_dev: [total_tokens, num_q_heads, head_dim]; k_dev, v_dev: [total_tokens,
+ *          num_kv_heads, head_dim], sequences packed;
+ *   cu_seqlens_dev, total_tokens, max_seqlen: as in dmc_prefill_compress. NULL: one
+ *          token for each sequence (total_tokens = num_seqs, max_seqlen = 1). Calls with
+ *          max_seqlen > 1 take up to max_prefill_tokens;
+ *   positions_dev: int32 [num_seqs], of each sequence's first token of this call; the
+ *          others follow one by one. (The cache cannot tell: it holds slots, not tokens.)
+ *   turns_dev, interleaved: the rotation, as above. turns_dev NULL: none; positions_dev
+ *          and q_out_dev are then not used and must be NULL;
+ *   q_out_dev (written): as q_dev, which it may be. */
+dmc_status dmc_cache_append(dmc_cache_t cache, int32_t layer, int32_t first_seq, int32_t num_seqs, const void* q_dev,
+                            const void* k_dev, const void* v_dev, const int32_t* cu_seqlens_dev, int32_t total_tokens,
+                            int32_t max_seqlen, const int32_t* positions_dev, const uint64_t* turns_dev,
+                            int32_t interleaved, void* q_out_dev, cudaStream_t stream);
+
+/* Attention of one token's queries per sequence over the cache as it stands: what
+ * dmc_decode_step does without its update (the token's own key and value are in the
+ * cache where dmc_cache_append has put them; a layer that shares another's cache has
+ * none). The score is q[1:]^T k[1:] / sqrt(head_dim); a head without slots gives zeros.
+ * The cache is not changed, its scratch is used.
+ *   q_dev: [batch, num_q_heads, head_dim]; out_dev (written): the same. */
+dmc_status dmc_cache_attend(dmc_cache_t cache, int32_t layer, const void* q_dev, void* out_dev, cudaStream_t stream);
+
+/* Sequence first_seq + j continues from what sequence first_seq + parents_dev[j] holds,
+ * in every layer, as if all were copied at once (beam search after a selection; several
+ * continuations of one prompt). Nothing is copied but each copy's last page: pages
+ * before it are never written again and are shared. Pages that no sequence
+ * holds any more return to the pool. A copy takes the last page of a sequence that
+ * nobody continues; where that one is empty, a page of the pool (when there is none left
+ * the sequence is emptied and DMC_FAULT_PAGES_EXHAUSTED set).
+ *   parents_dev: int32 [num_seqs], each in [0, num_seqs); num_seqs is at most 512. */
+dmc_status dmc_cache_reorder(dmc_cache_t cache, int32_t first_seq, int32_t num_seqs, const int32_t* parents_dev,
+                             cudaStream_t stream);
 
 /* Copies the slot count of every head of `layer`, int32 [batch, num_kv_heads],
  * into out_dev (asynchronous). */
@@ -401,6 +467,51 @@ dmc_status dmc_retrofit_loss_backward(dmc_retrofit_t h, int32_t num_tokens, cons
 /* Synchronizes `stream`, then reads the handle's sticky fault bits (into *bits if
  * not NULL). Returns DMC_OK or DMC_ERR_DEVICE_FAULT. */
 dmc_status dmc_retrofit_status(dmc_retrofit_t h, cudaStream_t stream, uint32_t* bits);
+
+/* ------------------------------------------------------------------------
+ * Beam search: selection. For every group of beams (one text) the `keep` best of
+ * beams x vocab continuations:
+ *   score(b, w) = scores[b] + logits[b, w] - log sum_w' exp(logits[b, w'])
+ * in descending order; ties go to the lower b * vocab + w. A finished beam has one
+ * continuation, the end word, at its own score. A beam whose score, or whose log-sum, is not
+ * a finite number offers its words at -infinity (so a search may begin with scores 0,
+ * -inf, -inf, ...); single logits may be -infinity (masked words). Scores are compared
+ * in 64 bits. The parents are what dmc_cache_reorder takes when keep = beams.
+ * The handle lays its scratch out in a caller's arena, as a cache does; calls on one
+ * handle must be ordered on the GPU, allocate nothing and can be captured.
+ * ------------------------------------------------------------------------ */
+
+typedef struct {
+  int32_t groups;
+  int32_t beams;  /* per group, at most 32 */
+  int32_t keep;   /* continuations per group, at most 32 (and beams * vocab) */
+  int32_t vocab;  /* at most 2^28 */
+  int32_t dtype;  /* dmc_dtype of the logits */
+} dmc_beam_config;
+
+typedef struct dmc_beam* dmc_beam_t;
+
+/* Bytes of device memory a handle with this config needs (0 if invalid). */
+size_t dmc_beam_required_bytes(const dmc_beam_config* cfg);
+
+/* Lays the scratch out inside the caller's device arena (256-byte aligned);
+ * ownership as in dmc_cache_create. The handle belongs to the current device. */
+dmc_status dmc_beam_create(const dmc_beam_config* cfg, void* arena_dev, size_t arena_bytes, cudaStream_t stream,
+                           dmc_beam_t* out);
+
+/* Frees the host-side handle (the arena stays the caller's). NULL is a no-op. */
+dmc_status dmc_beam_destroy(dmc_beam_t h);
+
+/* One selection.
+ *   logits_dev: row g * beams + b at logits_row_stride elements (>= vocab) from the one before;
+ *   scores_dev: fp32 [groups, beams]; finished_dev: [groups, beams], 0 or not, or NULL (none);
+ *   eos: the end word, or negative (none; then finished_dev must be NULL);
+ *   out_scores_dev, out_tokens_dev, out_parents_dev, out_done_dev (written): [groups, keep];
+ *          parents are rows, g * beams + b; done: 1 where the beam had finished or its word
+ *          is eos, else 0. With keep = beams, scores and finished may be updated in place. */
+dmc_status dmc_beam_select(dmc_beam_t h, const void* logits_dev, int64_t logits_row_stride, const float* scores_dev,
+                           const uint8_t* finished_dev, int32_t eos, float* out_scores_dev, int32_t* out_tokens_dev,
+                           int32_t* out_parents_dev, uint8_t* out_done_dev, cudaStream_t stream);
 
 /* Static description of a status code. */
 const char* dmc_status_string(dmc_status status);

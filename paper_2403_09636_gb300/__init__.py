@@ -29,6 +29,7 @@ DMC_FAULT_NAN_GATE = 0x4
 DMC_FAULT_BAD_SEQLENS = 0x8
 DMC_FAULT_WAIT_TIMEOUT = 0x10
 DMC_FAULT_BAD_TARGET = 0x20
+DMC_FAULT_BAD_PARENT = 0x40
 PAGE_SIZE = 32
 
 EXPORTED = ("dmc_cache_required_bytes", "dmc_cache_create", "dmc_cache_destroy",
@@ -38,7 +39,9 @@ EXPORTED = ("dmc_cache_required_bytes", "dmc_cache_create", "dmc_cache_destroy",
             "dmc_retrofit_required_bytes", "dmc_retrofit_create", "dmc_retrofit_destroy",
             "dmc_retrofit_saved_bytes", "dmc_retrofit_states", "dmc_retrofit_states_backward",
             "dmc_retrofit_attention", "dmc_retrofit_attention_backward", "dmc_retrofit_loss",
-            "dmc_retrofit_loss_backward", "dmc_retrofit_status")
+            "dmc_retrofit_loss_backward", "dmc_retrofit_status",
+            "dmc_rotate", "dmc_cache_append", "dmc_cache_attend", "dmc_cache_reorder",
+            "dmc_beam_required_bytes", "dmc_beam_create", "dmc_beam_destroy", "dmc_beam_select")
 
 
 class dmc_cache_config(C.Structure):
@@ -53,6 +56,11 @@ class dmc_retrofit_config(C.Structure):
     _fields_ = [("num_q_heads", C.c_int32), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("dtype", C.c_int32), ("max_tokens", C.c_int32), ("max_seqs", C.c_int32),
                 ("hidden", C.c_int32), ("vocab", C.c_int32)]
+
+
+class dmc_beam_config(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("beams", C.c_int32), ("keep", C.c_int32), ("vocab", C.c_int32),
+                ("dtype", C.c_int32)]
 
 
 class DmcError(RuntimeError):
@@ -76,6 +84,7 @@ def lib():
         vp, i32, i64, sz, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float
         cfgp = C.POINTER(dmc_cache_config)
         rcfgp = C.POINTER(dmc_retrofit_config)
+        bcfgp = C.POINTER(dmc_beam_config)
         sig = {
             "dmc_cache_required_bytes": (sz, [cfgp]),
             "dmc_cache_create": (C.c_int, [cfgp, vp, sz, vp, C.POINTER(vp)]),
@@ -106,6 +115,14 @@ def lib():
             "dmc_retrofit_loss": (C.c_int, [vp, i32, vp, vp, vp, vp, vp, vp]),
             "dmc_retrofit_loss_backward": (C.c_int, [vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]),
             "dmc_retrofit_status": (C.c_int, [vp, vp, C.POINTER(C.c_uint32)]),
+            "dmc_rotate": (C.c_int, [i32, i32, i32, vp, vp, i32, i32, i32, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp]),
+            "dmc_cache_append": (C.c_int, [vp, i32, i32, i32, vp, vp, vp, vp, i32, i32, vp, vp, i32, vp, vp]),
+            "dmc_cache_attend": (C.c_int, [vp, i32, vp, vp, vp]),
+            "dmc_cache_reorder": (C.c_int, [vp, i32, i32, vp, vp]),
+            "dmc_beam_required_bytes": (sz, [bcfgp]),
+            "dmc_beam_create": (C.c_int, [bcfgp, vp, sz, vp, C.POINTER(vp)]),
+            "dmc_beam_destroy": (C.c_int, [vp]),
+            "dmc_beam_select": (C.c_int, [vp, vp, i64, vp, vp, i32, vp, vp, vp, vp, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(l, name)
@@ -261,6 +278,49 @@ def dmc_retrofit_status(handle, stream):
     return st, int(bits.value)
 
 
+def dmc_rotate(dtype, head_dim, num_tokens, positions_ptr, turns_ptr, interleaved, inverse, num_q_heads, q_ptr,
+               q_token_stride, q_out_ptr, q_out_token_stride, num_k_heads, k_ptr, k_token_stride, k_out_ptr,
+               k_out_token_stride, stream) -> int:
+    return lib().dmc_rotate(dtype, head_dim, num_tokens, positions_ptr, turns_ptr, interleaved, inverse, num_q_heads,
+                            q_ptr, q_token_stride, q_out_ptr, q_out_token_stride, num_k_heads, k_ptr, k_token_stride,
+                            k_out_ptr, k_out_token_stride, stream)
+
+
+def dmc_cache_append(handle, layer, first_seq, num_seqs, q_ptr, k_ptr, v_ptr, cu_seqlens_ptr, total_tokens, max_seqlen,
+                     positions_ptr, turns_ptr, interleaved, q_out_ptr, stream) -> int:
+    return lib().dmc_cache_append(handle, layer, first_seq, num_seqs, q_ptr, k_ptr, v_ptr, cu_seqlens_ptr, total_tokens,
+                                  max_seqlen, positions_ptr, turns_ptr, interleaved, q_out_ptr, stream)
+
+
+def dmc_cache_attend(handle, layer, q_ptr, out_ptr, stream) -> int:
+    return lib().dmc_cache_attend(handle, layer, q_ptr, out_ptr, stream)
+
+
+def dmc_cache_reorder(handle, first_seq, num_seqs, parents_ptr, stream) -> int:
+    return lib().dmc_cache_reorder(handle, first_seq, num_seqs, parents_ptr, stream)
+
+
+def dmc_beam_required_bytes(cfg: dmc_beam_config) -> int:
+    return int(lib().dmc_beam_required_bytes(C.byref(cfg)))
+
+
+def dmc_beam_create(cfg: dmc_beam_config, arena_ptr: int, arena_bytes: int, stream: int):
+    """Returns (status, handle)."""
+    h = C.c_void_p()
+    st = lib().dmc_beam_create(C.byref(cfg), arena_ptr, arena_bytes, stream, C.byref(h))
+    return st, h.value
+
+
+def dmc_beam_destroy(handle) -> int:
+    return lib().dmc_beam_destroy(handle)
+
+
+def dmc_beam_select(handle, logits_ptr, logits_row_stride, scores_ptr, finished_ptr, eos, out_scores_ptr, out_tokens_ptr,
+                    out_parents_ptr, out_done_ptr, stream) -> int:
+    return lib().dmc_beam_select(handle, logits_ptr, logits_row_stride, scores_ptr, finished_ptr, eos, out_scores_ptr,
+                                 out_tokens_ptr, out_parents_ptr, out_done_ptr, stream)
+
+
 def _check(st: int, what: str):
     if st != DMC_OK:
         raise DmcError(st, what)
@@ -278,6 +338,8 @@ class DmcCache:
         import torch
         self.torch = torch
         self.device = torch.device(device if device is not None else "cuda")
+        cuda = self.device.type == "cuda" and torch.cuda.is_available()
+        self.index = (torch.cuda.current_device() if self.device.index is None else self.device.index) if cuda else -1
         tdt = {torch.float32: DMC_F32, torch.bfloat16: DMC_BF16}[dtype]
         self.dtype = dtype
         self.cfg = dmc_cache_config(num_layers, batch, num_q_heads, num_kv_heads, head_dim, tdt,
@@ -342,6 +404,84 @@ class DmcCache:
         _check(dmc_decode_step_layers(self.handle, first_layer, q.shape[0], q.data_ptr(),
                                       k.data_ptr(), v.data_ptr(), out.data_ptr(), self._s(stream)),
                "dmc_decode_step_layers")
+
+    # ---- calls that check their tensors (what does not fit is refused with ValueError)
+
+    def _is(self, name, t, shape, dtype):
+        torch = self.torch
+        if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_cuda
+                and t.get_device() == self.index and t.is_contiguous()):
+            return t.data_ptr()
+        what = f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
+        raise ValueError(f"{name} must be contiguous {dtype} {tuple(shape)} on {self.device}, got {what}")
+
+    def _out(self, name, out, like, stream):
+        """`out`, or a new tensor as `like`, of memory that belongs to the call's stream."""
+        torch = self.torch
+        if out is None:
+            raw = self._s(stream)
+            if stream is None or raw == self._s(None):
+                return torch.empty_like(like)
+            other = torch.cuda.ExternalStream(raw, device=self.device) if raw else torch.cuda.default_stream(self.device)
+            with torch.cuda.stream(other):
+                return torch.empty_like(like)
+        self._is(name, out, like.shape, like.dtype)
+        return out
+
+    def append(self, layer, q, k, v, positions=None, rotary=None, cu_seqlens=None, max_seqlen=1, first_seq=0, q_out=None,
+               stream=None):
+        """New tokens join the cache, rotated on the way; returns the rotated queries (None without a rotation).
+        q: [T, Hq, D]; k, v: [T, Hkv, D], of one token for each of T sequences from first_seq on, or packed
+        by cu_seqlens (int32 [sequences + 1]); positions: int32, one for each sequence's first token; rotary: a
+        `rotary.Rotary`; q_out may be q."""
+        c, t = self.cfg, self.torch
+        if not isinstance(k, t.Tensor) or k.dim() != 3:
+            raise ValueError("k must be [tokens, KV heads, head_dim]")
+        T, D = k.shape[0], c.head_dim
+        ptrs = (self._is("q", q, (T, c.num_q_heads, D), self.dtype), self._is("k", k, (T, c.num_kv_heads, D), self.dtype),
+                self._is("v", v, (T, c.num_kv_heads, D), self.dtype))
+        n, cu = T, None
+        if cu_seqlens is not None:
+            if not isinstance(cu_seqlens, t.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1:
+                raise ValueError("cu_seqlens must be int32 [sequences + 1]")
+            n = cu_seqlens.numel() - 1
+            cu = self._is("cu_seqlens", cu_seqlens, (n + 1,), t.int32)
+        at = turns = to = None
+        pairs = 0
+        if rotary is None:
+            if positions is not None or q_out is not None:
+                raise ValueError("positions and q_out are for a rotation")
+        else:
+            if rotary.head_dim != D or rotary.turns.get_device() != self.index:
+                raise ValueError(f"the rotation is for heads of {rotary.head_dim} on {rotary.turns.device}")
+            at = self._is("positions", positions, (n,), t.int32)
+            turns, pairs = rotary.turns.data_ptr(), int(rotary.interleaved)
+            q_out = self._out("q_out", q_out, q, stream)
+            to = q_out.data_ptr()
+        st = dmc_cache_append(self.handle, layer, first_seq, n, *ptrs, cu, T, min(int(max_seqlen), T), at, turns, pairs, to,
+                              self._s(stream))
+        if st:
+            _check(st, "dmc_cache_append")
+        return q_out
+
+    def attend(self, layer, q, out=None, stream=None):
+        """Attention of q [batch, Hq, D] over the cache as it stands; the cache is not changed."""
+        c = self.cfg
+        p = self._is("q", q, (c.batch, c.num_q_heads, c.head_dim), self.dtype)
+        out = self._out("out", out, q, stream)
+        st = dmc_cache_attend(self.handle, layer, p, out.data_ptr(), self._s(stream))
+        if st:
+            _check(st, "dmc_cache_attend")
+        return out
+
+    def reorder(self, parents, first_seq=0, stream=None):
+        """Sequence first_seq + j continues from the cache of sequence first_seq + parents[j] (int32 on the cache's
+        device), in every layer. What they have in common is shared."""
+        if not isinstance(parents, self.torch.Tensor) or parents.dim() < 1:
+            raise ValueError("parents must be int32, one for each sequence")
+        n = parents.numel()
+        p = self._is("parents", parents, parents.shape, self.torch.int32)
+        _check(dmc_cache_reorder(self.handle, first_seq, n, p, self._s(stream)), "dmc_cache_reorder")
 
     def lengths(self, layer, stream=None):
         t = self.torch

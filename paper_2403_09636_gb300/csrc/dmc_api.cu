@@ -1,13 +1,14 @@
 // Host side of the C ABI declared in include/dmc.h: config validation, the
 // layout of a cache inside the caller's arena, and the small utility kernels
-// (lengths copy, head export). The hot kernels live in dmc_decode.cu and
-// dmc_prefill.cu.
+// (lengths copy, head export). The hot kernels live in dmc_decode.cu,
+// dmc_prefill.cuh, dmc_append.cu and dmc_reorder.cu.
 #include <string.h>
 
 #include <new>
 
 #include "dmc_internal.cuh"
 #include "dmc_overlap.h"
+#include "dmc_reorder.h"
 
 namespace dmc {
 cudaError_t decode_setup(const Layout& L, int Gv, DecodePlan* plan);
@@ -22,6 +23,10 @@ cudaError_t prefill_attn_launch(const Layout& L, int layer, int first_seq, int n
                                 const void* q, const void* k, const void* v, const int* cu,
                                 int total_tokens, int max_seqlen, const float* carry,
                                 const float* weights, void* out, cudaStream_t stream);
+cudaError_t append_launch(const Layout& L, int layer, int first_seq, int num_seqs, const void* q, const void* k,
+                          const void* v, const int* cu, int total_tokens, int max_seqlen, const int* at,
+                          const unsigned long long* turns, bool pairs, void* q_out, cudaStream_t stream);
+cudaError_t reorder_launch(const Layout& L, int first, int n, const int* parents, cudaStream_t stream);
 cudaError_t decode_static_partials(int device, float** ptr, size_t* floats);
 bool gqa_supported(const Layout& L);
 cudaError_t gqa_setup(const Layout& L, DecodePlan* plan);
@@ -45,7 +50,7 @@ struct dmc_cache {
   bool gqa;  // grouped queries on the tensor-core kernel (one worker per KV head)
   dmc::DecodePlan plan;
   dmc::DecodeOrder order;
-  char* meta;  // lengths, ctl, counters, pool top, error: cleared by create / reset
+  char* meta;  // lengths, ctl, counters, pool, error, page use: cleared by create / reset
   size_t meta_bytes;
   float* carry;    // segment sums at prompt chunk starts (prompt attention)
   float* weights;  // decisions and omegas of the prompt's chunks (prompt attention)
@@ -75,7 +80,7 @@ bool valid_config(const dmc_cache_config* c) {
 
 // Byte offsets of every region; returns the total size.
 struct Offsets {
-  size_t pages, z, ptab, meta, lengths, ctl, counters, pool_top, error, unbounded, meta_end, partials,
+  size_t pages, z, ptab, meta, lengths, ctl, counters, pool_top, error, unbounded, page_use, meta_end, partials,
       pending, pending_at, pending_z, opens, plan, carry, weights, ring, ring_w, seglen, total;
   int MPH, plan_stride;
 };
@@ -98,9 +103,10 @@ Offsets offsets(const dmc_cache_config* c) {
   o.ctl = at; at = align_up(at + (size_t)c->num_layers * 4 * 4);
   o.counters = at; at = align_up(at + (size_t)c->num_layers * NH * G * 4);
   o.seglen = at; at = align_up(at + (c->window > 0 ? (size_t)c->num_layers * 2 * NH * 4 : 0));
-  o.pool_top = at; at = align_up(at + 8);
+  o.pool_top = at; at = align_up(at + 4 * 8);
   o.error = at; at = align_up(at + 4);
   o.unbounded = at; at = align_up(at + 4);
+  o.page_use = at; at = align_up(at + (size_t)c->num_pages * 8);
   o.meta_end = at;
   // Both decode kernels (the CUDA-core one for every cache but grouped bf16
   // queries of 2 to 8 per KV head, which run on the tensor-core kernel) keep
@@ -126,6 +132,14 @@ Offsets offsets(const dmc_cache_config* c) {
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+bool misaligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; }
+
+// Whether the current device is the cache's.
+bool on_device(const dmc_cache* c) {
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess && dev == c->device;
+}
 
 dmc_status cuda_status(cudaError_t e) { return e == cudaSuccess ? DMC_OK : DMC_ERR_CUDA; }
 
@@ -245,6 +259,7 @@ dmc_status dmc_cache_create(const dmc_cache_config* cfg, void* arena_dev, size_t
   L.pending_at = reinterpret_cast<int*>(base + o.pending_at);
   L.pending_z = reinterpret_cast<float*>(base + o.pending_z);
   L.pool_top = reinterpret_cast<unsigned long long*>(base + o.pool_top);
+  L.page_use = reinterpret_cast<int2*>(base + o.page_use);
   L.error = reinterpret_cast<unsigned int*>(base + o.error);
   L.unbounded = reinterpret_cast<unsigned int*>(base + o.unbounded);
   L.partials = reinterpret_cast<float*>(base + o.partials);
@@ -418,6 +433,51 @@ dmc_status dmc_decode_step_static_scratch(dmc_cache_t c, int32_t layer, const vo
                                         out_dev, stream));
 }
 
+dmc_status dmc_cache_append(dmc_cache_t c, int32_t layer, int32_t first_seq, int32_t num_seqs, const void* q_dev,
+                            const void* k_dev, const void* v_dev, const int32_t* cu_seqlens_dev, int32_t total_tokens,
+                            int32_t max_seqlen, const int32_t* positions_dev, const uint64_t* turns_dev,
+                            int32_t interleaved, void* q_out_dev, cudaStream_t stream) {
+  if (!c || !on_device(c)) return DMC_ERR_INVALID_ARG;
+  const Layout& L = c->lay;
+  if (layer < 0 || layer >= L.L || first_seq < 0 || num_seqs < 0 || num_seqs > L.B - first_seq) return DMC_ERR_INVALID_ARG;
+  if (total_tokens < 0 || max_seqlen < 0 || max_seqlen > total_tokens ||
+      (max_seqlen > 1 && total_tokens > L.max_prefill_tokens) || (max_seqlen <= 1 && total_tokens > num_seqs))
+    return DMC_ERR_INVALID_ARG;
+  if (!cu_seqlens_dev && total_tokens != num_seqs) return DMC_ERR_INVALID_ARG;
+  if (!cu_seqlens_dev && max_seqlen > 1) return DMC_ERR_INVALID_ARG;
+  if (num_seqs == 0 || total_tokens == 0) return total_tokens == 0 ? DMC_OK : DMC_ERR_INVALID_ARG;
+  if (max_seqlen == 0) return DMC_ERR_INVALID_ARG;
+  if (!aligned16(q_dev) || !aligned16(k_dev) || !aligned16(v_dev) || !q_dev || !k_dev || !v_dev) return DMC_ERR_INVALID_ARG;
+  if (turns_dev ? (!positions_dev || !q_out_dev || !aligned16(q_out_dev)) : (positions_dev || q_out_dev))
+    return DMC_ERR_INVALID_ARG;
+  if (misaligned(cu_seqlens_dev, 4) || misaligned(positions_dev, 4) || misaligned(turns_dev, 8)) return DMC_ERR_INVALID_ARG;
+  c->order.other();
+  return cuda_status(dmc::append_launch(L, layer, first_seq, num_seqs, q_dev, k_dev, v_dev, cu_seqlens_dev, total_tokens,
+                                        max_seqlen, positions_dev, reinterpret_cast<const unsigned long long*>(turns_dev),
+                                        interleaved != 0, q_out_dev, stream));
+}
+
+dmc_status dmc_cache_attend(dmc_cache_t c, int32_t layer, const void* q_dev, void* out_dev, cudaStream_t stream) {
+  if (!c || !on_device(c) || layer < 0 || layer >= c->lay.L) return DMC_ERR_INVALID_ARG;
+  if (!q_dev || !out_dev || !aligned16(q_dev) || !aligned16(out_dev) || q_dev == out_dev) return DMC_ERR_INVALID_ARG;
+  // it writes nothing but its layer's partial states, yet the decode after it must not take it for the decode before
+  c->order.other();
+  if (c->gqa)
+    return cuda_status(dmc::gqa_launch(c->lay, layer, 1, c->plan, false, q_dev, nullptr, nullptr, out_dev, stream));
+  return cuda_status(dmc::decode_launch(c->lay, layer, 1, c->Gv, c->plan, false, q_dev, nullptr, nullptr, out_dev, stream));
+}
+
+dmc_status dmc_cache_reorder(dmc_cache_t c, int32_t first_seq, int32_t num_seqs, const int32_t* parents_dev,
+                             cudaStream_t stream) {
+  if (!c || !on_device(c)) return DMC_ERR_INVALID_ARG;
+  if (first_seq < 0 || num_seqs < 0 || num_seqs > c->lay.B - first_seq || num_seqs > dmc::kReorderRows)
+    return DMC_ERR_INVALID_ARG;
+  if (num_seqs == 0) return DMC_OK;
+  if (!parents_dev || misaligned(parents_dev, 4)) return DMC_ERR_INVALID_ARG;
+  c->order.other();
+  return cuda_status(dmc::reorder_launch(c->lay, first_seq, num_seqs, parents_dev, stream));
+}
+
 dmc_status dmc_cache_lengths(dmc_cache_t c, int32_t layer, int32_t* out_dev, cudaStream_t stream) {
   if (!c || !out_dev || layer < 0 || layer >= c->lay.L) return DMC_ERR_INVALID_ARG;
   const int threads = 256, blocks = dmc::ceil_div(c->lay.NH, threads);
@@ -443,13 +503,13 @@ dmc_status dmc_cache_status(dmc_cache_t c, cudaStream_t stream, uint32_t* bits,
                             int64_t* pages_used) {
   if (!c) return DMC_ERR_INVALID_ARG;
   uint32_t b = 0;
-  unsigned long long top = 0;
+  unsigned long long top[2] = {0, 0};  // taken, given back
   cudaError_t e = cudaStreamSynchronize(stream);
   if (e == cudaSuccess) e = cudaMemcpy(&b, c->lay.error, 4, cudaMemcpyDeviceToHost);
-  if (e == cudaSuccess) e = cudaMemcpy(&top, c->lay.pool_top, 8, cudaMemcpyDeviceToHost);
+  if (e == cudaSuccess) e = cudaMemcpy(top, c->lay.pool_top, sizeof(top), cudaMemcpyDeviceToHost);
   if (e != cudaSuccess) return DMC_ERR_CUDA;
   if (bits) *bits = b;
-  if (pages_used) *pages_used = (int64_t)top;
+  if (pages_used) *pages_used = (int64_t)(top[0] - top[1]);
   if (b & DMC_FAULT_PAGES_EXHAUSTED) return DMC_ERR_PAGES_EXHAUSTED;
   if (b) return DMC_ERR_DEVICE_FAULT;
   return DMC_OK;

@@ -247,8 +247,10 @@ __device__ __noinline__ void write_pending(char* pages, float* z, int nh, const 
 
 // kWin: the cache uses the window-grouping approximation (L.window > 0);
 // NWARP: worker warps per block; kVirtual: several virtual heads per KV head (a kernel
-// of its own, since the code that only they need cost the others registers)
-template <typename T, int D, bool kWin, int NWARP, bool kVirtual>
+// of its own, since the code that only they need cost the others registers); kRead: the
+// cache is only read (dmc_cache_attend): no token joins it, so there are no owner units, and
+// a head without slots has no unit at all: its output is zero
+template <typename T, int D, bool kWin, int NWARP, bool kVirtual, bool kRead>
 __global__ void __launch_bounds__(NWARP * 32, 2)
 dmc_decode_kernel(const DecodeArgs a) {
   using G_ = DecodeGeom<T, D, NWARP>;
@@ -286,7 +288,7 @@ dmc_decode_kernel(const DecodeArgs a) {
 
   if (li > 0) __syncthreads();  // every warp is done with the previous layer's U and window
   // ---------------------------------------------------------------- prologue
-  scan_units(U, misc, ctl, L.lengths + (size_t)layer * 2 * L.NH, L.NH, NVH, Gv);
+  scan_units(U, misc, ctl, L.lengths + (size_t)layer * 2 * L.NH, L.NH, NVH, Gv, kRead ? 0 : 1);
   const long long Utot = U[NVH];
   // A layer with fewer units than warps gives the first Utot workers one unit
   // each, spread over the blocks so that every SM takes part. Such a launch is
@@ -320,7 +322,7 @@ dmc_decode_kernel(const DecodeArgs a) {
       if (u < u1) {
         const int hv = head_of_unit(U, NVH, u);
         const int j = u - U[hv];
-        if (j < U[hv + 1] - U[hv] - 1) {
+        if (kRead || j < U[hv + 1] - U[hv] - 1) {
           const int bh = hv / Gv;
           pid = ptab[(size_t)bh * L.MPH + j];
           rws = min(kPage, len_cur[bh] - j * kPage);
@@ -376,7 +378,7 @@ dmc_decode_kernel(const DecodeArgs a) {
     // the grid wait is over (7B shape, us per launch with the new token's rows
     // requested first: batch 1 10.9 -> 10.5, 4 17.5 -> 16.8, 8 21.6 -> 20.7, 32 49.1 ->
     // 48.7; without an overlap the look-up costs what it saves)
-    if (a.overlap && U[vh + 1] == u0 + 1 && last0 >= 0) {
+    if (!kRead && a.overlap && U[vh + 1] == u0 + 1 && last0 >= 0) {
       page0 = ptab[(size_t)bh0 * L.MPH + last0 / kPage];
       const char* row = L.pages + (size_t)page0 * L.page_bytes + (size_t)(last0 % kPage) * ROW;
       if (lane < 2 * NCH)
@@ -402,6 +404,14 @@ dmc_decode_kernel(const DecodeArgs a) {
     griddep_wait();
     griddep_launch_dependents();
   }
+  if constexpr (kRead) {
+    for (int hv = blockIdx.x * NWARP + warp; hv < NVH; hv += gridDim.x * NWARP) {
+      if (U[hv + 1] != U[hv]) continue;
+      const int bh = hv / Gv, b = bh / L.Hkv, h = bh % L.Hkv, g = hv % Gv;
+      char* row = outL + ((size_t)b * L.Hq + (size_t)h * L.G + g) * ROW;
+      for (int x = lane * 16; x < ROW; x += 32 * 16) *reinterpret_cast<uint4*>(row + x) = make_uint4(0, 0, 0, 0);
+    }
+  }
 
   if (u0 < u1) {
     // lane i holds the gates of head hb + i
@@ -416,12 +426,13 @@ dmc_decode_kernel(const DecodeArgs a) {
       if (hv < NVH && U[hv] < u1) {
         const int bh = hv / Gv, b = bh / L.Hkv, h = bh % L.Hkv;
         const int len = len_cur[bh];
+        t_len = len;
+        if constexpr (kRead) return;
         const float x = Elt<T>::to_f(reinterpret_cast<const T*>(kL)[(size_t)bh * D]);
         float qs = 0.f;
         for (int g = 0; g < L.G; ++g)
           qs += Elt<T>::to_f(
               reinterpret_cast<const T*>(qL)[((size_t)b * L.Hq + (size_t)h * L.G + g) * D]);
-        t_len = len;
         // alpha = round(sigmoid(k[0])) = [k[0] >= 0]; an empty head always appends
         t_flags = ((x >= 0.f && len > 0) ? kFlagAcc : 0) | ((x != x) ? kFlagNaN : 0);
         t_omega = sigmoidf_(qs / (float)L.G);  // omega = sigmoid(mean of the group's q[0])
@@ -450,7 +461,7 @@ dmc_decode_kernel(const DecodeArgs a) {
       const int u = u0 + k;
       while (U[vh + 1] <= u) ++vh;
       const int hu0 = U[vh], hend = U[vh + 1], nU = hend - hu0, j = u - hu0;
-      const bool owner = (j == nU - 1);
+      const bool last_unit = j == nU - 1, owner = !kRead && last_unit;
       const int bh = vh / Gv;
       if (k == 0 || j == 0) {
         if (vh - hb >= kHeadWindow) load_heads(vh);
@@ -467,14 +478,18 @@ dmc_decode_kernel(const DecodeArgs a) {
         }
         if (l8 == 0) qf[0] = 0.f;  // q[0] is the importance gate, not a feature
         // prefetch the query of the head that follows in this range
-        const int next = hend < u1 ? vh + 1 : -1;
+        int next = hend < u1 ? vh + 1 : -1;
+        if constexpr (kRead) {
+          if (next >= 0)
+            while (U[next + 1] == hend) ++next;  // heads without slots
+        }
         if (next >= 0) {
 #pragma unroll
           for (int c = 0; c < NCH; ++c)
             qraw[c] = __ldg(reinterpret_cast<const uint4*>(q_ptr(next) + c * 128));
         }
       }
-      const int accum = flags & kFlagAcc;
+      const int accum = kRead ? 0 : flags & kFlagAcc;
       if (!owner) {
         const int rows_copied = min(kPage, len_old - j * kPage);
         const int rows = min(kPage, len_old - accum - j * kPage);  // the merged slot is excluded
@@ -679,14 +694,8 @@ dmc_decode_kernel(const DecodeArgs a) {
           int page = tgt;
           if (ok && page < 0) {
             if (l8 == 0) {
-              const unsigned long long id = atomicAdd(L.pool_top, 1ull);
-              if (id >= (unsigned long long)L.num_pages) {
-                atomicOr(L.error, DMC_FAULT_PAGES_EXHAUSTED);
-                page = -1;
-              } else {
-                page = (int)id;
-                ptab[(size_t)bh * L.MPH + slot / kPage] = page;
-              }
+              page = take_page(L);
+              if (page >= 0) ptab[(size_t)bh * L.MPH + slot / kPage] = page;
             }
             page = __shfl_sync(gmask, page, 0, 8);
           }
@@ -737,7 +746,7 @@ dmc_decode_kernel(const DecodeArgs a) {
         }
       }
 
-      if (owner || k == n - 1) {
+      if (last_unit || k == n - 1) {
         // ---- this warp's part of the head is done: merge its 4 groups
 #pragma unroll
         for (int off = 8; off < 32; off <<= 1) {
@@ -812,6 +821,7 @@ dmc_decode_kernel(const DecodeArgs a) {
     }
   }
   cp_async_wait<0>();
+  if constexpr (kRead) continue;
 
   __syncthreads();
   if (tid == 0) {
@@ -836,22 +846,26 @@ dmc_decode_kernel(const DecodeArgs a) {
   }  // layers
 }
 
-// Shared memory and blocks per SM of one warp count (both window variants).
+// Shared memory and blocks per SM of one warp count (both window variants; the reading
+// one, which does less, runs on the same grid).
 template <typename T, int D, int NWARP, bool kVirtual>
 static cudaError_t setup_warps(int nvh, int optin, size_t* smem, int* occ) {
   *smem = DecodeGeom<T, D, NWARP>::smem_bytes(nvh);
   if (*smem > (size_t)optin) return cudaErrorInvalidConfiguration;
-  cudaError_t e = cudaFuncSetAttribute(dmc_decode_kernel<T, D, false, NWARP, kVirtual>,
+  cudaError_t e = cudaFuncSetAttribute(dmc_decode_kernel<T, D, false, NWARP, kVirtual, false>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, (int)*smem);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(dmc_decode_kernel<T, D, true, NWARP, kVirtual>,
+    e = cudaFuncSetAttribute(dmc_decode_kernel<T, D, true, NWARP, kVirtual, false>,
+                             cudaFuncAttributeMaxDynamicSharedMemorySize, (int)*smem);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(dmc_decode_kernel<T, D, false, NWARP, kVirtual, true>,
                              cudaFuncAttributeMaxDynamicSharedMemorySize, (int)*smem);
   int o = 0, ow = 0;
   if (e == cudaSuccess)
-    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&o, dmc_decode_kernel<T, D, false, NWARP, kVirtual>, NWARP * 32,
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&o, dmc_decode_kernel<T, D, false, NWARP, kVirtual, false>, NWARP * 32,
                                                       *smem);
   if (e == cudaSuccess)
-    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ow, dmc_decode_kernel<T, D, true, NWARP, kVirtual>, NWARP * 32,
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ow, dmc_decode_kernel<T, D, true, NWARP, kVirtual, false>, NWARP * 32,
                                                       *smem);
   if (e != cudaSuccess) return e;
   *occ = min(o, ow);
@@ -924,11 +938,14 @@ static cudaError_t launch_warps(const DecodeArgs& a, int grid, size_t smem, bool
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pdl ? 1 : 0;
+  if (a.k == nullptr)
+    return a.Gv > 1 ? cudaLaunchKernelEx(&cfg, dmc_decode_kernel<T, D, false, NWARP, true, true>, a)
+                    : cudaLaunchKernelEx(&cfg, dmc_decode_kernel<T, D, false, NWARP, false, true>, a);
   if (a.Gv > 1)
-    return a.lay.window > 0 ? cudaLaunchKernelEx(&cfg, dmc_decode_kernel<T, D, true, NWARP, true>, a)
-                            : cudaLaunchKernelEx(&cfg, dmc_decode_kernel<T, D, false, NWARP, true>, a);
-  return a.lay.window > 0 ? cudaLaunchKernelEx(&cfg, dmc_decode_kernel<T, D, true, NWARP, false>, a)
-                          : cudaLaunchKernelEx(&cfg, dmc_decode_kernel<T, D, false, NWARP, false>, a);
+    return a.lay.window > 0 ? cudaLaunchKernelEx(&cfg, dmc_decode_kernel<T, D, true, NWARP, true, false>, a)
+                            : cudaLaunchKernelEx(&cfg, dmc_decode_kernel<T, D, false, NWARP, true, false>, a);
+  return a.lay.window > 0 ? cudaLaunchKernelEx(&cfg, dmc_decode_kernel<T, D, true, NWARP, false, false>, a)
+                          : cudaLaunchKernelEx(&cfg, dmc_decode_kernel<T, D, false, NWARP, false, false>, a);
 }
 
 template <typename T, int D>
@@ -940,6 +957,7 @@ static cudaError_t launch_decode(const DecodeArgs& a, const DecodePlan& plan, bo
   return launch_warps<T, D, kWarpsOne>(a, plan.grid, plan.smem, pdl, stream);
 }
 
+// k and v null: the cache is only read.
 cudaError_t decode_launch(const Layout& L, int layer0, int nlayers, int Gv, const DecodePlan& plan,
                           bool pdl, const void* q, const void* k, const void* v, void* out,
                           cudaStream_t stream) {

@@ -175,8 +175,10 @@ __device__ __noinline__ void combine_gqa(const float* partials, int wf, int firs
     *reinterpret_cast<uint32_t*>(ob + (size_t)g * D + 8 * i + 2 * t) = pack_bf16x2(o[i].x * inv, o[i].y * inv);
 }
 
-// kWin: the cache uses the window-grouping approximation (L.window > 0)
-template <int D, bool kWin, int RING>
+// kWin: the cache uses the window-grouping approximation (L.window > 0); kRead: the cache
+// is only read (dmc_cache_attend), one layer of it: there are no owner units, and a head
+// without slots has no unit at all: its output is zero
+template <int D, bool kWin, int RING, bool kRead>
 __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaArgs a) {
   using G_ = GqaGeom<D, RING>;
   constexpr int ROW = G_::ROW, CPR = G_::CPR, KT = G_::KT;
@@ -200,7 +202,8 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
   // part of the current one is done: the block builds the first two layers'
   // unit prefixes here, and the last of its warps to leave layer li builds
   // layer li + 2's into the buffer it frees.
-  scan_units(Ubuf, misc, L.ctl + a.layer0 * 4, L.lengths + (size_t)a.layer0 * 2 * NH, NH, NH, 1);
+  scan_units(Ubuf, misc, L.ctl + a.layer0 * 4, L.lengths + (size_t)a.layer0 * 2 * NH, NH, NH, 1,
+             kRead ? 0 : 1);
   if (a.nlayers > 1)
     scan_units(Ubuf + NH + 1, misc, L.ctl + (a.layer0 + 1) * 4,
                L.lengths + (size_t)(a.layer0 + 1) * 2 * NH, NH, NH, 1);
@@ -267,7 +270,7 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
       if (u < u1) {
         const int hv = head_of_unit(U, NH, u);
         const int j = u - U[hv];
-        if (j < U[hv + 1] - U[hv] - 1) {
+        if (kRead || j < U[hv + 1] - U[hv] - 1) {
           pid = ptab[(size_t)hv * L.MPH + j];
           rws = min(kPage, len_cur[hv] - j * kPage);
         }
@@ -330,7 +333,7 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
     // the grid wait is over (64 query heads over 8, us per launch, with the new row
     // and z requested before the reserved tile: batch 1 18.3 -> 17.7, 4 21.8 -> 20.3,
     // 64 90.4 -> 89.7)
-    if (a.overlap && U[vh + 1] == u0 + 1 && last0 >= 0) {
+    if (!kRead && a.overlap && U[vh + 1] == u0 + 1 && last0 >= 0) {
       page0 = ptab[(size_t)vh * L.MPH + last0 / kPage];
       const char* row = L.pages + (size_t)page0 * L.page_bytes + (size_t)(last0 % kPage) * ROW;
       constexpr int NL = ROW / 128;
@@ -346,6 +349,13 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
     griddep_wait();
     griddep_launch_dependents();
   }
+  if constexpr (kRead) {
+    for (int hv = blockIdx.x * kGWarps + warp; hv < NH; hv += NWG) {
+      if (U[hv + 1] != U[hv]) continue;
+      char* rows = outL + ((size_t)(hv / L.Hkv) * L.Hq + (size_t)(hv % L.Hkv) * G) * ROW;
+      for (int x = lane * 16; x < G * ROW; x += 32 * 16) *reinterpret_cast<uint4*>(rows + x) = make_uint4(0, 0, 0, 0);
+    }
+  }
 
   if (n > 0) {
     // lane i holds the gates of KV head hb + i
@@ -360,12 +370,13 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
       if (hv < NH && U[hv] < u1) {
         const int b = hv / L.Hkv, h = hv % L.Hkv;
         const int len = len_cur[hv];
+        t_len = len;
+        if constexpr (kRead) return;
         const float x = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(kL)[(size_t)hv * D]);
         float qs = 0.f;
         for (int gg = 0; gg < G; ++gg)
           qs += __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(
               qL)[((size_t)b * L.Hq + (size_t)h * G + gg) * D]);
-        t_len = len;
         // alpha = round(sigmoid(k[0])) = [k[0] >= 0]; an empty head always appends
         t_flags = ((x >= 0.f && len > 0) ? kGFlagAcc : 0) | ((x != x) ? kGFlagNaN : 0);
         t_omega = sigmoidf_(qs / (float)G);  // omega = sigmoid(mean of the group's q[0])
@@ -467,7 +478,7 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
       const int u = u0 + k;
       while (U[vh + 1] <= u) ++vh;
       const int hu0 = U[vh], hend = U[vh + 1], nU = hend - hu0, j = u - hu0;
-      const bool owner = (j == nU - 1);
+      const bool last_unit = j == nU - 1, owner = !kRead && last_unit;
       if (k == 0 || j == 0) {
         if (vh - hb >= kGHeadWindow) load_heads(vh);
         const int src = vh - hb;
@@ -480,9 +491,14 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
           qa[kk][1] = qn[kk][1];
         }
         if (t == 0) qa[0][0] &= 0xffff0000u;  // q[0] (low half of dims 0, 1) is the gate
-        if (hend < u1) load_q(vh + 1, qn);    // the next head's queries, ahead of use
+        if (hend < u1) {  // the next head's queries, ahead of use
+          int next = vh + 1;
+          if constexpr (kRead)
+            while (U[next + 1] == hend) ++next;  // heads without slots
+          load_q(next, qn);
+        }
       }
-      const int accum = flags & kGFlagAcc;
+      const int accum = kRead ? 0 : flags & kGFlagAcc;
       if (!owner) {
         const int rows_copied = min(kPage, len_old - j * kPage);
         const int rows = min(kPage, len_old - accum - j * kPage);  // the merged slot is excluded
@@ -592,14 +608,8 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
         int page = tgt;
         if (ok && page < 0) {
           if (lane == 0) {
-            const unsigned long long id = atomicAdd(L.pool_top, 1ull);
-            if (id >= (unsigned long long)L.num_pages) {
-              atomicOr(L.error, DMC_FAULT_PAGES_EXHAUSTED);
-              page = -1;
-            } else {
-              page = (int)id;
-              ptab[(size_t)vh * L.MPH + slot / kPage] = page;
-            }
+            page = take_page(L);
+            if (page >= 0) ptab[(size_t)vh * L.MPH + slot / kPage] = page;
           }
           page = __shfl_sync(0xffffffffu, page, 0);
         }
@@ -632,12 +642,12 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
         do_tile(tile, 1, false);
       }
 
-      if (owner || k == n - 1) {
+      if (last_unit || k == n - 1) {
         // ---- this warp's part of the head is done
         const int b = vh / L.Hkv, h = vh % L.Hkv;
         __nv_bfloat16* ob = reinterpret_cast<__nv_bfloat16*>(outL) + ((size_t)b * L.Hq + (size_t)h * G) * D;
         const int q_lo = 2 * t, q_hi = 2 * t + 1;
-        if (hu0 >= u0 && owner) {
+        if (hu0 >= u0 && last_unit) {
           // the whole head was in this warp
           const float l_lo = __shfl_sync(0xffffffffu, lsum, 8 * t);
           const float l_hi = __shfl_sync(0xffffffffu, lsum, 8 * t + 4);
@@ -703,6 +713,7 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
     }
   }
   cp_async_wait<0>();
+  if constexpr (kRead) continue;
 
   // this warp is done with the layer: the grid's last warp out publishes the
   // new slot counts; the block's last warp out builds the prefix of layer
@@ -733,21 +744,25 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
   }  // layers
 }
 
-// Shared memory and blocks per SM with one ring depth (both window variants).
+// Shared memory and blocks per SM with one ring depth (both window variants; the reading
+// one, which does less, runs on the same grid).
 template <int D, int RING>
 static cudaError_t setup_ring(int nh, int optin, size_t* smem, int* occ) {
   *smem = GqaGeom<D, RING>::smem_bytes(nh);
   if (*smem > (size_t)optin) return cudaErrorInvalidConfiguration;
-  cudaError_t e = cudaFuncSetAttribute(dmc_decode_gqa_kernel<D, false, RING>,
+  cudaError_t e = cudaFuncSetAttribute(dmc_decode_gqa_kernel<D, false, RING, false>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, (int)*smem);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(dmc_decode_gqa_kernel<D, true, RING>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    e = cudaFuncSetAttribute(dmc_decode_gqa_kernel<D, true, RING, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)*smem);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(dmc_decode_gqa_kernel<D, false, RING, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              (int)*smem);
   int o = 0, ow = 0;
   if (e == cudaSuccess)
-    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&o, dmc_decode_gqa_kernel<D, false, RING>, kGThreads, *smem);
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&o, dmc_decode_gqa_kernel<D, false, RING, false>, kGThreads, *smem);
   if (e == cudaSuccess)
-    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ow, dmc_decode_gqa_kernel<D, true, RING>, kGThreads, *smem);
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ow, dmc_decode_gqa_kernel<D, true, RING, false>, kGThreads, *smem);
   if (e != cudaSuccess) return e;
   *occ = min(o, ow);
   return *occ < 1 ? cudaErrorInvalidConfiguration : cudaSuccess;
@@ -792,13 +807,17 @@ cudaError_t gqa_setup(const Layout& L, DecodePlan* plan) {
 
 template <int D>
 static cudaError_t launch_gqa(const cudaLaunchConfig_t& cfg, const DecodePlan& plan, const GqaArgs& a) {
+  if (a.k == nullptr)
+    return plan.stages == kGRing ? cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, false, kGRing, true>, a)
+                                 : cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, false, kGRingMany, true>, a);
   if (plan.stages == kGRing)
-    return a.lay.window > 0 ? cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, true, kGRing>, a)
-                            : cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, false, kGRing>, a);
-  return a.lay.window > 0 ? cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, true, kGRingMany>, a)
-                          : cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, false, kGRingMany>, a);
+    return a.lay.window > 0 ? cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, true, kGRing, false>, a)
+                            : cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, false, kGRing, false>, a);
+  return a.lay.window > 0 ? cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, true, kGRingMany, false>, a)
+                          : cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, false, kGRingMany, false>, a);
 }
 
+// k and v null: the cache is only read.
 cudaError_t gqa_launch(const Layout& L, int layer0, int nlayers, const DecodePlan& plan, bool pdl,
                        const void* q, const void* k, const void* v, void* out, cudaStream_t stream) {
   GqaArgs a;

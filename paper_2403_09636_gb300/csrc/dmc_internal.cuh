@@ -40,7 +40,9 @@ struct Layout {
   char* pending;           // [L][NH][2][D]: grouped queries: new last rows awaiting the layer's end
   int* pending_at;         // [L][NH]: their slot (page * 32 + row), -1 = none
   float* pending_z;        // [L][NH]: their z
-  unsigned long long* pool_top;
+  unsigned long long* pool_top;  // [4]: pages taken, pages given back, of those by the running launch too, its blocks done
+  int2* page_use;          // [num_pages]: x: heads that hold the page beside the first (reordered sequences share what
+                           // they have in common); y: the given back page of that turn (see take_page)
   unsigned int* error;
   unsigned int* unbounded; // prompt attention: the call has written a slot whose value is not finite
   float* partials;         // [partial_cap][D + 2]: split-K partial softmax states (m, l, acc)
@@ -148,6 +150,24 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   return d;
 }
 
+// The page of place `at` in the order in which pages are taken: 0, 1, ... num_pages - 1, then those given back,
+// first come first served. Place num_pages + i is the i-th page given back, kept at entry i % num_pages (there are
+// never more than num_pages of them waiting).
+__device__ __forceinline__ int page_in_turn(const Layout& L, unsigned long long at) {
+  return at < (unsigned long long)L.num_pages ? (int)at : L.page_use[at % (unsigned long long)L.num_pages].y;
+}
+// Whether the places [at, at + n) exist yet. (What a launch gives back can be taken by later ones.)
+__device__ __forceinline__ bool pages_in_pool(const Layout& L, unsigned long long at, unsigned long long n) {
+  return at + n <= (unsigned long long)L.num_pages || at + n <= (unsigned long long)L.num_pages + L.pool_top[1];
+}
+// One page for a head, or -1 with the fault bit set.
+__device__ __forceinline__ int take_page(const Layout& L) {
+  const unsigned long long at = atomicAdd(L.pool_top, 1ull);
+  if (pages_in_pool(L, at, 1)) return page_in_turn(L, at);
+  atomicOr(L.error, DMC_FAULT_PAGES_EXHAUSTED);
+  return -1;
+}
+
 __device__ __forceinline__ float sigmoidf_(float x) { return 1.0f / (1.0f + __expf(-x)); }
 
 // ---------------------------------------------------------------- PTX: mbarrier, cp.async, mma
@@ -253,6 +273,10 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
 // cp.async (LDGSTS) of 16 bytes, L2 only, into this thread's shared memory.
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// The same of 8 bytes, through L1 (the only form for fewer than 16).
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() {
   asm volatile("cp.async.commit_group;" ::: "memory");

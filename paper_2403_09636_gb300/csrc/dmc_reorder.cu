@@ -1,0 +1,215 @@
+// Reordering of a cache's sequences: sequence first + j continues from the cache of sequence first + parents[j], as
+// beam search has it after each selection (and as sampling several continuations of one prompt has it once).
+//
+// A slot is never written again once the head has opened a slot on a later page (Algorithm 1 changes the last slot
+// alone), so copies of a sequence share every page but the last: only the page table's entries are copied, and a
+// count beside the pool says how many heads hold a page beside the first. The page of the last slot has one holder:
+// the first of a sequence's heirs (itself, where it stays) keeps it, every other heir gets a page of its own with the
+// rows copied. There are as many of those as sequences that nobody continues, whose last pages they take; where such
+// a sequence was empty, they take one from the pool. Pages that nobody holds any more go back to the pool.
+//
+// One block per (layer, KV head), which holds the counts of its pages alone: sequences only ever share pages of one
+// layer and head. Bound by latency: the parents, lengths and last entries, a page's rows and the shares of the table
+// are four trips to memory, one after the other.
+#include "dmc_internal.cuh"
+#include "dmc_reorder.h"
+
+namespace dmc {
+
+namespace {
+
+constexpr int kReorderThreads = 256;
+constexpr int kStage = 4096;  // entries of the page table that a block holds at a time
+constexpr int kNobody = 0x7fffffff;
+
+struct ReorderArgs {
+  Layout lay;
+  int first, n;
+  const int* parents;
+};
+
+// Row j's numbers in shared memory.
+struct Row {
+  int parent;    // who it continues
+  int heir;      // of row j: its first heir, j itself as -1; kNobody where nobody continues it
+  int len, len_new;
+  int last;      // its last page
+  int last_new;
+};
+
+// Copies rows [0, rows) of K and V and their z from page src to page dst, by a warp.
+__device__ __forceinline__ void copy_page(const Layout& L, int src, int dst, int rows, int lane) {
+  const char* from = L.pages + (size_t)src * L.page_bytes;
+  char* to = L.pages + (size_t)dst * L.page_bytes;
+  const int half = kPage * L.row_bytes;
+  for (int x = lane * 16; x < rows * L.row_bytes; x += 32 * 16) {
+    *reinterpret_cast<uint4*>(to + x) = *reinterpret_cast<const uint4*>(from + x);
+    *reinterpret_cast<uint4*>(to + half + x) = *reinterpret_cast<const uint4*>(from + half + x);
+  }
+  if (lane < rows) L.z[(size_t)dst * kPage + lane] = L.z[(size_t)src * kPage + lane];
+}
+
+__device__ __forceinline__ void give_back(const Layout& L, int page) {
+  const unsigned long long at = atomicAdd(L.pool_top + 2, 1ull);
+  L.page_use[at % (unsigned long long)L.num_pages].y = page;
+}
+
+// The window's tokens (window grouping), `per` pieces of T for each row: row j gets its parent's. All rows' pieces
+// [x0, x0 + w) pass through shared memory together.
+template <typename T>
+__device__ void move_pieces(T* stage, const Row* rows, int n, T* base, size_t row_stride, int per) {
+  const int w = max(1, min(per, (int)(kStage * sizeof(int) / sizeof(T)) / n));
+  for (int x0 = 0; x0 < per; x0 += w) {
+    const int m = min(w, per - x0);
+    for (int i = threadIdx.x; i < n * m; i += kReorderThreads)
+      stage[i] = base[(size_t)(i / m) * row_stride + x0 + i % m];
+    __syncthreads();
+    for (int i = threadIdx.x; i < n * m; i += kReorderThreads) {
+      const int j = i / m;
+      if (rows[j].parent != j) base[(size_t)j * row_stride + x0 + i % m] = stage[rows[j].parent * m + i % m];
+    }
+    __syncthreads();
+  }
+}
+
+__global__ void __launch_bounds__(kReorderThreads) dmc_reorder_kernel(const ReorderArgs a) {
+  __shared__ Row rows[kReorderRows];
+  __shared__ int extra[kReorderRows], dead[kReorderRows];  // rows that need a last page, rows that give theirs
+  __shared__ __align__(16) int stage[kStage];
+  __shared__ int s_extras, s_deads, s_pages;
+  const Layout& L = a.lay;
+  const int n = a.n, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int layer = blockIdx.y, h = blockIdx.x;
+  const int parity = *reinterpret_cast<const volatile int*>(&L.ctl[layer * 4]);
+  const size_t head0 = (size_t)a.first * L.Hkv + h;  // row j's head of the layer: head0 + j * Hkv
+  int* len = L.lengths + ((size_t)layer * 2 + parity) * L.NH + head0;
+  int* table = L.page_table + ((size_t)layer * L.NH + head0) * L.MPH;
+  const size_t table_row = (size_t)L.Hkv * L.MPH;
+
+  bool moved = false;
+  for (int j = tid; j < n; j += kReorderThreads) {
+    int p = a.parents[j];
+    if (p < 0 || p >= n) {
+      atomicOr(L.error, DMC_FAULT_BAD_PARENT);
+      p = j;
+    }
+    const int l = len[(size_t)j * L.Hkv];
+    rows[j] = Row{p, kNobody, l, l, -1, -1};
+    moved |= p != j;
+  }
+  if (!__syncthreads_or(moved)) return;
+  for (int j = tid; j < n; j += kReorderThreads) {
+    const int p = rows[j].parent, l = rows[j].len;
+    atomicMin(&rows[p].heir, p == j ? -1 : j);
+    if (l > 0) rows[j].last = table[(size_t)j * table_row + (l - 1) / kPage];
+  }
+  __syncthreads();
+  if (warp == 0) {  // the lists, in the rows' order
+    int extras = 0, deads = 0, pages = 0;
+    for (int j0 = 0; j0 < n; j0 += 32) {
+      const int j = j0 + lane;
+      bool ex = false, de = false;
+      if (j < n) {
+        const Row r = rows[j];
+        ex = rows[r.parent].heir != (r.parent == j ? -1 : j) && rows[r.parent].len > 0;
+        de = r.heir == kNobody && r.len > 0;
+        pages = max(pages, ceil_div(r.len, kPage));
+      }
+      const unsigned eb = __ballot_sync(0xffffffffu, ex), db = __ballot_sync(0xffffffffu, de);
+      const unsigned below = (1u << lane) - 1u;
+      if (ex) extra[extras + __popc(eb & below)] = j;
+      if (de) dead[deads + __popc(db & below)] = j;
+      extras += __popc(eb);
+      deads += __popc(db);
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) pages = max(pages, __shfl_xor_sync(0xffffffffu, pages, off));
+    if (lane == 0) {
+      s_extras = extras;
+      s_deads = deads;
+      s_pages = pages;
+    }
+  }
+  for (int j = tid; j < n; j += kReorderThreads) {
+    const int p = rows[j].parent;
+    rows[j].len_new = rows[p].len;
+    rows[j].last_new = rows[p].last;  // its heir's; the others' below
+  }
+  __syncthreads();
+  const int extras = s_extras, deads = s_deads, pages = s_pages;
+  for (int i = tid; i < max(extras, deads); i += kReorderThreads) {
+    if (i >= extras) {
+      give_back(L, rows[dead[i]].last);
+      continue;
+    }
+    const int page = i < deads ? rows[dead[i]].last : take_page(L);
+    rows[extra[i]].last_new = page;
+    if (page < 0) rows[extra[i]].len_new = 0;  // the pool is empty: so is the sequence (the fault bit is set)
+  }
+  __syncthreads();
+  for (int i = warp; i < extras; i += kReorderThreads / 32) {
+    const Row r = rows[extra[i]];
+    if (r.last_new >= 0) copy_page(L, rows[r.parent].last, r.last_new, (r.len_new - 1) % kPage + 1, lane);
+  }
+
+  // the pages before the last: holders first come, then go, so that no page that stays in use is given back
+  const int w = max(1, min(pages, kStage / n));
+  for (int i0 = 0; i0 < pages - 1; i0 += w) {
+    const int m = min(w, pages - 1 - i0);
+    for (int x = tid; x < n * m; x += kReorderThreads) {
+      const int j = x / m, i = i0 + x % m;
+      stage[x] = i < ceil_div(rows[j].len, kPage) - 1 ? table[(size_t)j * table_row + i] : -1;
+    }
+    __syncthreads();
+    for (int x = tid; x < n * m; x += kReorderThreads) {
+      const int j = x / m, i = i0 + x % m, p = rows[j].parent;
+      if (p == j || i >= ceil_div(rows[j].len_new, kPage) - 1) continue;
+      const int page = stage[p * m + x % m];
+      if (page == stage[x]) continue;  // shared already
+      atomicAdd(&L.page_use[page].x, 1);
+      table[(size_t)j * table_row + i] = page;
+    }
+    __threadfence();
+    __syncthreads();
+    for (int x = tid; x < n * m; x += kReorderThreads) {
+      const int j = x / m, i = i0 + x % m, p = rows[j].parent;
+      const int page = stage[x];
+      if (p == j || page < 0) continue;
+      if (i < ceil_div(rows[j].len_new, kPage) - 1 && stage[p * m + x % m] == page) continue;
+      if (atomicSub(&L.page_use[page].x, 1) == 0) {  // the last holder
+        atomicExch(&L.page_use[page].x, 0);
+        give_back(L, page);
+      }
+    }
+    __syncthreads();
+  }
+  for (int j = tid; j < n; j += kReorderThreads) {
+    const Row r = rows[j];
+    if (r.parent == j) continue;
+    if (r.len_new > 0) table[(size_t)j * table_row + (r.len_new - 1) / kPage] = r.last_new;
+    len[(size_t)j * L.Hkv] = r.len_new;
+  }
+  if (L.window > 0) {
+    __syncthreads();
+    const size_t head = (size_t)layer * L.NH + head0;
+    move_pieces(stage, rows, n, L.seglen + ((size_t)layer * 2 + parity) * L.NH + head0, L.Hkv, 1);
+    move_pieces(reinterpret_cast<float*>(stage), rows, n, L.ring_w + head * L.window, (size_t)L.Hkv * L.window, L.window);
+    const int pieces = L.window * 2 * L.row_bytes / 16;
+    move_pieces(reinterpret_cast<uint4*>(stage), rows, n, reinterpret_cast<uint4*>(L.ring) + head * pieces,
+                (size_t)L.Hkv * pieces, pieces);
+  }
+}
+
+// What the launch before gave back can be taken from here on.
+__global__ void dmc_reorder_done_kernel(unsigned long long* pool) { pool[1] = pool[2]; }
+
+}  // namespace
+
+cudaError_t reorder_launch(const Layout& L, int first, int n, const int* parents, cudaStream_t stream) {
+  const ReorderArgs a{L, first, n, parents};
+  dmc_reorder_kernel<<<dim3(L.Hkv, L.L), kReorderThreads, 0, stream>>>(a);
+  dmc_reorder_done_kernel<<<1, 1, 0, stream>>>(L.pool_top);
+  return cudaGetLastError();
+}
+
+}  // namespace dmc
