@@ -8,9 +8,10 @@
 // rows copied. There are as many of those as sequences that nobody continues, whose last pages they take; where such
 // a sequence was empty, they take one from the pool. Pages that nobody holds any more go back to the pool.
 //
-// One block per (layer, KV head), which holds the counts of its pages alone: sequences only ever share pages of one
-// layer and head. Bound by latency: the parents, lengths and last entries, a page's rows and the shares of the table
-// are four trips to memory, one after the other.
+// Two kernels. The first, a block per (layer, KV head), does the tables and the counts, alone for its pages: sequences
+// only ever share pages of one layer and head. It leaves a list of the pages to copy (in the scratch of the layer's
+// split attention), which the second spreads over the GPU. Bound by latency: parents, lengths, last entries and the
+// table's shares are trips to memory one after the other, then the pages.
 #include "dmc_internal.cuh"
 #include "dmc_reorder.h"
 
@@ -21,6 +22,7 @@ namespace {
 constexpr int kReorderThreads = 256;
 constexpr int kStage = 4096;  // entries of the page table that a block holds at a time
 constexpr int kNobody = 0x7fffffff;
+constexpr int kCopyBlocks = 1216;  // of the copying kernel, where the heads leave room for more than one each
 
 struct ReorderArgs {
   Layout lay;
@@ -37,16 +39,12 @@ struct Row {
   int last_new;
 };
 
-// Copies rows [0, rows) of K and V and their z from page src to page dst, by a warp.
-__device__ __forceinline__ void copy_page(const Layout& L, int src, int dst, int rows, int lane) {
-  const char* from = L.pages + (size_t)src * L.page_bytes;
-  char* to = L.pages + (size_t)dst * L.page_bytes;
-  const int half = kPage * L.row_bytes;
-  for (int x = lane * 16; x < rows * L.row_bytes; x += 32 * 16) {
-    *reinterpret_cast<uint4*>(to + x) = *reinterpret_cast<const uint4*>(from + x);
-    *reinterpret_cast<uint4*>(to + half + x) = *reinterpret_cast<const uint4*>(from + half + x);
-  }
-  if (lane < rows) L.z[(size_t)dst * kPage + lane] = L.z[(size_t)src * kPage + lane];
+// A layer's lists of copies: the number of each KV head's, then n places of each head: (from, to, rows).
+__device__ __forceinline__ int* copy_counts(const Layout& L, int layer) {
+  return reinterpret_cast<int*>(L.partials + (size_t)layer * L.partials_layer_stride);
+}
+__device__ __forceinline__ int4* copies(const Layout& L, int layer, int h, int n) {
+  return reinterpret_cast<int4*>(copy_counts(L, layer) + (L.Hkv + 3) / 4 * 4) + (size_t)h * n;
 }
 
 __device__ __forceinline__ void give_back(const Layout& L, int page) {
@@ -97,7 +95,11 @@ __global__ void __launch_bounds__(kReorderThreads) dmc_reorder_kernel(const Reor
     rows[j] = Row{p, kNobody, l, l, -1, -1};
     moved |= p != j;
   }
-  if (!__syncthreads_or(moved)) return;
+  griddep_launch_dependents();  // the copying kernel may start its blocks
+  if (!__syncthreads_or(moved)) {
+    if (tid == 0) copy_counts(L, layer)[h] = 0;
+    return;
+  }
   for (int j = tid; j < n; j += kReorderThreads) {
     const int p = rows[j].parent, l = rows[j].len;
     atomicMin(&rows[p].heir, p == j ? -1 : j);
@@ -143,14 +145,13 @@ __global__ void __launch_bounds__(kReorderThreads) dmc_reorder_kernel(const Reor
       continue;
     }
     const int page = i < deads ? rows[dead[i]].last : take_page(L);
-    rows[extra[i]].last_new = page;
-    if (page < 0) rows[extra[i]].len_new = 0;  // the pool is empty: so is the sequence (the fault bit is set)
+    Row& r = rows[extra[i]];
+    r.last_new = page;
+    if (page < 0) r.len_new = 0;  // the pool is empty: so is the sequence (the fault bit is set)
+    copies(L, layer, h, n)[i] = make_int4(rows[r.parent].last, page, page < 0 ? 0 : (r.len_new - 1) % kPage + 1, 0);
   }
+  if (tid == 0) copy_counts(L, layer)[h] = extras;
   __syncthreads();
-  for (int i = warp; i < extras; i += kReorderThreads / 32) {
-    const Row r = rows[extra[i]];
-    if (r.last_new >= 0) copy_page(L, rows[r.parent].last, r.last_new, (r.len_new - 1) % kPage + 1, lane);
-  }
 
   // the pages before the last: holders first come, then go, so that no page that stays in use is given back
   const int w = max(1, min(pages, kStage / n));
@@ -200,16 +201,62 @@ __global__ void __launch_bounds__(kReorderThreads) dmc_reorder_kernel(const Reor
   }
 }
 
-// What the launch before gave back can be taken from here on.
-__global__ void dmc_reorder_done_kernel(unsigned long long* pool) { pool[1] = pool[2]; }
+// Copies rows [0, rows) of K and V and their z from page to page; what the launch before gave back can be taken from
+// here on.
+constexpr int kCopyThreads = 256;
+__global__ void __launch_bounds__(kCopyThreads) dmc_reorder_copy_kernel(const ReorderArgs a) {
+  const Layout& L = a.lay;
+  const int tid = threadIdx.x, h = blockIdx.y, layer = blockIdx.z;
+  griddep_wait();
+  if (tid == 0 && (blockIdx.x | blockIdx.y | blockIdx.z) == 0) L.pool_top[1] = L.pool_top[2];
+  const int count = copy_counts(L, layer)[h], half = kPage * L.row_bytes;
+  for (int i = blockIdx.x; i < count; i += gridDim.x) {
+    const int4 c = copies(L, layer, h, a.n)[i];
+    const char* from = L.pages + (size_t)c.x * L.page_bytes;
+    char* to = L.pages + (size_t)c.y * L.page_bytes;
+    const int all = c.z * L.row_bytes;
+    if (tid < c.z) L.z[(size_t)c.y * kPage + tid] = L.z[(size_t)c.x * kPage + tid];
+    constexpr int U = 2;  // of each half in flight: a page of 256-byte rows in one go
+    for (int x0 = tid * 16; x0 < all; x0 += U * kCopyThreads * 16) {
+      uint4 k[U], v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int x = x0 + u * kCopyThreads * 16;
+        if (x < all) {
+          k[u] = *reinterpret_cast<const uint4*>(from + x);
+          v[u] = *reinterpret_cast<const uint4*>(from + half + x);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int x = x0 + u * kCopyThreads * 16;
+        if (x < all) {
+          *reinterpret_cast<uint4*>(to + x) = k[u];
+          *reinterpret_cast<uint4*>(to + half + x) = v[u];
+        }
+      }
+    }
+  }
+}
 
 }  // namespace
 
 cudaError_t reorder_launch(const Layout& L, int first, int n, const int* parents, cudaStream_t stream) {
   const ReorderArgs a{L, first, n, parents};
   dmc_reorder_kernel<<<dim3(L.Hkv, L.L), kReorderThreads, 0, stream>>>(a);
-  dmc_reorder_done_kernel<<<1, 1, 0, stream>>>(L.pool_top);
-  return cudaGetLastError();
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(max(1, min(n, kCopyBlocks / (L.Hkv * L.L))), L.Hkv, L.L);
+  cfg.blockDim = dim3(kCopyThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, dmc_reorder_copy_kernel, a);
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace dmc
