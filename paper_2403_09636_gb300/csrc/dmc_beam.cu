@@ -4,9 +4,11 @@
 // so one pass over them gives both parts: the log-sum (running maximum and sum per lane) and the beam's own best `keep`.
 // A row is cut into pieces, a block each, whose warps keep their lists sorted across their lanes: lane i holds the
 // i-th best, as one 64-bit key (the logit's bits in an order that compares as whole numbers do, then the word's number
-// turned round, so that equal logits go to the lower word). Few elements pass a list's last: with n seen about
-// keep (1 + ln(n / keep)) of them. The group's last block (a counter, no waiting) joins the pieces: sums and lists of a
-// row by a warp, then the rows' lists by score, in 64 bits.
+// turned round, so that equal logits go to the lower word). Words are held to a bar that few more than `keep` of the
+// words so far reach: at first the keep-th largest of the lanes' maxima over the block's first 8192 words, then also the
+// least of the warps' ceil(keep / 8)-th best. The group's last block (a counter, no waiting) joins the pieces: sums and
+// lists of a row by a warp, then the rows' lists by score, in 64 bits; where sorted lists are joined, each entry counts
+// those before it.
 //
 // Bound by HBM (each logit is read once) where there are many, by the chain load - list - join otherwise.
 #include <math.h>
@@ -24,14 +26,14 @@ typedef unsigned long long u64;
 constexpr int kBeamWarps = 8;
 constexpr int kBeamThreads = kBeamWarps * 32;
 constexpr int kBeamMost = 32;             // beams of a group, and continuations kept: a lane each
-constexpr int kVector = 8;                // words of a lane at a time
-constexpr int kStep = 32 * kVector;       // and of a warp
-constexpr int kBeamBlocks = 608;          // pieces that rows are cut into, in all: four blocks per SM
+constexpr int kWords = 32;                // words of a lane at a time
+constexpr int kBlock = 32 * kWords;       // words of a warp at a time
+constexpr int kBeamBlocks = 304;          // pieces that rows are cut into, in all: two blocks per SM, as many as fit
 constexpr unsigned kFull = 0xffffffffu;
 
 struct BeamArgs {
   int groups, beams, keep, vocab;
-  int pieces, per;            // of a row; words of a piece, a multiple of kStep
+  int pieces, per;            // of a row; words of a piece, a multiple of kBlock
   const char* logits;
   long long stride;           // bytes between rows
   const float* scores;
@@ -58,227 +60,312 @@ __device__ __forceinline__ u64 key_of(float x, int word) { return (u64)ordered(x
 
 __device__ __forceinline__ u64 shfl64(u64 x, int src) { return __shfl_sync(kFull, x, src); }
 
-// Takes the lanes' keys (0: none) into the warp's list, best first.
-__device__ __forceinline__ void take(u64& list, u64& last, u64 key, int lane, int keep) {
-  unsigned m = __ballot_sync(kFull, key > last);
-  while (m) {
-    const u64 x = shfl64(key, __ffs(m) - 1);
-    m &= m - 1;
-    const int at = __popc(__ballot_sync(kFull, list > x));
-    const u64 up = __shfl_up_sync(kFull, list, 1);
-    list = lane < at ? list : lane == at ? x : up;
-    last = shfl64(list, keep - 1);
-    m &= __ballot_sync(kFull, key > last);
-  }
+// One compare-exchange of a warp's sorting network: lanes `j` apart, the larger key to the lower lane (or, rising, to
+// the upper).
+template <typename K>
+__device__ __forceinline__ K exchange(K key, int lane, int j, bool rising) {
+  const K other = __shfl_xor_sync(kFull, key, j);
+  return ((lane & j) == 0) != rising ? max(key, other) : min(key, other);
+}
+template <typename K>
+__device__ __forceinline__ K sorted(K key, int lane) {  // falling across the lanes
+#pragma unroll
+  for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+    for (int j = k / 2; j > 0; j >>= 1) key = exchange(key, lane, j, (lane & k) != 0);
+  return key;
 }
 
-// Eight words from element i on. Rows may begin at any element: then the 16-byte blocks around them are read and
-// shifted (a block that holds one of the row's elements is readable as a whole), so that sums are taken in the same
-// order wherever a row lies.
-template <typename T>
-struct Words {
-  static constexpr int N = kVector * (int)sizeof(T) / 16;  // 16-byte blocks
-  uint4 u[N + 1];
-  __device__ __forceinline__ void load(const char* p, int off, bool more) {  // p: aligned down by off bytes
-    const uint4* q = reinterpret_cast<const uint4*>(p);
-#pragma unroll
-    for (int i = 0; i < N; ++i) u[i] = __ldg(q + i);
-    if (off != 0 && more) u[N] = __ldg(q + N);
-  }
-  __device__ __forceinline__ void shift(int off) {
-    if (off == 0) return;
-    unsigned w[4 * N + 4];
-#pragma unroll
-    for (int i = 0; i <= N; ++i) {
-      w[4 * i] = u[i].x;
-      w[4 * i + 1] = u[i].y;
-      w[4 * i + 2] = u[i].z;
-      w[4 * i + 3] = u[i].w;
-    }
-#pragma unroll
-    for (int s = 2; s > 0; s >>= 1)  // whole words
-      if (off / 4 & s) {
-#pragma unroll
-        for (int i = 0; i < 4 * N + 4 - s; ++i) w[i] = w[i + s];
+// A warp's best keys, falling across its lanes, and the keep-th of them.
+struct List {
+  u64 key, last;
+  // Takes the lanes' keys (0: none). A key or four go in one by one (some 150 cycles each), more are sorted and merged
+  // (some 800).
+  __device__ __forceinline__ void take(u64 x, int lane, int keep) {
+    unsigned m = __ballot_sync(kFull, x > last);
+    if (__popc(m) > 4) {
+      x = sorted(x, lane);
+      if (!__any_sync(kFull, key != 0)) {
+        key = x;
+        last = shfl64(key, keep - 1);
+        return;
       }
-    if (off & 2) {
+      key = max(key, shfl64(x, 31 - lane));
 #pragma unroll
-      for (int i = 0; i < 4 * N; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+      for (int j = 16; j > 0; j >>= 1) key = exchange(key, lane, j, false);
+      last = shfl64(key, keep - 1);
+      return;
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) u[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    while (m) {
+      const u64 y = shfl64(x, __ffs(m) - 1);
+      m &= m - 1;
+      const int at = __popc(__ballot_sync(kFull, key > y));
+      const u64 up = __shfl_up_sync(kFull, key, 1);
+      key = lane < at ? key : lane == at ? y : up;
+    }
+    last = shfl64(key, keep - 1);
   }
-  __device__ __forceinline__ void unpack(float* x) const {
+};
+
+// A lane's words of a warp's block, by 4-byte loads: fp32 words lane + 32 j, or bf16 words 2 lane, 2 lane + 1 of each 64.
+// Which words a lane has, and so the order of its sum, does not depend on where the row lies: bf16 rows may begin in the
+// middle of four bytes, then each half comes from another lane's load.
+template <typename T>
+struct Words;
+template <>
+struct Words<float> {
+  static constexpr int N = kWords;  // loads
+  unsigned u[N];
+  static __device__ __forceinline__ int word(int lane, int j) { return lane + 32 * j; }
+  __device__ __forceinline__ void load(const char* p, int lane, bool) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) Chunk<T>::unpack(u[i], x + i * Chunk<T>::N);
+    for (int j = 0; j < N; ++j) u[j] = __ldg(reinterpret_cast<const unsigned*>(p) + lane + 32 * j);
+  }
+  __device__ __forceinline__ void unpack(float* x, int, bool) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = __uint_as_float(u[j]);
+  }
+};
+template <>
+struct Words<__nv_bfloat16> {
+  static constexpr int N = kWords / 2;
+  unsigned u[N], next;  // next: what lane j < N lacks of load j
+  static __device__ __forceinline__ int word(int lane, int j) { return j / 2 * 64 + 2 * lane + (j & 1); }
+  __device__ __forceinline__ void load(const char* p, int lane, bool odd) {
+    const unsigned* q = reinterpret_cast<const unsigned*>(p - (odd ? 2 : 0));
+#pragma unroll
+    for (int j = 0; j < N; ++j) u[j] = __ldg(q + lane + 32 * j);
+    if (odd && lane < N) next = __ldg(q + 32 * (lane + 1));
+  }
+  __device__ __forceinline__ void unpack(float* x, int lane, bool odd) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      unsigned w = u[j];
+      if (odd) {
+        const unsigned after = __shfl_down_sync(kFull, w, 1), end = __shfl_sync(kFull, next, j);
+        w = __funnelshift_r(w, lane == 31 ? end : after, 16);
+      }
+      Chunk<__nv_bfloat16>::unpack2(w, x[2 * j], x[2 * j + 1]);
+    }
   }
 };
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-__device__ __forceinline__ float2 join(float2 a, float2 b) {  // of (maximum, sum)
-  const float m = fmaxf(a.x, b.x), r = m == -INFINITY ? 0.f : m;
-  return make_float2(m, a.y * exp2f((a.x - r) * kLog2e) + b.y * exp2f((b.x - r) * kLog2e));
+// 2^x; what is below 2^-126 is 0 (a sum of exponentials of which one is 1 does not see it).
+__device__ __forceinline__ float pow2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
-// A continuation: its score, and beam and word as one number, in order of which ties go.
-struct Best {
-  double score;
-  u64 at;
-  __device__ __forceinline__ bool before(const Best& o) const {
-    return score > o.score || (score == o.score && at < o.at);
-  }
-};
-__device__ __forceinline__ Best shfl_best(const Best& b, int src) {
-  return Best{__shfl_sync(kFull, b.score, src), shfl64(b.at, src)};
+__device__ __forceinline__ float2 join(float2 a, float2 b) {  // of (maximum, sum)
+  const float m = fmaxf(a.x, b.x), r = m == -INFINITY ? 0.f : m;
+  return make_float2(m, a.y * pow2((a.x - r) * kLog2e) + b.y * pow2((b.x - r) * kLog2e));
+}
+__device__ __forceinline__ float2 join_lanes(float2 x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = join(x, make_float2(__shfl_xor_sync(kFull, x.x, o), __shfl_xor_sync(kFull, x.y, o)));
+  return x;
+}
+
+// A 64-bit number's bits in an order that compares as whole numbers do.
+__device__ __forceinline__ u64 ordered64(double x) {
+  const u64 u = (u64)__double_as_longlong(x);
+  return u >> 63 ? ~u : u | 1ull << 63;
+}
+__device__ __forceinline__ double unordered64(u64 u) {
+  return __longlong_as_double((long long)(u >> 63 ? u & ~(1ull << 63) : ~u));
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kBeamThreads) dmc_beam_kernel(const BeamArgs a) {
-  __shared__ u64 s_lists[kBeamMost][kBeamMost];  // a list per warp, at the end per beam
+__global__ void __launch_bounds__(kBeamThreads, 2) dmc_beam_kernel(const BeamArgs a) {
+  __shared__ u64 s_keys[kBeamMost][kBeamMost];   // a list per warp, at the end the scores of one per beam
+  __shared__ int s_words[kBeamMost][kBeamMost];  // and their words
+  __shared__ unsigned s_tops[kBeamWarps][32];    // the warps' lanes' maxima, falling
   __shared__ float2 s_sums[kBeamWarps];
-  __shared__ double s_lse[kBeamMost];
+  __shared__ float s_bar;
+  __shared__ volatile unsigned s_few[kBeamWarps];  // the warps' lists' ceil(keep / 8)-th best
   __shared__ int s_last;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, keep = a.keep;
   const int row = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces, group = row / a.beams;
   const bool skip = a.finished != nullptr && a.finished[row];
 
   if (!skip) {
+    using W = Words<T>;
     const char* p = a.logits + (size_t)row * a.stride;
-    const int off = (int)(reinterpret_cast<uintptr_t>(p) & 15);
+    const bool odd = sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(p) & 2) != 0;
     const int first = piece * a.per, end = min(first + a.per, a.vocab);
-    u64 list = 0, last = 0;
-    float m = -INFINITY, sum = 0.f;
-    constexpr int U = 4 / Words<T>::N;  // vectors in flight
-    for (int i0 = first + warp * kStep + lane * kVector; i0 - lane * kVector < end; i0 += U * kBeamWarps * kStep) {
-      Words<T> w[U];
+    List list{0, 0};
+    float m = -INFINITY, sum = 0.f, bar = -INFINITY;
+    bool fresh = true;
+    const int share = (keep + kBeamWarps - 1) / kBeamWarps;
+    if (lane == 0) s_few[warp] = 0;
+    W w;
+    if (first + (warp + 1) * kBlock <= end) w.load(p + (size_t)(first + warp * kBlock) * sizeof(T), lane, odd);
+    for (int i0 = first + warp * kBlock; i0 - warp * kBlock < end; i0 += kBeamWarps * kBlock) {
+      float x[kWords], top = -INFINITY;
+      if (i0 + kBlock <= end) {
+        w.unpack(x, lane, odd);
+        const int next = i0 + kBeamWarps * kBlock;  // on its way while this block is worked
+        if (next + kBlock <= end) w.load(p + (size_t)next * sizeof(T), lane, odd);
+      } else {  // the row's last words, one by one
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = i0 + u * kBeamWarps * kStep;
-        // whole blocks where the row has eight more words; else one word at a time, below
-        if (i + kVector <= end) w[u].load(p - off + (size_t)i * sizeof(T), off, true);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = i0 + u * kBeamWarps * kStep;
-        if (i - lane * kVector >= end) break;  // the whole warp
-        float x[kVector];
-        if (i + kVector <= end) {
-          w[u].shift(off);
-          w[u].unpack(x);
-        } else {
-#pragma unroll
-          for (int e = 0; e < kVector; ++e)
-            x[e] = i + e < end ? Elt<T>::to_f(reinterpret_cast<const T*>(p)[i + e]) : -INFINITY;
-        }
-        float top = x[0];
-#pragma unroll
-        for (int e = 1; e < kVector; ++e) top = fmaxf(top, x[e]);
-        const float mn = fmaxf(m, top), r = mn == -INFINITY ? 0.f : mn;
-        float s = sum * exp2f((m - r) * kLog2e);
-#pragma unroll
-        for (int e = 0; e < kVector; ++e) s += exp2f((x[e] - r) * kLog2e);
-        sum = s;
-        m = mn;
-        if (__any_sync(kFull, ordered(top) >= (unsigned)(last >> 32) && i < end)) {
-#pragma unroll
-          for (int e = 0; e < kVector; ++e)
-            take(list, last, i + e < end ? key_of(x[e], i + e) : 0ull, lane, a.keep);
+        for (int j = 0; j < kWords; ++j) {
+          const int i = i0 + W::word(lane, j);
+          x[j] = i < end ? Elt<T>::to_f(reinterpret_cast<const T*>(p)[i]) : -INFINITY;
         }
       }
+#pragma unroll
+      for (int j = 0; j < kWords; ++j) top = fmaxf(top, x[j]);
+      if (fresh) {  // a bar that `keep` words of the block's first ones reach: the keep-th of its lanes' maxima
+        const unsigned mine = sorted(ordered(top), lane);
+        s_tops[warp][lane] = mine;
+        __syncthreads();
+        if (lane < keep) {  // (a lane's place among all, as for the lists below)
+          int before = lane;
+          for (int v = 0; v < kBeamWarps && before < keep; ++v)
+            if (v != warp)
+              for (int j = 0; j < keep && (s_tops[v][j] > mine || (s_tops[v][j] == mine && v < warp)); ++j) ++before;
+          if (before == keep - 1) s_bar = unordered(mine);
+        }
+      }
+      const float mn = fmaxf(m, top), r = mn == -INFINITY ? 0.f : mn;
+      sum *= pow2((m - r) * kLog2e);
+      float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+      const float2 r2 = make_float2(-r, -r), l2 = make_float2(kLog2e, kLog2e);
+#pragma unroll
+      for (int j = 0; j < kWords; j += 4) {
+        const float2 d = mul2(add2(make_float2(x[j], x[j + 1]), r2), l2);
+        const float2 e = mul2(add2(make_float2(x[j + 2], x[j + 3]), r2), l2);
+        s0 = add2(s0, make_float2(pow2(d.x), pow2(d.y)));
+        s1 = add2(s1, make_float2(pow2(e.x), pow2(e.y)));
+      }
+      s0 = add2(s0, s1);
+      sum += s0.x + s0.y;
+      m = mn;
+      if (fresh) {
+        __syncthreads();
+        bar = s_bar;
+        fresh = false;
+      }
+      else {  // `keep` words or more reach the least of what each warp has a share of (later values of it are no less)
+        const unsigned least = __reduce_min_sync(kFull, lane < kBeamWarps ? s_few[lane] : 0xffffffffu);
+        if (least != 0) bar = fmaxf(bar, unordered(least));
+      }
+      if (!__any_sync(kFull, top >= bar)) continue;
+      // Words that reach the bar, a word of each lane at a time (read again: few are, and which of its registers a
+      // lane wants is not known).
+      unsigned mask = 0;
+#pragma unroll
+      for (int j = 0; j < kWords; ++j) mask |= (x[j] >= bar ? 1u : 0u) << j;
+      while (__any_sync(kFull, mask != 0)) {
+        const int j = __ffs(mask) - 1, i = i0 + W::word(lane, max(j, 0));
+        const bool in = j >= 0 && i < end;
+        list.take(in ? key_of(Elt<T>::to_f(reinterpret_cast<const T*>(p)[i]), i) : 0, lane, keep);
+        mask &= mask - 1;
+      }
+      if (lane == share - 1) s_few[warp] = (unsigned)(list.key >> 32);
     }
-    float2 ms = make_float2(m, sum);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-      ms = join(ms, make_float2(__shfl_xor_sync(kFull, ms.x, o), __shfl_xor_sync(kFull, ms.y, o)));
-    s_lists[warp][lane] = list;
+    const float2 ms = join_lanes(make_float2(m, sum));
+    // (an empty place's key is below every word's, and its own)
+    u64 key = list.key ? list.key : (u64)tid + 1;
+    s_keys[warp][lane] = key;
     if (lane == 0) s_sums[warp] = ms;
     __syncthreads();
-    if (warp == 0) {
-      for (int i = lane; i < (kBeamWarps - 1) * 32; i += 32) {
-        const u64 key = (i & 31) < a.keep ? s_lists[1 + i / 32][i & 31] : 0ull;
-        take(list, last, key, lane, a.keep);
-      }
-      const size_t at = (size_t)row * a.pieces + piece;
-      if (lane < a.keep) a.lists[at * a.keep + lane] = list;
-      float2 t = lane < kBeamWarps ? s_sums[lane] : make_float2(-INFINITY, 0.f);
-#pragma unroll
-      for (int o = kBeamWarps / 2; o > 0; o >>= 1)
-        t = join(t, make_float2(__shfl_xor_sync(kFull, t.x, o), __shfl_xor_sync(kFull, t.y, o)));
-      if (lane == 0) a.sums[at] = t;
-      __threadfence();
+    const size_t at = (size_t)row * a.pieces + piece;
+    if (lane < keep) {
+      int before = lane;  // in its own list; the others' that are before it, no further than keep
+      for (int v = 0; v < kBeamWarps && before < keep; ++v)
+        if (v != warp)
+          for (int j = 0; j < keep && s_keys[v][j] > key; ++j) ++before;
+      if (before < keep) a.lists[at * keep + before] = key;
     }
+    if (warp == 0) {
+      const float2 t = join_lanes(lane < kBeamWarps ? s_sums[lane] : make_float2(-INFINITY, 0.f));
+      if (lane == 0) a.sums[at] = t;
+    }
+    __threadfence();
   }
   __syncthreads();
   if (tid == 0) {
-    const int all = a.beams * a.pieces;
     const int old = atomicAdd(a.counters + group, 1);
-    s_last = old == all - 1;
+    s_last = old == a.beams * a.pieces - 1;
     if (s_last) a.counters[group] = 0;
   }
   __syncthreads();
   if (!s_last) return;
   __threadfence();
 
-  // the group's last block: a warp per beam joins its pieces
+  // the group's last block: a warp per beam joins its pieces and gives its words their scores
   for (int b = warp; b < a.beams; b += kBeamWarps) {
-    const size_t r = (size_t)group * a.beams + b;
-    if (a.finished != nullptr && a.finished[r]) continue;
-    float2 ms = make_float2(-INFINITY, 0.f);
-    for (int i = lane; i < a.pieces; i += 32) ms = join(ms, __ldcg(a.sums + r * a.pieces + i));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-      ms = join(ms, make_float2(__shfl_xor_sync(kFull, ms.x, o), __shfl_xor_sync(kFull, ms.y, o)));
-    u64 list = 0, last = 0;
-    const u64* from = a.lists + r * a.pieces * a.keep;
-    for (int i = lane; i - lane < a.pieces * a.keep; i += 32)
-      take(list, last, i < a.pieces * a.keep ? __ldcg(from + i) : 0ull, lane, a.keep);
-    s_lists[b][lane] = list;
-    if (lane == 0) s_lse[b] = (double)ms.x + log((double)ms.y);
-  }
-  __syncthreads();
-  if (warp != 0) return;
-  Best mine{-INFINITY, ~0ull}, worst = mine;
-  for (int b = 0; b < a.beams; ++b) {
     const size_t r = (size_t)group * a.beams + b;
     const double base = a.scores[r];
     const bool ended = a.finished != nullptr && a.finished[r];
-    Best c{-INFINITY, ~0ull};  // this lane's candidate of the beam
-    if (lane < a.keep) {
-      // a beam without a finite score (or without a finite log-sum) has nothing to offer: its words at -infinity
-      int word = lane;
-      double score = -INFINITY;
-      if (ended && isfinite(base)) {  // its end word, the others at -infinity
+    // a beam without a finite score (or without a finite log-sum) has nothing to offer: its words at -infinity
+    int word = lane;
+    double score = -INFINITY;
+    if (ended) {
+      if (isfinite(base)) {  // its end word, the others at -infinity
         word = lane == 0 ? a.eos : lane - 1 < a.eos ? lane - 1 : lane;
         if (lane == 0) score = base;
-      } else if (!ended && isfinite(base) && isfinite(s_lse[b])) {
-        const u64 key = s_lists[b][lane];
-        word = key ? (int)~(unsigned)key : a.vocab;
-        score = base + ((double)unordered((unsigned)(key >> 32)) - s_lse[b]);
       }
-      if (word < a.vocab) c = Best{score, (u64)b << 32 | (unsigned)word};
+    } else {
+      const u64* from = a.lists + r * a.pieces * keep;
+      const int n = a.pieces * keep;
+      List list{0, 0};
+      u64 next = lane < n ? __ldcg(from + lane) : 0;
+      float2 ms = make_float2(-INFINITY, 0.f);
+      for (int i = lane; i < a.pieces; i += 32) ms = join(ms, __ldcg(a.sums + r * a.pieces + i));
+      for (int i = lane; i - lane < n; i += 32) {
+        const u64 x = next;
+        next = i + 32 < n ? __ldcg(from + i + 32) : 0;
+        list.take(x >> 32 ? x : 0, lane, keep);
+      }
+      ms = join_lanes(ms);
+      const double lse = (double)ms.x + log((double)ms.y);
+      if (isfinite(base) && isfinite(lse)) {
+        word = list.key ? (int)~(unsigned)list.key : a.vocab;
+        score = base + ((double)unordered((unsigned)(list.key >> 32)) - lse);
+      }
     }
-    unsigned m = __ballot_sync(kFull, c.before(worst));
-    while (m) {
-      const Best x = shfl_best(c, __ffs(m) - 1);
-      m &= m - 1;
-      const int at = __popc(__ballot_sync(kFull, mine.before(x)));
-      const Best up{__shfl_up_sync(kFull, mine.score, 1), __shfl_up_sync(kFull, mine.at, 1)};
-      mine = lane < at ? mine : lane == at ? x : up;
-      worst = shfl_best(mine, a.keep - 1);
-      m &= __ballot_sync(kFull, c.before(worst));
+    s_keys[b][lane] = word < a.vocab ? ordered64(score) : 0;  // 0: no word
+    s_words[b][lane] = word;
+  }
+  __syncthreads();
+  // a continuation's place is the number of those before it: of higher scores, of equal ones of lower beams (and of its
+  // own beam's words before it, which its list has in order)
+  constexpr int kMore = kBeamMost * kBeamMost / kBeamThreads;
+  int place[kMore];
+#pragma unroll
+  for (int i = 0; i < kMore; ++i) {
+    const int c = tid + i * kBeamThreads, b = c / kBeamMost, j = c % kBeamMost;
+    place[i] = keep;
+    if (b < a.beams && j < keep && s_keys[b][j] != 0) {
+      const u64 key = s_keys[b][j];
+      int before = j;
+      for (int v = 0; v < a.beams && before < keep; ++v)
+        if (v != b)
+          for (int l = 0; l < keep && (s_keys[v][l] > key || (s_keys[v][l] == key && v < b)); ++l) ++before;
+      place[i] = before;
     }
   }
-  const size_t r = (size_t)group * a.beams + min((int)(mine.at >> 32), a.beams - 1);
-  const bool ended = a.finished != nullptr && a.finished[r];
-  __syncwarp();  // finished and out_done may be one
-  if (lane < a.keep) {
-    const size_t o = (size_t)group * a.keep + lane;
-    const int word = (int)(unsigned)mine.at;
-    a.out_scores[o] = (float)mine.score;
+  bool ended[kMore];
+#pragma unroll
+  for (int i = 0; i < kMore; ++i) {
+    const size_t r = (size_t)group * a.beams + min((tid + i * kBeamThreads) / kBeamMost, a.beams - 1);
+    ended[i] = a.finished != nullptr && a.finished[r];
+  }
+  __syncthreads();  // finished and out_done, scores and out_scores may be one
+#pragma unroll
+  for (int i = 0; i < kMore; ++i) {
+    if (place[i] >= keep) continue;
+    const int c = tid + i * kBeamThreads, b = c / kBeamMost, j = c % kBeamMost, word = s_words[b][j];
+    const size_t o = (size_t)group * keep + place[i];
+    a.out_scores[o] = (float)unordered64(s_keys[b][j]);
     a.out_tokens[o] = word;
-    a.out_parents[o] = (int)r;
-    a.out_done[o] = ended || word == a.eos;
+    a.out_parents[o] = group * a.beams + b;
+    a.out_done[o] = ended[i] || word == a.eos;
   }
 }
 
@@ -304,10 +391,10 @@ bool valid(const dmc_beam_config* c) {
 // Pieces of a row and the words of one.
 void cut(const dmc_beam_config* c, int* pieces, int* per) {
   const long long rows = (long long)c->groups * c->beams;
-  const int most = dmc::ceil_div(c->vocab, dmc::kBeamWarps * dmc::kStep);
-  const int want = (int)((dmc::kBeamBlocks + rows - 1) / rows);
+  const int most = dmc::ceil_div(c->vocab, dmc::kBeamWarps * dmc::kBlock);
+  const int want = (int)(rows < dmc::kBeamBlocks ? dmc::kBeamBlocks / rows : 1);
   const int n = most < want ? most : want;
-  *per = dmc::ceil_div(dmc::ceil_div(c->vocab, n), dmc::kStep) * dmc::kStep;
+  *per = dmc::ceil_div(dmc::ceil_div(c->vocab, n), dmc::kBlock) * dmc::kBlock;
   *pieces = dmc::ceil_div(c->vocab, *per);
 }
 
