@@ -67,6 +67,7 @@ struct GqaArgs {
   char* out;            // at out + i * q_ls: [B][Hq][D]
   long long q_ls, kv_ls;
   bool overlap;         // launched as a programmatic dependent
+  bool join;            // kRead: split heads are merged by dmc_attend_join_kernel, in the launch after this
 };
 
 template <int D, int RING>
@@ -251,7 +252,7 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
   // cut into so many parts that merging them takes longer than streaming them
   // (gqa_workers); those are spread over the blocks so that every SM takes part.
   const int NWG = (int)gridDim.x * kGWarps;
-  const int NW = have_units ? gqa_workers(Utot, NH, NWG) : NWG;
+  const int NW = kRead && a.join ? (int)min(Utot, (long long)NWG) : have_units ? gqa_workers(Utot, NH, NWG) : NWG;
   const int wid = NW < NWG ? warp * (int)gridDim.x + (int)blockIdx.x : (int)blockIdx.x * kGWarps + warp;
   const bool works = have_units && wid < NW;
   const int u0 = works ? (int)range_start(wid, Utot, NW) : 0;
@@ -689,7 +690,7 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
           const int wf = worker_of_unit(hu0, Utot, NW);
           const int wl = worker_of_unit(hend - 1, Utot, NW);
           int last = 0;
-          if (lane == 0) {
+          if (lane == 0 && !(kRead && a.join)) {
             // every worker in [wf, wl] holds part of the head
             int* cnt = L.counters + (size_t)layer * NH * G + vh;
             const int old = atomicAdd(cnt, 1);
@@ -742,6 +743,83 @@ __global__ void __launch_bounds__(kGThreads, 1) dmc_decode_gqa_kernel(const GqaA
     }
   }
   }  // layers
+}
+
+// The merge of split heads for caches of so few heads that each is cut into many parts (attend): one block per head and
+// query, whose thread groups of D threads sum a share of the parts each. The last warp of a head, which merges alone,
+// takes a microsecond for two of them: 65,536 tokens at 1.5x of 8 KV heads were 73 us with as many parts as it
+// could afford (52 a head), 44 with one for each warp of the grid and this (35 and 5, overlapping).
+constexpr int kJoinGroups = 4, kJoinBatch = 8;  // parts of a thread in flight
+template <int D>
+__global__ void __launch_bounds__(kJoinGroups * D) dmc_attend_join_kernel(const GqaArgs a, int NWG) {
+  __shared__ float s_w[kGMaxBlocks * kGWarps];  // a part's weight
+  __shared__ float s_red[2 * kJoinGroups * D / 32], s_acc[kJoinGroups][D];
+  __shared__ int s_units[2];
+  const Layout& L = a.lay;
+  const int hv = blockIdx.x, g = blockIdx.y, G = L.G, NH = L.NH, tid = threadIdx.x;
+  const int lane = tid & 31, warp = tid >> 5;
+  constexpr int kThreads = kJoinGroups * D;
+  griddep_wait();
+  const int parity = *reinterpret_cast<const volatile int*>(&L.ctl[a.layer0 * 4]);
+  const int* len = L.lengths + ((size_t)a.layer0 * 2 + parity) * NH;
+  if (tid == 0) s_units[0] = s_units[1] = 0;
+  __syncthreads();
+  int all = 0, ahead = 0;
+  for (int i = tid; i < NH; i += kThreads) {
+    const int u = ceil_div(len[i], kPage);
+    all += u;
+    if (i < hv) ahead += u;
+  }
+  if (all) atomicAdd(&s_units[0], all);
+  if (ahead) atomicAdd(&s_units[1], ahead);
+  const int mine = ceil_div(len[hv], kPage);
+  __syncthreads();
+  const long long Utot = s_units[0];
+  const int hu0 = s_units[1], NW = (int)min(Utot, (long long)NWG);
+  if (mine == 0) return;  // its zeros are there
+  const int wf = worker_of_unit(hu0, Utot, NW), nc = worker_of_unit(hu0 + mine - 1, Utot, NW) - wf + 1;
+  if (nc == 1) return;  // one warp had the whole head
+  const int first_off = hu0 > range_start(wf, Utot, NW) ? 1 : 0;
+  const float* parts = L.partials + (size_t)a.layer0 * L.partials_layer_stride + (size_t)g * (D + 2);
+  const size_t PS = (size_t)G * (D + 2);
+  auto part = [&](int i) { return parts + (size_t)(2 * (wf + i) + (i == 0 ? first_off : 0)) * PS; };
+  float m = -INFINITY;
+  for (int i = tid; i < nc; i += kThreads) m = fmaxf(m, __ldcg(part(i)));
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+  if (lane == 0) s_red[warp] = m;
+  __syncthreads();
+  for (int w = 0; w < kThreads / 32; ++w) m = fmaxf(m, s_red[w]);
+  float l = 0.f;
+  for (int i = tid; i < nc; i += kThreads) {
+    const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(i)));
+    const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);
+    s_w[i] = w;
+    l = fmaf(ml.y, w, l);
+  }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+  if (lane == 0) s_red[kThreads / 32 + warp] = l;
+  __syncthreads();
+  const int grp = tid / D, d = tid % D;
+  float acc = 0.f;
+  for (int i0 = grp; i0 < nc; i0 += kJoinGroups * kJoinBatch) {
+    float v[kJoinBatch];
+#pragma unroll
+    for (int b = 0; b < kJoinBatch; ++b) v[b] = __ldcg(part(min(i0 + b * kJoinGroups, nc - 1)) + 2 + d);
+#pragma unroll
+    for (int b = 0; b < kJoinBatch; ++b)
+      if (i0 + b * kJoinGroups < nc) acc = fmaf(v[b], s_w[i0 + b * kJoinGroups], acc);
+  }
+  s_acc[grp][d] = acc;
+  __syncthreads();
+  if (grp != 0) return;
+  float sum = 0.f;
+  for (int w = 0; w < kThreads / 32; ++w) sum += s_red[kThreads / 32 + w];
+#pragma unroll
+  for (int i = 1; i < kJoinGroups; ++i) acc += s_acc[i][d];
+  reinterpret_cast<__nv_bfloat16*>(a.out)[((size_t)(hv / L.Hkv) * L.Hq + (size_t)(hv % L.Hkv) * G + g) * D + d] =
+      __float2bfloat16_rn(acc / sum);
 }
 
 // Shared memory and blocks per SM with one ring depth (both window variants; the reading
@@ -805,11 +883,30 @@ cudaError_t gqa_setup(const Layout& L, DecodePlan* plan) {
   return cudaErrorInvalidValue;
 }
 
+// Warps of the grid per head from which heads are merged by a launch of their own. 8 query heads for each KV head of
+// 128, us per call with the last warp's merge / the launch, of 40, 500, 2000 and 16,000 slots: 8 heads 9.1 / 9.5, 15.7 /
+// 10.1, 22.6 / 13.7, 43.5 / 23.9; 32 heads 9.9 / 11.2, 16.2 / 13.9, 24.1 / 17.7, 56.5 / 51.8; 64 heads 10.0 / 13.3, 16.5 /
+// 15.8, 23.9 / 23.1, 89.3 / 89.3; 128 heads 10.6 / 16.4, 16.4 / 22.4, 33.8 / 38.9, 158 / 166. Lengths are not known on the
+// host.
+constexpr int kJoinFrom = 12;
+
 template <int D>
 static cudaError_t launch_gqa(const cudaLaunchConfig_t& cfg, const DecodePlan& plan, const GqaArgs& a) {
-  if (a.k == nullptr)
-    return plan.stages == kGRing ? cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, false, kGRing, true>, a)
-                                 : cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, false, kGRingMany, true>, a);
+  if (a.k == nullptr) {
+    cudaError_t e = plan.stages == kGRing ? cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, false, kGRing, true>, a)
+                                          : cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, false, kGRingMany, true>, a);
+    if (e != cudaSuccess || !a.join) return e;
+    cudaLaunchConfig_t join = {};
+    join.gridDim = dim3(a.lay.NH, a.lay.G);
+    join.blockDim = dim3(kJoinGroups * D);
+    join.stream = cfg.stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    join.attrs = attr;
+    join.numAttrs = 1;
+    return cudaLaunchKernelEx(&join, dmc_attend_join_kernel<D>, a, plan.grid * kGWarps);
+  }
   if (plan.stages == kGRing)
     return a.lay.window > 0 ? cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, true, kGRing, false>, a)
                             : cudaLaunchKernelEx(&cfg, dmc_decode_gqa_kernel<D, false, kGRing, false>, a);
@@ -827,6 +924,7 @@ cudaError_t gqa_launch(const Layout& L, int layer0, int nlayers, const DecodePla
   a.q_ls = (long long)L.B * L.Hq * L.row_bytes;
   a.kv_ls = (long long)L.B * L.Hkv * L.row_bytes;
   a.overlap = pdl;
+  a.join = k == nullptr && plan.grid * kGWarps >= kJoinFrom * L.NH;
   a.q = static_cast<const char*>(q);
   a.k = static_cast<const char*>(k);
   a.v = static_cast<const char*>(v);
