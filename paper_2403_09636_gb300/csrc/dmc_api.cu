@@ -25,7 +25,8 @@ cudaError_t prefill_attn_launch(const Layout& L, int layer, int first_seq, int n
                                 const float* weights, void* out, cudaStream_t stream);
 cudaError_t append_launch(const Layout& L, int layer, int first_seq, int num_seqs, const void* q, const void* k,
                           const void* v, const int* cu, int total_tokens, int max_seqlen, const int* at,
-                          const unsigned long long* turns, bool pairs, void* q_out, cudaStream_t stream);
+                          const unsigned long long* turns, bool pairs, void* q_out, float* weights,
+                          cudaStream_t stream);
 cudaError_t reorder_launch(const Layout& L, int first, int n, const int* parents, cudaStream_t stream);
 cudaError_t decode_static_partials(int device, float** ptr, size_t* floats);
 bool gqa_supported(const Layout& L);
@@ -454,7 +455,8 @@ dmc_status dmc_cache_append(dmc_cache_t c, int32_t layer, int32_t first_seq, int
   c->order.other();
   return cuda_status(dmc::append_launch(L, layer, first_seq, num_seqs, q_dev, k_dev, v_dev, cu_seqlens_dev, total_tokens,
                                         max_seqlen, positions_dev, reinterpret_cast<const unsigned long long*>(turns_dev),
-                                        interleaved != 0, q_out_dev, stream));
+                                        interleaved != 0, q_out_dev,
+                                        dmc::prompt_attention(L.esize, L.D, L.G, L.window) ? c->weights : nullptr, stream));
 }
 
 dmc_status dmc_cache_attend(dmc_cache_t c, int32_t layer, const void* q_dev, void* out_dev, cudaStream_t stream) {

@@ -5,7 +5,7 @@
 //    the key and the group's queries, applies Algorithm 1 to the head's last slot, or opens one, and writes the
 //    queries back. All of it is a chain of trips to memory (slot count, page, old row and z), beside which the key, the
 //    queries and their turns are on their way.
-//  longer texts: the plan and the scan of dmc_prefill.cuh with its rotation, and dmc_rotate's kernel for the queries.
+//  longer texts: the plan of dmc_prefill.cuh, dmc_rotate's kernel for the queries, and the scan with its rotation.
 #include <math.h>
 
 #include <type_traits>
@@ -19,7 +19,8 @@ cudaError_t prefill_launch(const Layout& L, int layer, int first_seq, int num_se
                            const int* cu, int total_tokens, int max_seqlen, float* carry,
                            float* weights, cudaStream_t stream);
 cudaError_t rotate_prompt_launch(const Layout& L, int num_seqs, int total_tokens, const void* q, void* q_out, const int* cu,
-                                 const int* at, const unsigned long long* turns, bool pairs, cudaStream_t stream);
+                                 const int* at, const unsigned long long* turns, bool pairs, float* weights,
+                                 cudaStream_t stream);
 
 namespace {
 
@@ -35,6 +36,7 @@ struct AppendArgs {
   const int* cu;  // null: one token each
   const int* at;
   const unsigned long long* turns;
+  float* weights;  // room for the omegas of a prompt, or null
 };
 
 // A lane's share of a row: D / 64 elements of either half of it, or the same number twice in a row (kRotPairs).
@@ -254,7 +256,15 @@ cudaError_t launch_text(const AppendArgs& a, int max_seqlen, cudaStream_t stream
   p.max_seqlen = max_seqlen;
   p.at = a.at;
   p.turns = a.turns;
-  return launch_prefill<T, D, kRot>(p, stream);
+  // The queries' rotation runs beside the plan, which is all latency, and leaves the omegas for the scan where the cache
+  // has room for them: a query's first component costs the scan a line of DRAM
+  cudaError_t e = launch_plan<T, D>(p, stream);
+  if (e != cudaSuccess) return e;
+  e = rotate_prompt_launch(L, a.num_seqs, a.total_tokens, a.q, a.q_out, a.cu, a.at, a.turns, kRot == kRotPairs, a.weights,
+                           stream);
+  if (e != cudaSuccess) return e;
+  p.omegas = a.weights;
+  return launch_scan<T, D, kRot>(p, stream);
 }
 
 template <typename T, int D>
@@ -272,20 +282,20 @@ cudaError_t launch_append(const AppendArgs& a, int max_seqlen, int rot, cudaStre
 // One token per sequence (cu null) or texts of up to max_seqlen tokens. turns null: no rotation.
 cudaError_t append_launch(const Layout& L, int layer, int first_seq, int num_seqs, const void* q, const void* k,
                           const void* v, const int* cu, int total_tokens, int max_seqlen, const int* at,
-                          const unsigned long long* turns, bool pairs, void* q_out, cudaStream_t stream) {
+                          const unsigned long long* turns, bool pairs, void* q_out, float* weights,
+                          cudaStream_t stream) {
   if (turns == nullptr && max_seqlen > 1)
     return prefill_launch(L, layer, first_seq, num_seqs, q, (long long)L.Hq * L.D, L.D, k, v, cu, total_tokens,
                           max_seqlen, nullptr, nullptr, stream);
   const AppendArgs a{L, layer, first_seq, num_seqs, total_tokens, static_cast<const char*>(q),
-                     static_cast<const char*>(k), static_cast<const char*>(v), static_cast<char*>(q_out), cu, at, turns};
+                     static_cast<const char*>(k), static_cast<const char*>(v), static_cast<char*>(q_out), cu, at, turns, weights};
   const int rot = turns == nullptr ? kRotNone : pairs ? kRotPairs : kRotHalf;
   cudaError_t e = cudaErrorInvalidValue;
   if (L.esize == 4 && L.D == 64) e = launch_append<float, 64>(a, max_seqlen, rot, stream);
   if (L.esize == 4 && L.D == 128) e = launch_append<float, 128>(a, max_seqlen, rot, stream);
   if (L.esize == 2 && L.D == 64) e = launch_append<__nv_bfloat16, 64>(a, max_seqlen, rot, stream);
   if (L.esize == 2 && L.D == 128) e = launch_append<__nv_bfloat16, 128>(a, max_seqlen, rot, stream);
-  if (e != cudaSuccess || max_seqlen <= 1) return e;
-  return rotate_prompt_launch(L, num_seqs, total_tokens, q, q_out, cu, at, turns, pairs, stream);
+  return e;
 }
 
 }  // namespace dmc

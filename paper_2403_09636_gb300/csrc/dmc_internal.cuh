@@ -62,6 +62,9 @@ struct Layout {
 
 __host__ __device__ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+// Where the c-th chunk of a prompt's sequence s, whose first token is t0, keeps what it hands on.
+__host__ __device__ inline int prompt_chunk(int t0, int c, int s) { return (t0 + c * kPrefillChunk) / kPrefillChunk + s; }
+
 // Launch shape of the decode kernel for one cache, fixed at create time.
 struct DecodePlan {
   int grid;            // blocks of a launch over one layer
@@ -273,10 +276,6 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
 // cp.async (LDGSTS) of 16 bytes, L2 only, into this thread's shared memory.
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-// The same of 8 bytes, through L1 (the only form for fewer than 16).
-__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() {
   asm volatile("cp.async.commit_group;" ::: "memory");

@@ -4,6 +4,12 @@
 
 namespace dmc {
 
+template <typename T, int D>
+static cudaError_t launch_prefill(const PrefillArgs& a, cudaStream_t stream) {
+  const cudaError_t e = launch_plan<T, D>(a, stream);
+  return e != cudaSuccess ? e : launch_scan<T, D, kRotNone>(a, stream);
+}
+
 cudaError_t prefill_launch(const Layout& L, int layer, int first_seq, int num_seqs, const void* q,
                            long long q_tok, long long q_head, const void* k, const void* v,
                            const int* cu, int total_tokens, int max_seqlen, float* carry,
@@ -25,10 +31,11 @@ cudaError_t prefill_launch(const Layout& L, int layer, int first_seq, int num_se
   a.weights = weights;
   a.at = nullptr;
   a.turns = nullptr;
-  if (L.esize == 4 && L.D == 64) return launch_prefill<float, 64, kRotNone>(a, stream);
-  if (L.esize == 4 && L.D == 128) return launch_prefill<float, 128, kRotNone>(a, stream);
-  if (L.esize == 2 && L.D == 64) return launch_prefill<__nv_bfloat16, 64, kRotNone>(a, stream);
-  if (L.esize == 2 && L.D == 128) return launch_prefill<__nv_bfloat16, 128, kRotNone>(a, stream);
+  a.omegas = nullptr;
+  if (L.esize == 4 && L.D == 64) return launch_prefill<float, 64>(a, stream);
+  if (L.esize == 4 && L.D == 128) return launch_prefill<float, 128>(a, stream);
+  if (L.esize == 2 && L.D == 64) return launch_prefill<__nv_bfloat16, 64>(a, stream);
+  if (L.esize == 2 && L.D == 128) return launch_prefill<__nv_bfloat16, 128>(a, stream);
   return cudaErrorInvalidValue;
 }
 

@@ -57,12 +57,16 @@ struct PrefillArgs {
   float* weights;  // with carry: [chunk id][Hkv][128], omega, its sign bit set where the token opens a slot
   const int* at;   // rotation: position of each sequence's first token, and the pairs' turns
   const unsigned long long* turns;
+  const float* omegas;  // or null: omega of every token, laid out as the weights, by the rotation of the queries
 };
 
-// The 16 bytes of a key row that lane lr of LPR holds are `first` and `second`, 8 bytes each: neighbours, or from
-// either half of the row where the rotation pairs dims i and i + D / 2.
-template <int ROW, int kRot>
+// The 16 bytes of a key row that lane lr of LPR holds: `first` and `second`, 8 bytes each, neighbours or, where the
+// rotation pairs dims i and i + D / 2, from either half of the row. As floats they are the first dims of the lane's
+// pairs, then the second ones (without a rotation: in the row's order).
+template <typename T, int D, int kRot>
 struct KeyPiece {
+  using CK = Chunk<T>;
+  static constexpr int ROW = D * (int)sizeof(T), P = CK::N / 2;
   static __device__ __forceinline__ int first(int lr) { return kRot == kRotHalf ? lr * 8 : lr * 16; }
   static __device__ __forceinline__ int second(int lr) { return kRot == kRotHalf ? ROW / 2 + lr * 8 : lr * 16 + 8; }
   static __device__ __forceinline__ uint4 load(const char* row, int lr) {
@@ -78,36 +82,83 @@ struct KeyPiece {
       *reinterpret_cast<uint2*>(row + second(lr)) = make_uint2(u.z, u.w);
     }
   }
+  static __device__ __forceinline__ void unpack(const uint4& u, float* f) {
+    if constexpr (kRot != kRotPairs) {
+      CK::unpack(u, f);
+    } else {
+      float x[CK::N];
+      CK::unpack(u, x);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        f[i] = x[2 * i];
+        f[P + i] = x[2 * i + 1];
+      }
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float* f) {
+    if constexpr (kRot != kRotPairs) {
+      return CK::pack(f);
+    } else {
+      float x[CK::N];
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        x[2 * i] = f[i];
+        x[2 * i + 1] = f[P + i];
+      }
+      return CK::pack(x);
+    }
+  }
 };
 
-// The turns of a lane's N / 2 pairs, at a token and from one to the next.
-template <int N, int kRot>
+// The turns (cos, sin) of a lane's P pairs at a token, and how they go on to the next one.
+template <int P, bool kOn>
 struct Turns {
-  static constexpr int P = N / 2;
-  float2 now[P], step[P];
+  float c[P], s[P];
   __device__ __forceinline__ void set(const unsigned long long* turns, int lr, long long at) {
 #pragma unroll
-    for (int i = 0; i < P; ++i) now[i] = turn_of(turns_of_pair(turns, lr * P + i), at);
+    for (int i = 0; i < P; ++i) {
+      const float2 t = turn_of(turns_of_pair(turns, lr * P + i), at);
+      c[i] = t.x;
+      s[i] = t.y;
+    }
   }
-  __device__ __forceinline__ void set_step(const unsigned long long* turns, int lr) {
+  __device__ __forceinline__ void advance(const Turns& step) {
 #pragma unroll
-    for (int i = 0; i < P; ++i) step[i] = turn_of(turns_of_pair(turns, lr * P + i), 1);
+    for (int i = 0; i < P; i += 2) {
+      const float2 c2 = make_float2(c[i], c[i + 1]), s2 = make_float2(s[i], s[i + 1]);
+      const float2 dc = make_float2(step.c[i], step.c[i + 1]), ds = make_float2(step.s[i], step.s[i + 1]);
+      const float2 cn = fma2(s2, make_float2(-ds.x, -ds.y), mul2(c2, dc)), sn = fma2(c2, ds, mul2(s2, dc));
+      c[i] = cn.x; c[i + 1] = cn.y;
+      s[i] = sn.x; s[i + 1] = sn.y;
+    }
   }
-  __device__ __forceinline__ void advance() {
+  // sum += w * (k turned), in packed multiply-adds: the weight goes into the turn first
+  __device__ __forceinline__ void add(float* sum, const float* k, float w) const {
+    const float2 w2 = make_float2(w, w), n2 = make_float2(-w, -w);
 #pragma unroll
-    for (int i = 0; i < P; ++i) turn(step[i], now[i].x, now[i].y);
-  }
-  __device__ __forceinline__ void apply(float* x) const {
-#pragma unroll
-    for (int i = 0; i < P; ++i) turn(now[i], x[kRot == kRotHalf ? i : 2 * i], x[kRot == kRotHalf ? i + P : 2 * i + 1]);
+    for (int i = 0; i < P; i += 2) {
+      const float2 a = make_float2(k[i], k[i + 1]), b = make_float2(k[P + i], k[P + i + 1]);
+      const float2 s2 = make_float2(s[i], s[i + 1]);
+      const float2 wc = mul2(w2, make_float2(c[i], c[i + 1])), ws = mul2(w2, s2), wn = mul2(n2, s2);
+      const float2 x = fma2(b, wn, fma2(a, wc, make_float2(sum[i], sum[i + 1])));
+      const float2 y = fma2(a, ws, fma2(b, wc, make_float2(sum[P + i], sum[P + i + 1])));
+      sum[i] = x.x; sum[i + 1] = x.y;
+      sum[P + i] = y.x; sum[P + i + 1] = y.y;
+    }
   }
 };
-template <int N>
-struct Turns<N, kRotNone> {
+template <int P>
+struct Turns<P, false> {
   __device__ __forceinline__ void set(const unsigned long long*, int, long long) {}
-  __device__ __forceinline__ void set_step(const unsigned long long*, int) {}
-  __device__ __forceinline__ void advance() {}
-  __device__ __forceinline__ void apply(float*) const {}
+  __device__ __forceinline__ void advance(const Turns&) {}
+  __device__ __forceinline__ void add(float* sum, const float* k, float w) const {
+    const float2 w2 = make_float2(w, w);
+#pragma unroll
+    for (int i = 0; i < 2 * P; i += 2) {
+      const float2 x = fma2(w2, make_float2(k[i], k[i + 1]), make_float2(sum[i], sum[i + 1]));
+      sum[i] = x.x; sum[i + 1] = x.y;
+    }
+  }
 };
 
 __device__ __forceinline__ bool seq_bounds(const PrefillArgs& a, int s, int& t0, int& t1) {
@@ -116,7 +167,7 @@ __device__ __forceinline__ bool seq_bounds(const PrefillArgs& a, int s, int& t0,
   return t0 >= 0 && t0 <= t1 && t1 <= a.total_tokens && (t1 - t0) <= a.max_seqlen;
 }
 
-__device__ __forceinline__ int chunk_id(int t0, int c, int s) { return (t0 + c * kPrefillChunk) / kPrefillChunk + s; }
+__device__ __forceinline__ int chunk_id(int t0, int c, int s) { return prompt_chunk(t0, c, s); }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kPlanThreads) dmc_prefill_plan_kernel(const PrefillArgs a) {
@@ -243,7 +294,7 @@ __device__ __forceinline__ float* carry_at(const PrefillArgs& a, int t0, int cs,
 template <typename T, int D, int kRot>
 __device__ __forceinline__ void fill_ring(const PrefillArgs& a, int s, int h, int bh, int tb, int te,
                                           int n_old) {
-  using KP = KeyPiece<D * (int)sizeof(T), kRot>;
+  using KP = KeyPiece<T, D, kRot>;
   constexpr int ROW = D * (int)sizeof(T);
   constexpr int LPR = ROW / 16;
   constexpr int RPI = 32 / LPR;
@@ -265,13 +316,16 @@ __device__ __forceinline__ void fill_ring(const PrefillArgs& a, int s, int h, in
       else kr.x = 0u;
     }
     if constexpr (kRot != kRotNone) {
-      float kf[Chunk<T>::N];
-      Turns<Chunk<T>::N, kRot> turns;
+      constexpr int N = Chunk<T>::N;
+      float kf[N], kt[N];
+      Turns<N / 2, true> turns;
       turns.set(a.turns, lr, (long long)a.at[s] + (t - a.cu[s]));
-      Chunk<T>::unpack(kr, kf);
-      turns.apply(kf);
-      if (lr == 0) kf[0] = 0.f;
-      kr = Chunk<T>::pack(kf);
+      KP::unpack(kr, kf);
+#pragma unroll
+      for (int i = 0; i < N; ++i) kt[i] = 0.f;
+      turns.add(kt, kf, 1.f);
+      if (lr == 0) kt[0] = 0.f;
+      kr = KP::pack(kt);
     }
     KP::store(ring + (size_t)pos * 2 * ROW, lr, kr);
     *reinterpret_cast<uint4*>(ring + (size_t)pos * 2 * ROW + ROW + lr * 16) = vr;
@@ -315,9 +369,9 @@ constexpr size_t kScanRingBytes = (size_t)kRing * 2 * kScanThreads * 16;
 // 118 (134; 349), CR 32 99 (125; 143), fp32 d 128 CR 32 112 (189; 165); a 7B layer at
 // 4x, W = 12 284 (323; 891).
 template <typename T, int D, bool kWin, int kRot>
-__global__ void __launch_bounds__(kScanThreads, 6) dmc_prefill_scan_kernel(const PrefillArgs a) {
+__global__ void __launch_bounds__(kScanThreads, kRot == kRotNone ? 6 : 5) dmc_prefill_scan_kernel(const PrefillArgs a) {
   using CK = Chunk<T>;
-  using KP = KeyPiece<D * (int)sizeof(T), kRot>;
+  using KP = KeyPiece<T, D, kRot>;
   constexpr int ROW = D * (int)sizeof(T);
   constexpr int LPR = ROW / 16;               // lanes per row
   constexpr int NG = kScanThreads / LPR;      // row groups
@@ -335,6 +389,7 @@ __global__ void __launch_bounds__(kScanThreads, 6) dmc_prefill_scan_kernel(const
   __shared__ unsigned s_bal[2 * kPrefillChunk / 32];  // opening bits: the chunk's, the next one's
   __shared__ int s_page[kMaxPages];
   __shared__ int s_next;
+  __shared__ __align__(16) float2 s_step[kRot == kRotNone ? 1 : D / 2];  // a token's turn of every pair
   const Layout& L = a.lay;
   const int c = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
   const int bh = (a.first_seq + s) * L.Hkv + h;
@@ -362,13 +417,7 @@ __global__ void __launch_bounds__(kScanThreads, 6) dmc_prefill_scan_kernel(const
       const int t = g0 + b * kRingBatch + u;
       if (b < NB && t < g1 && (!kWin || (counts >> (t - g0) & 1u))) {
         const uint32_t dk = rk((b % 2) * kRingBatch + u);
-        const char* kt = kb + (size_t)t * hrow;
-        if constexpr (kRot == kRotHalf) {
-          cp_async8(dk, kt + KP::first(lr));
-          cp_async8(dk + 8, kt + KP::second(lr));
-        } else {
-          cp_async16(dk, kt + lr * 16);
-        }
+        cp_async16(dk, kb + (size_t)t * hrow + lr * 16);
         cp_async16(dk + kScanThreads * 16, vb + (size_t)t * hrow);
       }
     }
@@ -395,6 +444,9 @@ __global__ void __launch_bounds__(kScanThreads, 6) dmc_prefill_scan_kernel(const
   // omega = sigmoid(q[0]) (group mean for GQA); the group's loads, up to eight
   // at a time, are in flight together
   auto omega = [&](int t) {
+    if (kRot != kRotNone && a.omegas != nullptr)
+      return __ldg(a.omegas + ((size_t)chunk_id(t0, (t - t0) / kPrefillChunk, s) * L.Hkv + h) * kPrefillChunk +
+                   (t - t0) % kPrefillChunk);
     const T* q0 = qq + (size_t)t * a.q_tok + (size_t)(h * L.G) * a.q_head;
     float y = Elt<T>::to_f(q0[0]);
     for (int g0 = 1; g0 < L.G; g0 += 7) {
@@ -431,6 +483,7 @@ __global__ void __launch_bounds__(kScanThreads, 6) dmc_prefill_scan_kernel(const
           __uint_as_float((__float_as_uint(w) & 0x7fffffffu) | ((mine >> lane) & 1u) << 31);
     if (lane == 0) { s_bal[warp] = mine; s_bal[kPrefillChunk / 32 + warp] = other; }
   }
+  if (kRot != kRotNone && tid < D / 2) s_step[tid] = turn_of(turns_of_pair(a.turns, tid), 1);
   __syncthreads();
   int nstart = 0, first = -1, next = -1;
 #pragma unroll
@@ -488,23 +541,18 @@ __global__ void __launch_bounds__(kScanThreads, 6) dmc_prefill_scan_kernel(const
     for (int e = 0; e < EPC; ++e) { ak[e] = 0.f; av[e] = 0.f; }
     zs = 0.f;
   };
-  using Turn = Turns<EPC, kRot>;
+  using Turn = Turns<EPC / 2, kRot != kRotNone>;
   const long long at0 = kRot != kRotNone ? (long long)a.at[s] - t0 : 0;  // a token's position less its index
   auto add_to = [&](float* xk, float* xv, float& xz, const uint4& kr, const uint4& vr, float w, const Turn& turns) {
     float kf[EPC], vf[EPC];
-    CK::unpack(kr, kf);
+    KP::unpack(kr, kf);
     CK::unpack(vr, vf);
     if (lr == 0) kf[0] = 0.f;  // k[0] <- 0 (Algorithm 1)
-    if constexpr (kRot != kRotNone) {
-      turns.apply(kf);
-      if (lr == 0) kf[0] = 0.f;  // (where its partner, which keeps its value, is infinite)
-    }
+    turns.add(xk, kf, w);
     const float2 ww = make_float2(w, w);
 #pragma unroll
     for (int e = 0; e < EPC; e += 2) {
-      const float2 sk = fma2(ww, make_float2(kf[e], kf[e + 1]), make_float2(xk[e], xk[e + 1]));
       const float2 sv = fma2(ww, make_float2(vf[e], vf[e + 1]), make_float2(xv[e], xv[e + 1]));
-      xk[e] = sk.x; xk[e + 1] = sk.y;
       xv[e] = sv.x; xv[e + 1] = sv.y;
     }
     xz += w;
@@ -536,7 +584,7 @@ __global__ void __launch_bounds__(kScanThreads, 6) dmc_prefill_scan_kernel(const
       if (x != x) *L.unbounded = 1;
     }
     if (lr == 0) kn[0] = 0.f;
-    KP::store(kdst, lr, CK::pack(kn));
+    KP::store(kdst, lr, KP::pack(kn));
     *reinterpret_cast<uint4*>(kdst + (size_t)kPage * ROW + lr * 16) = CK::pack(vn);
     if (lr == 0) L.z[(size_t)s_page[slot / kPage - pfirst] * kPage + slot % kPage] = zs;
   };
@@ -558,15 +606,23 @@ __global__ void __launch_bounds__(kScanThreads, 6) dmc_prefill_scan_kernel(const
   float hk[EPC], hv[EPC], hz = 0.f;  // the sums before the group's first opening
   bool open = false;                 // summing a segment that opened in this group
   reset();
-  Turn turns;
+  Turn turns, step;
   turns.set(a.turns, lr, at0 + g0);
-  turns.set_step(a.turns, lr);
+  if constexpr (kRot != kRotNone) {
+    constexpr int P = EPC / 2;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      step.c[i] = s_step[lr * P + i].x;
+      step.s[i] = s_step[lr * P + i].y;
+    }
+  }
   for (int b = 0; b < NB; ++b) {
     cp_async_wait<1>();  // copy group b has landed
+    if constexpr (kRot == kRotHalf) __syncwarp();  // (a lane's piece of a key row is in two lanes' copies)
 #pragma unroll 1
     for (int u = 0; u < kRingBatch; ++u) {
       const int t = g0 + b * kRingBatch + u;
-      if (kRot != kRotNone && t > g0) turns.advance();
+      if (kRot != kRotNone && t > g0) turns.advance(step);
       if (t >= wb && t < g1) {
         if ((gbits >> (t - g0)) & 1u) {  // t opens a slot: the segment before it ends
           if (open) {
@@ -583,14 +639,22 @@ __global__ void __launch_bounds__(kScanThreads, 6) dmc_prefill_scan_kernel(const
         if (kWin && !(counts >> (t - g0) & 1u)) continue;
         const uint32_t sk = rk((b % 2) * kRingBatch + u);
         uint4 kr, vr;
-        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(kr.x), "=r"(kr.y), "=r"(kr.z), "=r"(kr.w) : "r"(sk) : "memory");
+        if constexpr (kRot == kRotHalf) {
+          asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];"
+                       : "=r"(kr.x), "=r"(kr.y) : "r"(sk - lr * 8) : "memory");
+          asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];"
+                       : "=r"(kr.z), "=r"(kr.w) : "r"(sk - lr * 8 + ROW / 2) : "memory");
+        } else {
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(kr.x), "=r"(kr.y), "=r"(kr.z), "=r"(kr.w) : "r"(sk) : "memory");
+        }
         asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                      : "=r"(vr.x), "=r"(vr.y), "=r"(vr.z), "=r"(vr.w)
                      : "r"(sk + kScanThreads * 16) : "memory");
         add_row(kr, vr, s_w[t - a0], turns);
       }
     }
+    if constexpr (kRot == kRotHalf) __syncwarp();
     issue(b + 2);  // into the ring rows just read
   }
   if (!open) {  // no opening in the range: all of it joins an earlier segment
@@ -704,7 +768,7 @@ __global__ void __launch_bounds__(kScanThreads, 6) dmc_prefill_scan_kernel(const
       for (int e = 0; e < m; ++e) {
         const int pos = (n_old - 1 - e) % W;
         float kf[EPC], vf[EPC];
-        CK::unpack(KP::load(old + (size_t)pos * 2 * ROW, lr), kf);
+        KP::unpack(KP::load(old + (size_t)pos * 2 * ROW, lr), kf);
         CK::unpack(*reinterpret_cast<const uint4*>(old + (size_t)pos * 2 * ROW + ROW + lr * 16), vf);
         const float w = old_w[pos];
 #pragma unroll
@@ -718,7 +782,7 @@ __global__ void __launch_bounds__(kScanThreads, 6) dmc_prefill_scan_kernel(const
       // the old slot's K z_old, V z_old and z_old start the sums
       const char* kold = slot_ptr(slot);
       float ko[EPC], vo[EPC];
-      CK::unpack(KP::load(kold, lr), ko);
+      KP::unpack(KP::load(kold, lr), ko);
       CK::unpack(*reinterpret_cast<const uint4*>(kold + (size_t)kPage * ROW + lr * 16), vo);
       const float zo = L.z[(size_t)s_page[slot / kPage - pfirst] * kPage + slot % kPage];
 #pragma unroll
@@ -793,8 +857,8 @@ __global__ void __launch_bounds__(kPlanThreads) dmc_prefill_ring_kernel(const Pr
   fill_ring<T, D, kRot>(a, s, h, bh, last >= 0 ? last : t0, t1, n_old);
 }
 
-template <typename T, int D, int kRot>
-static cudaError_t launch_prefill(const PrefillArgs& a, cudaStream_t stream) {
+template <typename T, int D>
+static cudaError_t launch_plan(const PrefillArgs& a, cudaStream_t stream) {
   const int max_chunks = ceil_div(a.max_seqlen, kPrefillChunk);
   const size_t plan_smem = (size_t)max(max_chunks, 1) * sizeof(int);
   if (plan_smem > 48 * 1024) {
@@ -803,8 +867,13 @@ static cudaError_t launch_prefill(const PrefillArgs& a, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
   }
   dmc_prefill_plan_kernel<T, D><<<dim3(a.num_seqs, a.lay.Hkv), kPlanThreads, plan_smem, stream>>>(a);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
+  return cudaGetLastError();
+}
+
+template <typename T, int D, int kRot>
+static cudaError_t launch_scan(const PrefillArgs& a, cudaStream_t stream) {
+  const int max_chunks = ceil_div(a.max_seqlen, kPrefillChunk);
+  cudaError_t e = cudaSuccess;
   if (max_chunks > 0) {
     const dim3 grid(max_chunks, a.lay.Hkv, a.num_seqs);
     cudaLaunchConfig_t cfg = {};

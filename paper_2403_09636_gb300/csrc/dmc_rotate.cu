@@ -12,6 +12,7 @@ namespace {
 
 constexpr int kRotateThreads = 256;
 constexpr int kRotateTokens = 4;  // most tokens of a block
+constexpr int kRowsInFlight = 4;  // of a thread
 
 struct RotateArgs {
   int tokens, per;  // per block
@@ -24,67 +25,121 @@ struct RotateArgs {
   int seqs;
   const unsigned long long* turns;
   bool pairs, back;
+  bool prompt;     // the launch between the plan and the scan of a prompt that is appended
+  float* weights;  // or null: omega of every token and KV head, where the scan looks for it
+  int group;       // queries per KV head
 };
 
-__device__ __forceinline__ long long position(const RotateArgs& a, int t) {
-  if (a.cu == nullptr) return a.at[t];
+// The sequence of token t, and its place there.
+__device__ __forceinline__ void sequence(const RotateArgs& a, int t, int& s, int& at) {
   int lo = 0, hi = a.seqs - 1;  // the last sequence that begins at t or before
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (a.cu[mid] <= t) lo = mid; else hi = mid - 1;
   }
-  return (long long)a.at[lo] + (t - a.cu[lo]);
+  s = lo;
+  at = t - a.cu[lo];
 }
 
+__device__ __forceinline__ long long position(const RotateArgs& a, int t) {
+  if (a.cu == nullptr) return a.at[t];
+  int s, at;
+  sequence(a, t, s, at);
+  return (long long)a.at[s] + at;
+}
+
+// Turns of two pairs at a time, (cos, cos, sin, sin); thread p of a row needs places i * P + p (i = 0 .. E / 2 - 1: one
+// 128-byte line of shared memory for a row's threads at a time).
 template <typename T, int D>
-__global__ void __launch_bounds__(kRotateThreads) dmc_rotate_kernel(const RotateArgs a) {
+__global__ void __launch_bounds__(kRotateThreads, 3) dmc_rotate_kernel(const RotateArgs a) {
   using CK = Chunk<T>;
   constexpr int E = CK::N, ROW = D * (int)sizeof(T), P = ROW / 32;  // threads per row
-  __shared__ __align__(16) float2 cs[kRotateTokens][D / 2];
+  __shared__ __align__(16) float4 cs[kRotateTokens][D / 4];
+  if (a.prompt) griddep_launch_dependents();
   const int t0 = blockIdx.x * a.per, n = min(a.per, a.tokens - t0);
-  for (int i = threadIdx.x; i < n * (D / 2); i += kRotateThreads) {
-    const int pair = i % (D / 2);
-    float2 c = turn_of(turns_of_pair(a.turns, pair), position(a, t0 + i / (D / 2)));
-    if (a.back) c.y = -c.y;
-    cs[i / (D / 2)][pair] = c;
-  }
-  __syncthreads();
   const int p = threadIdx.x % P, all = a.heads[0] + a.heads[1];
-  constexpr int kStep = kRotateThreads / P, U = 2;  // rows of the block at a time, of a thread in flight
-  const int rows = n * all, first = blockIdx.y * kStep + threadIdx.x / P, step = gridDim.y * kStep;
-  for (int r0 = first; r0 < rows; r0 += U * step) {
+  constexpr int kStep = kRotateThreads / P, U = kRowsInFlight;
+  const int rows = n * all, step = gridDim.y * kStep;
+  bool ready = false;
+  int r = blockIdx.y * kStep + threadIdx.x / P;  // the thread's next row: head h of the block's token t
+  int t = r / all, h = r % all;
+  for (int r0 = blockIdx.y * kStep; r0 < rows; r0 += U * step) {
     uint4 lo[U], hi[U];
     char* to[U];
     int token[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int r = r0 + u * step;
-      if (r >= rows) break;
-      const int h = r % all, which = h >= a.heads[0];
-      token[u] = r / all;
-      const size_t off = (size_t)(h - (which ? a.heads[0] : 0)) * ROW + p * 16;
-      const char* from = a.x[which] + (size_t)(t0 + token[u]) * a.x_stride[which] + off;
-      to[u] = a.y[which] + (size_t)(t0 + token[u]) * a.y_stride[which] + off;
-      lo[u] = *reinterpret_cast<const uint4*>(from);
-      hi[u] = *reinterpret_cast<const uint4*>(from + ROW / 2);
+      to[u] = nullptr;
+      if (r < rows) {
+        const bool key = h >= a.heads[0];  // (chosen field by field: the arguments stay where they are)
+        const size_t off = (size_t)(h - (key ? a.heads[0] : 0)) * ROW + p * 16;
+        const char* from = (key ? a.x[1] : a.x[0]) + (size_t)(t0 + t) * (key ? a.x_stride[1] : a.x_stride[0]) + off;
+        to[u] = (key ? a.y[1] : a.y[0]) + (size_t)(t0 + t) * (key ? a.y_stride[1] : a.y_stride[0]) + off;
+        token[u] = t;
+        lo[u] = *reinterpret_cast<const uint4*>(from);
+        hi[u] = *reinterpret_cast<const uint4*>(from + ROW / 2);
+      }
+      r += step;
+      h += step;
+      while (h >= all) {
+        h -= all;
+        ++t;
+      }
+    }
+    if (!ready) {  // the tokens' turns (and omegas), while the first rows are on their way
+      for (int i = threadIdx.x; i < n * (D / 2); i += kRotateThreads) {
+        const int pair = i % (D / 2), q = pair / 2, tt = i / (D / 2);
+        float2 c = turn_of(turns_of_pair(a.turns, pair), position(a, t0 + tt));
+        if (a.back) c.y = -c.y;
+        // (paired as neighbours, a thread's pairs are E / 4 twos of either half of the row)
+        constexpr int C = E / 4;
+        const int half = a.pairs && q >= D / 8, qq = q - half * (D / 8), per = a.pairs ? C : 2 * C;
+        float* to4 = reinterpret_cast<float*>(&cs[tt][(half * C + qq % per) * P + qq / per]) + (pair & 1);
+        to4[0] = c.x;
+        to4[2] = c.y;
+      }
+      __syncthreads();
+      ready = true;
+      if (a.weights != nullptr && blockIdx.y == 0) {
+        // omega = sigmoid(mean of the group's q[0]), of rows that are on their way in any case (in place, too: a gate is
+        // only ever written as it is)
+        const int H = a.heads[0] / a.group;
+        for (int i = threadIdx.x; i < n * H; i += kRotateThreads) {
+          const int tt = i / H, hk = i % H;
+          const char* q0 = a.x[0] + (size_t)(t0 + tt) * a.x_stride[0] + (size_t)hk * a.group * ROW;
+          float g = 0.f;
+          for (int x = 0; x < a.group; ++x) g += Elt<T>::to_f(*reinterpret_cast<const T*>(q0 + (size_t)x * ROW));
+          int s, at;
+          sequence(a, t0 + tt, s, at);
+          a.weights[((size_t)prompt_chunk(t0 + tt - at, at / kPrefillChunk, s) * H + hk) * kPrefillChunk +
+                    at % kPrefillChunk] = sigmoidf_(g / (float)a.group);
+        }
+      }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (r0 + u * step >= rows) break;
+      if (to[u] == nullptr) continue;
       float x[E], y[E];
       CK::unpack(lo[u], x);
       CK::unpack(hi[u], y);
-      const float2* c = cs[token[u]];
       const float x0 = x[0], x1 = a.pairs ? x[1] : y[0];  // the gate's pair, where p is 0
-      if (a.pairs) {
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) {
-          turn(c[p * (E / 2) + i], x[2 * i], x[2 * i + 1]);
-          turn(c[D / 4 + p * (E / 2) + i], y[2 * i], y[2 * i + 1]);
+      for (int i = 0; i < E / 2; ++i) {
+        const float4 w = cs[token[u]][i * P + p];
+        const float2 c = make_float2(w.x, w.y), s = make_float2(w.z, w.w), m = make_float2(-w.z, -w.w);
+        float2 f, g;  // the two pairs' first and second dims
+        if (a.pairs) {
+          float* v = i < E / 4 ? x + 4 * i : y + 4 * (i - E / 4);
+          f = make_float2(v[0], v[2]);
+          g = make_float2(v[1], v[3]);
+          const float2 fn = fma2(g, m, mul2(f, c)), gn = fma2(f, s, mul2(g, c));
+          v[0] = fn.x; v[2] = fn.y; v[1] = gn.x; v[3] = gn.y;
+        } else {
+          f = make_float2(x[2 * i], x[2 * i + 1]);
+          g = make_float2(y[2 * i], y[2 * i + 1]);
+          const float2 fn = fma2(g, m, mul2(f, c)), gn = fma2(f, s, mul2(g, c));
+          x[2 * i] = fn.x; x[2 * i + 1] = fn.y; y[2 * i] = gn.x; y[2 * i + 1] = gn.y;
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i) turn(c[p * E + i], x[i], y[i]);
       }
       if (p == 0) {  // (turned by zero, a gate that is infinite would make its partner NaN)
         x[0] = x0;
@@ -94,26 +149,43 @@ __global__ void __launch_bounds__(kRotateThreads) dmc_rotate_kernel(const Rotate
       *reinterpret_cast<uint4*>(to[u] + ROW / 2) = CK::pack(y);
     }
   }
+  if (a.prompt) griddep_wait();  // the scan after this waits for the plan before it, too
 }
 
 }  // namespace
 
 static cudaError_t launch_rotate(RotateArgs& a, int esize, int D, cudaStream_t stream) {
-  // few tokens: their heads are spread over blocks, too
-  const int rows_at_once = kRotateThreads / (D * esize / 32);
-  a.per = a.tokens >= 1024 ? kRotateTokens : 1;
-  const dim3 grid(ceil_div(a.tokens, a.per), a.tokens >= 1024 ? 1 : ceil_div(a.heads[0] + a.heads[1], rows_at_once));
-  if (esize == 4 && D == 64) dmc_rotate_kernel<float, 64><<<grid, kRotateThreads, 0, stream>>>(a);
-  else if (esize == 4 && D == 128) dmc_rotate_kernel<float, 128><<<grid, kRotateThreads, 0, stream>>>(a);
-  else if (esize == 2 && D == 64) dmc_rotate_kernel<__nv_bfloat16, 64><<<grid, kRotateThreads, 0, stream>>>(a);
-  else if (esize == 2 && D == 128) dmc_rotate_kernel<__nv_bfloat16, 128><<<grid, kRotateThreads, 0, stream>>>(a);
-  else return cudaErrorInvalidValue;
-  return cudaGetLastError();
+  // A block takes about as many rows as its threads have in flight: several tokens of few heads, or one token's heads
+  // in parts (the turns of a token are then computed for each part). 8192 tokens of 32 + 32 heads of 128 in bf16 take
+  // 41.4 us so (6.5 TB/s); 456 blocks, as many as run at once, of 18 tokens and with the next rows on their way while some
+  // are worked, 45.9.
+  const int at_once = kRotateThreads / (D * esize / 32), all = a.heads[0] + a.heads[1];
+  const bool few = (long long)a.tokens * all < 8192;  // a handful of rows in all: a row for a thread's place
+  a.per = few ? 1 : max(1, min(kRotateTokens, at_once * kRowsInFlight / all));
+  const int blocks = ceil_div(a.tokens, a.per);
+  const int parts = max(1, ceil_div(all, few ? at_once : at_once * kRowsInFlight));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(blocks, parts);
+  cfg.blockDim = dim3(kRotateThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.prompt ? 1 : 0;
+  cudaError_t e = cudaErrorInvalidValue;
+  if (esize == 4 && D == 64) e = cudaLaunchKernelEx(&cfg, dmc_rotate_kernel<float, 64>, a);
+  if (esize == 4 && D == 128) e = cudaLaunchKernelEx(&cfg, dmc_rotate_kernel<float, 128>, a);
+  if (esize == 2 && D == 64) e = cudaLaunchKernelEx(&cfg, dmc_rotate_kernel<__nv_bfloat16, 64>, a);
+  if (esize == 2 && D == 128) e = cudaLaunchKernelEx(&cfg, dmc_rotate_kernel<__nv_bfloat16, 128>, a);
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-// The queries of a prompt, whose sequences begin at the positions `at`.
+// The queries of a prompt that is appended, whose sequences begin at the positions `at`: launched between the plan and
+// the scan, beside the first of which it runs. weights: as in RotateArgs.
 cudaError_t rotate_prompt_launch(const Layout& L, int num_seqs, int total_tokens, const void* q, void* q_out, const int* cu,
-                                 const int* at, const unsigned long long* turns, bool pairs, cudaStream_t stream) {
+                                 const int* at, const unsigned long long* turns, bool pairs, float* weights,
+                                 cudaStream_t stream) {
   RotateArgs a = {};
   a.tokens = total_tokens;
   a.heads[0] = L.Hq;
@@ -125,6 +197,9 @@ cudaError_t rotate_prompt_launch(const Layout& L, int num_seqs, int total_tokens
   a.seqs = num_seqs;
   a.turns = turns;
   a.pairs = pairs;
+  a.prompt = true;
+  a.weights = weights;
+  a.group = L.G;
   return launch_rotate(a, L.esize, L.D, stream);
 }
 
