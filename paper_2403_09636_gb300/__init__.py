@@ -352,6 +352,10 @@ class DmcCache:
         st, self.handle = dmc_cache_create(self.cfg, self.arena.data_ptr(), self.nbytes,
                                            self._s(stream))
         _check(st, "dmc_cache_create")
+        self.lib = lib()
+        self.num_q_heads, self.num_kv_heads, self.head_dim = int(num_q_heads), int(num_kv_heads), int(head_dim)
+        self.queries = (int(batch), self.num_q_heads, self.head_dim)
+        self._raw, self._empty_like, self._int32 = torch._C._cuda_getCurrentRawStream, torch.empty_like, torch.int32
 
     def _s(self, stream):
         if stream is None:
@@ -405,28 +409,48 @@ class DmcCache:
                                       k.data_ptr(), v.data_ptr(), out.data_ptr(), self._s(stream)),
                "dmc_decode_step_layers")
 
-    # ---- calls that check their tensors (what does not fit is refused with ValueError)
+    # ---- calls that check their tensors (what does not fit is refused with ValueError). The check is one expression,
+    # and only where it fails is the tensor looked for that does not fit: with a check for each tensor an append took the
+    # host 11.9 us, 6.9 so
 
     def _is(self, name, t, shape, dtype):
         torch = self.torch
-        if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_cuda
-                and t.get_device() == self.index and t.is_contiguous()):
+        if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == self.index
+                and t.is_contiguous()):
             return t.data_ptr()
         what = f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
         raise ValueError(f"{name} must be contiguous {dtype} {tuple(shape)} on {self.device}, got {what}")
 
-    def _out(self, name, out, like, stream):
-        """`out`, or a new tensor as `like`, of memory that belongs to the call's stream."""
+    def _new(self, like, stream):
+        """A tensor as `like`, of memory that belongs to the call's stream."""
         torch = self.torch
-        if out is None:
-            raw = self._s(stream)
-            if stream is None or raw == self._s(None):
-                return torch.empty_like(like)
-            other = torch.cuda.ExternalStream(raw, device=self.device) if raw else torch.cuda.default_stream(self.device)
-            with torch.cuda.stream(other):
-                return torch.empty_like(like)
-        self._is(name, out, like.shape, like.dtype)
-        return out
+        raw = self._s(stream)
+        if raw == self._s(None):
+            return torch.empty_like(like)
+        other = torch.cuda.ExternalStream(raw, device=self.device) if raw else torch.cuda.default_stream(self.device)
+        with torch.cuda.stream(other):
+            return torch.empty_like(like)
+
+    def _append_is_wrong(self, q, k, v, positions, rotary, cu_seqlens, n, q_out):
+        c, t = self.cfg, self.torch
+        if not isinstance(k, t.Tensor) or k.dim() != 3:
+            raise ValueError("k must be [tokens, KV heads, head_dim]")
+        T, D, dt = k.shape[0], c.head_dim, self.dtype
+        self._is("q", q, (T, c.num_q_heads, D), dt)
+        self._is("k", k, (T, c.num_kv_heads, D), dt)
+        self._is("v", v, (T, c.num_kv_heads, D), dt)
+        if cu_seqlens is not None:
+            if not isinstance(cu_seqlens, t.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1:
+                raise ValueError("cu_seqlens must be int32 [sequences + 1]")
+            n = cu_seqlens.numel() - 1
+            self._is("cu_seqlens", cu_seqlens, (n + 1,), t.int32)
+        if rotary is None:
+            raise ValueError("positions and q_out are for a rotation")
+        if rotary.head_dim != D or rotary.index != self.index:
+            raise ValueError(f"the rotation is for heads of {rotary.head_dim} on {rotary.turns.device}")
+        self._is("positions", positions, (n,), t.int32)
+        self._is("q_out", q_out, (T, c.num_q_heads, D), dt)
+        raise ValueError("the tensors do not fit")
 
     def append(self, layer, q, k, v, positions=None, rotary=None, cu_seqlens=None, max_seqlen=1, first_seq=0, q_out=None,
                stream=None):
@@ -434,42 +458,57 @@ class DmcCache:
         q: [T, Hq, D]; k, v: [T, Hkv, D], of one token for each of T sequences from first_seq on, or packed
         by cu_seqlens (int32 [sequences + 1]); positions: int32, one for each sequence's first token; rotary: a
         `rotary.Rotary`; q_out may be q."""
-        c, t = self.cfg, self.torch
-        if not isinstance(k, t.Tensor) or k.dim() != 3:
-            raise ValueError("k must be [tokens, KV heads, head_dim]")
-        T, D = k.shape[0], c.head_dim
-        ptrs = (self._is("q", q, (T, c.num_q_heads, D), self.dtype), self._is("k", k, (T, c.num_kv_heads, D), self.dtype),
-                self._is("v", v, (T, c.num_kv_heads, D), self.dtype))
-        n, cu = T, None
-        if cu_seqlens is not None:
-            if not isinstance(cu_seqlens, t.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1:
-                raise ValueError("cu_seqlens must be int32 [sequences + 1]")
-            n = cu_seqlens.numel() - 1
-            cu = self._is("cu_seqlens", cu_seqlens, (n + 1,), t.int32)
+        i32, dt, index = self._int32, self.dtype, self.index
+        try:
+            T, H, D = rows = k.shape
+            queries = (T, self.num_q_heads, D)
+            n = T if cu_seqlens is None else cu_seqlens.numel() - 1
+            fits = (H == self.num_kv_heads and D == self.head_dim and q.shape == queries and v.shape == rows
+                    and q.dtype is dt and k.dtype is dt and v.dtype is dt and q.get_device() == index
+                    and k.get_device() == index and v.get_device() == index and q.is_contiguous() and k.is_contiguous()
+                    and v.is_contiguous())
+            if cu_seqlens is not None:
+                fits = (fits and cu_seqlens.dim() == 1 and cu_seqlens.dtype is i32 and cu_seqlens.get_device() == index
+                        and cu_seqlens.is_contiguous())
+            if rotary is None:
+                fits = fits and positions is None and q_out is None
+            else:
+                fits = (fits and rotary.head_dim == D and rotary.index == index and positions.shape == (n,)
+                        and positions.dtype is i32 and positions.get_device() == index and positions.is_contiguous())
+                if q_out is not None:
+                    fits = (fits and q_out.shape == queries and q_out.dtype is dt and q_out.get_device() == index
+                            and q_out.is_contiguous())
+        except (AttributeError, TypeError, ValueError):
+            fits, n = False, 0
+        if not fits:
+            self._append_is_wrong(q, k, v, positions, rotary, cu_seqlens, n, q_out)
+        raw = self._raw(index) if stream is None else self._s(stream)
         at = turns = to = None
         pairs = 0
-        if rotary is None:
-            if positions is not None or q_out is not None:
-                raise ValueError("positions and q_out are for a rotation")
-        else:
-            if rotary.head_dim != D or rotary.turns.get_device() != self.index:
-                raise ValueError(f"the rotation is for heads of {rotary.head_dim} on {rotary.turns.device}")
-            at = self._is("positions", positions, (n,), t.int32)
-            turns, pairs = rotary.turns.data_ptr(), int(rotary.interleaved)
-            q_out = self._out("q_out", q_out, q, stream)
-            to = q_out.data_ptr()
-        st = dmc_cache_append(self.handle, layer, first_seq, n, *ptrs, cu, T, min(int(max_seqlen), T), at, turns, pairs, to,
-                              self._s(stream))
+        if rotary is not None:
+            if q_out is None:
+                q_out = self._empty_like(q) if stream is None else self._new(q, stream)
+            at, turns, pairs, to = positions.data_ptr(), rotary.pointer, rotary.pairs, q_out.data_ptr()
+        st = self.lib.dmc_cache_append(self.handle, layer, first_seq, n, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                       None if cu_seqlens is None else cu_seqlens.data_ptr(), T,
+                                       max_seqlen if max_seqlen < T else T, at, turns, pairs, to, raw)
         if st:
             _check(st, "dmc_cache_append")
         return q_out
 
     def attend(self, layer, q, out=None, stream=None):
         """Attention of q [batch, Hq, D] over the cache as it stands; the cache is not changed."""
-        c = self.cfg
-        p = self._is("q", q, (c.batch, c.num_q_heads, c.head_dim), self.dtype)
-        out = self._out("out", out, q, stream)
-        st = dmc_cache_attend(self.handle, layer, p, out.data_ptr(), self._s(stream))
+        try:
+            fits = (q.shape == self.queries and q.dtype is self.dtype and q.get_device() == self.index and q.is_contiguous())
+        except AttributeError:
+            fits = False
+        p = q.data_ptr() if fits else self._is("q", q, self.queries, self.dtype)
+        if out is None:
+            out = self._empty_like(q) if stream is None else self._new(q, stream)
+            to = out.data_ptr()
+        else:
+            to = self._is("out", out, self.queries, self.dtype)
+        st = self.lib.dmc_cache_attend(self.handle, layer, p, to, self._raw(self.index) if stream is None else self._s(stream))
         if st:
             _check(st, "dmc_cache_attend")
         return out
@@ -479,9 +518,10 @@ class DmcCache:
         device), in every layer. What they have in common is shared."""
         if not isinstance(parents, self.torch.Tensor) or parents.dim() < 1:
             raise ValueError("parents must be int32, one for each sequence")
-        n = parents.numel()
         p = self._is("parents", parents, parents.shape, self.torch.int32)
-        _check(dmc_cache_reorder(self.handle, first_seq, n, p, self._s(stream)), "dmc_cache_reorder")
+        st = self.lib.dmc_cache_reorder(self.handle, first_seq, parents.numel(), p, self._s(stream))
+        if st:
+            _check(st, "dmc_cache_reorder")
 
     def lengths(self, layer, stream=None):
         t = self.torch
@@ -492,17 +532,19 @@ class DmcCache:
 
     def export_heads(self, layer, head_ids, cap, stream=None):
         t = self.torch
-        ids = t.as_tensor(head_ids, dtype=t.int32, device=self.device)
+        ids = head_ids
+        if not (isinstance(ids, t.Tensor) and ids.dtype is t.int32 and ids.get_device() == self.index and ids.is_contiguous()):
+            ids = t.as_tensor(head_ids, dtype=t.int32, device=self.device)
         n = ids.numel()
-        D = self.cfg.head_dim
+        D = self.head_dim
         k = t.empty((n, cap, D), dtype=self.dtype, device=self.device)  # padded: every row is written
-        v = t.empty((n, cap, D), dtype=self.dtype, device=self.device)
+        v = self._empty_like(k)
         z = t.empty((n, cap), dtype=t.float32, device=self.device)
         ln = t.empty(n, dtype=t.int32, device=self.device)
-        _check(dmc_cache_export_heads_padded(self.handle, layer, n, ids.data_ptr(), cap,
-                                             k.data_ptr(), v.data_ptr(), z.data_ptr(),
-                                             ln.data_ptr(), self._s(stream)),
-               "dmc_cache_export_heads")
+        st = self.lib.dmc_cache_export_heads_padded(self.handle, layer, n, ids.data_ptr(), cap, k.data_ptr(), v.data_ptr(),
+                                                    z.data_ptr(), ln.data_ptr(), self._s(stream))
+        if st:
+            _check(st, "dmc_cache_export_heads")
         return k, v, z, ln
 
     def status(self, stream=None):

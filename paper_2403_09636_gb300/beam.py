@@ -40,6 +40,11 @@ class BeamSelect:
         st, self.handle = dmc_beam_create(self.cfg, self.arena.data_ptr(), self.nbytes, self._raw(stream))
         _check(st, "dmc_beam_create")
         self.lib = lib()
+        self._shape = (self.groups, self.beams)
+        self._rows = (self.groups * self.beams, self.vocab)
+        shape = (self.groups, self.keep)
+        self._kinds = tuple(zip(("scores", "tokens", "parents", "done"), (torch.float32, torch.int32, torch.int32, torch.bool)))
+        self._like = [torch.empty(shape, dtype=t, device=dev) for _, t in self._kinds]  # of the results
 
     def _raw(self, stream):
         if stream is None:
@@ -80,26 +85,36 @@ class BeamSelect:
         """(scores fp32, tokens int32, parents int32, done bool), [groups, keep]: the best continuations, best first.
         logits: [groups * beams, vocab], rows may be apart; scores: fp32 [groups, beams]; finished: bool
         [groups, beams] or None; eos: the end word, -1 for none. parents are rows of logits."""
-        G, B, V = self.groups, self.beams, self.vocab
-        if (not isinstance(logits, torch.Tensor) or logits.dtype is not self.dtype or logits.shape != (G * B, V)
-                or logits.get_device() != self.index or (V > 1 and logits.stride(1) != 1)
-                or (G * B > 1 and logits.stride(0) < V)):
-            raise ValueError(f"logits must be {self.dtype} {(G * B, V)} on {self.device}, words contiguous, rows apart")
-        sp = self._is("scores", scores, (G, B), torch.float32)
-        fp = None if finished is None else self._is("finished", finished, (G, B), torch.bool)
-        shape = (G, self.keep)
-        kinds = (torch.float32, torch.int32, torch.int32, torch.bool)
+        rows, index = self._rows, self.index
+        if (not isinstance(logits, torch.Tensor) or logits.dtype is not self.dtype or logits.shape != rows
+                or logits.get_device() != index):
+            raise ValueError(f"logits must be {self.dtype} {rows} on {self.device}")
+        apart, step = logits.stride()
+        if rows[0] == 1:
+            apart = rows[1]
+        if apart < rows[1] or (step != 1 and rows[1] > 1):
+            raise ValueError(f"logits' words must be contiguous and its rows apart, got strides {logits.stride()}")
+        shape = self._shape
+        if (isinstance(scores, torch.Tensor) and scores.dtype is torch.float32 and scores.shape == shape
+                and scores.get_device() == index and scores.is_contiguous()):
+            sp = scores.data_ptr()
+        else:
+            sp = self._is("scores", scores, shape, torch.float32)
+        fp = None if finished is None else self._is("finished", finished, shape, torch.bool)
+        raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else self._raw(stream)
+        like = self._like
         if out is None:
-            out = self._on(stream, lambda: tuple([torch.empty(shape, dtype=t, device=self.device) for t in kinds]))
-        elif len(out) != 4:
-            raise ValueError("out must hold 4 tensors: scores, tokens, parents, done")
-        ptrs = [self._is(n, t, shape, k) for n, t, k in zip(("scores", "tokens", "parents", "done"), out, kinds)]
-        raw = self._raw(stream)
+            out = s, t, p, d = (tuple(map(torch.empty_like, like)) if stream is None
+                                else self._on(stream, lambda: tuple(map(torch.empty_like, like))))
+            ptrs = (s.data_ptr(), t.data_ptr(), p.data_ptr(), d.data_ptr())
+        else:
+            if len(out) != 4:
+                raise ValueError("out must hold 4 tensors: scores, tokens, parents, done")
+            ptrs = [self._is(name, t, x.shape, kind) for (name, kind), t, x in zip(self._kinds, out, like)]
         if raw not in self._streams:
             self.arena.record_stream(self._stream(raw))
             self._streams.add(raw)
-        st = self.lib.dmc_beam_select(self.handle, logits.data_ptr(), logits.stride(0) if G * B > 1 else V, sp, fp, int(eos),
-                                      *ptrs, raw)
+        st = self.lib.dmc_beam_select(self.handle, logits.data_ptr(), apart, sp, fp, eos, *ptrs, raw)
         if st:
             _check(st, "dmc_beam_select")
         return out

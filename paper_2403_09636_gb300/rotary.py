@@ -12,7 +12,6 @@ The pair that holds dimension 0, the method's gate, is not rotated.
 from __future__ import annotations
 
 import math
-from fractions import Fraction
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -20,8 +19,15 @@ from torch.autograd.function import once_differentiable
 from . import DMC_BF16, DMC_F32, _check, lib
 
 _CODES = {torch.float32: DMC_F32, torch.bfloat16: DMC_BF16}
-# 1 / (2 pi), to 2^-140: turns times 2^64 of frequencies from 2^-64 up keep all of their 53 bits
-_TURN = Fraction(0x28BE60DB9391054A7F09D5F47D4D377036E, 1 << 140)
+# 1 / (2 pi), times 2^140: turns times 2^64 of frequencies from 2^-64 up keep all of their 53 bits
+_TURN = 0x28BE60DB9391054A7F09D5F47D4D377036E
+
+
+def _turns(x):
+    """x radians in turns modulo one, times 2^64, rounded, as the int64 with the same bits."""
+    n, d = float(x).as_integer_ratio()
+    bits = (((n * _TURN << 1) // (d << 76)) + 1 >> 1) % (1 << 64)  # 2^64 / 2^140
+    return bits - (1 << 64) if bits >> 63 else bits
 
 
 class Rotary:
@@ -39,60 +45,78 @@ class Rotary:
             values = inv_freq.tolist() if isinstance(inv_freq, torch.Tensor) else [float(x) for x in inv_freq]
         if len(values) != head_dim // 2 or not all(math.isfinite(x) for x in values):
             raise ValueError(f"inv_freq must hold {head_dim // 2} finite numbers")
-        # turns per token modulo one, times 2^64, as the int64 with the same bits
-        bits = [round(Fraction(x) * _TURN * (1 << 64)) % (1 << 64) for x in values]
         self.head_dim, self.interleaved = head_dim, bool(interleaved)
-        self.turns = torch.tensor([b - (1 << 64) if b >> 63 else b for b in bits], dtype=torch.int64,
+        self.turns = torch.tensor([_turns(x) for x in values], dtype=torch.int64,
                                   device=device if device is not None else "cuda")
+        self.index, self.pointer, self.pairs = self.turns.get_device(), self.turns.data_ptr(), int(self.interleaved)
 
 
-def _rows(rotary, name, x, tokens, dtype):
-    """Pointer, heads and token stride of [tokens, heads, head_dim] whose heads are contiguous."""
+def _stride(rotary, name, x, tokens, dtype):
+    """Token stride of [tokens, heads, head_dim] whose heads are contiguous."""
     D = rotary.head_dim
-    if (not isinstance(x, torch.Tensor) or x.dim() != 3 or x.shape[0] != tokens or x.shape[2] != D or x.dtype is not dtype
-            or x.device != rotary.turns.device):
-        raise ValueError(f"{name} must be {dtype} [{tokens}, heads, {D}] on {rotary.turns.device}")
-    H = x.shape[1]
-    stride = x.stride(0) if tokens > 1 else H * D
-    if x.numel() and ((H > 1 and x.stride(1) != D) or x.stride(2) != 1 or stride < H * D):
-        raise ValueError(f"{name}'s heads must be contiguous and its tokens apart, got strides {x.stride()}")
-    return H, x.data_ptr(), stride
+    try:
+        T, H, width = x.shape
+        a, b, c = x.stride()
+        row = H * D
+        if (T == tokens and width == D and x.dtype is dtype and x.get_device() == rotary.index and c == 1
+                and (b == D or H <= 1) and (a >= row or T <= 1)):
+            return a if T > 1 else row
+    except (AttributeError, TypeError, ValueError):
+        pass
+    what = f"{x.dtype} {tuple(x.shape)}, strides {x.stride()}, on {x.device}" if isinstance(x, torch.Tensor) else type(x).__name__
+    raise ValueError(f"{name} must be {dtype} [{tokens}, heads, {D}] on {rotary.turns.device}, its heads contiguous, its "
+                     f"tokens apart, got {what}")
 
 
 def rotate(rotary, q, k, positions, inverse=False, out=None, stream=None):
     """(q', k'): q [T, Hq, D] and k [T, Hkv, D] (or None) rotated to positions, int32 [T], in one launch; inverse rotates
     back. Heads are contiguous, tokens may be apart (a slice of a joint projection). out: (q', k') tensors, which may be
     q and k themselves."""
-    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.dtype not in _CODES:
+    dt = getattr(q, "dtype", None)
+    if dt not in _CODES or q.dim() != 3:
         raise ValueError("q must be float32 or bfloat16 [tokens, heads, head_dim]")
-    T, dt, dev = q.shape[0], q.dtype, rotary.turns.device
+    T, hq, D = q.shape
+    index = rotary.index
     if (not isinstance(positions, torch.Tensor) or positions.dtype is not torch.int32 or positions.shape != (T,)
-            or positions.device != dev or not positions.is_contiguous()):
-        raise ValueError(f"positions must be contiguous int32 ({T},) on {dev}")
-    given = (_rows(rotary, "q", q, T, dt), (0, None, 0) if k is None else _rows(rotary, "k", k, T, dt))
-    raw = torch._C._cuda_getCurrentRawStream(dev.index)
+            or positions.get_device() != index or not positions.is_contiguous()):
+        raise ValueError(f"positions must be contiguous int32 ({T},) on {rotary.turns.device}")
+    qs = _stride(rotary, "q", q, T, dt)
+    hk = ks = kos = 0
+    if k is not None:
+        ks, hk = _stride(rotary, "k", k, T, dt), k.shape[1]
+    raw = torch._C._cuda_getCurrentRawStream(index)
     number = raw if stream is None else stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
     if out is None:
-        def new(x):
-            return None if x is None else torch.empty(x.shape, dtype=dt, device=dev)
         if number == raw:
-            out = (new(q), new(k))
+            out = _new(q, k)
         else:
-            other = torch.cuda.ExternalStream(number, device=dev) if number else torch.cuda.default_stream(dev)
-            with torch.cuda.stream(other):
-                out = (new(q), new(k))
-    elif len(out) != 2 or (out[1] is None) != (k is None):
-        raise ValueError("out must hold q' and k'")
-    to = (_rows(rotary, "q'", out[0], T, dt), (0, None, 0) if k is None else _rows(rotary, "k'", out[1], T, dt))
-    if to[0][0] != given[0][0] or to[1][0] != given[1][0]:
-        raise ValueError("out must have the shapes of q and k")
-    (hq, qp, qs), (hk, kp, ks) = given
-    st = lib().dmc_rotate(_CODES[dt], rotary.head_dim, T, positions.data_ptr(), rotary.turns.data_ptr(),
-                          int(rotary.interleaved), int(bool(inverse)), hq, qp, qs, to[0][1], to[0][2], hk, kp, ks, to[1][1],
-                          to[1][2], number)
+            dev = rotary.turns.device
+            with torch.cuda.stream(torch.cuda.ExternalStream(number, device=dev) if number else torch.cuda.default_stream(dev)):
+                out = _new(q, k)
+        qos, kos = hq * D, hk * D
+    else:
+        if len(out) != 2 or (out[1] is None) != (k is None):
+            raise ValueError("out must hold q' and k'")
+        qos = _stride(rotary, "q'", out[0], T, dt)
+        if k is not None:
+            kos = _stride(rotary, "k'", out[1], T, dt)
+        if out[0].shape[1] != hq or (k is not None and out[1].shape[1] != hk):
+            raise ValueError("out must have the shapes of q and k")
+    qo, ko = out
+    st = lib().dmc_rotate(_CODES[dt], D, T, positions.data_ptr(), rotary.pointer, rotary.pairs, 1 if inverse else 0, hq,
+                          q.data_ptr(), qs, qo.data_ptr(), qos, hk, None if k is None else k.data_ptr(), ks,
+                          None if k is None else ko.data_ptr(), kos, number)
     if st:
         _check(st, "dmc_rotate")
     return out
+
+
+def _new(q, k):
+    # (empty_like keeps the strides of what is not dense)
+    qo = torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k is None:
+        return qo, None
+    return qo, torch.empty_like(k) if k.is_contiguous() else torch.empty(k.shape, dtype=k.dtype, device=k.device)
 
 
 class _Apply(torch.autograd.Function):
