@@ -51,7 +51,7 @@ struct dmc_cache {
   bool gqa;  // grouped queries on the tensor-core kernel (one worker per KV head)
   dmc::DecodePlan plan;
   dmc::DecodeOrder order;
-  char* meta;  // lengths, ctl, counters, pool, error, page use: cleared by create / reset
+  char* meta;  // lengths, ctl, counters, pool, error: cleared by create / reset
   size_t meta_bytes;
   float* carry;    // segment sums at prompt chunk starts (prompt attention)
   float* weights;  // decisions and omegas of the prompt's chunks (prompt attention)
@@ -107,8 +107,8 @@ Offsets offsets(const dmc_cache_config* c) {
   o.pool_top = at; at = align_up(at + 4 * 8);
   o.error = at; at = align_up(at + 4);
   o.unbounded = at; at = align_up(at + 4);
-  o.page_use = at; at = align_up(at + (size_t)c->num_pages * 8);
   o.meta_end = at;
+  o.page_use = at; at = align_up(at + (size_t)c->num_pages * 8);
   // Both decode kernels (the CUDA-core one for every cache but grouped bf16
   // queries of 2 to 8 per KV head, which run on the tensor-core kernel) keep
   // their split-K states per layer, and the CUDA-core one its pending rows: one
@@ -154,9 +154,11 @@ __global__ void lengths_copy_kernel(const Layout L, int layer, int* out) {
 // One block per kExportSlots slots of an exported head, as 16-byte pieces: a
 // head's share of a block, whatever its length, so that one long head is as well
 // spread as many short ones. pad: the slots from the head's count to cap become
-// zeros (otherwise they are left alone). Bound by HBM: 7B shape, 1024 heads of ~520
-// slots into buffers of 640, 268 MB read and 341 MB written in ~90 us; filling the
-// buffers with zeros and then copying took ~190.
+// zeros (otherwise they are left alone). A thread has eight pieces in flight, and the
+// block's page ids are read once. Bound by HBM: 7B shape, 1024 heads of ~520
+// slots into buffers of 640, 268 MB read and 341 MB written in 89 us (one piece of K and V
+// at a time 90; 128 heads 12 us, 14 so); filling the buffers with zeros and then copying
+// took ~190.
 constexpr int kExportSlots = 64;
 // Blocks of a plain export, what a GB300 holds at once: its heads' lengths are only
 // known on the device, so a block takes every gridDim.y-th piece of a head. (With a
@@ -164,10 +166,15 @@ constexpr int kExportSlots = 64;
 // into buffers of 8192 325 us, 91 so and 93 with one block per head, which takes 1049
 // for 8 heads of 16384 slots, 25 so.)
 constexpr int kExportBlocks = 1216;
+constexpr int kExportThreads = 256;
 
-template <bool kPad>
-__global__ void __launch_bounds__(256) export_kernel(const Layout L, int layer, const int* ids, int cap, char* kout,
-                                                     char* vout, float* zout, int* lout) {
+template <bool kPad, int kRow>
+__global__ void __launch_bounds__(kExportThreads) export_kernel(const Layout L, int layer, const int* ids, int cap,
+                                                                char* kout, char* vout, float* zout, int* lout) {
+  constexpr int kPieces = kRow / 16, kPagesOf = kExportSlots / dmc::kPage;
+  constexpr int U = 4;  // of K and of V in flight
+  static_assert(kExportSlots * kPieces % kExportThreads == 0, "whole rounds of the block");
+  __shared__ int s_page[kPagesOf];
   const int i = blockIdx.x;
   const int bh = ids[i];
   const int parity = *reinterpret_cast<volatile int*>(&L.ctl[layer * 4]);
@@ -175,26 +182,48 @@ __global__ void __launch_bounds__(256) export_kernel(const Layout L, int layer, 
   const int len = known ? L.lengths[((size_t)layer * 2 + parity) * L.NH + bh] : -1;
   if (threadIdx.x == 0 && blockIdx.y == 0) lout[i] = len;
   const int n = min(max(len, 0), cap), all = kPad ? cap : n;
-  const int pieces = L.row_bytes / 16;
   const int* pt = L.page_table + ((size_t)layer * L.NH + (known ? bh : 0)) * L.MPH;
   for (long long s0 = (long long)blockIdx.y * kExportSlots; s0 < all; s0 += (long long)gridDim.y * kExportSlots) {
     const int first = (int)s0, end = (int)min(s0 + kExportSlots, (long long)all);
-    for (int x = threadIdx.x; x < (end - first) * pieces; x += blockDim.x) {
-      const int s = first + x / pieces, p = x % pieces;
-      uint4 k = make_uint4(0, 0, 0, 0), v = k;
-      if (s < n) {
-        const char* src = L.pages + (size_t)pt[s / dmc::kPage] * L.page_bytes +
-                          (size_t)(s % dmc::kPage) * L.row_bytes + p * 16;
-        k = *reinterpret_cast<const uint4*>(src);
-        v = *reinterpret_cast<const uint4*>(src + (size_t)dmc::kPage * L.row_bytes);
+    __syncthreads();
+    if (threadIdx.x < kPagesOf && first + threadIdx.x * dmc::kPage < n)
+      s_page[threadIdx.x] = pt[first / dmc::kPage + threadIdx.x];
+    __syncthreads();
+    for (int x0 = threadIdx.x; x0 < (end - first) * kPieces; x0 += U * kExportThreads) {
+      uint4 k[U], v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int x = x0 + u * kExportThreads, s = x / kPieces, p = x % kPieces;
+        k[u] = v[u] = make_uint4(0, 0, 0, 0);
+        if (first + s < min(n, end)) {
+          const char* src = L.pages + (size_t)s_page[s / dmc::kPage] * L.page_bytes + (s % dmc::kPage) * kRow + p * 16;
+          k[u] = *reinterpret_cast<const uint4*>(src);
+          v[u] = *reinterpret_cast<const uint4*>(src + dmc::kPage * kRow);
+        }
       }
-      const size_t dst = ((size_t)i * cap + s) * L.row_bytes + p * 16;
-      *reinterpret_cast<uint4*>(kout + dst) = k;
-      *reinterpret_cast<uint4*>(vout + dst) = v;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int x = x0 + u * kExportThreads;
+        if (x < (end - first) * kPieces) {
+          const size_t dst = ((size_t)i * cap + first) * kRow + (size_t)x * 16;
+          *reinterpret_cast<uint4*>(kout + dst) = k[u];
+          *reinterpret_cast<uint4*>(vout + dst) = v[u];
+        }
+      }
     }
-    for (int s = first + threadIdx.x; s < end; s += blockDim.x)
-      zout[(size_t)i * cap + s] = s < n ? L.z[(size_t)pt[s / dmc::kPage] * dmc::kPage + s % dmc::kPage] : 0.f;
+    for (int s = threadIdx.x; s < end - first; s += kExportThreads)
+      zout[(size_t)i * cap + first + s] =
+          first + s < n ? L.z[(size_t)s_page[s / dmc::kPage] * dmc::kPage + s % dmc::kPage] : 0.f;
   }
+}
+
+template <bool kPad>
+void export_launch(const Layout& L, dim3 grid, int layer, const int* ids, int cap, char* k, char* v, float* z, int* len,
+                   cudaStream_t stream) {
+  auto* kernel = L.row_bytes == 128   ? export_kernel<kPad, 128>
+                 : L.row_bytes == 256 ? export_kernel<kPad, 256>
+                                      : export_kernel<kPad, 512>;
+  kernel<<<grid, kExportThreads, 0, stream>>>(L, layer, ids, cap, k, v, z, len);
 }
 
 dmc_status export_heads(dmc_cache_t c, bool pad, int32_t layer, int32_t n, const int32_t* head_ids_dev, int32_t cap,
@@ -209,9 +238,8 @@ dmc_status export_heads(dmc_cache_t c, bool pad, int32_t layer, int32_t n, const
   const int slots = pad ? cap : min(cap, c->lay.max_slots);
   const int most = pad ? 65535 : dmc::ceil_div(kExportBlocks, n);
   const dim3 grid(n, max(1, min(dmc::ceil_div(slots, kExportSlots), most)));
-  auto* kernel = pad ? export_kernel<true> : export_kernel<false>;
-  kernel<<<grid, 256, 0, stream>>>(c->lay, layer, head_ids_dev, cap, static_cast<char*>(k_out_dev),
-                                   static_cast<char*>(v_out_dev), z_out_dev, len_out_dev);
+  (pad ? export_launch<true> : export_launch<false>)(c->lay, grid, layer, head_ids_dev, cap, static_cast<char*>(k_out_dev),
+                                                     static_cast<char*>(v_out_dev), z_out_dev, len_out_dev, stream);
   return cuda_status(cudaGetLastError());
 }
 

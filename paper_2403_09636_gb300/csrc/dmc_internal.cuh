@@ -42,7 +42,8 @@ struct Layout {
   float* pending_z;        // [L][NH]: their z
   unsigned long long* pool_top;  // [4]: pages taken, pages given back, of those by the running launch too, its blocks done
   int2* page_use;          // [num_pages]: x: heads that hold the page beside the first (reordered sequences share what
-                           // they have in common); y: the given back page of that turn (see take_page)
+                           // they have in common), set when the page is taken; y: the given back page of that turn
+                           // (page_in_turn). Neither has to be cleared when the cache is emptied.
   unsigned int* error;
   unsigned int* unbounded; // prompt attention: the call has written a slot whose value is not finite
   float* partials;         // [partial_cap][D + 2]: split-K partial softmax states (m, l, acc)
@@ -166,7 +167,11 @@ __device__ __forceinline__ bool pages_in_pool(const Layout& L, unsigned long lon
 // One page for a head, or -1 with the fault bit set.
 __device__ __forceinline__ int take_page(const Layout& L) {
   const unsigned long long at = atomicAdd(L.pool_top, 1ull);
-  if (pages_in_pool(L, at, 1)) return page_in_turn(L, at);
+  if (pages_in_pool(L, at, 1)) {
+    const int page = page_in_turn(L, at);
+    L.page_use[page].x = 0;
+    return page;
+  }
   atomicOr(L.error, DMC_FAULT_PAGES_EXHAUSTED);
   return -1;
 }

@@ -259,8 +259,9 @@ __global__ void __launch_bounds__(kPlanThreads) dmc_prefill_plan_kernel(const Pr
       atomicOr(L.error, DMC_FAULT_SLOT_CAPACITY);
       fail = 1;
     } else if (need > 0) {
-      s_first = atomicAdd(L.pool_top, (unsigned long long)need);
-      if (!pages_in_pool(L, s_first, (unsigned long long)need)) {
+      const unsigned long long first = atomicAdd(L.pool_top, (unsigned long long)need);
+      s_first = first;
+      if (!pages_in_pool(L, first, (unsigned long long)need)) {
         atomicOr(L.error, DMC_FAULT_PAGES_EXHAUSTED);
         fail = 1;
       }
@@ -277,7 +278,11 @@ __global__ void __launch_bounds__(kPlanThreads) dmc_prefill_plan_kernel(const Pr
   }
   if (!fail) {
     int* pt = L.page_table + ((size_t)a.layer * L.NH + bh) * L.MPH;
-    for (int i = tid; i < need; i += kPlanThreads) pt[old_pages + i] = page_in_turn(L, s_first + i);
+    for (int i = tid; i < need; i += kPlanThreads) {
+      const int page = page_in_turn(L, s_first + i);
+      pt[old_pages + i] = page;
+      L.page_use[page].x = 0;
+    }
     if (tid == 0) len[bh] = len_new;
   }
 }

@@ -150,6 +150,26 @@ def test_pages_are_shared_and_come_back(cuda_dev):
     assert cache.status() == (0, 0, B * hkv)
 
 
+def test_emptied_after_sharing(cuda_dev):
+    """A cache that is emptied while its sequences share pages begins anew: the same steps give the same, over and over."""
+    cache = cache_of(4, 2, 2, 64, F32, 200, prompt=200, pages=40)
+    first = None
+    for _ in range(3):
+        g = torch.Generator().manual_seed(14)
+        q, k, v = (t.cuda() for t in tokens(g, 100, 2, 2, 64, F32, 0.9))
+        cache.prefill(0, q[..., 0], k, v, torch.tensor([0, 100], dtype=torch.int32).cuda(), 100)
+        reorder(cache, [0] * 4)
+        for i in range(60):
+            step(cache, g, opens=0.8)
+            if i % 9 == 8:
+                reorder(cache, torch.randint(0, 4, (4,), generator=g).tolist())
+        assert cache.status()[:2] == (0, 0)
+        got = exported(cache, 0, 200)
+        first = first or got
+        assert all(torch.equal(a, b) for a, b in zip(got, first))
+        cache.reset()
+
+
 def test_sequences_outside_the_call_stay(cuda_dev):
     cache = cache_of(7, 2, 2, 64, BF16, 80, layers=2)
     g = torch.Generator().manual_seed(8)
