@@ -228,7 +228,8 @@ dmc_status dmc_decode_step_static_scratch(dmc_cache_t cache, int32_t layer, cons
  * are those of fp32. Each result is rounded once.
  * ------------------------------------------------------------------------ */
 
-/* Rotates queries and keys of num_tokens tokens, in one launch.
+/* Rotates queries and keys of num_tokens tokens, in one launch. There is no handle: the
+ * pointers are of the current device.
  *   dtype: DMC_F32 or DMC_BF16; head_dim: 64 or 128;
  *   positions_dev: int32 [num_tokens];
  *   inverse: rotates back (the rotation's gradient);
@@ -256,7 +257,7 @@ dmc_status dmc_rotate(int32_t dtype, int32_t head_dim, int32_t num_tokens, const
  *          others follow one by one. (The cache cannot tell: it holds slots, not tokens.)
  *   turns_dev, interleaved: the rotation, as above. turns_dev NULL: none; positions_dev
  *          and q_out_dev are then not used and must be NULL;
- *   q_out_dev (written): as q_dev, which it may be. */
+ *   q_out_dev (written): as q_dev, which it may be. Rows of no sequence are left as they are. */
 dmc_status dmc_cache_append(dmc_cache_t cache, int32_t layer, int32_t first_seq, int32_t num_seqs, const void* q_dev,
                             const void* k_dev, const void* v_dev, const int32_t* cu_seqlens_dev, int32_t total_tokens,
                             int32_t max_seqlen, const int32_t* positions_dev, const uint64_t* turns_dev,
@@ -472,7 +473,7 @@ dmc_status dmc_retrofit_status(dmc_retrofit_t h, cudaStream_t stream, uint32_t* 
  * Beam search: selection. For every group of beams (one text) the `keep` best of
  * beams x vocab continuations:
  *   score(b, w) = scores[b] + logits[b, w] - log sum_w' exp(logits[b, w'])
- * in descending order; ties go to the lower b * vocab + w. A finished beam has one
+ * in descending order (a beam's own in that of its logits); ties go to the lower b * vocab + w. A finished beam has one
  * continuation, the end word, at its own score. A beam whose score, or whose log-sum, is not
  * a finite number offers its words at -infinity (so a search may begin with scores 0,
  * -inf, -inf, ...); single logits may be -infinity (masked words). Scores are compared

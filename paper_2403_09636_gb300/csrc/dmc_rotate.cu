@@ -30,8 +30,8 @@ struct RotateArgs {
   int group;       // queries per KV head
 };
 
-// The sequence of token t, and its place there.
-__device__ __forceinline__ void sequence(const RotateArgs& a, int t, int& s, int& at) {
+// The sequence of token t, and its place there; false if it is of none (before the first or behind the last).
+__device__ __forceinline__ bool sequence(const RotateArgs& a, int t, int& s, int& at) {
   int lo = 0, hi = a.seqs - 1;  // the last sequence that begins at t or before
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -39,12 +39,14 @@ __device__ __forceinline__ void sequence(const RotateArgs& a, int t, int& s, int
   }
   s = lo;
   at = t - a.cu[lo];
+  return at >= 0 && t < a.cu[lo + 1];
 }
 
-__device__ __forceinline__ long long position(const RotateArgs& a, int t) {
+__device__ __forceinline__ long long position(const RotateArgs& a, int t, bool& any) {
+  any = true;
   if (a.cu == nullptr) return a.at[t];
   int s, at;
-  sequence(a, t, s, at);
+  any = sequence(a, t, s, at);
   return (long long)a.at[s] + at;
 }
 
@@ -55,6 +57,7 @@ __global__ void __launch_bounds__(kRotateThreads, 3) dmc_rotate_kernel(const Rot
   using CK = Chunk<T>;
   constexpr int E = CK::N, ROW = D * (int)sizeof(T), P = ROW / 32;  // threads per row
   __shared__ __align__(16) float4 cs[kRotateTokens][D / 4];
+  __shared__ bool s_any[kRotateTokens];  // of a sequence
   if (a.prompt) griddep_launch_dependents();
   const int t0 = blockIdx.x * a.per, n = min(a.per, a.tokens - t0);
   const int p = threadIdx.x % P, all = a.heads[0] + a.heads[1];
@@ -89,7 +92,9 @@ __global__ void __launch_bounds__(kRotateThreads, 3) dmc_rotate_kernel(const Rot
     if (!ready) {  // the tokens' turns (and omegas), while the first rows are on their way
       for (int i = threadIdx.x; i < n * (D / 2); i += kRotateThreads) {
         const int pair = i % (D / 2), q = pair / 2, tt = i / (D / 2);
-        float2 c = turn_of(turns_of_pair(a.turns, pair), position(a, t0 + tt));
+        bool any;
+        float2 c = turn_of(turns_of_pair(a.turns, pair), position(a, t0 + tt, any));
+        if (pair == 0) s_any[tt] = any;
         if (a.back) c.y = -c.y;
         // (paired as neighbours, a thread's pairs are E / 4 twos of either half of the row)
         constexpr int C = E / 4;
@@ -110,7 +115,7 @@ __global__ void __launch_bounds__(kRotateThreads, 3) dmc_rotate_kernel(const Rot
           float g = 0.f;
           for (int x = 0; x < a.group; ++x) g += Elt<T>::to_f(*reinterpret_cast<const T*>(q0 + (size_t)x * ROW));
           int s, at;
-          sequence(a, t0 + tt, s, at);
+          if (!sequence(a, t0 + tt, s, at)) continue;
           a.weights[((size_t)prompt_chunk(t0 + tt - at, at / kPrefillChunk, s) * H + hk) * kPrefillChunk +
                     at % kPrefillChunk] = sigmoidf_(g / (float)a.group);
         }
@@ -118,7 +123,7 @@ __global__ void __launch_bounds__(kRotateThreads, 3) dmc_rotate_kernel(const Rot
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (to[u] == nullptr) continue;
+      if (to[u] == nullptr || (a.cu != nullptr && !s_any[token[u]])) continue;
       float x[E], y[E];
       CK::unpack(lo[u], x);
       CK::unpack(hi[u], y);

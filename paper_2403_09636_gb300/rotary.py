@@ -77,6 +77,8 @@ def rotate(rotary, q, k, positions, inverse=False, out=None, stream=None):
         raise ValueError("q must be float32 or bfloat16 [tokens, heads, head_dim]")
     T, hq, D = q.shape
     index = rotary.index
+    if torch._C._cuda_getDevice() != index:
+        raise ValueError(f"the rotation is for {rotary.turns.device}, which is not the current device")
     if (not isinstance(positions, torch.Tensor) or positions.dtype is not torch.int32 or positions.shape != (T,)
             or positions.get_device() != index or not positions.is_contiguous()):
         raise ValueError(f"positions must be contiguous int32 ({T},) on {rotary.turns.device}")
@@ -129,9 +131,14 @@ class _Apply(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dq, dk):
-        return None, *rotate(ctx.rotary, dq.contiguous(), dk.contiguous(), *ctx.saved_tensors, inverse=True), None
+        at, (_, needs_q, needs_k, _) = ctx.saved_tensors[0], ctx.needs_input_grad
+        if needs_q:
+            dq, dk = rotate(ctx.rotary, dq.contiguous(), dk.contiguous() if needs_k else None, at, inverse=True)
+        else:
+            dq, dk = None, rotate(ctx.rotary, dk.contiguous(), None, at, inverse=True)[0]
+        return None, dq, dk, None
 
 
 def apply(rotary, q, k, positions):
-    """(q', k') of `rotate`, differentiable (once) in q and k."""
+    """(q', k') of `rotate`, differentiable (once) in q and k; k may be None."""
     return _Apply.apply(rotary, q, k, positions)

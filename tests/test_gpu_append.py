@@ -122,6 +122,39 @@ def test_tokens_for_some_by_cu_seqlens(cuda_dev):
     near(qr.cpu(), want, 16 * 2.0 ** -24 * q.abs().max().double())
 
 
+@pytest.mark.parametrize("G", [1, 2])
+def test_rows_of_no_sequence_are_left_as_they_are(cuda_dev, G):
+    """cu_seqlens that end before the tokens do: queries behind the last sequence are not rotated, keys join nothing."""
+    hq, hkv, D, dt, T = 2 * G, 2, 128, BF16, 300
+    cache, plain = cache_of(3, hq, hkv, D, dt, T, prompt=T), Plain(3, hq, hkv, D, dt)
+    g = torch.Generator().manual_seed(9)
+    q, k, v = tokens(g, T, hq, hkv, D, dt, 0.5)
+    cu = torch.tensor([0, 100, 100, 260], dtype=torch.int32).cuda()
+    at = torch.tensor([5, 6, 7], dtype=torch.int32).cuda()
+    out = torch.full((T, hq, D), 3.0, dtype=dt).cuda()
+    freq = inv_freq(D)
+    cache.append(0, q.cuda(), k.cuda(), v.cuda(), at, R.Rotary(D, inv_freq=freq), cu_seqlens=cu, max_seqlen=160, q_out=out)
+    assert bool((out[260:] == 3.0).all()) and not bool((out[:260] == 3.0).all())
+    plain.append(0, q[:100], k[:100], v[:100], 5, freq)
+    plain.append(2, q[100:260], k[100:260], v[100:260], 7, freq)
+    compare(cache, 0, plain, T, 1, 4.0)
+    assert cache.status()[:2] == (0, 0)
+
+
+def test_sequences_that_contradict_one_another(cuda_dev):
+    """cu_seqlens that go back or begin late: the fault bit, and the caches of sequences that are whole."""
+    hq, hkv, D, dt, T = 2, 2, 128, BF16, 300
+    g = torch.Generator().manual_seed(10)
+    q, k, v = (t.cuda() for t in tokens(g, T, hq, hkv, D, dt, 0.5))
+    at = torch.zeros(3, dtype=torch.int32).cuda()
+    for cu in ([0, 200, 100, 300], [40, 90, 200, 300], [0, 100, 200, 301], [-9, 100, 200, 300]):
+        cache = cache_of(3, hq, hkv, D, dt, T, prompt=T)
+        cache.append(0, q, k, v, at, R.Rotary(D), cu_seqlens=torch.tensor(cu, dtype=torch.int32).cuda(), max_seqlen=200)
+        faulty = cu[2] < cu[1] or cu[0] < 0 or cu[3] > T
+        assert cache.status()[1] == (P.DMC_FAULT_BAD_SEQLENS if faulty else 0), cu
+        assert int(cache.lengths(0).max()) <= T
+
+
 @pytest.mark.parametrize("T", [1, 70])
 def test_in_place_queries_and_no_rotation(cuda_dev, T):
     hq, hkv, D, dt = 4, 4, 128, BF16
@@ -246,6 +279,29 @@ def test_refusals(cuda_dev):
     assert call(*p, None, 3, 1, at.data_ptr(), r.turns.data_ptr() + 4, 0, p[0]) == P.DMC_ERR_INVALID_ARG
     assert call(*p, None, 3, 0, None, None, 0, None) == P.DMC_ERR_INVALID_ARG
     assert c.status() == (0, 0, 0) and int(c.lengths(0).sum()) == 0
+
+
+def test_a_prompt_captured_and_replayed(cuda_dev):
+    hq, hkv, D, dt, T = 8, 2, 128, BF16, 500
+    g = torch.Generator().manual_seed(11)
+    x = [tokens(g, T, hq, hkv, D, dt, 0.4) for _ in range(3)]
+    q, k, v = (t.cuda() for t in x[0])
+    cu = torch.tensor([0, 13, T], dtype=torch.int32).cuda()
+    at = torch.tensor([0, 90], dtype=torch.int32).cuda()
+    r, a, b = R.Rotary(D), cache_of(2, hq, hkv, D, dt, 2 * T, prompt=T), cache_of(2, hq, hkv, D, dt, 2 * T, prompt=T)
+    out = torch.empty_like(q)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        a.append(0, q, k, v, at, r, cu_seqlens=cu, max_seqlen=T, q_out=out)
+    for y in x[1:]:
+        for to, t in zip((q, k, v), y):
+            to.copy_(t)
+        graph.replay()
+        want = b.append(0, *(t.cuda() for t in y), at, r, cu_seqlens=cu, max_seqlen=T)
+        assert torch.equal(out, want)
+    for s, t in zip(exported(a, 0, 2 * T), exported(b, 0, 2 * T)):
+        assert torch.equal(s, t)
 
 
 def test_captured_and_replayed(cuda_dev):

@@ -124,6 +124,22 @@ def test_gradient_of_one_output_alone(cuda_dev):
     assert bool(a.grad.any()) and not bool(b.grad.any())
 
 
+def test_gradients_of_what_needs_them(cuda_dev):
+    r = R.Rotary(64)
+    q, k, at = made(5, 2, 1, 64, F32, 6)
+    for which in ("q", "k", "q alone"):
+        a, b = q.cuda(), None if which == "q alone" else k.cuda()
+        leaf = b if which == "k" else a
+        leaf.requires_grad_()
+        y, z = R.apply(r, a, b, at.cuda())
+        assert (z is None) == (b is None)
+        out = z if which == "k" else y
+        out.sum().backward()
+        up = torch.ones(out.shape)
+        want = turned(up, at, inv_freq(64), False, True)
+        near(leaf.grad.cpu(), want, bound(up, want, F32))
+
+
 def test_nothing_to_do(cuda_dev):
     r = R.Rotary(64)
     q, k = R.rotate(r, torch.empty(0, 2, 64, device=cuda_dev), torch.empty(0, 1, 64, device=cuda_dev),
