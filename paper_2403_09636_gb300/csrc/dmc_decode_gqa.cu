@@ -883,12 +883,13 @@ cudaError_t gqa_setup(const Layout& L, DecodePlan* plan) {
   return cudaErrorInvalidValue;
 }
 
-// Warps of the grid per head from which heads are merged by a launch of their own. 8 query heads for each KV head of
-// 128, us per call with the last warp's merge / the launch, of 40, 500, 2000 and 16,000 slots: 8 heads 9.1 / 9.5, 15.7 /
-// 10.1, 22.6 / 13.7, 43.5 / 23.9; 32 heads 9.9 / 11.2, 16.2 / 13.9, 24.1 / 17.7, 56.5 / 51.8; 64 heads 10.0 / 13.3, 16.5 /
-// 15.8, 23.9 / 23.1, 89.3 / 89.3; 128 heads 10.6 / 16.4, 16.4 / 22.4, 33.8 / 38.9, 158 / 166. Lengths are not known on the
-// host.
-constexpr int kJoinFrom = 12;
+// Heads are merged by a launch of their own where each may be cut into four parts or more, and there are at most 64 of
+// them and 256 queries (what a cache can hold is known on the host, its lengths are not). us per call with the last
+// warp's merge / the launch, of 40, 300, 1000 and 4000 slots: 8 heads of 8 queries 9.4 / 9.5, 14.7 / 9.9, 16.7 / 12.3,
+// 26.5 / 17.0; 32 of 2 9.3 / 9.8, 16.9 / 12.1, 16.2 / 13.7, 26.2 / 20.6; 64 of 2 9.4 / 11.8, 17.6 / 13.5, 16.6 / 16.7,
+// 36.0 / 33.6; 64 of 8 9.8 / 13.3, 15.5 / 15.0, 18.0 / 18.6, 36.3 / 35.5; 96 of 4 9.7 / 13.0, 17.7 / 15.9, 18.6 / 19.9,
+// 44.2 / 44.5.
+constexpr int kJoinHeads = 64, kJoinQueries = 256, kJoinParts = 4;
 
 template <int D>
 static cudaError_t launch_gqa(const cudaLaunchConfig_t& cfg, const DecodePlan& plan, const GqaArgs& a) {
@@ -924,7 +925,8 @@ cudaError_t gqa_launch(const Layout& L, int layer0, int nlayers, const DecodePla
   a.q_ls = (long long)L.B * L.Hq * L.row_bytes;
   a.kv_ls = (long long)L.B * L.Hkv * L.row_bytes;
   a.overlap = pdl;
-  a.join = k == nullptr && plan.grid * kGWarps >= kJoinFrom * L.NH;
+  a.join = k == nullptr && L.NH <= kJoinHeads && L.NH * L.G <= kJoinQueries &&
+           plan.grid * kGWarps >= kJoinParts * L.NH;
   a.q = static_cast<const char*>(q);
   a.k = static_cast<const char*>(k);
   a.v = static_cast<const char*>(v);
