@@ -42,14 +42,6 @@ __device__ __forceinline__ bool sequence(const RotateArgs& a, int t, int& s, int
   return at >= 0 && t < a.cu[lo + 1];
 }
 
-__device__ __forceinline__ long long position(const RotateArgs& a, int t, bool& any) {
-  any = true;
-  if (a.cu == nullptr) return a.at[t];
-  int s, at;
-  any = sequence(a, t, s, at);
-  return (long long)a.at[s] + at;
-}
-
 // Turns of two pairs at a time, (cos, cos, sin, sin); thread p of a row needs places i * P + p (i = 0 .. E / 2 - 1: one
 // 128-byte line of shared memory for a row's threads at a time).
 template <typename T, int D>
@@ -57,7 +49,7 @@ __global__ void __launch_bounds__(kRotateThreads, 3) dmc_rotate_kernel(const Rot
   using CK = Chunk<T>;
   constexpr int E = CK::N, ROW = D * (int)sizeof(T), P = ROW / 32;  // threads per row
   __shared__ __align__(16) float4 cs[kRotateTokens][D / 4];
-  __shared__ bool s_any[kRotateTokens];  // of a sequence
+  __shared__ int s_seq[kRotateTokens], s_place[kRotateTokens];  // a token's sequence (-1: of none), and its place there
   if (a.prompt) griddep_launch_dependents();
   const int t0 = blockIdx.x * a.per, n = min(a.per, a.tokens - t0);
   const int p = threadIdx.x % P, all = a.heads[0] + a.heads[1];
@@ -92,9 +84,19 @@ __global__ void __launch_bounds__(kRotateThreads, 3) dmc_rotate_kernel(const Rot
     if (!ready) {  // the tokens' turns (and omegas), while the first rows are on their way
       for (int i = threadIdx.x; i < n * (D / 2); i += kRotateThreads) {
         const int pair = i % (D / 2), q = pair / 2, tt = i / (D / 2);
-        bool any;
-        float2 c = turn_of(turns_of_pair(a.turns, pair), position(a, t0 + tt, any));
-        if (pair == 0) s_any[tt] = any;
+        long long pos;
+        if (a.cu == nullptr) {
+          pos = a.at[t0 + tt];
+        } else {
+          int s, at;
+          const bool any = sequence(a, t0 + tt, s, at);
+          pos = (long long)a.at[s] + at;
+          if (pair == 0) {
+            s_seq[tt] = any ? s : -1;
+            s_place[tt] = at;
+          }
+        }
+        float2 c = turn_of(turns_of_pair(a.turns, pair), pos);
         if (a.back) c.y = -c.y;
         // (paired as neighbours, a thread's pairs are E / 4 twos of either half of the row)
         constexpr int C = E / 4;
@@ -110,12 +112,11 @@ __global__ void __launch_bounds__(kRotateThreads, 3) dmc_rotate_kernel(const Rot
         // only ever written as it is)
         const int H = a.heads[0] / a.group;
         for (int i = threadIdx.x; i < n * H; i += kRotateThreads) {
-          const int tt = i / H, hk = i % H;
+          const int tt = i / H, hk = i % H, s = s_seq[tt], at = s_place[tt];
+          if (s < 0) continue;
           const char* q0 = a.x[0] + (size_t)(t0 + tt) * a.x_stride[0] + (size_t)hk * a.group * ROW;
           float g = 0.f;
           for (int x = 0; x < a.group; ++x) g += Elt<T>::to_f(*reinterpret_cast<const T*>(q0 + (size_t)x * ROW));
-          int s, at;
-          if (!sequence(a, t0 + tt, s, at)) continue;
           a.weights[((size_t)prompt_chunk(t0 + tt - at, at / kPrefillChunk, s) * H + hk) * kPrefillChunk +
                     at % kPrefillChunk] = sigmoidf_(g / (float)a.group);
         }
@@ -123,7 +124,7 @@ __global__ void __launch_bounds__(kRotateThreads, 3) dmc_rotate_kernel(const Rot
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (to[u] == nullptr || (a.cu != nullptr && !s_any[token[u]])) continue;
+      if (to[u] == nullptr || (a.cu != nullptr && s_seq[token[u]] < 0)) continue;
       float x[E], y[E];
       CK::unpack(lo[u], x);
       CK::unpack(hi[u], y);
