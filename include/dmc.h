@@ -477,7 +477,7 @@ dmc_status dmc_retrofit_status(dmc_retrofit_t h, cudaStream_t stream, uint32_t* 
  * continuation, the end word, at its own score. A beam whose score, or whose log-sum, is not
  * a finite number offers its words at -infinity (so a search may begin with scores 0,
  * -inf, -inf, ...); single logits may be -infinity (masked words). Scores are compared
- * in 64 bits. The parents are what dmc_cache_reorder takes when keep = beams.
+ * in 48 bits. The parents are what dmc_cache_reorder takes when keep = beams.
  * The handle lays its scratch out in a caller's arena, as a cache does; calls on one
  * handle must be ordered on the GPU, allocate nothing and can be captured.
  * ------------------------------------------------------------------------ */

@@ -7,7 +7,7 @@
 // turned round, so that equal logits go to the lower word). Words are held to a bar that few more than `keep` of the
 // words so far reach: at first the keep-th largest of the lanes' maxima over the block's first 8192 words, then also the
 // least of the warps' ceil(keep / 8)-th best. The group's last block (a counter, no waiting) joins the pieces: sums and
-// lists of a row by a warp, then the rows' lists by score, in 64 bits; where sorted lists are joined, each entry looks up
+// lists of a row by a warp, then the rows' lists by score, in 48 bits; where sorted lists are joined, each entry looks up
 // how many are before it.
 //
 // Bound by HBM (each logit is read once) where there are many, by the chain load - list - join otherwise.
@@ -28,7 +28,9 @@ constexpr int kBeamThreads = kBeamWarps * 32;
 constexpr int kBeamMost = 32;             // beams of a group, and continuations kept: a lane each
 constexpr int kWords = 32;                // words of a lane at a time
 constexpr int kBlock = 32 * kWords;       // words of a warp at a time
-constexpr int kBeamBlocks = 304;          // pieces that rows are cut into, in all: two blocks per SM, as many as fit
+// Pieces that rows are cut into, in all: two blocks per SM, as many as fit. 256 rows of 130,003 fp32 words take 32.7 us
+// with one piece each, 38.6 with two, 50.6 with four.
+constexpr int kBeamBlocks = 304;
 constexpr unsigned kFull = 0xffffffffu;
 
 struct BeamArgs {
@@ -76,25 +78,43 @@ __device__ __forceinline__ K sorted(K key, int lane) {  // falling across the la
   return key;
 }
 
-// How many of n falling keys are before `key`: larger, or (of lower lists) its equal. n is at most 32; `most`: more than so
-// many need not be told from each other. A few keys are counted one by one, more are searched, several lists side by side:
-// 64 groups of 8 beams over 32,000 words (bf16), us with counting / searching: keep 8 30.3 / 31.4, 32 48.7 / 36.5; one of
-// 4 beams, keep 4, 10.2 / 11.2.
+// The place of a key that has `before` others before it in its own list, `own`, among N lists of `keep` falling keys: larger
+// ones are before it, and (kTies) its equals of lower lists. Places from keep on are not told from each other. A few keys
+// are counted one by one, more are searched in five steps, the lists side by side. us of 64 groups of 8 beams over 32,000
+// words (bf16) with counting / searching: keep 8 30.3 / 31.4, 32 48.7 / 36.0 (and 33.0 / 31.4 once the scores were no longer
+// fp64); of one of 4 beams, keep 4, 10.2 / 11.2.
 constexpr int kCountTo = 8;
-template <typename K>
-__device__ __forceinline__ int before_in(const K* list, int n, int most, K key, bool equals) {
-  int at = 0;
-  if (n <= kCountTo) {
-    while (at < n && at < most && (list[at] > key || (equals && list[at] == key))) ++at;
-    return at;
+template <int N, bool kTies, typename K>
+__device__ __forceinline__ int place_of(const K (*lists)[32], int n, int own, int before, int keep, K key) {
+  if (keep <= kCountTo) {
+    for (int v = 0; v < n && before < keep; ++v) {
+      if (v == own) continue;
+      const bool ties = kTies && v < own;
+      for (int j = 0; j < keep && (lists[v][j] > key || (ties && lists[v][j] == key)); ++j) ++before;
+    }
+    return before;
   }
 #pragma unroll
-  for (int step = 16; step > 0; step >>= 1) {
-    const int i = at + step - 1;
-    const K x = list[min(i, 31)];
-    if (i < n && (x > key || (equals && x == key))) at += step;
+  for (int v0 = 0; v0 < N; v0 += 8) {
+    if (v0 >= n) break;
+    int at[8] = {};
+#pragma unroll
+    for (int step = 16; step > 0; step >>= 1)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int v = min(v0 + u, n - 1), i = at[u] + step - 1;
+        const K x = lists[v][min(i, 31)];
+        if (i < keep && (x > key || (kTies && v < own && x == key))) at[u] += step;
+      }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {  // (31 of 32: the last one is still to be looked at)
+      const int v = v0 + u;
+      if (v >= n || v == own) continue;
+      const K x = lists[v][31];
+      before += at[u] + (at[u] == 31 && keep == 32 && (x > key || (kTies && v < own && x == key)) ? 1 : 0);
+    }
   }
-  return at + (at == 31 && n == 32 && (list[31] > key || (equals && list[31] == key)) ? 1 : 0);
+  return before;
 }
 
 // A warp's best keys, falling across its lanes, and the keep-th of them.
@@ -194,13 +214,41 @@ __device__ __forceinline__ float2 join_lanes(float2 x) {
   return x;
 }
 
-// A 64-bit number's bits in an order that compares as whole numbers do.
-__device__ __forceinline__ u64 ordered64(double x) {
-  const u64 u = (u64)__double_as_longlong(x);
-  return u >> 63 ? ~u : u | 1ull << 63;
+// Scores and log-sums as sums of two fp32 numbers, the second below half a step of the first: 48 bits. (In fp64 the log-sums
+// and scores of eight beams kept a block's warps waiting for an SM's one slow fp64 unit: 3 us of a call's 11.)
+struct Two {
+  float hi, lo;
+};
+__device__ __forceinline__ Two two_sum(float a, float b) {  // exactly a + b
+  const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+  return Two{s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
 }
-__device__ __forceinline__ double unordered64(u64 u) {
-  return __longlong_as_double((long long)(u >> 63 ? u & ~(1ull << 63) : ~u));
+__device__ __forceinline__ Two normal(Two x) {
+  const float s = __fadd_rn(x.hi, x.lo);
+  return Two{s, __fsub_rn(x.lo, __fsub_rn(s, x.hi))};
+}
+// m + log(s) of s in fp32's normal range: s = 2^e (1 + f), 1 + f within sqrt(2) of 1; log(1 + f) = 2 atanh(q), q = f / (2 + f)
+// with its rounding, as 2 q + 2 q (q^2 / 3 + q^4 / 5 + ...), |q| < 0.172: what the series leaves out is below 2^-32.
+__device__ __forceinline__ Two log_sum(float m, float s) {
+  const unsigned u = __float_as_uint(s);
+  int e = (int)(u >> 23) - 127;
+  float x = __uint_as_float((u & 0x7fffffu) | 0x3f800000u);
+  if (x > 1.41421356f) {
+    x *= 0.5f;
+    ++e;
+  }
+  const float f = x - 1.f, d = __fadd_rn(2.f, f), dl = __fsub_rn(f, __fsub_rn(d, 2.f));
+  const float q = __fdiv_rn(f, d), ql = __fdiv_rn(fmaf(-q, dl, fmaf(-q, d, f)), d), t = q * q;
+  const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.f / 11, 1.f / 9), 1.f / 7), 1.f / 5), 1.f / 3);
+  constexpr float kLn2 = 2839.f / 4096, kLn2Rest = 3.19461849453e-5f;  // log 2: twelve bits, which e does not round, and the rest
+  const Two a = two_sum((float)e * kLn2, 2.f * q), b = two_sum(m, a.hi);
+  const float rest = fmaf(2.f * q, p, fmaf((float)e, kLn2Rest, 2.f * ql));
+  // (not a number, infinite or zero: as log says)
+  return s > 0.f && s < INFINITY ? normal(Two{b.hi, __fadd_rn(b.lo, __fadd_rn(a.lo, rest))}) : Two{m + logf(s), 0.f};
+}
+__device__ __forceinline__ Two score_of(float base, float x, Two lse) {
+  const Two a = two_sum(base, x), b = two_sum(a.hi, -lse.hi);
+  return normal(Two{b.hi, __fadd_rn(b.lo, __fsub_rn(a.lo, lse.lo))});
 }
 
 template <typename T>
@@ -250,10 +298,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) dmc_beam_kernel(const BeamArg
         s_tops[warp][lane] = mine;
         __syncthreads();
         if (lane < keep) {  // (a lane's place among all, as for the lists below)
-          int before = lane;
-#pragma unroll
-          for (int v = 0; v < kBeamWarps; ++v)
-            if (v != warp && before < keep) before += before_in(s_tops[v], keep, keep - before, mine, v < warp);
+          const int before = place_of<kBeamWarps, true>(s_tops, kBeamWarps, warp, lane, keep, mine);
           if (before == keep - 1) s_bar = unordered(mine);
         }
       }
@@ -311,10 +356,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) dmc_beam_kernel(const BeamArg
     __syncthreads();
     const size_t at = (size_t)row * a.pieces + piece;
     if (lane < keep) {
-      int before = lane;  // in its own list
-#pragma unroll
-      for (int v = 0; v < kBeamWarps; ++v)
-        if (v != warp && before < keep) before += before_in(s_keys[v], keep, keep - before, key, false);
+      const int before = place_of<kBeamWarps, false>(s_keys, kBeamWarps, warp, lane, keep, key);
       if (before < keep) a.lists[at * keep + before] = key;
     }
     if (warp == 0) {
@@ -336,15 +378,15 @@ __global__ void __launch_bounds__(kBeamThreads, 2) dmc_beam_kernel(const BeamArg
   // the group's last block: a warp per beam joins its pieces and gives its words their scores
   for (int b = warp; b < a.beams; b += kBeamWarps) {
     const size_t r = (size_t)group * a.beams + b;
-    const double base = a.scores[r];
+    const float base = a.scores[r];
     const bool ended = a.finished != nullptr && a.finished[r];
     // a beam without a finite score (or without a finite log-sum) has nothing to offer: its words at -infinity
     int word = lane;
-    double score = -INFINITY;
+    Two score{-INFINITY, 0.f};
     if (ended) {
       if (isfinite(base)) {  // its end word, the others at -infinity
         word = lane == 0 ? a.eos : lane - 1 < a.eos ? lane - 1 : lane;
-        if (lane == 0) score = base;
+        if (lane == 0) score.hi = base;
       }
     } else {
       const u64* from = a.lists + r * a.pieces * keep;
@@ -353,19 +395,25 @@ __global__ void __launch_bounds__(kBeamThreads, 2) dmc_beam_kernel(const BeamArg
       u64 next = lane < n ? __ldcg(from + lane) : 0;
       float2 ms = make_float2(-INFINITY, 0.f);
       for (int i = lane; i < a.pieces; i += 32) ms = join(ms, __ldcg(a.sums + r * a.pieces + i));
-      for (int i = lane; i - lane < n; i += 32) {
-        const u64 x = next;
-        next = i + 32 < n ? __ldcg(from + i + 32) : 0;
-        list.take(x >> 32 ? x : 0, lane, keep);
+      if (a.pieces == 1) {
+        list.key = next >> 32 ? next : 0;  // in order as it is
+      } else {
+        for (int i = lane; i - lane < n; i += 32) {
+          const u64 x = next;
+          next = i + 32 < n ? __ldcg(from + i + 32) : 0;
+          list.take(x >> 32 ? x : 0, lane, keep);
+        }
       }
       ms = join_lanes(ms);
-      const double lse = (double)ms.x + log((double)ms.y);
-      if (isfinite(base) && isfinite(lse)) {
+      const Two lse = log_sum(ms.x, ms.y);
+      if (isfinite(base) && isfinite(lse.hi)) {
         word = list.key ? (int)~(unsigned)list.key : a.vocab;
-        score = base + ((double)unordered((unsigned)(list.key >> 32)) - lse);
+        const float x = unordered((unsigned)(list.key >> 32));
+        if (x != -INFINITY) score = score_of(base, x, lse);
       }
     }
-    s_keys[b][lane] = word < a.vocab ? ordered64(score) : 0;  // 0: no word
+    // 0: no word
+    s_keys[b][lane] = word < a.vocab ? (u64)ordered(score.hi) << 32 | ordered(score.lo) : 0;
     s_words[b][lane] = word;
   }
   __syncthreads();
@@ -379,11 +427,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) dmc_beam_kernel(const BeamArg
     place[i] = keep;
     if (b < a.beams && j < keep && s_keys[b][j] != 0) {
       const u64 key = s_keys[b][j];
-      int before = j;
-#pragma unroll 4
-      for (int v = 0; v < a.beams; ++v)
-        if (v != b && before < keep) before += before_in(s_keys[v], keep, keep - before, key, v < b);
-      place[i] = before;
+      place[i] = place_of<kBeamMost, true>(s_keys, a.beams, b, j, keep, key);
     }
   }
   bool ended[kMore];
@@ -398,7 +442,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) dmc_beam_kernel(const BeamArg
     if (place[i] >= keep) continue;
     const int c = tid + i * kBeamThreads, b = c / kBeamMost, j = c % kBeamMost, word = s_words[b][j];
     const size_t o = (size_t)group * keep + place[i];
-    a.out_scores[o] = (float)unordered64(s_keys[b][j]);
+    a.out_scores[o] = unordered((unsigned)(s_keys[b][j] >> 32));
     a.out_tokens[o] = word;
     a.out_parents[o] = group * a.beams + b;
     a.out_done[o] = ended[i] || word == a.eos;
