@@ -356,6 +356,7 @@ class DmcCache:
         self.num_q_heads, self.num_kv_heads, self.head_dim = int(num_q_heads), int(num_kv_heads), int(head_dim)
         self.queries = (int(batch), self.num_q_heads, self.head_dim)
         self._raw, self._empty_like, self._int32 = torch._C._cuda_getCurrentRawStream, torch.empty_like, torch.int32
+        self._streams = {self._s(stream)}  # that the arena's memory waits for when it is given up (_used_on)
 
     def _s(self, stream):
         if stream is None:
@@ -421,14 +422,22 @@ class DmcCache:
         what = f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
         raise ValueError(f"{name} must be contiguous {dtype} {tuple(shape)} on {self.device}, got {what}")
 
+    def _stream(self, raw):
+        # (an ExternalStream of the number 0 would be another one)
+        cuda = self.torch.cuda
+        return cuda.ExternalStream(raw, device=self.device) if raw else cuda.default_stream(self.device)
+
+    def _used_on(self, raw):
+        self.arena.record_stream(self._stream(raw))
+        self._streams.add(raw)
+
     def _new(self, like, stream):
         """A tensor as `like`, of memory that belongs to the call's stream."""
         torch = self.torch
         raw = self._s(stream)
         if raw == self._s(None):
             return torch.empty_like(like)
-        other = torch.cuda.ExternalStream(raw, device=self.device) if raw else torch.cuda.default_stream(self.device)
-        with torch.cuda.stream(other):
+        with torch.cuda.stream(self._stream(raw)):
             return torch.empty_like(like)
 
     def _append_is_wrong(self, q, k, v, positions, rotary, cu_seqlens, n, q_out):
@@ -483,11 +492,15 @@ class DmcCache:
         if not fits:
             self._append_is_wrong(q, k, v, positions, rotary, cu_seqlens, n, q_out)
         raw = self._raw(index) if stream is None else self._s(stream)
+        if raw not in self._streams:
+            self._used_on(raw)
         at = turns = to = None
         pairs = 0
         if rotary is not None:
             if q_out is None:
                 q_out = self._empty_like(q) if stream is None else self._new(q, stream)
+            if raw not in rotary.streams:
+                rotary.used_on(raw)
             at, turns, pairs, to = positions.data_ptr(), rotary.pointer, rotary.pairs, q_out.data_ptr()
         st = self.lib.dmc_cache_append(self.handle, layer, first_seq, n, q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                        None if cu_seqlens is None else cu_seqlens.data_ptr(), T,
@@ -508,7 +521,10 @@ class DmcCache:
             to = out.data_ptr()
         else:
             to = self._is("out", out, self.queries, self.dtype)
-        st = self.lib.dmc_cache_attend(self.handle, layer, p, to, self._raw(self.index) if stream is None else self._s(stream))
+        raw = self._raw(self.index) if stream is None else self._s(stream)
+        if raw not in self._streams:
+            self._used_on(raw)
+        st = self.lib.dmc_cache_attend(self.handle, layer, p, to, raw)
         if st:
             _check(st, "dmc_cache_attend")
         return out
@@ -519,7 +535,10 @@ class DmcCache:
         if not isinstance(parents, self.torch.Tensor) or parents.dim() < 1:
             raise ValueError("parents must be int32, one for each sequence")
         p = self._is("parents", parents, parents.shape, self.torch.int32)
-        st = self.lib.dmc_cache_reorder(self.handle, first_seq, parents.numel(), p, self._s(stream))
+        raw = self._s(stream)
+        if raw not in self._streams:
+            self._used_on(raw)
+        st = self.lib.dmc_cache_reorder(self.handle, first_seq, parents.numel(), p, raw)
         if st:
             _check(st, "dmc_cache_reorder")
 

@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) dmc_beam_kernel(const BeamArg
     for (int u = 0; u < kRing - 1; ++u) issue(first + (u * kBeamWarps + warp) * kBlock, u);
     int slot = 0;
     List list{0, 0};
-    float m = -INFINITY, sum = 0.f, bar = -INFINITY;
+    float m = -INFINITY, sum = 0.f, rest = 0.f, bar = -INFINITY;  // rest: what rounding kept from the sum
     bool fresh = true;
     const int share = (keep + kBeamWarps - 1) / kBeamWarps;
     if (lane == 0) s_few[warp] = 0;
@@ -303,7 +303,9 @@ __global__ void __launch_bounds__(kBeamThreads, 2) dmc_beam_kernel(const BeamArg
         }
       }
       const float mn = fmaxf(m, top), r = mn == -INFINITY ? 0.f : mn;
-      sum *= pow2((m - r) * kLog2e);
+      const float scale = pow2((m - r) * kLog2e);
+      sum *= scale;
+      rest *= scale;
       float2 s0 = make_float2(0.f, 0.f), s1 = s0, s2 = s0, s3 = s0;
       const float2 r2 = make_float2(-r, -r), l2 = make_float2(kLog2e, kLog2e);
 #pragma unroll
@@ -318,7 +320,11 @@ __global__ void __launch_bounds__(kBeamThreads, 2) dmc_beam_kernel(const BeamArg
         s3 = add2(s3, make_float2(pow2(h.x), pow2(h.y)));
       }
       s0 = add2(add2(s0, s1), add2(s2, s3));
-      sum += s0.x + s0.y;
+      // (added as they are, the words of a long row far below its largest would be lost one block after another: 4 M words
+      // 22 below it took 4e-6 off the log-sum)
+      const Two t = two_sum(sum, s0.x + s0.y);
+      sum = t.hi;
+      rest += t.lo;
       m = mn;
       if (fresh) {
         __syncthreads();
@@ -348,7 +354,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) dmc_beam_kernel(const BeamArg
       if (lane == share - 1) s_few[warp] = (unsigned)(list.key >> 32);
     }
     cp_async_wait<0>();
-    const float2 ms = join_lanes(make_float2(m, sum));
+    const float2 ms = join_lanes(make_float2(m, sum + rest));
     // (an empty place's key is below every word's, and its own)
     u64 key = list.key ? list.key : (u64)tid + 1;
     s_keys[warp][lane] = key;

@@ -49,6 +49,14 @@ class Rotary:
         self.turns = torch.tensor([_turns(x) for x in values], dtype=torch.int64,
                                   device=device if device is not None else "cuda")
         self.index, self.pointer, self.pairs = self.turns.get_device(), self.turns.data_ptr(), int(self.interleaved)
+        # that the turns' memory waits for when it is given up
+        self.streams = {torch._C._cuda_getCurrentRawStream(self.index)} if self.index >= 0 else set()
+
+    def used_on(self, raw):
+        """Notes that the stream of this number reads the turns."""
+        dev = self.turns.device
+        self.turns.record_stream(torch.cuda.ExternalStream(raw, device=dev) if raw else torch.cuda.default_stream(dev))
+        self.streams.add(raw)
 
 
 def _stride(rotary, name, x, tokens, dtype):
@@ -105,6 +113,8 @@ def rotate(rotary, q, k, positions, inverse=False, out=None, stream=None):
         if out[0].shape[1] != hq or (k is not None and out[1].shape[1] != hk):
             raise ValueError("out must have the shapes of q and k")
     qo, ko = out
+    if number not in rotary.streams:
+        rotary.used_on(number)
     st = lib().dmc_rotate(_CODES[dt], D, T, positions.data_ptr(), rotary.pointer, rotary.pairs, 1 if inverse else 0, hq,
                           q.data_ptr(), qs, qo.data_ptr(), qos, hk, None if k is None else k.data_ptr(), ks,
                           None if k is None else ko.data_ptr(), kos, number)

@@ -100,9 +100,10 @@ def test_finished_beams(cuda_dev, dt):
     scores[2, 0], finished[2, 0] = -math.inf, True
     scores[3, 1], finished[3, 1] = math.nan, True
     logits[~finished.view(-1).cuda(), eos] += 9.0  # some end now
+    logits[finished.view(-1).cuda()] = math.nan  # not read
     for keep in (4, 9, 32):
         check(BeamSelect(G, B, V, keep=keep, dtype=dt), logits, scores, finished, eos)
-    check(BeamSelect(G, B, V, keep=5, dtype=dt), logits, scores.nan_to_num(0.0, 0.0, -1.0), None, eos)  # none finished yet
+    check(BeamSelect(G, B, V, keep=5, dtype=dt), logits.nan_to_num(0.0), scores.nan_to_num(0.0, 0.0, -1.0), None, eos)
     for end in (0, V - 1):
         check(BeamSelect(G, B, V, keep=6, dtype=dt), logits, scores, torch.ones(G, B, dtype=torch.bool), end)
 
