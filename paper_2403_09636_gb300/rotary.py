@@ -143,10 +143,16 @@ class _Apply(torch.autograd.Function):
     def backward(ctx, dq, dk):
         at, (_, needs_q, needs_k, _) = ctx.saved_tensors[0], ctx.needs_input_grad
         if needs_q:
-            dq, dk = rotate(ctx.rotary, dq.contiguous(), dk.contiguous() if needs_k else None, at, inverse=True)
+            dq, dk = rotate(ctx.rotary, _dense(dq), _dense(dk) if needs_k else None, at, inverse=True)
         else:
-            dq, dk = None, rotate(ctx.rotary, dk.contiguous(), None, at, inverse=True)[0]
+            dq, dk = None, rotate(ctx.rotary, _dense(dk), None, at, inverse=True)[0]
         return None, dq, dk, None
+
+
+def _dense(g):
+    # (a gradient can be a piece of another one that begins anywhere)
+    g = g.contiguous()
+    return g if g.data_ptr() % 16 == 0 else g.clone()
 
 
 def apply(rotary, q, k, positions):

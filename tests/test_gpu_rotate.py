@@ -140,6 +140,22 @@ def test_gradients_of_what_needs_them(cuda_dev):
         near(leaf.grad.cpu(), want, bound(up, want, F32))
 
 
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_gradients_that_begin_anywhere(cuda_dev, dt):
+    """What follows the rotation may hand back a piece of a longer gradient, one element off its start, or one that is
+    laid out in another order."""
+    r = R.Rotary(64)
+    q, k, at = made(5, 2, 2, 64, dt, 7)
+    a, b = q.cuda().requires_grad_(), k.cuda().requires_grad_()
+    y, z = R.apply(r, a, b, at.cuda())
+    up = torch.randn(2, 641, generator=torch.Generator().manual_seed(8)).to(dt)
+    x = torch.cat((torch.zeros(1, dtype=dt, device=cuda_dev), y.reshape(-1)))
+    ((x * up[0].cuda()).sum() + (z.transpose(0, 1) * up[1, 1:].view(2, 5, 64).cuda()).sum()).backward()
+    for got, g in ((a.grad, up[0, 1:].view(5, 2, 64)), (b.grad, up[1, 1:].view(2, 5, 64).transpose(0, 1))):
+        want = turned(g, at, inv_freq(64), False, True)
+        near(got.cpu(), want, bound(g, want, dt))
+
+
 def test_nothing_to_do(cuda_dev):
     r = R.Rotary(64)
     q, k = R.rotate(r, torch.empty(0, 2, 64, device=cuda_dev), torch.empty(0, 1, 64, device=cuda_dev),
