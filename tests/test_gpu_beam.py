@@ -124,6 +124,17 @@ def test_masked_words_and_rows_that_offer_nothing(cuda_dev, dt):
         check(BeamSelect(G, B, V, keep=keep, dtype=dt), logits, scores)
 
 
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("B,V,keep", [(1, 5, 5), (1, 700, 4), (2, 9000, 32), (4, 33000, 4)])
+def test_rows_of_values_that_are_not_numbers(cuda_dev, dt, B, V, keep):
+    """Every place of the results is written, also where no logit is a number: words in their order, at -infinity."""
+    logits, scores, _ = made(3, B, V, dt, 6)
+    logits[:B] = math.nan          # a group of nothing else
+    logits[B, V // 2 + 1:] = math.nan
+    logits[2 * B, 2:] = math.nan   # fewer numbers than continuations
+    check(BeamSelect(3, B, V, keep=keep, dtype=dt), logits, scores)
+
+
 def test_scores_that_are_not_finite(cuda_dev):
     logits, scores, _ = made(2, 3, 100, F32, 3)
     scores[0, 0], scores[0, 1], scores[1, 2] = math.nan, math.inf, -math.inf
