@@ -411,7 +411,8 @@ __global__ void __launch_bounds__(kBeamThreads, 2) dmc_beam_kernel(const BeamArg
         }
       }
       ms = join_lanes(ms);
-      const Two lse = log_sum(ms.x, ms.y);
+      // (one lane's: where products are contracted with sums, the two lanes of a pair round different ones)
+      const Two lse = log_sum(__shfl_sync(kFull, ms.x, 0), __shfl_sync(kFull, ms.y, 0));
       if (isfinite(base) && isfinite(lse.hi)) {
         word = list.key ? (int)~(unsigned)list.key : a.vocab;
         const float x = unordered((unsigned)(list.key >> 32));
