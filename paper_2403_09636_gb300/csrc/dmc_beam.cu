@@ -419,8 +419,15 @@ __global__ void __launch_bounds__(kBeamThreads, 2) dmc_beam_kernel(const BeamArg
         if (x != -INFINITY) score = score_of(base, x, lse);
       }
     }
-    // 0: no word
-    s_keys[b][lane] = word < a.vocab ? (u64)ordered(score.hi) << 32 | ordered(score.lo) : 0;
+    // 0: no word. Rounded to 48 bits, the score of a higher logit can come out a step below a lower one's (a beam at minus
+    // its log-sum, logits around half a step of it): no score is above one before it, so that the list is in order.
+    u64 key = word < a.vocab ? (u64)ordered(score.hi) << 32 | ordered(score.lo) : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 up = __shfl_up_sync(kFull, key, o);
+      if (lane >= o) key = min(key, up);
+    }
+    s_keys[b][lane] = key;
     s_words[b][lane] = word;
   }
   __syncthreads();

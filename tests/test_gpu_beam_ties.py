@@ -23,3 +23,24 @@ def test_beams_that_are_alike_in_rows_of_several_pieces(cuda_dev, dt, B, V, keep
         row[torch.randperm(V, generator=g)[:5]] = row.max() * 1.0625
         logits = row.to(dt).expand(B, V).contiguous().cuda()
         check(select, logits, torch.full((1, B), -3.0 - 0.37 * seed))
+
+
+def test_logits_whose_scores_round_to_a_step_apart(cuda_dev):
+    """A beam at minus its log-sum and two logits next to each other around -2^-22, half a step of its sum with them:
+    rounded to 48 bits, some 4 % of the rows gave the lower one the higher score. With two such beams each, alike: every
+    continuation is there once, in an order of scores, and a beam's in the order of its logits."""
+    G, V = 4000, 64
+    g = torch.Generator().manual_seed(0)
+    row = -1e-3 - 0.1 * torch.rand(G, V, generator=g)
+    low = torch.tensor(-2.0 ** -22)
+    row[:, 9], row[:, 40] = low, torch.nextafter(low, torch.tensor(1.0))
+    base = -torch.logsumexp(row.double(), 1).float()
+    logits = row.repeat_interleave(2, 0).cuda()
+    scores, tokens, parents, done = (t.cpu() for t in BeamSelect(G, 2, V, keep=4, dtype=F32).select(
+        logits, base[:, None].expand(G, 2).contiguous().cuda()))
+    where = (parents - 2 * torch.arange(G)[:, None]) * 2 + (tokens == 9)
+    assert bool(((tokens == 9) | (tokens == 40)).all()) and not bool(done.any())
+    assert torch.equal(where.sort(1)[0], torch.arange(4).expand(G, 4).to(where.dtype))
+    assert bool((scores[:, 1:] <= scores[:, :-1]).all())
+    place = where.argsort(1)  # of (beam 0, 40), (beam 0, 9), (beam 1, 40), (beam 1, 9)
+    assert bool((place[:, 0] < place[:, 1]).all()) and bool((place[:, 2] < place[:, 3]).all())
