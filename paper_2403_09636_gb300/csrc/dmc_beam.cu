@@ -50,9 +50,10 @@ struct BeamArgs {
   unsigned char* out_done;
 };
 
-// A logit's bits in an order that compares as whole numbers do; one that is not a number counts as -infinity.
+// A logit's bits in an order that compares as whole numbers do; one that is not a number counts as -infinity, and the
+// zeros of both signs are one number.
 __device__ __forceinline__ unsigned ordered(float x) {
-  const unsigned u = __float_as_uint(x == x ? x : -INFINITY);
+  const unsigned u = __float_as_uint(x == x ? __fadd_rn(x, 0.f) : -INFINITY);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float unordered(unsigned u) {

@@ -44,3 +44,23 @@ def test_logits_whose_scores_round_to_a_step_apart(cuda_dev):
     assert bool((scores[:, 1:] <= scores[:, :-1]).all())
     place = where.argsort(1)  # of (beam 0, 40), (beam 0, 9), (beam 1, 40), (beam 1, 9)
     assert bool((place[:, 0] < place[:, 1]).all()) and bool((place[:, 2] < place[:, 3]).all())
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("B,V,keep", [(1, 40, 8), (2, 5001, 5), (3, 40000, 32)])
+def test_zeros_of_both_signs_are_equal(cuda_dev, dt, B, V, keep):
+    """Logits multiplied by a mask hold zeros of both signs, and so do scores: the lower word goes first, then the lower
+    beam."""
+    select = BeamSelect(2, B, V, keep=keep, dtype=dt)
+    for seed in range(6):
+        g = torch.Generator().manual_seed(seed)
+        logits = -torch.randn(2 * B, V, generator=g).abs() * (torch.rand(2 * B, V, generator=g) < 0.7)
+        logits[torch.rand(2 * B, V, generator=g) < 0.1] = 0.0  # beside those of -0.0
+        assert bool((torch.signbit(logits) & (logits == 0)).any()) and bool((~torch.signbit(logits) & (logits == 0)).any())
+        check(select, logits.to(dt).cuda(), torch.full((2, B), -1.0))
+
+
+def test_finished_beams_whose_scores_are_zeros_of_both_signs(cuda_dev):
+    for order in ([-0.0, 0.0, -0.0, 0.0], [0.0, -0.0, 0.0, -0.0]):
+        select = BeamSelect(1, 4, 50, dtype=F32)
+        check(select, torch.zeros(4, 50).cuda(), torch.tensor([order]), torch.ones(1, 4, dtype=torch.bool), 7)
