@@ -356,7 +356,7 @@ class DmcCache:
         self.num_q_heads, self.num_kv_heads, self.head_dim = int(num_q_heads), int(num_kv_heads), int(head_dim)
         self.queries = (int(batch), self.num_q_heads, self.head_dim)
         self._raw, self._empty_like, self._int32 = torch._C._cuda_getCurrentRawStream, torch.empty_like, torch.int32
-        self._export_shape = None
+        self._export = None
         self._streams = {self._s(stream)}  # that the arena's memory waits for when it is given up (_used_on)
 
     def _s(self, stream):
@@ -556,11 +556,13 @@ class DmcCache:
         if not (isinstance(ids, t.Tensor) and ids.dtype is t.int32 and ids.get_device() == self.index and ids.is_contiguous()):
             ids = t.as_tensor(head_ids, dtype=t.int32, device=self.device)
         n = ids.numel()
-        if self._export_shape != (n, cap):
-            self._export_like = [t.empty(1, dtype=d, device=self.device).expand(shape) for d, shape in (
-                (self.dtype, (n, cap, self.head_dim)), (t.float32, (n, cap)), (t.int32, (n,)))]
-            self._export_shape = n, cap
-        rows, sums, counts = self._export_like  # (an element each: the host makes a tensor like another sooner than anew)
+        # (an element each: the host makes a tensor like another sooner than anew. Shapes and tensors are one attribute, read
+        # once: another thread may export other shapes meanwhile)
+        kept = self._export
+        if kept is None or kept[0] != (n, cap):
+            kept = self._export = (n, cap), *(t.empty(1, dtype=d, device=self.device).expand(shape) for d, shape in (
+                (self.dtype, (n, cap, self.head_dim)), (t.float32, (n, cap)), (t.int32, (n,))))
+        _, rows, sums, counts = kept
         new = self._empty_like
         k, v, z, ln = new(rows), new(rows), new(sums), new(counts)  # padded: every row is written
         st = self.lib.dmc_cache_export_heads_padded(self.handle, layer, n, ids.data_ptr(), cap, k.data_ptr(), v.data_ptr(),
