@@ -554,7 +554,7 @@ class DmcCache:
         t = self.torch
         ids = head_ids
         if not (isinstance(ids, t.Tensor) and ids.dtype is t.int32 and ids.get_device() == self.index and ids.is_contiguous()):
-            ids = t.as_tensor(head_ids, dtype=t.int32, device=self.device)
+            ids = t.as_tensor(head_ids, dtype=t.int32, device=self.device).contiguous()
         n = ids.numel()
         # (an element each: the host makes a tensor like another sooner than anew. Shapes and tensors are one attribute, read
         # once: another thread may export other shapes meanwhile)

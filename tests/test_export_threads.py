@@ -1,4 +1,5 @@
 """Exports of one cache by two host threads (CPU; the call of the library is replaced)."""
+import ctypes
 import sys
 import threading
 
@@ -57,3 +58,19 @@ def test_results_are_dense_and_of_the_call(cache):
         assert (k.shape, z.shape, ln.shape) == ((n, cap, 64), (n, cap), (n,)) and v.shape == k.shape
         assert all(t.is_contiguous() for t in (k, v, z, ln))
         assert (k.dtype, v.dtype, z.dtype, ln.dtype) == (torch.bfloat16, torch.bfloat16, torch.float32, torch.int32)
+
+
+def test_heads_named_by_every_other_element(cache):
+    """Ids of a tensor with a stride are those of its elements, not of its memory."""
+    seen = []
+
+    class Reads(Library):
+        @staticmethod
+        def dmc_cache_export_heads_padded(handle, layer, n, ids, *rest):
+            seen.append(list((ctypes.c_int32 * n).from_address(ids)))
+            return P.DMC_OK
+
+    cache.lib = Reads
+    for ids in (torch.arange(12, dtype=torch.int32)[::2], torch.arange(12)[1::3], [7, 1]):
+        cache.export_heads(0, ids, 4, stream=0)
+    assert seen == [[0, 2, 4, 6, 8, 10], [1, 4, 7, 10], [7, 1]]
