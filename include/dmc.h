@@ -27,6 +27,8 @@
  *    capacity, a NaN gate, inconsistent cu_seqlens, a wait that timed out) set
  *    sticky bits that dmc_cache_status reports; the kernels skip the faulty
  *    write and never trap. Results after a fault are unspecified.
+ *    A request for pages that the pool cannot serve takes none; later requests may
+ *    fail until dmc_cache_reorder or dmc_cache_reset has brought pages back.
  *  - Inputs are const: the library never writes q[0] or k[0] of caller buffers.
  */
 #ifndef DMC_H_
@@ -306,8 +308,8 @@ dmc_status dmc_cache_export_heads_padded(dmc_cache_t cache, int32_t layer, int32
                                          cudaStream_t stream);
 
 /* Synchronizes `stream`, then reads the sticky fault bits (into *bits if not
- * NULL) and the number of pool pages handed out so far (into *pages_used if
- * not NULL). Returns DMC_OK, DMC_ERR_PAGES_EXHAUSTED or DMC_ERR_DEVICE_FAULT. */
+ * NULL) and the number of pages that heads hold, one that several share once
+ * (into *pages_used if not NULL). Returns DMC_OK, DMC_ERR_PAGES_EXHAUSTED or DMC_ERR_DEVICE_FAULT. */
 dmc_status dmc_cache_status(dmc_cache_t cache, cudaStream_t stream, uint32_t* bits,
                             int64_t* pages_used);
 

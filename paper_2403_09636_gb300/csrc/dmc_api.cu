@@ -533,13 +533,13 @@ dmc_status dmc_cache_status(dmc_cache_t c, cudaStream_t stream, uint32_t* bits,
                             int64_t* pages_used) {
   if (!c) return DMC_ERR_INVALID_ARG;
   uint32_t b = 0;
-  unsigned long long top[2] = {0, 0};  // taken, given back
+  unsigned long long top[4] = {0, 0, 0, 0};  // Layout::pool_top
   cudaError_t e = cudaStreamSynchronize(stream);
   if (e == cudaSuccess) e = cudaMemcpy(&b, c->lay.error, 4, cudaMemcpyDeviceToHost);
   if (e == cudaSuccess) e = cudaMemcpy(top, c->lay.pool_top, sizeof(top), cudaMemcpyDeviceToHost);
   if (e != cudaSuccess) return DMC_ERR_CUDA;
   if (bits) *bits = b;
-  if (pages_used) *pages_used = (int64_t)(top[0] - top[1]);
+  if (pages_used) *pages_used = (int64_t)(dmc::places_taken(top, c->lay.num_pages) - top[1]);
   if (b & DMC_FAULT_PAGES_EXHAUSTED) return DMC_ERR_PAGES_EXHAUSTED;
   if (b) return DMC_ERR_DEVICE_FAULT;
   return DMC_OK;

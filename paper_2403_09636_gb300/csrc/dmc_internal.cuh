@@ -40,7 +40,8 @@ struct Layout {
   char* pending;           // [L][NH][2][D]: grouped queries: new last rows awaiting the layer's end
   int* pending_at;         // [L][NH]: their slot (page * 32 + row), -1 = none
   float* pending_z;        // [L][NH]: their z
-  unsigned long long* pool_top;  // [4]: pages taken, pages given back, of those by the running launch too, its blocks done
+  unsigned long long* pool_top;  // [4]: places of the pool asked for, pages given back, of those by the running launch too,
+                           // places before the pool's end that a request which wanted more has passed over (places_taken)
   int2* page_use;          // [num_pages]: x: heads that hold the page beside the first (reordered sequences share what
                            // they have in common), set when the page is taken; y: the given back page of that turn
                            // (page_in_turn). Neither has to be cleared when the cache is emptied.
@@ -160,20 +161,30 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
 __device__ __forceinline__ int page_in_turn(const Layout& L, unsigned long long at) {
   return at < (unsigned long long)L.num_pages ? (int)at : L.page_use[at % (unsigned long long)L.num_pages].y;
 }
-// Whether the places [at, at + n) exist yet. (What a launch gives back can be taken by later ones.)
-__device__ __forceinline__ bool pages_in_pool(const Layout& L, unsigned long long at, unsigned long long n) {
-  return at + n <= (unsigned long long)L.num_pages || at + n <= (unsigned long long)L.num_pages + L.pool_top[1];
+// n pages for a head, in a row of places from `first` on (what a launch gives back can be taken by later ones); or false,
+// with the fault bit set. The places of a request that fails stay asked for, so that later ones fail as well, until the
+// next reordering puts the count right (places_taken). At most one request reaches over the pool's end until then.
+__device__ __forceinline__ bool take_places(const Layout& L, unsigned long long n, unsigned long long& first) {
+  first = atomicAdd(L.pool_top, n);
+  if (first + n <= (unsigned long long)L.num_pages) return true;
+  const unsigned long long end = (unsigned long long)L.num_pages + L.pool_top[1];
+  if (first + n <= end) return true;
+  if (first < end) L.pool_top[3] = end - first;
+  atomicOr(L.error, DMC_FAULT_PAGES_EXHAUSTED);
+  return false;
+}
+// How many places have been taken, of what pool_top holds.
+__host__ __device__ inline unsigned long long places_taken(const unsigned long long* pool_top, int64_t num_pages) {
+  const unsigned long long end = (unsigned long long)num_pages + pool_top[1];
+  return pool_top[0] > end ? end - pool_top[3] : pool_top[0];
 }
 // One page for a head, or -1 with the fault bit set.
 __device__ __forceinline__ int take_page(const Layout& L) {
-  const unsigned long long at = atomicAdd(L.pool_top, 1ull);
-  if (pages_in_pool(L, at, 1)) {
-    const int page = page_in_turn(L, at);
-    L.page_use[page].x = 0;
-    return page;
-  }
-  atomicOr(L.error, DMC_FAULT_PAGES_EXHAUSTED);
-  return -1;
+  unsigned long long at;
+  if (!take_places(L, 1, at)) return -1;
+  const int page = page_in_turn(L, at);
+  L.page_use[page].x = 0;
+  return page;
 }
 
 __device__ __forceinline__ float sigmoidf_(float x) { return 1.0f / (1.0f + __expf(-x)); }

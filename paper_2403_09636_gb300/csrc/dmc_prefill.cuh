@@ -259,12 +259,9 @@ __global__ void __launch_bounds__(kPlanThreads) dmc_prefill_plan_kernel(const Pr
       atomicOr(L.error, DMC_FAULT_SLOT_CAPACITY);
       fail = 1;
     } else if (need > 0) {
-      const unsigned long long first = atomicAdd(L.pool_top, (unsigned long long)need);
+      unsigned long long first;
+      if (!take_places(L, (unsigned long long)need, first)) fail = 1;
       s_first = first;
-      if (!pages_in_pool(L, first, (unsigned long long)need)) {
-        atomicOr(L.error, DMC_FAULT_PAGES_EXHAUSTED);
-        fail = 1;
-      }
     }
     if (s_nan) atomicOr(L.error, DMC_FAULT_NAN_GATE);
     s_fail = fail;

@@ -214,13 +214,17 @@ __global__ void __launch_bounds__(kReorderThreads) dmc_reorder_kernel(const Reor
 }
 
 // Copies rows [0, rows) of K and V and their z from page to page; what the launch before gave back can be taken from
-// here on.
+// here on, and places that failed requests have asked for are there again.
 constexpr int kCopyThreads = 256;
 __global__ void __launch_bounds__(kCopyThreads) dmc_reorder_copy_kernel(const ReorderArgs a) {
   const Layout& L = a.lay;
   const int tid = threadIdx.x, h = blockIdx.y, layer = blockIdx.z;
   griddep_wait();
-  if (tid == 0 && (blockIdx.x | blockIdx.y | blockIdx.z) == 0) L.pool_top[1] = L.pool_top[2];
+  if (tid == 0 && (blockIdx.x | blockIdx.y | blockIdx.z) == 0) {  // (nothing else takes pages now)
+    L.pool_top[0] = places_taken(L.pool_top, L.num_pages);
+    L.pool_top[3] = 0;
+    L.pool_top[1] = L.pool_top[2];
+  }
   const int count = copy_counts(L, layer)[h], half = kPage * L.row_bytes;
   for (int i = blockIdx.x; i < count; i += gridDim.x) {
     const int4 c = copies(L, layer, h, a.n)[i];
