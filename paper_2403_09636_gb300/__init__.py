@@ -330,7 +330,8 @@ def _check(st: int, what: str):
 
 class DmcCache:
     """A cache living in a torch-allocated device arena. Tensors passed to the
-    methods must be contiguous, on the cache's device, in the cache dtype."""
+    methods must be contiguous, on the cache's device, in the cache dtype. The arena is memory of the constructor's
+    stream, and waits for every stream that a method used when the cache is dropped: streams must outlive it."""
 
     def __init__(self, num_layers, batch, num_q_heads, num_kv_heads, head_dim, dtype,
                  max_slots_per_head, num_pages, max_prefill_tokens=0, device=None, stream=None,
@@ -348,16 +349,16 @@ class DmcCache:
         self.nbytes = dmc_cache_required_bytes(self.cfg)
         if self.nbytes == 0:
             raise DmcError(DMC_ERR_INVALID_ARG, "dmc_cache_required_bytes")
-        self.arena = torch.empty(self.nbytes, dtype=torch.uint8, device=self.device)
-        st, self.handle = dmc_cache_create(self.cfg, self.arena.data_ptr(), self.nbytes,
-                                           self._s(stream))
+        raw = self._s(stream)
+        self.arena = self._on(raw, lambda: torch.empty(self.nbytes, dtype=torch.uint8, device=self.device))
+        self._streams = {raw}  # that the arena's memory waits for when it is given up (_used_on)
+        st, self.handle = dmc_cache_create(self.cfg, self.arena.data_ptr(), self.nbytes, raw)
         _check(st, "dmc_cache_create")
         self.lib = lib()
         self.num_q_heads, self.num_kv_heads, self.head_dim = int(num_q_heads), int(num_kv_heads), int(head_dim)
         self.queries = (int(batch), self.num_q_heads, self.head_dim)
         self._raw, self._empty_like, self._int32 = torch._C._cuda_getCurrentRawStream, torch.empty_like, torch.int32
         self._export = None
-        self._streams = {self._s(stream)}  # that the arena's memory waits for when it is given up (_used_on)
 
     def _s(self, stream):
         if stream is None:
@@ -367,6 +368,29 @@ class DmcCache:
             index = self.device.index
             return c._cuda_getCurrentRawStream(c._cuda_getDevice() if index is None else index)
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+    def _stream(self, raw):
+        # (an ExternalStream of the number 0 would be another one)
+        cuda = self.torch.cuda
+        return cuda.ExternalStream(raw, device=self.device) if raw else cuda.default_stream(self.device)
+
+    def _used_on(self, raw):
+        self.arena.record_stream(self._stream(raw))
+        self._streams.add(raw)
+
+    def _call(self, stream):
+        """The number of a call's stream, which the arena's memory waits for when it is given up."""
+        raw = self._s(stream)
+        if raw not in self._streams:
+            self._used_on(raw)
+        return raw
+
+    def _on(self, raw, make):
+        """make(), its memory that of the stream of this number."""
+        if self.device.type != "cuda" or raw == self._s(None):
+            return make()
+        with self.torch.cuda.stream(self._stream(raw)):
+            return make()
 
     def close(self):
         if getattr(self, "handle", None):
@@ -380,7 +404,7 @@ class DmcCache:
             pass
 
     def reset(self, stream=None):
-        _check(dmc_cache_reset(self.handle, self._s(stream)), "dmc_cache_reset")
+        _check(dmc_cache_reset(self.handle, self._call(stream)), "dmc_cache_reset")
 
     def prefill(self, layer, q0, k, v, cu_seqlens, max_seqlen, first_seq=0, stream=None):
         """q0: [total, Hq] (or any tensor whose element (t, j, 0) sits at
@@ -390,7 +414,7 @@ class DmcCache:
         _check(dmc_prefill_compress(self.handle, layer, first_seq, n, q0.data_ptr(),
                                     q0.stride(0), q0.stride(1), k.data_ptr(), v.data_ptr(),
                                     cu_seqlens.data_ptr(), total, int(max_seqlen),
-                                    self._s(stream)), "dmc_prefill_compress")
+                                    self._call(stream)), "dmc_prefill_compress")
 
     def prefill_attention(self, layer, q, k, v, cu_seqlens, max_seqlen, out, first_seq=0,
                           stream=None):
@@ -398,17 +422,17 @@ class DmcCache:
         n = cu_seqlens.numel() - 1
         _check(dmc_prefill_attention(self.handle, layer, first_seq, n, q.data_ptr(), k.data_ptr(),
                                      v.data_ptr(), cu_seqlens.data_ptr(), k.shape[0],
-                                     int(max_seqlen), out.data_ptr(), self._s(stream)),
+                                     int(max_seqlen), out.data_ptr(), self._call(stream)),
                "dmc_prefill_attention")
 
     def decode(self, layer, q, k, v, out, stream=None):
         _check(dmc_decode_step(self.handle, layer, q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                               out.data_ptr(), self._s(stream)), "dmc_decode_step")
+                               out.data_ptr(), self._call(stream)), "dmc_decode_step")
 
     def decode_layers(self, first_layer, q, k, v, out, stream=None):
         """q, out: [n, B, Hq, D]; k, v: [n, B, Hkv, D] for layers first_layer .. + n - 1."""
         _check(dmc_decode_step_layers(self.handle, first_layer, q.shape[0], q.data_ptr(),
-                                      k.data_ptr(), v.data_ptr(), out.data_ptr(), self._s(stream)),
+                                      k.data_ptr(), v.data_ptr(), out.data_ptr(), self._call(stream)),
                "dmc_decode_step_layers")
 
     # ---- calls that check their tensors (what does not fit is refused with ValueError). The check is one expression,
@@ -423,23 +447,9 @@ class DmcCache:
         what = f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
         raise ValueError(f"{name} must be contiguous {dtype} {tuple(shape)} on {self.device}, got {what}")
 
-    def _stream(self, raw):
-        # (an ExternalStream of the number 0 would be another one)
-        cuda = self.torch.cuda
-        return cuda.ExternalStream(raw, device=self.device) if raw else cuda.default_stream(self.device)
-
-    def _used_on(self, raw):
-        self.arena.record_stream(self._stream(raw))
-        self._streams.add(raw)
-
     def _new(self, like, stream):
         """A tensor as `like`, of memory that belongs to the call's stream."""
-        torch = self.torch
-        raw = self._s(stream)
-        if raw == self._s(None):
-            return torch.empty_like(like)
-        with torch.cuda.stream(self._stream(raw)):
-            return torch.empty_like(like)
+        return self._on(self._s(stream), lambda: self.torch.empty_like(like))
 
     def _append_is_wrong(self, q, k, v, positions, rotary, cu_seqlens, n, q_out):
         c, t = self.cfg, self.torch
@@ -536,17 +546,14 @@ class DmcCache:
         if not isinstance(parents, self.torch.Tensor) or parents.dim() < 1:
             raise ValueError("parents must be int32, one for each sequence")
         p = self._is("parents", parents, parents.shape, self.torch.int32)
-        raw = self._s(stream)
-        if raw not in self._streams:
-            self._used_on(raw)
-        st = self.lib.dmc_cache_reorder(self.handle, first_seq, parents.numel(), p, raw)
+        st = self.lib.dmc_cache_reorder(self.handle, first_seq, parents.numel(), p, self._call(stream))
         if st:
             _check(st, "dmc_cache_reorder")
 
     def lengths(self, layer, stream=None):
         t = self.torch
         out = t.empty((self.cfg.batch, self.cfg.num_kv_heads), dtype=t.int32, device=self.device)
-        _check(dmc_cache_lengths(self.handle, layer, out.data_ptr(), self._s(stream)),
+        _check(dmc_cache_lengths(self.handle, layer, out.data_ptr(), self._call(stream)),
                "dmc_cache_lengths")
         return out
 
@@ -566,7 +573,7 @@ class DmcCache:
         new = self._empty_like
         k, v, z, ln = new(rows), new(rows), new(sums), new(counts)  # padded: every row is written
         st = self.lib.dmc_cache_export_heads_padded(self.handle, layer, n, ids.data_ptr(), cap, k.data_ptr(), v.data_ptr(),
-                                                    z.data_ptr(), ln.data_ptr(), self._s(stream))
+                                                    z.data_ptr(), ln.data_ptr(), self._call(stream))
         if st:
             _check(st, "dmc_cache_export_heads")
         return k, v, z, ln
