@@ -551,13 +551,21 @@ class DmcCache:
             _check(st, "dmc_cache_reorder")
 
     def lengths(self, layer, stream=None):
-        t = self.torch
-        out = t.empty((self.cfg.batch, self.cfg.num_kv_heads), dtype=t.int32, device=self.device)
-        _check(dmc_cache_lengths(self.handle, layer, out.data_ptr(), self._call(stream)),
-               "dmc_cache_lengths")
+        t, raw = self.torch, self._call(stream)
+        out = self._on(raw, lambda: t.empty((self.cfg.batch, self.cfg.num_kv_heads), dtype=t.int32, device=self.device))
+        _check(dmc_cache_lengths(self.handle, layer, out.data_ptr(), raw), "dmc_cache_lengths")
         return out
 
     def export_heads(self, layer, head_ids, cap, stream=None):
+        """(k, v, z, len) of the heads head_ids (int32 on the cache's device, or a list), padded to cap slots with zeros:
+        new tensors of the call's stream."""
+        raw = self._call(stream)
+        if stream is not None and self.device.type == "cuda" and raw != self._s(None):
+            with self.torch.cuda.stream(self._stream(raw)):
+                return self._export_heads(layer, head_ids, cap, raw)
+        return self._export_heads(layer, head_ids, cap, raw)
+
+    def _export_heads(self, layer, head_ids, cap, raw):
         t = self.torch
         ids = head_ids
         if not (isinstance(ids, t.Tensor) and ids.dtype is t.int32 and ids.get_device() == self.index and ids.is_contiguous()):
@@ -573,7 +581,7 @@ class DmcCache:
         new = self._empty_like
         k, v, z, ln = new(rows), new(rows), new(sums), new(counts)  # padded: every row is written
         st = self.lib.dmc_cache_export_heads_padded(self.handle, layer, n, ids.data_ptr(), cap, k.data_ptr(), v.data_ptr(),
-                                                    z.data_ptr(), ln.data_ptr(), self._call(stream))
+                                                    z.data_ptr(), ln.data_ptr(), raw)
         if st:
             _check(st, "dmc_cache_export_heads")
         return k, v, z, ln

@@ -83,6 +83,28 @@ def test_the_arena_is_memory_of_the_constructors_stream(cuda_dev):
     torch.cuda.synchronize()
 
 
+def test_results_are_memory_of_the_calls_stream(cuda_dev):
+    """A place that the current stream has just freed, and may still write, is not given to a call on another stream."""
+    side, cache = torch.cuda.Stream(), made()
+    q, k, v = (t.cuda() for t in tokens(torch.Generator().manual_seed(3), 2, 2, 2, 128, BF16, 1.0))
+    cache.append(0, q, k, v)
+    ids = torch.arange(4, dtype=torch.int32).cuda()
+    torch.cuda.synchronize()
+    for name in (side, side.cuda_stream):
+        for call in (lambda **k: (cache.lengths(0, **k),), lambda **k: cache.export_heads(0, ids, 4, **k),
+                     lambda **k: cache.export_heads(0, [0, 1, 2, 3], 4, **k)):
+            want = [t.clone() for t in call()]
+            torch.cuda.synchronize()
+            freed = [torch.empty_like(t) for _ in range(4) for t in want]
+            places = {t.data_ptr() for t in freed}
+            del freed  # the current stream's to use again
+            got = call(stream=name)
+            side.synchronize()
+            assert not places & {t.data_ptr() for t in got}
+            assert all(stream_of(t) == [side.cuda_stream] for t in got)
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_a_cache_used_in_a_captured_graph_alone(cuda_dev):
     """The capture's stream is noted like any other; the graph replays, and the cache can be dropped after it."""
     q, k, v = (t.cuda() for t in tokens(torch.Generator().manual_seed(2), 2, 2, 2, 64, F32, 1.0))
