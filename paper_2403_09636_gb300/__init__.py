@@ -551,10 +551,14 @@ class DmcCache:
             _check(st, "dmc_cache_reorder")
 
     def lengths(self, layer, stream=None):
-        t, raw = self.torch, self._call(stream)
-        out = self._on(raw, lambda: t.empty((self.cfg.batch, self.cfg.num_kv_heads), dtype=t.int32, device=self.device))
+        raw = self._call(stream)
+        out = self._counts() if stream is None else self._on(raw, self._counts)
         _check(dmc_cache_lengths(self.handle, layer, out.data_ptr(), raw), "dmc_cache_lengths")
         return out
+
+    def _counts(self):
+        t = self.torch
+        return t.empty((self.cfg.batch, self.cfg.num_kv_heads), dtype=t.int32, device=self.device)
 
     def export_heads(self, layer, head_ids, cap, stream=None):
         """(k, v, z, len) of the heads head_ids (int32 on the cache's device, or a list), padded to cap slots with zeros:
