@@ -259,7 +259,8 @@ dmc_status dmc_rotate(int32_t dtype, int32_t head_dim, int32_t num_tokens, const
  *          others follow one by one. (The cache cannot tell: it holds slots, not tokens.)
  *   turns_dev, interleaved: the rotation, as above. turns_dev NULL: none; positions_dev
  *          and q_out_dev are then not used and must be NULL;
- *   q_out_dev (written): as q_dev, which it may be. Rows of no sequence are left as they are. */
+ *   q_out_dev (written): as q_dev, which it may be. Rows of no sequence (before the first, behind the
+ *          last) are left as they are. */
 dmc_status dmc_cache_append(dmc_cache_t cache, int32_t layer, int32_t first_seq, int32_t num_seqs, const void* q_dev,
                             const void* k_dev, const void* v_dev, const int32_t* cu_seqlens_dev, int32_t total_tokens,
                             int32_t max_seqlen, const int32_t* positions_dev, const uint64_t* turns_dev,
@@ -475,11 +476,14 @@ dmc_status dmc_retrofit_status(dmc_retrofit_t h, cudaStream_t stream, uint32_t* 
  * Beam search: selection. For every group of beams (one text) the `keep` best of
  * beams x vocab continuations:
  *   score(b, w) = scores[b] + logits[b, w] - log sum_w' exp(logits[b, w'])
- * in descending order (a beam's own in that of its logits); ties go to the lower b * vocab + w. A finished beam has one
- * continuation, the end word, at its own score. A beam whose score, or whose log-sum, is not
+ * in descending order (a beam's own in that of its logits); ties go to the lower b * vocab + w (zeros of both signs
+ * are equal). A finished beam has one continuation, the end word, at its own score. A beam whose score, or whose log-sum, is not
  * a finite number offers its words at -infinity (so a search may begin with scores 0,
- * -inf, -inf, ...); single logits may be -infinity (masked words). Scores are compared
- * in 48 bits. The parents are what dmc_cache_reorder takes when keep = beams.
+ * -inf, -inf, ...); single logits may be -infinity (masked words). Scores are added up and
+ * compared in 48 bits, so that within a beam nothing is lost beside its logits; a row's log-sum,
+ * a sum of fp32 exponentials, is off by up to some 2^-20, and continuations of different
+ * beams whose scores are closer than that may come in either order (those of beams that are alike
+ * come in the order of ties). The parents are what dmc_cache_reorder takes when keep = beams.
  * The handle lays its scratch out in a caller's arena, as a cache does; calls on one
  * handle must be ordered on the GPU, allocate nothing and can be captured.
  * ------------------------------------------------------------------------ */

@@ -477,7 +477,8 @@ class DmcCache:
         """New tokens join the cache, rotated on the way; returns the rotated queries (None without a rotation).
         q: [T, Hq, D]; k, v: [T, Hkv, D], of one token for each of T sequences from first_seq on, or packed
         by cu_seqlens (int32 [sequences + 1]); positions: int32, one for each sequence's first token; rotary: a
-        `rotary.Rotary`; q_out may be q."""
+        `rotary.Rotary`; q_out may be q. Rows of no sequence (cu_seqlens that end before T) are left as they are: in a
+        tensor that this call makes, as its memory came."""
         i32, dt, index = self._int32, self.dtype, self.index
         try:
             T, H, D = rows = k.shape

@@ -7,8 +7,9 @@
 // turned round, so that equal logits go to the lower word). Words are held to a bar that few more than `keep` of the
 // words so far reach: at first the keep-th largest of the lanes' maxima over the block's first 8192 words, then also the
 // least of the warps' ceil(keep / 8)-th best. The group's last block (a counter, no waiting) joins the pieces: sums and
-// lists of a row by a warp, then the rows' lists by score, in 48 bits; where sorted lists are joined, each entry looks up
-// how many are before it.
+// lists of a row by a warp, then the rows' lists by score, in 48 bits (the log-sum in them is that of fp32 exponentials, off
+// by up to some 2^-20, but the same for all of a row's words and for rows that are alike); where sorted lists are joined,
+// each entry looks up how many are before it.
 //
 // Bound by HBM (each logit is read once) where there are many, by the chain load - list - join otherwise.
 #include <math.h>
@@ -28,8 +29,9 @@ constexpr int kBeamThreads = kBeamWarps * 32;
 constexpr int kBeamMost = 32;             // beams of a group, and continuations kept: a lane each
 constexpr int kWords = 32;                // words of a lane at a time
 constexpr int kBlock = 32 * kWords;       // words of a warp at a time
-// Pieces that rows are cut into, in all: two blocks per SM, as many as fit. 256 rows of 130,003 fp32 words take 32.7 us
-// with one piece each, 38.6 with two, 50.6 with four.
+// Pieces that rows are cut into, in all: two blocks per SM, as many as fit. 256 rows of 130,003 words, 16 kept, take 32.5 us
+// in fp32 and 30 in bf16 with one piece each, 38.7 and 38 with two, 50.5 and 49 with four (one kept: 28 and 23, 30 and 26.5,
+// 35 and 32). bf16 has half the bytes but the same instructions for a word, which bound it.
 constexpr int kBeamBlocks = 304;
 constexpr unsigned kFull = 0xffffffffu;
 

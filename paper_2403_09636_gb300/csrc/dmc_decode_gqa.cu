@@ -885,10 +885,10 @@ cudaError_t gqa_setup(const Layout& L, DecodePlan* plan) {
 
 // Heads are merged by a launch of their own where each may be cut into four parts or more, and there are at most 64 of
 // them and 256 queries (what a cache can hold is known on the host, its lengths are not). us per call with the last
-// warp's merge / the launch, of 40, 300, 1000 and 4000 slots: 8 heads of 8 queries 9.4 / 9.5, 14.7 / 9.9, 16.7 / 12.3,
-// 26.5 / 17.0; 32 of 2 9.3 / 9.8, 16.9 / 12.1, 16.2 / 13.7, 26.2 / 20.6; 64 of 2 9.4 / 11.8, 17.6 / 13.5, 16.6 / 16.7,
-// 36.0 / 33.6; 64 of 8 9.8 / 13.3, 15.5 / 15.0, 18.0 / 18.6, 36.3 / 35.5; 96 of 4 9.7 / 13.0, 17.7 / 15.9, 18.6 / 19.9,
-// 44.2 / 44.5.
+// warp's merge / the launch, caches of 300, 1000 and 4000 slots (with 40 the rule takes the last warp: 9.1-9.4 for all, 2 us
+// more with the launch for 64 heads): 8 heads of 8 queries 14.4 / 10.2, 16.4 / 10.4, 26.5 / 17.0; 32 of 2 17.9 / 10.2,
+// 16.1 / 13.7, 30.4 / 23.2; 64 of 2 17.9 / 13.6, 19.7 / 19.3, 35.9 / 33.4; 64 of 4 18.0 / 13.8, 18.6 / 19.8, 35.1 / 34.1;
+// beyond the rule 64 of 8 18.2 / 14.7, 19.4 / 20.4, 36.2 / 35.4.
 constexpr int kJoinHeads = 64, kJoinQueries = 256, kJoinParts = 4;
 
 template <int D>

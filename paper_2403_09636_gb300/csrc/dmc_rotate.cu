@@ -164,9 +164,12 @@ static cudaError_t launch_rotate(RotateArgs& a, int esize, int D, cudaStream_t s
   // A block takes about as many rows as its threads have in flight: several tokens of few heads, or one token's heads
   // in parts (the turns of a token are then computed for each part). 8192 tokens of 32 + 32 heads of 128 in bf16 take
   // 41.4 us so (6.5 TB/s); 456 blocks, as many as run at once, of 18 tokens and with the next rows on their way while some
-  // are worked, 45.9.
+  // are worked, 45.9. Few rows in all go one to a thread's place instead, for latency: us of 512, 2048, 6144, 12,288 and
+  // 32,768 rows so / with several in flight: 32 + 32 heads of 128 in bf16 2.3 / 3.0, 2.5 / 3.3, 2.8 / 3.4, 3.1 / 3.4,
+  // 6.8 / 5.5; 64 + 8 2.5 / 2.8, 2.6 / 3.0, 2.8 / 3.0, 3.9 / 3.4, 7.2 / 5.2; 8 + 8 in fp32 2.5 / 3.2, 2.6 / 3.3, 3.0 / 3.3,
+  // 4.9 / 4.6, 10.2 / 8.6.
   const int at_once = kRotateThreads / (D * esize / 32), all = a.heads[0] + a.heads[1];
-  const bool few = (long long)a.tokens * all < 8192;  // a handful of rows in all: a row for a thread's place
+  const bool few = (long long)a.tokens * all < 8192;
   a.per = few ? 1 : max(1, min(kRotateTokens, at_once * kRowsInFlight / all));
   const int blocks = ceil_div(a.tokens, a.per);
   const int parts = max(1, ceil_div(all, few ? at_once : at_once * kRowsInFlight));
